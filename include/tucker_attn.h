@@ -184,6 +184,77 @@ TA_API int tucker_attn_decode_static(const tucker_attn_desc* desc, const void* x
                               void* y, void* cuda_stream);
 
 /*
+ * Paged latent cache (Sec. 3.1's cache, kept in pages so that sequences of any lengths share one pool).
+ *
+ * The pools hold n_pages pages of page_size consecutive slots: K [n_pages, page_size, r3], V [n_pages, page_size, t3].
+ * Slot i of sequence b is row i % page_size of page block_table[b * max_pages + i / page_size].  Pages need not be in
+ * any order.  What lies in slots past a sequence's length, in table entries past its last page, and in pages that no
+ * entry names is never used, whatever it is.  V == K is the shared key / value projection: one pool of latent rows,
+ * accepted when U3 == Ut3 (same pointer) and r3 == t3; with rope it holds UN-rotated rows, as in tucker_attn_decode.
+ *
+ * block_table, cache_len, tok_start and prefix_table are DEVICE memory and are read when the call's kernels run.  A
+ * table entry that is needed and lies outside [0, n_pages) sets TA_DEVERR_BAD_PAGE: its rows count as zeros, nothing is
+ * written through it.  A cache_len outside [0, max_pages * page_size) sets TA_DEVERR_BAD_CACHE_LEN (decode clamps it as
+ * tucker_attn_decode does; append drops the tokens concerned).  Two sequences may read the same page (a prefix that
+ * both hold); a page that a call WRITES belongs to one sequence only, else it is not defined whose row it holds.
+ *
+ * Limits: B <= 65535, B n_H <= 2^24, max_pages * page_size + (pos0 or prefix_len) < 2^31.  Any page_size >= 1.
+ */
+typedef struct {
+  void* K;                    /* [n_pages, page_size, r3]  device */
+  void* V;                    /* [n_pages, page_size, t3]  device; == K: one shared latent pool */
+  const int32_t* block_table; /* [B, max_pages]  device */
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t max_pages;
+} tucker_paged_cache;
+
+/*
+ * Append a ragged batch of tokens to a paged cache: latent keys X U3, rotated by R(position, r3) when desc->rope, and
+ * latent values X Ut3 (Sec. 3.1, Definition 2), written to the slots that follow each sequence's cached ones.
+ *   X          [T, d_model]  token rows of all sequences, one after another
+ *   cache_len  [B] tokens that each sequence has already; the caller adds what it appended afterwards
+ *   tok_start  [B + 1] ascending: sequence b brings rows tok_start[b] .. tok_start[b + 1] - 1 (none is allowed); rows of X
+ *              outside [tok_start[0], tok_start[B]) are padding and are not used
+ * Row i of sequence b goes to slot cache_len[b] + i, at absolute position pos0 + cache_len[b] + i (pos0 >= 0: what stands in
+ * front of slot 0, such as a shared prefix).  Used of desc: B, d_model, r3, t3, rope, rope_base, pos0, dtype, flags (the other
+ * fields must be valid).  T = 0 is allowed.  Nothing else in the pools is touched.  No workspace.
+ */
+TA_API int tucker_cache_append_paged(const tucker_attn_desc* desc, const void* X, const void* U3, const void* Ut3,
+                              const tucker_paged_cache* cache, const int32_t* cache_len, const int32_t* tok_start, int32_t T,
+                              void* cuda_stream);
+
+/*
+ * One cached decode step over a paged cache: tucker_attn_decode with its caches in pages.  The new token of sequence b
+ * attends to slots 0 .. cache_len[b] - 1 and to itself, at position cache_len[b]; with append its key / value row is
+ * written to slot cache_len[b], whose page must then be in the table.  Arguments otherwise as tucker_attn_decode.
+ */
+TA_API size_t tucker_attn_decode_paged_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache* cache);
+TA_API int tucker_attn_decode_paged(const tucker_attn_desc* desc, const void* x,
+                             const void* C, const void* U1, const void* U2, const void* U3,
+                             const void* Ct, const void* Ut1, const void* Ut2, const void* Ut3,
+                             const tucker_paged_cache* cache, const int32_t* cache_len, int32_t append,
+                             void* y, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * The same step for a batch whose sequences all start with the same prefix_len tokens, stored once: slot i of the prefix
+ * is row i % page_size of page prefix_table[i / page_size] of the same pools (filled, for instance, by an append with
+ * B = 1 and prefix_table as its block table).  The new token of sequence b attends to the prefix, to its own slots
+ * 0 .. cache_len[b] - 1 and to itself; its own slot i has position prefix_len + i.  The prefix is attended to once for
+ * all B n_H query rows and joined with the own part by the softmax's maxima and sums: the result is that of the paged
+ * step on sequences that hold the prefix themselves.  prefix_len = 0 (prefix_table may be NULL) is that step.
+ * prefix_len is read on the host; the rest as for tucker_attn_decode_paged.
+ */
+TA_API size_t tucker_attn_decode_prefix_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache* cache,
+                                                 int32_t prefix_len);
+TA_API int tucker_attn_decode_prefix(const tucker_attn_desc* desc, const void* x,
+                              const void* C, const void* U1, const void* U2, const void* U3,
+                              const void* Ct, const void* Ut1, const void* Ut2, const void* Ut3,
+                              const tucker_paged_cache* cache, const int32_t* cache_len,
+                              const int32_t* prefix_table, int32_t prefix_len, int32_t append,
+                              void* y, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Weight packers: the paper's special cases as Tucker attention (Sec. 2.2; Lemma 1 and
  * Theorems 1-3 and their proofs).  They write the two cores and six factors that
  * tucker_attn_fwd / tucker_attn_decode take, so that MHA, GQA / MQA and MLA weights run
@@ -269,6 +340,7 @@ TA_API const char* tucker_attn_status_string(int status);
 enum {
   TA_DEVERR_WAIT_TIMEOUT = 1,   /* an mbarrier / flag wait hit its iteration limit */
   TA_DEVERR_BAD_CACHE_LEN = 2,  /* cache_len[b] outside [0, Lmax) */
+  TA_DEVERR_BAD_PAGE = 8,       /* a needed entry of a block_table / prefix_table outside [0, n_pages) */
   TA_DEVERR_BAD_INDEX = 4       /* a bounds check failed (only in the -DTA_BOUNDS_CHECK build, see tucker_attn_bounds_checked) */
 };
 TA_API int tucker_attn_last_device_error(void* cuda_stream);
@@ -278,7 +350,7 @@ TA_API int tucker_attn_last_device_error(void* cuda_stream);
  * far went through (no counterpart in the paper).  Synchronises `cuda_stream`, reads and clears the device
  * error word and returns TA_OK when it was clean, else TA_ERR_DEVICE_TIMEOUT (a bounded wait gave up: results
  * of the calls since the last read are invalid), TA_ERR_INVALID_ARG (a cache_len entry was out of range and
- * was clamped) or TA_ERR_CUDA (the read itself failed, or a bounds check of the checking build fired), in
+ * was clamped, or a page table entry was) or TA_ERR_CUDA (the read itself failed, or a bounds check of the checking build fired), in
  * that order of precedence.
  */
 TA_API int tucker_attn_sync_status(void* cuda_stream);

@@ -21,7 +21,7 @@ TA_OK = 0
 TA_DTYPE_F32, TA_DTYPE_BF16 = 0, 1
 TA_FLAG_FORCE_GENERIC = 1
 TA_FLAG_FMA_ATTENTION, TA_FLAG_SEPARATE_QUERIES, TA_FLAG_SEPARATE_OUTPUT_GEMMS = 0x200, 0x400, 0x800
-TA_DEVERR_WAIT_TIMEOUT, TA_DEVERR_BAD_CACHE_LEN, TA_DEVERR_BAD_INDEX = 1, 2, 4
+TA_DEVERR_WAIT_TIMEOUT, TA_DEVERR_BAD_CACHE_LEN, TA_DEVERR_BAD_INDEX, TA_DEVERR_BAD_PAGE = 1, 2, 4, 8
 
 EXPORTS = (
     "tucker_attn_fwd_workspace_bytes", "tucker_attn_decode_workspace_bytes", "tucker_attn_fwd",
@@ -29,6 +29,8 @@ EXPORTS = (
     "tucker_attn_last_path", "tucker_attn_last_launch_count", "tucker_attn_set_profile_events",
     "tucker_attn_decode_static", "tucker_attn_selftest_wait_timeout", "tucker_attn_sync_status",
     "tucker_attn_bounds_checked",
+    "tucker_cache_append_paged", "tucker_attn_decode_paged", "tucker_attn_decode_paged_workspace_bytes",
+    "tucker_attn_decode_prefix", "tucker_attn_decode_prefix_workspace_bytes",
     "tucker_pack_gqa", "tucker_pack_mha", "tucker_pack_mla",
     "tucker_hosvd_workspace_bytes", "tucker_hosvd_init", "tucker_mha_weight_tensors", "tucker_probe_plane_mix", "tucker_probe_mma_rate",
 )
@@ -44,6 +46,14 @@ class TuckerAttnDesc(ctypes.Structure):
         ("causal", ctypes.c_int32), ("rope", ctypes.c_int32), ("rope_base", ctypes.c_float),
         ("pos0", ctypes.c_int32), ("scale", ctypes.c_float), ("dtype", ctypes.c_int32),
         ("flags", ctypes.c_int32),
+    ]
+
+
+class TuckerPagedCache(ctypes.Structure):
+    """Mirror of `tucker_paged_cache`."""
+    _fields_ = [
+        ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+        ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
     ]
 
 
@@ -78,6 +88,17 @@ def load_library() -> ctypes.CDLL:
     lib.tucker_attn_decode.argtypes = [dp] + [vp] * 11 + [i32, vp, i32, vp, vp, sz, vp]
     lib.tucker_attn_decode_static.restype = ctypes.c_int
     lib.tucker_attn_decode_static.argtypes = [dp] + [vp] * 11 + [i32, vp, i32, vp, vp]
+    pp = ctypes.POINTER(TuckerPagedCache)
+    lib.tucker_cache_append_paged.restype = ctypes.c_int
+    lib.tucker_cache_append_paged.argtypes = [dp] + [vp] * 3 + [pp, vp, vp, i32, vp]
+    lib.tucker_attn_decode_paged_workspace_bytes.restype = sz
+    lib.tucker_attn_decode_paged_workspace_bytes.argtypes = [dp, pp]
+    lib.tucker_attn_decode_paged.restype = ctypes.c_int
+    lib.tucker_attn_decode_paged.argtypes = [dp] + [vp] * 9 + [pp, vp, i32, vp, vp, sz, vp]
+    lib.tucker_attn_decode_prefix_workspace_bytes.restype = sz
+    lib.tucker_attn_decode_prefix_workspace_bytes.argtypes = [dp, pp, i32]
+    lib.tucker_attn_decode_prefix.restype = ctypes.c_int
+    lib.tucker_attn_decode_prefix.argtypes = [dp] + [vp] * 9 + [pp, vp, vp, i32, i32, vp, vp, sz, vp]
     lib.tucker_attn_status_string.restype = ctypes.c_char_p
     lib.tucker_attn_status_string.argtypes = [ctypes.c_int]
     lib.tucker_attn_last_device_error.restype = ctypes.c_int
@@ -293,6 +314,102 @@ def tucker_attn_decode_static(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kcache, Vcach
     if rc != TA_OK:
         raise TuckerAttnError(rc, "tucker_attn_decode_static")
     return out
+
+
+def _paged_cache(Kpages, Vpages, block_table, B, r3, t3, dtype, device):
+    """Checks the pools and the block table of a paged cache; returns its `tucker_paged_cache`."""
+    torch = _torch()
+    if Kpages.dim() != 3 or block_table.dim() != 2:
+        raise ValueError("Kpages must be [n_pages, page_size, r3] and block_table [B, max_pages]")
+    n_pages, page_size, _ = Kpages.shape
+    _check(Kpages, "Kpages", (n_pages, page_size, r3), dtype, device)
+    _check(Vpages, "Vpages", (n_pages, page_size, t3), dtype, device)
+    _check(block_table, "block_table", (B, block_table.shape[1]), torch.int32, device)
+    return TuckerPagedCache(Kpages.data_ptr(), Vpages.data_ptr(), block_table.data_ptr(), n_pages, page_size,
+                            block_table.shape[1])
+
+
+def tucker_cache_append_paged(X, U3, Ut3, Kpages, Vpages, block_table, cache_len, tok_start, *, rope: bool,
+                              rope_base: float = 10000.0, pos0: int = 0, flags: int = 0) -> None:
+    """Appends a ragged batch of tokens to a paged cache (same name and argument meaning as the C entry point).
+    X [T, d]: rows tok_start[b] .. tok_start[b + 1] - 1 are the new tokens of sequence b; Kpages [n_pages, page_size, r3],
+    Vpages [n_pages, page_size, t3] (the same tensor: one shared latent pool, with U3 and Ut3 the same tensor);
+    block_table [B, max_pages], cache_len [B] and tok_start [B + 1] int32 on the device."""
+    torch = _torch()
+    lib = load_library()
+    if X.dim() != 2 or cache_len.dim() != 1:
+        raise ValueError("X must be [T, d_model] and cache_len [B]")
+    T, d = X.shape
+    B = cache_len.shape[0]
+    dev, dt = X.device, X.dtype
+    r3, t3 = U3.shape[-1], Ut3.shape[-1]
+    _check(X, "X", (T, d), dt, dev)
+    _check(U3, "U3", (d, r3), dt, dev)
+    _check(Ut3, "Ut3", (d, t3), dt, dev)
+    _check(cache_len, "cache_len", (B,), torch.int32, dev)
+    _check(tok_start, "tok_start", (B + 1,), torch.int32, dev)
+    cache = _paged_cache(Kpages, Vpages, block_table, B, r3, t3, dt, dev)
+    desc = make_desc(B=B, N=1, d_model=d, n_H=1, r=(1, 1, r3), t=(1, 1, t3), causal=True, rope=rope, rope_base=rope_base,
+                     pos0=pos0, dtype=_dtype_code(X), flags=flags)
+    with torch.cuda.device(dev):
+        rc = lib.tucker_cache_append_paged(ctypes.byref(desc), X.data_ptr(), U3.data_ptr(), Ut3.data_ptr(), ctypes.byref(cache),
+                                           cache_len.data_ptr(), tok_start.data_ptr(), int(T), _stream_ptr(dev))
+    if rc != TA_OK:
+        raise TuckerAttnError(rc, "tucker_cache_append_paged")
+
+
+def tucker_attn_decode_prefix(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kpages, Vpages, block_table, cache_len, prefix_table,
+                              prefix_len: int, *, n_H: int, rope: bool, rope_base: float = 10000.0, scale: float = 0.0,
+                              append: bool = True, out=None, workspace=None, flags: int = 0):
+    """One decode step for a batch whose sequences share a stored prefix (same name and argument meaning as the C entry
+    point).  x [B, d]; pools, block_table and cache_len as for tucker_cache_append_paged (the sequences' own part);
+    prefix_table int32 [>= ceil(prefix_len / page_size)] on the device (None when prefix_len is 0).  Returns y [B, d]."""
+    torch = _torch()
+    lib = load_library()
+    if x.dim() != 2:
+        raise ValueError("x must be [B, d_model]")
+    B, d = x.shape
+    dev, dt = x.device, x.dtype
+    _check(x, "x", (B, d), dt, dev)
+    r, t = _weights_check((C, U1, U2, U3, Ct, Ut1, Ut2, Ut3), d, n_H, dt, dev)
+    _check(cache_len, "cache_len", (B,), torch.int32, dev)
+    cache = _paged_cache(Kpages, Vpages, block_table, B, r[2], t[2], dt, dev)
+    prefix_len = int(prefix_len)
+    if prefix_len < 0:
+        raise ValueError("prefix_len must not be negative")
+    if prefix_len > 0:
+        if prefix_table is None or prefix_table.dim() != 1 or prefix_table.shape[0] * cache.page_size < prefix_len:
+            raise ValueError("prefix_table must hold the ceil(prefix_len / page_size) pages of the prefix")
+        _check(prefix_table, "prefix_table", tuple(prefix_table.shape), torch.int32, dev)
+    desc = make_desc(B=B, N=1, d_model=d, n_H=n_H, r=r, t=t, causal=True, rope=rope, rope_base=rope_base, pos0=0, scale=scale,
+                     dtype=_dtype_code(x), flags=flags)
+    if out is None:
+        out = torch.empty_like(x)
+    _check(out, "out", (B, d), dt, dev)
+    if workspace is None:
+        workspace = alloc_workspace(lib.tucker_attn_decode_prefix_workspace_bytes(ctypes.byref(desc), ctypes.byref(cache),
+                                                                                  prefix_len), dev)
+    _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
+    with torch.cuda.device(dev):
+        rc = lib.tucker_attn_decode_prefix(ctypes.byref(desc), x.data_ptr(), C.data_ptr(), U1.data_ptr(), U2.data_ptr(),
+                                           U3.data_ptr(), Ct.data_ptr(), Ut1.data_ptr(), Ut2.data_ptr(), Ut3.data_ptr(),
+                                           ctypes.byref(cache), cache_len.data_ptr(),
+                                           prefix_table.data_ptr() if prefix_len > 0 else None, prefix_len,
+                                           int(bool(append)), out.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                           _stream_ptr(dev))
+    if rc != TA_OK:
+        raise TuckerAttnError(rc, "tucker_attn_decode_prefix")
+    return out
+
+
+def tucker_attn_decode_paged(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kpages, Vpages, block_table, cache_len, *, n_H: int,
+                             rope: bool, rope_base: float = 10000.0, scale: float = 0.0, append: bool = True, out=None,
+                             workspace=None, flags: int = 0):
+    """One cached decode step over a paged cache (same name and argument meaning as the C entry point): the step of
+    tucker_attn_decode_prefix without a prefix.  Returns y [B, d]."""
+    return tucker_attn_decode_prefix(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kpages, Vpages, block_table, cache_len, None, 0,
+                                     n_H=n_H, rope=rope, rope_base=rope_base, scale=scale, append=append, out=out,
+                                     workspace=workspace, flags=flags)
 
 
 _PACK_KEYS = ("C", "U1", "U2", "U3", "Ct", "Ut1", "Ut2", "Ut3")

@@ -59,6 +59,18 @@ static bool shared_kv_weights(const tucker_attn_desc& d, const void* U3, const v
   return U3 == Ut3 && d.r3 == d.t3;
 }
 
+// A paged cache's host-side description.  Slots are counted in 32 bits: max_pages * page_size + `before` (the tokens in
+// front of slot 0) must stay below 2^31.
+static bool paged_ok(const tucker_paged_cache* c, int64_t before) {
+  if (!c || !c->K || !c->V || !c->block_table) return false;
+  if (c->n_pages <= 0 || c->page_size <= 0 || c->max_pages <= 0 || before < 0) return false;
+  return (int64_t)c->max_pages * c->page_size + before < (int64_t)1 << 31;
+}
+static int64_t paged_slots(const tucker_paged_cache& c) { return (int64_t)c.max_pages * c.page_size; }
+
+// Grid limits of the paged kernels.
+static bool paged_batch_ok(const tucker_attn_desc& d) { return d.B <= 65535 && (int64_t)d.B * d.n_H <= (1 << 24); }
+
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 }  // namespace ta
@@ -95,7 +107,7 @@ int tucker_attn_fwd(const tucker_attn_desc* desc, const void* X, const void* C, 
   const size_t need = fast ? fast_fwd_workspace(*desc) : generic_fwd_workspace(*desc);
   if (need == 0) return TA_ERR_UNSUPPORTED_SHAPE;
   if (workspace_bytes < need) return TA_ERR_WORKSPACE_TOO_SMALL;
-  Problem p;
+  Problem p = {};
   p.d = *desc;
   p.scale = resolve_scale(*desc);
   p.X = X; p.C = C; p.U1 = U1; p.U2 = U2; p.U3 = U3; p.Ct = Ct; p.Ut1 = Ut1; p.Ut2 = Ut2; p.Ut3 = Ut3;
@@ -132,7 +144,7 @@ int tucker_attn_decode(const tucker_attn_desc* desc, const void* x, const void* 
   const size_t need = fast ? fast_decode_workspace(*desc, Lmax) : generic_decode_workspace(*desc, Lmax);
   if (need == 0) return TA_ERR_UNSUPPORTED_SHAPE;
   if (workspace_bytes < need) return TA_ERR_WORKSPACE_TOO_SMALL;
-  Problem p;
+  Problem p = {};
   p.d = *desc;
   p.scale = resolve_scale(*desc);
   p.X = x; p.C = C; p.U1 = U1; p.U2 = U2; p.U3 = U3; p.Ct = Ct; p.Ut1 = Ut1; p.Ut2 = Ut2; p.Ut3 = Ut3;
@@ -148,6 +160,94 @@ int tucker_attn_decode(const tucker_attn_desc* desc, const void* x, const void* 
   if (!p.dev_err) return TA_ERR_CUDA;
   const int rc = fast ? fast_decode(p) : generic_decode(p);
   tl_last_path = fast ? 2 : 1;
+  tl_last_launches = p.launches;
+  return rc;
+}
+
+static size_t paged_decode_need(const tucker_attn_desc& d, const tucker_paged_cache& c, int32_t prefix_len) {
+  if (!paged_batch_ok(d)) return 0;
+  return generic_paged_decode_workspace(d, paged_slots(c), prefix_len);
+}
+
+size_t tucker_attn_decode_paged_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache* cache) {
+  if (!desc_ok(desc, true) || !paged_ok(cache, 0)) return 0;
+  return paged_decode_need(*desc, *cache, 0);
+}
+
+size_t tucker_attn_decode_prefix_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache* cache,
+                                                 int32_t prefix_len) {
+  if (!desc_ok(desc, true) || !paged_ok(cache, prefix_len)) return 0;
+  return paged_decode_need(*desc, *cache, prefix_len);
+}
+
+int tucker_attn_decode_prefix(const tucker_attn_desc* desc, const void* x, const void* C, const void* U1, const void* U2,
+                              const void* U3, const void* Ct, const void* Ut1, const void* Ut2, const void* Ut3,
+                              const tucker_paged_cache* cache, const int32_t* cache_len, const int32_t* prefix_table,
+                              int32_t prefix_len, int32_t append, void* y, void* workspace, size_t workspace_bytes,
+                              void* cuda_stream) {
+  if (!desc_ok(desc, true) || !paged_ok(cache, prefix_len)) return TA_ERR_INVALID_ARG;
+  if (!x || !C || !U1 || !U2 || !U3 || !Ct || !Ut1 || !Ut2 || !Ut3 || !y || !workspace) return TA_ERR_INVALID_ARG;
+  if (!cache_len || (prefix_len > 0 && !prefix_table)) return TA_ERR_INVALID_ARG;
+  if (cache->K == cache->V && !shared_kv_weights(*desc, U3, Ut3)) return TA_ERR_INVALID_ARG;
+  const void* ptrs[] = {x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, y, cache->K, cache->V};
+  for (const void* q : ptrs)
+    if (!aligned16(q)) return TA_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return TA_ERR_INVALID_ARG;
+  const size_t need = paged_decode_need(*desc, *cache, prefix_len);
+  if (need == 0) return TA_ERR_UNSUPPORTED_SHAPE;
+  if (workspace_bytes < need) return TA_ERR_WORKSPACE_TOO_SMALL;
+  Problem p = {};
+  p.d = *desc;
+  p.scale = resolve_scale(*desc);
+  p.X = x; p.C = C; p.U1 = U1; p.U2 = U2; p.U3 = U3; p.Ct = Ct; p.Ut1 = Ut1; p.Ut2 = Ut2; p.Ut3 = Ut3;
+  p.Y = y; p.Kc = cache->K; p.Vc = cache->V; p.Lmax = (int32_t)paged_slots(*cache);
+  p.cache_len = cache_len; p.append = append ? 1 : 0;
+  p.paged = 1;
+  p.pv = PagedView{cache->block_table, cache->n_pages, cache->page_size, cache->max_pages};
+  p.prefix_table = prefix_table; p.prefix_len = prefix_len;
+  p.shared_kv = (cache->K == cache->V) ? 1 : 0;
+  p.shared_rope = (p.shared_kv && desc->rope) ? 1 : 0;
+  p.ws = static_cast<char*>(workspace); p.ws_bytes = workspace_bytes;
+  p.stream = static_cast<cudaStream_t>(cuda_stream);
+  p.dev_err = device_error_ptr();
+  p.prof_start = tl_prof_start; p.prof_stop = tl_prof_stop;
+  if (!p.dev_err) return TA_ERR_CUDA;
+  const int rc = generic_paged_decode(p);
+  tl_last_path = 1;
+  tl_last_launches = p.launches;
+  return rc;
+}
+
+int tucker_attn_decode_paged(const tucker_attn_desc* desc, const void* x, const void* C, const void* U1, const void* U2,
+                             const void* U3, const void* Ct, const void* Ut1, const void* Ut2, const void* Ut3,
+                             const tucker_paged_cache* cache, const int32_t* cache_len, int32_t append, void* y,
+                             void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  return tucker_attn_decode_prefix(desc, x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, cache, cache_len, nullptr, 0, append, y,
+                                   workspace, workspace_bytes, cuda_stream);
+}
+
+int tucker_cache_append_paged(const tucker_attn_desc* desc, const void* X, const void* U3, const void* Ut3,
+                              const tucker_paged_cache* cache, const int32_t* cache_len, const int32_t* tok_start, int32_t T,
+                              void* cuda_stream) {
+  if (!desc_ok(desc, true) || !paged_ok(cache, desc->pos0) || T < 0) return TA_ERR_INVALID_ARG;
+  if (!U3 || !Ut3 || !cache_len || !tok_start || (T > 0 && !X)) return TA_ERR_INVALID_ARG;
+  if (cache->K == cache->V && !shared_kv_weights(*desc, U3, Ut3)) return TA_ERR_INVALID_ARG;
+  const void* ptrs[] = {X, U3, Ut3, cache->K, cache->V};
+  for (const void* q : ptrs)
+    if (!aligned16(q)) return TA_ERR_INVALID_ARG;
+  Problem p = {};
+  p.d = *desc;
+  p.X = X; p.U3 = U3; p.Ut3 = Ut3; p.Kc = cache->K; p.Vc = cache->V; p.cache_len = cache_len;
+  p.paged = 1;
+  p.pv = PagedView{cache->block_table, cache->n_pages, cache->page_size, cache->max_pages};
+  p.shared_kv = (cache->K == cache->V) ? 1 : 0;
+  p.shared_rope = (p.shared_kv && desc->rope) ? 1 : 0;
+  p.stream = static_cast<cudaStream_t>(cuda_stream);
+  p.dev_err = device_error_ptr();
+  p.prof_start = tl_prof_start; p.prof_stop = tl_prof_stop;
+  if (!p.dev_err) return TA_ERR_CUDA;
+  const int rc = T > 0 ? generic_paged_append(p, tok_start, T) : TA_OK;
+  tl_last_path = 1;
   tl_last_launches = p.launches;
   return rc;
 }
@@ -219,7 +319,7 @@ int tucker_attn_sync_status(void* cuda_stream) {
   const int word = tucker_attn_last_device_error(cuda_stream);
   if (word < 0) return word;
   if (word & TA_DEVERR_WAIT_TIMEOUT) return TA_ERR_DEVICE_TIMEOUT;
-  if (word & TA_DEVERR_BAD_CACHE_LEN) return TA_ERR_INVALID_ARG;
+  if (word & (TA_DEVERR_BAD_CACHE_LEN | TA_DEVERR_BAD_PAGE)) return TA_ERR_INVALID_ARG;
   if (word & TA_DEVERR_BAD_INDEX) return TA_ERR_CUDA;
   return TA_OK;
 }

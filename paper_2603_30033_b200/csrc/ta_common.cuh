@@ -18,6 +18,12 @@ typedef __nv_bfloat16 bf16;
 // Device address of the current device's error word (nullptr if it cannot be resolved); ta_api.cu.
 unsigned int* device_error_word();
 
+// A paged latent cache as the kernels see it (the pools themselves travel as Problem::Kc / Vc).
+struct PagedView {
+  const int32_t* table;     // [B, max_pages]
+  int32_t n_pages, page_size, max_pages;
+};
+
 // Everything a path needs to run one call; filled by the API layer after validation.
 struct Problem {
   tucker_attn_desc d;
@@ -28,6 +34,10 @@ struct Problem {
   int32_t Lmax;
   const int32_t* cache_len; // decode only (device)
   int32_t append;           // decode only
+  int paged;                // decode: Kc / Vc are pools of pages, Lmax = max_pages * page_size
+  PagedView pv;
+  const int32_t* prefix_table;  // pages of the prefix that all sequences share (prefix_len > 0 only)
+  int32_t prefix_len;       // tokens in front of slot 0 of every sequence
   int shared_kv;            // one latent cache / one projection serves keys and values (U3 == Ut3)
   int shared_rope;          // ... together with latent RoPE: the one cache holds UN-rotated latent rows
   char* ws;                 // workspace base (256-byte aligned)
@@ -84,6 +94,12 @@ int wait_selftest(unsigned int* dev_err, int budget_us, int* out_dev, cudaStream
 int umma_gemm_f32_partials(Problem& p, const bf16* A, long lda, int M, const bf16* B, long ldb, int N, int K, int splits,
                            float* out, long split_stride);
 
+// Paged cache, shape-generic FMA path (ta_paged_generic.cu).  Decode with p.paged; append with p.X [T, d],
+// p.U3, p.Ut3, p.Kc, p.Vc, p.pv, p.cache_len.
+size_t generic_paged_decode_workspace(const tucker_attn_desc& d, int64_t Lmax, int32_t prefix_len);
+int generic_paged_decode(Problem& p);
+int generic_paged_append(Problem& p, const int32_t* tok_start, int32_t T);
+
 // HOSVD initialiser (ta_hosvd.cu)
 size_t hosvd_workspace(int n1, int n2, int n3, int r2, int r3);
 int hosvd_run(Problem& p, int n1, int n2, int n3, int r1, int r2, int r3, const float* T, float* core, float* U1,
@@ -113,6 +129,21 @@ __device__ __forceinline__ void pdl_enter() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
+#endif
+
+#if defined(__CUDACC__)
+namespace dec {
+// (cos, sin) of pos * theta for a rotation frequency theta given in double precision: the angle is
+// reduced to a fraction of a turn in double (positions of tens of thousands would lose ~1e-3 rad
+// in fp32) and only then handed to the fp32 sincospi.
+__device__ __forceinline__ float2 rope_cos_sin_theta(int pos, double theta) {
+  double turns = (double)pos * theta * 0.15915494309189535;   // angle / (2 pi)
+  turns -= rint(turns);
+  float sn, co;
+  sincospif((float)(2.0 * turns), &sn, &co);
+  return make_float2(co, sn);
+}
+}  // namespace dec
 #endif
 
 template <typename... KArgs, typename... Args>

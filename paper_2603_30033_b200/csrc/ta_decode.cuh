@@ -74,17 +74,6 @@ __device__ __forceinline__ long block_tile_scan(const int32_t* __restrict__ cach
   return (long)total;
 }
 
-// (cos, sin) of pos * theta for a rotation frequency theta given in double precision: the angle is
-// reduced to a fraction of a turn in double (positions of tens of thousands would lose ~1e-3 rad
-// in fp32) and only then handed to the fp32 sincospi.
-__device__ __forceinline__ float2 rope_cos_sin_theta(int pos, double theta) {
-  double turns = (double)pos * theta * 0.15915494309189535;   // angle / (2 pi)
-  turns -= rint(turns);
-  float sn, co;
-  sincospif((float)(2.0 * turns), &sn, &co);
-  return make_float2(co, sn);
-}
-
 // Rotation frequencies theta_i = base^(-2 i / r), i < r / 2 <= 128, computed on the host in double
 // precision and passed to the kernels by value.
 struct RopeFreqs {

@@ -1,0 +1,579 @@
+// Shape-generic FMA kernels of the paged cache: append, decode, decode behind a shared prefix; fp32 storage, and bf16
+// shapes the tensor-core kernels do not cover.  Everything between the inputs and the outputs is fp32.
+//
+// Unlike the contiguous decode step's generic kernel, which walks a whole sequence in one block, the keys are split
+// over blocks and joined by their (max, sum, output) partials: a step with few sequences still fills the GPU.
+#include "ta_gemm_fma.cuh"
+#include "ta_paged.cuh"
+
+#include <math.h>
+
+#include <algorithm>
+
+namespace ta {
+namespace {
+
+using fma::ld;
+using fma::st;
+
+// ---------------------------------------------------------------------------------------
+// 32 x 32 tile of A [M, K] B [K, N], fp32 accumulation.  256 threads: four groups of 64 threads take a quarter of every
+// 64-deep K block each (4 x 4 outputs per thread) and are summed through shared memory at the end, so that the short
+// and narrow products of a decode step (few rows, K = d) have four times the threads a plain tile would.  The next
+// K block is in registers while the current one is multiplied.
+// ---------------------------------------------------------------------------------------
+constexpr int GM = 32, GN = 32, GK = 64;
+
+struct TileSmem {
+  union {
+    struct { float a[GK][GM + 1], b[GK][GN + 1]; } in;
+    float part[4][GM][GN + 1];
+  };
+};
+
+struct MatB {              // element (k, n) at k * sk + n * sn
+  long sk, sn;
+};
+
+// On return s.part[0] holds the tile (rows and columns past the edge are zero); all threads are synchronised.
+template <typename TA, typename TB>
+__device__ __forceinline__ void gemm_tile(const TA* __restrict__ A, long lda, const TB* __restrict__ Bm, MatB sb, int M, int N, int K,
+                                          int m0, int n0, TileSmem& s) {
+  const int tid = threadIdx.x, grp = tid / 64, tx = tid % 8, ty = (tid % 64) / 8;
+  float acc[4][4] = {};
+  float ra[8], rb[8];
+  auto fetch = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int idx = tid + i * 256;
+      const int m = idx / GK, k = k0 + idx % GK;
+      ra[i] = (m0 + m < M && k < K) ? ld(A + (long)(m0 + m) * lda + k) : 0.f;
+      const int n = sb.sn == 1 ? idx % GN : idx / GK, kb = k0 + (sb.sn == 1 ? idx / GN : idx % GK);
+      rb[i] = (n0 + n < N && kb < K) ? ld(Bm + (long)kb * sb.sk + (long)(n0 + n) * sb.sn) : 0.f;
+    }
+  };
+  fetch(0);
+  for (int k0 = 0; k0 < K; k0 += GK) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int idx = tid + i * 256;
+      s.in.a[idx % GK][idx / GK] = ra[i];
+      if (sb.sn == 1) s.in.b[idx / GN][idx % GN] = rb[i];
+      else s.in.b[idx % GK][idx / GK] = rb[i];
+    }
+    __syncthreads();
+    if (k0 + GK < K) fetch(k0 + GK);
+#pragma unroll
+    for (int kk = 0; kk < GK / 4; ++kk) {
+      const int k = grp * (GK / 4) + kk;
+      float a[4], b[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { a[i] = s.in.a[k][ty * 4 + i]; b[i] = s.in.b[k][tx * 4 + i]; }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s.part[grp][ty * 4 + i][tx * 4 + j] = acc[i][j];
+  __syncthreads();
+  for (int i = tid; i < GM * GN; i += 256) {
+    float* c = &s.part[0][i / GN][i % GN];
+    *c = (s.part[0][i / GN][i % GN] + s.part[1][i / GN][i % GN]) + (s.part[2][i / GN][i % GN] + s.part[3][i / GN][i % GN]);
+  }
+  __syncthreads();
+}
+
+// C [M, N] (ld ldc) = A B for up to three (B, C) pairs that share A and K: blockIdx.z picks the pair.
+template <typename TB, typename TC>
+struct GemmPart {
+  const TB* B;
+  MatB sb;
+  TC* C;
+  long ldc;
+  int N;
+};
+template <typename TA, typename TB, typename TC>
+struct GemmArgs {
+  const TA* A;
+  long lda;
+  int M, K;
+  GemmPart<TB, TC> part[3];
+};
+template <typename TA, typename TB, typename TC>
+__global__ void __launch_bounds__(256) k_pg_gemm(const GemmArgs<TA, TB, TC> g) {
+  __shared__ TileSmem s;
+  const GemmPart<TB, TC> pt = g.part[blockIdx.z];
+  const int m0 = blockIdx.x * GM, n0 = blockIdx.y * GN;
+  if (n0 >= pt.N) return;
+  gemm_tile(g.A, g.lda, pt.B, pt.sb, g.M, pt.N, g.K, m0, n0, s);
+  for (int i = threadIdx.x; i < GM * GN; i += 256) {
+    const int m = m0 + i / GN, n = n0 + i % GN;
+    if (m < g.M && n < pt.N) st(pt.C + (long)m * pt.ldc + n, s.part[0][i / GN][i % GN]);
+  }
+}
+
+// Rotation frequency of coordinate pair i of r; (cos, sin) at a position: dec::rope_cos_sin_theta.
+__device__ __forceinline__ double pair_theta(int i, int r, double base) { return pow(base, -2.0 * (double)i / (double)r); }
+constexpr int kMaxPairs = 544;      // r3 / 2; shape_ok() bounds r3 well below this
+
+// ---------------------------------------------------------------------------------------
+// Append: 32 tokens x 32 latent coordinates per block; blockIdx.z = 0 keys, 1 values.
+// ---------------------------------------------------------------------------------------
+template <typename T>
+struct AppendArgs {
+  const T *X, *U3, *Ut3;
+  T *K, *V;
+  PagedView pv;
+  const int32_t *tok_start, *cache_len;
+  int B, T_, d, r3, t3, rope, pos0;
+  int keys_shared;      // 1: only the value rows are written (one pool; un-rotated rows when rope)
+  double base;
+  unsigned int* err;
+};
+template <typename T>
+__global__ void __launch_bounds__(256) k_pg_append(const AppendArgs<T> g) {
+  __shared__ TileSmem s;
+  __shared__ long row_s[GM];
+  __shared__ int pos_s[GM];
+  __shared__ double theta_s[GN / 2];
+  const bool is_k = blockIdx.z == 0 && !g.keys_shared;
+  const int r = is_k ? g.r3 : g.t3;
+  const int m0 = blockIdx.x * GM, n0 = blockIdx.y * GN;
+  if (n0 >= r) return;
+  if (is_k && g.rope && threadIdx.x >= 64 && threadIdx.x < 64 + GN / 2)
+    theta_s[threadIdx.x - 64] = pair_theta(n0 / 2 + threadIdx.x - 64, r, g.base);
+  if (threadIdx.x < GM) {
+    AppendDst dst;
+    dst.row = -1; dst.pos = 0;
+    if (m0 + (int)threadIdx.x < g.T_)
+      dst = append_dst(m0 + threadIdx.x, g.tok_start, g.cache_len, g.B, g.pos0, g.pv, g.err);
+    row_s[threadIdx.x] = dst.row;
+    pos_s[threadIdx.x] = dst.pos;
+  }
+  MatB sb = {r, 1};
+  gemm_tile(g.X, (long)g.d, is_k ? g.U3 : g.Ut3, sb, g.T_, r, g.d, m0, n0, s);
+  T* pool = is_k ? g.K : g.V;
+  for (int i = threadIdx.x; i < GM * GN; i += 256) {
+    const int m = i / GN, c = i % GN, n = n0 + c;
+    if (row_s[m] < 0 || n >= r) continue;
+    float v = s.part[0][m][c];
+    if (is_k && g.rope) {            // r3 is even and tiles start at even columns: both halves of a pair are here
+      const float other = s.part[0][m][c ^ 1];
+      const float2 cs = dec::rope_cos_sin_theta(pos_s[m], theta_s[c >> 1]);
+      v = (c & 1) ? other * cs.y + v * cs.x : v * cs.x - other * cs.y;
+    }
+    if (TA_IDX_OK(g.err, row_s[m] * r + n, 1, (long)g.pv.n_pages * g.pv.page_size * r)) st(pool + row_s[m] * r + n, v);
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// Per-head queries and the new token: w [r1][B][r3] = qt C[a];  qhat[b, h] = scale * sum_a U1[h, a] w[a, b], rotated at
+// the new token's position prefix_len + cache_len[b]; the new key rotated in place; both appended.
+// ---------------------------------------------------------------------------------------
+template <typename T>
+__global__ void __launch_bounds__(256) k_pg_queries(const float* __restrict__ w, const T* __restrict__ U1, float* __restrict__ qhat,
+                                                    float* __restrict__ knew, const float* __restrict__ vnew, T* __restrict__ K,
+                                                    T* __restrict__ V, const PagedView pv, const int32_t* __restrict__ cache_len,
+                                                    int B, int nH, int r1, int r3, int t3, int Lmax, int prefix_len, float scale, int rope,
+                                                    double base, int append, int shared_kv, int shared_rope, unsigned int* err) {
+  const int b = blockIdx.x;
+  __shared__ long dst_s;
+  __shared__ float2 cs_s[kMaxPairs];          // (cos, sin) of the new token's position
+  int L = cache_len[b];
+  if (L < 0 || L >= Lmax) {
+    if (threadIdx.x == 0 && blockIdx.y == 0) atomicOr(err, (unsigned)TA_DEVERR_BAD_CACHE_LEN);
+    L = L < 0 ? 0 : Lmax - 1;
+  }
+  const int half = (r3 + 1) / 2;
+  if (rope)
+    for (int i = threadIdx.x; i < r3 / 2; i += blockDim.x)
+      cs_s[i] = dec::rope_cos_sin_theta(prefix_len + L, pair_theta(i, r3, base));
+  __syncthreads();
+  for (int i = blockIdx.y * blockDim.x + threadIdx.x; i < nH * half; i += gridDim.y * blockDim.x) {
+    const int h = i / half, c = 2 * (i % half);
+    float xe = 0.f, xo = 0.f;
+    for (int a = 0; a < r1; ++a) {
+      const float u = ld(U1 + (long)h * r1 + a);
+      const float* wr = w + ((long)a * B + b) * r3 + c;
+      xe = fmaf(u, wr[0], xe);
+      if (c + 1 < r3) xo = fmaf(u, wr[1], xo);
+    }
+    xe *= scale; xo *= scale;
+    float* q = qhat + ((long)b * nH + h) * r3 + c;
+    if (rope) {
+      const float2 cs = cs_s[c >> 1];
+      q[0] = xe * cs.x - xo * cs.y;
+      q[1] = xe * cs.y + xo * cs.x;
+    } else {
+      q[0] = xe;
+      if (c + 1 < r3) q[1] = xo;
+    }
+  }
+  if (blockIdx.y != 0) return;
+  if (threadIdx.x == 0) dst_s = append ? paged_row(pv.table + (long)b * pv.max_pages, L, pv, err) : -1;
+  if (rope)
+    for (int i = threadIdx.x; i < r3 / 2; i += blockDim.x) {
+      float* px = knew + (long)b * r3 + 2 * i;
+      const float2 cs = cs_s[i];
+      const float xe = px[0], xo = px[1];
+      px[0] = xe * cs.x - xo * cs.y;
+      px[1] = xe * cs.y + xo * cs.x;
+    }
+  __syncthreads();
+  if (dst_s < 0) return;
+  [[maybe_unused]] const long rows = (long)pv.n_pages * pv.page_size;
+  if (!shared_kv && TA_IDX_OK(err, dst_s, 1, rows))
+    for (int c = threadIdx.x; c < r3; c += blockDim.x) st(K + dst_s * r3 + c, knew[(long)b * r3 + c]);
+  if (TA_IDX_OK(err, dst_s, 1, rows))      // one pool: the value row, which is the un-rotated latent row
+    for (int c = threadIdx.x; c < t3; c += blockDim.x) st(V + dst_s * t3 + c, vnew[(long)b * t3 + c]);
+}
+
+// ---------------------------------------------------------------------------------------
+// Attention partials of 16 query rows against one share of a list of keys.
+//   own part    grid (ceil(nH / 16), splits, B): rows = heads of sequence z, keys = its cached slots and the new token
+//   prefix      grid (ceil(B nH / 16), splits, 1): rows = all heads of all sequences, keys = the prefix
+// Thread (row, l) of 16 x 16: scores of keys l and l + 16 of a 32-key tile, then output columns 4 l + 64 i .. + 3.
+// Partial of (row, split): max, sum, unnormalised output; a share without keys leaves max = -inf, sum = 0, and its
+// output is not written (and not read).
+// ---------------------------------------------------------------------------------------
+constexpr int AR = 16, AK = 32, kMaxO4 = 8;       // t3 <= 64 * kMaxO4
+__host__ __device__ inline int pitch4(int r) { return (r + 3) / 4 * 4 + 4; }
+__host__ __device__ inline size_t pg_attn_smem(int r3, int t3) {
+  return sizeof(float) * ((size_t)(AR + AK) * pitch4(r3) + (size_t)AK * pitch4(t3) + AR * (AK + 1)) + sizeof(long) * AK;
+}
+template <typename T>
+struct AttnArgs {
+  const float* q;          // [rows, r3]
+  const T *K, *V;          // pools
+  PagedView pv;            // table: row z of it is used (the prefix: its only row)
+  const int32_t* cache_len;// nullptr: the prefix, n_keys keys
+  const float *knew, *vnew;// [B, r3] rotated, [B, t3]
+  int rows_per_z, n_keys, Lmax, r3, t3, splits;
+  int rotate_keys, pos_base;   // one pool with latent RoPE: keys are formed by rotation; position of slot 0
+  double base;
+  float *part_o, *part_ml; // [z * rows_per_z + row][splits][t3] / [..][splits][2]
+  unsigned int* err;
+};
+template <typename T>
+__global__ void __launch_bounds__(256) k_pg_attn(const AttnArgs<T> g) {
+  extern __shared__ __align__(16) float sm[];
+  __shared__ double theta_s[kMaxPairs];
+  const int rp = pitch4(g.r3), tp = pitch4(g.t3);
+  float* qs = sm;                       // [AR][rp]
+  float* Ks = qs + AR * rp;             // [AK][rp]
+  float* Vs = Ks + AK * rp;             // [AK][tp]
+  float* ps = Vs + AK * tp;             // [AR][AK + 1]
+  long* rows_s = reinterpret_cast<long*>(ps + AR * (AK + 1));   // AR * (AK + 1) is even: 8-byte aligned
+  const int tid = threadIdx.x, r = tid / 16, l = tid % 16;
+  const int split = blockIdx.y, row0 = blockIdx.x * AR, z = blockIdx.z;
+  const int row = row0 + r;
+  const bool valid = row < g.rows_per_z;
+  int L = 0, limit = g.n_keys;
+  if (g.cache_len) {
+    L = g.cache_len[z];
+    L = L < 0 ? 0 : (L >= g.Lmax ? g.Lmax - 1 : L);
+    limit = L + 1;
+  }
+  const int tiles = (limit + AK - 1) / AK;
+  const int t_beg = (int)((long)tiles * split / g.splits), t_end = (int)((long)tiles * (split + 1) / g.splits);
+  const int32_t* table = g.pv.table + (long)z * g.pv.max_pages;
+  if (g.rotate_keys)
+    for (int i = tid; i < g.r3 / 2; i += 256) theta_s[i] = pair_theta(i, g.r3, g.base);
+  for (int i = tid; i < AR * rp; i += 256) {
+    const int rr = i / rp, c = i % rp;
+    qs[i] = (row0 + rr < g.rows_per_z && c < g.r3) ? g.q[((long)z * g.rows_per_z + row0 + rr) * g.r3 + c] : 0.f;
+  }
+  float m = -INFINITY, lsum = 0.f;
+  float4 o[kMaxO4];
+#pragma unroll
+  for (int i = 0; i < kMaxO4; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int n4 = (g.r3 + 3) / 4;
+  for (int t = t_beg; t < t_end; ++t) {
+    const int k0 = t * AK;
+    __syncthreads();
+    if (tid < AK) {                     // -1: no such row (zeros), -2: the new token
+      const int s = k0 + tid;
+      rows_s[tid] = s >= limit ? -1 : (g.cache_len && s == L ? -2 : paged_row(table, s, g.pv, g.err));
+    }
+    __syncthreads();
+    for (int i = tid; i < AK * rp; i += 256) {
+      const int j = i / rp, c = i % rp;
+      const long rw = rows_s[j];
+      float v = 0.f;
+      if (c < g.r3) {
+        if (rw == -2) v = g.knew[(long)z * g.r3 + c];
+        else if (rw >= 0) {
+          v = ld(g.K + rw * g.r3 + c);
+          if (g.rotate_keys) {          // one pool with latent RoPE: the key is the cached row, rotated
+            const float other = ld(g.K + rw * g.r3 + (c ^ 1));
+            const float2 cs = dec::rope_cos_sin_theta(g.pos_base + k0 + j, theta_s[c >> 1]);
+            v = (c & 1) ? other * cs.y + v * cs.x : v * cs.x - other * cs.y;
+          }
+        }
+      }
+      Ks[i] = v;
+    }
+    for (int i = tid; i < AK * tp; i += 256) {
+      const int j = i / tp, c = i % tp;
+      const long rw = rows_s[j];
+      float v = 0.f;
+      if (c < g.t3) v = rw == -2 ? g.vnew[(long)z * g.t3 + c] : (rw >= 0 ? ld(g.V + rw * g.t3 + c) : 0.f);
+      Vs[i] = v;
+    }
+    __syncthreads();
+    float s0 = 0.f, s1 = 0.f;
+    const float4* q4 = reinterpret_cast<const float4*>(qs + r * rp);
+    const float4* ka = reinterpret_cast<const float4*>(Ks + l * rp);
+    const float4* kb = reinterpret_cast<const float4*>(Ks + (l + 16) * rp);
+    for (int c = 0; c < n4; ++c) {
+      const float4 q = q4[c], a = ka[c], b = kb[c];
+      s0 = fmaf(q.x, a.x, s0); s0 = fmaf(q.y, a.y, s0); s0 = fmaf(q.z, a.z, s0); s0 = fmaf(q.w, a.w, s0);
+      s1 = fmaf(q.x, b.x, s1); s1 = fmaf(q.y, b.y, s1); s1 = fmaf(q.z, b.z, s1); s1 = fmaf(q.w, b.w, s1);
+    }
+    if (k0 + l >= limit) s0 = -INFINITY;
+    if (k0 + l + 16 >= limit) s1 = -INFINITY;
+    float mt = fmaxf(s0, s1);
+#pragma unroll
+    for (int d = 8; d >= 1; d >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, d));
+    const float mn = fmaxf(m, mt);      // a tile holds at least one key below `limit`
+    const float p0 = expf(s0 - mn), p1 = expf(s1 - mn), f = expf(m - mn);
+    float pt = p0 + p1;
+#pragma unroll
+    for (int d = 8; d >= 1; d >>= 1) pt += __shfl_xor_sync(0xffffffffu, pt, d);
+    lsum = lsum * f + pt;
+    m = mn;
+    ps[r * (AK + 1) + l] = p0;
+    ps[r * (AK + 1) + l + 16] = p1;
+    __syncwarp();                       // a row's 16 threads are half a warp
+#pragma unroll
+    for (int i = 0; i < kMaxO4; ++i)
+      if (4 * l + 64 * i < g.t3) { o[i].x *= f; o[i].y *= f; o[i].z *= f; o[i].w *= f; }
+    for (int j = 0; j < AK; ++j) {
+      const float p = ps[r * (AK + 1) + j];
+      const float4* v4 = reinterpret_cast<const float4*>(Vs + j * tp);
+#pragma unroll
+      for (int i = 0; i < kMaxO4; ++i)
+        if (4 * l + 64 * i < g.t3) {
+          const float4 v = v4[l + 16 * i];
+          o[i].x = fmaf(p, v.x, o[i].x); o[i].y = fmaf(p, v.y, o[i].y);
+          o[i].z = fmaf(p, v.z, o[i].z); o[i].w = fmaf(p, v.w, o[i].w);
+        }
+    }
+  }
+  if (!valid) return;
+  const long slot = ((long)z * g.rows_per_z + row) * g.splits + split;
+  if (l == 0) { g.part_ml[2 * slot] = m; g.part_ml[2 * slot + 1] = lsum; }
+  if (t_beg >= t_end) return;
+  float* po = g.part_o + slot * g.t3;
+#pragma unroll
+  for (int i = 0; i < kMaxO4; ++i) {
+    const int c = 4 * l + 64 * i;
+    const float v[4] = {o[i].x, o[i].y, o[i].z, o[i].w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < g.t3) po[c + e] = v[e];
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// o[b, h] from the partials of its own keys (splits_o) and of the prefix (splits_p, may be 0), one warp per (b, h).
+// ---------------------------------------------------------------------------------------
+__global__ void __launch_bounds__(256) k_pg_merge(const float* __restrict__ po, const float* __restrict__ ml, int splits_o,
+                                                  const float* __restrict__ po_p, const float* __restrict__ ml_p, int splits_p,
+                                                  float* __restrict__ o, int rows, int t3) {
+  const int row = blockIdx.x * 8 + threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (row >= rows) return;
+  const float2* a = reinterpret_cast<const float2*>(ml) + (long)row * splits_o;
+  const float2* p = reinterpret_cast<const float2*>(ml_p) + (long)row * splits_p;
+  const int n = splits_o + splits_p;
+  float m = -INFINITY;
+  for (int i = lane; i < n; i += 32) m = fmaxf(m, i < splits_o ? a[i].x : p[i - splits_o].x);
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  float l = 0.f;                        // the new token's share holds a key: m is finite
+  for (int i = lane; i < n; i += 32) {
+    const float2 v = i < splits_o ? a[i] : p[i - splits_o];
+    l += v.y * expf(v.x - m);
+  }
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+  const float inv = 1.f / l;
+  for (int c = lane; c < t3; c += 32) {
+    float acc = 0.f;
+    for (int i = 0; i < n; ++i) {
+      const float2 v = i < splits_o ? a[i] : p[i - splits_o];
+      if (v.y > 0.f)                    // a share without keys wrote no output
+        acc = fmaf(expf(v.x - m), i < splits_o ? po[((long)row * splits_o + i) * t3 + c]
+                                               : po_p[((long)row * splits_p + (i - splits_o)) * t3 + c], acc);
+    }
+    o[(long)row * t3 + c] = acc * inv;
+  }
+}
+
+// Output-side core: u[b, a, c] = sum_h Ut1[h, a] o[b, h, c];  z[b, j] = sum_a sum_c Ct[a, j, c] u[b, a, c] (a warp per j).
+template <typename T>
+__global__ void __launch_bounds__(256) k_pg_u(const float* __restrict__ o, const T* __restrict__ Ut1, float* __restrict__ u, int B,
+                                              int nH, int t1, int t3) {
+  const long total = (long)B * t1 * t3;
+  for (long i = blockIdx.x * 256L + threadIdx.x; i < total; i += gridDim.x * 256L) {
+    const int c = (int)(i % t3), a = (int)((i / t3) % t1), b = (int)(i / ((long)t3 * t1));
+    float acc = 0.f;
+    for (int h = 0; h < nH; ++h) acc = fmaf(ld(Ut1 + (long)h * t1 + a), o[((long)b * nH + h) * t3 + c], acc);
+    u[i] = acc;
+  }
+}
+template <typename T>
+__global__ void __launch_bounds__(256) k_pg_z(const float* __restrict__ u, const T* __restrict__ Ct, float* __restrict__ z, int t1,
+                                              int t2, int t3) {
+  const int b = blockIdx.y, j = blockIdx.x * 8 + threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (j >= t2) return;
+  float acc = 0.f;
+  for (int a = 0; a < t1; ++a)
+    for (int c = lane; c < t3; c += 32) acc = fmaf(ld(Ct + ((long)a * t2 + j) * t3 + c), u[((long)b * t1 + a) * t3 + c], acc);
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, d);
+  if (lane == 0) z[(long)b * t2 + j] = acc;
+}
+
+// ---- host side ----------------------------------------------------------------------------------------------------
+
+bool shape_ok(const tucker_attn_desc& d) {
+  return d.t3 <= 64 * kMaxO4 && d.r3 <= 2 * kMaxPairs && pg_attn_smem(d.r3, d.t3) <= 200 * 1024;
+}
+
+// Shares per list of keys: about two blocks per SM, no more than there are tiles.
+int pick_splits(long blocks, long keys) {
+  const long tiles = (keys + AK - 1) / AK;
+  return (int)std::max<long>(1, std::min<long>(std::min<long>(tiles, 128), (2 * 148 + blocks - 1) / blocks));
+}
+int own_splits(const tucker_attn_desc& d, int64_t Lmax) { return pick_splits((long)d.B * ((d.n_H + AR - 1) / AR), Lmax); }
+int prefix_splits(const tucker_attn_desc& d, int32_t P) { return P > 0 ? pick_splits(((long)d.B * d.n_H + AR - 1) / AR, P) : 0; }
+
+struct Ws {
+  float *qt, *knew, *vnew, *w, *qhat, *po, *ml, *po_p, *ml_p, *o, *u, *z;
+};
+size_t carve(const tucker_attn_desc& d, int64_t Lmax, int32_t P, char* base, Ws* out) {
+  Carver c(base);
+  Ws t;
+  const size_t B = d.B, rows = B * d.n_H, so = own_splits(d, Lmax), sp = prefix_splits(d, P);
+  t.qt = c.take<float>(B * d.r2);
+  t.knew = c.take<float>(B * d.r3);
+  t.vnew = c.take<float>(B * d.t3);
+  t.w = c.take<float>(B * d.r1 * d.r3);
+  t.qhat = c.take<float>(rows * d.r3);
+  t.po = c.take<float>(rows * so * d.t3);
+  t.ml = c.take<float>(rows * so * 2);
+  t.po_p = c.take<float>(rows * sp * d.t3);
+  t.ml_p = c.take<float>(rows * sp * 2);
+  t.o = c.take<float>(rows * d.t3);
+  t.u = c.take<float>(B * d.t1 * d.t3);
+  t.z = c.take<float>(B * d.t2);
+  if (out) *out = t;
+  return c.off;
+}
+
+template <typename TA, typename TB, typename TC>
+int launch_gemm(Problem& p, const GemmArgs<TA, TB, TC>& g, int parts, int max_n) {
+  k_pg_gemm<TA, TB, TC><<<dim3((g.M + GM - 1) / GM, (max_n + GN - 1) / GN, parts), 256, 0, p.stream>>>(g);
+  TA_LAUNCH_CHECK(p);
+  return TA_OK;
+}
+
+template <typename T>
+int attn(Problem& p, const AttnArgs<T>& g, int zs) {
+  const size_t smem = pg_attn_smem(g.r3, g.t3);
+  TA_CUDA_TRY(cudaFuncSetAttribute(k_pg_attn<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  k_pg_attn<T><<<dim3((g.rows_per_z + AR - 1) / AR, g.splits, zs), 256, smem, p.stream>>>(g);
+  TA_LAUNCH_CHECK(p);
+  return TA_OK;
+}
+
+template <typename T>
+int decode_typed(Problem& p) {
+  const tucker_attn_desc& d = p.d;
+  const int P = p.prefix_len;
+  Ws w;
+  carve(d, p.Lmax, P, p.ws, &w);
+  int rc;
+  {
+    GemmArgs<T, T, float> g = {};
+    g.A = (const T*)p.X; g.lda = d.d_model; g.M = d.B; g.K = d.d_model;
+    g.part[0] = {(const T*)p.U2, {d.r2, 1}, w.qt, d.r2, d.r2};
+    g.part[1] = {(const T*)p.U3, {d.r3, 1}, w.knew, d.r3, d.r3};
+    g.part[2] = {(const T*)p.Ut3, {d.t3, 1}, w.vnew, d.t3, d.t3};
+    if ((rc = launch_gemm(p, g, 3, std::max(d.r2, std::max(d.r3, d.t3))))) return rc;
+  }
+  {
+    // w[a] = qt C[a], all a in one launch
+    fma::GemmShape g = fma::plain(d.B, d.r3, d.r2, d.r2, d.r3, 1, d.r3);
+    g.Z2 = d.r1; g.b2 = (long)d.r2 * d.r3; g.c2 = (long)d.B * d.r3;
+    if ((rc = fma::gemm(p, w.qt, (const T*)p.C, w.w, g, d.r1))) return rc;
+  }
+  k_pg_queries<T><<<dim3(d.B, std::max(1, std::min(8, 296 / d.B))), 256, 0, p.stream>>>(
+      w.w, (const T*)p.U1, w.qhat, w.knew, w.vnew, (T*)p.Kc, (T*)p.Vc, p.pv, p.cache_len, d.B, d.n_H, d.r1, d.r3, d.t3, p.Lmax, P,
+      p.scale, d.rope, (double)d.rope_base, p.append, p.shared_kv, p.shared_rope, p.dev_err);
+  TA_LAUNCH_CHECK(p);
+  AttnArgs<T> a = {};
+  a.q = w.qhat; a.K = (const T*)p.Kc; a.V = (const T*)p.Vc; a.pv = p.pv; a.cache_len = p.cache_len;
+  a.knew = w.knew; a.vnew = w.vnew; a.rows_per_z = d.n_H; a.Lmax = p.Lmax; a.r3 = d.r3; a.t3 = d.t3;
+  a.splits = own_splits(d, p.Lmax); a.rotate_keys = p.shared_rope; a.pos_base = P; a.base = (double)d.rope_base;
+  a.part_o = w.po; a.part_ml = w.ml; a.err = p.dev_err;
+  prof_begin(p);
+  if ((rc = attn(p, a, d.B))) return rc;
+  const int sp = prefix_splits(d, P);
+  if (P > 0) {
+    a.pv.table = p.prefix_table; a.pv.max_pages = (P + p.pv.page_size - 1) / p.pv.page_size;
+    a.cache_len = nullptr; a.n_keys = P; a.pos_base = 0; a.rows_per_z = d.B * d.n_H; a.splits = sp;
+    a.part_o = w.po_p; a.part_ml = w.ml_p;
+    if ((rc = attn(p, a, 1))) return rc;
+  }
+  prof_end(p);
+  const int rows = d.B * d.n_H;
+  k_pg_merge<<<(rows + 7) / 8, 256, 0, p.stream>>>(w.po, w.ml, own_splits(d, p.Lmax), w.po_p, w.ml_p, sp, w.o, rows, d.t3);
+  TA_LAUNCH_CHECK(p);
+  k_pg_u<T><<<(int)std::min<long>(148 * 8, ((long)d.B * d.t1 * d.t3 + 255) / 256), 256, 0, p.stream>>>(w.o, (const T*)p.Ut1, w.u, d.B,
+                                                                                                      d.n_H, d.t1, d.t3);
+  TA_LAUNCH_CHECK(p);
+  k_pg_z<T><<<dim3((d.t2 + 7) / 8, d.B), 256, 0, p.stream>>>(w.u, (const T*)p.Ct, w.z, d.t1, d.t2, d.t3);
+  TA_LAUNCH_CHECK(p);
+  GemmArgs<float, T, T> g = {};
+  g.A = w.z; g.lda = d.t2; g.M = d.B; g.K = d.t2;
+  g.part[0] = {(const T*)p.Ut2, {1, d.t2}, (T*)p.Y, d.d_model, d.d_model};
+  return launch_gemm(p, g, 1, d.d_model);
+}
+
+template <typename T>
+int append_typed(Problem& p, const int32_t* tok_start, int32_t T_) {
+  const tucker_attn_desc& d = p.d;
+  AppendArgs<T> g = {};
+  g.X = (const T*)p.X; g.U3 = (const T*)p.U3; g.Ut3 = (const T*)p.Ut3;
+  g.K = (T*)p.Kc; g.V = (T*)p.Vc; g.pv = p.pv; g.tok_start = tok_start; g.cache_len = p.cache_len;
+  g.B = d.B; g.T_ = T_; g.d = d.d_model; g.r3 = d.r3; g.t3 = d.t3; g.rope = d.rope; g.pos0 = d.pos0;
+  g.keys_shared = p.shared_kv; g.base = (double)d.rope_base; g.err = p.dev_err;
+  const int wide = p.shared_kv ? d.t3 : std::max(d.r3, d.t3);
+  k_pg_append<T><<<dim3((T_ + GM - 1) / GM, (wide + GN - 1) / GN, p.shared_kv ? 1 : 2), 256, 0, p.stream>>>(g);
+  TA_LAUNCH_CHECK(p);
+  return TA_OK;
+}
+
+}  // namespace
+
+size_t generic_paged_decode_workspace(const tucker_attn_desc& d, int64_t Lmax, int32_t prefix_len) {
+  return shape_ok(d) ? carve(d, Lmax, prefix_len, nullptr, nullptr) : 0;
+}
+
+int generic_paged_decode(Problem& p) {
+  if (!shape_ok(p.d)) return TA_ERR_UNSUPPORTED_SHAPE;
+  return p.d.dtype == TA_DTYPE_F32 ? decode_typed<float>(p) : decode_typed<bf16>(p);
+}
+
+int generic_paged_append(Problem& p, const int32_t* tok_start, int32_t T) {
+  return p.d.dtype == TA_DTYPE_F32 ? append_typed<float>(p, tok_start, T) : append_typed<bf16>(p, tok_start, T);
+}
+
+}  // namespace ta
