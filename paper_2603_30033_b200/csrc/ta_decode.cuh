@@ -102,11 +102,11 @@ __device__ __forceinline__ float2 rope_cos_sin(int pos, int i, int r, double log
 //   w[a, c]  = sum_q qt[q] C[a, q, c]         (the core contracted with the query first:
 //   qhat_h   = mult * sum_a U1[h, a] w[a, :]   C x_2 qt x_1 U1, Eq. 9, so that the n_H
 //                                              per-head matrices G_h are never formed)
-//   qhat_h  <- qhat_h R(L, r3), stored bf16 [B, nH, r3]
+//   qhat_h  <- qhat_h R(L, r3), stored bf16 [B, nH, r3]; with qhat_lo the rounded rest as well
 // The core is read with 16-byte loads that are all issued before anything waits on them:
 // warp w, lane (rg = lane / 4, ch = lane % 4) owns chunk ch of the CTA's 64-byte column range
 // in the core rows q = 8 w + rg + 64 i, for AB = 8 / NQ slices a at a time (NQ = ceil(r2/64)).
-// part: [splits][Mpad][r2 + r3 + t3] fp32.
+// part: [splits][Mpad][r2 + r3 + t3] fp32.  With pv.table the caches are pools of pages; pos_base is the position of slot 0.
 // ---------------------------------------------------------------------------------------
 constexpr int DQ_CW = 32;       // latent key coordinates per CTA
 constexpr int DQ_MAX_R1 = 32;   // head ranks r1, t1 supported by the shared-memory tables
@@ -118,7 +118,7 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
            const bf16* __restrict__ C, const bf16* __restrict__ U1, float mult, bf16* __restrict__ qhat,
            bf16* __restrict__ knew, bf16* __restrict__ vnew, bf16* __restrict__ Kc, bf16* __restrict__ Vc, int Lmax,
            const int32_t* __restrict__ cache_len, int rope, const RopeFreqs freqs, int append, int shared_kv,
-           unsigned int* err) {
+           const PagedView pv, int pos_base, bf16* __restrict__ qhat_lo, unsigned int* err) {
   constexpr int AB = 8 / NQ;                        // core slices per batch (8 loads of 16 bytes in flight per thread)
   __shared__ float qt_s[DQ_MAX_R2];                 // latent query of the new token
   __shared__ float k_s[DQ_CW];                      // this CTA's coordinates of the new key (unrotated)
@@ -149,12 +149,25 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
     if (threadIdx.x == 0 && blockIdx.y == 0) atomicOr(err, (unsigned)TA_DEVERR_BAD_CACHE_LEN);
     L = clamp_len(L, Lmax);
   }
+  // cache row of the new token (-1: the page it needs does not exist, flagged) and rows that exist
+  long new_row = (long)b * Lmax + L;
+  [[maybe_unused]] long n_rows = (long)gridDim.x * Lmax;
+  if (pv.table) {
+    n_rows = (long)pv.n_pages * pv.page_size;
+    const int j = L / pv.page_size;
+    const int pg = append ? pv.table[(long)b * pv.max_pages + j] : -1;
+    new_row = (pg < 0 || pg >= pv.n_pages) ? -1 : (long)pg * pv.page_size + (L - j * pv.page_size);
+    if (append && new_row < 0) {
+      if (threadIdx.x == 0 && blockIdx.y == 0) atomicOr(err, (unsigned)TA_DEVERR_BAD_PAGE);
+      append = 0;
+    }
+  }
   // Everything above and the two tables below depend on the call's inputs only (core, U1, cache_len)
   // and runs while the projection GEMM before this kernel finishes; its partial sums are read after
   // pdl_enter(), and nothing is written before it.
   for (int i = threadIdx.x; i < nH * r1; i += blockDim.x) u1_s[i] = __bfloat162float(U1[i]);
   if (threadIdx.x < DQ_CW / 2) {
-    cs_s[threadIdx.x] = rope ? rope_cos_sin_theta(L, freqs.theta[c0 / 2 + threadIdx.x]) : make_float2(1.f, 0.f);
+    cs_s[threadIdx.x] = rope ? rope_cos_sin_theta(pos_base + L, freqs.theta[c0 / 2 + threadIdx.x]) : make_float2(1.f, 0.f);
   }
   pdl_enter();
   // split-K sums: all of qt, this CTA's 32 key coordinates, and the value coordinates c with
@@ -178,8 +191,8 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
     if (TA_IDX_OK(err, (long)b * t3 + c, 1, (long)nB * t3)) vnew[(long)b * t3 + c] = vv;
     // shared_kv == 1 (one cache, no RoPE): the key row written below is the value row; == 2 (one cache with
     // latent RoPE): the cache holds un-rotated rows, i.e. this value row, and the rotated key is not stored
-    if (append && shared_kv != 1 && TA_IDX_OK(err, ((long)b * Lmax + L) * t3 + c, 1, (long)nB * Lmax * t3))
-      Vc[((long)b * Lmax + L) * t3 + c] = vv;   // shared cache: the key row written below is the value row
+    if (append && shared_kv != 1 && TA_IDX_OK(err, new_row * t3 + c, 1, n_rows * t3))
+      Vc[new_row * t3 + c] = vv;   // shared cache: the key row written below is the value row
   }
   __syncthreads();
   if (threadIdx.x < DQ_CW / 2) {                    // new key, rotated
@@ -189,8 +202,8 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
     const __nv_bfloat162 kv = __floats2bfloat162_rn(xe * cs.x - xo * cs.y, xe * cs.y + xo * cs.x);
     if (TA_IDX_OK(err, (long)b * r3 + c0 + 2 * i, 2, (long)nB * r3))
       *reinterpret_cast<__nv_bfloat162*>(knew + (long)b * r3 + c0 + 2 * i) = kv;
-    if (append && shared_kv != 2 && TA_IDX_OK(err, ((long)b * Lmax + L) * r3 + c0 + 2 * i, 2, (long)nB * Lmax * r3))
-      *reinterpret_cast<__nv_bfloat162*>(Kc + ((long)b * Lmax + L) * r3 + c0 + 2 * i) = kv;
+    if (append && shared_kv != 2 && TA_IDX_OK(err, new_row * r3 + c0 + 2 * i, 2, n_rows * r3))
+      *reinterpret_cast<__nv_bfloat162*>(Kc + new_row * r3 + c0 + 2 * i) = kv;
   }
   // ---- w[a, c0 + .] for batches of AB slices ----
   for (int a0 = 0; a0 < r1; a0 += AB) {
@@ -245,9 +258,16 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
     }
     xe *= mult; xo *= mult;
     const float2 cs = cs_s[cp];
-    if (TA_IDX_OK(err, ((long)b * nH + h) * r3 + c0 + 2 * cp, 2, (long)nB * nH * r3))
-      *reinterpret_cast<__nv_bfloat162*>(qhat + ((long)b * nH + h) * r3 + c0 + 2 * cp) =
-          __floats2bfloat162_rn(xe * cs.x - xo * cs.y, xe * cs.y + xo * cs.x);
+    const float qe = xe * cs.x - xo * cs.y, qo = xe * cs.y + xo * cs.x;
+    const __nv_bfloat162 hi = __floats2bfloat162_rn(qe, qo);
+    const long at = ((long)b * nH + h) * r3 + c0 + 2 * cp;
+    if (TA_IDX_OK(err, at, 2, (long)nB * nH * r3)) {
+      *reinterpret_cast<__nv_bfloat162*>(qhat + at) = hi;
+      if (qhat_lo) {
+        const float2 f = __bfloat1622float2(hi);
+        *reinterpret_cast<__nv_bfloat162*>(qhat_lo + at) = __floats2bfloat162_rn(qe - f.x, qo - f.y);
+      }
+    }
   }
 }
 
@@ -259,7 +279,8 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
 //   o_h      = merged, normalised attention output of head h             [nH][t3]
 //   u[a, :]  = sum_h Ut1[h, a] o_h                                       [t1][t3]
 //   z[j]     = sum_a sum_c Ct[a, j, c] u[a, c]                           (= sum_h Gt_h o_h)
-// z is written as bf16 [B, t2].  Dynamic shared memory: see dec_out_smem().
+// z is written as bf16 [B, t2], or with z_lo > 0 (t2 rounded up to 64) as the rounded values and the rounded rests,
+// [B, 2 z_lo] with zeros between t2 and z_lo: the output GEMM runs over both halves.  Dynamic shared memory: see dec_out_smem().
 // ---------------------------------------------------------------------------------------
 constexpr int DO_JS = 4;        // CTAs per sequence (t2 is a multiple of 32, so each gets >= 8 rows)
 
@@ -270,7 +291,7 @@ __host__ __device__ inline size_t dec_out_smem(int nH, int t1, int t3) {
 __global__ void __launch_bounds__(256)
 k_dec_out(const float* __restrict__ part_o, const float* __restrict__ part_ml, const int32_t* __restrict__ cache_len,
           int B, int Lmax, int nH, int t1, int t2, int t3, int grid_attn, const bf16* __restrict__ Ct,
-          const bf16* __restrict__ Ut1, bf16* __restrict__ z, unsigned int* err) {
+          const bf16* __restrict__ Ut1, bf16* __restrict__ z, int z_lo, unsigned int* err) {
   extern __shared__ __align__(16) float do_smem[];
   float* o_s = do_smem;                    // [32][t3]
   float* w_s = o_s + 32 * t3;              // [MAX_GRID][32]
@@ -457,10 +478,20 @@ k_dec_out(const float* __restrict__ part_o, const float* __restrict__ part_ml, c
         if (ch + off < nch) t += o;
       }
       const int jrow = jl + jj * 8 * rpl;
-      if (g < rpl && ch == 0 && jrow < jn && TA_IDX_OK(err, (long)b * t2 + jbeg + jrow, 1, (long)B * t2))
-        z[(long)b * t2 + jbeg + jrow] = __float2bfloat16_rn(t);
+      const int zp = z_lo > 0 ? 2 * z_lo : t2;           // row pitch
+      if (g < rpl && ch == 0 && jrow < jn && TA_IDX_OK(err, (long)b * zp + jbeg + jrow, 1, (long)B * zp)) {
+        const bf16 hi = __float2bfloat16_rn(t);
+        z[(long)b * zp + jbeg + jrow] = hi;
+        if (z_lo > 0) z[(long)b * zp + z_lo + jbeg + jrow] = __float2bfloat16_rn(t - __bfloat162float(hi));
+      }
     }
   }
+  if (z_lo > t2 && blockIdx.y == 0)
+    for (int j = t2 + threadIdx.x; j < z_lo; j += blockDim.x)
+      if (TA_IDX_OK(err, (long)b * 2 * z_lo + z_lo + j, 1, (long)B * 2 * z_lo)) {
+        z[(long)b * 2 * z_lo + j] = __float2bfloat16_rn(0.f);
+        z[(long)b * 2 * z_lo + z_lo + j] = __float2bfloat16_rn(0.f);
+      }
 }
 
 }  // namespace dec

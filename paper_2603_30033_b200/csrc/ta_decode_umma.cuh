@@ -30,6 +30,17 @@
 // cos / sin of n theta_i = (k0 + row) theta_i come by angle addition from the thread's own constants for `row`
 // (registers) and the tile's 64 base values for k0 (formed per tile with the angle reduced in double precision).
 //   warps 12..15  rotation warpgroup (ROT only)
+//
+// PAGED = true: the caches are pools of pages and the tensor maps are [page][row][column].  A 128-key tile is one box when a
+// page holds a multiple of 128 rows, else 128 / page_size boxes of a page each, side by side in the same shared-memory
+// tile (a box of 16 rows or more keeps the 8-row groups of the 128-byte swizzle).  The producer is then a whole warp: lane i
+// looks up page i of the tile one tile ahead and issues its boxes.  Pages that hold no cached row of the sequence are not
+// loaded: what is left of an earlier tile there is masked (keys) or zeroed (values) as rows past the length always are.
+// This form also takes the query as the sum of two bf16 numbers (the rounded value and the rounded rest, 2^-17 together):
+// a query rounded once moves every score by 2^-9 of its size, which at scores of a standard deviation of 2 was two thirds of
+// the step's whole error (4.7e-3 of the output's norm, 2.3e-3 with the second half).  The second half is eight more MMAs of
+// N = 32 per tile, hidden behind the loads.  The two halves share the room of two segments' queries, so that with r3 > 64 one
+// segment's queries are in flight instead of two.
 #pragma once
 
 #include "ta_common.cuh"
@@ -70,6 +81,8 @@ struct Params {
   float* part_o;       // [grid + B][32][t3]
   float* part_ml;      // [grid + B][32][2]  (max in log2 units, sum)
   unsigned int* err;
+  PagedView pv;        // PAGED
+  int pos_base;        // ROT: position of slot 0
 };
 
 // Walks this CTA's range of the flat tile list, sequence by sequence.
@@ -132,7 +145,7 @@ template <> struct TmemCols<8> {
   static __device__ __forceinline__ void st(uint32_t a, const uint32_t (&r)[8]) { tmem_st8(a, r); }
 };
 
-template <bool ROT, int R3C>
+template <bool ROT, int R3C, bool PAGED>
 __global__ void __launch_bounds__(ROT ? THREADS_ROT : THREADS, 1)
 k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                 const __grid_constant__ CUtensorMap tmQ, const Params p, const dec::RopeFreqs freqs) {
@@ -166,6 +179,8 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   Abort ab{&abort_flag, p.err};
   const int ksub = (p.r3 + 63) / 64, vsub = (p.t3 + 63) / 64;
+  // segments whose queries are in flight (a power of two), and its logarithm
+  const int NQ = PAGED ? (ksub == 1 ? 2 : 1) : 2, QSH = NQ >> 1;
 
   if (threadIdx.x == 0) {
     abort_flag = 0;
@@ -223,7 +238,62 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
    if (have_work && warp == 0) {
     // ------------------------------- TMA producer -------------------------------
-    if (elect_one()) {
+    if constexpr (PAGED) {
+      if (elect_one()) { tma_prefetch_desc(&tmK); tma_prefetch_desc(&tmV); tma_prefetch_desc(&tmQ); }
+      __syncwarp();
+      const int ps = p.pv.page_size;
+      const int box_rows = ps < TK ? ps : TK, n_box = TK / box_rows;
+      Walk w, wn;                                  // the tile in hand and the next one
+      w.init(p, t_begin, t_end, b0, seq_first);
+      wn.init(p, t_begin, t_end, b0, seq_first);
+      // page of box `lane` of tile t (wn is positioned on it); -1 where the box holds no cached row
+      auto lookup = [&](long t) -> int {
+        wn.seek(t);
+        const int r = wn.k0(t) + lane * box_rows;
+        return (lane < n_box && r < wn.L) ? p.pv.table[(long)wn.b * p.pv.max_pages + r / ps] : -1;
+      };
+      // what the table and cache_len hold was final before the preceding kernel began
+      int pg_next = lookup(t_begin);
+      pdl_enter();
+      int it = 0, seg = -1;
+      for (long t = t_begin; t < t_end; ++t, ++it) {
+        w.seek(t);
+        int pg = pg_next;
+        if (t + 1 < t_end) pg_next = lookup(t + 1);
+        const int row = w.k0(t) + lane * box_rows;
+        const bool mine = lane < n_box && row < w.L;
+        if (mine && (pg < 0 || pg >= p.pv.n_pages)) {
+          atomicOr(p.err, (unsigned)TA_DEVERR_BAD_PAGE);
+          pg = p.pv.n_pages;                       // outside the tensor: the box is filled with zeros
+        }
+        if (w.seg_start(t)) {
+          ++seg;
+          const int qb = seg & (NQ - 1);
+          if (!__all_sync(0xffffffffu, mbar_wait(&q_empty[qb], ((seg >> QSH) & 1) ^ 1, ab))) break;
+          if (lane == 0) {
+            mbar_expect_tx(&q_full[qb], (uint32_t)(2 * ksub * QSUB_BYTES));
+            for (int kk = 0; kk < 2 * ksub; ++kk)          // the second halves lie B nH rows behind the first
+              tma_load_2d(qbuf + (qb * 2 * ksub + kk) * QSUB_BYTES, &tmQ, &q_full[qb], (kk % ksub) * 64,
+                          w.b * p.nH + (kk < ksub ? 0 : p.B * p.nH));
+          }
+        }
+        const int s = it % STAGES;
+        if (!__all_sync(0xffffffffu, mbar_wait(&empty_bar[s], ((it / STAGES) & 1) ^ 1, ab))) break;
+        const uint32_t box_bytes = (uint32_t)box_rows * 128u;
+        const uint32_t per_page = (uint32_t)(ksub + (p.shared_kv ? 0 : vsub)) * box_bytes;
+        const uint32_t n_mine = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine));
+        if (lane == 0) mbar_expect_tx(&full_bar[s], n_mine * per_page);
+        __syncwarp();
+        if (mine) {
+          uint8_t* kt = ring + (size_t)s * stage_bytes + (size_t)lane * box_bytes;
+          uint8_t* vt = kt + MAX_SUB * SUB_BYTES;
+          const int in_page = row % ps;
+          for (int kk = 0; kk < ksub; ++kk) tma_load_3d(kt + kk * SUB_BYTES, &tmK, &full_bar[s], kk * 64, in_page, pg);
+          if (!p.shared_kv)
+            for (int kk = 0; kk < vsub; ++kk) tma_load_3d(vt + kk * SUB_BYTES, &tmV, &full_bar[s], kk * 64, in_page, pg);
+        }
+      }
+    } else if (elect_one()) {
       tma_prefetch_desc(&tmK); tma_prefetch_desc(&tmV); tma_prefetch_desc(&tmQ);
       Walk w;
       w.init(p, t_begin, t_end, b0, seq_first);
@@ -311,7 +381,7 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         const bool first = w.seg_start(t);
         if (first) {
           ++seg;
-          if (!(ok = mbar_wait(&q_full[seg & 1], (uint32_t)((seg >> 1) & 1), ab))) break;
+          if (!(ok = mbar_wait(&q_full[seg & (NQ - 1)], (uint32_t)((seg >> QSH) & 1), ab))) break;
         }
         if (ROT) {
           // the rotation warpgroup has seen the tile arrive, written its rotated copy and (last tile of a
@@ -331,7 +401,7 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         tc_fence_after();
         {
           const uint64_t dk = dk0 + stage_step * (uint64_t)st;
-          const uint64_t dq = dq0 + (uint64_t)((seg & 1) * (QBUF_BYTES >> 4));
+          const uint64_t dq = dq0 + (uint64_t)((seg & (NQ - 1)) * (PAGED ? 2 * ksub * (QSUB_BYTES >> 4) : (QBUF_BYTES >> 4)));
           const uint32_t d = tmem + (uint32_t)buf * 32u;
           const uint32_t akr = tmem + TMEM_KROT + (uint32_t)buf * 64u;    // ROT: the rotated key tile, 8 columns per K step
 #pragma unroll
@@ -341,9 +411,19 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
               if (ROT) umma_ts(d, akr + (uint32_t)ks * 8u, dqk, idesc_qk, ks != 0 ? 1u : 0u);
               else umma_ss(d, dk + (uint64_t)((ks >> 2) * (SUB_BYTES >> 4) + (ks & 3) * 2), dqk, idesc_qk, ks != 0 ? 1u : 0u);
             }
+          if constexpr (PAGED) {       // the queries' second halves
+            const uint64_t dlo = dq + (uint64_t)(ksub * (QSUB_BYTES >> 4));
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks)
+              if (ks < ksteps) {
+                const uint64_t dqk = dlo + (uint64_t)((ks >> 2) * (QSUB_BYTES >> 4) + (ks & 3) * 2);
+                if (ROT) umma_ts(d, akr + (uint32_t)ks * 8u, dqk, idesc_qk, 1u);
+                else umma_ss(d, dk + (uint64_t)((ks >> 2) * (SUB_BYTES >> 4) + (ks & 3) * 2), dqk, idesc_qk, 1u);
+              }
+          }
           umma_commit(&s_full[buf]);
           if (ROT) umma_commit(&kr_free[buf]);
-          if (w.seg_end(t)) umma_commit(&q_empty[seg & 1]);   // the segment's Qhat buffer is free once these complete
+          if (w.seg_end(t)) umma_commit(&q_empty[seg & (NQ - 1)]);   // the segment's Qhat buffer is free once these complete
         }
         {
           const uint32_t code = ((uint32_t)it << 8) | ((uint32_t)st << 4) | (first ? 1u : 0u);
@@ -401,8 +481,8 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
        // first tile of a segment they are formed with the angle reduced in double precision; from tile to tile
        // they advance by the rotation through 128 theta_i (at most 256 steps of 1e-7 each: far below bf16).
        if (w.seg_start(t)) {
-         base_lo = dec::rope_cos_sin_theta(k0, freqs.theta[lane]);
-         base_hi = (HALF > 32) ? dec::rope_cos_sin_theta(k0, freqs.theta[32 + (lane & 31)]) : make_float2(1.f, 0.f);
+         base_lo = dec::rope_cos_sin_theta(p.pos_base + k0, freqs.theta[lane]);
+         base_hi = (HALF > 32) ? dec::rope_cos_sin_theta(p.pos_base + k0, freqs.theta[32 + (lane & 31)]) : make_float2(1.f, 0.f);
        } else {
          base_lo = make_float2(base_lo.x * step_lo.x - base_lo.y * step_lo.y, base_lo.y * step_lo.x + base_lo.x * step_lo.y);
          base_hi = make_float2(base_hi.x * step_hi.x - base_hi.y * step_hi.y, base_hi.y * step_hi.x + base_hi.x * step_hi.y);

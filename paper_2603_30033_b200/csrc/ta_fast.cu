@@ -242,7 +242,8 @@ int launch_gemm(Problem& p, const bf16* A, long lda, int M, int K, const BOperan
   for (int i = 0; i < 3; ++i) {
     const BOperand& b = bops[i < nb ? i : 0];
     if (!gp.b_mn_major) {
-      if (!tmap_2d(&tmB[i], b.ptr, (uint64_t)K, (uint64_t)b.n, (uint64_t)b.ld, 64, (uint32_t)BN)) return TA_ERR_CUDA;
+      // with b_kb_wrap B has fewer columns than A (its row pitch, which is then its width)
+      if (!tmap_2d(&tmB[i], b.ptr, gp.b_kb_wrap > 0 ? (uint64_t)b.ld : (uint64_t)K, (uint64_t)b.n, (uint64_t)b.ld, 64, (uint32_t)BN)) return TA_ERR_CUDA;
     } else {
       if (!tmap_2d(&tmB[i], b.ptr, (uint64_t)b.n, (uint64_t)K, (uint64_t)b.ld, 64, 64)) return TA_ERR_CUDA;
     }
@@ -561,7 +562,10 @@ struct FastDecWs {
   float *part_o, *part_ml;
 };
 
-size_t carve_fast_dec(const tucker_attn_desc& d, char* base, FastDecWs* w) {
+// Width of one half of z in the paged step (see k_dec_out).
+int z_half(const tucker_attn_desc& d) { return (d.t2 + 63) / 64 * 64; }
+
+size_t carve_fast_dec(const tucker_attn_desc& d, bool paged, char* base, FastDecWs* w) {
   Carver c(base);
   FastDecWs t;
   const size_t Mpad = (size_t)((d.B + 127) / 128) * 128;
@@ -569,8 +573,8 @@ size_t carve_fast_dec(const tucker_attn_desc& d, char* base, FastDecWs* w) {
   t.proj_part = c.take<float>((size_t)kProjSplits * Mpad * ncol);
   t.knew = c.take<bf16>((size_t)d.B * d.r3);
   t.vnew = c.take<bf16>((size_t)d.B * d.t3);
-  t.qhat = c.take<bf16>((size_t)d.B * d.n_H * d.r3);
-  t.z = c.take<bf16>((size_t)d.B * d.t2);
+  t.qhat = c.take<bf16>((size_t)d.B * d.n_H * d.r3 * (paged ? 2 : 1));   // paged: the second halves behind the first
+  t.z = c.take<bf16>((size_t)d.B * (paged ? 2 * z_half(d) : d.t2));
   const size_t slots = (size_t)dec::MAX_GRID + d.B;
   t.part_o = c.take<float>(slots * 32 * d.t3);
   t.part_ml = c.take<float>(slots * 64);
@@ -580,38 +584,40 @@ size_t carve_fast_dec(const tucker_attn_desc& d, char* base, FastDecWs* w) {
 
 // The cache-streaming kernel (tcgen05, keys on the M dimension, ranks at run time).  With one shared cache and
 // latent RoPE (p.shared_rope) the instance with the rotation warpgroup runs: the cache holds un-rotated rows.
-template <bool ROT, int R3C>
+template <bool ROT, int R3C, bool PAGED>
 int launch_dec_attn_inst(Problem& p, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmQ,
                          const decu::Params& up, int grid, const dec::RopeFreqs& freqs) {
   static PerDeviceFlag attr;
-  TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)decu::k_dec_attn_umma<ROT, R3C>, (int)decu::SMEM_BYTES));
+  TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)decu::k_dec_attn_umma<ROT, R3C, PAGED>, (int)decu::SMEM_BYTES));
   prof_begin(p);
-  (void)launch_pdl(decu::k_dec_attn_umma<ROT, R3C>, dim3(grid), dim3(ROT ? decu::THREADS_ROT : decu::THREADS),
+  (void)launch_pdl(decu::k_dec_attn_umma<ROT, R3C, PAGED>, dim3(grid), dim3(ROT ? decu::THREADS_ROT : decu::THREADS),
                    decu::SMEM_BYTES, p.stream, tmK, tmV, tmQ, up, freqs);
   prof_end(p);
   TA_LAUNCH_CHECK(p);
   return TA_OK;
 }
 
+template <bool PAGED>
 int launch_dec_attn_umma(Problem& p, const CUtensorMap& tmK, const CUtensorMap& tmV, const dec::Params& dp, int grid) {
   const tucker_attn_desc& d = p.d;
   CUtensorMap tmQ;   // Qhat [B * n_H rows, r3]: one box = 32 rows (all heads of a sequence) x 64 columns
-  if (!tmap_2d(&tmQ, dp.qhat, (uint64_t)d.r3, (uint64_t)d.B * d.n_H, (uint64_t)d.r3, 64, 32)) return TA_ERR_CUDA;
+  if (!tmap_2d(&tmQ, dp.qhat, (uint64_t)d.r3, (uint64_t)d.B * d.n_H * (PAGED ? 2 : 1), (uint64_t)d.r3, 64, 32)) return TA_ERR_CUDA;
   decu::Params up;
   up.B = dp.B; up.nH = dp.nH; up.Lmax = dp.Lmax; up.r3 = d.r3; up.t3 = d.t3; up.shared_kv = dp.shared_kv;
   up.cache_len = dp.cache_len; up.knew = dp.knew; up.vnew = dp.vnew;
   up.part_o = dp.part_o; up.part_ml = dp.part_ml; up.err = dp.err;
+  up.pv = p.pv; up.pos_base = p.prefix_len;
   if (p.shared_rope) {
     const dec::RopeFreqs freqs = rope_freqs(d);
     switch (d.r3) {
-      case 64: return launch_dec_attn_inst<true, 64>(p, tmK, tmV, tmQ, up, grid, freqs);
-      case 96: return launch_dec_attn_inst<true, 96>(p, tmK, tmV, tmQ, up, grid, freqs);
-      case 128: return launch_dec_attn_inst<true, 128>(p, tmK, tmV, tmQ, up, grid, freqs);
+      case 64: return launch_dec_attn_inst<true, 64, PAGED>(p, tmK, tmV, tmQ, up, grid, freqs);
+      case 96: return launch_dec_attn_inst<true, 96, PAGED>(p, tmK, tmV, tmQ, up, grid, freqs);
+      case 128: return launch_dec_attn_inst<true, 128, PAGED>(p, tmK, tmV, tmQ, up, grid, freqs);
       default: return TA_ERR_UNSUPPORTED_SHAPE;
     }
   }
   dec::RopeFreqs none = {};
-  return launch_dec_attn_inst<false, 0>(p, tmK, tmV, tmQ, up, grid, none);
+  return launch_dec_attn_inst<false, 0, PAGED>(p, tmK, tmV, tmQ, up, grid, none);
 }
 
 bool dec_rank_ok(int r3, int t3) {
@@ -630,7 +636,14 @@ bool fast_decode_supported(const tucker_attn_desc& d, int32_t Lmax) {
   return true;
 }
 
-size_t fast_decode_workspace(const tucker_attn_desc& d, int32_t) { return carve_fast_dec(d, nullptr, nullptr); }
+bool fast_paged_supported(const tucker_attn_desc& d, int32_t page_size, int32_t prefix_len) {
+  if (d.dtype != TA_DTYPE_BF16 || (d.flags & TA_FLAG_FORCE_GENERIC) || prefix_len > 0) return false;
+  const bool page_ok = page_size == 16 || page_size == 32 || page_size == 64 || page_size % 128 == 0;
+  return page_ok && fast_decode_supported(d, 0);
+}
+
+size_t fast_decode_workspace(const tucker_attn_desc& d, int32_t) { return carve_fast_dec(d, false, nullptr, nullptr); }
+size_t fast_paged_workspace(const tucker_attn_desc& d) { return carve_fast_dec(d, true, nullptr, nullptr); }
 
 // Launch sequence of one decode step (Eq. 9):
 //   1  split-K GEMM   partial [qt | k | v] = x [U2 | U3 | Ut3]           (factors read in place)
@@ -642,7 +655,7 @@ size_t fast_decode_workspace(const tucker_attn_desc& d, int32_t) { return carve_
 int fast_decode(Problem& p) {
   const tucker_attn_desc& d = p.d;
   FastDecWs w;
-  carve_fast_dec(d, p.ws, &w);
+  carve_fast_dec(d, p.paged, p.ws, &w);
   const float LOG2E = 1.4426950408889634f;
   const int ncol = d.r2 + d.r3 + d.t3;
   const int Mpad = (d.B + 127) / 128 * 128;
@@ -670,7 +683,8 @@ int fast_decode(Problem& p) {
     auto launch = [&](auto kernel) {
       (void)launch_pdl(kernel, grid, dim3(256), 0, p.stream, w.proj_part, splits, (long)Mpad * ncol, d.n_H, d.r1, d.r2,
                        d.r3, d.t3, (const bf16*)p.C, (const bf16*)p.U1, p.scale * LOG2E, w.qhat, w.knew, w.vnew,
-                       (bf16*)p.Kc, (bf16*)p.Vc, p.Lmax, p.cache_len, d.rope, freqs, p.append, p.shared_rope ? 2 : p.shared_kv, p.dev_err);
+                       (bf16*)p.Kc, (bf16*)p.Vc, p.Lmax, p.cache_len, d.rope, freqs, p.append, p.shared_rope ? 2 : p.shared_kv, p.pv, p.prefix_len,
+                       p.paged ? w.qhat + (size_t)d.B * d.n_H * d.r3 : (bf16*)nullptr, p.dev_err);
     };
     switch ((d.r2 + 63) / 64) {
       case 1: launch(dec::k_dec_qhat<1>); break;
@@ -683,21 +697,24 @@ int fast_decode(Problem& p) {
   // ---- 3: attention over the latent cache ----
   {
     CUtensorMap tmK, tmV;
-    if (!tmap_3d(&tmK, p.Kc, d.r3, p.Lmax, d.B, d.r3, (uint64_t)p.Lmax * d.r3, 64, 128)) return TA_ERR_CUDA;
-    if (!tmap_3d(&tmV, p.Vc, d.t3, p.Lmax, d.B, d.t3, (uint64_t)p.Lmax * d.t3, 64, 128)) return TA_ERR_CUDA;
+    // [sequence][slot][column], or [page][row][column] with boxes that stay inside a page
+    const uint64_t rows = p.paged ? p.pv.page_size : p.Lmax, outer = p.paged ? p.pv.n_pages : d.B;
+    const uint32_t box = rows < 128 && p.paged ? (uint32_t)rows : 128u;
+    if (!tmap_3d(&tmK, p.Kc, d.r3, rows, outer, d.r3, rows * d.r3, 64, box)) return TA_ERR_CUDA;
+    if (!tmap_3d(&tmV, p.Vc, d.t3, rows, outer, d.t3, rows * d.t3, 64, box)) return TA_ERR_CUDA;
     dec::Params dp;
     dp.B = d.B; dp.nH = d.n_H; dp.Lmax = p.Lmax; dp.grid = decode_grid();
     dp.shared_kv = p.shared_kv;
     dp.cache_len = p.cache_len; dp.qhat = w.qhat; dp.knew = w.knew; dp.vnew = w.vnew;
     dp.part_o = w.part_o; dp.part_ml = w.part_ml; dp.err = p.dev_err;
-    rc = launch_dec_attn_umma(p, tmK, tmV, dp, dp.grid);
+    rc = p.paged ? launch_dec_attn_umma<true>(p, tmK, tmV, dp, dp.grid) : launch_dec_attn_umma<false>(p, tmK, tmV, dp, dp.grid);
     if (rc) return rc;
     // ---- 4: merge the partials, output-side core ----
     static PerDeviceFlag out_attr;
     TA_CUDA_TRY(ensure_dynamic_smem(out_attr, (const void*)dec::k_dec_out, (int)dec::dec_out_smem(32, 32, 128)));
     (void)launch_pdl(dec::k_dec_out, dim3(d.B, dec::DO_JS), dim3(256), dec::dec_out_smem(d.n_H, d.t1, d.t3), p.stream,
                      w.part_o, w.part_ml, p.cache_len, d.B, p.Lmax, d.n_H, d.t1, d.t2, d.t3, dp.grid, (const bf16*)p.Ct,
-                     (const bf16*)p.Ut1, w.z, p.dev_err);
+                     (const bf16*)p.Ut1, w.z, p.paged ? z_half(d) : 0, p.dev_err);
     TA_LAUNCH_CHECK(p);
   }
   // ---- 5: y = z Ut2^T ----
@@ -708,7 +725,9 @@ int fast_decode(Problem& p) {
     gp.seg[0] = seg(0, d.d_model, umma_gemm::EP_BF16, p.Y, d.d_model);
     const BOperand bop = {(const bf16*)p.Ut2, d.t2, d.d_model};
     gp.early = 2;   // the factor Ut2 is an input of the call; z comes from the preceding kernel
-    if ((rc = launch_gemm(p, w.z, d.t2, d.B, d.t2, &bop, 1, d.d_model, pick_bn(d.d_model), gp))) return rc;
+    const int zk = p.paged ? 2 * z_half(d) : d.t2;      // paged: both halves of z against the same factor
+    gp.b_kb_wrap = p.paged ? z_half(d) / 64 : 0;
+    if ((rc = launch_gemm(p, w.z, zk, d.B, zk, &bop, 1, d.d_model, pick_bn(d.d_model), gp))) return rc;
   }
   return TA_OK;
 }

@@ -63,6 +63,7 @@ struct Params {
                            // preceding kernel started, only the epilogue (tables, outputs) waits; 2: B only
   int kb_per_split;        // split-K: 64-wide K blocks per blockIdx.z (0 = no split); EP_F32 outputs only
   long split_stride;       // elements between the partial outputs of consecutive splits
+  int b_kb_wrap;           // > 0: the K blocks of B repeat after this many (A = [hi | lo] halves of the same columns)
   unsigned int* err;
 };
 
@@ -133,7 +134,7 @@ k_umma_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
       tma_prefetch_desc(bmap_of(seg_of(0)));
       auto load_b = [&](int kb) {
         const int s = kb % STAGES;
-        const int kx = (kb_begin + kb) * BK;
+        const int kx = (p.b_kb_wrap > 0 ? (kb_begin + kb) % p.b_kb_wrap : kb_begin + kb) * BK;
         for (int cb = 0; cb < ncb; ++cb) {
           const int si = seg_of(cb);
           const int bn0 = n0 + cb * p.BN - p.seg[si].n_begin + p.seg[si].b_n_off;

@@ -29,6 +29,15 @@ def workload(shape, dtype, rope=True, shared=False, seed=91, **kw):
     return H.custom_workload(kind="decode", dtype=dtype, rope=rope, rope_base=500000.0, shared_kv=shared, seed=seed, **{**shape, **kw})
 
 
+def expected_path(st, flags=0):
+    """2 (tensor-core kernels) for the bf16 shapes of the contiguous tensor-core decode step with pages of 16, 32, 64 or a
+    multiple of 128 rows, else 1."""
+    w = st.w
+    ranks = (w.r[2], w.t[2]) in [(128, 128), (64, 64), (96, 96), (128, 64), (64, 128)] and w.r[1] % 32 == 0 and w.t[1] % 32 == 0
+    tc = w.dtype == "bf16" and ranks and w.d_model % 64 == 0 and (st.page in (16, 32, 64) or st.page % 128 == 0)
+    return 2 if tc and not flags & Bd.TA_FLAG_FORCE_GENERIC else 1
+
+
 def run_step(st, append=True, flags=0, prefix_call=None, **kw):
     x, dw, K, V, table, lens, ptab = st.device()
     w = st.w
@@ -37,6 +46,7 @@ def run_step(st, append=True, flags=0, prefix_call=None, **kw):
         y = Bd.tucker_attn_decode_prefix(x, *dw, K, V, table, lens, ptab if st.P else None, st.P, **args)
     else:
         y = Bd.tucker_attn_decode_paged(x, *dw, K, V, table, lens, **args)
+        assert Bd.last_path() == expected_path(st, flags)
     assert Bd.last_device_error() == 0
     return y, K, V
 
