@@ -166,7 +166,7 @@ int tucker_attn_decode(const tucker_attn_desc* desc, const void* x, const void* 
 
 static size_t paged_decode_need(const tucker_attn_desc& d, const tucker_paged_cache& c, int32_t prefix_len) {
   if (!paged_batch_ok(d)) return 0;
-  if (fast_paged_supported(d, c.page_size, prefix_len)) return fast_paged_workspace(d);
+  if (fast_paged_supported(d, c.page_size)) return fast_paged_workspace(d, prefix_len, c.K == c.V);
   return generic_paged_decode_workspace(d, paged_slots(c), prefix_len);
 }
 
@@ -213,7 +213,7 @@ int tucker_attn_decode_prefix(const tucker_attn_desc* desc, const void* x, const
   p.dev_err = device_error_ptr();
   p.prof_start = tl_prof_start; p.prof_stop = tl_prof_stop;
   if (!p.dev_err) return TA_ERR_CUDA;
-  const bool fast = fast_paged_supported(*desc, cache->page_size, prefix_len);
+  const bool fast = fast_paged_supported(*desc, cache->page_size);
   const int rc = fast ? fast_decode(p) : generic_paged_decode(p);
   tl_last_path = fast ? 2 : 1;
   tl_last_launches = p.launches;

@@ -83,8 +83,8 @@ size_t fast_fwd_workspace(const tucker_attn_desc& d);
 int fast_fwd(Problem& p);
 bool fast_decode_supported(const tucker_attn_desc& d, int32_t Lmax);
 // the same step over a paged cache (p.paged), behind a prefix of prefix_len shared tokens
-bool fast_paged_supported(const tucker_attn_desc& d, int32_t page_size, int32_t prefix_len);
-size_t fast_paged_workspace(const tucker_attn_desc& d);
+bool fast_paged_supported(const tucker_attn_desc& d, int32_t page_size);
+size_t fast_paged_workspace(const tucker_attn_desc& d, int32_t prefix_len, bool one_pool);
 size_t fast_decode_workspace(const tucker_attn_desc& d, int32_t Lmax);
 int fast_decode(Problem& p);
 int wait_selftest(unsigned int* dev_err, int budget_us, int* out_dev, cudaStream_t stream);

@@ -279,8 +279,7 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
 //   o_h      = merged, normalised attention output of head h             [nH][t3]
 //   u[a, :]  = sum_h Ut1[h, a] o_h                                       [t1][t3]
 //   z[j]     = sum_a sum_c Ct[a, j, c] u[a, c]                           (= sum_h Gt_h o_h)
-// z is written as bf16 [B, t2], or with z_lo > 0 (t2 rounded up to 64) as the rounded values and the rounded rests,
-// [B, 2 z_lo] with zeros between t2 and z_lo: the output GEMM runs over both halves.  Dynamic shared memory: see dec_out_smem().
+// z is written as bf16 [B, t2].  Dynamic shared memory: see dec_out_smem().
 // ---------------------------------------------------------------------------------------
 constexpr int DO_JS = 4;        // CTAs per sequence (t2 is a multiple of 32, so each gets >= 8 rows)
 
@@ -291,7 +290,7 @@ __host__ __device__ inline size_t dec_out_smem(int nH, int t1, int t3) {
 __global__ void __launch_bounds__(256)
 k_dec_out(const float* __restrict__ part_o, const float* __restrict__ part_ml, const int32_t* __restrict__ cache_len,
           int B, int Lmax, int nH, int t1, int t2, int t3, int grid_attn, const bf16* __restrict__ Ct,
-          const bf16* __restrict__ Ut1, bf16* __restrict__ z, int z_lo, unsigned int* err) {
+          const bf16* __restrict__ Ut1, bf16* __restrict__ z, unsigned int* err) {
   extern __shared__ __align__(16) float do_smem[];
   float* o_s = do_smem;                    // [32][t3]
   float* w_s = o_s + 32 * t3;              // [MAX_GRID][32]
@@ -478,20 +477,10 @@ k_dec_out(const float* __restrict__ part_o, const float* __restrict__ part_ml, c
         if (ch + off < nch) t += o;
       }
       const int jrow = jl + jj * 8 * rpl;
-      const int zp = z_lo > 0 ? 2 * z_lo : t2;           // row pitch
-      if (g < rpl && ch == 0 && jrow < jn && TA_IDX_OK(err, (long)b * zp + jbeg + jrow, 1, (long)B * zp)) {
-        const bf16 hi = __float2bfloat16_rn(t);
-        z[(long)b * zp + jbeg + jrow] = hi;
-        if (z_lo > 0) z[(long)b * zp + z_lo + jbeg + jrow] = __float2bfloat16_rn(t - __bfloat162float(hi));
-      }
+      if (g < rpl && ch == 0 && jrow < jn && TA_IDX_OK(err, (long)b * t2 + jbeg + jrow, 1, (long)B * t2))
+        z[(long)b * t2 + jbeg + jrow] = __float2bfloat16_rn(t);
     }
   }
-  if (z_lo > t2 && blockIdx.y == 0)
-    for (int j = t2 + threadIdx.x; j < z_lo; j += blockDim.x)
-      if (TA_IDX_OK(err, (long)b * 2 * z_lo + z_lo + j, 1, (long)B * 2 * z_lo)) {
-        z[(long)b * 2 * z_lo + j] = __float2bfloat16_rn(0.f);
-        z[(long)b * 2 * z_lo + z_lo + j] = __float2bfloat16_rn(0.f);
-      }
 }
 
 }  // namespace dec

@@ -219,8 +219,10 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
   int lo, hi;
   long excl;
   const long total = dec::block_tile_scan(p.cache_len, p.B, p.Lmax, lo, hi, excl, wtot_s);
-  const long t_begin = dec::cta_first_tile(blockIdx.x, total, gridDim.x);
-  const long t_end = dec::cta_first_tile(blockIdx.x + 1, total, gridDim.x);
+  // PAGED: with fewer tiles than CTAs the first `total` CTAs take one each, so that the CTAs of a sequence are neighbours
+  const long parts = PAGED ? min((long)gridDim.x, total) : (long)gridDim.x;
+  const long t_begin = min(dec::cta_first_tile(blockIdx.x, total, parts), total);
+  const long t_end = min(dec::cta_first_tile(blockIdx.x + 1, total, parts), total);
   {
     long f = excl;
     for (int b = lo; b < hi; ++b) {

@@ -13,6 +13,8 @@
 #include "ta_attn_prefill.cuh"
 #include "ta_decode.cuh"
 #include "ta_decode_umma.cuh"
+#include "ta_paged_out.cuh"
+#include "ta_prefix_attn.cuh"
 #include "ta_zy_fused.cuh"
 
 #include <math.h>
@@ -560,12 +562,26 @@ struct FastDecWs {
   bf16* qhat;         // [B][n_H][r3] rotated, scaled per-head queries
   bf16* z;            // [B][t2]
   float *part_o, *part_ml;
+  float *pre_o, *pre_ml;   // partials of the shared prefix
+  bf16* pre_k;             // one pool with latent RoPE: the prefix's keys, rotated (rows padded to whole tiles)
 };
 
 // Width of one half of z in the paged step (see k_dec_out).
 int z_half(const tucker_attn_desc& d) { return (d.t2 + 63) / 64 * 64; }
 
-size_t carve_fast_dec(const tucker_attn_desc& d, bool paged, char* base, FastDecWs* w) {
+// Units of work, CTAs and partial slots of the prefix kernel.
+struct PrefixPlan {
+  int n_kt, n_rb, grid;
+};
+PrefixPlan prefix_plan(const tucker_attn_desc& d, int32_t P) {
+  PrefixPlan q;
+  q.n_kt = (P + prefix::TK - 1) / prefix::TK;
+  q.n_rb = (int)(((long)d.B * d.n_H + prefix::RB - 1) / prefix::RB);
+  q.grid = (int)std::min<long>(decode_grid(), (long)q.n_kt * q.n_rb);
+  return q;
+}
+
+size_t carve_fast_dec(const tucker_attn_desc& d, bool paged, int32_t prefix_len, bool rotated, char* base, FastDecWs* w) {
   Carver c(base);
   FastDecWs t;
   const size_t Mpad = (size_t)((d.B + 127) / 128) * 128;
@@ -578,6 +594,15 @@ size_t carve_fast_dec(const tucker_attn_desc& d, bool paged, char* base, FastDec
   const size_t slots = (size_t)dec::MAX_GRID + d.B;
   t.part_o = c.take<float>(slots * 32 * d.t3);
   t.part_ml = c.take<float>(slots * 64);
+  t.pre_o = t.pre_ml = nullptr;
+  t.pre_k = nullptr;
+  if (prefix_len > 0) {
+    const PrefixPlan q = prefix_plan(d, prefix_len);
+    const size_t rows = (size_t)(dec::MAX_GRID + q.n_rb) * prefix::RB;
+    t.pre_o = c.take<float>(rows * d.t3);
+    t.pre_ml = c.take<float>(rows * 2);
+    t.pre_k = c.take<bf16>(rotated ? (size_t)q.n_kt * prefix::TK * d.r3 : 0);
+  }
   if (w) *w = t;
   return c.off;
 }
@@ -620,6 +645,53 @@ int launch_dec_attn_umma(Problem& p, const CUtensorMap& tmK, const CUtensorMap& 
   return launch_dec_attn_inst<false, 0, PAGED>(p, tmK, tmV, tmQ, up, grid, none);
 }
 
+// The pools of a paged cache as [page][row][column], boxes of at most 128 rows that stay inside a page.
+bool tmap_pages(CUtensorMap* m, const void* pool, int r, int n_pages, int page_size) {
+  return tmap_3d(m, pool, r, page_size, n_pages, r, (uint64_t)page_size * r, 64, (uint32_t)std::min(page_size, 128));
+}
+
+int launch_prefix(Problem& p, const FastDecWs& w, const PrefixPlan& q) {
+  const tucker_attn_desc& d = p.d;
+  prefix::Params pp;
+  pp.R = d.B * d.n_H; pp.P = p.prefix_len; pp.r3 = d.r3; pp.t3 = d.t3; pp.n_kt = q.n_kt; pp.n_rb = q.n_rb;
+  pp.v = prefix::Rows{p.prefix_table, p.pv.n_pages, p.pv.page_size};
+  pp.k = pp.v;
+  pp.part_o = w.pre_o; pp.part_ml = w.pre_ml; pp.err = p.dev_err;
+  const void* keys = p.Kc;
+  if (p.shared_rope) {
+    const long n = (long)p.prefix_len * (d.r3 / 8);
+    (void)launch_pdl(prefix::k_prefix_rotate, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, p.stream, (const bf16*)p.Kc, pp.v,
+                     w.pre_k, p.prefix_len, d.r3, rope_freqs(d), p.dev_err);
+    TA_LAUNCH_CHECK(p);
+    keys = w.pre_k;
+    pp.k = prefix::Rows{nullptr, q.n_kt, prefix::TK};
+  }
+  CUtensorMap tmQ, tmK, tmV;
+  if (!tmap_2d(&tmQ, w.qhat, (uint64_t)d.r3, (uint64_t)2 * pp.R, (uint64_t)d.r3, 64, prefix::TQ)) return TA_ERR_CUDA;
+  if (!tmap_pages(&tmK, keys, d.r3, pp.k.n_pages, pp.k.page_size)) return TA_ERR_CUDA;
+  if (!tmap_pages(&tmV, p.Vc, d.t3, pp.v.n_pages, pp.v.page_size)) return TA_ERR_CUDA;
+  static PerDeviceFlag attr;
+  TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)prefix::k_prefix_attn, (int)prefix::SMEM_BYTES));
+  (void)launch_pdl(prefix::k_prefix_attn, dim3(q.grid), dim3(prefix::THREADS), prefix::SMEM_BYTES, p.stream, tmQ, tmK, tmV, pp);
+  TA_LAUNCH_CHECK(p);
+  return TA_OK;
+}
+
+int launch_paged_out(Problem& p, const FastDecWs& w, const PrefixPlan& q, int grid) {
+  const tucker_attn_desc& d = p.d;
+  pgout::Params op;
+  op.B = d.B; op.nH = d.n_H; op.Lmax = p.Lmax; op.t1 = d.t1; op.t2 = d.t2; op.t3 = d.t3; op.z_half = z_half(d);
+  op.cache_len = p.cache_len; op.part_o = w.part_o; op.part_ml = w.part_ml; op.grid = grid;
+  op.pre_o = w.pre_o; op.pre_ml = w.pre_ml; op.grid_p = q.grid; op.n_kt = q.n_kt; op.n_rb = q.n_rb;
+  op.Ct = (const bf16*)p.Ct; op.Ut1 = (const bf16*)p.Ut1; op.z = w.z; op.err = p.dev_err;
+  static PerDeviceFlag attr;
+  TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)pgout::k_pg_out, (int)pgout::smem_bytes(32, 128, 32, true)));
+  (void)launch_pdl(pgout::k_pg_out, dim3((unsigned)d.B * pgout::CL), dim3(pgout::THREADS),
+                   pgout::smem_bytes(d.t1, d.t3, d.n_H, q.n_rb > 0), p.stream, op);
+  TA_LAUNCH_CHECK(p);
+  return TA_OK;
+}
+
 bool dec_rank_ok(int r3, int t3) {
   return (r3 == 128 && t3 == 128) || (r3 == 64 && t3 == 64) || (r3 == 96 && t3 == 96) || (r3 == 128 && t3 == 64) ||
          (r3 == 64 && t3 == 128);
@@ -636,14 +708,16 @@ bool fast_decode_supported(const tucker_attn_desc& d, int32_t Lmax) {
   return true;
 }
 
-bool fast_paged_supported(const tucker_attn_desc& d, int32_t page_size, int32_t prefix_len) {
-  if (d.dtype != TA_DTYPE_BF16 || (d.flags & TA_FLAG_FORCE_GENERIC) || prefix_len > 0) return false;
+bool fast_paged_supported(const tucker_attn_desc& d, int32_t page_size) {
+  if (d.dtype != TA_DTYPE_BF16 || (d.flags & TA_FLAG_FORCE_GENERIC)) return false;
   const bool page_ok = page_size == 16 || page_size == 32 || page_size == 64 || page_size % 128 == 0;
   return page_ok && fast_decode_supported(d, 0);
 }
 
-size_t fast_decode_workspace(const tucker_attn_desc& d, int32_t) { return carve_fast_dec(d, false, nullptr, nullptr); }
-size_t fast_paged_workspace(const tucker_attn_desc& d) { return carve_fast_dec(d, true, nullptr, nullptr); }
+size_t fast_decode_workspace(const tucker_attn_desc& d, int32_t) { return carve_fast_dec(d, false, 0, false, nullptr, nullptr); }
+size_t fast_paged_workspace(const tucker_attn_desc& d, int32_t prefix_len, bool one_pool) {
+  return carve_fast_dec(d, true, prefix_len, one_pool && d.rope, nullptr, nullptr);
+}
 
 // Launch sequence of one decode step (Eq. 9):
 //   1  split-K GEMM   partial [qt | k | v] = x [U2 | U3 | Ut3]           (factors read in place)
@@ -655,7 +729,7 @@ size_t fast_paged_workspace(const tucker_attn_desc& d) { return carve_fast_dec(d
 int fast_decode(Problem& p) {
   const tucker_attn_desc& d = p.d;
   FastDecWs w;
-  carve_fast_dec(d, p.paged, p.ws, &w);
+  carve_fast_dec(d, p.paged, p.prefix_len, p.shared_rope, p.ws, &w);
   const float LOG2E = 1.4426950408889634f;
   const int ncol = d.r2 + d.r3 + d.t3;
   const int Mpad = (d.B + 127) / 128 * 128;
@@ -694,14 +768,19 @@ int fast_decode(Problem& p) {
     }
     TA_LAUNCH_CHECK(p);
   }
+  // ---- 2b: attention of all rows to the shared prefix ----
+  const PrefixPlan pq = p.prefix_len > 0 ? prefix_plan(d, p.prefix_len) : PrefixPlan{0, 0, 0};
+  if (p.prefix_len > 0 && (rc = launch_prefix(p, w, pq))) return rc;
   // ---- 3: attention over the latent cache ----
   {
     CUtensorMap tmK, tmV;
-    // [sequence][slot][column], or [page][row][column] with boxes that stay inside a page
-    const uint64_t rows = p.paged ? p.pv.page_size : p.Lmax, outer = p.paged ? p.pv.n_pages : d.B;
-    const uint32_t box = rows < 128 && p.paged ? (uint32_t)rows : 128u;
-    if (!tmap_3d(&tmK, p.Kc, d.r3, rows, outer, d.r3, rows * d.r3, 64, box)) return TA_ERR_CUDA;
-    if (!tmap_3d(&tmV, p.Vc, d.t3, rows, outer, d.t3, rows * d.t3, 64, box)) return TA_ERR_CUDA;
+    if (p.paged) {
+      if (!tmap_pages(&tmK, p.Kc, d.r3, p.pv.n_pages, p.pv.page_size)) return TA_ERR_CUDA;
+      if (!tmap_pages(&tmV, p.Vc, d.t3, p.pv.n_pages, p.pv.page_size)) return TA_ERR_CUDA;
+    } else {
+      if (!tmap_3d(&tmK, p.Kc, d.r3, p.Lmax, d.B, d.r3, (uint64_t)p.Lmax * d.r3, 64, 128)) return TA_ERR_CUDA;
+      if (!tmap_3d(&tmV, p.Vc, d.t3, p.Lmax, d.B, d.t3, (uint64_t)p.Lmax * d.t3, 64, 128)) return TA_ERR_CUDA;
+    }
     dec::Params dp;
     dp.B = d.B; dp.nH = d.n_H; dp.Lmax = p.Lmax; dp.grid = decode_grid();
     dp.shared_kv = p.shared_kv;
@@ -710,12 +789,16 @@ int fast_decode(Problem& p) {
     rc = p.paged ? launch_dec_attn_umma<true>(p, tmK, tmV, dp, dp.grid) : launch_dec_attn_umma<false>(p, tmK, tmV, dp, dp.grid);
     if (rc) return rc;
     // ---- 4: merge the partials, output-side core ----
-    static PerDeviceFlag out_attr;
-    TA_CUDA_TRY(ensure_dynamic_smem(out_attr, (const void*)dec::k_dec_out, (int)dec::dec_out_smem(32, 32, 128)));
-    (void)launch_pdl(dec::k_dec_out, dim3(d.B, dec::DO_JS), dim3(256), dec::dec_out_smem(d.n_H, d.t1, d.t3), p.stream,
-                     w.part_o, w.part_ml, p.cache_len, d.B, p.Lmax, d.n_H, d.t1, d.t2, d.t3, dp.grid, (const bf16*)p.Ct,
-                     (const bf16*)p.Ut1, w.z, p.paged ? z_half(d) : 0, p.dev_err);
-    TA_LAUNCH_CHECK(p);
+    if (p.paged) {
+      if ((rc = launch_paged_out(p, w, pq, dp.grid))) return rc;
+    } else {
+      static PerDeviceFlag out_attr;
+      TA_CUDA_TRY(ensure_dynamic_smem(out_attr, (const void*)dec::k_dec_out, (int)dec::dec_out_smem(32, 32, 128)));
+      (void)launch_pdl(dec::k_dec_out, dim3(d.B, dec::DO_JS), dim3(256), dec::dec_out_smem(d.n_H, d.t1, d.t3), p.stream,
+                       w.part_o, w.part_ml, p.cache_len, d.B, p.Lmax, d.n_H, d.t1, d.t2, d.t3, dp.grid, (const bf16*)p.Ct,
+                       (const bf16*)p.Ut1, w.z, p.dev_err);
+      TA_LAUNCH_CHECK(p);
+    }
   }
   // ---- 5: y = z Ut2^T ----
   {

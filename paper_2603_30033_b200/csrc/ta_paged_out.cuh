@@ -1,0 +1,238 @@
+// Output side of the paged decode step: joins the partials of a sequence -- those of its own keys (streaming kernel) and of
+// the shared prefix (prefix kernel) -- by their maxima and sums and applies the output-side core:
+//   o_h = merged, normalised output of head h;  u[a, :] = sum_h Ut1[h, a] o_h;  z[j] = sum_a sum_c Ct[a, j, c] u[a, c]
+// A cluster of CL CTAs per sequence.  CTA y merges t3 / CL value columns of all heads (every partial is read once per
+// sequence, where CTAs that split the rows of z would each have to merge everything), forms its columns of u, hands them to the
+// other CTAs through distributed shared memory, and computes t2 / CL rows of z.  One user with a long cache has a partial
+// from every SM: the maxima, weights and sums of the partials are spread over all warps instead of walked by one.
+#pragma once
+
+#include "ta_common.cuh"
+#include "ta_decode.cuh"
+#include "ta_prefix_attn.cuh"
+
+namespace ta {
+namespace pgout {
+
+constexpr int CL = 8;
+constexpr int THREADS = 512, WARPS = THREADS / 32;
+constexpr int MAX_PART = 2 * dec::MAX_GRID;      // partials of one head: one per CTA of either attention kernel at most
+constexpr int MAX_COLS = 128 / CL;
+
+struct Params {
+  int B, nH, Lmax, t1, t2, t3, z_half;
+  const int32_t* cache_len;
+  const float *part_o, *part_ml;                 // own keys: [grid + B][32][t3], [grid + B][32][2]
+  int grid;
+  const float *pre_o, *pre_ml;                   // prefix: [grid_p + n_rb][RB][t3], [..][RB][2]
+  int grid_p, n_kt, n_rb;                        // n_rb = 0: no prefix
+  const bf16 *Ct, *Ut1;
+  bf16* z;                                       // [B, 2 z_half]: rounded values, rounded rests
+  unsigned int* err;
+};
+
+__host__ __device__ inline size_t smem_bytes(int t1, int t3, int nH, bool with_prefix) {
+  const int parts = with_prefix ? MAX_PART : dec::MAX_GRID;
+  return sizeof(float) * ((size_t)parts * 32 + (size_t)t1 * t3 + (size_t)nH * t1 + (size_t)THREADS * 4 + 32 * MAX_COLS);
+}
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void st_cluster(float* own, uint32_t rank, float v) {      // `own`'s counterpart in CTA `rank`
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(sm100::smem_u32(own)), "r"(rank));
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory");
+}
+
+__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS) k_pg_out(const Params p) {
+  extern __shared__ __align__(16) float sm[];
+  const int t3 = p.t3, cw = t3 / CL, q4 = cw / 4;          // columns of this CTA: 8, 12 or 16, as float4
+  float4* red_s = reinterpret_cast<float4*>(sm);           // [THREADS]
+  float* o_s = sm + THREADS * 4;                           // [32][MAX_COLS]
+  float* u_s = o_s + 32 * MAX_COLS;                        // [t1][t3]
+  float* ut1_s = u_s + p.t1 * t3;                          // [nH][t1]
+  float* w_s = ut1_s + p.nH * p.t1;                        // [partials][32]
+  __shared__ long long wtot_s[WARPS];
+  __shared__ long long first_s;
+  __shared__ float hm_s[WARPS][32], hl_s[WARPS][32];
+  const int b = blockIdx.x / CL, y = blockIdx.x % CL, c0 = y * cw;
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const int jn = p.t2 / CL, jbeg = y * jn;
+  cluster_arrive();                                        // "this CTA has started": waited for before the first remote store
+  {
+    // this CTA's rows of the output core towards L2 while the merge runs
+    const char* cbase = reinterpret_cast<const char*>(p.Ct);
+    const long row_bytes = (long)t3 * 2, span = (long)jn * row_bytes;
+    const int lines = (int)((span + 127) / 128);
+    for (int i = tid; i < p.t1 * lines; i += THREADS)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(cbase + ((long)(i / lines) * p.t2 + jbeg) * row_bytes + (long)(i % lines) * 128));
+  }
+  for (int i = tid; i < p.nH * p.t1; i += THREADS) ut1_s[i] = __bfloat162float(p.Ut1[i]);
+  int lo, hi;
+  long excl;
+  const long total = dec::block_tile_scan(p.cache_len, p.B, p.Lmax, lo, hi, excl, wtot_s);
+  if (b >= lo && b < hi) {
+    long f = excl;
+    for (int i = lo; i < b; ++i) f += dec::tiles_of(dec::clamp_len(p.cache_len[i], p.Lmax));
+    first_s = f;
+  }
+  __syncthreads();
+  const long first = (long)first_s;
+  const long nt = dec::tiles_of(dec::clamp_len(p.cache_len[b], p.Lmax));
+  const long eff = min((long)p.grid, total);               // the streaming kernel's CTAs that have tiles
+  const long i0 = prefix::owner_of(first, total, eff), i1 = prefix::owner_of(first + nt - 1, total, eff);
+  int np = (int)(i1 - i0 + 1);
+  if (!TA_IDX_OK(p.err, i0 + b, np, (long)p.grid + p.B)) np = 0;
+  // The prefix's partials of head h: rows of a sequence may lie in two (or, never here, more) row blocks.
+  auto pre_range = [&](int h, long& slot0, int& cnt, int& rloc) {
+    slot0 = 0; cnt = 0; rloc = 0;
+    if (p.n_rb == 0 || h >= p.nH) return;
+    const int row = b * p.nH + h, rb = row / prefix::RB;
+    rloc = row % prefix::RB;
+    const long tot = (long)p.n_rb * p.n_kt, f = (long)rb * p.n_kt;
+    const long a = prefix::owner_of(f, tot, p.grid_p), e = prefix::owner_of(f + p.n_kt - 1, tot, p.grid_p);
+    slot0 = a + rb;
+    cnt = (int)(e - a + 1);
+    if (!TA_IDX_OK(p.err, slot0, cnt, (long)p.grid_p + p.n_rb)) cnt = 0;
+  };
+  // Up to here only inputs of the call were read; the partials come from the kernels before this one.
+  pdl_enter();
+  // ---- weights: warp w takes the partials w, w + WARPS, ... of all heads (lane = head) ----
+  {
+    const int h = lane;
+    long ps0;
+    int pc, prl;
+    pre_range(h, ps0, pc, prl);
+    const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + (i0 + b) * 32 + h;
+    const float2* pml = reinterpret_cast<const float2*>(p.pre_ml) + ps0 * prefix::RB + prl;
+    float m = -INFINITY;
+    for (int k = warp; k < np; k += WARPS) m = fmaxf(m, ml[(long)k * 32].x);
+    for (int k = warp; k < pc; k += WARPS) m = fmaxf(m, pml[(long)k * prefix::RB].x);
+    hm_s[warp][h] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) m = fmaxf(m, hm_s[w][h]);      // finite: a sequence's own part holds the new token
+    float l = 0.f;
+    for (int k = warp; k < np; k += WARPS) {
+      const float2 v = ml[(long)k * 32];
+      const float e = dec::ex2(v.x - m);
+      w_s[k * 32 + h] = e;
+      l = fmaf(v.y, e, l);
+    }
+    for (int k = warp; k < pc; k += WARPS) {
+      const float2 v = pml[(long)k * prefix::RB];
+      const float e = dec::ex2(v.x - m);
+      w_s[(np + k) * 32 + h] = e;
+      l = fmaf(v.y, e, l);
+    }
+    hl_s[warp][h] = l;
+  }
+  __syncthreads();
+  // ---- merge: item = (head, four columns), the partials dealt over the groups of threads ----
+  const int items = p.nH * q4, groups = min(16, THREADS / items);
+  {
+    const int g = tid / items, it = tid % items, h = it / q4, c = c0 + (it % q4) * 4;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (g < groups) {
+      long ps0;
+      int pc, prl;
+      pre_range(h, ps0, pc, prl);
+      const float* po = p.part_o + ((i0 + b) * 32 + h) * t3 + c;
+      const float* pp = p.pre_o + (ps0 * prefix::RB + prl) * t3 + c;
+      auto add = [&](const float* src, long stride, int n, int w0) {
+        for (int k0 = g; k0 < n; k0 += 4 * groups) {
+          float4 v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int k = k0 + e * groups;
+            v[e] = k < n ? *reinterpret_cast<const float4*>(src + (long)k * stride) : make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int k = k0 + e * groups;
+            const float wt = k < n ? w_s[(w0 + k) * 32 + h] : 0.f;
+            acc.x = fmaf(wt, v[e].x, acc.x); acc.y = fmaf(wt, v[e].y, acc.y);
+            acc.z = fmaf(wt, v[e].z, acc.z); acc.w = fmaf(wt, v[e].w, acc.w);
+          }
+        }
+      };
+      add(po, 32L * t3, np, 0);
+      add(pp, (long)prefix::RB * t3, pc, np);
+    }
+    red_s[tid] = acc;
+  }
+  __syncthreads();
+  if (tid < items) {
+    const int h = tid / q4;
+    float4 s = red_s[tid];
+    for (int g = 1; g < groups; ++g) {
+      const float4 v = red_s[g * items + tid];
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    float l = 0.f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) l += hl_s[w][h];
+    const float inv = 1.f / l;
+    *reinterpret_cast<float4*>(o_s + h * MAX_COLS + (tid % q4) * 4) = make_float4(s.x * inv, s.y * inv, s.z * inv, s.w * inv);
+  }
+  __syncthreads();
+  cluster_wait();
+  // ---- this CTA's columns of u, to every CTA of the cluster ----
+  for (int i = tid; i < p.t1 * cw; i += THREADS) {
+    const int a = i / cw, c = i % cw;
+    float acc = 0.f;
+    for (int h = 0; h < p.nH; ++h) acc = fmaf(ut1_s[h * p.t1 + a], o_s[h * MAX_COLS + c], acc);
+#pragma unroll
+    for (int r = 0; r < CL; ++r) st_cluster(&u_s[a * t3 + c0 + c], r, acc);
+  }
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  // ---- z: a warp per row; lane = (slice a of rpl, 16-byte chunk) ----
+  const int nch = t3 / 8, rpl = 32 / nch;                  // 8, 12 or 16 chunks; 4, 2 or 2 slices at a time
+  const int ga = lane / nch, ch = lane % nch;
+  const uint4* Cq = reinterpret_cast<const uint4*>(p.Ct);
+  for (int jl = warp; jl < jn; jl += WARPS) {
+    const int j = jbeg + jl;
+    float acc = 0.f;
+    for (int a0 = 0; a0 < p.t1; a0 += 4 * rpl) {
+      uint4 v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int a = a0 + e * rpl + ga;
+        v[e] = (ga < rpl && a < p.t1) ? Cq[((long)a * p.t2 + j) * nch + ch] : make_uint4(0u, 0u, 0u, 0u);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int a = a0 + e * rpl + ga;
+        if (ga < rpl && a < p.t1) {
+          const float4 u0 = reinterpret_cast<const float4*>(u_s + a * t3 + ch * 8)[0];
+          const float4 u1 = reinterpret_cast<const float4*>(u_s + a * t3 + ch * 8)[1];
+          const uint32_t wv[4] = {v[e].x, v[e].y, v[e].z, v[e].w};
+          const float2 k0 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[0]));
+          const float2 k1 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[1]));
+          const float2 k2 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[2]));
+          const float2 k3 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[3]));
+          acc = fmaf(u0.x, k0.x, acc); acc = fmaf(u0.y, k0.y, acc); acc = fmaf(u0.z, k1.x, acc); acc = fmaf(u0.w, k1.y, acc);
+          acc = fmaf(u1.x, k2.x, acc); acc = fmaf(u1.y, k2.y, acc); acc = fmaf(u1.z, k3.x, acc); acc = fmaf(u1.w, k3.y, acc);
+        }
+      }
+    }
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
+    if (lane == 0 && TA_IDX_OK(p.err, (long)b * 2 * p.z_half + p.z_half + j, 1, (long)p.B * 2 * p.z_half)) {
+      const bf16 zh = __float2bfloat16_rn(acc);
+      p.z[(long)b * 2 * p.z_half + j] = zh;
+      p.z[(long)b * 2 * p.z_half + p.z_half + j] = __float2bfloat16_rn(acc - __bfloat162float(zh));
+    }
+  }
+  if (y == 0)
+    for (int j = p.t2 + tid; j < p.z_half; j += THREADS)
+      if (TA_IDX_OK(p.err, (long)b * 2 * p.z_half + p.z_half + j, 1, (long)p.B * 2 * p.z_half)) {
+        p.z[(long)b * 2 * p.z_half + j] = __float2bfloat16_rn(0.f);
+        p.z[(long)b * 2 * p.z_half + p.z_half + j] = __float2bfloat16_rn(0.f);
+      }
+}
+
+}  // namespace pgout
+}  // namespace ta

@@ -46,7 +46,7 @@ def run_step(st, append=True, flags=0, prefix_call=None, **kw):
         y = Bd.tucker_attn_decode_prefix(x, *dw, K, V, table, lens, ptab if st.P else None, st.P, **args)
     else:
         y = Bd.tucker_attn_decode_paged(x, *dw, K, V, table, lens, **args)
-        assert Bd.last_path() == expected_path(st, flags)
+    assert Bd.last_path() == expected_path(st, flags)
     assert Bd.last_device_error() == 0
     return y, K, V
 
