@@ -1,7 +1,7 @@
 // Output side of the paged decode step: joins the partials of a sequence -- those of its own keys (streaming kernel) and of
 // the shared prefix (prefix kernel) -- by their maxima and sums and applies the output-side core:
 //   o_h = merged, normalised output of head h;  u[a, :] = sum_h Ut1[h, a] o_h;  z[j] = sum_a sum_c Ct[a, j, c] u[a, c]
-// A cluster of CL CTAs per sequence.  CTA y merges t3 / CL value columns of all heads (every partial is read once per
+// A cluster of CL CTAs per sequence (8, 4 or 2: the most that still lets all of them run at once, two CTAs per SM).  CTA y merges t3 / CL value columns of all heads (every partial is read once per
 // sequence, where CTAs that split the rows of z would each have to merge everything), forms its columns of u, hands them to the
 // other CTAs through distributed shared memory, and computes t2 / CL rows of z.  One user with a long cache has a partial
 // from every SM: the maxima, weights and sums of the partials are spread over all warps instead of walked by one.
@@ -14,10 +14,8 @@
 namespace ta {
 namespace pgout {
 
-constexpr int CL = 8;
 constexpr int THREADS = 512, WARPS = THREADS / 32;
 constexpr int MAX_PART = 2 * dec::MAX_GRID;      // partials of one head: one per CTA of either attention kernel at most
-constexpr int MAX_COLS = 128 / CL;
 
 struct Params {
   int B, nH, Lmax, t1, t2, t3, z_half;
@@ -31,9 +29,9 @@ struct Params {
   unsigned int* err;
 };
 
-__host__ __device__ inline size_t smem_bytes(int t1, int t3, int nH, bool with_prefix) {
+__host__ __device__ inline size_t smem_bytes(int cl, int t1, int t3, int nH, bool with_prefix) {
   const int parts = with_prefix ? MAX_PART : dec::MAX_GRID;
-  return sizeof(float) * ((size_t)parts * 32 + (size_t)t1 * t3 + (size_t)nH * t1 + (size_t)THREADS * 4 + 32 * MAX_COLS);
+  return sizeof(float) * ((size_t)parts * 32 + (size_t)t1 * t3 + (size_t)nH * t1 + (size_t)THREADS * 4 + 32 * (128 / cl));
 }
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
@@ -44,9 +42,11 @@ __device__ __forceinline__ void st_cluster(float* own, uint32_t rank, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory");
 }
 
-__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS) k_pg_out(const Params p) {
+template <int CL>
+__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_out(const Params p) {
+  constexpr int MAX_COLS = 128 / CL;
   extern __shared__ __align__(16) float sm[];
-  const int t3 = p.t3, cw = t3 / CL, q4 = cw / 4;          // columns of this CTA: 8, 12 or 16, as float4
+  const int t3 = p.t3, cw = t3 / CL, q4 = cw / 4;          // columns of this CTA (t3 = 64, 96 or 128), as float4
   float4* red_s = reinterpret_cast<float4*>(sm);           // [THREADS]
   float* o_s = sm + THREADS * 4;                           // [32][MAX_COLS]
   float* u_s = o_s + 32 * MAX_COLS;                        // [t1][t3]

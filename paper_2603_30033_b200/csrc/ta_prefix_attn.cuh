@@ -52,6 +52,12 @@ struct Params {
   unsigned int* err;
 };
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
 // The CTA that works on unit t when `total` units are divided over `grid` CTAs (see dec::cta_first_tile).
 __device__ __forceinline__ long owner_of(long t, long total, long grid) { return ((t + 1) * grid - 1) / total; }
 
@@ -59,7 +65,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
               const __grid_constant__ CUtensorMap tmV, const Params p) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t q_full, q_empty, kv_full[MAX_BUF], kv_empty[MAX_BUF], s_full[2], p_full[2], o_full[2], o_read[2], patched;
+  __shared__ uint64_t q_full, q_empty, kv_full[MAX_BUF], kv_empty[MAX_BUF], s_full[2], p_half[2], p_full[2], o_full[2], o_read[2], patched;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -79,7 +85,8 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     for (int i = 0; i < MAX_BUF; ++i) { mbar_init(&kv_full[i], 1); mbar_init(&kv_empty[i], 1); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s_full[i], 1);
-      mbar_init(&p_full[i], 4);         // P is in TMEM: one arrival per warp of the group
+      mbar_init(&p_half[i], 4);         // the first 64 keys' P is in TMEM: one arrival per warp of the group
+      mbar_init(&p_full[i], 4);         // all of it
       mbar_init(&o_full[i], 1);         // the P V product is complete
       mbar_init(&o_read[i], 4);         // the accumulator of a finished segment has been read
     }
@@ -209,8 +216,7 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           }
           sk = n % n_buf;
           for (int w = 0; w < nw && ok; ++w) {
-            if (!(ok = mbar_wait_poll(&p_full[w], (pf >> w) & 1u, ab))) break;
-            pf ^= 1u << w;
+            if (!(ok = mbar_wait_poll(&p_half[w], (pf >> w) & 1u, ab))) break;
             if (i == 0) {                 // the accumulator of the group's previous segment must have been read
               if ((begun >> w) & 1u) {
                 if (!(ok = mbar_wait(&o_read[w], (od >> w) & 1u, ab))) break;
@@ -221,9 +227,16 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             tc_fence_after();
             const uint64_t dv = dv0 + (uint64_t)(sv * (buf_bytes >> 4));
             const uint32_t a = tmem + (uint32_t)w * 128u, d = tmem + 256u + (uint32_t)w * 128u;
+            // the product starts with the keys whose P is there while the group still works on the others
 #pragma unroll
-            for (int ks = 0; ks < TK / 16; ++ks)
+            for (int ks = 0; ks < TK / 32; ++ks)
               umma_ts(d, a + (uint32_t)ks * 8u, dv + (uint64_t)(ks * 128), idesc_pv, (i | ks) != 0 ? 1u : 0u);
+            if (!(ok = mbar_wait_poll(&p_full[w], (pf >> w) & 1u, ab))) break;
+            pf ^= 1u << w;
+            tc_fence_after();
+#pragma unroll
+            for (int ks = TK / 32; ks < TK / 16; ++ks)
+              umma_ts(d, a + (uint32_t)ks * 8u, dv + (uint64_t)(ks * 128), idesc_pv, 1u);
             umma_commit(&o_full[w]);
             if (i + 1 < nt) {
               if (w == 0 && !(ok = mbar_wait(&kv_full[sk], (uint32_t)((n / n_buf) & 1), ab))) break;
@@ -301,10 +314,10 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
          float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
 #pragma unroll
          for (int c = 0; c < 128; c += 8) {
-           m0 = fmaxf(m0, fmaxf(__uint_as_float(sr[c]), __uint_as_float(sr[c + 1])));
-           m1 = fmaxf(m1, fmaxf(__uint_as_float(sr[c + 2]), __uint_as_float(sr[c + 3])));
-           m2 = fmaxf(m2, fmaxf(__uint_as_float(sr[c + 4]), __uint_as_float(sr[c + 5])));
-           m3 = fmaxf(m3, fmaxf(__uint_as_float(sr[c + 6]), __uint_as_float(sr[c + 7])));
+           m0 = max3(m0, __uint_as_float(sr[c]), __uint_as_float(sr[c + 1]));
+           m1 = max3(m1, __uint_as_float(sr[c + 2]), __uint_as_float(sr[c + 3]));
+           m2 = max3(m2, __uint_as_float(sr[c + 4]), __uint_as_float(sr[c + 5]));
+           m3 = max3(m3, __uint_as_float(sr[c + 6]), __uint_as_float(sr[c + 7]));
          }
          mt = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
        }
@@ -328,28 +341,25 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
          l *= f;
          m_used = m_new;
        }
-       {
-         const float2 negm = make_float2(-m_used, -m_used);
-         float2 rs[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+       const float2 negm = make_float2(-m_used, -m_used);
+       float2 rs[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-         for (int c = 0; c < 64; ++c) {
+       for (int half = 0; half < 2; ++half) {
+#pragma unroll
+         for (int c = half * 32; c < half * 32 + 32; ++c) {
            const float2 x = __fadd2_rn(make_float2(__uint_as_float(sr[2 * c]), __uint_as_float(sr[2 * c + 1])), negm);
            const float2 e = make_float2(dec::ex2(x.x), dec::ex2(x.y));
            rs[c & 3] = __fadd2_rn(rs[c & 3], e);
            sr[c] = pack_bf16(e.x, e.y);
          }
-         const float2 r01 = __fadd2_rn(rs[0], rs[1]), r23 = __fadd2_rn(rs[2], rs[3]);
-         l += (r01.x + r01.y) + (r23.x + r23.y);
-       }
-       {
-         uint32_t (*c)[32] = reinterpret_cast<uint32_t (*)[32]>(sr);
-         tmem_st32(tm_s + 0, c[0]);
-         tmem_st32(tm_s + 32, c[1]);
+         tmem_st32(tm_s + half * 32, reinterpret_cast<uint32_t (*)[32]>(sr)[half]);
          tmem_st_wait();
+         tc_fence_before();
+         __syncwarp();
+         if (lane == 0) mbar_arrive(half ? &p_full[w] : &p_half[w]);
        }
-       tc_fence_before();
-       __syncwarp();
-       if (lane == 0) mbar_arrive(&p_full[w]);
+       const float2 r01 = __fadd2_rn(rs[0], rs[1]), r23 = __fadd2_rn(rs[2], rs[3]);
+       l += (r01.x + r01.y) + (r23.x + r23.y);
      }
      if (!ok) break;
      if (present) {
