@@ -248,8 +248,9 @@ int tucker_cache_append_paged(const tucker_attn_desc* desc, const void* X, const
   p.dev_err = device_error_ptr();
   p.prof_start = tl_prof_start; p.prof_stop = tl_prof_stop;
   if (!p.dev_err) return TA_ERR_CUDA;
-  const int rc = T > 0 ? generic_paged_append(p, tok_start, T) : TA_OK;
-  tl_last_path = 1;
+  const bool fast = fast_append_supported(*desc);
+  const int rc = T == 0 ? TA_OK : (fast ? fast_append(p, tok_start, T) : generic_paged_append(p, tok_start, T));
+  tl_last_path = fast ? 2 : 1;
   tl_last_launches = p.launches;
   return rc;
 }

@@ -1,0 +1,265 @@
+// Append to a paged latent cache on tcgen05: [K | V] = X [U3 | Ut3], latent RoPE on K, rows scattered to their pages; one
+// launch, nothing between X and the pages touches memory.
+//
+// One CTA multiplies MT tiles of 128 token rows (A, K-major) with the factors as they lie in memory (B, MN-major), all columns of
+// both or of one of them, over a share of d.  The S CTAs of a cluster share the rows and split d: a batch of a few tokens is
+// bound by reading the factors, which S (times two) SMs then do at once, and a long prompt whose row tiles do not fill
+// the GPU gets more CTAs without reading X or the factors twice.  The sum over the cluster runs through distributed shared memory:
+//   unit       16 columns x 128 rows of fp32 sums; the units of a cluster are dealt evenly to its CTAs
+//   every CTA  writes the units of the others from TMEM to its own shared memory (the ring, idle by then), then
+//              reads its own units from the S - 1 others and adds them in the order of the shares (its own from TMEM):
+//              no atomics, the result does not depend on timing
+//   epilogue   thread = token row: rotation at the row's position, one rounding to bf16, 32 bytes to the row's page
+// Bounds: X read once and the pages written once when T is large; per-CTA bytes of X and the factors over L2 otherwise,
+// which is what the choice of MT, S and the column split minimises (append_plan).
+//   warp 0  TMA producer      warp 1  TMEM, MMA issue      warps 2..9  epilogue, two per TMEM lane quadrant
+#pragma once
+
+#include "ta_paged.cuh"
+#include "ta_sm100.cuh"
+
+namespace ta {
+namespace append {
+
+using namespace sm100;
+
+constexpr int BM = 128, BK = 64, UC = 16;        // UC: columns of a unit
+constexpr int THREADS = 320;
+constexpr int MAX_STAGES = 8;
+constexpr int RING_BYTES = 192 * 1024;
+constexpr size_t SMEM_BYTES = 1024 + (size_t)RING_BYTES;
+constexpr int A_BYTES = BM * BK * 2, BOX_BYTES = 64 * BK * 2, UNIT_BYTES = UC * BM * 4;
+constexpr int MAX_S = 8;
+
+// A factor [d, width] and where its products go.
+struct Part {
+  bf16* pool;
+  int width;          // r3 or t3, a multiple of 32, at most 256
+  int rope;           // 1: rotated before rounding
+};
+struct Params {
+  int T, d, S, MT;               // token rows, embedding width, CTAs per cluster, row tiles per CTA
+  int n_parts;                   // parts a CTA computes: n_parts of part[], from part[blockIdx.y] on
+  Part part[2];
+  const int32_t *tok_start, *cache_len;
+  int B, pos0;
+  PagedView pv;
+  unsigned int* err;
+};
+
+// TMEM columns of one accumulator
+__host__ __device__ constexpr uint32_t acc_cols(int width) { return width <= 32 ? 32u : (width <= 64 ? 64u : (width <= 128 ? 128u : 256u)); }
+__host__ __device__ inline int boxes(int width) { return (width + 63) / 64; }
+
+__global__ void __launch_bounds__(THREADS, 1)
+k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmB1,
+         const Params p, const dec::RopeFreqs freqs) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t full_bar[MAX_STAGES], empty_bar[MAX_STAGES], acc_bar;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag;
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* ring = smem_raw + (base - smem_u32(smem_raw));
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int S = p.S, MT = p.MT, s = (int)(blockIdx.x % (unsigned)S);
+  const int m0 = (int)(blockIdx.x / (unsigned)S) * MT * BM;
+  Abort ab{&abort_flag, p.err};
+  // this CTA's parts, their place among a row tile's TMEM columns, and the K blocks of its share of d
+  const Part p0 = p.part[blockIdx.y];
+  const Part p1 = p.n_parts > 1 ? p.part[1] : Part{nullptr, 0, 0};
+  const int width = p0.width + p1.width;
+  const uint32_t c1 = acc_cols(p0.width);                                  // first column of the second part
+  const uint32_t tile_cols = c1 + (p1.width ? acc_cols(p1.width) : 0u);
+  uint32_t ncols = 32;
+  while (ncols < tile_cols * (uint32_t)MT) ncols *= 2;
+  const int nb = boxes(p0.width) + (p1.width ? boxes(p1.width) : 0);
+  const uint32_t stage_bytes = (uint32_t)(MT * A_BYTES + nb * BOX_BYTES);
+  const int stages = min(MAX_STAGES, (int)(RING_BYTES / stage_bytes));
+  const int nkb = p.d / BK, kb0 = (int)((long)nkb * s / S), kb1 = (int)((long)nkb * (s + 1) / S);
+  // units of the cluster: (row tile, column chunk); this CTA finishes [u0, u1)
+  const int upt = width / UC, units = MT * upt;
+  const int u0 = units * s / S, u1 = units * (s + 1) / S;
+
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int i = 0; i < MAX_STAGES; ++i) { mbar_init(&full_bar[i], 1); mbar_init(&empty_bar[i], 1); }
+    mbar_init(&acc_bar, 1);
+    fence_barrier_init();
+  }
+  pdl_enter();
+  if (warp == 1) {
+    tmem_alloc(&tmem_slot, ncols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+
+  bool ok = true;
+  AppendDst dst[2];
+  const int q = warp % 4, hf = (warp - 2) >> 2, rloc = q * 32 + lane;
+  if (warp == 0) {
+    if (elect_one()) {
+      tma_prefetch_desc(&tmX); tma_prefetch_desc(&tmB0); tma_prefetch_desc(&tmB1);
+      const CUtensorMap* tb0 = blockIdx.y == 0 ? &tmB0 : &tmB1;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        const int i = kb - kb0, st = i % stages;
+        if (!mbar_wait(&empty_bar[st], ((i / stages) & 1) ^ 1, ab)) break;
+        mbar_expect_tx(&full_bar[st], stage_bytes);
+        uint8_t* a = ring + (size_t)st * stage_bytes;
+        uint8_t* b = a + MT * A_BYTES;
+        for (int t = 0; t < MT; ++t) tma_load_2d(a + t * A_BYTES, &tmX, &full_bar[st], kb * BK, m0 + t * BM);
+        for (int j = 0; j < boxes(p0.width); ++j) tma_load_2d(b + j * BOX_BYTES, tb0, &full_bar[st], j * 64, kb * BK);
+        b += boxes(p0.width) * BOX_BYTES;
+        if (p1.width)
+          for (int j = 0; j < boxes(p1.width); ++j) tma_load_2d(b + j * BOX_BYTES, &tmB1, &full_bar[st], j * 64, kb * BK);
+      }
+    }
+  } else if (warp == 1) {
+    if (elect_one()) {
+      const uint32_t id0 = umma_idesc_bf16(BM, (uint32_t)p0.width) | (1u << 16), id1 = umma_idesc_bf16(BM, (uint32_t)p1.width) | (1u << 16);
+      for (int kb = kb0; kb < kb1; ++kb) {
+        const int i = kb - kb0, st = i % stages;
+        if (!(ok = mbar_wait(&full_bar[st], (i / stages) & 1, ab))) break;
+        tc_fence_after();
+        const uint32_t a = smem_u32(ring + (size_t)st * stage_bytes), b = a + MT * A_BYTES;
+        for (int t = 0; t < MT; ++t) {
+          const uint64_t da = umma_desc_kmajor_sw128(a + t * A_BYTES);
+          const uint64_t db0 = umma_desc_mnmajor_sw128(b, BOX_BYTES);
+          const uint64_t db1 = umma_desc_mnmajor_sw128(b + boxes(p0.width) * BOX_BYTES, BOX_BYTES);
+          const uint32_t d = tmem + (uint32_t)t * tile_cols;
+#pragma unroll
+          for (int k = 0; k < BK / 16; ++k)
+            umma_ss(d, da + (uint64_t)(k * 2), db0 + (uint64_t)(k * 128), id0, (i | k) != 0 ? 1u : 0u);
+          if (p1.width) {
+#pragma unroll
+            for (int k = 0; k < BK / 16; ++k)
+              umma_ss(d + c1, da + (uint64_t)(k * 2), db1 + (uint64_t)(k * 128), id1, (i | k) != 0 ? 1u : 0u);
+          }
+        }
+        umma_commit(&empty_bar[st]);
+      }
+      umma_commit(&acc_bar);
+    }
+  } else {
+    // ------------------------------- epilogue warps -------------------------------
+    // while the products run: where this thread's rows go
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      dst[t].row = -1; dst[t].pos = 0;
+      const int row = m0 + t * BM + rloc;
+      if (t < MT && row < p.T) dst[t] = append_dst(row, p.tok_start, p.cache_len, p.B, p.pos0, p.pv, p.err);
+    }
+    ok = mbar_wait(&acc_bar, 0, ab);
+    ok = __all_sync(0xffffffffu, ok);
+    tc_fence_after();
+    if (ok && S > 1) {
+      // the others' units to shared memory, [unit][column][row]
+      for (int u = hf; u < units; u += 2) {
+        if (u >= u0 && u < u1) continue;
+        const int t = u / upt, c = (u % upt) * UC;
+        uint32_t r[16];
+        tmem_ld16(tmem + (uint32_t)t * tile_cols + (c < p0.width ? (uint32_t)c : c1 + (uint32_t)(c - p0.width)) + ((uint32_t)(q * 32) << 16), r);
+        tmem_ld_wait();
+        float* out = reinterpret_cast<float*>(ring + (size_t)(u < u0 ? u : u - (u1 - u0)) * UNIT_BYTES) + rloc;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) out[e * BM] = __uint_as_float(r[e]);
+      }
+    }
+  }
+  if (S > 1) {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+  if (warp >= 2 && ok) {
+    for (int u = u0 + hf; u < u1; u += 2) {
+      __syncwarp();                               // rows of nobody skip the end of the body
+      const int t = u / upt, c = (u % upt) * UC;
+      float v[16];
+      {
+        uint32_t r[16];
+        tmem_ld16(tmem + (uint32_t)t * tile_cols + (c < p0.width ? (uint32_t)c : c1 + (uint32_t)(c - p0.width)) + ((uint32_t)(q * 32) << 16), r);
+        tmem_ld_wait();
+        float own[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) { own[e] = __uint_as_float(r[e]); v[e] = 0.f; }
+        for (int o = 0; o < S; ++o) {             // in the order of the shares of d
+          if (o == s) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] += own[e];
+          } else {
+            const int ou0 = units * o / S, ou1 = units * (o + 1) / S;       // CTA o's own units are not in its list
+            uint32_t addr;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                         : "=r"(addr) : "r"(smem_u32(ring) + (uint32_t)((u < ou0 ? u : u - (ou1 - ou0)) * UNIT_BYTES + rloc * 4)), "r"(o));
+            float w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w[e]) : "r"(addr + (uint32_t)(e * BM * 4)));
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] += w[e];
+          }
+        }
+      }
+      const AppendDst to = t == 0 ? dst[0] : dst[1];
+      const Part& pt = c < p0.width ? p0 : p1;
+      const int cc = c < p0.width ? c : c - p0.width;
+      if (to.row < 0) continue;
+      if (pt.rope) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float2 cs = dec::rope_cos_sin_theta(to.pos, freqs.theta[cc / 2 + e]);
+          const float xe = v[2 * e], xo = v[2 * e + 1];
+          v[2 * e] = xe * cs.x - xo * cs.y;
+          v[2 * e + 1] = xe * cs.y + xo * cs.x;
+        }
+      }
+      if (TA_IDX_OK(p.err, to.row * pt.width + cc, 16, (long)p.pv.n_pages * p.pv.page_size * pt.width)) {
+        uint4* out = reinterpret_cast<uint4*>(pt.pool + to.row * pt.width + cc);
+        out[0] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        out[1] = make_uint4(pack_bf16(v[8], v[9]), pack_bf16(v[10], v[11]), pack_bf16(v[12], v[13]), pack_bf16(v[14], v[15]));
+      }
+    }
+  }
+  tc_fence_before();
+  if (S > 1) {                       // nobody leaves while another CTA may still read its shared memory
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+  __syncthreads();
+  if (warp == 1) tmem_dealloc(tmem, ncols);
+}
+
+// How a call is divided: MT row tiles per CTA, S shares of d per cluster, and whether the two factors go to different CTAs.
+// The CTA's time is taken as proportional to the bytes it moves into shared memory, times the waves of one CTA per SM;
+// a share of d costs a pass of the partial sums through shared memory.
+struct Plan {
+  int MT, S, split_parts;
+};
+inline Plan append_plan(int T, int d, int w0, int w1, int sms) {
+  Plan best{1, 1, 0};
+  double best_cost = -1;
+  const int tiles = (T + BM - 1) / BM, nkb = d / BK;
+  for (int mt = 1; mt <= 2; ++mt)
+    for (int split = 0; split <= (w1 > 0 ? 1 : 0); ++split)
+      for (int S = 1; S <= MAX_S && S <= nkb; S *= 2) {
+        const int width = split ? (w0 > w1 ? w0 : w1) : w0 + w1;
+        const uint32_t cols = split ? acc_cols(width) : acc_cols(w0) + (w1 ? acc_cols(w1) : 0u);
+        const int units = mt * width / UC;
+        if (mt > tiles || cols * mt > 512) continue;
+        if ((long)(units - units / S) * UNIT_BYTES > RING_BYTES && S > 1) continue;
+        const long ctas = (long)((tiles + mt - 1) / mt) * S * (split ? 2 : 1);
+        const long waves = (ctas + sms - 1) / sms;
+        const int rows = T < mt * BM ? T : mt * BM;
+        const double bytes = 2.0 * ((double)rows + width) * d / S + (S > 1 ? 2.0 * 4.0 * rows * width / S : 0.0) + 16384.0;
+        const double cost = waves * bytes;
+        if (best_cost < 0 || cost < best_cost) { best_cost = cost; best = Plan{mt, S, split}; }
+      }
+  return best;
+}
+
+}  // namespace append
+}  // namespace ta

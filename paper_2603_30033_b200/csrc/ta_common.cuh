@@ -87,6 +87,8 @@ bool fast_paged_supported(const tucker_attn_desc& d, int32_t page_size);
 size_t fast_paged_workspace(const tucker_attn_desc& d, int32_t prefix_len, bool one_pool);
 size_t fast_decode_workspace(const tucker_attn_desc& d, int32_t Lmax);
 int fast_decode(Problem& p);
+bool fast_append_supported(const tucker_attn_desc& d);
+int fast_append(Problem& p, const int32_t* tok_start, int32_t T);
 int wait_selftest(unsigned int* dev_err, int budget_us, int* out_dev, cudaStream_t stream);
 
 // Tensor-core GEMM with fp32 split-K partial outputs (ta_fast.cu): for z < splits,

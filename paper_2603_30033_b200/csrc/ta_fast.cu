@@ -13,6 +13,7 @@
 #include "ta_attn_prefill.cuh"
 #include "ta_decode.cuh"
 #include "ta_decode_umma.cuh"
+#include "ta_append_umma.cuh"
 #include "ta_paged_out.cuh"
 #include "ta_prefix_attn.cuh"
 #include "ta_zy_fused.cuh"
@@ -820,6 +821,53 @@ int fast_decode(Problem& p) {
     gp.b_kb_wrap = p.paged ? z_half(d) / 64 : 0;
     if ((rc = launch_gemm(p, w.z, zk, d.B, zk, &bop, 1, d.d_model, pick_bn(d.d_model), gp))) return rc;
   }
+  return TA_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
+// append to a paged cache
+// ---------------------------------------------------------------------------------------------
+bool fast_append_supported(const tucker_attn_desc& d) {
+  auto ok32 = [](int r) { return r >= 32 && r <= 256 && r % 32 == 0; };
+  return d.dtype == TA_DTYPE_BF16 && !(d.flags & TA_FLAG_FORCE_GENERIC) && ok32(d.r3) && ok32(d.t3) && d.d_model % 64 == 0;
+}
+
+int fast_append(Problem& p, const int32_t* tok_start, int32_t T) {
+  const tucker_attn_desc& d = p.d;
+  append::Params ap = {};
+  ap.T = T; ap.d = d.d_model; ap.tok_start = tok_start; ap.cache_len = p.cache_len; ap.B = d.B; ap.pos0 = d.pos0;
+  ap.pv = p.pv; ap.err = p.dev_err;
+  // one pool: the value rows, which are the un-rotated latent rows, are all there is
+  const append::Part keys = {(bf16*)p.Kc, d.r3, d.rope ? 1 : 0}, values = {(bf16*)p.Vc, d.t3, 0};
+  ap.part[0] = p.shared_kv ? values : keys;
+  ap.part[1] = values;
+  const append::Plan plan = append::append_plan(T, d.d_model, ap.part[0].width, p.shared_kv ? 0 : d.t3, sm_count());
+  ap.S = plan.S; ap.MT = plan.MT;
+  ap.n_parts = (p.shared_kv || plan.split_parts) ? 1 : 2;
+  CUtensorMap tmX, tm0, tm1;
+  if (!tmap_2d(&tmX, p.X, (uint64_t)d.d_model, (uint64_t)T, (uint64_t)d.d_model, 64, append::BM)) return TA_ERR_CUDA;
+  if (!tmap_2d(&tm1, p.Ut3, (uint64_t)d.t3, (uint64_t)d.d_model, (uint64_t)d.t3, 64, 64)) return TA_ERR_CUDA;
+  if (p.shared_kv) tm0 = tm1;
+  else if (!tmap_2d(&tm0, p.U3, (uint64_t)d.r3, (uint64_t)d.d_model, (uint64_t)d.r3, 64, 64)) return TA_ERR_CUDA;
+  static PerDeviceFlag attr;
+  TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)append::k_append, (int)append::SMEM_BYTES));
+  const long tiles = ((long)T + append::BM * plan.MT - 1) / (append::BM * plan.MT);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * plan.S), plan.split_parts ? 2 : 1);
+  cfg.blockDim = dim3(append::THREADS);
+  cfg.dynamicSmemBytes = append::SMEM_BYTES;
+  cfg.stream = p.stream;
+  cudaLaunchAttribute la[2];
+  la[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  la[0].val.programmaticStreamSerializationAllowed = 1;
+  la[1].id = cudaLaunchAttributeClusterDimension;
+  la[1].val.clusterDim.x = (unsigned)plan.S; la[1].val.clusterDim.y = 1; la[1].val.clusterDim.z = 1;
+  cfg.attrs = la;
+  cfg.numAttrs = 2;
+  prof_begin(p);
+  (void)cudaLaunchKernelEx(&cfg, append::k_append, tmX, tm0, tm1, ap, rope_freqs(d));
+  prof_end(p);
+  TA_LAUNCH_CHECK(p);
   return TA_OK;
 }
 

@@ -180,6 +180,8 @@ def check_append(st, new, pad=0, front=0, pos0=0, flags=0, seed=3):
     k0, v0 = host(K), host(V)
     Bd.tucker_cache_append_paged(Xd, dw[3], dw[7], K, V, table, lens, torch.from_numpy(start.astype(np.int32)).cuda(),
                                  rope=w.rope, rope_base=w.rope_base, pos0=pos0, flags=flags)
+    tc = w.dtype == "bf16" and w.d_model % 64 == 0 and all(32 <= r <= 256 and r % 32 == 0 for r in (w.r[2], w.t[2]))
+    assert Bd.last_path() == (2 if tc else 1)
     assert Bd.last_device_error() == 0
     kr, vr = [], []
     for b in range(B):
