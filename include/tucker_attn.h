@@ -218,11 +218,13 @@ typedef struct {
  *              outside [tok_start[0], tok_start[B]) are padding and are not used
  * Row i of sequence b goes to slot cache_len[b] + i, at absolute position pos0 + cache_len[b] + i (pos0 >= 0: what stands in
  * front of slot 0, such as a shared prefix).  Used of desc: B, d_model, r3, t3, rope, rope_base, pos0, dtype, flags (the other
- * fields must be valid).  T = 0 is allowed.  Nothing else in the pools is touched.  No workspace.
+ * fields must be valid).  T = 0 is allowed.  Nothing else in the pools is touched.
+ * workspace: >= tucker_cache_append_paged_workspace_bytes(desc, cache, T) bytes, 256-byte aligned.
  */
+TA_API size_t tucker_cache_append_paged_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache* cache, int32_t T);
 TA_API int tucker_cache_append_paged(const tucker_attn_desc* desc, const void* X, const void* U3, const void* Ut3,
                               const tucker_paged_cache* cache, const int32_t* cache_len, const int32_t* tok_start, int32_t T,
-                              void* cuda_stream);
+                              void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
  * One cached decode step over a paged cache: tucker_attn_decode with its caches in pages.  The new token of sequence b

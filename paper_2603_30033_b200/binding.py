@@ -29,7 +29,7 @@ EXPORTS = (
     "tucker_attn_last_path", "tucker_attn_last_launch_count", "tucker_attn_set_profile_events",
     "tucker_attn_decode_static", "tucker_attn_selftest_wait_timeout", "tucker_attn_sync_status",
     "tucker_attn_bounds_checked",
-    "tucker_cache_append_paged", "tucker_attn_decode_paged", "tucker_attn_decode_paged_workspace_bytes",
+    "tucker_cache_append_paged", "tucker_cache_append_paged_workspace_bytes", "tucker_attn_decode_paged", "tucker_attn_decode_paged_workspace_bytes",
     "tucker_attn_decode_prefix", "tucker_attn_decode_prefix_workspace_bytes",
     "tucker_pack_gqa", "tucker_pack_mha", "tucker_pack_mla",
     "tucker_hosvd_workspace_bytes", "tucker_hosvd_init", "tucker_mha_weight_tensors", "tucker_probe_plane_mix", "tucker_probe_mma_rate",
@@ -90,7 +90,9 @@ def load_library() -> ctypes.CDLL:
     lib.tucker_attn_decode_static.argtypes = [dp] + [vp] * 11 + [i32, vp, i32, vp, vp]
     pp = ctypes.POINTER(TuckerPagedCache)
     lib.tucker_cache_append_paged.restype = ctypes.c_int
-    lib.tucker_cache_append_paged.argtypes = [dp] + [vp] * 3 + [pp, vp, vp, i32, vp]
+    lib.tucker_cache_append_paged.argtypes = [dp] + [vp] * 3 + [pp, vp, vp, i32, vp, sz, vp]
+    lib.tucker_cache_append_paged_workspace_bytes.restype = sz
+    lib.tucker_cache_append_paged_workspace_bytes.argtypes = [dp, pp, i32]
     lib.tucker_attn_decode_paged_workspace_bytes.restype = sz
     lib.tucker_attn_decode_paged_workspace_bytes.argtypes = [dp, pp]
     lib.tucker_attn_decode_paged.restype = ctypes.c_int
@@ -330,7 +332,7 @@ def _paged_cache(Kpages, Vpages, block_table, B, r3, t3, dtype, device):
 
 
 def tucker_cache_append_paged(X, U3, Ut3, Kpages, Vpages, block_table, cache_len, tok_start, *, rope: bool,
-                              rope_base: float = 10000.0, pos0: int = 0, flags: int = 0) -> None:
+                              rope_base: float = 10000.0, pos0: int = 0, workspace=None, flags: int = 0) -> None:
     """Appends a ragged batch of tokens to a paged cache (same name and argument meaning as the C entry point).
     X [T, d]: rows tok_start[b] .. tok_start[b + 1] - 1 are the new tokens of sequence b; Kpages [n_pages, page_size, r3],
     Vpages [n_pages, page_size, t3] (the same tensor: one shared latent pool, with U3 and Ut3 the same tensor);
@@ -351,9 +353,13 @@ def tucker_cache_append_paged(X, U3, Ut3, Kpages, Vpages, block_table, cache_len
     cache = _paged_cache(Kpages, Vpages, block_table, B, r3, t3, dt, dev)
     desc = make_desc(B=B, N=1, d_model=d, n_H=1, r=(1, 1, r3), t=(1, 1, t3), causal=True, rope=rope, rope_base=rope_base,
                      pos0=pos0, dtype=_dtype_code(X), flags=flags)
+    if workspace is None:
+        workspace = alloc_workspace(lib.tucker_cache_append_paged_workspace_bytes(ctypes.byref(desc), ctypes.byref(cache), int(T)), dev)
+    _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
     with torch.cuda.device(dev):
         rc = lib.tucker_cache_append_paged(ctypes.byref(desc), X.data_ptr(), U3.data_ptr(), Ut3.data_ptr(), ctypes.byref(cache),
-                                           cache_len.data_ptr(), tok_start.data_ptr(), int(T), _stream_ptr(dev))
+                                           cache_len.data_ptr(), tok_start.data_ptr(), int(T), workspace.data_ptr(),
+                                           workspace.numel(), _stream_ptr(dev))
     if rc != TA_OK:
         raise TuckerAttnError(rc, "tucker_cache_append_paged")
 

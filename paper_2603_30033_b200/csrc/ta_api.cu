@@ -228,18 +228,27 @@ int tucker_attn_decode_paged(const tucker_attn_desc* desc, const void* x, const 
                                    workspace, workspace_bytes, cuda_stream);
 }
 
+size_t tucker_cache_append_paged_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache* cache, int32_t T) {
+  if (!desc_ok(desc, true) || !paged_ok(cache, desc->pos0) || T < 0) return 0;
+  const size_t need = T > 0 && fast_append_supported(*desc) ? fast_append_workspace(*desc, T, cache->K == cache->V) : 0;
+  return need < 256 ? 256 : need;
+}
+
 int tucker_cache_append_paged(const tucker_attn_desc* desc, const void* X, const void* U3, const void* Ut3,
                               const tucker_paged_cache* cache, const int32_t* cache_len, const int32_t* tok_start, int32_t T,
-                              void* cuda_stream) {
+                              void* workspace, size_t workspace_bytes, void* cuda_stream) {
   if (!desc_ok(desc, true) || !paged_ok(cache, desc->pos0) || T < 0) return TA_ERR_INVALID_ARG;
-  if (!U3 || !Ut3 || !cache_len || !tok_start || (T > 0 && !X)) return TA_ERR_INVALID_ARG;
+  if (!U3 || !Ut3 || !cache_len || !tok_start || !workspace || (T > 0 && !X)) return TA_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return TA_ERR_INVALID_ARG;
   if (cache->K == cache->V && !shared_kv_weights(*desc, U3, Ut3)) return TA_ERR_INVALID_ARG;
   const void* ptrs[] = {X, U3, Ut3, cache->K, cache->V};
   for (const void* q : ptrs)
     if (!aligned16(q)) return TA_ERR_INVALID_ARG;
+  if (workspace_bytes < tucker_cache_append_paged_workspace_bytes(desc, cache, T)) return TA_ERR_WORKSPACE_TOO_SMALL;
   Problem p = {};
   p.d = *desc;
   p.X = X; p.U3 = U3; p.Ut3 = Ut3; p.Kc = cache->K; p.Vc = cache->V; p.cache_len = cache_len;
+  p.ws = static_cast<char*>(workspace); p.ws_bytes = workspace_bytes;
   p.paged = 1;
   p.pv = PagedView{cache->block_table, cache->n_pages, cache->page_size, cache->max_pages};
   p.shared_kv = (cache->K == cache->V) ? 1 : 0;

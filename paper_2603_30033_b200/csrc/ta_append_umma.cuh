@@ -4,12 +4,15 @@
 // One CTA multiplies MT tiles of 128 token rows (A, K-major) with the factors as they lie in memory (B, MN-major), all columns of
 // both or of one of them, over a share of d.  The S CTAs of a cluster share the rows and split d: a batch of a few tokens is
 // bound by reading the factors, which S (times two) SMs then do at once, and a long prompt whose row tiles do not fill
-// the GPU gets more CTAs without reading X or the factors twice.  The sum over the cluster runs through distributed shared memory:
-//   unit       16 columns x 128 rows of fp32 sums; the units of a cluster are dealt evenly to its CTAs
-//   every CTA  writes the units of the others from TMEM to its own shared memory (the ring, idle by then), then
-//              reads its own units from the S - 1 others and adds them in the order of the shares (its own from TMEM):
-//              no atomics, the result does not depend on timing
-//   epilogue   thread = token row: rotation at the row's position, one rounding to bf16, 32 bytes to the row's page
+// the GPU gets more CTAs without reading X or the factors twice.  The sum over the cluster goes through the caller's
+// workspace, i.e. the L2 cache:
+//   unit       32 columns x 128 rows of fp32 sums; the units of a cluster are dealt evenly to its CTAs
+//   every CTA  writes the others' units, meets them at the cluster's barrier, reads its own units back and adds them in the
+//              order of the shares (its own share straight from TMEM): no atomics, the result does not depend on timing
+// (Through distributed shared memory, written or read, the same exchange moved about 13 bytes per cycle and SM: 128 KB per CTA
+// took 10 thousand cycles of the 16384-token call, and 7 of the 16 thousand cycles of the 64-token call.)
+//   epilogue   thread = token row: rotation at the row's position (angles formed while the products run), one rounding to bf16,
+//              64 adjacent bytes of eight rows per store instruction
 // Bounds: X read once and the pages written once when T is large; per-CTA bytes of X and the factors over L2 otherwise,
 // which is what the choice of MT, S and the column split minimises (append_plan).
 //   warp 0  TMA producer      warp 1  TMEM, MMA issue      warps 2..9  epilogue, two per TMEM lane quadrant
@@ -23,13 +26,14 @@ namespace append {
 
 using namespace sm100;
 
-constexpr int BM = 128, BK = 64, UC = 16;        // UC: columns of a unit
+constexpr int BM = 128, BK = 64, UC = 32;        // UC: columns of a unit
 constexpr int THREADS = 320;
 constexpr int MAX_STAGES = 8;
 constexpr int RING_BYTES = 192 * 1024;
 constexpr size_t SMEM_BYTES = 1024 + (size_t)RING_BYTES;
 constexpr int A_BYTES = BM * BK * 2, BOX_BYTES = 64 * BK * 2, UNIT_BYTES = UC * BM * 4;
 constexpr int MAX_S = 8;
+constexpr int CSU = 2;                           // units per thread whose angles are formed ahead
 
 // A factor [d, width] and where its products go.
 struct Part {
@@ -44,12 +48,19 @@ struct Params {
   const int32_t *tok_start, *cache_len;
   int B, pos0;
   PagedView pv;
+  float* part_sums;              // S > 1: [part, when split][cluster][share][unit][128 x UC]
+  int y_units;                   // units of a cluster of the first part (split)
   unsigned int* err;
 };
 
 // TMEM columns of one accumulator
 __host__ __device__ constexpr uint32_t acc_cols(int width) { return width <= 32 ? 32u : (width <= 64 ? 64u : (width <= 128 ? 128u : 256u)); }
 __host__ __device__ inline int boxes(int width) { return (width + 63) / 64; }
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 
 __global__ void __launch_bounds__(THREADS, 1)
 k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmB1,
@@ -98,6 +109,7 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
 
   bool ok = true;
   AppendDst dst[2];
+  float2 cs[CSU][UC / 2];
   const int q = warp % 4, hf = (warp - 2) >> 2, rloc = q * 32 + lane;
   if (warp == 0) {
     if (elect_one()) {
@@ -151,91 +163,126 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
       const int row = m0 + t * BM + rloc;
       if (t < MT && row < p.T) dst[t] = append_dst(row, p.tok_start, p.cache_len, p.B, p.pos0, p.pv, p.err);
     }
+    // ... and the angles of its first two units, where they are rotated (all of its rotated units, unless r3 > 128 or the CTA
+    // finishes two row tiles by itself)
+#pragma unroll
+    for (int k = 0; k < CSU; ++k) {
+      const int u = u0 + hf + 2 * k, t = u / upt, c = (u % upt) * UC;
+      if (u < u1 && c < p0.width && p0.rope)
+#pragma unroll
+        for (int e = 0; e < UC / 2; ++e) cs[k][e] = dec::rope_cos_sin_theta((t == 0 ? dst[0] : dst[1]).pos, freqs.theta[c / 2 + e]);
+    }
     ok = mbar_wait(&acc_bar, 0, ab);
     ok = __all_sync(0xffffffffu, ok);
     tc_fence_after();
-    if (ok && S > 1) {
-      // the others' units to shared memory, [unit][column][row]
+  }
+  auto unit_tmem = [&](int u) -> uint32_t {
+    const int t = u / upt, c = (u % upt) * UC;
+    return tmem + (uint32_t)t * tile_cols + (c < p0.width ? (uint32_t)c : c1 + (uint32_t)(c - p0.width)) + ((uint32_t)(q * 32) << 16);
+  };
+  // rows of this warp that exist: none of the others' sums are needed
+  auto warp_rows = [&](int u) -> bool { return m0 + (u / upt) * BM + q * 32 < p.T; };
+  // 16-byte chunk `ch` of row `row` of a staged unit: a warp's rows of one chunk are adjacent, and the eight chunks of one
+  // row lie on different banks
+  auto chunk_at = [&](int slot, int row, int ch) -> uint32_t {
+    return (uint32_t)(slot * UNIT_BYTES + ch * (BM * 16) + ((row ^ ch) << 4));
+  };
+  // this cluster's partial sums, [share][unit][chunk][row] of 16 bytes
+  float4* const part = reinterpret_cast<float4*>(p.part_sums) + ((long)blockIdx.y * (gridDim.x / S) * p.y_units + (long)(blockIdx.x / S) * units) * S * (UNIT_BYTES / 16);
+  [[maybe_unused]] const long part_n = (long)S * units * (UNIT_BYTES / 16);
+  if (S > 1) {
+    if (warp >= 2 && ok) {
       for (int u = hf; u < units; u += 2) {
-        if (u >= u0 && u < u1) continue;
-        const int t = u / upt, c = (u % upt) * UC;
-        uint32_t r[16];
-        tmem_ld16(tmem + (uint32_t)t * tile_cols + (c < p0.width ? (uint32_t)c : c1 + (uint32_t)(c - p0.width)) + ((uint32_t)(q * 32) << 16), r);
+        if ((u >= u0 && u < u1) || !warp_rows(u)) continue;
+        uint32_t r[32];
+        tmem_ld32(unit_tmem(u), r);
         tmem_ld_wait();
-        float* out = reinterpret_cast<float*>(ring + (size_t)(u < u0 ? u : u - (u1 - u0)) * UNIT_BYTES) + rloc;
+        const long at = ((long)s * units + u) * (UNIT_BYTES / 16) + rloc;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) out[e * BM] = __uint_as_float(r[e]);
+        for (int e = 0; e < 8; ++e)
+          if (TA_IDX_OK(p.err, at + e * BM, 1, part_n))
+            __stcg(part + at + e * BM, make_float4(__uint_as_float(r[4 * e]), __uint_as_float(r[4 * e + 1]), __uint_as_float(r[4 * e + 2]),
+                                                   __uint_as_float(r[4 * e + 3])));
       }
     }
-  }
-  if (S > 1) {
     __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    cluster_sync();                     // orders the writes above before the reads below, across the cluster
   }
   if (warp >= 2 && ok) {
-    for (int u = u0 + hf; u < u1; u += 2) {
-      __syncwarp();                               // rows of nobody skip the end of the body
+    auto finish = [&](int u, bool have, const float2 (&a)[UC / 2]) {
       const int t = u / upt, c = (u % upt) * UC;
-      float v[16];
+      const AppendDst& to = t == 0 ? dst[0] : dst[1];
+      float v[32];
       {
-        uint32_t r[16];
-        tmem_ld16(tmem + (uint32_t)t * tile_cols + (c < p0.width ? (uint32_t)c : c1 + (uint32_t)(c - p0.width)) + ((uint32_t)(q * 32) << 16), r);
+        uint32_t r[32];
+        tmem_ld32(unit_tmem(u), r);
         tmem_ld_wait();
-        float own[16];
+        if (S == 1) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) { own[e] = __uint_as_float(r[e]); v[e] = 0.f; }
-        for (int o = 0; o < S; ++o) {             // in the order of the shares of d
-          if (o == s) {
+          for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(r[e]);
+        } else {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] += own[e];
-          } else {
-            const int ou0 = units * o / S, ou1 = units * (o + 1) / S;       // CTA o's own units are not in its list
-            uint32_t addr;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
-                         : "=r"(addr) : "r"(smem_u32(ring) + (uint32_t)((u < ou0 ? u : u - (ou1 - ou0)) * UNIT_BYTES + rloc * 4)), "r"(o));
-            float w[16];
+          for (int e = 0; e < 32; ++e) v[e] = 0.f;
+          for (int o = 0; o < S; ++o) {           // in the order of the shares of d
+            if (o == s) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-              asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w[e]) : "r"(addr + (uint32_t)(e * BM * 4)));
+              for (int e = 0; e < 32; ++e) v[e] += __uint_as_float(r[e]);
+            } else {
+              const long at = ((long)o * units + u) * (UNIT_BYTES / 16) + rloc;
+              float4 w[8];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] += w[e];
+              for (int e = 0; e < 8; ++e) w[e] = TA_IDX_OK(p.err, at + e * BM, 1, part_n) ? __ldcg(part + at + e * BM) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) { v[4 * e] += w[e].x; v[4 * e + 1] += w[e].y; v[4 * e + 2] += w[e].z; v[4 * e + 3] += w[e].w; }
+            }
           }
         }
       }
-      const AppendDst to = t == 0 ? dst[0] : dst[1];
-      const Part& pt = c < p0.width ? p0 : p1;
-      const int cc = c < p0.width ? c : c - p0.width;
-      if (to.row < 0) continue;
-      if (pt.rope) {
+      const bool first = c < p0.width;
+      if (first && p0.rope) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float2 cs = dec::rope_cos_sin_theta(to.pos, freqs.theta[cc / 2 + e]);
+        for (int e = 0; e < UC / 2; ++e) {
+          const float2 cse = have ? a[e] : dec::rope_cos_sin_theta(to.pos, freqs.theta[c / 2 + e]);
           const float xe = v[2 * e], xo = v[2 * e + 1];
-          v[2 * e] = xe * cs.x - xo * cs.y;
-          v[2 * e + 1] = xe * cs.y + xo * cs.x;
+          v[2 * e] = xe * cse.x - xo * cse.y;
+          v[2 * e + 1] = xe * cse.y + xo * cse.x;
         }
       }
-      if (TA_IDX_OK(p.err, to.row * pt.width + cc, 16, (long)p.pv.n_pages * p.pv.page_size * pt.width)) {
-        uint4* out = reinterpret_cast<uint4*>(pt.pool + to.row * pt.width + cc);
-        out[0] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-        out[1] = make_uint4(pack_bf16(v[8], v[9]), pack_bf16(v[10], v[11]), pack_bf16(v[12], v[13]), pack_bf16(v[14], v[15]));
+      // the rounded row into this thread's own place in the idle ring ...
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<uint4*>(ring + chunk_at(u - u0, rloc, e)) =
+            make_uint4(pack_bf16(v[8 * e], v[8 * e + 1]), pack_bf16(v[8 * e + 2], v[8 * e + 3]), pack_bf16(v[8 * e + 4], v[8 * e + 5]),
+                       pack_bf16(v[8 * e + 6], v[8 * e + 7]));
+      __syncwarp();
+      // ... and from there to the pages, the 64 bytes of eight rows per store instruction
+      bf16* pool = first ? p0.pool : p1.pool;
+      const int wd = first ? p0.width : p1.width, cc = (first ? c : c - p0.width) + (lane & 3) * 8;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int rr = i * 8 + lane / 4;
+        const long row = __shfl_sync(0xffffffffu, to.row, rr);
+        const uint4 w = *reinterpret_cast<const uint4*>(ring + chunk_at(u - u0, q * 32 + rr, lane & 3));
+        if (row >= 0 && TA_IDX_OK(p.err, row * wd + cc, 8, (long)p.pv.n_pages * p.pv.page_size * wd))
+          *reinterpret_cast<uint4*>(pool + row * wd + cc) = w;
       }
+    };
+#pragma unroll
+    for (int k = 0; k < CSU; ++k) {
+      const int u = u0 + hf + 2 * k;
+      if (u < u1 && warp_rows(u)) finish(u, true, cs[k]);
     }
+    for (int u = u0 + hf + 2 * CSU; u < u1; u += 2)
+      if (warp_rows(u)) finish(u, false, cs[0]);
   }
   tc_fence_before();
-  if (S > 1) {                       // nobody leaves while another CTA may still read its shared memory
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-  }
   __syncthreads();
   if (warp == 1) tmem_dealloc(tmem, ncols);
 }
 
 // How a call is divided: MT row tiles per CTA, S shares of d per cluster, and whether the two factors go to different CTAs.
 // The CTA's time is taken as proportional to the bytes it moves into shared memory, times the waves of one CTA per SM;
-// a share of d costs a pass of the partial sums through shared memory.
+// a share of d costs the partial sums once to the L2 cache and back.
 struct Plan {
   int MT, S, split_parts;
 };
@@ -248,9 +295,7 @@ inline Plan append_plan(int T, int d, int w0, int w1, int sms) {
       for (int S = 1; S <= MAX_S && S <= nkb; S *= 2) {
         const int width = split ? (w0 > w1 ? w0 : w1) : w0 + w1;
         const uint32_t cols = split ? acc_cols(width) : acc_cols(w0) + (w1 ? acc_cols(w1) : 0u);
-        const int units = mt * width / UC;
         if (mt > tiles || cols * mt > 512) continue;
-        if ((long)(units - units / S) * UNIT_BYTES > RING_BYTES && S > 1) continue;
         const long ctas = (long)((tiles + mt - 1) / mt) * S * (split ? 2 : 1);
         const long waves = (ctas + sms - 1) / sms;
         const int rows = T < mt * BM ? T : mt * BM;
@@ -259,6 +304,12 @@ inline Plan append_plan(int T, int d, int w0, int w1, int sms) {
         if (best_cost < 0 || cost < best_cost) { best_cost = cost; best = Plan{mt, S, split}; }
       }
   return best;
+}
+// Bytes of partial sums the plan needs.
+inline size_t append_part_bytes(const Plan& q, int T, int w0, int w1) {
+  if (q.S == 1) return 0;
+  const size_t clusters = ((size_t)T + q.MT * BM - 1) / (q.MT * BM);
+  return clusters * q.S * q.MT * BM * sizeof(float) * (q.split_parts ? 2 * (size_t)(w0 > w1 ? w0 : w1) : (size_t)w0 + w1);
 }
 
 }  // namespace append

@@ -88,6 +88,7 @@ size_t fast_paged_workspace(const tucker_attn_desc& d, int32_t prefix_len, bool 
 size_t fast_decode_workspace(const tucker_attn_desc& d, int32_t Lmax);
 int fast_decode(Problem& p);
 bool fast_append_supported(const tucker_attn_desc& d);
+size_t fast_append_workspace(const tucker_attn_desc& d, int32_t T, bool one_pool);
 int fast_append(Problem& p, const int32_t* tok_start, int32_t T);
 int wait_selftest(unsigned int* dev_err, int budget_us, int* out_dev, cudaStream_t stream);
 

@@ -832,6 +832,13 @@ bool fast_append_supported(const tucker_attn_desc& d) {
   return d.dtype == TA_DTYPE_BF16 && !(d.flags & TA_FLAG_FORCE_GENERIC) && ok32(d.r3) && ok32(d.t3) && d.d_model % 64 == 0;
 }
 
+static append::Plan plan_append(const tucker_attn_desc& d, int32_t T, bool one_pool) {
+  return append::append_plan(T, d.d_model, one_pool ? d.t3 : d.r3, one_pool ? 0 : d.t3, sm_count());
+}
+size_t fast_append_workspace(const tucker_attn_desc& d, int32_t T, bool one_pool) {
+  return append::append_part_bytes(plan_append(d, T, one_pool), T, one_pool ? d.t3 : d.r3, one_pool ? 0 : d.t3);
+}
+
 int fast_append(Problem& p, const int32_t* tok_start, int32_t T) {
   const tucker_attn_desc& d = p.d;
   append::Params ap = {};
@@ -841,9 +848,11 @@ int fast_append(Problem& p, const int32_t* tok_start, int32_t T) {
   const append::Part keys = {(bf16*)p.Kc, d.r3, d.rope ? 1 : 0}, values = {(bf16*)p.Vc, d.t3, 0};
   ap.part[0] = p.shared_kv ? values : keys;
   ap.part[1] = values;
-  const append::Plan plan = append::append_plan(T, d.d_model, ap.part[0].width, p.shared_kv ? 0 : d.t3, sm_count());
+  const append::Plan plan = plan_append(d, T, p.shared_kv);
   ap.S = plan.S; ap.MT = plan.MT;
   ap.n_parts = (p.shared_kv || plan.split_parts) ? 1 : 2;
+  ap.part_sums = reinterpret_cast<float*>(p.ws);
+  ap.y_units = plan.MT * ap.part[0].width / append::UC;
   CUtensorMap tmX, tm0, tm1;
   if (!tmap_2d(&tmX, p.X, (uint64_t)d.d_model, (uint64_t)T, (uint64_t)d.d_model, 64, append::BM)) return TA_ERR_CUDA;
   if (!tmap_2d(&tm1, p.Ut3, (uint64_t)d.t3, (uint64_t)d.d_model, (uint64_t)d.t3, 64, 64)) return TA_ERR_CUDA;

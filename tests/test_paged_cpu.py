@@ -31,9 +31,9 @@ def decode(lib, d=None, c=None, x=FAKE, w=FAKE, ut3=None, lens=FAKE, ptab=FAKE, 
     return lib.tucker_attn_decode_prefix(ctypes.byref(d), x, w, w, w, w, w, w, w, ut3, ctypes.byref(c), lens, ptab, plen, 1, y, ws, n, None)
 
 
-def append(lib, d=None, c=None, X=FAKE, U3=FAKE, Ut3=None, lens=FAKE, start=FAKE, T=5):
+def append(lib, d=None, c=None, X=FAKE, U3=FAKE, Ut3=None, lens=FAKE, start=FAKE, T=5, ws=FAKE, n=1 << 30):
     d, c = d or desc(), c or cache()
-    return lib.tucker_cache_append_paged(ctypes.byref(d), X, U3, Ut3 or ctypes.c_void_p(12288), ctypes.byref(c), lens, start, T, None)
+    return lib.tucker_cache_append_paged(ctypes.byref(d), X, U3, Ut3 or ctypes.c_void_p(12288), ctypes.byref(c), lens, start, T, ws, n, None)
 
 
 BAD_CACHES = [dict(K=None), dict(V=None), dict(table=None), dict(n_pages=0), dict(page_size=0), dict(max_pages=0), dict(page_size=-16),
@@ -59,12 +59,19 @@ def test_bad_decode_arguments(lib):
 
 
 def test_bad_append_arguments(lib):
-    for kw in (dict(X=None), dict(U3=None), dict(lens=None), dict(start=None), dict(T=-1), dict(X=ctypes.c_void_p(4104)),
+    for kw in (dict(X=None), dict(U3=None), dict(lens=None), dict(start=None), dict(T=-1), dict(ws=None), dict(ws=ctypes.c_void_p(4112)), dict(X=ctypes.c_void_p(4104)),
                dict(d=desc(pos0=-1)), dict(d=desc(pos0=(1 << 31) - 1)), dict(d=desc(r=(2, 16, 15)))):
         assert append(lib, **kw) == -1, kw
 
 
+    assert append(lib, n=16) == -3
+
+
 def test_workspace_queries(lib):
+    tokens = lambda d, T: lib.tucker_cache_append_paged_workspace_bytes(ctypes.byref(d), ctypes.byref(cache()), T)
+    assert tokens(desc(), 0) > 0 and tokens(desc(), 5) > 0 and tokens(desc(), -1) == 0 and tokens(desc(B=0), 5) == 0
+    big = desc(d_model=4096, n_H=32, r=(2, 128, 128), t=(2, 128, 128), dtype=Bd.TA_DTYPE_BF16)
+    assert tokens(big, 1000) > 1000 * 256 * 4                              # partial sums of the shares of d
     need = lambda d, c, p: lib.tucker_attn_decode_prefix_workspace_bytes(ctypes.byref(d), ctypes.byref(c), p)
     paged = lambda d, c: lib.tucker_attn_decode_paged_workspace_bytes(ctypes.byref(d), ctypes.byref(c))
     assert paged(desc(), cache()) == need(desc(), cache(), 0) > 0
