@@ -153,6 +153,8 @@ def _dtype_code(t) -> int:
 
 
 def _check(t, name, shape, dtype, device):
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.device == device and t.is_contiguous():
+        return
     if t.device != device or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor on {device}")
     if t.dtype != dtype:
@@ -184,7 +186,27 @@ def alloc_workspace(nbytes: int, device):
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
+class _on_device:
+    """`with torch.cuda.device(device)`, which costs several microseconds, only where another device is current."""
+    __slots__ = ("ctx",)
+
+    def __init__(self, device):
+        cuda = _torch().cuda
+        self.ctx = None if cuda.current_device() == device.index else cuda.device(device)
+
+    def __enter__(self):
+        if self.ctx is not None:
+            self.ctx.__enter__()
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+
+
 def _stream_ptr(device) -> int:
+    raw = getattr(_torch()._C, "_cuda_getCurrentRawStream", None)      # the handle alone, without a Stream object around it
+    if raw is not None and device.index is not None:
+        return int(raw(device.index))
     return int(_torch().cuda.current_stream(device).cuda_stream)
 
 
@@ -356,7 +378,7 @@ def tucker_cache_append_paged(X, U3, Ut3, Kpages, Vpages, block_table, cache_len
     if workspace is None:
         workspace = alloc_workspace(lib.tucker_cache_append_paged_workspace_bytes(ctypes.byref(desc), ctypes.byref(cache), int(T)), dev)
     _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
-    with torch.cuda.device(dev):
+    with _on_device(dev):
         rc = lib.tucker_cache_append_paged(ctypes.byref(desc), X.data_ptr(), U3.data_ptr(), Ut3.data_ptr(), ctypes.byref(cache),
                                            cache_len.data_ptr(), tok_start.data_ptr(), int(T), workspace.data_ptr(),
                                            workspace.numel(), _stream_ptr(dev))
@@ -396,7 +418,7 @@ def tucker_attn_decode_prefix(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kpages, Vpage
         workspace = alloc_workspace(lib.tucker_attn_decode_prefix_workspace_bytes(ctypes.byref(desc), ctypes.byref(cache),
                                                                                   prefix_len), dev)
     _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
-    with torch.cuda.device(dev):
+    with _on_device(dev):
         rc = lib.tucker_attn_decode_prefix(ctypes.byref(desc), x.data_ptr(), C.data_ptr(), U1.data_ptr(), U2.data_ptr(),
                                            U3.data_ptr(), Ct.data_ptr(), Ut1.data_ptr(), Ut2.data_ptr(), Ut3.data_ptr(),
                                            ctypes.byref(cache), cache_len.data_ptr(),

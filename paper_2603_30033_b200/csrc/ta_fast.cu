@@ -243,7 +243,8 @@ int launch_gemm(Problem& p, const bf16* A, long lda, int M, int K, const BOperan
   CUtensorMap tmA, tmB[3];
   if (!tmap_2d(&tmA, A, (uint64_t)K, (uint64_t)M, (uint64_t)lda, 64, 128)) return TA_ERR_CUDA;
   for (int i = 0; i < 3; ++i) {
-    const BOperand& b = bops[i < nb ? i : 0];
+    if (i >= nb) { tmB[i] = tmB[0]; continue; }
+    const BOperand& b = bops[i];
     if (!gp.b_mn_major) {
       // with b_kb_wrap B has fewer columns than A (its row pitch, which is then its width)
       if (!tmap_2d(&tmB[i], b.ptr, gp.b_kb_wrap > 0 ? (uint64_t)b.ld : (uint64_t)K, (uint64_t)b.n, (uint64_t)b.ld, 64, (uint32_t)BN)) return TA_ERR_CUDA;

@@ -17,17 +17,17 @@ using fma::ld;
 using fma::st;
 
 // ---------------------------------------------------------------------------------------
-// 32 x 32 tile of A [M, K] B [K, N], fp32 accumulation.  256 threads: four groups of 64 threads take a quarter of every
-// 64-deep K block each (4 x 4 outputs per thread) and are summed through shared memory at the end, so that the short
-// and narrow products of a decode step (few rows, K = d) have four times the threads a plain tile would.  The next
-// K block is in registers while the current one is multiplied.
+// 32 x 32 tile of A [M, K] B [K, N], fp32 accumulation.  512 threads: eight groups of 64 threads take an eighth of every
+// 128-deep K block each (4 x 4 outputs per thread) and are summed through shared memory at the end, so that the short
+// and narrow products of a decode step (few rows, K = d) have eight times the threads a plain tile would and a round trip
+// to memory covers 128 of K.  The next K block is in registers while the current one is multiplied.
 // ---------------------------------------------------------------------------------------
-constexpr int GM = 32, GN = 32, GK = 64;
+constexpr int GM = 32, GN = 32, GK = 128, GG = 8, GT = 64 * GG;
 
 struct TileSmem {
   union {
     struct { float a[GK][GM + 1], b[GK][GN + 1]; } in;
-    float part[4][GM][GN + 1];
+    float part[GG][GM][GN + 1];
   };
 };
 
@@ -45,7 +45,7 @@ __device__ __forceinline__ void gemm_tile(const TA* __restrict__ A, long lda, co
   auto fetch = [&](int k0) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int idx = tid + i * 256;
+      const int idx = tid + i * GT;
       const int m = idx / GK, k = k0 + idx % GK;
       ra[i] = (m0 + m < M && k < K) ? ld(A + (long)(m0 + m) * lda + k) : 0.f;
       const int n = sb.sn == 1 ? idx % GN : idx / GK, kb = k0 + (sb.sn == 1 ? idx / GN : idx % GK);
@@ -56,7 +56,7 @@ __device__ __forceinline__ void gemm_tile(const TA* __restrict__ A, long lda, co
   for (int k0 = 0; k0 < K; k0 += GK) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int idx = tid + i * 256;
+      const int idx = tid + i * GT;
       s.in.a[idx % GK][idx / GK] = ra[i];
       if (sb.sn == 1) s.in.b[idx / GN][idx % GN] = rb[i];
       else s.in.b[idx % GK][idx / GK] = rb[i];
@@ -64,8 +64,8 @@ __device__ __forceinline__ void gemm_tile(const TA* __restrict__ A, long lda, co
     __syncthreads();
     if (k0 + GK < K) fetch(k0 + GK);
 #pragma unroll
-    for (int kk = 0; kk < GK / 4; ++kk) {
-      const int k = grp * (GK / 4) + kk;
+    for (int kk = 0; kk < GK / GG; ++kk) {
+      const int k = grp * (GK / GG) + kk;
       float a[4], b[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) { a[i] = s.in.a[k][ty * 4 + i]; b[i] = s.in.b[k][tx * 4 + i]; }
@@ -81,9 +81,11 @@ __device__ __forceinline__ void gemm_tile(const TA* __restrict__ A, long lda, co
 #pragma unroll
     for (int j = 0; j < 4; ++j) s.part[grp][ty * 4 + i][tx * 4 + j] = acc[i][j];
   __syncthreads();
-  for (int i = tid; i < GM * GN; i += 256) {
-    float* c = &s.part[0][i / GN][i % GN];
-    *c = (s.part[0][i / GN][i % GN] + s.part[1][i / GN][i % GN]) + (s.part[2][i / GN][i % GN] + s.part[3][i / GN][i % GN]);
+  for (int i = tid; i < GM * GN; i += GT) {
+    float c = 0.f;
+#pragma unroll
+    for (int g = 0; g < GG; ++g) c += s.part[g][i / GN][i % GN];
+    s.part[0][i / GN][i % GN] = c;       // read above by this thread only
   }
   __syncthreads();
 }
@@ -105,13 +107,13 @@ struct GemmArgs {
   GemmPart<TB, TC> part[3];
 };
 template <typename TA, typename TB, typename TC>
-__global__ void __launch_bounds__(256) k_pg_gemm(const GemmArgs<TA, TB, TC> g) {
+__global__ void __launch_bounds__(GT) k_pg_gemm(const GemmArgs<TA, TB, TC> g) {
   __shared__ TileSmem s;
   const GemmPart<TB, TC> pt = g.part[blockIdx.z];
   const int m0 = blockIdx.x * GM, n0 = blockIdx.y * GN;
   if (n0 >= pt.N) return;
   gemm_tile(g.A, g.lda, pt.B, pt.sb, g.M, pt.N, g.K, m0, n0, s);
-  for (int i = threadIdx.x; i < GM * GN; i += 256) {
+  for (int i = threadIdx.x; i < GM * GN; i += GT) {
     const int m = m0 + i / GN, n = n0 + i % GN;
     if (m < g.M && n < pt.N) st(pt.C + (long)m * pt.ldc + n, s.part[0][i / GN][i % GN]);
   }
@@ -136,7 +138,7 @@ struct AppendArgs {
   unsigned int* err;
 };
 template <typename T>
-__global__ void __launch_bounds__(256) k_pg_append(const AppendArgs<T> g) {
+__global__ void __launch_bounds__(GT) k_pg_append(const AppendArgs<T> g) {
   __shared__ TileSmem s;
   __shared__ long row_s[GM];
   __shared__ int pos_s[GM];
@@ -158,7 +160,7 @@ __global__ void __launch_bounds__(256) k_pg_append(const AppendArgs<T> g) {
   MatB sb = {r, 1};
   gemm_tile(g.X, (long)g.d, is_k ? g.U3 : g.Ut3, sb, g.T_, r, g.d, m0, n0, s);
   T* pool = is_k ? g.K : g.V;
-  for (int i = threadIdx.x; i < GM * GN; i += 256) {
+  for (int i = threadIdx.x; i < GM * GN; i += GT) {
     const int m = i / GN, c = i % GN, n = n0 + c;
     if (row_s[m] < 0 || n >= r) continue;
     float v = s.part[0][m][c];
@@ -168,6 +170,34 @@ __global__ void __launch_bounds__(256) k_pg_append(const AppendArgs<T> g) {
       v = (c & 1) ? other * cs.y + v * cs.x : v * cs.x - other * cs.y;
     }
     if (TA_IDX_OK(g.err, row_s[m] * r + n, 1, (long)g.pv.n_pages * g.pv.page_size * r)) st(pool + row_s[m] * r + n, v);
+  }
+}
+
+// w[a, b, c] = sum_q qt[b, q] C[a, q, c].  A block forms 32 columns of one slice for four sequences: thread (c, g) of 32 x 8 walks
+// the rows q = g, g + 8, ..., the eight sums per column are joined through shared memory.
+constexpr int WB = 4;
+template <typename T>
+__global__ void __launch_bounds__(256) k_pg_w(const float* __restrict__ qt, const T* __restrict__ C, float* __restrict__ w, int B, int r1,
+                                              int r2, int r3) {
+  __shared__ float red[8][WB][32];
+  const int b0 = blockIdx.x * WB, a = blockIdx.y, c = blockIdx.z * 32 + threadIdx.x % 32, g = threadIdx.x / 32;
+  float acc[WB] = {};
+  if (c < r3)
+#pragma unroll 4
+    for (int q = g; q < r2; q += 8) {
+      const float v = ld(C + ((long)a * r2 + q) * r3 + c);
+#pragma unroll
+      for (int i = 0; i < WB; ++i)
+        if (b0 + i < B) acc[i] = fmaf(qt[(long)(b0 + i) * r2 + q], v, acc[i]);
+    }
+#pragma unroll
+  for (int i = 0; i < WB; ++i) red[g][i][threadIdx.x % 32] = acc[i];
+  __syncthreads();
+  if (g < WB && b0 + g < B && c < r3) {
+    float t = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) t += red[k][g][threadIdx.x % 32];
+    w[((long)a * B + b0 + g) * r3 + c] = t;
   }
 }
 
@@ -197,6 +227,7 @@ __global__ void __launch_bounds__(256) k_pg_queries(const float* __restrict__ w,
   for (int i = blockIdx.y * blockDim.x + threadIdx.x; i < nH * half; i += gridDim.y * blockDim.x) {
     const int h = i / half, c = 2 * (i % half);
     float xe = 0.f, xo = 0.f;
+#pragma unroll 4
     for (int a = 0; a < r1; ++a) {
       const float u = ld(U1 + (long)h * r1 + a);
       const float* wr = w + ((long)a * B + b) * r3 + c;
@@ -259,7 +290,42 @@ struct AttnArgs {
   float *part_o, *part_ml; // [z * rows_per_z + row][splits][t3] / [..][splits][2]
   unsigned int* err;
 };
-template <typename T>
+__device__ __forceinline__ float4 ld4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 ld4(const bf16* p) {
+  const uint2 v = *reinterpret_cast<const uint2*>(p);
+  const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.x));
+  const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.y));
+  return make_float4(a.x, a.y, b.x, b.y);
+}
+
+// Rows of a tile to shared memory, zero-padded to the pitch.  VEC: r is a multiple of 4, so that rows can be read four
+// elements at a time (a tile's loads are then in flight together instead of one after another).
+template <bool VEC, typename T>
+__device__ __forceinline__ void load_rows(float* __restrict__ out, const T* __restrict__ pool, const float* __restrict__ fresh,
+                                          const long* __restrict__ rows_s, int r, int pitch) {
+  if (VEC) {
+    const int n4 = pitch / 4;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < AK * n4; i += 256) {
+      const int j = i / n4, c = (i - j * n4) * 4;
+      const long rw = rows_s[j];
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (c < r) {
+        if (rw == -2) v = ld4(fresh + c);
+        else if (rw >= 0) v = ld4(pool + rw * r + c);
+      }
+      *reinterpret_cast<float4*>(out + j * pitch + c) = v;
+    }
+  } else {
+    for (int i = threadIdx.x; i < AK * pitch; i += 256) {
+      const int j = i / pitch, c = i - j * pitch;
+      const long rw = rows_s[j];
+      out[i] = c >= r ? 0.f : (rw == -2 ? fresh[c] : (rw >= 0 ? ld(pool + rw * r + c) : 0.f));
+    }
+  }
+}
+
+template <bool VEC, typename T>
 __global__ void __launch_bounds__(256) k_pg_attn(const AttnArgs<T> g) {
   extern __shared__ __align__(16) float sm[];
   __shared__ double theta_s[kMaxPairs];
@@ -301,31 +367,22 @@ __global__ void __launch_bounds__(256) k_pg_attn(const AttnArgs<T> g) {
       rows_s[tid] = s >= limit ? -1 : (g.cache_len && s == L ? -2 : paged_row(table, s, g.pv, g.err));
     }
     __syncthreads();
-    for (int i = tid; i < AK * rp; i += 256) {
-      const int j = i / rp, c = i % rp;
-      const long rw = rows_s[j];
-      float v = 0.f;
-      if (c < g.r3) {
-        if (rw == -2) v = g.knew[(long)z * g.r3 + c];
-        else if (rw >= 0) {
-          v = ld(g.K + rw * g.r3 + c);
-          if (g.rotate_keys) {          // one pool with latent RoPE: the key is the cached row, rotated
-            const float other = ld(g.K + rw * g.r3 + (c ^ 1));
-            const float2 cs = dec::rope_cos_sin_theta(g.pos_base + k0 + j, theta_s[c >> 1]);
-            v = (c & 1) ? other * cs.y + v * cs.x : v * cs.x - other * cs.y;
-          }
-        }
-      }
-      Ks[i] = v;
-    }
-    for (int i = tid; i < AK * tp; i += 256) {
-      const int j = i / tp, c = i % tp;
-      const long rw = rows_s[j];
-      float v = 0.f;
-      if (c < g.t3) v = rw == -2 ? g.vnew[(long)z * g.t3 + c] : (rw >= 0 ? ld(g.V + rw * g.t3 + c) : 0.f);
-      Vs[i] = v;
-    }
+    load_rows<VEC>(Ks, g.K, g.knew + (long)z * g.r3, rows_s, g.r3, rp);
+    load_rows<VEC>(Vs, g.V, g.vnew + (long)z * g.t3, rows_s, g.t3, tp);
     __syncthreads();
+    if (g.rotate_keys) {                // one pool with latent RoPE: the key is the cached row, rotated (the new token's is already)
+      const int half = g.r3 / 2;
+      for (int i = tid; i < AK * half; i += 256) {
+        const int j = i / half, c = i - j * half;
+        if (rows_s[j] < 0) continue;
+        const float2 cs = dec::rope_cos_sin_theta(g.pos_base + k0 + j, theta_s[c]);
+        float* px = Ks + j * rp + 2 * c;
+        const float xe = px[0], xo = px[1];
+        px[0] = xe * cs.x - xo * cs.y;
+        px[1] = xe * cs.y + xo * cs.x;
+      }
+      __syncthreads();
+    }
     float s0 = 0.f, s1 = 0.f;
     const float4* q4 = reinterpret_cast<const float4*>(qs + r * rp);
     const float4* ka = reinterpret_cast<const float4*>(Ks + l * rp);
@@ -381,37 +438,60 @@ __global__ void __launch_bounds__(256) k_pg_attn(const AttnArgs<T> g) {
 }
 
 // ---------------------------------------------------------------------------------------
-// o[b, h] from the partials of its own keys (splits_o) and of the prefix (splits_p, may be 0), one warp per (b, h).
+// o[b, h] from the partials of its own keys (splits_o) and of the prefix (splits_p, may be 0).  A block per (b, h); the partials are
+// dealt over its eight warps, whose sums are joined in order.
 // ---------------------------------------------------------------------------------------
+constexpr int kMaxSplits = 128;       // of either kind, see pick_splits
 __global__ void __launch_bounds__(256) k_pg_merge(const float* __restrict__ po, const float* __restrict__ ml, int splits_o,
                                                   const float* __restrict__ po_p, const float* __restrict__ ml_p, int splits_p,
-                                                  float* __restrict__ o, int rows, int t3) {
-  const int row = blockIdx.x * 8 + threadIdx.x / 32, lane = threadIdx.x % 32;
-  if (row >= rows) return;
-  const float2* a = reinterpret_cast<const float2*>(ml) + (long)row * splits_o;
-  const float2* p = reinterpret_cast<const float2*>(ml_p) + (long)row * splits_p;
-  const int n = splits_o + splits_p;
-  float m = -INFINITY;
-  for (int i = lane; i < n; i += 32) m = fmaxf(m, i < splits_o ? a[i].x : p[i - splits_o].x);
+                                                  float* __restrict__ o, int t3) {
+  __shared__ float w_s[2 * kMaxSplits], red_s[8], acc_s[8][64];
+  const long row = blockIdx.x;
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const float2* a = reinterpret_cast<const float2*>(ml) + row * splits_o;
+  const float2* p = reinterpret_cast<const float2*>(ml_p) + row * splits_p;
+  const int n = splits_o + splits_p;    // at most 256: one partial per thread
+  const float2 v = tid < n ? (tid < splits_o ? a[tid] : p[tid - splits_o]) : make_float2(-INFINITY, 0.f);
+  float m = v.x;
 #pragma unroll
   for (int d = 16; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-  float l = 0.f;                        // the new token's share holds a key: m is finite
-  for (int i = lane; i < n; i += 32) {
-    const float2 v = i < splits_o ? a[i] : p[i - splits_o];
-    l += v.y * expf(v.x - m);
-  }
+  if (lane == 0) red_s[warp] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, red_s[i]);      // the new token's share holds a key: finite
+  const float wt = v.y > 0.f ? expf(v.x - m) : 0.f;        // a share without keys wrote no output
+  if (tid < n) w_s[tid] = wt;
+  float l = v.y * wt;
 #pragma unroll
   for (int d = 16; d >= 1; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+  __syncthreads();                      // red_s is read above
+  if (lane == 0) red_s[warp] = l;
+  __syncthreads();
+  l = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) l += red_s[i];
   const float inv = 1.f / l;
-  for (int c = lane; c < t3; c += 32) {
-    float acc = 0.f;
-    for (int i = 0; i < n; ++i) {
-      const float2 v = i < splits_o ? a[i] : p[i - splits_o];
-      if (v.y > 0.f)                    // a share without keys wrote no output
-        acc = fmaf(expf(v.x - m), i < splits_o ? po[((long)row * splits_o + i) * t3 + c]
-                                               : po_p[((long)row * splits_p + (i - splits_o)) * t3 + c], acc);
+  for (int c0 = 0; c0 < t3; c0 += 64) { // 64 columns at a time, two per lane
+    float s0 = 0.f, s1 = 0.f;
+    const int c = c0 + lane;
+#pragma unroll 4
+    for (int i = warp; i < n; i += 8) {
+      const float wi = w_s[i];
+      if (wi == 0.f) continue;
+      const float* src = i < splits_o ? po + (row * splits_o + i) * t3 : po_p + (row * splits_p + (i - splits_o)) * t3;
+      if (c < t3) s0 = fmaf(wi, src[c], s0);
+      if (c + 32 < t3) s1 = fmaf(wi, src[c + 32], s1);
     }
-    o[(long)row * t3 + c] = acc * inv;
+    acc_s[warp][lane] = s0;
+    acc_s[warp][lane + 32] = s1;
+    __syncthreads();
+    if (tid < 64 && c0 + tid < t3) {
+      float t = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t += acc_s[i][tid];
+      o[row * t3 + c0 + tid] = t * inv;
+    }
+    __syncthreads();
   }
 }
 
@@ -423,6 +503,7 @@ __global__ void __launch_bounds__(256) k_pg_u(const float* __restrict__ o, const
   for (long i = blockIdx.x * 256L + threadIdx.x; i < total; i += gridDim.x * 256L) {
     const int c = (int)(i % t3), a = (int)((i / t3) % t1), b = (int)(i / ((long)t3 * t1));
     float acc = 0.f;
+#pragma unroll 4
     for (int h = 0; h < nH; ++h) acc = fmaf(ld(Ut1 + (long)h * t1 + a), o[((long)b * nH + h) * t3 + c], acc);
     u[i] = acc;
   }
@@ -433,8 +514,12 @@ __global__ void __launch_bounds__(256) k_pg_z(const float* __restrict__ u, const
   const int b = blockIdx.y, j = blockIdx.x * 8 + threadIdx.x / 32, lane = threadIdx.x % 32;
   if (j >= t2) return;
   float acc = 0.f;
-  for (int a = 0; a < t1; ++a)
-    for (int c = lane; c < t3; c += 32) acc = fmaf(ld(Ct + ((long)a * t2 + j) * t3 + c), u[((long)b * t1 + a) * t3 + c], acc);
+  const float* ub = u + (long)b * t1 * t3;
+#pragma unroll 8
+  for (int i = lane; i < t1 * t3; i += 32) {
+    const int a = i / t3, c = i - a * t3;
+    acc = fmaf(ld(Ct + ((long)a * t2 + j) * t3 + c), ub[i], acc);
+  }
 #pragma unroll
   for (int d = 16; d >= 1; d >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, d);
   if (lane == 0) z[(long)b * t2 + j] = acc;
@@ -449,7 +534,7 @@ bool shape_ok(const tucker_attn_desc& d) {
 // Shares per list of keys: about two blocks per SM, no more than there are tiles.
 int pick_splits(long blocks, long keys) {
   const long tiles = (keys + AK - 1) / AK;
-  return (int)std::max<long>(1, std::min<long>(std::min<long>(tiles, 128), (2 * 148 + blocks - 1) / blocks));
+  return (int)std::max<long>(1, std::min<long>(std::min<long>(tiles, kMaxSplits), (2 * 148 + blocks - 1) / blocks));
 }
 int own_splits(const tucker_attn_desc& d, int64_t Lmax) { return pick_splits((long)d.B * ((d.n_H + AR - 1) / AR), Lmax); }
 int prefix_splits(const tucker_attn_desc& d, int32_t P) { return P > 0 ? pick_splits(((long)d.B * d.n_H + AR - 1) / AR, P) : 0; }
@@ -479,7 +564,7 @@ size_t carve(const tucker_attn_desc& d, int64_t Lmax, int32_t P, char* base, Ws*
 
 template <typename TA, typename TB, typename TC>
 int launch_gemm(Problem& p, const GemmArgs<TA, TB, TC>& g, int parts, int max_n) {
-  k_pg_gemm<TA, TB, TC><<<dim3((g.M + GM - 1) / GM, (max_n + GN - 1) / GN, parts), 256, 0, p.stream>>>(g);
+  k_pg_gemm<TA, TB, TC><<<dim3((g.M + GM - 1) / GM, (max_n + GN - 1) / GN, parts), GT, 0, p.stream>>>(g);
   TA_LAUNCH_CHECK(p);
   return TA_OK;
 }
@@ -487,8 +572,9 @@ int launch_gemm(Problem& p, const GemmArgs<TA, TB, TC>& g, int parts, int max_n)
 template <typename T>
 int attn(Problem& p, const AttnArgs<T>& g, int zs) {
   const size_t smem = pg_attn_smem(g.r3, g.t3);
-  TA_CUDA_TRY(cudaFuncSetAttribute(k_pg_attn<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  k_pg_attn<T><<<dim3((g.rows_per_z + AR - 1) / AR, g.splits, zs), 256, smem, p.stream>>>(g);
+  const auto kernel = (g.r3 % 4 == 0 && g.t3 % 4 == 0) ? k_pg_attn<true, T> : k_pg_attn<false, T>;
+  TA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  kernel<<<dim3((g.rows_per_z + AR - 1) / AR, g.splits, zs), 256, smem, p.stream>>>(g);
   TA_LAUNCH_CHECK(p);
   return TA_OK;
 }
@@ -508,12 +594,8 @@ int decode_typed(Problem& p) {
     g.part[2] = {(const T*)p.Ut3, {d.t3, 1}, w.vnew, d.t3, d.t3};
     if ((rc = launch_gemm(p, g, 3, std::max(d.r2, std::max(d.r3, d.t3))))) return rc;
   }
-  {
-    // w[a] = qt C[a], all a in one launch
-    fma::GemmShape g = fma::plain(d.B, d.r3, d.r2, d.r2, d.r3, 1, d.r3);
-    g.Z2 = d.r1; g.b2 = (long)d.r2 * d.r3; g.c2 = (long)d.B * d.r3;
-    if ((rc = fma::gemm(p, w.qt, (const T*)p.C, w.w, g, d.r1))) return rc;
-  }
+  k_pg_w<T><<<dim3((d.B + WB - 1) / WB, d.r1, (d.r3 + 31) / 32), 256, 0, p.stream>>>(w.qt, (const T*)p.C, w.w, d.B, d.r1, d.r2, d.r3);
+  TA_LAUNCH_CHECK(p);
   k_pg_queries<T><<<dim3(d.B, std::max(1, std::min(8, 296 / d.B))), 256, 0, p.stream>>>(
       w.w, (const T*)p.U1, w.qhat, w.knew, w.vnew, (T*)p.Kc, (T*)p.Vc, p.pv, p.cache_len, d.B, d.n_H, d.r1, d.r3, d.t3, p.Lmax, P,
       p.scale, d.rope, (double)d.rope_base, p.append, p.shared_kv, p.shared_rope, p.dev_err);
@@ -534,7 +616,7 @@ int decode_typed(Problem& p) {
   }
   prof_end(p);
   const int rows = d.B * d.n_H;
-  k_pg_merge<<<(rows + 7) / 8, 256, 0, p.stream>>>(w.po, w.ml, own_splits(d, p.Lmax), w.po_p, w.ml_p, sp, w.o, rows, d.t3);
+  k_pg_merge<<<rows, 256, 0, p.stream>>>(w.po, w.ml, own_splits(d, p.Lmax), w.po_p, w.ml_p, sp, w.o, d.t3);
   TA_LAUNCH_CHECK(p);
   k_pg_u<T><<<(int)std::min<long>(148 * 8, ((long)d.B * d.t1 * d.t3 + 255) / 256), 256, 0, p.stream>>>(w.o, (const T*)p.Ut1, w.u, d.B,
                                                                                                       d.n_H, d.t1, d.t3);
@@ -556,7 +638,7 @@ int append_typed(Problem& p, const int32_t* tok_start, int32_t T_) {
   g.B = d.B; g.T_ = T_; g.d = d.d_model; g.r3 = d.r3; g.t3 = d.t3; g.rope = d.rope; g.pos0 = d.pos0;
   g.keys_shared = p.shared_kv; g.base = (double)d.rope_base; g.err = p.dev_err;
   const int wide = p.shared_kv ? d.t3 : std::max(d.r3, d.t3);
-  k_pg_append<T><<<dim3((T_ + GM - 1) / GM, (wide + GN - 1) / GN, p.shared_kv ? 1 : 2), 256, 0, p.stream>>>(g);
+  k_pg_append<T><<<dim3((T_ + GM - 1) / GM, (wide + GN - 1) / GN, p.shared_kv ? 1 : 2), GT, 0, p.stream>>>(g);
   TA_LAUNCH_CHECK(p);
   return TA_OK;
 }
