@@ -18,6 +18,14 @@ typedef __nv_bfloat16 bf16;
 // Device address of the current device's error word (nullptr if it cannot be resolved); ta_api.cu.
 unsigned int* device_error_word();
 
+namespace dec {
+// Rotation frequencies theta_i = base^(-2 i / r), i < r / 2 <= 128, computed on the host in double
+// precision and passed to the kernels by value.
+struct RopeFreqs {
+  double theta[128];
+};
+}  // namespace dec
+
 // A paged latent cache as the kernels see it (the pools themselves travel as Problem::Kc / Vc).
 struct PagedView {
   const int32_t* table;     // [B, max_pages]
@@ -67,6 +75,9 @@ struct Carver {
     return base ? reinterpret_cast<T*>(base + o) : nullptr;
   }
 };
+
+// theta_i = base^(-2 i / r3) in double precision for the first 128 pairs (ta_fast.cu); zeros without RoPE
+dec::RopeFreqs rope_freqs(const tucker_attn_desc& d);
 
 // shape-generic FMA path (ta_generic.cu)
 size_t generic_fwd_workspace(const tucker_attn_desc& d);

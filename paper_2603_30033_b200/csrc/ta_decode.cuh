@@ -74,12 +74,6 @@ __device__ __forceinline__ long block_tile_scan(const int32_t* __restrict__ cach
   return (long)total;
 }
 
-// Rotation frequencies theta_i = base^(-2 i / r), i < r / 2 <= 128, computed on the host in double
-// precision and passed to the kernels by value.
-struct RopeFreqs {
-  double theta[128];
-};
-
 // (cos, sin) of pos * base^(-2 i / r).  The angle is formed in double precision (positions of
 // tens of thousands would lose ~1e-3 rad in fp32), reduced to a fraction of a turn in double,
 // and only then handed to the fp32 sincospi.  log2_base = log2(base).

@@ -23,6 +23,16 @@
 #include <algorithm>
 
 namespace ta {
+
+// theta_i = base^(-2 i / r3) in double precision, i < r3 / 2; the first 128 (all of them on the tensor-core path)
+dec::RopeFreqs rope_freqs(const tucker_attn_desc& d) {
+  dec::RopeFreqs f;
+  const int half = d.r3 / 2;
+  for (int i = 0; i < 128; ++i)
+    f.theta[i] = (d.rope && i < half) ? pow((double)d.rope_base, -2.0 * (double)i / (double)d.r3) : 0.0;
+  return f;
+}
+
 namespace {
 
 // ---- driver entry point for tensor-map creation (no link-time dependency on libcuda) --------
@@ -169,15 +179,6 @@ __global__ void __launch_bounds__(PREP_THREADS) k_prefill_prep(const PrepParams 
       if (TA_IDX_OK(p.err, o, 1, total)) p.rope[o] = make_float4(c0.x, c0.y, c1.x, c1.y);
     }
   }
-}
-
-// theta_i = base^(-2 i / r3) in double precision, i < r3 / 2 (r3 <= 256 on this path)
-dec::RopeFreqs rope_freqs(const tucker_attn_desc& d) {
-  dec::RopeFreqs f;
-  const int half = d.r3 / 2;
-  for (int i = 0; i < 128; ++i)
-    f.theta[i] = (d.rope && i < half) ? pow((double)d.rope_base, -2.0 * (double)i / (double)d.r3) : 0.0;
-  return f;
 }
 
 bool umma_attention_ok(const tucker_attn_desc& d) { return d.r3 <= 128 && d.t3 <= 128; }

@@ -35,10 +35,10 @@ struct MatB {              // element (k, n) at k * sk + n * sn
   long sk, sn;
 };
 
-// On return s.part[0] holds the tile (rows and columns past the edge are zero); all threads are synchronised.
+// K blocks [k_beg, K).  On return s.part[0] holds the tile (rows and columns past the edge are zero); all threads are synchronised.
 template <typename TA, typename TB>
-__device__ __forceinline__ void gemm_tile(const TA* __restrict__ A, long lda, const TB* __restrict__ Bm, MatB sb, int M, int N, int K,
-                                          int m0, int n0, TileSmem& s) {
+__device__ __forceinline__ void gemm_tile(const TA* __restrict__ A, long lda, const TB* __restrict__ Bm, MatB sb, int M, int N, int k_beg,
+                                          int K, int m0, int n0, TileSmem& s) {
   const int tid = threadIdx.x, grp = tid / 64, tx = tid % 8, ty = (tid % 64) / 8;
   float acc[4][4] = {};
   float ra[8], rb[8];
@@ -52,8 +52,8 @@ __device__ __forceinline__ void gemm_tile(const TA* __restrict__ A, long lda, co
       rb[i] = (n0 + n < N && kb < K) ? ld(Bm + (long)kb * sb.sk + (long)(n0 + n) * sb.sn) : 0.f;
     }
   };
-  fetch(0);
-  for (int k0 = 0; k0 < K; k0 += GK) {
+  fetch(k_beg);
+  for (int k0 = k_beg; k0 < K; k0 += GK) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int idx = tid + i * GT;
@@ -90,7 +90,8 @@ __device__ __forceinline__ void gemm_tile(const TA* __restrict__ A, long lda, co
   __syncthreads();
 }
 
-// C [M, N] (ld ldc) = A B for up to three (B, C) pairs that share A and K: blockIdx.z picks the pair.
+// C [M, N] (ld ldc) = A B for up to three (B, C) pairs that share A and K: blockIdx.z = share of K * pairs + pair.  The shares'
+// products lie `split` elements apart and are added up by whoever reads them.
 template <typename TB, typename TC>
 struct GemmPart {
   const TB* B;
@@ -98,24 +99,27 @@ struct GemmPart {
   TC* C;
   long ldc;
   int N;
+  long split;
 };
 template <typename TA, typename TB, typename TC>
 struct GemmArgs {
   const TA* A;
   long lda;
-  int M, K;
+  int M, K, parts, kb_per_split;   // kb_per_split: GK-deep blocks of K per share
   GemmPart<TB, TC> part[3];
 };
 template <typename TA, typename TB, typename TC>
 __global__ void __launch_bounds__(GT) k_pg_gemm(const GemmArgs<TA, TB, TC> g) {
+  pdl_enter();
   __shared__ TileSmem s;
-  const GemmPart<TB, TC> pt = g.part[blockIdx.z];
+  const GemmPart<TB, TC> pt = g.part[blockIdx.z % g.parts];
+  const int share = blockIdx.z / g.parts, k_beg = share * g.kb_per_split * GK;
   const int m0 = blockIdx.x * GM, n0 = blockIdx.y * GN;
   if (n0 >= pt.N) return;
-  gemm_tile(g.A, g.lda, pt.B, pt.sb, g.M, pt.N, g.K, m0, n0, s);
+  gemm_tile(g.A, g.lda, pt.B, pt.sb, g.M, pt.N, k_beg, min(g.K, k_beg + g.kb_per_split * GK), m0, n0, s);
   for (int i = threadIdx.x; i < GM * GN; i += GT) {
     const int m = m0 + i / GN, n = n0 + i % GN;
-    if (m < g.M && n < pt.N) st(pt.C + (long)m * pt.ldc + n, s.part[0][i / GN][i % GN]);
+    if (m < g.M && n < pt.N) st(pt.C + share * pt.split + (long)m * pt.ldc + n, s.part[0][i / GN][i % GN]);
   }
 }
 
@@ -139,6 +143,7 @@ struct AppendArgs {
 };
 template <typename T>
 __global__ void __launch_bounds__(GT) k_pg_append(const AppendArgs<T> g) {
+  pdl_enter();
   __shared__ TileSmem s;
   __shared__ long row_s[GM];
   __shared__ int pos_s[GM];
@@ -158,7 +163,7 @@ __global__ void __launch_bounds__(GT) k_pg_append(const AppendArgs<T> g) {
     pos_s[threadIdx.x] = dst.pos;
   }
   MatB sb = {r, 1};
-  gemm_tile(g.X, (long)g.d, is_k ? g.U3 : g.Ut3, sb, g.T_, r, g.d, m0, n0, s);
+  gemm_tile(g.X, (long)g.d, is_k ? g.U3 : g.Ut3, sb, g.T_, r, 0, g.d, m0, n0, s);
   T* pool = is_k ? g.K : g.V;
   for (int i = threadIdx.x; i < GM * GN; i += GT) {
     const int m = i / GN, c = i % GN, n = n0 + c;
@@ -177,9 +182,20 @@ __global__ void __launch_bounds__(GT) k_pg_append(const AppendArgs<T> g) {
 // the rows q = g, g + 8, ..., the eight sums per column are joined through shared memory.
 constexpr int WB = 4;
 template <typename T>
-__global__ void __launch_bounds__(256) k_pg_w(const float* __restrict__ qt, const T* __restrict__ C, float* __restrict__ w, int B, int r1,
-                                              int r2, int r3) {
+__global__ void __launch_bounds__(256) k_pg_w(const float* __restrict__ qt_parts, int shares, const T* __restrict__ C,
+                                              float* __restrict__ w, int B, int r1, int r2, int r3) {
+  pdl_enter();
+  extern __shared__ float qt[];                 // [WB][r2]
   __shared__ float red[8][WB][32];
+  for (int i = threadIdx.x; i < WB * r2; i += 256) {
+    const int b = blockIdx.x * WB + i / r2;
+    float t = 0.f;
+    if (b < B)
+#pragma unroll 4
+      for (int k = 0; k < shares; ++k) t += qt_parts[((long)k * B + b) * r2 + i % r2];
+    qt[i] = t;
+  }
+  __syncthreads();
   const int b0 = blockIdx.x * WB, a = blockIdx.y, c = blockIdx.z * 32 + threadIdx.x % 32, g = threadIdx.x / 32;
   float acc[WB] = {};
   if (c < r3)
@@ -188,7 +204,7 @@ __global__ void __launch_bounds__(256) k_pg_w(const float* __restrict__ qt, cons
       const float v = ld(C + ((long)a * r2 + q) * r3 + c);
 #pragma unroll
       for (int i = 0; i < WB; ++i)
-        if (b0 + i < B) acc[i] = fmaf(qt[(long)(b0 + i) * r2 + q], v, acc[i]);
+        acc[i] = fmaf(qt[i * r2 + q], v, acc[i]);
     }
 #pragma unroll
   for (int i = 0; i < WB; ++i) red[g][i][threadIdx.x % 32] = acc[i];
@@ -207,10 +223,12 @@ __global__ void __launch_bounds__(256) k_pg_w(const float* __restrict__ qt, cons
 // ---------------------------------------------------------------------------------------
 template <typename T>
 __global__ void __launch_bounds__(256) k_pg_queries(const float* __restrict__ w, const T* __restrict__ U1, float* __restrict__ qhat,
-                                                    float* __restrict__ knew, const float* __restrict__ vnew, T* __restrict__ K,
+                                                    const float* __restrict__ k_parts, const float* __restrict__ v_parts, int shares,
+                                                    float* __restrict__ knew, float* __restrict__ vnew, T* __restrict__ K,
                                                     T* __restrict__ V, const PagedView pv, const int32_t* __restrict__ cache_len,
                                                     int B, int nH, int r1, int r3, int t3, int Lmax, int prefix_len, float scale, int rope,
-                                                    double base, int append, int shared_kv, int shared_rope, unsigned int* err) {
+                                                    double base, const dec::RopeFreqs freqs, int append, int shared_kv, int shared_rope, unsigned int* err) {
+  pdl_enter();
   const int b = blockIdx.x;
   __shared__ long dst_s;
   __shared__ float2 cs_s[kMaxPairs];          // (cos, sin) of the new token's position
@@ -222,7 +240,7 @@ __global__ void __launch_bounds__(256) k_pg_queries(const float* __restrict__ w,
   const int half = (r3 + 1) / 2;
   if (rope)
     for (int i = threadIdx.x; i < r3 / 2; i += blockDim.x)
-      cs_s[i] = dec::rope_cos_sin_theta(prefix_len + L, pair_theta(i, r3, base));
+      cs_s[i] = dec::rope_cos_sin_theta(prefix_len + L, i < 128 ? freqs.theta[i] : pair_theta(i, r3, base));
   __syncthreads();
   for (int i = blockIdx.y * blockDim.x + threadIdx.x; i < nH * half; i += gridDim.y * blockDim.x) {
     const int h = i / half, c = 2 * (i % half);
@@ -247,14 +265,22 @@ __global__ void __launch_bounds__(256) k_pg_queries(const float* __restrict__ w,
   }
   if (blockIdx.y != 0) return;
   if (threadIdx.x == 0) dst_s = append ? paged_row(pv.table + (long)b * pv.max_pages, L, pv, err) : -1;
-  if (rope)
-    for (int i = threadIdx.x; i < r3 / 2; i += blockDim.x) {
-      float* px = knew + (long)b * r3 + 2 * i;
-      const float2 cs = cs_s[i];
-      const float xe = px[0], xo = px[1];
-      px[0] = xe * cs.x - xo * cs.y;
-      px[1] = xe * cs.y + xo * cs.x;
+  for (int i = threadIdx.x; i < half; i += blockDim.x) {
+    float xe = 0.f, xo = 0.f;
+    for (int k = 0; k < shares; ++k) {
+      const float* px = k_parts + ((long)k * B + b) * r3 + 2 * i;
+      xe += px[0];
+      if (2 * i + 1 < r3) xo += px[1];
     }
+    const float2 cs = rope ? cs_s[i] : make_float2(1.f, 0.f);
+    knew[(long)b * r3 + 2 * i] = xe * cs.x - xo * cs.y;
+    if (2 * i + 1 < r3) knew[(long)b * r3 + 2 * i + 1] = xe * cs.y + xo * cs.x;
+  }
+  for (int c = threadIdx.x; c < t3; c += blockDim.x) {
+    float t = 0.f;
+    for (int k = 0; k < shares; ++k) t += v_parts[((long)k * B + b) * t3 + c];
+    vnew[(long)b * t3 + c] = t;
+  }
   __syncthreads();
   if (dst_s < 0) return;
   [[maybe_unused]] const long rows = (long)pv.n_pages * pv.page_size;
@@ -327,6 +353,7 @@ __device__ __forceinline__ void load_rows(float* __restrict__ out, const T* __re
 
 template <bool VEC, typename T>
 __global__ void __launch_bounds__(256) k_pg_attn(const AttnArgs<T> g) {
+  pdl_enter();
   extern __shared__ __align__(16) float sm[];
   __shared__ double theta_s[kMaxPairs];
   const int rp = pitch4(g.r3), tp = pitch4(g.t3);
@@ -445,6 +472,7 @@ constexpr int kMaxSplits = 128;       // of either kind, see pick_splits
 __global__ void __launch_bounds__(256) k_pg_merge(const float* __restrict__ po, const float* __restrict__ ml, int splits_o,
                                                   const float* __restrict__ po_p, const float* __restrict__ ml_p, int splits_p,
                                                   float* __restrict__ o, int t3) {
+  pdl_enter();
   __shared__ float w_s[2 * kMaxSplits], red_s[8], acc_s[8][64];
   const long row = blockIdx.x;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -499,6 +527,7 @@ __global__ void __launch_bounds__(256) k_pg_merge(const float* __restrict__ po, 
 template <typename T>
 __global__ void __launch_bounds__(256) k_pg_u(const float* __restrict__ o, const T* __restrict__ Ut1, float* __restrict__ u, int B,
                                               int nH, int t1, int t3) {
+  pdl_enter();
   const long total = (long)B * t1 * t3;
   for (long i = blockIdx.x * 256L + threadIdx.x; i < total; i += gridDim.x * 256L) {
     const int c = (int)(i % t3), a = (int)((i / t3) % t1), b = (int)(i / ((long)t3 * t1));
@@ -511,6 +540,7 @@ __global__ void __launch_bounds__(256) k_pg_u(const float* __restrict__ o, const
 template <typename T>
 __global__ void __launch_bounds__(256) k_pg_z(const float* __restrict__ u, const T* __restrict__ Ct, float* __restrict__ z, int t1,
                                               int t2, int t3) {
+  pdl_enter();
   const int b = blockIdx.y, j = blockIdx.x * 8 + threadIdx.x / 32, lane = threadIdx.x % 32;
   if (j >= t2) return;
   float acc = 0.f;
@@ -527,8 +557,10 @@ __global__ void __launch_bounds__(256) k_pg_z(const float* __restrict__ u, const
 
 // ---- host side ----------------------------------------------------------------------------------------------------
 
+constexpr int kMaxAttnSmem = 200 * 1024, kMaxQuerySmem = 160 * 1024;
 bool shape_ok(const tucker_attn_desc& d) {
-  return d.t3 <= 64 * kMaxO4 && d.r3 <= 2 * kMaxPairs && pg_attn_smem(d.r3, d.t3) <= 200 * 1024;
+  return d.t3 <= 64 * kMaxO4 && d.r3 <= 2 * kMaxPairs && pg_attn_smem(d.r3, d.t3) <= kMaxAttnSmem &&
+         WB * (size_t)d.r2 * sizeof(float) <= kMaxQuerySmem;
 }
 
 // Shares per list of keys: about two blocks per SM, no more than there are tiles.
@@ -539,14 +571,23 @@ int pick_splits(long blocks, long keys) {
 int own_splits(const tucker_attn_desc& d, int64_t Lmax) { return pick_splits((long)d.B * ((d.n_H + AR - 1) / AR), Lmax); }
 int prefix_splits(const tucker_attn_desc& d, int32_t P) { return P > 0 ? pick_splits(((long)d.B * d.n_H + AR - 1) / AR, P) : 0; }
 
+// Shares of K = d of the new tokens' projections: one 128-deep block each while few tiles would otherwise be all there is.
+int proj_shares(const tucker_attn_desc& d) {
+  const int kb = (d.d_model + GK - 1) / GK;
+  return d.B <= 4 * GM ? std::min(kb, 8) : 1;
+}
+
 struct Ws {
-  float *qt, *knew, *vnew, *w, *qhat, *po, *ml, *po_p, *ml_p, *o, *u, *z;
+  float *qt_parts, *k_parts, *v_parts, *knew, *vnew, *w, *qhat, *po, *ml, *po_p, *ml_p, *o, *u, *z;
 };
 size_t carve(const tucker_attn_desc& d, int64_t Lmax, int32_t P, char* base, Ws* out) {
   Carver c(base);
   Ws t;
   const size_t B = d.B, rows = B * d.n_H, so = own_splits(d, Lmax), sp = prefix_splits(d, P);
-  t.qt = c.take<float>(B * d.r2);
+  const size_t sh = proj_shares(d);
+  t.qt_parts = c.take<float>(sh * B * d.r2);
+  t.k_parts = c.take<float>(sh * B * d.r3);
+  t.v_parts = c.take<float>(sh * B * d.t3);
   t.knew = c.take<float>(B * d.r3);
   t.vnew = c.take<float>(B * d.t3);
   t.w = c.take<float>(B * d.r1 * d.r3);
@@ -563,8 +604,9 @@ size_t carve(const tucker_attn_desc& d, int64_t Lmax, int32_t P, char* base, Ws*
 }
 
 template <typename TA, typename TB, typename TC>
-int launch_gemm(Problem& p, const GemmArgs<TA, TB, TC>& g, int parts, int max_n) {
-  k_pg_gemm<TA, TB, TC><<<dim3((g.M + GM - 1) / GM, (max_n + GN - 1) / GN, parts), GT, 0, p.stream>>>(g);
+int launch_gemm(Problem& p, const GemmArgs<TA, TB, TC>& g, int max_n) {
+  const int kb = (g.K + GK - 1) / GK, shares = (kb + g.kb_per_split - 1) / g.kb_per_split;
+  (void)launch_pdl(k_pg_gemm<TA, TB, TC>, dim3((g.M + GM - 1) / GM, (max_n + GN - 1) / GN, g.parts * shares), dim3(GT), 0, p.stream, g);
   TA_LAUNCH_CHECK(p);
   return TA_OK;
 }
@@ -572,9 +614,11 @@ int launch_gemm(Problem& p, const GemmArgs<TA, TB, TC>& g, int parts, int max_n)
 template <typename T>
 int attn(Problem& p, const AttnArgs<T>& g, int zs) {
   const size_t smem = pg_attn_smem(g.r3, g.t3);
-  const auto kernel = (g.r3 % 4 == 0 && g.t3 % 4 == 0) ? k_pg_attn<true, T> : k_pg_attn<false, T>;
-  TA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  kernel<<<dim3((g.rows_per_z + AR - 1) / AR, g.splits, zs), 256, smem, p.stream>>>(g);
+  const bool vec = g.r3 % 4 == 0 && g.t3 % 4 == 0;
+  const auto kernel = vec ? k_pg_attn<true, T> : k_pg_attn<false, T>;
+  static PerDeviceFlag attr_vec, attr_any;
+  TA_CUDA_TRY(ensure_dynamic_smem(vec ? attr_vec : attr_any, (const void*)kernel, kMaxAttnSmem));
+  (void)launch_pdl(kernel, dim3((g.rows_per_z + AR - 1) / AR, g.splits, zs), dim3(256), smem, p.stream, g);
   TA_LAUNCH_CHECK(p);
   return TA_OK;
 }
@@ -586,19 +630,23 @@ int decode_typed(Problem& p) {
   Ws w;
   carve(d, p.Lmax, P, p.ws, &w);
   int rc;
+  const int kb = (d.d_model + GK - 1) / GK, per = (kb + proj_shares(d) - 1) / proj_shares(d), shares = (kb + per - 1) / per;
   {
     GemmArgs<T, T, float> g = {};
-    g.A = (const T*)p.X; g.lda = d.d_model; g.M = d.B; g.K = d.d_model;
-    g.part[0] = {(const T*)p.U2, {d.r2, 1}, w.qt, d.r2, d.r2};
-    g.part[1] = {(const T*)p.U3, {d.r3, 1}, w.knew, d.r3, d.r3};
-    g.part[2] = {(const T*)p.Ut3, {d.t3, 1}, w.vnew, d.t3, d.t3};
-    if ((rc = launch_gemm(p, g, 3, std::max(d.r2, std::max(d.r3, d.t3))))) return rc;
+    g.A = (const T*)p.X; g.lda = d.d_model; g.M = d.B; g.K = d.d_model; g.parts = 3; g.kb_per_split = per;
+    g.part[0] = {(const T*)p.U2, {d.r2, 1}, w.qt_parts, d.r2, d.r2, (long)d.B * d.r2};
+    g.part[1] = {(const T*)p.U3, {d.r3, 1}, w.k_parts, d.r3, d.r3, (long)d.B * d.r3};
+    g.part[2] = {(const T*)p.Ut3, {d.t3, 1}, w.v_parts, d.t3, d.t3, (long)d.B * d.t3};
+    if ((rc = launch_gemm(p, g, std::max(d.r2, std::max(d.r3, d.t3))))) return rc;
   }
-  k_pg_w<T><<<dim3((d.B + WB - 1) / WB, d.r1, (d.r3 + 31) / 32), 256, 0, p.stream>>>(w.qt, (const T*)p.C, w.w, d.B, d.r1, d.r2, d.r3);
+  static PerDeviceFlag attr_w;
+  TA_CUDA_TRY(ensure_dynamic_smem(attr_w, (const void*)k_pg_w<T>, kMaxQuerySmem));
+  (void)launch_pdl(k_pg_w<T>, dim3((d.B + WB - 1) / WB, d.r1, (d.r3 + 31) / 32), dim3(256), WB * d.r2 * sizeof(float), p.stream, w.qt_parts,
+                   shares, (const T*)p.C, w.w, d.B, d.r1, d.r2, d.r3);
   TA_LAUNCH_CHECK(p);
-  k_pg_queries<T><<<dim3(d.B, std::max(1, std::min(8, 296 / d.B))), 256, 0, p.stream>>>(
-      w.w, (const T*)p.U1, w.qhat, w.knew, w.vnew, (T*)p.Kc, (T*)p.Vc, p.pv, p.cache_len, d.B, d.n_H, d.r1, d.r3, d.t3, p.Lmax, P,
-      p.scale, d.rope, (double)d.rope_base, p.append, p.shared_kv, p.shared_rope, p.dev_err);
+  (void)launch_pdl(k_pg_queries<T>, dim3(d.B, std::max(1, std::min(8, 296 / d.B))), dim3(256), 0, p.stream, w.w, (const T*)p.U1, w.qhat,
+                   w.k_parts, w.v_parts, shares, w.knew, w.vnew, (T*)p.Kc, (T*)p.Vc, p.pv, p.cache_len, d.B, d.n_H, d.r1, d.r3, d.t3, p.Lmax,
+                   P, p.scale, d.rope, (double)d.rope_base, rope_freqs(d), p.append, p.shared_kv, p.shared_rope, p.dev_err);
   TA_LAUNCH_CHECK(p);
   AttnArgs<T> a = {};
   a.q = w.qhat; a.K = (const T*)p.Kc; a.V = (const T*)p.Vc; a.pv = p.pv; a.cache_len = p.cache_len;
@@ -616,17 +664,17 @@ int decode_typed(Problem& p) {
   }
   prof_end(p);
   const int rows = d.B * d.n_H;
-  k_pg_merge<<<rows, 256, 0, p.stream>>>(w.po, w.ml, own_splits(d, p.Lmax), w.po_p, w.ml_p, sp, w.o, d.t3);
+  (void)launch_pdl(k_pg_merge, dim3(rows), dim3(256), 0, p.stream, w.po, w.ml, own_splits(d, p.Lmax), w.po_p, w.ml_p, sp, w.o, d.t3);
   TA_LAUNCH_CHECK(p);
-  k_pg_u<T><<<(int)std::min<long>(148 * 8, ((long)d.B * d.t1 * d.t3 + 255) / 256), 256, 0, p.stream>>>(w.o, (const T*)p.Ut1, w.u, d.B,
-                                                                                                      d.n_H, d.t1, d.t3);
+  (void)launch_pdl(k_pg_u<T>, dim3((unsigned)std::min<long>(148 * 8, ((long)d.B * d.t1 * d.t3 + 255) / 256)), dim3(256), 0, p.stream, w.o,
+                   (const T*)p.Ut1, w.u, d.B, d.n_H, d.t1, d.t3);
   TA_LAUNCH_CHECK(p);
-  k_pg_z<T><<<dim3((d.t2 + 7) / 8, d.B), 256, 0, p.stream>>>(w.u, (const T*)p.Ct, w.z, d.t1, d.t2, d.t3);
+  (void)launch_pdl(k_pg_z<T>, dim3((d.t2 + 7) / 8, d.B), dim3(256), 0, p.stream, w.u, (const T*)p.Ct, w.z, d.t1, d.t2, d.t3);
   TA_LAUNCH_CHECK(p);
   GemmArgs<float, T, T> g = {};
-  g.A = w.z; g.lda = d.t2; g.M = d.B; g.K = d.t2;
-  g.part[0] = {(const T*)p.Ut2, {1, d.t2}, (T*)p.Y, d.d_model, d.d_model};
-  return launch_gemm(p, g, 1, d.d_model);
+  g.A = w.z; g.lda = d.t2; g.M = d.B; g.K = d.t2; g.parts = 1; g.kb_per_split = (d.t2 + GK - 1) / GK;
+  g.part[0] = {(const T*)p.Ut2, {1, d.t2}, (T*)p.Y, d.d_model, d.d_model, 0};
+  return launch_gemm(p, g, d.d_model);
 }
 
 template <typename T>
@@ -638,7 +686,7 @@ int append_typed(Problem& p, const int32_t* tok_start, int32_t T_) {
   g.B = d.B; g.T_ = T_; g.d = d.d_model; g.r3 = d.r3; g.t3 = d.t3; g.rope = d.rope; g.pos0 = d.pos0;
   g.keys_shared = p.shared_kv; g.base = (double)d.rope_base; g.err = p.dev_err;
   const int wide = p.shared_kv ? d.t3 : std::max(d.r3, d.t3);
-  k_pg_append<T><<<dim3((T_ + GM - 1) / GM, (wide + GN - 1) / GN, p.shared_kv ? 1 : 2), GT, 0, p.stream>>>(g);
+  (void)launch_pdl(k_pg_append<T>, dim3((T_ + GM - 1) / GM, (wide + GN - 1) / GN, p.shared_kv ? 1 : 2), dim3(GT), 0, p.stream, g);
   TA_LAUNCH_CHECK(p);
   return TA_OK;
 }
