@@ -603,7 +603,7 @@ size_t carve_fast_dec(const tucker_attn_desc& d, bool paged, int32_t prefix_len,
     const PrefixPlan q = prefix_plan(d, prefix_len);
     const size_t rows = (size_t)(dec::MAX_GRID + q.n_rb) * prefix::RB;
     t.pre_o = c.take<float>(rows * d.t3);
-    t.pre_ml = c.take<float>(rows * 2);
+    t.pre_ml = c.take<float>(rows * 4);
     t.pre_k = c.take<bf16>(rotated ? (size_t)q.n_kt * prefix::TK * d.r3 : 0);
   }
   if (w) *w = t;
@@ -653,22 +653,26 @@ bool tmap_pages(CUtensorMap* m, const void* pool, int r, int n_pages, int page_s
   return tmap_3d(m, pool, r, page_size, n_pages, r, (uint64_t)page_size * r, 64, (uint32_t)std::min(page_size, 128));
 }
 
+// One pool with latent RoPE: the prefix's keys, rotated, one after another in the workspace.
+int launch_prefix_rotate(Problem& p, const FastDecWs& w) {
+  const tucker_attn_desc& d = p.d;
+  const long n = (long)p.prefix_len * (d.r3 / 8);
+  (void)launch_pdl(prefix::k_prefix_rotate, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, p.stream, (const bf16*)p.Kc,
+                   prefix::Rows{p.prefix_table, p.pv.n_pages, p.pv.page_size}, w.pre_k, p.prefix_len, d.r3, rope_freqs(d), p.dev_err);
+  TA_LAUNCH_CHECK(p);
+  return TA_OK;
+}
+
+// Launched behind the streaming kernel, which does not write anything that it reads and lets it be launched only after it has
+// itself waited for the kernels in front (queries, rotated keys): see ta_prefix_attn.cuh.
 int launch_prefix(Problem& p, const FastDecWs& w, const PrefixPlan& q) {
   const tucker_attn_desc& d = p.d;
   prefix::Params pp;
   pp.R = d.B * d.n_H; pp.P = p.prefix_len; pp.r3 = d.r3; pp.t3 = d.t3; pp.n_kt = q.n_kt; pp.n_rb = q.n_rb;
   pp.v = prefix::Rows{p.prefix_table, p.pv.n_pages, p.pv.page_size};
-  pp.k = pp.v;
+  pp.k = p.shared_rope ? prefix::Rows{nullptr, q.n_kt, prefix::TK} : pp.v;
   pp.part_o = w.pre_o; pp.part_ml = w.pre_ml; pp.err = p.dev_err;
-  const void* keys = p.Kc;
-  if (p.shared_rope) {
-    const long n = (long)p.prefix_len * (d.r3 / 8);
-    (void)launch_pdl(prefix::k_prefix_rotate, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, p.stream, (const bf16*)p.Kc, pp.v,
-                     w.pre_k, p.prefix_len, d.r3, rope_freqs(d), p.dev_err);
-    TA_LAUNCH_CHECK(p);
-    keys = w.pre_k;
-    pp.k = prefix::Rows{nullptr, q.n_kt, prefix::TK};
-  }
+  const void* keys = p.shared_rope ? w.pre_k : p.Kc;
   CUtensorMap tmQ, tmK, tmV;
   if (!tmap_2d(&tmQ, w.qhat, (uint64_t)d.r3, (uint64_t)2 * pp.R, (uint64_t)d.r3, 64, prefix::TQ)) return TA_ERR_CUDA;
   if (!tmap_pages(&tmK, keys, d.r3, pp.k.n_pages, pp.k.page_size)) return TA_ERR_CUDA;
@@ -779,9 +783,8 @@ int fast_decode(Problem& p) {
     }
     TA_LAUNCH_CHECK(p);
   }
-  // ---- 2b: attention of all rows to the shared prefix ----
   const PrefixPlan pq = p.prefix_len > 0 ? prefix_plan(d, p.prefix_len) : PrefixPlan{0, 0, 0};
-  if (p.prefix_len > 0 && (rc = launch_prefix(p, w, pq))) return rc;
+  if (p.prefix_len > 0 && p.shared_rope && (rc = launch_prefix_rotate(p, w))) return rc;
   // ---- 3: attention over the latent cache ----
   {
     CUtensorMap tmK, tmV;
@@ -799,6 +802,8 @@ int fast_decode(Problem& p) {
     dp.part_o = w.part_o; dp.part_ml = w.part_ml; dp.err = p.dev_err;
     rc = p.paged ? launch_dec_attn_umma<true>(p, tmK, tmV, dp, dp.grid) : launch_dec_attn_umma<false>(p, tmK, tmV, dp, dp.grid);
     if (rc) return rc;
+    // ---- 3b: attention of all rows to the shared prefix ----
+    if (p.prefix_len > 0 && (rc = launch_prefix(p, w, pq))) return rc;
     // ---- 4: merge the partials, output-side core ----
     if (p.paged) {
       if ((rc = launch_paged_out(p, w, pq, dp.grid))) return rc;
