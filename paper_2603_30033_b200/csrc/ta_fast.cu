@@ -603,7 +603,7 @@ size_t carve_fast_dec(const tucker_attn_desc& d, bool paged, int32_t prefix_len,
     const PrefixPlan q = prefix_plan(d, prefix_len);
     const size_t rows = (size_t)(dec::MAX_GRID + q.n_rb) * prefix::RB;
     t.pre_o = c.take<float>(rows * d.t3);
-    t.pre_ml = c.take<float>(rows * 4);
+    t.pre_ml = c.take<float>(rows * 2);
     t.pre_k = c.take<bf16>(rotated ? (size_t)q.n_kt * prefix::TK * d.r3 : 0);
   }
   if (w) *w = t;
@@ -663,6 +663,15 @@ int launch_prefix_rotate(Problem& p, const FastDecWs& w) {
   return TA_OK;
 }
 
+template <int KS>
+int launch_prefix_inst(Problem& p, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const prefix::Params& pp, int grid) {
+  static PerDeviceFlag attr;
+  TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)prefix::k_prefix_attn<KS>, (int)prefix::SMEM_BYTES));
+  (void)launch_pdl(prefix::k_prefix_attn<KS>, dim3(grid), dim3(prefix::THREADS), prefix::SMEM_BYTES, p.stream, tmQ, tmK, tmV, pp);
+  TA_LAUNCH_CHECK(p);
+  return TA_OK;
+}
+
 // Launched behind the streaming kernel, which does not write anything that it reads and lets it be launched only after it has
 // itself waited for the kernels in front (queries, rotated keys): see ta_prefix_attn.cuh.
 int launch_prefix(Problem& p, const FastDecWs& w, const PrefixPlan& q) {
@@ -677,11 +686,12 @@ int launch_prefix(Problem& p, const FastDecWs& w, const PrefixPlan& q) {
   if (!tmap_2d(&tmQ, w.qhat, (uint64_t)d.r3, (uint64_t)2 * pp.R, (uint64_t)d.r3, 64, prefix::TQ)) return TA_ERR_CUDA;
   if (!tmap_pages(&tmK, keys, d.r3, pp.k.n_pages, pp.k.page_size)) return TA_ERR_CUDA;
   if (!tmap_pages(&tmV, p.Vc, d.t3, pp.v.n_pages, pp.v.page_size)) return TA_ERR_CUDA;
-  static PerDeviceFlag attr;
-  TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)prefix::k_prefix_attn, (int)prefix::SMEM_BYTES));
-  (void)launch_pdl(prefix::k_prefix_attn, dim3(q.grid), dim3(prefix::THREADS), prefix::SMEM_BYTES, p.stream, tmQ, tmK, tmV, pp);
-  TA_LAUNCH_CHECK(p);
-  return TA_OK;
+  switch (d.r3) {
+    case 64: return launch_prefix_inst<4>(p, tmQ, tmK, tmV, pp, q.grid);
+    case 96: return launch_prefix_inst<6>(p, tmQ, tmK, tmV, pp, q.grid);
+    case 128: return launch_prefix_inst<8>(p, tmQ, tmK, tmV, pp, q.grid);
+    default: return TA_ERR_UNSUPPORTED_SHAPE;
+  }
 }
 
 template <int CL>

@@ -22,7 +22,7 @@ struct Params {
   const int32_t* cache_len;
   const float *part_o, *part_ml;                 // own keys: [grid + B][32][t3], [grid + B][32][2]
   int grid;
-  const float *pre_o, *pre_ml;                   // prefix: [grid_p + n_rb][t3 / 4][RB][4], [..][RB][4]
+  const float *pre_o, *pre_ml;                   // prefix: [grid_p + n_rb][t3 / 4][RB][4], [..][RB][2]
   int grid_p, n_kt, n_rb;                        // n_rb = 0: no prefix
   const bf16 *Ct, *Ut1;
   bf16* z;                                       // [B, 2 z_half]: rounded values, rounded rests
@@ -104,7 +104,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
     int pc, prl;
     pre_range(h, ps0, pc, prl);
     const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + (i0 + b) * 32 + h;
-    const float4* pml = reinterpret_cast<const float4*>(p.pre_ml) + ps0 * prefix::RB + prl;     // max, two sums
+    const float2* pml = reinterpret_cast<const float2*>(p.pre_ml) + ps0 * prefix::RB + prl;
     float m = -INFINITY;
     for (int k = warp; k < np; k += WARPS) m = fmaxf(m, ml[(long)k * 32].x);
     for (int k = warp; k < pc; k += WARPS) m = fmaxf(m, pml[(long)k * prefix::RB].x);
@@ -120,10 +120,10 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
       l = fmaf(v.y, e, l);
     }
     for (int k = warp; k < pc; k += WARPS) {
-      const float4 v = pml[(long)k * prefix::RB];
+      const float2 v = pml[(long)k * prefix::RB];
       const float e = dec::ex2(v.x - m);
       w_s[(np + k) * 32 + h] = e;
-      l = fmaf(v.y + v.z, e, l);
+      l = fmaf(v.y, e, l);
     }
     hl_s[warp][h] = l;
   }

@@ -2,21 +2,19 @@
 //
 // Every row attends to the same keys, so the prefix is a plain product pair S = Q K^T, O = P V with M = B n_H rows: the
 // cache is read once per 256 rows instead of once per sequence, and the step turns from HBM bound into tensor bound.
-//   row block   256 query rows = two tiles of 128 rows (row = TMEM lane)
+//   row block   256 query rows = two tiles of 128, one per softmax warpgroup (thread = row = TMEM lane)
 //   unit        (row block, tile of 128 keys); the flat list of units, row block by row block, is divided evenly over one
 //               CTA per SM, so any mix of few rows with a long prefix and many rows with a short one fills the GPU.  A CTA
 //               leaves one partial (max, sum, unnormalised O) per row block it touched, in slot (CTA + row block).
 //   warp 0      TMA producer (all lanes: one page box of the tile per lane), ring of K and V tiles in order of need
 //   warp 1      TMEM, MMA issue:  S_w = Qhi_w K^T + Qlo_w K^T ;  O_w += P_w V
-//   warps 4..7, 8..11   softmax warpgroups 0 and 1: keys [64 g, 64 g + 64) of EVERY score tile
+//   warps 4..7, 8..11   softmax warpgroup w
 // TMEM columns: S_0 [0,128) S_1 [128,256) O_0 [256,384) O_1 [384,512).  P_w (bf16) overwrites the first 64 columns of
 // S_w: the next scores of the same tile are issued behind the P V product that reads it, in the same thread's order.
-//
-// Both warpgroups work on the same tile, half a row per thread, and exchange the rows' maxima through shared memory: while they
-// are in the softmax of one tile the tensor core runs P V and the next scores of the other, 1536 cycles at ranks 128, and a
-// tile's softmax takes about as long.  (With a warpgroup per tile a group's own chain, softmax 2340 cycles, then 1280 of
-// MMAs and 500 of hand-over, set the pace: 5000 cycles per unit against 3072 of MMAs.)
-// P is handed over in two halves, so that P V starts while the second half is exponentiated.
+// While one warpgroup is in its softmax the tensor core works for the other; P is handed over in two halves, so that P V
+// starts while the second half is exponentiated.
+// (Both warpgroups on every tile, half a row per thread, was measured: the exchange of the row maxima and the phases in which
+// neither of them uses the exponential unit cost more than the shorter hand-over gains, 4900 cycles per unit against CYC.)
 //
 // The kernel follows the streaming kernel of the sequences' own keys in the stream but does not depend on it: what it reads was
 // complete before that kernel let it be launched.  So its CTAs start as the streaming kernel's leave their SMs, and it only
@@ -45,8 +43,7 @@ constexpr int MAX_BUF = 6;
 constexpr int TILE_BYTES = 224 * 1024;    // queries and ring
 // All shared memory is dynamic, so that its start, and with it the tiles', is 1024-byte aligned (checked) and nothing is lost to alignment.
 struct Ctl {
-  uint64_t q_full, q_empty, kv_full[MAX_BUF], kv_empty[MAX_BUF], s_full[2], p_half[2], p_full[2], o_full[2], o_read[2], patched, x_bar;
-  float mx[2][2][TQ];        // [parity][half][row]: row maxima of a tile's halves
+  uint64_t q_full, q_empty, kv_full[MAX_BUF], kv_empty[MAX_BUF], s_full[2], p_half[2], p_full[2], o_full[2], o_read[2], patched;
   uint32_t tmem_slot;
   int abort_flag;
 };
@@ -65,7 +62,7 @@ struct Params {
   int n_kt, n_rb;          // key tiles, row blocks
   Rows k, v;
   float* part_o;           // [grid + n_rb][t3 / 4][RB][4]: a warp's rows are adjacent, for its stores and for the reader's heads
-  float* part_ml;          // [grid + n_rb][RB][4]   (max in log2 units, sums of the two halves of the key tiles)
+  float* part_ml;          // [grid + n_rb][RB][2]   (max in log2 units, sum)
   unsigned int* err;
 };
 
@@ -78,6 +75,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // The CTA that works on unit t when `total` units are divided over `grid` CTAs (see dec::cta_first_tile).
 __device__ __forceinline__ long owner_of(long t, long total, long grid) { return ((t + 1) * grid - 1) / total; }
 
+// KS = r3 / 16: with the number of K steps known the issue of an MMA takes about as long as the MMA; with a test in front of each
+// one the issuing thread set the pace (ISS).
+template <int KS>
 __global__ void __launch_bounds__(THREADS, 1)
 k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
               const __grid_constant__ CUtensorMap tmV, const Params p) {
@@ -87,7 +87,7 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     return;
   }
   Ctl& ctl = *reinterpret_cast<Ctl*>(smem + TILE_BYTES);
-  uint64_t &q_full = ctl.q_full, &q_empty = ctl.q_empty, &patched = ctl.patched, &x_bar = ctl.x_bar;
+  uint64_t &q_full = ctl.q_full, &q_empty = ctl.q_empty, &patched = ctl.patched;
   uint64_t *kv_full = ctl.kv_full, *kv_empty = ctl.kv_empty, *s_full = ctl.s_full, *p_half = ctl.p_half, *p_full = ctl.p_full,
            *o_full = ctl.o_full, *o_read = ctl.o_read;
   const int ksub = (p.r3 + 63) / 64, vsub = (p.t3 + 63) / 64;
@@ -105,13 +105,12 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     for (int i = 0; i < MAX_BUF; ++i) { mbar_init(&kv_full[i], 1); mbar_init(&kv_empty[i], 1); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s_full[i], 1);
-      mbar_init(&p_half[i], 8);         // the first 32 keys' P of either half is in TMEM: one arrival per softmax warp
-      mbar_init(&p_full[i], 8);         // all of it
+      mbar_init(&p_half[i], 4);         // the first 64 keys' P is in TMEM: one arrival per warp of the group
+      mbar_init(&p_full[i], 4);         // all of it
       mbar_init(&o_full[i], 1);         // the P V product is complete
-      mbar_init(&o_read[i], 8);         // the accumulator of a finished segment has been read
+      mbar_init(&o_read[i], 4);         // the accumulator of a finished segment has been read
     }
     mbar_init(&patched, 4);
-    mbar_init(&x_bar, 8);
     fence_barrier_init();
   }
   if (warp == 1) {
@@ -190,27 +189,27 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     if (elect_one()) {
       const uint32_t idesc_qk = umma_idesc_bf16(TQ, TK);
       const uint32_t idesc_pv = umma_idesc_bf16(TQ, (uint32_t)p.t3) | (1u << 16);     // B = V tile, MN-major
-      const int ksteps = p.r3 / 16;
       const uint64_t dq0 = umma_desc_kmajor_sw128(smem_u32(smem));
       const uint64_t dk0 = umma_desc_kmajor_sw128(smem_u32(ring));
       const uint64_t dv0 = umma_desc_mnmajor_sw128(smem_u32(ring), SUB_BYTES);
       auto issue_qk = [&](int w, int s) {
         const uint64_t dk = dk0 + (uint64_t)(s * (buf_bytes >> 4));
+        const uint64_t dq = dq0 + (uint64_t)((w * q_tile) >> 4), dl = dq + (uint64_t)((ksub * SUB_BYTES) >> 4);
         const uint32_t d = tmem + (uint32_t)w * 128u;
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-          const uint64_t dq = dq0 + (uint64_t)((w * q_tile + half * ksub * SUB_BYTES) >> 4);
 #pragma unroll
-          for (int ks = 0; ks < 8; ++ks)
-            if (ks < ksteps) {
-              const uint64_t o = (uint64_t)((ks >> 2) * (SUB_BYTES >> 4) + (ks & 3) * 2);
-              umma_ss(d, dq + o, dk + o, idesc_qk, (half | ks) != 0 ? 1u : 0u);
-            }
+        for (int ks = 0; ks < KS; ++ks) {
+          const uint64_t o = (uint64_t)((ks >> 2) * (SUB_BYTES >> 4) + (ks & 3) * 2);
+          umma_ss(d, dq + o, dk + o, idesc_qk, ks != 0 ? 1u : 0u);
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const uint64_t o = (uint64_t)((ks >> 2) * (SUB_BYTES >> 4) + (ks & 3) * 2);
+          umma_ss(d, dl + o, dk + o, idesc_qk, 1u);
         }
         umma_commit(&s_full[w]);
       };
       int n = 0;                          // ring buffers consumed so far
-      uint32_t pf = 0, od = 0, begun = 0; // per row tile, a bit each: parity of p_full, of o_read, any segment before
+      uint32_t pf = 0, od = 0, begun = 0; // per warpgroup, a bit each: parity of p_full, of o_read, any segment before
       int seg = 0, n_patch = 0;
       bool ok = true;
       for (long u = u_begin; u < u_end && ok;) {
@@ -236,7 +235,7 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           sk = n % n_buf;
           for (int w = 0; w < nw && ok; ++w) {
             if (!(ok = mbar_wait_poll(&p_half[w], (pf >> w) & 1u, ab))) break;
-            if (i == 0) {                 // the accumulator of the tile's previous segment must have been read
+            if (i == 0) {                 // the accumulator of the group's previous segment must have been read
               if ((begun >> w) & 1u) {
                 if (!(ok = mbar_wait(&o_read[w], (od >> w) & 1u, ab))) break;
                 od ^= 1u << w;
@@ -246,20 +245,16 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             tc_fence_after();
             const uint64_t dv = dv0 + (uint64_t)(sv * (buf_bytes >> 4));
             const uint32_t a = tmem + (uint32_t)w * 128u, d = tmem + 256u + (uint32_t)w * 128u;
-            // the product starts with the keys whose P is there while the groups still work on the others
+            // the product starts with the keys whose P is there while the group still works on the others
 #pragma unroll
-            for (int k = 0; k < TK / 32; ++k) {
-              const int ks = (k & 1) + (k >> 1) * 4;       // keys 0 .. 31 and 64 .. 95
-              umma_ts(d, a + (uint32_t)ks * 8u, dv + (uint64_t)(ks * 128), idesc_pv, (i | k) != 0 ? 1u : 0u);
-            }
+            for (int ks = 0; ks < TK / 32; ++ks)
+              umma_ts(d, a + (uint32_t)ks * 8u, dv + (uint64_t)(ks * 128), idesc_pv, (i | ks) != 0 ? 1u : 0u);
             if (!(ok = mbar_wait_poll(&p_full[w], (pf >> w) & 1u, ab))) break;
             pf ^= 1u << w;
             tc_fence_after();
 #pragma unroll
-            for (int k = 0; k < TK / 32; ++k) {
-              const int ks = 2 + (k & 1) + (k >> 1) * 4;
+            for (int ks = TK / 32; ks < TK / 16; ++ks)
               umma_ts(d, a + (uint32_t)ks * 8u, dv + (uint64_t)(ks * 128), idesc_pv, 1u);
-            }
             umma_commit(&o_full[w]);
             if (i + 1 < nt) {
               if (w == 0 && !(ok = mbar_wait(&kv_full[sk], (uint32_t)((n / n_buf) & 1), ab))) break;
@@ -283,35 +278,26 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
    // launched with 168 registers x 384 threads = 64512 = 128 x 72 + 256 x 216
    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
    // ------------------------------- softmax warpgroups --------------------------
-   const int g = (warp - 4) / 4, q = warp % 4, rloc = q * 32 + lane;
+   const int w = (warp - 4) / 4, q = warp % 4, rloc = q * 32 + lane;
    const uint32_t lane_addr = (uint32_t)(q * 32) << 16;
+   const uint32_t tm_s = tmem + (uint32_t)w * 128u + lane_addr, tm_o = tmem + 256u + (uint32_t)w * 128u + lane_addr;
    auto wait_all = [&](uint64_t* bar, uint32_t parity) -> bool {
      const bool good = mbar_wait(bar, parity, ab);
      return __all_sync(0xffffffffu, good);
    };
-   uint32_t nx = 0;                       // exchanges so far
-   // the row's maximum over both halves, from this half's
-   auto exchange = [&](float& m) -> bool {
-     ctl.mx[nx & 1][g][rloc] = m;
-     __syncwarp();
-     if (lane == 0) mbar_arrive(&x_bar);
-     if (!wait_all(&x_bar, nx & 1u)) return false;
-     m = fmaxf(m, ctl.mx[nx & 1][g ^ 1][rloc]);
-     ++nx;
-     return true;
-   };
-   int jt[2] = {0, 0};                    // score tiles so far per row tile
+   int jt = 0;                            // tiles of this group so far
    int n = 0;                             // ring buffers of the segments before this one
    bool ok = true;
    for (long u = u_begin; u < u_end && ok;) {
      const int rb = (int)(u / p.n_kt), kt0 = (int)(u - (long)rb * p.n_kt);
      const int nt = (int)min((long)(p.n_kt - kt0), u_end - u);
-     const int nw = (p.R - rb * RB) > TQ ? 2 : 1;
-     float m_used[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-     for (int i = 0; i < nt && ok; ++i) {
-       const int k0 = (kt0 + i) * TK + g * 64;             // first key of this half
-       const bool last = ragged && (kt0 + i) == p.n_kt - 1;
-       if (last && g == 0) {
+     const int row = rb * RB + w * TQ + rloc;
+     const bool present = (p.R - rb * RB) > w * TQ;        // uniform in the group
+     float m_used = -INFINITY, l = 0.f;
+     for (int i = 0; present && i < nt && ok; ++i, ++jt) {
+       const int k0 = (kt0 + i) * TK;
+       const bool last = ragged && k0 + TK > p.P;
+       if (last && w == 0) {
          // value rows past the prefix must not be trusted: zeros (a zero row is zero in any swizzle)
          const int nv = n + 2 * i + 1, s = nv % n_buf;
          if (!(ok = wait_all(&kv_full[s], (uint32_t)((nv / n_buf) & 1)))) break;
@@ -324,113 +310,95 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
          __syncwarp();
          if (lane == 0) mbar_arrive(&patched);
        }
-#pragma unroll
-       for (int w = 0; w < 2; ++w) {
-         if (w >= nw || !ok) continue;
-         const uint32_t tm_s = tmem + (uint32_t)w * 128u + lane_addr, tm_o = tmem + 256u + (uint32_t)w * 128u + lane_addr;
-         if (!(ok = wait_all(&s_full[w], (uint32_t)(jt[w] & 1)))) continue;
-         tc_fence_after();
-         uint32_t sr[64];
-         {
-           uint32_t (*c)[32] = reinterpret_cast<uint32_t (*)[32]>(sr);
-           tmem_ld32(tm_s + g * 64, c[0]);
-           tmem_ld32(tm_s + g * 64 + 32, c[1]);
-           tmem_ld_wait();
-         }
-         if (last) {
-#pragma unroll
-           for (int c = 0; c < 64; ++c)
-             if (k0 + c >= p.P) sr[c] = 0xff800000u;        // -inf
-         }
-         float mt;
-         {
-           float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
-#pragma unroll
-           for (int c = 0; c < 64; c += 8) {
-             m0 = max3(m0, __uint_as_float(sr[c]), __uint_as_float(sr[c + 1]));
-             m1 = max3(m1, __uint_as_float(sr[c + 2]), __uint_as_float(sr[c + 3]));
-             m2 = max3(m2, __uint_as_float(sr[c + 4]), __uint_as_float(sr[c + 5]));
-             m3 = max3(m3, __uint_as_float(sr[c + 6]), __uint_as_float(sr[c + 7]));
-           }
-           mt = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
-         }
-         // after the exchange both halves of the scores are in registers: P may overwrite them
-         tc_fence_before();
-         if (!(ok = exchange(mt))) continue;
-         tc_fence_after();
-         // the reference maximum only moves when it would grow by more than a factor of 256: the accumulator is rescaled rarely.
-         // Both groups see the same maxima and decide alike; each rescales its half of the columns.
-         const bool need = mt > m_used[w] + kRescaleThreshold;   // a tile holds a key: mt > -inf, and the first tile needs
-         if (__any_sync(0xffffffffu, need)) {
-           const float m_new = need ? mt : m_used[w];
-           const float f = need ? dec::ex2(m_used[w] - m_new) : 1.f;
-           if (i > 0) {
-             if (!(ok = wait_all(&o_full[w], (uint32_t)((jt[w] - 1) & 1)))) continue;
-             tc_fence_after();
-             for (int ch = 0; ch < p.t3 / 32; ++ch) {
-               uint32_t o[16];
-               const uint32_t at = tm_o + (uint32_t)(g * (p.t3 / 2) + ch * 16);
-               tmem_ld16(at, o);
-               tmem_ld_wait();
-#pragma unroll
-               for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
-               tmem_st16(at, o);
-             }
-           }
-           l[w] *= f;
-           m_used[w] = m_new;
-         }
-         const float2 negm = make_float2(-m_used[w], -m_used[w]);
-         float2 rs[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-         for (int half = 0; half < 2; ++half) {
-#pragma unroll
-           for (int c = half * 16; c < half * 16 + 16; ++c) {
-             const float2 x = __fadd2_rn(make_float2(__uint_as_float(sr[2 * c]), __uint_as_float(sr[2 * c + 1])), negm);
-             const float2 e = make_float2(dec::ex2(x.x), dec::ex2(x.y));
-             rs[c & 1] = __fadd2_rn(rs[c & 1], e);
-             sr[c] = pack_bf16(e.x, e.y);
-           }
-           tmem_st16(tm_s + g * 32 + half * 16, reinterpret_cast<uint32_t (*)[16]>(sr)[half]);
-           tmem_st_wait();
-           tc_fence_before();
-           __syncwarp();
-           if (lane == 0) mbar_arrive(half ? &p_full[w] : &p_half[w]);
-         }
-         const float2 r01 = __fadd2_rn(rs[0], rs[1]);
-         l[w] += r01.x + r01.y;
-         ++jt[w];
+       if (!(ok = wait_all(&s_full[w], (uint32_t)(jt & 1)))) break;
+       tc_fence_after();
+       uint32_t sr[128];
+       {
+         uint32_t (*c)[32] = reinterpret_cast<uint32_t (*)[32]>(sr);
+         tmem_ld32(tm_s + 0, c[0]);
+         tmem_ld32(tm_s + 32, c[1]);
+         tmem_ld32(tm_s + 64, c[2]);
+         tmem_ld32(tm_s + 96, c[3]);
+         tmem_ld_wait();
        }
+       if (last) {
+#pragma unroll
+         for (int c = 0; c < 128; ++c)
+           if (k0 + c >= p.P) sr[c] = 0xff800000u;          // -inf
+       }
+       float mt;
+       {
+         float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
+#pragma unroll
+         for (int c = 0; c < 128; c += 8) {
+           m0 = max3(m0, __uint_as_float(sr[c]), __uint_as_float(sr[c + 1]));
+           m1 = max3(m1, __uint_as_float(sr[c + 2]), __uint_as_float(sr[c + 3]));
+           m2 = max3(m2, __uint_as_float(sr[c + 4]), __uint_as_float(sr[c + 5]));
+           m3 = max3(m3, __uint_as_float(sr[c + 6]), __uint_as_float(sr[c + 7]));
+         }
+         mt = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+       }
+       // the reference maximum only moves when it would grow by more than a factor of 256: the accumulator is rescaled rarely
+       const bool need = mt > m_used + kRescaleThreshold;   // every tile holds a key: mt > -inf, and the first tile needs
+       if (__any_sync(0xffffffffu, need)) {
+         const float m_new = need ? mt : m_used;
+         const float f = need ? dec::ex2(m_used - m_new) : 1.f;
+         if (i > 0) {
+           if (!(ok = wait_all(&o_full[w], (uint32_t)((jt - 1) & 1)))) break;
+           tc_fence_after();
+           for (int ch = 0; ch < p.t3 / 32; ++ch) {
+             uint32_t o[32];
+             tmem_ld32(tm_o + ch * 32, o);
+             tmem_ld_wait();
+#pragma unroll
+             for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
+             tmem_st32(tm_o + ch * 32, o);
+           }
+         }
+         l *= f;
+         m_used = m_new;
+       }
+       const float2 negm = make_float2(-m_used, -m_used);
+       float2 rs[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+       for (int half = 0; half < 2; ++half) {
+#pragma unroll
+         for (int c = half * 32; c < half * 32 + 32; ++c) {
+           const float2 x = __fadd2_rn(make_float2(__uint_as_float(sr[2 * c]), __uint_as_float(sr[2 * c + 1])), negm);
+           const float2 e = make_float2(dec::ex2(x.x), dec::ex2(x.y));
+           rs[c & 3] = __fadd2_rn(rs[c & 3], e);
+           sr[c] = pack_bf16(e.x, e.y);
+         }
+         tmem_st32(tm_s + half * 32, reinterpret_cast<uint32_t (*)[32]>(sr)[half]);
+         tmem_st_wait();
+         tc_fence_before();
+         __syncwarp();
+         if (lane == 0) mbar_arrive(half ? &p_full[w] : &p_half[w]);
+       }
+       const float2 r01 = __fadd2_rn(rs[0], rs[1]), r23 = __fadd2_rn(rs[2], rs[3]);
+       l += (r01.x + r01.y) + (r23.x + r23.y);
      }
      if (!ok) break;
-     const long slot = (long)blockIdx.x + rb;
-#pragma unroll
-     for (int w = 0; w < 2; ++w) {
-       if (w >= nw || !ok) continue;
-       if (!(ok = wait_all(&o_full[w], (uint32_t)((jt[w] - 1) & 1)))) continue;
+     if (present) {
+       if (!(ok = wait_all(&o_full[w], (uint32_t)((jt - 1) & 1)))) break;
        tc_fence_after();
-       const int row = w * TQ + rloc;
-       const bool slot_ok = rb * RB + row < p.R && TA_IDX_OK(p.err, slot, 1, (long)gridDim.x + p.n_rb);
-       float4* dst = reinterpret_cast<float4*>(p.part_o) + slot * RB * (p.t3 / 4) + row;
+       const long slot = (long)blockIdx.x + rb;
+       const bool slot_ok = row < p.R && TA_IDX_OK(p.err, slot, 1, (long)gridDim.x + p.n_rb);
+       float4* dst = reinterpret_cast<float4*>(p.part_o) + slot * RB * (p.t3 / 4) + w * TQ + rloc;
        for (int ch = 0; ch < p.t3 / 32; ++ch) {
-         uint32_t o[16];
-         const int c = g * (p.t3 / 2) + ch * 16;
-         tmem_ld16(tmem + 256u + (uint32_t)w * 128u + lane_addr + (uint32_t)c, o);
+         uint32_t o[32];
+         tmem_ld32(tm_o + ch * 32, o);
          tmem_ld_wait();
          if (slot_ok)
 #pragma unroll
-           for (int e = 0; e < 4; ++e)
-             dst[(long)(c / 4 + e) * RB] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
-                                                       __uint_as_float(o[4 * e + 3]));
+           for (int c = 0; c < 8; ++c)
+             dst[(long)(ch * 8 + c) * RB] = make_float4(__uint_as_float(o[4 * c]), __uint_as_float(o[4 * c + 1]), __uint_as_float(o[4 * c + 2]),
+                                                        __uint_as_float(o[4 * c + 3]));
        }
        tc_fence_before();
        __syncwarp();
        if (lane == 0) mbar_arrive(&o_read[w]);               // the next segment may overwrite the accumulator
-       if (slot_ok) {
-         float* ml = p.part_ml + (slot * RB + row) * 4;
-         if (g == 0) ml[0] = m_used[w];
-         ml[1 + g] = l[w];
-       }
+       if (slot_ok) *reinterpret_cast<float2*>(p.part_ml + (slot * RB + w * TQ + rloc) * 2) = make_float2(m_used, l);
      }
      n += 2 * nt;
      u += nt;
