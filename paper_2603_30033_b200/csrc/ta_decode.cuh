@@ -29,6 +29,7 @@ struct Params {
   const bf16* vnew;    // [B, T3] new value
   float* part_o;       // [grid + B][32][T3]
   float* part_ml;      // [grid + B][32][2]  (max in log2 units, sum)
+  int* seq_cta;        // paged form: [B][2] first and last CTA of the streaming kernel that hold a part of the sequence
   unsigned int* err;
 };
 

@@ -83,6 +83,7 @@ struct Params {
   unsigned int* err;
   PagedView pv;        // PAGED
   int pos_base;        // ROT: position of slot 0
+  int* seq_cta;        // PAGED: [B][2] first and last CTA that holds a part of the sequence, for the join
 };
 
 // Walks this CTA's range of the flat tile list, sequence by sequence.
@@ -699,6 +700,10 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
           if (lane == h) sum_s[wg][q][h] = ws;
         }
         if (!(ok = wg_sync())) break;
+        if (PAGED && threadIdx.x == 128) {
+          if (t_begin <= w.first && TA_IDX_OK(p.err, 2 * w.b, 2, 2L * p.B)) p.seq_cta[2 * w.b] = (int)blockIdx.x;
+          if (t == w.first + w.nt - 1 && TA_IDX_OK(p.err, 2 * w.b, 2, 2L * p.B)) p.seq_cta[2 * w.b + 1] = (int)blockIdx.x;
+        }
         const long slot = (long)blockIdx.x + w.b;
         // one partial slot per (CTA, sequence) pair that can occur: gridDim.x + B of them
         const bool slot_ok = TA_IDX_OK(p.err, slot, 1, (long)gridDim.x + p.B);

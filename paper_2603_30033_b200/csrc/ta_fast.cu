@@ -565,6 +565,7 @@ struct FastDecWs {
   bf16* qhat;         // [B][n_H][r3] rotated, scaled per-head queries
   bf16* z;            // [B][t2]
   float *part_o, *part_ml;
+  int* seq_cta;            // [B][2], paged: CTAs of the streaming kernel that hold a sequence
   float *pre_o, *pre_ml;   // partials of the shared prefix
   bf16* pre_k;             // one pool with latent RoPE: the prefix's keys, rotated (rows padded to whole tiles)
 };
@@ -597,6 +598,7 @@ size_t carve_fast_dec(const tucker_attn_desc& d, bool paged, int32_t prefix_len,
   const size_t slots = (size_t)dec::MAX_GRID + d.B;
   t.part_o = c.take<float>(slots * 32 * d.t3);
   t.part_ml = c.take<float>(slots * 64);
+  t.seq_cta = c.take<int>(paged ? (size_t)d.B * 2 : 0);
   t.pre_o = t.pre_ml = nullptr;
   t.pre_k = nullptr;
   if (prefix_len > 0) {
@@ -634,7 +636,7 @@ int launch_dec_attn_umma(Problem& p, const CUtensorMap& tmK, const CUtensorMap& 
   up.B = dp.B; up.nH = dp.nH; up.Lmax = dp.Lmax; up.r3 = d.r3; up.t3 = d.t3; up.shared_kv = dp.shared_kv;
   up.cache_len = dp.cache_len; up.knew = dp.knew; up.vnew = dp.vnew;
   up.part_o = dp.part_o; up.part_ml = dp.part_ml; up.err = dp.err;
-  up.pv = p.pv; up.pos_base = p.prefix_len;
+  up.pv = p.pv; up.pos_base = p.prefix_len; up.seq_cta = dp.seq_cta;
   if (p.shared_rope) {
     const dec::RopeFreqs freqs = rope_freqs(d);
     switch (d.r3) {
@@ -707,8 +709,8 @@ int launch_paged_out_cl(Problem& p, const pgout::Params& op) {
 int launch_paged_out(Problem& p, const FastDecWs& w, const PrefixPlan& q, int grid) {
   const tucker_attn_desc& d = p.d;
   pgout::Params op;
-  op.B = d.B; op.nH = d.n_H; op.Lmax = p.Lmax; op.t1 = d.t1; op.t2 = d.t2; op.t3 = d.t3; op.z_half = z_half(d);
-  op.cache_len = p.cache_len; op.part_o = w.part_o; op.part_ml = w.part_ml; op.grid = grid;
+  op.B = d.B; op.nH = d.n_H; op.t1 = d.t1; op.t2 = d.t2; op.t3 = d.t3; op.z_half = z_half(d);
+  op.seq_cta = w.seq_cta; op.part_o = w.part_o; op.part_ml = w.part_ml; op.grid = grid;
   op.pre_o = w.pre_o; op.pre_ml = w.pre_ml; op.grid_p = q.grid; op.n_kt = q.n_kt; op.n_rb = q.n_rb;
   op.Ct = (const bf16*)p.Ct; op.Ut1 = (const bf16*)p.Ut1; op.z = w.z; op.err = p.dev_err;
   // measured at 64 sequences of 32 heads, two to three partials each: 20.6 us with 8 CTAs per sequence (two waves), OUT4 us with 4
@@ -809,7 +811,7 @@ int fast_decode(Problem& p) {
     dp.B = d.B; dp.nH = d.n_H; dp.Lmax = p.Lmax; dp.grid = decode_grid();
     dp.shared_kv = p.shared_kv;
     dp.cache_len = p.cache_len; dp.qhat = w.qhat; dp.knew = w.knew; dp.vnew = w.vnew;
-    dp.part_o = w.part_o; dp.part_ml = w.part_ml; dp.err = p.dev_err;
+    dp.part_o = w.part_o; dp.part_ml = w.part_ml; dp.err = p.dev_err; dp.seq_cta = w.seq_cta;
     rc = p.paged ? launch_dec_attn_umma<true>(p, tmK, tmV, dp, dp.grid) : launch_dec_attn_umma<false>(p, tmK, tmV, dp, dp.grid);
     if (rc) return rc;
     // ---- 3b: attention of all rows to the shared prefix ----

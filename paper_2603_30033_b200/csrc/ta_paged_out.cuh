@@ -5,6 +5,8 @@
 // sequence, where CTAs that split the rows of z would each have to merge everything), forms its columns of u, hands them to the
 // other CTAs through distributed shared memory, and computes t2 / CL rows of z.  One user with a long cache has a partial
 // from every SM: the maxima, weights and sums of the partials are spread over all warps instead of walked by one.
+// The kernels before it fill their SMs, so that next to nothing of this one overlaps them: it takes the CTAs that hold a sequence
+// from the streaming kernel instead of scanning the lengths.
 #pragma once
 
 #include "ta_common.cuh"
@@ -18,8 +20,8 @@ constexpr int THREADS = 512, WARPS = THREADS / 32;
 constexpr int MAX_PART = 2 * dec::MAX_GRID;      // partials of one head: one per CTA of either attention kernel at most
 
 struct Params {
-  int B, nH, Lmax, t1, t2, t3, z_half;
-  const int32_t* cache_len;
+  int B, nH, t1, t2, t3, z_half;
+  const int* seq_cta;                            // [B][2]
   const float *part_o, *part_ml;                 // own keys: [grid + B][32][t3], [grid + B][32][2]
   int grid;
   const float *pre_o, *pre_ml;                   // prefix: [grid_p + n_rb][t3 / 4][RB][4], [..][RB][2]
@@ -31,7 +33,7 @@ struct Params {
 
 __host__ __device__ inline size_t smem_bytes(int cl, int t1, int t3, int nH, bool with_prefix) {
   const int parts = with_prefix ? MAX_PART : dec::MAX_GRID;
-  return sizeof(float) * ((size_t)parts * 32 + (size_t)t1 * t3 + (size_t)nH * t1 + (size_t)THREADS * 4 + 32 * (128 / cl));
+  return sizeof(float) * ((size_t)parts * 64 + (size_t)t1 * t3 + (size_t)nH * t1 + (size_t)THREADS * 4 + 32 * (128 / cl));
 }
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
@@ -51,38 +53,20 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
   float* o_s = sm + THREADS * 4;                           // [32][MAX_COLS]
   float* u_s = o_s + 32 * MAX_COLS;                        // [t1][t3]
   float* ut1_s = u_s + p.t1 * t3;                          // [nH][t1]
-  float* w_s = ut1_s + p.nH * p.t1;                        // [partials][32]
-  __shared__ long long wtot_s[WARPS];
-  __shared__ long long first_s;
+  float2* w_s = reinterpret_cast<float2*>(ut1_s + (p.nH * p.t1 + 1) / 2 * 2);      // [partials][32]: (max, sum), then (weight, -)
   __shared__ float hm_s[WARPS][32], hl_s[WARPS][32];
   const int b = blockIdx.x / CL, y = blockIdx.x % CL, c0 = y * cw;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const int jn = p.t2 / CL, jbeg = y * jn;
   cluster_arrive();                                        // "this CTA has started": waited for before the first remote store
-  {
-    // this CTA's rows of the output core towards L2 while the merge runs
-    const char* cbase = reinterpret_cast<const char*>(p.Ct);
-    const long row_bytes = (long)t3 * 2, span = (long)jn * row_bytes;
-    const int lines = (int)((span + 127) / 128);
-    for (int i = tid; i < p.t1 * lines; i += THREADS)
-      asm volatile("prefetch.global.L2 [%0];" ::"l"(cbase + ((long)(i / lines) * p.t2 + jbeg) * row_bytes + (long)(i % lines) * 128));
-  }
+  // z: lane = (slice a of rpl, 16-byte chunk) of a row of the core
+  const int nch = t3 / 8, rpl = 32 / nch;                  // 8, 12 or 16 chunks; 4, 2 or 2 slices at a time
+  const int ga = lane / nch, ch = lane % nch;
+  const uint4* Cq = reinterpret_cast<const uint4*>(p.Ct);
+  auto core = [&](int jl, int a) -> uint4 {
+    return (jl < jn && ga < rpl && a < p.t1) ? Cq[((long)a * p.t2 + jbeg + jl) * nch + ch] : make_uint4(0u, 0u, 0u, 0u);
+  };
   for (int i = tid; i < p.nH * p.t1; i += THREADS) ut1_s[i] = __bfloat162float(p.Ut1[i]);
-  int lo, hi;
-  long excl;
-  const long total = dec::block_tile_scan(p.cache_len, p.B, p.Lmax, lo, hi, excl, wtot_s);
-  if (b >= lo && b < hi) {
-    long f = excl;
-    for (int i = lo; i < b; ++i) f += dec::tiles_of(dec::clamp_len(p.cache_len[i], p.Lmax));
-    first_s = f;
-  }
-  __syncthreads();
-  const long first = (long)first_s;
-  const long nt = dec::tiles_of(dec::clamp_len(p.cache_len[b], p.Lmax));
-  const long eff = min((long)p.grid, total);               // the streaming kernel's CTAs that have tiles
-  const long i0 = prefix::owner_of(first, total, eff), i1 = prefix::owner_of(first + nt - 1, total, eff);
-  int np = (int)(i1 - i0 + 1);
-  if (!TA_IDX_OK(p.err, i0 + b, np, (long)p.grid + p.B)) np = 0;
   // The prefix's partials of head h: rows of a sequence may lie in two (or, never here, more) row blocks.
   auto pre_range = [&](int h, long& slot0, int& cnt, int& rloc) {
     slot0 = 0; cnt = 0; rloc = 0;
@@ -97,33 +81,44 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
   };
   // Up to here only inputs of the call were read; the partials come from the kernels before this one.
   pdl_enter();
+  const int i0 = p.seq_cta[2 * b];
+  int np = p.seq_cta[2 * b + 1] - i0 + 1;
+  if (!TA_IDX_OK(p.err, i0 + b, np, (long)p.grid + p.B)) np = 0;
   // ---- weights: warp w takes the partials w, w + WARPS, ... of all heads (lane = head) ----
   {
     const int h = lane;
     long ps0;
     int pc, prl;
     pre_range(h, ps0, pc, prl);
-    const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + (i0 + b) * 32 + h;
+    const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + (long)(i0 + b) * 32 + h;
     const float2* pml = reinterpret_cast<const float2*>(p.pre_ml) + ps0 * prefix::RB + prl;
     float m = -INFINITY;
-    for (int k = warp; k < np; k += WARPS) m = fmaxf(m, ml[(long)k * 32].x);
-    for (int k = warp; k < pc; k += WARPS) m = fmaxf(m, pml[(long)k * prefix::RB].x);
+#pragma unroll 2
+    for (int k = warp; k < np; k += WARPS) {
+      const float2 v = ml[(long)k * 32];
+      w_s[k * 32 + h] = v;
+      m = fmaxf(m, v.x);
+    }
+#pragma unroll 2
+    for (int k = warp; k < pc; k += WARPS) {
+      const float2 v = pml[(long)k * prefix::RB];
+      w_s[(np + k) * 32 + h] = v;
+      m = fmaxf(m, v.x);
+    }
     hm_s[warp][h] = m;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < WARPS; ++w) m = fmaxf(m, hm_s[w][h]);      // finite: a sequence's own part holds the new token
     float l = 0.f;
     for (int k = warp; k < np; k += WARPS) {
-      const float2 v = ml[(long)k * 32];
-      const float e = dec::ex2(v.x - m);
-      w_s[k * 32 + h] = e;
-      l = fmaf(v.y, e, l);
+      float2& v = w_s[k * 32 + h];
+      v.x = dec::ex2(v.x - m);
+      l = fmaf(v.y, v.x, l);
     }
     for (int k = warp; k < pc; k += WARPS) {
-      const float2 v = pml[(long)k * prefix::RB];
-      const float e = dec::ex2(v.x - m);
-      w_s[(np + k) * 32 + h] = e;
-      l = fmaf(v.y, e, l);
+      float2& v = w_s[(np + k) * 32 + h];
+      v.x = dec::ex2(v.x - m);
+      l = fmaf(v.y, v.x, l);
     }
     hl_s[warp][h] = l;
   }
@@ -140,17 +135,18 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
       const float* po = p.part_o + ((i0 + b) * 32 + h) * t3 + c;
       const float* pp = p.pre_o + ps0 * prefix::RB * t3 + ((long)(c / 4) * prefix::RB + prl) * 4;
       auto add = [&](const float* src, long stride, int n, int w0) {
-        for (int k0 = g; k0 < n; k0 += 4 * groups) {
-          float4 v[4];
+        constexpr int PF = 6;           // partials in flight per thread
+        for (int k0 = g; k0 < n; k0 += PF * groups) {
+          float4 v[PF];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+          for (int e = 0; e < PF; ++e) {
             const int k = k0 + e * groups;
             v[e] = k < n ? *reinterpret_cast<const float4*>(src + (long)k * stride) : make_float4(0.f, 0.f, 0.f, 0.f);
           }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+          for (int e = 0; e < PF; ++e) {
             const int k = k0 + e * groups;
-            const float wt = k < n ? w_s[(w0 + k) * 32 + h] : 0.f;
+            const float wt = k < n ? w_s[(w0 + k) * 32 + h].x : 0.f;
             acc.x = fmaf(wt, v[e].x, acc.x); acc.y = fmaf(wt, v[e].y, acc.y);
             acc.z = fmaf(wt, v[e].z, acc.z); acc.w = fmaf(wt, v[e].w, acc.w);
           }
@@ -188,42 +184,47 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
   __syncthreads();
   cluster_arrive();
   cluster_wait();
-  // ---- z: a warp per row; lane = (slice a of rpl, 16-byte chunk) ----
-  const int nch = t3 / 8, rpl = 32 / nch;                  // 8, 12 or 16 chunks; 4, 2 or 2 slices at a time
-  const int ga = lane / nch, ch = lane % nch;
-  const uint4* Cq = reinterpret_cast<const uint4*>(p.Ct);
-  for (int jl = warp; jl < jn; jl += WARPS) {
-    const int j = jbeg + jl;
+  // ---- z: a warp per row ----
+  auto dot = [&](const uint4 (&v)[4], int a0) -> float {
     float acc = 0.f;
-    for (int a0 = 0; a0 < p.t1; a0 += 4 * rpl) {
-      uint4 v[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int a = a0 + e * rpl + ga;
-        v[e] = (ga < rpl && a < p.t1) ? Cq[((long)a * p.t2 + j) * nch + ch] : make_uint4(0u, 0u, 0u, 0u);
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int a = a0 + e * rpl + ga;
-        if (ga < rpl && a < p.t1) {
-          const float4 u0 = reinterpret_cast<const float4*>(u_s + a * t3 + ch * 8)[0];
-          const float4 u1 = reinterpret_cast<const float4*>(u_s + a * t3 + ch * 8)[1];
-          const uint32_t wv[4] = {v[e].x, v[e].y, v[e].z, v[e].w};
-          const float2 k0 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[0]));
-          const float2 k1 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[1]));
-          const float2 k2 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[2]));
-          const float2 k3 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[3]));
-          acc = fmaf(u0.x, k0.x, acc); acc = fmaf(u0.y, k0.y, acc); acc = fmaf(u0.z, k1.x, acc); acc = fmaf(u0.w, k1.y, acc);
-          acc = fmaf(u1.x, k2.x, acc); acc = fmaf(u1.y, k2.y, acc); acc = fmaf(u1.z, k3.x, acc); acc = fmaf(u1.w, k3.y, acc);
-        }
+    for (int e = 0; e < 4; ++e) {
+      const int a = a0 + e * rpl + ga;
+      if (ga < rpl && a < p.t1) {
+        const float4 u0 = reinterpret_cast<const float4*>(u_s + a * t3 + ch * 8)[0];
+        const float4 u1 = reinterpret_cast<const float4*>(u_s + a * t3 + ch * 8)[1];
+        const uint32_t wv[4] = {v[e].x, v[e].y, v[e].z, v[e].w};
+        const float2 k0 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[0]));
+        const float2 k1 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[1]));
+        const float2 k2 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[2]));
+        const float2 k3 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[3]));
+        acc = fmaf(u0.x, k0.x, acc); acc = fmaf(u0.y, k0.y, acc); acc = fmaf(u0.z, k1.x, acc); acc = fmaf(u0.w, k1.y, acc);
+        acc = fmaf(u1.x, k2.x, acc); acc = fmaf(u1.y, k2.y, acc); acc = fmaf(u1.z, k3.x, acc); acc = fmaf(u1.w, k3.y, acc);
       }
     }
+    return acc;
+  };
+  for (int jl = warp; jl < jn; jl += 2 * WARPS) {            // two rows at a time
+    float acc[2] = {0.f, 0.f};
+    for (int a0 = 0; a0 < p.t1; a0 += 4 * rpl) {
+      uint4 v[2][4];
 #pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
-    if (lane == 0 && TA_IDX_OK(p.err, (long)b * 2 * p.z_half + p.z_half + j, 1, (long)p.B * 2 * p.z_half)) {
-      const bf16 zh = __float2bfloat16_rn(acc);
-      p.z[(long)b * 2 * p.z_half + j] = zh;
-      p.z[(long)b * 2 * p.z_half + p.z_half + j] = __float2bfloat16_rn(acc - __bfloat162float(zh));
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[r][e] = core(jl + r * WARPS, a0 + e * rpl + ga);
+#pragma unroll
+      for (int r = 0; r < 2; ++r) acc[r] += dot(v[r], a0);
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int j = jbeg + jl + r * WARPS;
+#pragma unroll
+      for (int off = 16; off >= 1; off >>= 1) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], off);
+      if (lane == 0 && jl + r * WARPS < jn && TA_IDX_OK(p.err, (long)b * 2 * p.z_half + p.z_half + j, 1, (long)p.B * 2 * p.z_half)) {
+        const bf16 zh = __float2bfloat16_rn(acc[r]);
+        p.z[(long)b * 2 * p.z_half + j] = zh;
+        p.z[(long)b * 2 * p.z_half + p.z_half + j] = __float2bfloat16_rn(acc[r] - __bfloat162float(zh));
+      }
     }
   }
   if (y == 0)
