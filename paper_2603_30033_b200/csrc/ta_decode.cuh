@@ -100,12 +100,25 @@ __device__ __forceinline__ float2 rope_cos_sin(int pos, int i, int r, double log
 //   qhat_h  <- qhat_h R(L, r3), stored bf16 [B, nH, r3]; with qhat_lo the rounded rest as well
 // The core is read with 16-byte loads that are all issued before anything waits on them:
 // warp w, lane (rg = lane / 4, ch = lane % 4) owns chunk ch of the CTA's 64-byte column range
-// in the core rows q = 8 w + rg + 64 i, for AB = 8 / NQ slices a at a time (NQ = ceil(r2/64)).
+// in the core rows q = 8 w + rg + 64 i, AB slices a at a time (NQ = ceil(r2/64)); the eight row groups
+// of a warp are summed by exchanging halves (56 shuffles for 64 values instead of 192).
 // part: [splits][Mpad][r2 + r3 + t3] fp32.  With pv.table the caches are pools of pages; pos_base is the position of slot 0.
 // ---------------------------------------------------------------------------------------
 constexpr int DQ_CW = 32;       // latent key coordinates per CTA
 constexpr int DQ_MAX_R1 = 32;   // head ranks r1, t1 supported by the shared-memory tables
 constexpr int DQ_MAX_R2 = 256;
+
+// p[0] + p[stride] + ... (n terms, n <= 16: all of them requested before the first is added), in that order
+__device__ __forceinline__ float split_sum(const float* __restrict__ p, int n, long stride) {
+  float v[16];
+#pragma unroll
+  for (int s = 0; s < 16; ++s) v[s] = s < n ? p[s * stride] : 0.f;
+  float acc = 0.f;
+#pragma unroll
+  for (int s = 0; s < 16; ++s)
+    if (s < n) acc += v[s];
+  return acc;
+}
 
 template <int NQ>
 __global__ void __launch_bounds__(256, 2)
@@ -114,7 +127,7 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
            bf16* __restrict__ knew, bf16* __restrict__ vnew, bf16* __restrict__ Kc, bf16* __restrict__ Vc, int Lmax,
            const int32_t* __restrict__ cache_len, int rope, const RopeFreqs freqs, int append, int shared_kv,
            const PagedView pv, int pos_base, bf16* __restrict__ qhat_lo, unsigned int* err) {
-  constexpr int AB = 8 / NQ;                        // core slices per batch (8 loads of 16 bytes in flight per thread)
+  constexpr int AB = NQ == 1 ? 8 : 4;               // core slices per batch (8 to 16 loads of 16 bytes in flight per thread)
   __shared__ float qt_s[DQ_MAX_R2];                 // latent query of the new token
   __shared__ float k_s[DQ_CW];                      // this CTA's coordinates of the new key (unrotated)
   __shared__ float2 cs_s[DQ_CW / 2];                // (cos, sin) at position L for this CTA's pairs
@@ -174,14 +187,12 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
                        TA_IDX_OK(err, (long)(splits - 1) * split_stride + (long)b * ncol, ncol, (long)splits * split_stride);
   for (int c = threadIdx.x; c < r2 + DQ_CW; c += blockDim.x) {
     const int col = c < r2 ? c : r2 + c0 + (c - r2);
-    float acc = 0.f;
-    if (prow_ok) for (int s = 0; s < splits; ++s) acc += prow[s * split_stride + col];
+    const float acc = prow_ok ? split_sum(prow + col, splits, split_stride) : 0.f;
     if (c < r2) qt_s[c] = acc; else k_s[c - r2] = acc;
   }
   for (int c = threadIdx.x; c < t3; c += blockDim.x) {
     if ((c / DQ_CW) % gridDim.y != blockIdx.y) continue;
-    float acc = 0.f;
-    if (prow_ok) for (int s = 0; s < splits; ++s) acc += prow[s * split_stride + r2 + r3 + c];
+    const float acc = prow_ok ? split_sum(prow + r2 + r3 + c, splits, split_stride) : 0.f;
     const bf16 vv = __float2bfloat16_rn(acc);
     if (TA_IDX_OK(err, (long)b * t3 + c, 1, (long)nB * t3)) vnew[(long)b * t3 + c] = vv;
     // shared_kv == 1 (one cache, no RoPE): the key row written below is the value row; == 2 (one cache with
@@ -220,16 +231,29 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
       }
     }
     if (a0 + AB < r1) load_batch(a0 + AB, v);       // next batch in flight during the reduction
+    // sums over the eight row groups (lane bits 2, 3, 4), in that order: at each level a lane keeps one half of its values
+    // and hands the other half to its partner
+    {
+      float* v = &acc[0][0];
+      constexpr int NV = AB * 8;
 #pragma unroll
-    for (int j = 0; j < AB; ++j)
+      for (int lev = 0; lev < 3; ++lev) {
+        const int half = NV >> (lev + 1);
+        const bool up = (rg >> lev) & 1;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float t = acc[j][e];
-        t += __shfl_xor_sync(0xffffffffu, t, 4);
-        t += __shfl_xor_sync(0xffffffffu, t, 8);
-        t += __shfl_xor_sync(0xffffffffu, t, 16);
-        if (rg == 0) red_s[warp][j][ch * 8 + e] = t;
+        for (int i = 0; i < half; ++i) {
+          const float mine = up ? v[i + half] : v[i], give = up ? v[i] : v[i + half];
+          v[i] = mine + __shfl_xor_sync(0xffffffffu, give, 4 << lev);
+        }
       }
+      // the lane is left with NV / 8 = AB values: those of index i + first
+      const int first = ((rg & 1) ? NV / 2 : 0) + ((rg & 2) ? NV / 4 : 0) + ((rg & 4) ? NV / 8 : 0);
+#pragma unroll
+      for (int i = 0; i < NV / 8; ++i) {
+        const int idx = first + i;
+        red_s[warp][idx / 8][ch * 8 + idx % 8] = v[i];
+      }
+    }
     __syncthreads();
     for (int i = threadIdx.x; i < AB * DQ_CW; i += blockDim.x) {
       const int j = i / DQ_CW, c = i % DQ_CW;
