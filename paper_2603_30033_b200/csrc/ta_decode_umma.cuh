@@ -78,7 +78,7 @@ struct Params {
   const int32_t* cache_len;
   const bf16* knew;    // [B, r3] rotated new key
   const bf16* vnew;    // [B, t3] new value
-  float* part_o;       // [grid + B][32][t3]
+  float* part_o;       // [grid + B][32][t3]; PAGED [grid + B][t3 / 4][32][4]
   float* part_ml;      // [grid + B][32][2]  (max in log2 units, sum)
   unsigned int* err;
   PagedView pv;        // PAGED
@@ -713,9 +713,15 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
           ml[1] = sum_s[wg][0][lane] + sum_s[wg][1][lane] + sum_s[wg][2][lane] + sum_s[wg][3][lane];
         }
         if (slot_ok && tid < p.t3) {
-          float* dst = p.part_o + slot * 32 * p.t3 + (long)(wg * HPW) * p.t3 + tid;
+          if constexpr (PAGED) {        // [t3 / 4][32 heads][4]: the join reads a column group of all heads at once
+            float* dst = p.part_o + slot * 32 * p.t3 + ((long)(tid / 4) * 32 + wg * HPW) * 4 + tid % 4;
 #pragma unroll
-          for (int h = 0; h < HPW; ++h) dst[h * p.t3] = __uint_as_float(o[h]);
+            for (int h = 0; h < HPW; ++h) dst[h * 4] = __uint_as_float(o[h]);
+          } else {
+            float* dst = p.part_o + slot * 32 * p.t3 + (long)(wg * HPW) * p.t3 + tid;
+#pragma unroll
+            for (int h = 0; h < HPW; ++h) dst[h * p.t3] = __uint_as_float(o[h]);
+          }
         }
         if (!(ok = wg_sync())) break;      // sum_s is free again before the next segment's flush writes it
       }

@@ -22,7 +22,7 @@ constexpr int MAX_PART = 2 * dec::MAX_GRID;      // partials of one head: one pe
 struct Params {
   int B, nH, t1, t2, t3, z_half;
   const int* seq_cta;                            // [B][2]
-  const float *part_o, *part_ml;                 // own keys: [grid + B][32][t3], [grid + B][32][2]
+  const float *part_o, *part_ml;                 // own keys: [grid + B][t3 / 4][32][4], [grid + B][32][2]
   int grid;
   const float *pre_o, *pre_ml;                   // prefix: [grid_p + n_rb][t3 / 4][RB][4], [..][RB][2]
   int grid_p, n_kt, n_rb;                        // n_rb = 0: no prefix
@@ -66,6 +66,14 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
   auto core = [&](int jl, int a) -> uint4 {
     return (jl < jn && ga < rpl && a < p.t1) ? Cq[((long)a * p.t2 + jbeg + jl) * nch + ch] : make_uint4(0u, 0u, 0u, 0u);
   };
+  {
+    // this CTA's rows of the core towards L2 (a long cache streamed through it has pushed them out) while the partials are merged
+    const char* rows = reinterpret_cast<const char*>(p.Ct) + (long)jbeg * t3 * 2;
+    const int lines = (jn * t3 * 2 + 127) / 128;
+    for (int a = warp; a < p.t1; a += WARPS)
+      for (int i = lane; i < lines; i += 32)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(rows + (long)a * p.t2 * t3 * 2 + i * 128));
+  }
   for (int i = tid; i < p.nH * p.t1; i += THREADS) ut1_s[i] = __bfloat162float(p.Ut1[i]);
   // The prefix's partials of head h: rows of a sequence may lie in two (or, never here, more) row blocks.
   auto pre_range = [&](int h, long& slot0, int& cnt, int& rloc) {
@@ -123,16 +131,16 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
     hl_s[warp][h] = l;
   }
   __syncthreads();
-  // ---- merge: item = (head, four columns), the partials dealt over the groups of threads ----
+  // ---- merge: item = (four columns, head), heads adjacent (512 bytes per load of 32 heads); partials dealt over groups of threads ----
   const int items = p.nH * q4, groups = min(16, THREADS / items);
   {
-    const int g = tid / items, it = tid % items, h = it / q4, c = c0 + (it % q4) * 4;
+    const int g = tid / items, it = tid % items, h = it % p.nH, c = c0 + it / p.nH * 4;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (g < groups) {
       long ps0;
       int pc, prl;
       pre_range(h, ps0, pc, prl);
-      const float* po = p.part_o + ((i0 + b) * 32 + h) * t3 + c;
+      const float* po = p.part_o + (long)(i0 + b) * 32 * t3 + ((long)(c / 4) * 32 + h) * 4;
       const float* pp = p.pre_o + ps0 * prefix::RB * t3 + ((long)(c / 4) * prefix::RB + prl) * 4;
       auto add = [&](const float* src, long stride, int n, int w0) {
         constexpr int PF = 6;           // partials in flight per thread
@@ -159,7 +167,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
   }
   __syncthreads();
   if (tid < items) {
-    const int h = tid / q4;
+    const int h = tid % p.nH;
     float4 s = red_s[tid];
     for (int g = 1; g < groups; ++g) {
       const float4 v = red_s[g * items + tid];
@@ -169,7 +177,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
 #pragma unroll
     for (int w = 0; w < WARPS; ++w) l += hl_s[w][h];
     const float inv = 1.f / l;
-    *reinterpret_cast<float4*>(o_s + h * MAX_COLS + (tid % q4) * 4) = make_float4(s.x * inv, s.y * inv, s.z * inv, s.w * inv);
+    *reinterpret_cast<float4*>(o_s + h * MAX_COLS + tid / p.nH * 4) = make_float4(s.x * inv, s.y * inv, s.z * inv, s.w * inv);
   }
   __syncthreads();
   cluster_wait();
