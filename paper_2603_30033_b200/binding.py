@@ -138,9 +138,15 @@ def status_string(status: int) -> str:
     return load_library().tucker_attn_status_string(int(status)).decode()
 
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _dtype_code(t) -> int:
@@ -183,7 +189,7 @@ def decode_workspace_bytes(desc: TuckerAttnDesc, Lmax: int) -> int:
 def alloc_workspace(nbytes: int, device):
     """Device scratch buffer (256-byte aligned by the torch allocator)."""
     torch = _torch()
-    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+    return torch.empty(nbytes if nbytes > 256 else 256, dtype=torch.uint8, device=device)
 
 
 class _on_device:
@@ -340,15 +346,25 @@ def tucker_attn_decode_static(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kcache, Vcach
     return out
 
 
-def _paged_cache(Kpages, Vpages, block_table, B, r3, t3, dtype, device):
-    """Checks the pools and the block table of a paged cache; returns its `tucker_paged_cache`."""
-    torch = _torch()
+def _check_all(items, dtype, device):
+    """_check of every (tensor, name, shape), with the usual outcome decided in one pass."""
+    idx = device.index
+    for t, name, shape in items:
+        if not (t.dtype is dtype and t.shape == shape and t.get_device() == idx and t.is_contiguous()):
+            _check(t, name, shape, dtype, device)
+
+
+def _paged_items(Kpages, Vpages, block_table, cache_len, B, r3, t3):
+    """What _check_all checks of a paged cache: (items of the storage type, int32 items)."""
     if Kpages.dim() != 3 or block_table.dim() != 2:
         raise ValueError("Kpages must be [n_pages, page_size, r3] and block_table [B, max_pages]")
     n_pages, page_size, _ = Kpages.shape
-    _check(Kpages, "Kpages", (n_pages, page_size, r3), dtype, device)
-    _check(Vpages, "Vpages", (n_pages, page_size, t3), dtype, device)
-    _check(block_table, "block_table", (B, block_table.shape[1]), torch.int32, device)
+    return (((Kpages, "Kpages", (n_pages, page_size, r3)), (Vpages, "Vpages", (n_pages, page_size, t3))),
+            ((block_table, "block_table", (B, block_table.shape[1])), (cache_len, "cache_len", (B,))))
+
+
+def _paged_struct(Kpages, Vpages, block_table):
+    n_pages, page_size, _ = Kpages.shape
     return TuckerPagedCache(Kpages.data_ptr(), Vpages.data_ptr(), block_table.data_ptr(), n_pages, page_size,
                             block_table.shape[1])
 
@@ -361,27 +377,26 @@ def tucker_cache_append_paged(X, U3, Ut3, Kpages, Vpages, block_table, cache_len
     block_table [B, max_pages], cache_len [B] and tok_start [B + 1] int32 on the device."""
     torch = _torch()
     lib = load_library()
-    if X.dim() != 2 or cache_len.dim() != 1:
-        raise ValueError("X must be [T, d_model] and cache_len [B]")
+    if X.dim() != 2 or cache_len.dim() != 1 or U3.dim() != 2 or Ut3.dim() != 2:
+        raise ValueError("X must be [T, d_model], cache_len [B], U3 and Ut3 [d_model, rank]")
     T, d = X.shape
     B = cache_len.shape[0]
     dev, dt = X.device, X.dtype
-    r3, t3 = U3.shape[-1], Ut3.shape[-1]
-    _check(X, "X", (T, d), dt, dev)
-    _check(U3, "U3", (d, r3), dt, dev)
-    _check(Ut3, "Ut3", (d, t3), dt, dev)
-    _check(cache_len, "cache_len", (B,), torch.int32, dev)
-    _check(tok_start, "tok_start", (B + 1,), torch.int32, dev)
-    cache = _paged_cache(Kpages, Vpages, block_table, B, r3, t3, dt, dev)
-    desc = make_desc(B=B, N=1, d_model=d, n_H=1, r=(1, 1, r3), t=(1, 1, t3), causal=True, rope=rope, rope_base=rope_base,
-                     pos0=pos0, dtype=_dtype_code(X), flags=flags)
+    code = _dtype_code(X)
+    r3, t3 = U3.shape[1], Ut3.shape[1]
+    data, ints = _paged_items(Kpages, Vpages, block_table, cache_len, B, r3, t3)
+    _check_all(((X, "X", (T, d)), (U3, "U3", (d, r3)), (Ut3, "Ut3", (d, t3))) + data, dt, dev)
+    _check_all(ints + ((tok_start, "tok_start", (B + 1,)),), torch.int32, dev)
+    cache = _paged_struct(Kpages, Vpages, block_table)
+    desc = TuckerAttnDesc(B, 1, d, 1, 1, 1, r3, 1, 1, t3, 1, int(bool(rope)), float(rope_base), int(pos0), 0.0, code, int(flags))
+    pd, pc = ctypes.byref(desc), ctypes.byref(cache)
     if workspace is None:
-        workspace = alloc_workspace(lib.tucker_cache_append_paged_workspace_bytes(ctypes.byref(desc), ctypes.byref(cache), int(T)), dev)
-    _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
+        workspace = alloc_workspace(lib.tucker_cache_append_paged_workspace_bytes(pd, pc, T), dev)
+    else:
+        _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
     with _on_device(dev):
-        rc = lib.tucker_cache_append_paged(ctypes.byref(desc), X.data_ptr(), U3.data_ptr(), Ut3.data_ptr(), ctypes.byref(cache),
-                                           cache_len.data_ptr(), tok_start.data_ptr(), int(T), workspace.data_ptr(),
-                                           workspace.numel(), _stream_ptr(dev))
+        rc = lib.tucker_cache_append_paged(pd, X.data_ptr(), U3.data_ptr(), Ut3.data_ptr(), pc, cache_len.data_ptr(),
+                                           tok_start.data_ptr(), T, workspace.data_ptr(), workspace.numel(), _stream_ptr(dev))
     if rc != TA_OK:
         raise TuckerAttnError(rc, "tucker_cache_append_paged")
 
@@ -396,33 +411,38 @@ def tucker_attn_decode_prefix(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kpages, Vpage
     lib = load_library()
     if x.dim() != 2:
         raise ValueError("x must be [B, d_model]")
+    if C.dim() != 3 or Ct.dim() != 3:
+        raise ValueError("cores must be 3-way tensors")
     B, d = x.shape
     dev, dt = x.device, x.dtype
-    _check(x, "x", (B, d), dt, dev)
-    r, t = _weights_check((C, U1, U2, U3, Ct, Ut1, Ut2, Ut3), d, n_H, dt, dev)
-    _check(cache_len, "cache_len", (B,), torch.int32, dev)
-    cache = _paged_cache(Kpages, Vpages, block_table, B, r[2], t[2], dt, dev)
+    code = _dtype_code(x)
+    (r1, r2, r3), (t1, t2, t3) = C.shape, Ct.shape
+    data, ints = _paged_items(Kpages, Vpages, block_table, cache_len, B, r3, t3)
+    if out is None:
+        out = torch.empty_like(x)
+    _check_all(((x, "x", (B, d)), (C, "C", (r1, r2, r3)), (U1, "U1", (n_H, r1)), (U2, "U2", (d, r2)), (U3, "U3", (d, r3)),
+                (Ct, "Ct", (t1, t2, t3)), (Ut1, "Ut1", (n_H, t1)), (Ut2, "Ut2", (d, t2)), (Ut3, "Ut3", (d, t3)),
+                (out, "out", (B, d))) + data, dt, dev)
     prefix_len = int(prefix_len)
     if prefix_len < 0:
         raise ValueError("prefix_len must not be negative")
     if prefix_len > 0:
-        if prefix_table is None or prefix_table.dim() != 1 or prefix_table.shape[0] * cache.page_size < prefix_len:
+        if prefix_table is None or prefix_table.dim() != 1 or prefix_table.shape[0] * Kpages.shape[1] < prefix_len:
             raise ValueError("prefix_table must hold the ceil(prefix_len / page_size) pages of the prefix")
-        _check(prefix_table, "prefix_table", tuple(prefix_table.shape), torch.int32, dev)
-    desc = make_desc(B=B, N=1, d_model=d, n_H=n_H, r=r, t=t, causal=True, rope=rope, rope_base=rope_base, pos0=0, scale=scale,
-                     dtype=_dtype_code(x), flags=flags)
-    if out is None:
-        out = torch.empty_like(x)
-    _check(out, "out", (B, d), dt, dev)
+        ints += ((prefix_table, "prefix_table", prefix_table.shape),)
+    _check_all(ints, torch.int32, dev)
+    cache = _paged_struct(Kpages, Vpages, block_table)
+    desc = TuckerAttnDesc(B, 1, d, int(n_H), r1, r2, r3, t1, t2, t3, 1, int(bool(rope)), float(rope_base), 0, float(scale), code,
+                          int(flags))
+    pd, pc = ctypes.byref(desc), ctypes.byref(cache)
     if workspace is None:
-        workspace = alloc_workspace(lib.tucker_attn_decode_prefix_workspace_bytes(ctypes.byref(desc), ctypes.byref(cache),
-                                                                                  prefix_len), dev)
-    _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
+        workspace = alloc_workspace(lib.tucker_attn_decode_prefix_workspace_bytes(pd, pc, prefix_len), dev)
+    else:
+        _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
     with _on_device(dev):
-        rc = lib.tucker_attn_decode_prefix(ctypes.byref(desc), x.data_ptr(), C.data_ptr(), U1.data_ptr(), U2.data_ptr(),
-                                           U3.data_ptr(), Ct.data_ptr(), Ut1.data_ptr(), Ut2.data_ptr(), Ut3.data_ptr(),
-                                           ctypes.byref(cache), cache_len.data_ptr(),
-                                           prefix_table.data_ptr() if prefix_len > 0 else None, prefix_len,
+        rc = lib.tucker_attn_decode_prefix(pd, x.data_ptr(), C.data_ptr(), U1.data_ptr(), U2.data_ptr(), U3.data_ptr(),
+                                           Ct.data_ptr(), Ut1.data_ptr(), Ut2.data_ptr(), Ut3.data_ptr(), pc,
+                                           cache_len.data_ptr(), prefix_table.data_ptr() if prefix_len else None, prefix_len,
                                            int(bool(append)), out.data_ptr(), workspace.data_ptr(), workspace.numel(),
                                            _stream_ptr(dev))
     if rc != TA_OK:
