@@ -39,7 +39,7 @@
 // This form also takes the query as the sum of two bf16 numbers (the rounded value and the rounded rest, 2^-17 together):
 // a query rounded once moves every score by 2^-9 of its size, which at scores of a standard deviation of 2 was two thirds of
 // the step's whole error (4.7e-3 of the output's norm, 2.3e-3 with the second half).  The second half is eight more MMAs of
-// N = 32 per tile, hidden behind the loads.  The two halves share the room of two segments' queries, so that with r3 > 64 one
+// N = 32 per tile, hidden behind the loads.  With ROT the rotated keys are carried the same way (3.5e-3 -> 2.1e-3; 39 -> 42 us at 24 sequences of up to 3001 tokens).  The two halves share the room of two segments' queries, so that with r3 > 64 one
 // segment's queries are in flight instead of two.
 #pragma once
 
@@ -60,6 +60,7 @@ constexpr int HPW = 32 / NWG;             // head columns per warpgroup
 constexpr int THREADS = 128 + 128 * NWG;
 constexpr int THREADS_ROT = THREADS + 128;           // plus the rotation warpgroup
 constexpr uint32_t TMEM_KROT = 128;                   // first TMEM column of the two rotated key tiles (64 columns each)
+constexpr uint32_t TMEM_KROT_LO = 256;                // PAGED: of their rounded rests
 constexpr int MAX_STAGES = 6;
 constexpr int SUB_BYTES = 128 * 64 * 2;  // [128 keys x 64] bf16
 constexpr int MAX_SUB = 2;               // r3, t3 <= 128
@@ -154,6 +155,7 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
   // began: set-up and the tile split run while it finishes, and every role passes pdl_enter() before it
   // touches anything else.  (Requesting the first cache tiles ahead of that wait as well was measured:
   // no gain with two caches, 6 us slower with the shared cache.)
+  constexpr uint32_t TMEM_COLS = ROT ? (PAGED ? 512u : 256u) : 128u;
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full_bar[MAX_STAGES], empty_bar[MAX_STAGES], q_full[2], q_empty[2];
   __shared__ uint64_t s_full[2], s_free[2], p_full[2], p_free[2], o_read, patched, wg_bar[NWG];
@@ -207,7 +209,7 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     fence_barrier_init();
   }
   if (warp == 1) {
-    tmem_alloc(&tmem_slot, ROT ? 256 : 128);
+    tmem_alloc(&tmem_slot, TMEM_COLS);
     tmem_relinquish();
   }
   tc_fence_before();
@@ -423,6 +425,13 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 if (ROT) umma_ts(d, akr + (uint32_t)ks * 8u, dqk, idesc_qk, 1u);
                 else umma_ss(d, dk + (uint64_t)((ks >> 2) * (SUB_BYTES >> 4) + (ks & 3) * 2), dqk, idesc_qk, 1u);
               }
+            if constexpr (ROT) {       // ... and the rotated keys' (the rows in the cache are exact, their rotation is not)
+#pragma unroll
+              for (int ks = 0; ks < 8; ++ks)
+                if (ks < ksteps)
+                  umma_ts(d, akr + (TMEM_KROT_LO - TMEM_KROT) + (uint32_t)ks * 8u,
+                          dq + (uint64_t)((ks >> 2) * (QSUB_BYTES >> 4) + (ks & 3) * 2), idesc_qk, 1u);
+            }
           }
           umma_commit(&s_full[buf]);
           if (ROT) umma_commit(&kr_free[buf]);
@@ -495,6 +504,7 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
        const int rnew = w.L - k0;               // row of the new token (last tile of a sequence only)
        const bool is_new = last && tid == rnew;
        const uint32_t kaddr = tmem + TMEM_KROT + (uint32_t)buf * 64u + ((uint32_t)(q * 32) << 16);
+       if constexpr (!PAGED) {
 #pragma unroll
        for (int hf = 0; hf < 2; ++hf) {         // 32 TMEM columns = 64 coordinates at a time
          if (hf * 64 < R3C) {
@@ -532,6 +542,42 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
            }
            tmem_st32(kaddr + (uint32_t)hf * 32u, o);
          }
+       }
+       } else {
+#pragma unroll
+       for (int hf = 0; hf < R3C / 32; ++hf) {  // 16 TMEM columns = 32 coordinates at a time, rounded values and rounded rests
+         uint32_t o[16], ol[16];
+#pragma unroll
+         for (int cc = 0; cc < 4; ++cc) {
+           const int c = hf * 4 + cc;           // 16-byte chunk of the row
+           const uint4 v = *reinterpret_cast<const uint4*>(raw + swz(tid, c));
+           const uint32_t wv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+           for (int e = 0; e < 4; ++e) {
+             const int i = 4 * c + e;
+             const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[e]));
+             const float2 bs = make_float2(__shfl_sync(0xffffffffu, i < 32 ? base_lo.x : base_hi.x, i & 31),
+                                           __shfl_sync(0xffffffffu, i < 32 ? base_lo.y : base_hi.y, i & 31));
+             const float cs_c = ac[i] * bs.x - as_[i] * bs.y, cs_s = as_[i] * bs.x + ac[i] * bs.y;   // angle addition
+             const float re = x.x * cs_c - x.y * cs_s, ro = x.x * cs_s + x.y * cs_c;
+             o[4 * cc + e] = pack_bf16(re, ro);
+             const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&o[4 * cc + e]));
+             ol[4 * cc + e] = pack_bf16(re - f.x, ro - f.y);
+           }
+         }
+         if (is_new) {
+           // the new token's rotated key comes from the workspace
+           const uint4* kn = reinterpret_cast<const uint4*>(p.knew + (long)w.b * p.r3) + hf * 4;
+#pragma unroll
+           for (int cc = 0; cc < 4; ++cc) {
+             const uint4 v = kn[cc];
+             o[4 * cc] = v.x; o[4 * cc + 1] = v.y; o[4 * cc + 2] = v.z; o[4 * cc + 3] = v.w;
+             ol[4 * cc] = ol[4 * cc + 1] = ol[4 * cc + 2] = ol[4 * cc + 3] = 0u;
+           }
+         }
+         tmem_st16(kaddr + (uint32_t)hf * 16u, o);
+         tmem_st16(kaddr + (TMEM_KROT_LO - TMEM_KROT) + (uint32_t)hf * 16u, ol);
+       }
        }
        tmem_st_wait();
        if (last) {
@@ -730,7 +776,7 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 1) tmem_dealloc(tmem, ROT ? 256 : 128);
+  if (warp == 1) tmem_dealloc(tmem, TMEM_COLS);
 }
 
 }  // namespace decu
