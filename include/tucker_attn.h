@@ -195,10 +195,14 @@ TA_API int tucker_attn_decode_static(const tucker_attn_desc* desc, const void* x
  * block_table, cache_len, tok_start and prefix_table are DEVICE memory and are read when the call's kernels run.  A
  * table entry that is needed and lies outside [0, n_pages) sets TA_DEVERR_BAD_PAGE: its rows count as zeros, nothing is
  * written through it.  A cache_len outside [0, max_pages * page_size) sets TA_DEVERR_BAD_CACHE_LEN (decode clamps it as
- * tucker_attn_decode does; append drops the tokens concerned).  Two sequences may read the same page (a prefix that
+ * tucker_attn_decode does, and appends nothing to that sequence; append drops the tokens concerned).  Two sequences may read the same page (a prefix that
  * both hold); a page that a call WRITES belongs to one sequence only, else it is not defined whose row it holds.
  *
- * Limits: B <= 65535, B n_H <= 2^24, max_pages * page_size + (pos0 or prefix_len) < 2^31.  Any page_size >= 1.
+ * Limits: B <= 65535, B n_H <= 2^24, max_pages * page_size + (pos0 or prefix_len) < 2^31 - 4096.  Any page_size >= 1.
+ * bf16 decode shapes that the contiguous step runs on tensor cores do so here with a page_size of 16, 32, 64 or a multiple of
+ * 128; bf16 appends with d_model a multiple of 64 and ranks that are multiples of 32 up to 256, with any page_size.  Everything
+ * else runs on fp32 FMA kernels.  A workspace must not be in use by another call that may overlap on the GPU (other streams,
+ * other captured graphs); nothing in it is kept from one call to the next.
  */
 typedef struct {
   void* K;                    /* [n_pages, page_size, r3]  device */

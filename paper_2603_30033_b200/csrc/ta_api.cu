@@ -60,11 +60,11 @@ static bool shared_kv_weights(const tucker_attn_desc& d, const void* U3, const v
 }
 
 // A paged cache's host-side description.  Slots are counted in 32 bits: max_pages * page_size + `before` (the tokens in
-// front of slot 0) must stay below 2^31.
+// front of slot 0) must stay below 2^31 - 4096, so that a tile that starts at an existing slot ends in 32 bits.
 static bool paged_ok(const tucker_paged_cache* c, int64_t before) {
   if (!c || !c->K || !c->V || !c->block_table) return false;
   if (c->n_pages <= 0 || c->page_size <= 0 || c->max_pages <= 0 || before < 0) return false;
-  return (int64_t)c->max_pages * c->page_size + before < (int64_t)1 << 31;
+  return (int64_t)c->max_pages * c->page_size + before < ((int64_t)1 << 31) - 4096;
 }
 static int64_t paged_slots(const tucker_paged_cache& c) { return (int64_t)c.max_pages * c.page_size; }
 

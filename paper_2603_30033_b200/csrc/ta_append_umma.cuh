@@ -115,7 +115,8 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
     if (elect_one()) {
       tma_prefetch_desc(&tmX); tma_prefetch_desc(&tmB0); tma_prefetch_desc(&tmB1);
       const CUtensorMap* tb0 = blockIdx.y == 0 ? &tmB0 : &tmB1;
-      for (int kb = kb0; kb < kb1; ++kb) {
+      int issued = 0;
+      for (int kb = kb0; kb < kb1; ++kb, ++issued) {
         const int i = kb - kb0, st = i % stages;
         if (!mbar_wait(&empty_bar[st], ((i / stages) & 1) ^ 1, ab)) break;
         mbar_expect_tx(&full_bar[st], stage_bytes);
@@ -127,6 +128,8 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
         if (p1.width)
           for (int j = 0; j < boxes(p1.width); ++j) tma_load_2d(b + j * BOX_BYTES, &tmB1, &full_bar[st], j * 64, kb * BK);
       }
+      if (ab.raised())                             // the copies in flight end before the CTA does
+        for (int i = max(0, issued - stages); i < issued; ++i) mbar_drain(&full_bar[i % stages], (uint32_t)((i / stages) & 1));
     }
   } else if (warp == 1) {
     if (elect_one()) {

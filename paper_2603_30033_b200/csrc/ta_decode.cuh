@@ -156,6 +156,7 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
   if (L < 0 || L >= Lmax) {
     if (threadIdx.x == 0 && blockIdx.y == 0) atomicOr(err, (unsigned)TA_DEVERR_BAD_CACHE_LEN);
     L = clamp_len(L, Lmax);
+    if (pv.table) append = 0;                       // a page is not written on the strength of a clamped length
   }
   // cache row of the new token (-1: the page it needs does not exist, flagged) and rows that exist
   long new_row = (long)b * Lmax + L;

@@ -298,6 +298,10 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             for (int kk = 0; kk < vsub; ++kk) tma_load_3d(vt + kk * SUB_BYTES, &tmV, &full_bar[s], kk * 64, in_page, pg);
         }
       }
+      if (ab.raised()) {                           // the copies in flight end before the CTA does
+        for (int i = max(0, it - STAGES); i < it; ++i) mbar_drain(&full_bar[i % STAGES], (uint32_t)((i / STAGES) & 1));
+        if (seg >= 0) mbar_drain(&q_full[seg & (NQ - 1)], (uint32_t)((seg >> QSH) & 1));
+      }
     } else if (elect_one()) {
       tma_prefetch_desc(&tmK); tma_prefetch_desc(&tmV); tma_prefetch_desc(&tmQ);
       Walk w;
@@ -721,8 +725,11 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
 #pragma unroll
         for (int h = 0; h < HPW; ++h) {
           const float pv = ex2(sc[h] - m_used[h]);
-          l_acc[h] += pv;
-          *reinterpret_cast<__nv_bfloat16*>(my_p + (h >> 3) * 1024 + p_sw[h & 7]) = __float2bfloat16_rn(pv);
+          const __nv_bfloat16 pb = __float2bfloat16_rn(pv);
+          // PAGED: the sum of the ROUNDED probabilities, so that a rounding which all of a row's weight shares cancels
+          // in the quotient (one dominant key: completely)
+          l_acc[h] += PAGED ? __bfloat162float(pb) : pv;
+          *reinterpret_cast<__nv_bfloat16*>(my_p + (h >> 3) * 1024 + p_sw[h & 7]) = pb;
         }
       }
       fence_proxy_async_smem();

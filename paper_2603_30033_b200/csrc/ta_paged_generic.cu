@@ -236,6 +236,7 @@ __global__ void __launch_bounds__(256) k_pg_queries(const float* __restrict__ w,
   if (L < 0 || L >= Lmax) {
     if (threadIdx.x == 0 && blockIdx.y == 0) atomicOr(err, (unsigned)TA_DEVERR_BAD_CACHE_LEN);
     L = L < 0 ? 0 : Lmax - 1;
+    append = 0;                               // a page is not written on the strength of a clamped length
   }
   const int half = (r3 + 1) / 2;
   if (rope)

@@ -33,7 +33,7 @@ struct Params {
 
 __host__ __device__ inline size_t smem_bytes(int cl, int t1, int t3, int nH, bool with_prefix) {
   const int parts = with_prefix ? MAX_PART : dec::MAX_GRID;
-  return sizeof(float) * ((size_t)parts * 64 + (size_t)t1 * t3 + (size_t)nH * t1 + (size_t)THREADS * 4 + 32 * (128 / cl));
+  return sizeof(float) * ((size_t)parts * 64 + (size_t)t1 * t3 + ((size_t)nH * t1 + 1) / 2 * 2 + (size_t)THREADS * 4 + 32 * (128 / cl));
 }
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }

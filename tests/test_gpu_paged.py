@@ -157,7 +157,7 @@ def test_far_positions():
     stored: its slots are read through a one-page table, so prefix_len stays small and pos0 of the append carries the offset."""
     w = workload(TC64, "bf16")
     st = P.PagedState(w, [3, 0], 16, new=[5, 2])
-    pos0 = 2 ** 31 - 1 - 4096
+    pos0 = 2 ** 31 - 1 - 8192
     check_append(st, [5, 2], pos0=pos0)
 
 
@@ -194,6 +194,14 @@ def check_append(st, new, pad=0, front=0, pos0=0, flags=0, seed=3):
     for name, pool, before, rows in (("K", K, k0, vr if st.shared else kr), ("V", V, v0, vr)):
         want, mask = st.expect_pool(before.astype(np.float64), rows, 0)
         P.check_pool(host(pool), before, want, mask, w.dtype, f"append {name} {new}")
+
+
+@pytest.mark.parametrize("r3,t3", [(32, 32), (32, 256), (160, 64), (256, 256), (96, 224)])
+@pytest.mark.parametrize("rope", [True, False])
+def test_append_rank_widths(r3, t3, rope):
+    new = [70, 1, 140]
+    shape = dict(d_model=640, n_H=4, r=(2, 32, r3), t=(2, 32, t3))
+    check_append(P.PagedState(workload(shape, "bf16", rope=rope), [3, 0, 90], 16, new=new), new, pad=9)
 
 
 APPENDS = [[1], [0, 1], [3, 0, 0, 7], [1] * 9, [127], [128], [129], [40, 0, 300, 1], [0, 0, 2]]
@@ -314,6 +322,58 @@ def test_binding_refuses():
     assert Bd.last_device_error() == 0
 
 
+def test_pages_past_32_bit_offsets():
+    """Pages whose rows lie past 2^32 bytes and past 2^31 elements of the pool: the same rows, and the same results bit for bit, as
+    in a small pool.  One pool serves keys and values (half the memory); both ways of appending, both attention kernels."""
+    import torch
+    shape = dict(d_model=256, n_H=8, r=(4, 64, 128), t=(4, 64, 128))
+    w = workload(shape, "bf16", rope=False, shared=True)
+    st = P.PagedState(w, [300, 0, 129], 128, P=260, new=5)
+    x, dw, K, _, table, lens, ptab = st.device()
+    big_pages = 2 ** 31 // (128 * 128) + 64
+    free, _ = torch.cuda.mem_get_info()
+    if free < 3 * big_pages * 128 * 128 * 2:
+        pytest.skip("needs 13 GB of device memory")
+    big = torch.empty(big_pages, 128, 128, device="cuda", dtype=torch.bfloat16)
+    shift = big_pages - st.n_pages
+    big[shift:] = K
+    X = torch.randn(6, 256, device="cuda").bfloat16()
+    start = torch.tensor([0, 4, 4, 6], dtype=torch.int32, device="cuda")
+    up = lambda t: torch.where((t >= 0) & (t < st.n_pages), t + shift, t).int()
+    out = []
+    for pool, tb, pt in ((K, table, ptab), (big, up(table), up(ptab))):
+        Bd.tucker_cache_append_paged(X, dw[3], dw[7], pool, pool, tb, lens, start, rope=False)
+        n = lens + torch.tensor([4, 0, 2], dtype=torch.int32, device="cuda")
+        out.append(Bd.tucker_attn_decode_prefix(x, *dw, pool, pool, tb, n, pt, 260, n_H=8, rope=False))
+        out.append(Bd.tucker_attn_decode_paged(x, *dw, pool, pool, tb, n, n_H=8, rope=False, flags=Bd.TA_FLAG_FORCE_GENERIC))
+        assert Bd.last_device_error() == 0
+    bits = lambda t: t.view(torch.int16)
+    assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[3])
+    assert torch.equal(bits(big[shift:]), bits(K))
+
+
+def test_bad_length_appends_nothing():
+    import torch
+    for dtype, shape in (("fp32", SMALL), ("bf16", TC64)):
+        st = P.PagedState(workload(shape, dtype), [5, 20], 16)
+        x, dw, K, V, table, lens, _ = st.device()
+        lens[1] = -1
+        K0, V0 = K.clone(), V.clone()
+        Bd.tucker_attn_decode_paged(x, *dw, K, V, table, lens, n_H=st.w.n_H, rope=True)
+        assert Bd.last_device_error() == Bd.TA_DEVERR_BAD_CACHE_LEN
+        pg = int(table[1, 0])
+        bits = torch.int16 if dtype == "bf16" else torch.int32
+        assert torch.equal(K[pg].view(bits), K0[pg].view(bits)) and torch.equal(V[pg].view(bits), V0[pg].view(bits))
+
+
+def test_flagged_generic_path_agrees():
+    """TA_FLAG_FORCE_GENERIC runs bf16 on the FMA kernels: within the roundings of the tensor-core path of it."""
+    st = P.PagedState(workload(TC128, "bf16"), [700, 0, 33], 16, P=150)
+    a, Ka, Va = run_step(st)
+    b, Kb, Vb = run_step(st, flags=Bd.TA_FLAG_FORCE_GENERIC)
+    P.check_rows(host(a), host(b).astype(np.float64), "bf16", "generic against tensor-core")
+
+
 # ---- together --------------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype,shape", [("fp32", SMALL), ("bf16", TC64)])
@@ -429,3 +489,21 @@ def test_two_streams_at_once():
         assert Bd.last_device_error() == 0
         for a, g in zip(alone, got):
             assert torch.equal(a, g)
+
+
+# ---- bounds-checking build ---------------------------------------------------------------------------------------------------
+
+@pytest.mark.skipif(__import__("os").environ.get("TA_BOUNDS_CHECK_CHILD") == "1", reason="already inside a bounds-checking run")
+def test_paged_calls_under_the_bounds_checking_build():
+    """The paged tests once more in a child process that loads the library built with -DTA_BOUNDS_CHECK: every global index that the
+    kernels form for a store, or for a load from the workspace, is compared with its tensor's extent; each test asserts a clean
+    error word."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    env = dict(os.environ, TUCKER_ATTN_LIB="checked", TA_BOUNDS_CHECK_CHILD="1")
+    r = subprocess.run([sys.executable, "-m", "pytest", "-x", "-q", "-m", "gpu", "-p", "no:cacheprovider", "-k",
+                        "page_sizes or paged_shapes or prefix_lengths or prefix_batches or append or shared_latent_pool or together",
+                        os.path.abspath(__file__)], env=env, cwd=root, capture_output=True, text=True, timeout=900)
+    assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
