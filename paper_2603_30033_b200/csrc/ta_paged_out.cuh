@@ -165,6 +165,12 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
     }
     red_s[tid] = acc;
   }
+  // the first slices of this warp's first two rows of the core: requested here, used behind two barriers
+  uint4 pre[2][4];
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) pre[r][e] = core(warp + r * WARPS, e * rpl + ga);
   __syncthreads();
   if (tid < items) {
     const int h = tid % p.nH;
@@ -193,35 +199,38 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
   cluster_arrive();
   cluster_wait();
   // ---- z: a warp per row ----
-  auto dot = [&](const uint4 (&v)[4], int a0) -> float {
-    float acc = 0.f;
+  auto dot = [&](const uint4 (&v)[2][4], int a0, float (&acc)[2]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int a = a0 + e * rpl + ga;
       if (ga < rpl && a < p.t1) {
         const float4 u0 = reinterpret_cast<const float4*>(u_s + a * t3 + ch * 8)[0];
         const float4 u1 = reinterpret_cast<const float4*>(u_s + a * t3 + ch * 8)[1];
-        const uint32_t wv[4] = {v[e].x, v[e].y, v[e].z, v[e].w};
-        const float2 k0 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[0]));
-        const float2 k1 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[1]));
-        const float2 k2 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[2]));
-        const float2 k3 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[3]));
-        acc = fmaf(u0.x, k0.x, acc); acc = fmaf(u0.y, k0.y, acc); acc = fmaf(u0.z, k1.x, acc); acc = fmaf(u0.w, k1.y, acc);
-        acc = fmaf(u1.x, k2.x, acc); acc = fmaf(u1.y, k2.y, acc); acc = fmaf(u1.z, k3.x, acc); acc = fmaf(u1.w, k3.y, acc);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const uint32_t wv[4] = {v[r][e].x, v[r][e].y, v[r][e].z, v[r][e].w};
+          const float2 k0 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[0]));
+          const float2 k1 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[1]));
+          const float2 k2 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[2]));
+          const float2 k3 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[3]));
+          float t = acc[r];
+          t = fmaf(u0.x, k0.x, t); t = fmaf(u0.y, k0.y, t); t = fmaf(u0.z, k1.x, t); t = fmaf(u0.w, k1.y, t);
+          t = fmaf(u1.x, k2.x, t); t = fmaf(u1.y, k2.y, t); t = fmaf(u1.z, k3.x, t); t = fmaf(u1.w, k3.y, t);
+          acc[r] = t;
+        }
       }
     }
-    return acc;
   };
   for (int jl = warp; jl < jn; jl += 2 * WARPS) {            // two rows at a time
     float acc[2] = {0.f, 0.f};
     for (int a0 = 0; a0 < p.t1; a0 += 4 * rpl) {
-      uint4 v[2][4];
+      if (jl != warp || a0 != 0) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r)
+        for (int r = 0; r < 2; ++r)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[r][e] = core(jl + r * WARPS, a0 + e * rpl + ga);
-#pragma unroll
-      for (int r = 0; r < 2; ++r) acc[r] += dot(v[r], a0);
+          for (int e = 0; e < 4; ++e) pre[r][e] = core(jl + r * WARPS, a0 + e * rpl + ga);
+      }
+      dot(pre, a0, acc);
     }
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
