@@ -75,18 +75,22 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
         asm volatile("prefetch.global.L2 [%0];" ::"l"(rows + (long)a * p.t2 * t3 * 2 + i * 128));
   }
   for (int i = tid; i < p.nH * p.t1; i += THREADS) ut1_s[i] = __bfloat162float(p.Ut1[i]);
-  // The prefix's partials of head h: rows of a sequence may lie in two (or, never here, more) row blocks.
-  auto pre_range = [&](int h, long& slot0, int& cnt, int& rloc) {
-    slot0 = 0; cnt = 0; rloc = 0;
-    if (p.n_rb == 0 || h >= p.nH) return;
-    const int row = b * p.nH + h, rb = row / prefix::RB;
-    rloc = row % prefix::RB;
-    const long tot = (long)p.n_rb * p.n_kt, f = (long)rb * p.n_kt;
-    const long a = prefix::owner_of(f, tot, p.grid_p), e = prefix::owner_of(f + p.n_kt - 1, tot, p.grid_p);
-    slot0 = a + rb;
-    cnt = (int)(e - a + 1);
-    if (!TA_IDX_OK(p.err, slot0, cnt, (long)p.grid_p + p.n_rb)) cnt = 0;
-  };
+  // The prefix's partials of head h (rows of a sequence may lie in two row blocks): first slot, number, row in the block.
+  __shared__ int ps0_s[32], pc_s[32];
+  if (warp == 0) {
+    int slot0 = 0, cnt = 0;
+    if (p.n_rb > 0 && lane < p.nH) {
+      const int rb = (b * p.nH + lane) / prefix::RB;
+      const long tot = (long)p.n_rb * p.n_kt, f = (long)rb * p.n_kt;
+      const int first = (int)prefix::owner_of(f, tot, p.grid_p), last = (int)prefix::owner_of(f + p.n_kt - 1, tot, p.grid_p);
+      slot0 = first + rb;
+      cnt = last - first + 1;
+      if (!TA_IDX_OK(p.err, slot0, cnt, (long)p.grid_p + p.n_rb)) cnt = 0;
+    }
+    ps0_s[lane] = slot0;
+    pc_s[lane] = cnt;
+  }
+  __syncthreads();
   // Up to here only inputs of the call were read; the partials come from the kernels before this one.
   pdl_enter();
   const int i0 = p.seq_cta[2 * b];
@@ -94,10 +98,8 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
   if (!TA_IDX_OK(p.err, i0 + b, np, (long)p.grid + p.B)) np = 0;
   // ---- weights: warp w takes the partials w, w + WARPS, ... of all heads (lane = head) ----
   {
-    const int h = lane;
-    long ps0;
-    int pc, prl;
-    pre_range(h, ps0, pc, prl);
+    const int h = lane, pc = pc_s[h], prl = (b * p.nH + h) % prefix::RB;
+    const long ps0 = ps0_s[h];
     const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + (long)(i0 + b) * 32 + h;
     const float2* pml = reinterpret_cast<const float2*>(p.pre_ml) + ps0 * prefix::RB + prl;
     float m = -INFINITY;
@@ -137,9 +139,8 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
     const int g = tid / items, it = tid % items, h = it % p.nH, c = c0 + it / p.nH * 4;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (g < groups) {
-      long ps0;
-      int pc, prl;
-      pre_range(h, ps0, pc, prl);
+      const int pc = pc_s[h], prl = (b * p.nH + h) % prefix::RB;
+      const long ps0 = ps0_s[h];
       const float* po = p.part_o + (long)(i0 + b) * 32 * t3 + ((long)(c / 4) * 32 + h) * 4;
       const float* pp = p.pre_o + ps0 * prefix::RB * t3 + ((long)(c / 4) * prefix::RB + prl) * 4;
       auto add = [&](const float* src, long stride, int n, int w0) {

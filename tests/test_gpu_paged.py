@@ -111,6 +111,12 @@ def test_prefix_shapes(dtype, shape, append, page):
     check_step(st, append=append, what=f"prefix {shape}")
 
 
+@pytest.mark.parametrize("dtype,shape", STEP_SHAPES)
+def test_prefix_without_rope(dtype, shape):
+    st = P.PagedState(workload(shape, dtype, rope=False), [3, 0, 90, 17], 64, P=520)
+    check_step(st, what=f"prefix, no rope {shape}")
+
+
 @pytest.mark.parametrize("B,n_H", [(1, 1), (1, 32), (2, 2), (9, 8), (40, 16), (130, 4)])
 def test_prefix_batches(B, n_H):
     shape = dict(TC64, n_H=n_H, r=(min(4, n_H), 64, 64), t=(min(4, n_H), 64, 64))
