@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -88,19 +89,19 @@ def load_library() -> ctypes.CDLL:
     lib.tucker_attn_decode.argtypes = [dp] + [vp] * 11 + [i32, vp, i32, vp, vp, sz, vp]
     lib.tucker_attn_decode_static.restype = ctypes.c_int
     lib.tucker_attn_decode_static.argtypes = [dp] + [vp] * 11 + [i32, vp, i32, vp, vp]
-    pp = ctypes.POINTER(TuckerPagedCache)
+    # descriptor and cache by address: packed bytes or a structure by reference
     lib.tucker_cache_append_paged.restype = ctypes.c_int
-    lib.tucker_cache_append_paged.argtypes = [dp] + [vp] * 3 + [pp, vp, vp, i32, vp, sz, vp]
+    lib.tucker_cache_append_paged.argtypes = [vp] + [vp] * 3 + [vp, vp, vp, i32, vp, sz, vp]
     lib.tucker_cache_append_paged_workspace_bytes.restype = sz
-    lib.tucker_cache_append_paged_workspace_bytes.argtypes = [dp, pp, i32]
+    lib.tucker_cache_append_paged_workspace_bytes.argtypes = [vp, vp, i32]
     lib.tucker_attn_decode_paged_workspace_bytes.restype = sz
-    lib.tucker_attn_decode_paged_workspace_bytes.argtypes = [dp, pp]
+    lib.tucker_attn_decode_paged_workspace_bytes.argtypes = [vp, vp]
     lib.tucker_attn_decode_paged.restype = ctypes.c_int
-    lib.tucker_attn_decode_paged.argtypes = [dp] + [vp] * 9 + [pp, vp, i32, vp, vp, sz, vp]
+    lib.tucker_attn_decode_paged.argtypes = [vp] + [vp] * 9 + [vp, vp, i32, vp, vp, sz, vp]
     lib.tucker_attn_decode_prefix_workspace_bytes.restype = sz
-    lib.tucker_attn_decode_prefix_workspace_bytes.argtypes = [dp, pp, i32]
+    lib.tucker_attn_decode_prefix_workspace_bytes.argtypes = [vp, vp, i32]
     lib.tucker_attn_decode_prefix.restype = ctypes.c_int
-    lib.tucker_attn_decode_prefix.argtypes = [dp] + [vp] * 9 + [pp, vp, vp, i32, i32, vp, vp, sz, vp]
+    lib.tucker_attn_decode_prefix.argtypes = [vp] + [vp] * 9 + [vp, vp, vp, i32, i32, vp, vp, sz, vp]
     lib.tucker_attn_status_string.restype = ctypes.c_char_p
     lib.tucker_attn_status_string.argtypes = [ctypes.c_int]
     lib.tucker_attn_last_device_error.restype = ctypes.c_int
@@ -346,27 +347,15 @@ def tucker_attn_decode_static(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kcache, Vcach
     return out
 
 
+# The serving calls are short and are made once per layer and token, so their host time counts: the structures are packed in one
+# call, and the usual outcome of the argument checks is decided in one expression (the checks one by one name the culprit).
+_DESC_PACK = struct.Struct("=12ififii").pack
+_CACHE_PACK = struct.Struct("=QQQiii4x").pack
+
+
 def _check_all(items, dtype, device):
-    """_check of every (tensor, name, shape), with the usual outcome decided in one pass."""
-    idx = device.index
     for t, name, shape in items:
-        if not (t.dtype is dtype and t.shape == shape and t.get_device() == idx and t.is_contiguous()):
-            _check(t, name, shape, dtype, device)
-
-
-def _paged_items(Kpages, Vpages, block_table, cache_len, B, r3, t3):
-    """What _check_all checks of a paged cache: (items of the storage type, int32 items)."""
-    if Kpages.dim() != 3 or block_table.dim() != 2:
-        raise ValueError("Kpages must be [n_pages, page_size, r3] and block_table [B, max_pages]")
-    n_pages, page_size, _ = Kpages.shape
-    return (((Kpages, "Kpages", (n_pages, page_size, r3)), (Vpages, "Vpages", (n_pages, page_size, t3))),
-            ((block_table, "block_table", (B, block_table.shape[1])), (cache_len, "cache_len", (B,))))
-
-
-def _paged_struct(Kpages, Vpages, block_table):
-    n_pages, page_size, _ = Kpages.shape
-    return TuckerPagedCache(Kpages.data_ptr(), Vpages.data_ptr(), block_table.data_ptr(), n_pages, page_size,
-                            block_table.shape[1])
+        _check(t, name, shape, dtype, device)
 
 
 def tucker_cache_append_paged(X, U3, Ut3, Kpages, Vpages, block_table, cache_len, tok_start, *, rope: bool,
@@ -377,25 +366,38 @@ def tucker_cache_append_paged(X, U3, Ut3, Kpages, Vpages, block_table, cache_len
     block_table [B, max_pages], cache_len [B] and tok_start [B + 1] int32 on the device."""
     torch = _torch()
     lib = load_library()
-    if X.dim() != 2 or cache_len.dim() != 1 or U3.dim() != 2 or Ut3.dim() != 2:
-        raise ValueError("X must be [T, d_model], cache_len [B], U3 and Ut3 [d_model, rank]")
+    if X.dim() != 2 or cache_len.dim() != 1 or U3.dim() != 2 or Ut3.dim() != 2 or Kpages.dim() != 3 or block_table.dim() != 2:
+        raise ValueError("X must be [T, d_model], U3 and Ut3 [d_model, rank], Kpages [n_pages, page_size, r3], "
+                         "block_table [B, max_pages] and cache_len [B]")
     T, d = X.shape
-    B = cache_len.shape[0]
-    dev, dt = X.device, X.dtype
-    code = _dtype_code(X)
     r3, t3 = U3.shape[1], Ut3.shape[1]
-    data, ints = _paged_items(Kpages, Vpages, block_table, cache_len, B, r3, t3)
-    _check_all(((X, "X", (T, d)), (U3, "U3", (d, r3)), (Ut3, "Ut3", (d, t3))) + data, dt, dev)
-    _check_all(ints + ((tok_start, "tok_start", (B + 1,)),), torch.int32, dev)
-    cache = _paged_struct(Kpages, Vpages, block_table)
-    desc = TuckerAttnDesc(B, 1, d, 1, 1, 1, r3, 1, 1, t3, 1, int(bool(rope)), float(rope_base), int(pos0), 0.0, code, int(flags))
-    pd, pc = ctypes.byref(desc), ctypes.byref(cache)
+    n_pages, page_size, _ = Kpages.shape
+    B, max_pages = block_table.shape
+    dt, dev = X.dtype, X.device
+    i32, idx = torch.int32, dev.index
+    code = _dtype_code(X)
+    if not (X.is_cuda and dt is U3.dtype is Ut3.dtype is Kpages.dtype is Vpages.dtype
+            and i32 is block_table.dtype is cache_len.dtype is tok_start.dtype
+            and idx == U3.get_device() == Ut3.get_device() == Kpages.get_device() == Vpages.get_device()
+            == block_table.get_device() == cache_len.get_device() == tok_start.get_device()
+            and U3.shape == (d, r3) and Ut3.shape == (d, t3) and Kpages.shape == (n_pages, page_size, r3)
+            and Vpages.shape == (n_pages, page_size, t3) and cache_len.shape == (B,) and tok_start.shape == (B + 1,)
+            and X.is_contiguous() and U3.is_contiguous() and Ut3.is_contiguous() and Kpages.is_contiguous()
+            and Vpages.is_contiguous() and block_table.is_contiguous() and cache_len.is_contiguous()
+            and tok_start.is_contiguous()):
+        B = cache_len.shape[0]
+        _check_all(((X, "X", (T, d)), (U3, "U3", (d, r3)), (Ut3, "Ut3", (d, t3)), (Kpages, "Kpages", (n_pages, page_size, r3)),
+                    (Vpages, "Vpages", (n_pages, page_size, t3))), dt, dev)
+        _check_all(((block_table, "block_table", (B, max_pages)), (cache_len, "cache_len", (B,)),
+                    (tok_start, "tok_start", (B + 1,))), i32, dev)
+    desc = _DESC_PACK(B, 1, d, 1, 1, 1, r3, 1, 1, t3, 1, bool(rope), rope_base, pos0, 0.0, code, flags)
+    cache = _CACHE_PACK(Kpages.data_ptr(), Vpages.data_ptr(), block_table.data_ptr(), n_pages, page_size, max_pages)
     if workspace is None:
-        workspace = alloc_workspace(lib.tucker_cache_append_paged_workspace_bytes(pd, pc, T), dev)
+        workspace = alloc_workspace(lib.tucker_cache_append_paged_workspace_bytes(desc, cache, T), dev)
     else:
         _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
     with _on_device(dev):
-        rc = lib.tucker_cache_append_paged(pd, X.data_ptr(), U3.data_ptr(), Ut3.data_ptr(), pc, cache_len.data_ptr(),
+        rc = lib.tucker_cache_append_paged(desc, X.data_ptr(), U3.data_ptr(), Ut3.data_ptr(), cache, cache_len.data_ptr(),
                                            tok_start.data_ptr(), T, workspace.data_ptr(), workspace.numel(), _stream_ptr(dev))
     if rc != TA_OK:
         raise TuckerAttnError(rc, "tucker_cache_append_paged")
@@ -409,42 +411,57 @@ def tucker_attn_decode_prefix(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kpages, Vpage
     prefix_table int32 [>= ceil(prefix_len / page_size)] on the device (None when prefix_len is 0).  Returns y [B, d]."""
     torch = _torch()
     lib = load_library()
-    if x.dim() != 2:
-        raise ValueError("x must be [B, d_model]")
-    if C.dim() != 3 or Ct.dim() != 3:
-        raise ValueError("cores must be 3-way tensors")
+    if x.dim() != 2 or C.dim() != 3 or Ct.dim() != 3 or Kpages.dim() != 3 or block_table.dim() != 2:
+        raise ValueError("x must be [B, d_model], the cores 3-way tensors, Kpages [n_pages, page_size, r3] and block_table "
+                         "[B, max_pages]")
     B, d = x.shape
-    dev, dt = x.device, x.dtype
+    r1, r2, r3 = C.shape
+    t1, t2, t3 = Ct.shape
+    n_pages, page_size, _ = Kpages.shape
+    max_pages = block_table.shape[1]
+    dt, dev = x.dtype, x.device
+    i32, idx = torch.int32, dev.index
     code = _dtype_code(x)
-    (r1, r2, r3), (t1, t2, t3) = C.shape, Ct.shape
-    data, ints = _paged_items(Kpages, Vpages, block_table, cache_len, B, r3, t3)
     if out is None:
         out = torch.empty_like(x)
-    _check_all(((x, "x", (B, d)), (C, "C", (r1, r2, r3)), (U1, "U1", (n_H, r1)), (U2, "U2", (d, r2)), (U3, "U3", (d, r3)),
-                (Ct, "Ct", (t1, t2, t3)), (Ut1, "Ut1", (n_H, t1)), (Ut2, "Ut2", (d, t2)), (Ut3, "Ut3", (d, t3)),
-                (out, "out", (B, d))) + data, dt, dev)
+    if not (x.is_cuda and dt is C.dtype is U1.dtype is U2.dtype is U3.dtype is Ct.dtype is Ut1.dtype is Ut2.dtype is Ut3.dtype
+            is Kpages.dtype is Vpages.dtype is out.dtype and i32 is block_table.dtype is cache_len.dtype
+            and idx == C.get_device() == U1.get_device() == U2.get_device() == U3.get_device() == Ct.get_device()
+            == Ut1.get_device() == Ut2.get_device() == Ut3.get_device() == Kpages.get_device() == Vpages.get_device()
+            == out.get_device() == block_table.get_device() == cache_len.get_device()
+            and U1.shape == (n_H, r1) and U2.shape == (d, r2) and U3.shape == (d, r3) and Ut1.shape == (n_H, t1)
+            and Ut2.shape == (d, t2) and Ut3.shape == (d, t3) and Kpages.shape == (n_pages, page_size, r3)
+            and Vpages.shape == (n_pages, page_size, t3) and out.shape == (B, d) and block_table.shape == (B, max_pages)
+            and cache_len.shape == (B,)
+            and x.is_contiguous() and C.is_contiguous() and U1.is_contiguous() and U2.is_contiguous() and U3.is_contiguous()
+            and Ct.is_contiguous() and Ut1.is_contiguous() and Ut2.is_contiguous() and Ut3.is_contiguous()
+            and Kpages.is_contiguous() and Vpages.is_contiguous() and out.is_contiguous() and block_table.is_contiguous()
+            and cache_len.is_contiguous()):
+        _check_all(((x, "x", (B, d)), (C, "C", (r1, r2, r3)), (U1, "U1", (n_H, r1)), (U2, "U2", (d, r2)), (U3, "U3", (d, r3)),
+                    (Ct, "Ct", (t1, t2, t3)), (Ut1, "Ut1", (n_H, t1)), (Ut2, "Ut2", (d, t2)), (Ut3, "Ut3", (d, t3)),
+                    (Kpages, "Kpages", (n_pages, page_size, r3)), (Vpages, "Vpages", (n_pages, page_size, t3)),
+                    (out, "out", (B, d))), dt, dev)
+        _check_all(((block_table, "block_table", (B, max_pages)), (cache_len, "cache_len", (B,))), i32, dev)
     prefix_len = int(prefix_len)
     if prefix_len < 0:
         raise ValueError("prefix_len must not be negative")
+    prefix_ptr = None
     if prefix_len > 0:
-        if prefix_table is None or prefix_table.dim() != 1 or prefix_table.shape[0] * Kpages.shape[1] < prefix_len:
+        if prefix_table is None or prefix_table.dim() != 1 or prefix_table.shape[0] * page_size < prefix_len:
             raise ValueError("prefix_table must hold the ceil(prefix_len / page_size) pages of the prefix")
-        ints += ((prefix_table, "prefix_table", prefix_table.shape),)
-    _check_all(ints, torch.int32, dev)
-    cache = _paged_struct(Kpages, Vpages, block_table)
-    desc = TuckerAttnDesc(B, 1, d, int(n_H), r1, r2, r3, t1, t2, t3, 1, int(bool(rope)), float(rope_base), 0, float(scale), code,
-                          int(flags))
-    pd, pc = ctypes.byref(desc), ctypes.byref(cache)
+        _check(prefix_table, "prefix_table", prefix_table.shape, i32, dev)
+        prefix_ptr = prefix_table.data_ptr()
+    desc = _DESC_PACK(B, 1, d, n_H, r1, r2, r3, t1, t2, t3, 1, bool(rope), rope_base, 0, scale, code, flags)
+    cache = _CACHE_PACK(Kpages.data_ptr(), Vpages.data_ptr(), block_table.data_ptr(), n_pages, page_size, max_pages)
     if workspace is None:
-        workspace = alloc_workspace(lib.tucker_attn_decode_prefix_workspace_bytes(pd, pc, prefix_len), dev)
+        workspace = alloc_workspace(lib.tucker_attn_decode_prefix_workspace_bytes(desc, cache, prefix_len), dev)
     else:
         _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
     with _on_device(dev):
-        rc = lib.tucker_attn_decode_prefix(pd, x.data_ptr(), C.data_ptr(), U1.data_ptr(), U2.data_ptr(), U3.data_ptr(),
-                                           Ct.data_ptr(), Ut1.data_ptr(), Ut2.data_ptr(), Ut3.data_ptr(), pc,
-                                           cache_len.data_ptr(), prefix_table.data_ptr() if prefix_len else None, prefix_len,
-                                           int(bool(append)), out.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                                           _stream_ptr(dev))
+        rc = lib.tucker_attn_decode_prefix(desc, x.data_ptr(), C.data_ptr(), U1.data_ptr(), U2.data_ptr(), U3.data_ptr(),
+                                           Ct.data_ptr(), Ut1.data_ptr(), Ut2.data_ptr(), Ut3.data_ptr(), cache,
+                                           cache_len.data_ptr(), prefix_ptr, prefix_len, bool(append), out.data_ptr(),
+                                           workspace.data_ptr(), workspace.numel(), _stream_ptr(dev))
     if rc != TA_OK:
         raise TuckerAttnError(rc, "tucker_attn_decode_prefix")
     return out

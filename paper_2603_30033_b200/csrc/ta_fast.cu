@@ -24,13 +24,17 @@
 
 namespace ta {
 
-// theta_i = base^(-2 i / r3) in double precision, i < r3 / 2; the first 128 (all of them on the tensor-core path)
+// theta_i = base^(-2 i / r3) in double precision, i < r3 / 2; the first 128 (all of them on the tensor-core path).
+// The last table of each thread is kept (a table depends on the base and the rank only; 64 pow() take 0.7 us of every call).
 dec::RopeFreqs rope_freqs(const tucker_attn_desc& d) {
-  dec::RopeFreqs f;
-  const int half = d.r3 / 2;
-  for (int i = 0; i < 128; ++i)
-    f.theta[i] = (d.rope && i < half) ? pow((double)d.rope_base, -2.0 * (double)i / (double)d.r3) : 0.0;
-  return f;
+  static thread_local struct { int r3 = 0; float base = 0.f; dec::RopeFreqs f; } last;
+  if (!d.rope) return dec::RopeFreqs{};
+  if (last.r3 != d.r3 || last.base != d.rope_base) {
+    const int half = d.r3 / 2;
+    for (int i = 0; i < 128; ++i) last.f.theta[i] = i < half ? pow((double)d.rope_base, -2.0 * (double)i / (double)d.r3) : 0.0;
+    last.r3 = d.r3; last.base = d.rope_base;
+  }
+  return last.f;
 }
 
 namespace {
