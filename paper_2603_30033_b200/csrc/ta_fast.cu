@@ -700,6 +700,12 @@ int launch_prefix(Problem& p, const FastDecWs& w, const PrefixPlan& q) {
   }
 }
 
+// Whether the join goes on to y: the output factor is then read once per sequence instead of once per 128 sequences, and a launch
+// (2 us of host time and a kernel boundary) is saved.  Whole step on the GPU, in the join against as a GEMM: d 768, t2 64: 22.1
+// against 23.0 us with one sequence, 25.7 against 27.5 with six behind a prefix; t2 96, 24 sequences (3.5 MB): 39.8 against 42.2;
+// d 4096, t2 128: 27.6 against 27.1 with 4 sequences (4 MB), 28.2 against 28.3 with 8, 32.9 against 30.3 with 16.
+bool paged_out_fuses_y(const tucker_attn_desc& d) { return (size_t)d.B * d.d_model * d.t2 * sizeof(bf16) <= (size_t)4 << 20; }
+
 template <int CL>
 int launch_paged_out_cl(Problem& p, const pgout::Params& op) {
   static PerDeviceFlag attr;
@@ -717,6 +723,7 @@ int launch_paged_out(Problem& p, const FastDecWs& w, const PrefixPlan& q, int gr
   op.seq_cta = w.seq_cta; op.part_o = w.part_o; op.part_ml = w.part_ml; op.grid = grid;
   op.pre_o = w.pre_o; op.pre_ml = w.pre_ml; op.grid_p = q.grid; op.n_kt = q.n_kt; op.n_rb = q.n_rb;
   op.Ct = (const bf16*)p.Ct; op.Ut1 = (const bf16*)p.Ut1; op.z = w.z; op.err = p.dev_err;
+  op.Ut2 = paged_out_fuses_y(d) ? (const bf16*)p.Ut2 : nullptr; op.y = (bf16*)p.Y; op.d = d.d_model;
   // measured at 64 sequences of 32 heads, two to three partials each: 20.6 us with 8 CTAs per sequence (two waves), 13.8 us with 4
   if (d.B * 8 <= 2 * sm_count()) return launch_paged_out_cl<8>(p, op);
   if (d.B * 4 <= 2 * sm_count()) return launch_paged_out_cl<4>(p, op);
@@ -833,7 +840,7 @@ int fast_decode(Problem& p) {
     }
   }
   // ---- 5: y = z Ut2^T ----
-  {
+  if (!(p.paged && paged_out_fuses_y(d))) {
     umma_gemm::Params gp = {};
     gp.n_pos = d.B;
     gp.nseg = 1;

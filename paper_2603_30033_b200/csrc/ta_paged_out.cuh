@@ -3,7 +3,9 @@
 //   o_h = merged, normalised output of head h;  u[a, :] = sum_h Ut1[h, a] o_h;  z[j] = sum_a sum_c Ct[a, j, c] u[a, c]
 // A cluster of CL CTAs per sequence (8, 4 or 2: the most that still lets all of them run at once, two CTAs per SM).  CTA y merges t3 / CL value columns of all heads (every partial is read once per
 // sequence, where CTAs that split the rows of z would each have to merge everything), forms its columns of u, hands them to the
-// other CTAs through distributed shared memory, and computes t2 / CL rows of z.  One user with a long cache has a partial
+// other CTAs through distributed shared memory, and computes t2 / CL rows of z.  For small batches (paged_out_fuses_y) it
+// goes on to y = z Ut2^T: z is handed round the cluster and every CTA computes d / CL outputs, each sequence reading the factor
+// again, which a launch and its boundary outweigh as long as there are few.  One user with a long cache has a partial
 // from every SM: the maxima, weights and sums of the partials are spread over all warps instead of walked by one.
 // The kernels before it fill their SMs, so that next to nothing of this one overlaps them: it takes the CTAs that hold a sequence
 // from the streaming kernel instead of scanning the lengths.
@@ -28,6 +30,9 @@ struct Params {
   int grid_p, n_kt, n_rb;                        // n_rb = 0: no prefix
   const bf16 *Ct, *Ut1;
   bf16* z;                                       // [B, 2 z_half]: rounded values, rounded rests
+  const bf16* Ut2;                               // not null: y = z Ut2^T here, z stays on chip
+  bf16* y;                                       // [B, d]
+  int d;
   unsigned int* err;
 };
 
@@ -55,6 +60,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
   float* ut1_s = u_s + p.t1 * t3;                          // [nH][t1]
   float2* w_s = reinterpret_cast<float2*>(ut1_s + (p.nH * p.t1 + 1) / 2 * 2);      // [partials][32]: (max, sum), then (weight, -)
   __shared__ float hm_s[WARPS][32], hl_s[WARPS][32];
+  __shared__ float z_s[256];
   const int b = blockIdx.x / CL, y = blockIdx.x % CL, c0 = y * cw;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const int jn = p.t2 / CL, jbeg = y * jn;
@@ -238,12 +244,54 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
       const int j = jbeg + jl + r * WARPS;
 #pragma unroll
       for (int off = 16; off >= 1; off >>= 1) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], off);
-      if (lane == 0 && jl + r * WARPS < jn && TA_IDX_OK(p.err, (long)b * 2 * p.z_half + p.z_half + j, 1, (long)p.B * 2 * p.z_half)) {
+      if (p.Ut2) {
+        if (lane < CL && jl + r * WARPS < jn) st_cluster(&z_s[j], (uint32_t)lane, acc[r]);
+      } else if (lane == 0 && jl + r * WARPS < jn && TA_IDX_OK(p.err, (long)b * 2 * p.z_half + p.z_half + j, 1, (long)p.B * 2 * p.z_half)) {
         const bf16 zh = __float2bfloat16_rn(acc[r]);
         p.z[(long)b * 2 * p.z_half + j] = zh;
         p.z[(long)b * 2 * p.z_half + p.z_half + j] = __float2bfloat16_rn(acc[r] - __bfloat162float(zh));
       }
     }
+  }
+  if (p.Ut2) {
+    // ---- y: lane = (row of rpw, 16-byte chunk of the factor's row); a lane's eight values of z stay in registers ----
+    __syncthreads();
+    cluster_arrive();
+    cluster_wait();
+    const int nc = p.t2 / 8, rpw = 32 / nc, sub = lane / nc, cz = lane % nc;
+    const bool on = sub < rpw;
+    float zr[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) zr[e] = z_s[cz * 8 + e];
+    const uint4* F = reinterpret_cast<const uint4*>(p.Ut2);
+    const int rows = p.d / CL, end = (y + 1) * rows;
+    constexpr int YU = 4;                  // row groups in flight per warp
+    for (int j0 = y * rows + warp * rpw * YU; j0 < end; j0 += WARPS * rpw * YU) {
+      uint4 v[YU];
+#pragma unroll
+      for (int k = 0; k < YU; ++k) {
+        const int j = j0 + k * rpw + sub;
+        v[k] = (on && j < end) ? F[(long)j * nc + cz] : make_uint4(0u, 0u, 0u, 0u);
+      }
+#pragma unroll
+      for (int k = 0; k < YU; ++k) {
+        const int j = j0 + k * rpw + sub;
+        const uint32_t wv[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+        float t = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[e]));
+          t = fmaf(zr[2 * e], f.x, t);
+          t = fmaf(zr[2 * e + 1], f.y, t);
+        }
+        for (int off = 1; off < nc; off <<= 1) {           // sum over the nc lanes of the row
+          const float o = __shfl_down_sync(0xffffffffu, t, off);
+          if (cz + off < nc) t += o;
+        }
+        if (on && cz == 0 && j < end && TA_IDX_OK(p.err, (long)b * p.d + j, 1, (long)p.B * p.d)) p.y[(long)b * p.d + j] = __float2bfloat16_rn(t);
+      }
+    }
+    return;
   }
   if (y == 0)
     for (int j = p.t2 + tid; j < p.z_half; j += THREADS)
