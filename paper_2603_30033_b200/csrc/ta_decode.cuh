@@ -133,7 +133,7 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
   __shared__ float2 cs_s[DQ_CW / 2];                // (cos, sin) at position L for this CTA's pairs
   __shared__ float u1_s[32 * DQ_MAX_R1];            // U1 as fp32
   __shared__ float w_s[DQ_MAX_R1][DQ_CW];
-  __shared__ float red_s[8][AB][DQ_CW];
+  __shared__ float red_s[2][8][AB][DQ_CW];          // by batch parity
   const int b = blockIdx.x, c0 = blockIdx.y * DQ_CW;
   const int ncol = r2 + r3 + t3;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -186,20 +186,23 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
   // the split-K partials are [splits][rows padded to 128][ncol]: this sequence's row must lie in every split
   const bool prow_ok = TA_IDX_OK(err, (long)b * ncol, ncol, split_stride) &&
                        TA_IDX_OK(err, (long)(splits - 1) * split_stride + (long)b * ncol, ncol, (long)splits * split_stride);
-  for (int c = threadIdx.x; c < r2 + DQ_CW; c += blockDim.x) {
-    const int col = c < r2 ? c : r2 + c0 + (c - r2);
+  // (one pass over all of them: the loads of a thread's column are in flight together, and so are the columns)
+  const int ny = (int)gridDim.y, vblocks = max(0, (t3 / DQ_CW - (int)blockIdx.y + ny - 1) / ny);
+  for (int c = threadIdx.x; c < r2 + DQ_CW + vblocks * DQ_CW; c += blockDim.x) {
+    const int e = c - r2 - DQ_CW;                      // >= 0: value coordinate vc
+    const int vc = (e / DQ_CW * ny + (int)blockIdx.y) * DQ_CW + e % DQ_CW;
+    const int col = c < r2 ? c : (e < 0 ? r2 + c0 + (c - r2) : r2 + r3 + vc);
     const float acc = prow_ok ? split_sum(prow + col, splits, split_stride) : 0.f;
-    if (c < r2) qt_s[c] = acc; else k_s[c - r2] = acc;
-  }
-  for (int c = threadIdx.x; c < t3; c += blockDim.x) {
-    if ((c / DQ_CW) % gridDim.y != blockIdx.y) continue;
-    const float acc = prow_ok ? split_sum(prow + r2 + r3 + c, splits, split_stride) : 0.f;
-    const bf16 vv = __float2bfloat16_rn(acc);
-    if (TA_IDX_OK(err, (long)b * t3 + c, 1, (long)nB * t3)) vnew[(long)b * t3 + c] = vv;
-    // shared_kv == 1 (one cache, no RoPE): the key row written below is the value row; == 2 (one cache with
-    // latent RoPE): the cache holds un-rotated rows, i.e. this value row, and the rotated key is not stored
-    if (append && shared_kv != 1 && TA_IDX_OK(err, new_row * t3 + c, 1, n_rows * t3))
-      Vc[new_row * t3 + c] = vv;   // shared cache: the key row written below is the value row
+    if (c < r2) qt_s[c] = acc;
+    else if (e < 0) k_s[c - r2] = acc;
+    else {
+      const bf16 vv = __float2bfloat16_rn(acc);
+      if (TA_IDX_OK(err, (long)b * t3 + vc, 1, (long)nB * t3)) vnew[(long)b * t3 + vc] = vv;
+      // shared_kv == 1 (one cache, no RoPE): the key row written below is the value row; == 2 (one cache with
+      // latent RoPE): the cache holds un-rotated rows, i.e. this value row, and the rotated key is not stored
+      if (append && shared_kv != 1 && TA_IDX_OK(err, new_row * t3 + vc, 1, n_rows * t3))
+        Vc[new_row * t3 + vc] = vv;   // shared cache: the key row written below is the value row
+    }
   }
   __syncthreads();
   if (threadIdx.x < DQ_CW / 2) {                    // new key, rotated
@@ -252,7 +255,7 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
 #pragma unroll
       for (int i = 0; i < NV / 8; ++i) {
         const int idx = first + i;
-        red_s[warp][idx / 8][ch * 8 + idx % 8] = v[i];
+        red_s[(a0 / AB) & 1][warp][idx / 8][ch * 8 + idx % 8] = v[i];
       }
     }
     __syncthreads();
@@ -261,12 +264,12 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
       if (a0 + j < r1) {
         float t = 0.f;
 #pragma unroll
-        for (int w8 = 0; w8 < 8; ++w8) t += red_s[w8][j][c];
+        for (int w8 = 0; w8 < 8; ++w8) t += red_s[(a0 / AB) & 1][w8][j][c];
         w_s[a0 + j][c] = t;
       }
     }
-    __syncthreads();
   }
+  __syncthreads();
   // ---- qhat_h for this CTA's coordinates ----
   for (int item = threadIdx.x; item < nH * (DQ_CW / 2); item += blockDim.x) {
     const int h = item / (DQ_CW / 2), cp = item % (DQ_CW / 2);
