@@ -82,6 +82,15 @@ def test_decode_paged_shapes(dtype, shape, rope, append):
     check_step(st, append=append, what=f"{shape}")
 
 
+@pytest.mark.parametrize("dtype,shape", [("fp32", dict(d_model=96, n_H=24, r=(24, 16, 8), t=(24, 40, 500))),
+                                         ("bf16", dict(d_model=128, n_H=32, r=(32, 160, 64), t=(32, 224, 128))),
+                                         ("bf16", dict(d_model=256, n_H=2, r=(2, 256, 128), t=(2, 256, 128)))])
+def test_large_core_ranks(dtype, shape):
+    """Head and output ranks at the limits of the shared-memory tables (and, fp32, past them)."""
+    for pre in (0, 70):
+        check_step(P.PagedState(workload(shape, dtype), [20, 0, 150], 16, P=pre), what=f"{shape}")
+
+
 @pytest.mark.parametrize("B,n", [(1, 0), (1, 1), (1, 2500), (200, 3), (3, 1023)])
 def test_decode_paged_batches(B, n):
     st = P.PagedState(workload(TC64, "bf16"), [max(0, n - 7 * (b % 5)) for b in range(B)], 16)
