@@ -384,8 +384,8 @@ TA_API int tucker_attn_bounds_checked(void);
 TA_API int tucker_attn_selftest_wait_timeout(int32_t budget_us, int32_t* out, void* cuda_stream);
 
 /* Which path the last tucker_attn_fwd / tucker_attn_decode call on this thread took:
- * 0 = none yet, 1 = generic FMA kernels, 2 = tensor-core kernels.  Number of kernels that
- * call launched. */
+ * 0 = none yet, 1 = generic FMA kernels, 2 = tensor-core kernels, 3 = the paged step's one-launch
+ * form for small batches of short contexts.  Number of kernels that call launched. */
 TA_API int tucker_attn_last_path(void);
 TA_API int tucker_attn_last_launch_count(void);
 

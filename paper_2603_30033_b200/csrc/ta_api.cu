@@ -214,8 +214,9 @@ int tucker_attn_decode_prefix(const tucker_attn_desc* desc, const void* x, const
   p.prof_start = tl_prof_start; p.prof_stop = tl_prof_stop;
   if (!p.dev_err) return TA_ERR_CUDA;
   const bool fast = fast_paged_supported(*desc, cache->page_size);
-  const int rc = fast ? fast_decode(p) : generic_paged_decode(p);
-  tl_last_path = fast ? 2 : 1;
+  const bool small = cluster_step_supported(*desc, p.shared_kv) && cluster_step_pays(*desc, p.Lmax, prefix_len, fast);
+  const int rc = small ? cluster_paged_decode(p) : (fast ? fast_decode(p) : generic_paged_decode(p));
+  tl_last_path = small ? 3 : (fast ? 2 : 1);
   tl_last_launches = p.launches;
   return rc;
 }

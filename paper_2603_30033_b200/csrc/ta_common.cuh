@@ -117,6 +117,11 @@ size_t generic_paged_decode_workspace(const tucker_attn_desc& d, int64_t Lmax, i
 int generic_paged_decode(Problem& p);
 int generic_paged_append(Problem& p, const int32_t* tok_start, int32_t T);
 
+// Paged decode step of few sequences with short contexts in one launch, both types (ta_paged_cluster.cu); needs no workspace.
+bool cluster_step_supported(const tucker_attn_desc& d, bool one_pool);
+bool cluster_step_pays(const tucker_attn_desc& d, int64_t slots, int32_t prefix_len, bool tensor_cores);
+int cluster_paged_decode(Problem& p);
+
 // HOSVD initialiser (ta_hosvd.cu)
 size_t hosvd_workspace(int n1, int n2, int n3, int r2, int r3);
 int hosvd_run(Problem& p, int n1, int n2, int n3, int r1, int r2, int r3, const float* T, float* core, float* U1,
@@ -159,6 +164,11 @@ __device__ __forceinline__ float2 rope_cos_sin_theta(int pos, double theta) {
   float sn, co;
   sincospif((float)(2.0 * turns), &sn, &co);
   return make_float2(co, sn);
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 }  // namespace dec
 #endif

@@ -39,11 +39,6 @@ __device__ __forceinline__ int tiles_of(int L) { return L / TK + 1; }   // keys 
 // First global tile of CTA i when `total` tiles are split over `grid` CTAs.
 __device__ __forceinline__ long cta_first_tile(long i, long total, long grid) { return i * total / grid; }
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 
 // Block-wide scan over the tile counts of all sequences.  Thread t owns the sequences
 // [lo, hi) = [t * chunk, (t + 1) * chunk); returns the total number of tiles and sets `excl` to the

@@ -13,6 +13,11 @@ def half_step(dtype):
     return U_BF16 if dtype == "bf16" else U_FP32
 
 
+# Slots that a state's table has room for at least.  A step chooses its kernels by what the table can hold, not by lengths it cannot see:
+# with room for 32768 the kernels for long contexts run, with just enough the one-launch form wherever it is built for the shape.
+ROOM = 32768
+
+
 class PagedState:
     """Random paged caches of `lens` own slots per sequence behind a prefix of P slots.  Everything that no call may use
     (unused slots, unowned pages, table entries past a sequence's last page) holds NaN, infinities and bad page numbers."""
@@ -25,7 +30,7 @@ class PagedState:
         need = [-(-(n + m) // page) for n, m in zip(lens, new)]
         pre = -(-P // page)
         self.n_pages = sum(need) + pre + spare
-        self.max_pages = max(max(need), 1) + 1
+        self.max_pages = max(max(max(need), 1) + 1, -(-ROOM // page))
         order = rng.permutation(self.n_pages).astype(np.int32)
         self.table = np.full((B, self.max_pages), -7, np.int32)
         self.table[:, -1] = 1 << 30
