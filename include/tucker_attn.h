@@ -250,7 +250,12 @@ TA_API int tucker_attn_decode_paged(const tucker_attn_desc* desc, const void* x,
  * all B n_H query rows and joined with the own part by the softmax's maxima and sums: the result is that of the paged
  * step on sequences that hold the prefix themselves.  prefix_len = 0 (prefix_table may be NULL) is that step.
  * prefix_len is read on the host; the rest as for tucker_attn_decode_paged.
+ *
+ * Small batches of short contexts (by the sizes of the descriptor and the table, on the current device) run as one launch
+ * that keeps everything on chip.  The queries then return TA_WORKSPACE_NONE, and a call of exactly those sizes may pass NULL
+ * and 0 for the workspace.
  */
+#define TA_WORKSPACE_NONE ((size_t)1)
 TA_API size_t tucker_attn_decode_prefix_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache* cache,
                                                  int32_t prefix_len);
 TA_API int tucker_attn_decode_prefix(const tucker_attn_desc* desc, const void* x,

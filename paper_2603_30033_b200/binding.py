@@ -21,6 +21,7 @@ LIB_PATH = os.path.join(_HERE, "libtucker_attn_checked.so" if os.environ.get("TU
 TA_OK = 0
 TA_DTYPE_F32, TA_DTYPE_BF16 = 0, 1
 TA_FLAG_FORCE_GENERIC = 1
+TA_WORKSPACE_NONE = 1           # a workspace query's answer: the call needs none
 TA_FLAG_FMA_ATTENTION, TA_FLAG_SEPARATE_QUERIES, TA_FLAG_SEPARATE_OUTPUT_GEMMS = 0x200, 0x400, 0x800
 TA_DEVERR_WAIT_TIMEOUT, TA_DEVERR_BAD_CACHE_LEN, TA_DEVERR_BAD_INDEX, TA_DEVERR_BAD_PAGE = 1, 2, 4, 8
 
@@ -453,15 +454,20 @@ def tucker_attn_decode_prefix(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kpages, Vpage
         prefix_ptr = prefix_table.data_ptr()
     desc = _DESC_PACK(B, 1, d, n_H, r1, r2, r3, t1, t2, t3, 1, bool(rope), rope_base, 0, scale, code, flags)
     cache = _CACHE_PACK(Kpages.data_ptr(), Vpages.data_ptr(), block_table.data_ptr(), n_pages, page_size, max_pages)
-    if workspace is None:
-        workspace = alloc_workspace(lib.tucker_attn_decode_prefix_workspace_bytes(desc, cache, prefix_len), dev)
-    else:
-        _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
+    ws_ptr, ws_bytes = None, 0
     with _on_device(dev):
+        if workspace is not None:
+            _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
+            ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel()
+        else:
+            need = lib.tucker_attn_decode_prefix_workspace_bytes(desc, cache, prefix_len)
+            if need != TA_WORKSPACE_NONE:
+                workspace = alloc_workspace(need, dev)
+                ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel()
         rc = lib.tucker_attn_decode_prefix(desc, x.data_ptr(), C.data_ptr(), U1.data_ptr(), U2.data_ptr(), U3.data_ptr(),
                                            Ct.data_ptr(), Ut1.data_ptr(), Ut2.data_ptr(), Ut3.data_ptr(), cache,
                                            cache_len.data_ptr(), prefix_ptr, prefix_len, bool(append), out.data_ptr(),
-                                           workspace.data_ptr(), workspace.numel(), _stream_ptr(dev))
+                                           ws_ptr, ws_bytes, _stream_ptr(dev))
     if rc != TA_OK:
         raise TuckerAttnError(rc, "tucker_attn_decode_prefix")
     return out

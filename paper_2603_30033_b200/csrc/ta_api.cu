@@ -164,8 +164,14 @@ int tucker_attn_decode(const tucker_attn_desc* desc, const void* x, const void* 
   return rc;
 }
 
+// Whether a step runs in its one-launch form, which needs no workspace.
+static bool paged_decode_small(const tucker_attn_desc& d, const tucker_paged_cache& c, int32_t prefix_len) {
+  return paged_batch_ok(d) && cluster_step_supported(d, c.K == c.V) &&
+         cluster_step_pays(d, paged_slots(c), prefix_len, fast_paged_supported(d, c.page_size));
+}
 static size_t paged_decode_need(const tucker_attn_desc& d, const tucker_paged_cache& c, int32_t prefix_len) {
   if (!paged_batch_ok(d)) return 0;
+  if (paged_decode_small(d, c, prefix_len)) return TA_WORKSPACE_NONE;
   if (fast_paged_supported(d, c.page_size)) return fast_paged_workspace(d, prefix_len, c.K == c.V);
   return generic_paged_decode_workspace(d, paged_slots(c), prefix_len);
 }
@@ -187,16 +193,17 @@ int tucker_attn_decode_prefix(const tucker_attn_desc* desc, const void* x, const
                               int32_t prefix_len, int32_t append, void* y, void* workspace, size_t workspace_bytes,
                               void* cuda_stream) {
   if (!desc_ok(desc, true) || !paged_ok(cache, prefix_len)) return TA_ERR_INVALID_ARG;
-  if (!x || !C || !U1 || !U2 || !U3 || !Ct || !Ut1 || !Ut2 || !Ut3 || !y || !workspace) return TA_ERR_INVALID_ARG;
+  if (!x || !C || !U1 || !U2 || !U3 || !Ct || !Ut1 || !Ut2 || !Ut3 || !y) return TA_ERR_INVALID_ARG;
   if (!cache_len || (prefix_len > 0 && !prefix_table)) return TA_ERR_INVALID_ARG;
   if (cache->K == cache->V && !shared_kv_weights(*desc, U3, Ut3)) return TA_ERR_INVALID_ARG;
   const void* ptrs[] = {x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, y, cache->K, cache->V};
   for (const void* q : ptrs)
     if (!aligned16(q)) return TA_ERR_INVALID_ARG;
-  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return TA_ERR_INVALID_ARG;
   const size_t need = paged_decode_need(*desc, *cache, prefix_len);
+  const bool small = need == TA_WORKSPACE_NONE;
+  if (!small && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u))) return TA_ERR_INVALID_ARG;
   if (need == 0) return TA_ERR_UNSUPPORTED_SHAPE;
-  if (workspace_bytes < need) return TA_ERR_WORKSPACE_TOO_SMALL;
+  if (!small && workspace_bytes < need) return TA_ERR_WORKSPACE_TOO_SMALL;
   Problem p = {};
   p.d = *desc;
   p.scale = resolve_scale(*desc);
@@ -214,7 +221,6 @@ int tucker_attn_decode_prefix(const tucker_attn_desc* desc, const void* x, const
   p.prof_start = tl_prof_start; p.prof_stop = tl_prof_stop;
   if (!p.dev_err) return TA_ERR_CUDA;
   const bool fast = fast_paged_supported(*desc, cache->page_size);
-  const bool small = cluster_step_supported(*desc, p.shared_kv) && cluster_step_pays(*desc, p.Lmax, prefix_len, fast);
   const int rc = small ? cluster_paged_decode(p) : (fast ? fast_decode(p) : generic_paged_decode(p));
   tl_last_path = small ? 3 : (fast ? 2 : 1);
   tl_last_launches = p.launches;

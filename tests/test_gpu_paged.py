@@ -337,9 +337,20 @@ def test_binding_refuses():
             Bd.tucker_attn_decode_prefix(x, *dw, o["K"], o["V"], o["table"], o["lens"], o["ptab"], o["n"], **kw)
     with pytest.raises(ValueError):
         Bd.tucker_attn_decode_paged(x, *dw, K, V, table, lens, workspace=torch.empty(1 << 20, dtype=torch.uint8), **kw)
-    with pytest.raises(Bd.TuckerAttnError) as e:
-        Bd.tucker_attn_decode_paged(x, *dw, K, V, table, lens, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"), **kw)
-    assert e.value.status == -3
+    small = dict(workspace=torch.empty(64, dtype=torch.uint8, device="cuda"), **kw)
+    if P.ROOM:
+        with pytest.raises(Bd.TuckerAttnError) as e:
+            Bd.tucker_attn_decode_paged(x, *dw, K, V, table, lens, **small)
+        assert e.value.status == -3
+    else:                                                     # one launch, no workspace: the tensor is not looked at
+        small["workspace"][:] = 7
+        Bd.tucker_attn_decode_paged(x, *dw, K, V, table, lens, **small)
+        assert Bd.last_path() == 3 and small["workspace"].eq(7).all()
+    k0 = K.clone()
+    for bad in (ok(lens=lens.float()), ok(ptab=ptab[None])):
+        with pytest.raises((TypeError, ValueError)):
+            Bd.tucker_attn_decode_prefix(x, *dw, K, V, table, bad["lens"], bad["ptab"], 40, **kw)
+    assert torch.equal(k0.view(torch.int16), K.view(torch.int16))
     X = torch.zeros(3, st.w.d_model, device="cuda", dtype=torch.bfloat16)
     with pytest.raises(Bd.TuckerAttnError):                   # one pool, two projections
         Bd.tucker_cache_append_paged(X, dw[3], dw[7], K, K, table, lens, torch.zeros(3, dtype=torch.int32, device="cuda"), rope=True)
@@ -550,6 +561,27 @@ def test_step_in_one_launch_of_one_pool(dtype, monkeypatch):
     for rope, path in ((False, 3), (True, 2 if dtype == "bf16" else 1)):
         check_step(P.PagedState(workload(shape, dtype, rope=rope, shared=True), [130, 0, 7], 16, P=90), what=f"rope {rope}")
         assert Bd.last_path() == path
+
+
+def test_step_in_one_launch_takes_no_workspace(monkeypatch):
+    """The C entry points: NULL for the workspace where the query says so, refused where it does not."""
+    import ctypes
+    lib = Bd.load_library()
+    ask = lib.tucker_attn_decode_prefix_workspace_bytes
+    w = workload(TC64, "bf16")
+    for rooms, none in ((0, True), (32768, False)):
+        monkeypatch.setattr(P, "ROOM", rooms)
+        st = P.PagedState(w, [5, 20], 16, P=40)
+        x, dw, K, V, table, lens, ptab = st.device()
+        desc = Bd.make_desc(B=2, N=1, d_model=w.d_model, n_H=w.n_H, r=w.r, t=w.t, causal=True, rope=True, rope_base=w.rope_base)
+        cache = Bd.TuckerPagedCache(K.data_ptr(), V.data_ptr(), table.data_ptr(), st.n_pages, st.page, st.max_pages)
+        d, c = bytes(desc), bytes(cache)
+        assert (ask(d, c, 40) == Bd.TA_WORKSPACE_NONE) == none
+        y = __import__("torch").empty_like(x)
+        rc = lib.tucker_attn_decode_prefix(d, x.data_ptr(), *[t.data_ptr() for t in dw], c, lens.data_ptr(), ptab.data_ptr(), 40, 1,
+                                           y.data_ptr(), None, 0, 0)
+        assert rc == (0 if none else -1)
+    assert Bd.last_device_error() == 0
 
 
 def test_step_in_one_launch_more_sequences_than_clusters(monkeypatch):
