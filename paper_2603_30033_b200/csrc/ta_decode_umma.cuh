@@ -38,7 +38,7 @@
 // loaded: what is left of an earlier tile there is masked (keys) or zeroed (values) as rows past the length always are.
 // This form also takes the query as the sum of two bf16 numbers (the rounded value and the rounded rest, 2^-17 together):
 // a query rounded once moves every score by 2^-9 of its size, which at scores of a standard deviation of 2 was two thirds of
-// the step's whole error (4.7e-3 of the output's norm, 2.3e-3 with the second half).  The second half is eight more MMAs of
+// the step's whole error (4.7e-3 of the output's norm, about 2e-3 with the second half).  The second half is eight more MMAs of
 // N = 32 per tile, hidden behind the loads.  With ROT the rotated keys are carried the same way (3.5e-3 -> 2.1e-3; 39 -> 42 us at 24 sequences of up to 3001 tokens).  The two halves share the room of two segments' queries, so that with r3 > 64 one
 // segment's queries are in flight instead of two.
 #pragma once
