@@ -64,7 +64,7 @@ __device__ __forceinline__ void cluster_sync() {
 
 __global__ void __launch_bounds__(THREADS, 1)
 k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmB1,
-         const Params p, const dec::RopeFreqs freqs) {
+         const Params p, const dec::RopeTurns turns) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full_bar[MAX_STAGES], empty_bar[MAX_STAGES], acc_bar;
   __shared__ uint32_t tmem_slot;
@@ -173,7 +173,7 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
       const int u = u0 + hf + 2 * k, t = u / upt, c = (u % upt) * UC;
       if (u < u1 && c < p0.width && p0.rope)
 #pragma unroll
-        for (int e = 0; e < UC / 2; ++e) cs[k][e] = dec::rope_cos_sin_theta((t == 0 ? dst[0] : dst[1]).pos, freqs.theta[c / 2 + e]);
+        for (int e = 0; e < UC / 2; ++e) cs[k][e] = dec::rope_at((t == 0 ? dst[0] : dst[1]).pos, turns, c / 2 + e);
     }
     ok = mbar_wait(&acc_bar, 0, ab);
     ok = __all_sync(0xffffffffu, ok);
@@ -245,7 +245,7 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
       if (first && p0.rope) {
 #pragma unroll
         for (int e = 0; e < UC / 2; ++e) {
-          const float2 cse = have ? a[e] : dec::rope_cos_sin_theta(to.pos, freqs.theta[c / 2 + e]);
+          const float2 cse = have ? a[e] : dec::rope_at(to.pos, turns, c / 2 + e);
           const float xe = v[2 * e], xo = v[2 * e + 1];
           v[2 * e] = xe * cse.x - xo * cse.y;
           v[2 * e + 1] = xe * cse.y + xo * cse.x;

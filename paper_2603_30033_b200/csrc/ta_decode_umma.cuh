@@ -43,6 +43,8 @@
 // segment's queries are in flight instead of two.
 #pragma once
 
+#include <type_traits>
+
 #include "ta_common.cuh"
 #include "ta_decode.cuh"
 #include "ta_sm100.cuh"
@@ -147,10 +149,13 @@ template <> struct TmemCols<8> {
   static __device__ __forceinline__ void st(uint32_t a, const uint32_t (&r)[8]) { tmem_st8(a, r); }
 };
 
+template <bool PAGED>
+using RopeTable = typename std::conditional<PAGED, dec::RopeTurns, dec::RopeFreqs>::type;
+
 template <bool ROT, int R3C, bool PAGED>
 __global__ void __launch_bounds__(ROT ? THREADS_ROT : THREADS, 1)
 k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                const __grid_constant__ CUtensorMap tmQ, const Params p, const dec::RopeFreqs freqs) {
+                const __grid_constant__ CUtensorMap tmQ, const Params p, const RopeTable<PAGED> freqs) {
   // cache_len was final before the preceding kernel (which forms the queries and appends the new row)
   // began: set-up and the tile split run while it finishes, and every role passes pdl_enter() before it
   // touches anything else.  (Requesting the first cache tiles ahead of that wait as well was measured:
@@ -502,15 +507,15 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
      float ac[HALF > 0 ? HALF : 1], as_[HALF > 0 ? HALF : 1];   // (cos, sin)(tid theta_i)
 #pragma unroll
      for (int i = 0; i < HALF; ++i) {
-       const float2 cs = dec::rope_cos_sin_theta(tid, freqs.theta[i]);
+       const float2 cs = dec::rope_at(tid, freqs, i);
        ac[i] = cs.x; as_[i] = cs.y;
      }
      auto wait_all = [&](uint64_t* bar, uint32_t parity) -> bool {
        bool good = mbar_wait(bar, parity, ab);
        return __all_sync(0xffffffffu, good);
      };
-     const float2 step_lo = dec::rope_cos_sin_theta(TK, freqs.theta[lane]);
-     const float2 step_hi = dec::rope_cos_sin_theta(TK, freqs.theta[32 + (lane & 31)]);
+     const float2 step_lo = dec::rope_at(TK, freqs, lane);
+     const float2 step_hi = dec::rope_at(TK, freqs, 32 + (lane & 31));
      pdl_enter();                                // the constants above depend on nothing
      float2 base_lo = make_float2(1.f, 0.f), base_hi = make_float2(1.f, 0.f);
      Walk w;
@@ -529,8 +534,8 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
        // first tile of a segment they are formed with the angle reduced in double precision; from tile to tile
        // they advance by the rotation through 128 theta_i (at most 256 steps of 1e-7 each: far below bf16).
        if (w.seg_start(t)) {
-         base_lo = dec::rope_cos_sin_theta(p.pos_base + k0, freqs.theta[lane]);
-         base_hi = (HALF > 32) ? dec::rope_cos_sin_theta(p.pos_base + k0, freqs.theta[32 + (lane & 31)]) : make_float2(1.f, 0.f);
+         base_lo = dec::rope_at(p.pos_base + k0, freqs, lane);
+         base_hi = (HALF > 32) ? dec::rope_at(p.pos_base + k0, freqs, 32 + (lane & 31)) : make_float2(1.f, 0.f);
        } else {
          base_lo = make_float2(base_lo.x * step_lo.x - base_lo.y * step_lo.y, base_lo.y * step_lo.x + base_lo.x * step_lo.y);
          base_hi = make_float2(base_hi.x * step_hi.x - base_hi.y * step_hi.y, base_hi.y * step_hi.x + base_hi.x * step_hi.y);

@@ -37,6 +37,20 @@ dec::RopeFreqs rope_freqs(const tucker_attn_desc& d) {
   return last.f;
 }
 
+dec::RopeTurns rope_turns(const tucker_attn_desc& d) {
+  static thread_local struct { int r3 = 0; float base = 0.f; dec::RopeTurns f; } last;
+  if (!d.rope) return dec::RopeTurns{};
+  if (last.r3 != d.r3 || last.base != d.rope_base) {
+    const dec::RopeFreqs f = rope_freqs(d);
+    for (int i = 0; i < 128; ++i) {
+      const double turns = f.theta[i] * 0.15915494309189535;                 // 1 / (2 pi)
+      last.f.turn[i] = (unsigned long long)ldexp(turns - floor(turns), 64);  // below 1, hence at most 2^64 - 2^11
+    }
+    last.r3 = d.r3; last.base = d.rope_base;
+  }
+  return last.f;
+}
+
 namespace {
 
 // ---- driver entry point for tensor-map creation (no link-time dependency on libcuda) --------
@@ -620,7 +634,7 @@ size_t carve_fast_dec(const tucker_attn_desc& d, bool paged, int32_t prefix_len,
 // latent RoPE (p.shared_rope) the instance with the rotation warpgroup runs: the cache holds un-rotated rows.
 template <bool ROT, int R3C, bool PAGED>
 int launch_dec_attn_inst(Problem& p, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmQ,
-                         const decu::Params& up, int grid, const dec::RopeFreqs& freqs) {
+                         const decu::Params& up, int grid, const decu::RopeTable<PAGED>& freqs) {
   static PerDeviceFlag attr;
   TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)decu::k_dec_attn_umma<ROT, R3C, PAGED>, (int)decu::SMEM_BYTES));
   prof_begin(p);
@@ -642,7 +656,9 @@ int launch_dec_attn_umma(Problem& p, const CUtensorMap& tmK, const CUtensorMap& 
   up.part_o = dp.part_o; up.part_ml = dp.part_ml; up.err = dp.err;
   up.pv = p.pv; up.pos_base = p.prefix_len; up.seq_cta = dp.seq_cta;
   if (p.shared_rope) {
-    const dec::RopeFreqs freqs = rope_freqs(d);
+    decu::RopeTable<PAGED> freqs;
+    if constexpr (PAGED) freqs = rope_turns(d);
+    else freqs = rope_freqs(d);
     switch (d.r3) {
       case 64: return launch_dec_attn_inst<true, 64, PAGED>(p, tmK, tmV, tmQ, up, grid, freqs);
       case 96: return launch_dec_attn_inst<true, 96, PAGED>(p, tmK, tmV, tmQ, up, grid, freqs);
@@ -650,7 +666,7 @@ int launch_dec_attn_umma(Problem& p, const CUtensorMap& tmK, const CUtensorMap& 
       default: return TA_ERR_UNSUPPORTED_SHAPE;
     }
   }
-  dec::RopeFreqs none = {};
+  decu::RopeTable<PAGED> none = {};
   return launch_dec_attn_inst<false, 0, PAGED>(p, tmK, tmV, tmQ, up, grid, none);
 }
 
@@ -664,7 +680,7 @@ int launch_prefix_rotate(Problem& p, const FastDecWs& w) {
   const tucker_attn_desc& d = p.d;
   const long n = (long)p.prefix_len * (d.r3 / 8);
   (void)launch_pdl(prefix::k_prefix_rotate, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, p.stream, (const bf16*)p.Kc,
-                   prefix::Rows{p.prefix_table, p.pv.n_pages, p.pv.page_size}, w.pre_k, p.prefix_len, d.r3, rope_freqs(d), p.dev_err);
+                   prefix::Rows{p.prefix_table, p.pv.n_pages, p.pv.page_size}, w.pre_k, p.prefix_len, d.r3, rope_turns(d), p.dev_err);
   TA_LAUNCH_CHECK(p);
   return TA_OK;
 }
@@ -904,7 +920,7 @@ int fast_append(Problem& p, const int32_t* tok_start, int32_t T) {
   cfg.attrs = la;
   cfg.numAttrs = 2;
   prof_begin(p);
-  (void)cudaLaunchKernelEx(&cfg, append::k_append, tmX, tm0, tm1, ap, rope_freqs(d));
+  (void)cudaLaunchKernelEx(&cfg, append::k_append, tmX, tm0, tm1, ap, rope_turns(d));
   prof_end(p);
   TA_LAUNCH_CHECK(p);
   return TA_OK;

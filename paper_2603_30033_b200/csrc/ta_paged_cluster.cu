@@ -51,7 +51,7 @@ struct Params {
   const int32_t *cache_len, *prefix_table;
   int B, d, nH, r1, r2, r3, t1, t2, t3, Lmax, P, append, one_pool, rope;
   float scale;
-  dec::RopeFreqs freqs;
+  dec::RopeTurns turns;
   unsigned int* err;
   // columns of the projections, of a key and of a value in groups of eight; (four heads, eight columns) pairs; ...
   Div nc3, ch3, ch, combos, half, t1d, t2d, nc, nh8;
@@ -368,7 +368,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
   }
   if (p.rope && tid >= THREADS - r3 / 2) {             // the last two warps, which have the least to add up
     const int i = THREADS - 1 - tid;
-    cs_s[i] = dec::rope_cos_sin_theta(p.P + L, p.freqs.theta[i]);
+    cs_s[i] = dec::rope_at(p.P + L, p.turns, i);
   }
   __syncthreads();
   cluster_wait();
@@ -754,7 +754,7 @@ int launch(Problem& p) {
   g.pv = p.pv; g.cache_len = p.cache_len; g.prefix_table = p.prefix_table;
   g.B = d.B; g.d = d.d_model; g.nH = d.n_H; g.r1 = d.r1; g.r2 = d.r2; g.r3 = d.r3; g.t1 = d.t1; g.t2 = d.t2; g.t3 = d.t3;
   g.Lmax = p.Lmax; g.P = p.prefix_len; g.append = p.append; g.one_pool = p.shared_kv; g.rope = d.rope;
-  g.scale = p.scale; g.freqs = rope_freqs(d); g.err = p.dev_err;
+  g.scale = p.scale; g.turns = rope_turns(d); g.err = p.dev_err;
   static PerDeviceFlag attr;
   TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)k_pg_step<T>, kMaxSmem));
   prof_begin(p);

@@ -139,6 +139,7 @@ struct AppendArgs {
   int B, T_, d, r3, t3, rope, pos0;
   int keys_shared;      // 1: only the value rows are written (one pool; un-rotated rows when rope)
   double base;
+  dec::RopeTurns turns; // of the first 128 pairs; those behind are formed from `base`
   unsigned int* err;
 };
 template <typename T>
@@ -147,13 +148,20 @@ __global__ void __launch_bounds__(GT) k_pg_append(const AppendArgs<T> g) {
   __shared__ TileSmem s;
   __shared__ long row_s[GM];
   __shared__ int pos_s[GM];
-  __shared__ double theta_s[GN / 2];
+  __shared__ unsigned long long turn_s[GN / 2];
   const bool is_k = blockIdx.z == 0 && !g.keys_shared;
   const int r = is_k ? g.r3 : g.t3;
   const int m0 = blockIdx.x * GM, n0 = blockIdx.y * GN;
   if (n0 >= r) return;
-  if (is_k && g.rope && threadIdx.x >= 64 && threadIdx.x < 64 + GN / 2)
-    theta_s[threadIdx.x - 64] = pair_theta(n0 / 2 + threadIdx.x - 64, r, g.base);
+  if (is_k && g.rope && threadIdx.x >= 64 && threadIdx.x < 64 + GN / 2) {
+    const int i = n0 / 2 + threadIdx.x - 64;
+    if (i < 128) {
+      turn_s[threadIdx.x - 64] = g.turns.turn[i];
+    } else {
+      const double turns = pair_theta(i, r, g.base) * 0.15915494309189535;
+      turn_s[threadIdx.x - 64] = (unsigned long long)((turns - floor(turns)) * 18446744073709551616.0);
+    }
+  }
   if (threadIdx.x < GM) {
     AppendDst dst;
     dst.row = -1; dst.pos = 0;
@@ -171,7 +179,7 @@ __global__ void __launch_bounds__(GT) k_pg_append(const AppendArgs<T> g) {
     float v = s.part[0][m][c];
     if (is_k && g.rope) {            // r3 is even and tiles start at even columns: both halves of a pair are here
       const float other = s.part[0][m][c ^ 1];
-      const float2 cs = dec::rope_cos_sin_theta(pos_s[m], theta_s[c >> 1]);
+      const float2 cs = dec::rope_cos_sin_turn(pos_s[m], turn_s[c >> 1]);
       v = (c & 1) ? other * cs.y + v * cs.x : v * cs.x - other * cs.y;
     }
     if (TA_IDX_OK(g.err, row_s[m] * r + n, 1, (long)g.pv.n_pages * g.pv.page_size * r)) st(pool + row_s[m] * r + n, v);
@@ -685,7 +693,7 @@ int append_typed(Problem& p, const int32_t* tok_start, int32_t T_) {
   g.X = (const T*)p.X; g.U3 = (const T*)p.U3; g.Ut3 = (const T*)p.Ut3;
   g.K = (T*)p.Kc; g.V = (T*)p.Vc; g.pv = p.pv; g.tok_start = tok_start; g.cache_len = p.cache_len;
   g.B = d.B; g.T_ = T_; g.d = d.d_model; g.r3 = d.r3; g.t3 = d.t3; g.rope = d.rope; g.pos0 = d.pos0;
-  g.keys_shared = p.shared_kv; g.base = (double)d.rope_base; g.err = p.dev_err;
+  g.keys_shared = p.shared_kv; g.base = (double)d.rope_base; g.turns = rope_turns(d); g.err = p.dev_err;
   const int wide = p.shared_kv ? d.t3 : std::max(d.r3, d.t3);
   (void)launch_pdl(k_pg_append<T>, dim3((T_ + GM - 1) / GM, (wide + GN - 1) / GN, p.shared_kv ? 1 : 2), dim3(GT), 0, p.stream, g);
   TA_LAUNCH_CHECK(p);

@@ -417,7 +417,7 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 // One pool with latent RoPE holds un-rotated rows: the prefix's keys, rotated at positions 0 .. P - 1 and laid one after
 // another (bf16 [P, r3]), for the call's attention kernel.  A thread per 8 columns of a row.
 __global__ void __launch_bounds__(256) k_prefix_rotate(const bf16* __restrict__ pool, const Rows rows, bf16* __restrict__ out, int P,
-                                                       int r3, const dec::RopeFreqs freqs, unsigned int* err) {
+                                                       int r3, const dec::RopeTurns turns, unsigned int* err) {
   pdl_enter();
   const int per = r3 / 8;
   const long i = (long)blockIdx.x * 256 + threadIdx.x;
@@ -431,7 +431,7 @@ __global__ void __launch_bounds__(256) k_prefix_rotate(const bf16* __restrict__ 
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[e]));
-    const float2 cs = dec::rope_cos_sin_theta(n, freqs.theta[c / 2 + e]);
+    const float2 cs = dec::rope_at(n, turns, c / 2 + e);
     wv[e] = pack_bf16(x.x * cs.x - x.y * cs.y, x.x * cs.y + x.y * cs.x);
   }
   if (TA_IDX_OK(err, (long)n * r3 + c, 8, (long)P * r3))
