@@ -181,7 +181,8 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
   uint8_t* qbuf = ring + (size_t)RING_BYTES;
   uint8_t* pbuf = qbuf + 2 * QBUF_BYTES;
   // With one shared latent cache a stage holds a K tile only: twice the stages.
-  const int STAGES = p.shared_kv ? 6 : 3;
+  // PAGED with ROT: four of them, the last two hold the rotation's table.
+  const int STAGES = p.shared_kv ? (ROT && PAGED ? 4 : 6) : 3;
   const int stage_bytes = p.shared_kv ? MAX_SUB * SUB_BYTES : STAGE_BYTES;
 
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -504,11 +505,22 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
      constexpr int HALF = R3C / 2;                // coordinate pairs per row
      const int q = warp - 12;
      const int tid = q * 32 + lane;              // key row of a tile
-     float ac[HALF > 0 ? HALF : 1], as_[HALF > 0 ? HALF : 1];   // (cos, sin)(tid theta_i)
+     // (cos, sin)(tid theta_i): in registers, which takes loops without an index left in them, or (PAGED) in shared memory, where the
+     // loops stay loops.  Code that runs once or a few times per CTA arrives at 3 to 4 bytes per cycle, and unrolled both the
+     // table (38 KB of code, 10.6 thousand cycles) and the first tile's rotation (7.9 thousand, later ones 4.2) were bound by that.
+     constexpr int NREG = PAGED ? 1 : (HALF > 0 ? HALF : 1);
+     float ac[NREG], as_[NREG];
+     float2* const tab = reinterpret_cast<float2*>(ring + 4 * (size_t)stage_bytes) + tid;      // PAGED: pair i at i * 128
+     static_assert(!PAGED || (size_t)HALF * 128 * sizeof(float2) <= 2 * (size_t)MAX_SUB * SUB_BYTES, "two stages of the ring");
+     if constexpr (PAGED) {
+#pragma unroll 4
+       for (int i = 0; i < HALF; ++i) tab[i * 128] = dec::rope_at(tid, freqs, i);
+     } else {
 #pragma unroll
-     for (int i = 0; i < HALF; ++i) {
-       const float2 cs = dec::rope_at(tid, freqs, i);
-       ac[i] = cs.x; as_[i] = cs.y;
+       for (int i = 0; i < HALF; ++i) {
+         const float2 cs = dec::rope_at(tid, freqs, i);
+         ac[i] = cs.x; as_[i] = cs.y;
+       }
      }
      auto wait_all = [&](uint64_t* bar, uint32_t parity) -> bool {
        bool good = mbar_wait(bar, parity, ab);
@@ -525,6 +537,17 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
      for (long t = t_begin; t < t_end && ok; ++t, ++it) {
        w.seek(t);
        const int s = it % STAGES, buf = it & 1, j = it >> 1;
+       // the new token's rows, by the warp whose tile rows they replace one of: lane = 16-byte chunk
+       const bool mine = PAGED && w.last_tile(t) && (w.L - w.k0(t)) >> 5 == q;
+       uint4 nk = make_uint4(0u, 0u, 0u, 0u), nv = nk;
+       if (mine && lane < R3C / 8) {
+         nk = reinterpret_cast<const uint4*>(p.knew + (long)w.b * p.r3)[lane];
+         nv = reinterpret_cast<const uint4*>(p.vnew + (long)w.b * p.t3)[lane];
+       }
+       auto chunk_of = [&](const uint4& v, int c) -> uint4 {
+         return make_uint4(__shfl_sync(0xffffffffu, v.x, c), __shfl_sync(0xffffffffu, v.y, c), __shfl_sync(0xffffffffu, v.z, c),
+                           __shfl_sync(0xffffffffu, v.w, c));
+       };
        if (!(ok = wait_all(&full_bar[s], (uint32_t)((it / STAGES) & 1)))) break;
        if (j > 0 && !(ok = wait_all(&kr_free[buf], (uint32_t)((j - 1) & 1)))) break;   // score product of tile it - 2 is done
        tc_fence_after();
@@ -585,35 +608,35 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
          }
        }
        } else {
-#pragma unroll
+#pragma unroll 1
        for (int hf = 0; hf < R3C / 32; ++hf) {  // 16 TMEM columns = 32 coordinates at a time, rounded values and rounded rests
          uint32_t o[16], ol[16];
+         const float2 bl = hf < 2 ? base_lo : base_hi;
 #pragma unroll
          for (int cc = 0; cc < 4; ++cc) {
-           const int c = hf * 4 + cc;           // 16-byte chunk of the row
-           const uint4 v = *reinterpret_cast<const uint4*>(raw + swz(tid, c));
+           const uint4 v = *reinterpret_cast<const uint4*>(raw + swz(tid, hf * 4 + cc));
            const uint32_t wv[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
            for (int e = 0; e < 4; ++e) {
-             const int i = 4 * c + e;
+             const int i = hf * 16 + 4 * cc + e;
              const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[e]));
-             const float2 bs = make_float2(__shfl_sync(0xffffffffu, i < 32 ? base_lo.x : base_hi.x, i & 31),
-                                           __shfl_sync(0xffffffffu, i < 32 ? base_lo.y : base_hi.y, i & 31));
-             const float cs_c = ac[i] * bs.x - as_[i] * bs.y, cs_s = as_[i] * bs.x + ac[i] * bs.y;   // angle addition
+             const float2 bs = make_float2(__shfl_sync(0xffffffffu, bl.x, i & 31), __shfl_sync(0xffffffffu, bl.y, i & 31));
+             const float2 a = tab[i * 128];
+             const float cs_c = a.x * bs.x - a.y * bs.y, cs_s = a.y * bs.x + a.x * bs.y;   // angle addition
              const float re = x.x * cs_c - x.y * cs_s, ro = x.x * cs_s + x.y * cs_c;
              o[4 * cc + e] = pack_bf16(re, ro);
              const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&o[4 * cc + e]));
              ol[4 * cc + e] = pack_bf16(re - f.x, ro - f.y);
            }
          }
-         if (is_new) {
-           // the new token's rotated key comes from the workspace
-           const uint4* kn = reinterpret_cast<const uint4*>(p.knew + (long)w.b * p.r3) + hf * 4;
+         if (mine) {                            // the new token's rotated key comes from the workspace
 #pragma unroll
            for (int cc = 0; cc < 4; ++cc) {
-             const uint4 v = kn[cc];
-             o[4 * cc] = v.x; o[4 * cc + 1] = v.y; o[4 * cc + 2] = v.z; o[4 * cc + 3] = v.w;
-             ol[4 * cc] = ol[4 * cc + 1] = ol[4 * cc + 2] = ol[4 * cc + 3] = 0u;
+             const uint4 v = chunk_of(nk, hf * 4 + cc);
+             if (is_new) {
+               o[4 * cc] = v.x; o[4 * cc + 1] = v.y; o[4 * cc + 2] = v.z; o[4 * cc + 3] = v.w;
+               ol[4 * cc] = ol[4 * cc + 1] = ol[4 * cc + 2] = ol[4 * cc + 3] = 0u;
+             }
            }
          }
          tmem_st16(kaddr + (uint32_t)hf * 16u, o);
@@ -624,12 +647,19 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
        if (last) {
          // as VALUES the new token's un-rotated latent row comes from the workspace and rows past it must be
          // zero (their probabilities are zero, but the slots may hold anything)
-         if (tid == rnew) {
+         if constexpr (PAGED) {
+           if (mine)
+#pragma unroll 2
+             for (int c = 0; c < R3C / 8; ++c) {
+               const uint4 v = chunk_of(nv, c);
+               if (tid == rnew) *reinterpret_cast<uint4*>(raw + swz(tid, c)) = v;
+             }
+         } else if (tid == rnew) {
            const uint4* vs = reinterpret_cast<const uint4*>(p.vnew + (long)w.b * p.t3);
            for (int c = 0; c < R3C / 8; ++c) *reinterpret_cast<uint4*>(raw + swz(tid, c)) = vs[c];
-         } else if (tid > rnew) {
-           for (int c = 0; c < R3C / 8; ++c) *reinterpret_cast<uint4*>(raw + swz(tid, c)) = make_uint4(0u, 0u, 0u, 0u);
          }
+         if (tid > rnew)
+           for (int c = 0; c < R3C / 8; ++c) *reinterpret_cast<uint4*>(raw + swz(tid, c)) = make_uint4(0u, 0u, 0u, 0u);
        }
        tc_fence_before();
        fence_proxy_async_smem();
