@@ -172,9 +172,8 @@ __device__ __forceinline__ float2 rope_cos_sin_theta(int pos, double theta) {
   return make_float2(co, sn);
 }
 // The same from the frequency as a fraction of a turn.  Exact but for the fraction's own rounding (2^-56 of a turn, as a double has it, times
-// the position) and the 2^-32 of a turn that the upper half drops.  The chain of eight 64-bit floating-point operations that
-// it replaces takes about 1000 cycles alone and 220 per value when pipelined: the table of 48 pairs that a thread of the
-// un-rotated pool's kernel starts with went from 10.6 thousand cycles to TABLE.
+// the position) and the 2^-32 of a turn that the upper half drops.  It replaces a chain of eight 64-bit floating-point operations:
+// append of 16384 tokens 41.1 -> 40.6 us, of 5792 (d 768) 11.0 -> 10.5, fp32 14.4 -> 14.0.
 __device__ __forceinline__ float2 rope_cos_sin_turn(int pos, unsigned long long turn) {
   const unsigned long long a = (unsigned long long)(unsigned)pos * turn;
   float sn, co;
