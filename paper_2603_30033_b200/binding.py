@@ -194,21 +194,14 @@ def alloc_workspace(nbytes: int, device):
     return torch.empty(nbytes if nbytes > 256 else 256, dtype=torch.uint8, device=device)
 
 
-class _on_device:
-    """`with torch.cuda.device(device)`, which costs several microseconds, only where another device is current."""
-    __slots__ = ("ctx",)
-
-    def __init__(self, device):
-        cuda = _torch().cuda
-        self.ctx = None if cuda.current_device() == device.index else cuda.device(device)
-
-    def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
-
-    def __exit__(self, *exc):
-        if self.ctx is not None:
-            self.ctx.__exit__(*exc)
+def _enter_device(cuda, device):
+    """Makes `device` current if it is not, and returns what to leave afterwards (None: nothing).  `with torch.cuda.device(device)`
+    around every call costs several microseconds."""
+    if cuda.current_device() == device.index:
+        return None
+    ctx = cuda.device(device)
+    ctx.__enter__()
+    return ctx
 
 
 def _stream_ptr(device) -> int:
@@ -397,9 +390,13 @@ def tucker_cache_append_paged(X, U3, Ut3, Kpages, Vpages, block_table, cache_len
         workspace = alloc_workspace(lib.tucker_cache_append_paged_workspace_bytes(desc, cache, T), dev)
     else:
         _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
-    with _on_device(dev):
+    other = _enter_device(torch.cuda, dev)
+    try:
         rc = lib.tucker_cache_append_paged(desc, X.data_ptr(), U3.data_ptr(), Ut3.data_ptr(), cache, cache_len.data_ptr(),
                                            tok_start.data_ptr(), T, workspace.data_ptr(), workspace.numel(), _stream_ptr(dev))
+    finally:
+        if other is not None:
+            other.__exit__(None, None, None)
     if rc != TA_OK:
         raise TuckerAttnError(rc, "tucker_cache_append_paged")
 
@@ -455,7 +452,8 @@ def tucker_attn_decode_prefix(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kpages, Vpage
     desc = _DESC_PACK(B, 1, d, n_H, r1, r2, r3, t1, t2, t3, 1, bool(rope), rope_base, 0, scale, code, flags)
     cache = _CACHE_PACK(Kpages.data_ptr(), Vpages.data_ptr(), block_table.data_ptr(), n_pages, page_size, max_pages)
     ws_ptr, ws_bytes = None, 0
-    with _on_device(dev):
+    other = _enter_device(torch.cuda, dev)
+    try:
         if workspace is not None:
             _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
             ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel()
@@ -468,6 +466,9 @@ def tucker_attn_decode_prefix(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kpages, Vpage
                                            Ct.data_ptr(), Ut1.data_ptr(), Ut2.data_ptr(), Ut3.data_ptr(), cache,
                                            cache_len.data_ptr(), prefix_ptr, prefix_len, bool(append), out.data_ptr(),
                                            ws_ptr, ws_bytes, _stream_ptr(dev))
+    finally:
+        if other is not None:
+            other.__exit__(None, None, None)
     if rc != TA_OK:
         raise TuckerAttnError(rc, "tucker_attn_decode_prefix")
     return out
