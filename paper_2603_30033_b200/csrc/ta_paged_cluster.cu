@@ -22,12 +22,14 @@
 // first loads and 0.6 to 1.5 go to each later phase; a tile of 64 keys per CTA 1.3 us (scores and values are issue and shared-memory
 // bound).  Exchanges by cluster barrier and remote reads, with less of the rest overlapped, were 16.3 us.
 #include "ta_paged.cuh"
-#include "ta_sm100.cuh"
+#include "ta_cluster.cuh"
 
 #include <algorithm>
 
 namespace ta {
 namespace pgc {
+
+using namespace cluster;
 
 constexpr int CL = 8, THREADS = 512, WARPS = THREADS / 32;
 constexpr int TK = 64;                                 // keys per tile
@@ -100,51 +102,6 @@ struct Layout {
   }
 };
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-using sm100::smem_u32;
-__device__ __forceinline__ uint32_t map_rank(const void* own, uint32_t rank) {      // `own`'s counterpart in CTA `rank`
-  uint32_t a;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(own)), "r"(rank));
-  return a;
-}
-// Sends values to the counterpart of `own` in CTA `rank`; their bytes complete on that CTA's barrier.
-__device__ __forceinline__ void send(const float* own, uint32_t rank, uint64_t* bar, float v) {
-  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];"
-               ::"r"(map_rank(own, rank)), "f"(v), "r"(map_rank(bar, rank)) : "memory");
-}
-__device__ __forceinline__ void send2(const float* own, uint32_t rank, uint64_t* bar, float2 v) {
-  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
-               ::"r"(map_rank(own, rank)), "f"(v.x), "f"(v.y), "r"(map_rank(bar, rank)) : "memory");
-}
-__device__ __forceinline__ void send4(const float* own, uint32_t rank, uint64_t* bar, float4 v) {
-  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
-               ::"r"(map_rank(own, rank)), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(map_rank(bar, rank)) : "memory");
-}
-__device__ __forceinline__ bool received_now(uint64_t* bar) {
-  uint32_t ok;
-  asm volatile(
-      "{\n"
-      ".reg .pred p;\n"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], 0;\n"
-      "selp.u32 %0, 1, 0, p;\n"
-      "}\n"
-      : "=r"(ok)
-      : "r"(smem_u32(bar))
-      : "memory");
-  return ok != 0;
-}
-// Waits for everything that one exchange sends to this CTA.  Bounded: a wait that runs out is flagged and the CTA goes on (every CTA
-// sends whatever happens, so that no other one is left waiting), its result void.
-__device__ __forceinline__ void received(uint64_t* bar, unsigned int* err) {
-  if (received_now(bar)) return;
-  const long long t0 = clock64();
-  while (!received_now(bar))
-    if (clock64() - t0 > sm100::kWaitBudgetCycles) {
-      atomicOr(err, (unsigned)TA_DEVERR_WAIT_TIMEOUT);
-      return;
-    }
-}
 __device__ __forceinline__ void cp16(void* dst, const void* src, bool there) {      // zeros where there is no row
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
 }

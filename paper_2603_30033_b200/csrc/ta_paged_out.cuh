@@ -11,6 +11,7 @@
 // from the streaming kernel instead of scanning the lengths.
 #pragma once
 
+#include "ta_cluster.cuh"
 #include "ta_common.cuh"
 #include "ta_decode.cuh"
 #include "ta_prefix_attn.cuh"
@@ -41,14 +42,6 @@ __host__ __device__ inline size_t smem_bytes(int cl, int t1, int t3, int nH, boo
   return sizeof(float) * ((size_t)parts * 64 + (size_t)t1 * t3 + ((size_t)nH * t1 + 1) / 2 * 2 + (size_t)THREADS * 4 + 32 * (128 / cl));
 }
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ void st_cluster(float* own, uint32_t rank, float v) {      // `own`'s counterpart in CTA `rank`
-  uint32_t a;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(sm100::smem_u32(own)), "r"(rank));
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory");
-}
-
 template <int CL>
 __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_out(const Params p) {
   constexpr int MAX_COLS = 128 / CL;
@@ -64,7 +57,15 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
   const int b = blockIdx.x / CL, y = blockIdx.x % CL, c0 = y * cw;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const int jn = p.t2 / CL, jbeg = y * jn;
-  cluster_arrive();                                        // "this CTA has started": waited for before the first remote store
+  __shared__ uint64_t bar_u, bar_z;                        // everybody's columns of u; (fused y) everybody's rows of z
+  if (tid == 0) {
+    sm100::mbar_init(&bar_u, 1);
+    sm100::mbar_init(&bar_z, 1);
+    sm100::fence_barrier_init();
+    sm100::mbar_expect_tx(&bar_u, p.t1 * t3 * 4);
+    if (p.Ut2) sm100::mbar_expect_tx(&bar_z, p.t2 * 4);
+  }
+  cluster::cluster_arrive();                               // "started, ready to receive": waited for before anything is sent
   // z: lane = (slice a of rpl, 16-byte chunk) of a row of the core
   const int nch = t3 / 8, rpl = 32 / nch;                  // 8, 12 or 16 chunks; 4, 2 or 2 slices at a time
   const int ga = lane / nch, ch = lane % nch;
@@ -193,18 +194,16 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
     *reinterpret_cast<float4*>(o_s + h * MAX_COLS + tid / p.nH * 4) = make_float4(s.x * inv, s.y * inv, s.z * inv, s.w * inv);
   }
   __syncthreads();
-  cluster_wait();
+  cluster::cluster_wait();
   // ---- this CTA's columns of u, to every CTA of the cluster ----
   for (int i = tid; i < p.t1 * cw; i += THREADS) {
     const int a = i / cw, c = i % cw;
     float acc = 0.f;
     for (int h = 0; h < p.nH; ++h) acc = fmaf(ut1_s[h * p.t1 + a], o_s[h * MAX_COLS + c], acc);
 #pragma unroll
-    for (int r = 0; r < CL; ++r) st_cluster(&u_s[a * t3 + c0 + c], r, acc);
+    for (int r = 0; r < CL; ++r) cluster::send(&u_s[a * t3 + c0 + c], r, &bar_u, acc);
   }
-  __syncthreads();
-  cluster_arrive();
-  cluster_wait();
+  cluster::received(&bar_u, p.err);
   // ---- z: a warp per row ----
   auto dot = [&](const uint4 (&v)[2][4], int a0, float (&acc)[2]) {
 #pragma unroll
@@ -245,7 +244,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
 #pragma unroll
       for (int off = 16; off >= 1; off >>= 1) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], off);
       if (p.Ut2) {
-        if (lane < CL && jl + r * WARPS < jn) st_cluster(&z_s[j], (uint32_t)lane, acc[r]);
+        if (lane < CL && jl + r * WARPS < jn) cluster::send(&z_s[j], (uint32_t)lane, &bar_z, acc[r]);
       } else if (lane == 0 && jl + r * WARPS < jn && TA_IDX_OK(p.err, (long)b * 2 * p.z_half + p.z_half + j, 1, (long)p.B * 2 * p.z_half)) {
         const bf16 zh = __float2bfloat16_rn(acc[r]);
         p.z[(long)b * 2 * p.z_half + j] = zh;
@@ -255,9 +254,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
   }
   if (p.Ut2) {
     // ---- y: lane = (row of rpw, 16-byte chunk of the factor's row); a lane's eight values of z stay in registers ----
-    __syncthreads();
-    cluster_arrive();
-    cluster_wait();
+    cluster::received(&bar_z, p.err);
     const int nc = p.t2 / 8, rpw = 32 / nc, sub = lane / nc, cz = lane % nc;
     const bool on = sub < rpw;
     float zr[8];
