@@ -14,6 +14,7 @@
 #include "ta_cluster.cuh"
 #include "ta_common.cuh"
 #include "ta_decode.cuh"
+#include "ta_paged.cuh"
 #include "ta_prefix_attn.cuh"
 
 namespace ta {
@@ -100,9 +101,8 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
   __syncthreads();
   // Up to here only inputs of the call were read; the partials come from the kernels before this one.
   pdl_enter();
-  const int i0 = p.seq_cta[2 * b];
-  int np = p.seq_cta[2 * b + 1] - i0 + 1;
-  if (!TA_IDX_OK(p.err, i0 + b, np, (long)p.grid + p.B)) np = 0;
+  const int noted = p.seq_cta[2 * b], np = noted_parts(noted, p.seq_cta[2 * b + 1], p.grid), i0 = np > 0 ? noted : 0;
+  if (np == 0 && tid == 0) atomicOr(p.err, (unsigned)TA_DEVERR_WAIT_TIMEOUT);      // the streaming kernel gave up: y is void
   // ---- weights: warp w takes the partials w, w + WARPS, ... of all heads (lane = head) ----
   {
     const int h = lane, pc = pc_s[h], prl = (b * p.nH + h) % prefix::RB;
