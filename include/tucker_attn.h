@@ -388,6 +388,16 @@ TA_API int tucker_attn_bounds_checked(void);
  */
 TA_API int tucker_attn_selftest_wait_timeout(int32_t budget_us, int32_t* out, void* cuda_stream);
 
+/*
+ * The same for the waits between the thread blocks of a cluster (paged decode step; no counterpart in the paper).
+ * One block waits, with a budget of about `budget_us` microseconds (1 .. 100000), for a number that the other block
+ * sends into its shared memory only after four times that long.  The wait must give up and set TA_DEVERR_WAIT_TIMEOUT,
+ * and the block must stay until the number has come.  `out` is caller-owned device memory for two int32: what the wait
+ * returned (0 = gave up) and whether the number was there when the block ended.  Asynchronous on `cuda_stream`;
+ * returns TA_OK, TA_ERR_INVALID_ARG or TA_ERR_CUDA.
+ */
+TA_API int tucker_attn_selftest_cluster_wait(int32_t budget_us, int32_t* out, void* cuda_stream);
+
 /* Which path the last tucker_attn_fwd / tucker_attn_decode call on this thread took:
  * 0 = none yet, 1 = generic FMA kernels, 2 = tensor-core kernels, 3 = the paged step's one-launch
  * form for small batches of short contexts.  Number of kernels that call launched. */

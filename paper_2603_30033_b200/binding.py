@@ -30,7 +30,7 @@ EXPORTS = (
     "tucker_attn_decode", "tucker_attn_status_string", "tucker_attn_last_device_error",
     "tucker_attn_last_path", "tucker_attn_last_launch_count", "tucker_attn_set_profile_events",
     "tucker_attn_decode_static", "tucker_attn_selftest_wait_timeout", "tucker_attn_sync_status",
-    "tucker_attn_bounds_checked",
+    "tucker_attn_bounds_checked", "tucker_attn_selftest_cluster_wait",
     "tucker_cache_append_paged", "tucker_cache_append_paged_workspace_bytes", "tucker_attn_decode_paged", "tucker_attn_decode_paged_workspace_bytes",
     "tucker_attn_decode_prefix", "tucker_attn_decode_prefix_workspace_bytes",
     "tucker_pack_gqa", "tucker_pack_mha", "tucker_pack_mla",
@@ -116,6 +116,8 @@ def load_library() -> ctypes.CDLL:
     lib.tucker_attn_set_profile_events.argtypes = [vp, vp]
     lib.tucker_attn_selftest_wait_timeout.restype = ctypes.c_int
     lib.tucker_attn_selftest_wait_timeout.argtypes = [i32, vp, vp]
+    lib.tucker_attn_selftest_cluster_wait.restype = ctypes.c_int
+    lib.tucker_attn_selftest_cluster_wait.argtypes = [i32, vp, vp]
     lib.tucker_pack_gqa.restype = ctypes.c_int
     lib.tucker_pack_gqa.argtypes = [i32] * 4 + [vp] * 13
     lib.tucker_pack_mha.restype = ctypes.c_int
@@ -663,6 +665,19 @@ def selftest_wait_timeout(budget_us: int = 2000, device=None):
         rc = load_library().tucker_attn_selftest_wait_timeout(int(budget_us), out.data_ptr(), _stream_ptr(dev))
     if rc != TA_OK:
         raise TuckerAttnError(rc, "tucker_attn_selftest_wait_timeout")
+    return out
+
+
+def selftest_cluster_wait(budget_us: int = 2000, device=None):
+    """Runs the self-test of the bounded waits within a cluster; returns the int32 tensor [the wait returned, what was
+    sent late had come when the block ended] (read it after synchronising)."""
+    torch = _torch()
+    dev = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+    out = torch.full((2,), -1, dtype=torch.int32, device=dev)
+    with torch.cuda.device(dev):
+        rc = load_library().tucker_attn_selftest_cluster_wait(int(budget_us), out.data_ptr(), _stream_ptr(dev))
+    if rc != TA_OK:
+        raise TuckerAttnError(rc, "tucker_attn_selftest_cluster_wait")
     return out
 
 

@@ -108,6 +108,7 @@ bool fast_append_supported(const tucker_attn_desc& d);
 size_t fast_append_workspace(const tucker_attn_desc& d, int32_t T, bool one_pool);
 int fast_append(Problem& p, const int32_t* tok_start, int32_t T);
 int wait_selftest(unsigned int* dev_err, int budget_us, int* out_dev, cudaStream_t stream);
+int cluster_wait_selftest(unsigned int* dev_err, int budget_us, int* out_dev, cudaStream_t stream);
 
 // Tensor-core GEMM with fp32 split-K partial outputs (ta_fast.cu): for z < splits,
 //   out[z * split_stride + row * N + col] = sum over the z-th share of K of A[row, k] B[col, k],

@@ -953,7 +953,37 @@ __global__ void k_wait_selftest(unsigned int* err, long long budget_cycles, int*
     out[2] = (int)((clock64() - t0) >> 10);
   }
 }
+// A cluster of two CTAs.  CTA 1 sends one number to CTA 0, but only after four times the budget that CTA 0's wait for it has: the
+// wait must give up and set the device error word, and CTA 0 must still be there when the number comes.  out[0] receives what
+// the wait returned (0 = gave up), out[1] whether the number had come when CTA 0 was about to end.
+__global__ void __cluster_dims__(2, 1, 1) k_cluster_wait_selftest(unsigned int* err, long long budget_cycles, int* out) {
+  __shared__ uint64_t bar;
+  __shared__ float slot;
+  if (threadIdx.x == 0) {
+    slot = 0.f;
+    sm100::mbar_init(&bar, 1);
+    sm100::fence_barrier_init();
+    sm100::mbar_expect_tx(&bar, blockIdx.x == 0 ? 4 : 0);
+  }
+  cluster::cluster_arrive();
+  cluster::cluster_wait();
+  if (threadIdx.x != 0) return;
+  if (blockIdx.x == 1) {
+    const long long t0 = clock64();
+    while (clock64() - t0 < 4 * budget_cycles) {}
+    cluster::send(&slot, 0, &bar, 1.f);
+  } else {
+    const bool came = cluster::received(&bar, err, budget_cycles);
+    if (!came) cluster::stay_for(&bar);
+    out[0] = came ? 1 : 0;
+    out[1] = cluster::received_now(&bar) && *reinterpret_cast<volatile float*>(&slot) == 1.f ? 1 : 0;
+  }
+}
 }  // namespace
+int cluster_wait_selftest(unsigned int* dev_err, int budget_us, int* out_dev, cudaStream_t stream) {
+  k_cluster_wait_selftest<<<2, 32, 0, stream>>>(dev_err, (long long)budget_us * 2000LL, out_dev);
+  return cudaGetLastError() == cudaSuccess ? TA_OK : TA_ERR_CUDA;
+}
 int wait_selftest(unsigned int* dev_err, int budget_us, int* out_dev, cudaStream_t stream) {
   const long long cycles = (long long)budget_us * 2000LL;      // about 2 GHz
   k_wait_selftest<<<1, 64, 0, stream>>>(dev_err, cycles, out_dev);

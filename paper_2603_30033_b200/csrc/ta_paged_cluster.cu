@@ -335,7 +335,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
   }
   request(0);
   request(1);
-  received(&bar_x, p.err);
+  bool came = received(&bar_x, p.err);
   for (int c = tid; c < N; c += THREADS) {
     float t = 0.f;
 #pragma unroll
@@ -382,7 +382,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
     xq[r2 + 2 * tid] = xe * cs.x - xo * cs.y;
     xq[r2 + 2 * tid + 1] = xe * cs.y + xo * cs.x;
   }
-  received(&bar_v, p.err);
+  came &= received(&bar_v, p.err);
   // queries, in units of log2
   for (int i = tid; i < nH * (r3 / 2); i += THREADS) {
     const int h = p.half(i), c = i - h * p.half.d;
@@ -558,7 +558,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
       if (!p.one_pool && tid >= THREADS - r3) put(p.K + dst_s * r3 + tid - (THREADS - r3), xq[r2 + tid - (THREADS - r3)]);
     }
   }
-  received(&bar_o, p.err);
+  came &= received(&bar_o, p.err);
   if (tid < nH) {
     float m = -INFINITY, l = 0.f, wr[CL];
 #pragma unroll
@@ -631,7 +631,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
     const int j = i / CL * 4;
     send4(zg + rank * t2 + j, i % CL, &bar_z, *reinterpret_cast<const float4*>(sum_s + j));
   }
-  received(&bar_z, p.err);
+  came &= received(&bar_z, p.err);
   if (tid < t2) {
     float t = 0.f;
 #pragma unroll
@@ -663,6 +663,9 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
       const int j = j0 + k * y_step;
       if (sub < rpw && cz == 0 && j < k_end && TA_IDX_OK(p.err, (long)b * d + j, 1, (long)p.B * d)) put(p.y + (long)b * d + j, t[k]);
     }
+  }
+  if (!came) {                                         // a wait ran out: y is void, and what comes late must find this CTA here
+    stay_for(&bar_x); stay_for(&bar_v); stay_for(&bar_o); stay_for(&bar_z);
   }
 }
 

@@ -203,7 +203,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
 #pragma unroll
     for (int r = 0; r < CL; ++r) cluster::send(&u_s[a * t3 + c0 + c], r, &bar_u, acc);
   }
-  cluster::received(&bar_u, p.err);
+  bool came = cluster::received(&bar_u, p.err);
   // ---- z: a warp per row ----
   auto dot = [&](const uint4 (&v)[2][4], int a0, float (&acc)[2]) {
 #pragma unroll
@@ -254,7 +254,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
   }
   if (p.Ut2) {
     // ---- y: lane = (row of rpw, 16-byte chunk of the factor's row); a lane's eight values of z stay in registers ----
-    cluster::received(&bar_z, p.err);
+    came &= cluster::received(&bar_z, p.err);
     const int nc = p.t2 / 8, rpw = 32 / nc, sub = lane / nc, cz = lane % nc;
     const bool on = sub < rpw;
     float zr[8];
@@ -288,14 +288,17 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
         if (on && cz == 0 && j < end && TA_IDX_OK(p.err, (long)b * p.d + j, 1, (long)p.B * p.d)) p.y[(long)b * p.d + j] = __float2bfloat16_rn(t);
       }
     }
-    return;
-  }
-  if (y == 0)
+  } else if (y == 0) {
     for (int j = p.t2 + tid; j < p.z_half; j += THREADS)
       if (TA_IDX_OK(p.err, (long)b * 2 * p.z_half + p.z_half + j, 1, (long)p.B * 2 * p.z_half)) {
         p.z[(long)b * 2 * p.z_half + j] = __float2bfloat16_rn(0.f);
         p.z[(long)b * 2 * p.z_half + p.z_half + j] = __float2bfloat16_rn(0.f);
       }
+  }
+  if (!came) {                                             // a wait ran out: what comes late must find this CTA here
+    cluster::stay_for(&bar_u);
+    if (p.Ut2) cluster::stay_for(&bar_z);
+  }
 }
 
 }  // namespace pgout

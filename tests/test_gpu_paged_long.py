@@ -71,3 +71,18 @@ def test_append_of_long_prompts(d, r3, t3, T, one_pool, rope):
         others = torch.ones(len(flat), dtype=torch.bool, device="cuda")
         others[at] = False
         assert torch.equal(flat[others], old[others])
+
+
+# ---- waits that run out ------------------------------------------------------------------------------------------------
+
+def test_block_whose_wait_ran_out_stays_until_the_late_bytes_have_come():
+    """Between the blocks of a cluster: the wait gives up and is flagged, the block does not end before its peer has sent."""
+    assert Bd.last_device_error() == 0
+    for budget_us in (500, 5000):
+        out = Bd.selftest_cluster_wait(budget_us)
+        assert Bd.last_device_error() == Bd.TA_DEVERR_WAIT_TIMEOUT
+        assert out.tolist() == [0, 1]
+    assert Bd.last_device_error() == 0
+    for bad in (0, -1, 100001):
+        with pytest.raises(Bd.TuckerAttnError):
+            Bd.selftest_cluster_wait(bad)
