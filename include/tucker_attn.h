@@ -223,7 +223,10 @@ typedef struct {
  * Row i of sequence b goes to slot cache_len[b] + i, at absolute position pos0 + cache_len[b] + i (pos0 >= 0: what stands in
  * front of slot 0, such as a shared prefix).  Used of desc: B, d_model, r3, t3, rope, rope_base, pos0, dtype, flags (the other
  * fields must be valid).  T = 0 is allowed.  Nothing else in the pools is touched.
- * workspace: >= tucker_cache_append_paged_workspace_bytes(desc, cache, T) bytes, 256-byte aligned.
+ * workspace: >= tucker_cache_append_paged_workspace_bytes(desc, cache, T) bytes, 256-byte aligned.  The size depends on how the
+ * call is divided over the current device's SMs: query with the device that the call will use, and note that it does not grow
+ * with T (a few tokens split d and need partial sums, long prompts do not).  One buffer for calls of several T takes the largest
+ * of their sizes.
  */
 TA_API size_t tucker_cache_append_paged_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache* cache, int32_t T);
 TA_API int tucker_cache_append_paged(const tucker_attn_desc* desc, const void* X, const void* U3, const void* Ut3,

@@ -388,12 +388,12 @@ def tucker_cache_append_paged(X, U3, Ut3, Kpages, Vpages, block_table, cache_len
                     (tok_start, "tok_start", (B + 1,))), i32, dev)
     desc = _DESC_PACK(B, 1, d, 1, 1, 1, r3, 1, 1, t3, 1, bool(rope), rope_base, pos0, 0.0, code, flags)
     cache = _CACHE_PACK(Kpages.data_ptr(), Vpages.data_ptr(), block_table.data_ptr(), n_pages, page_size, max_pages)
-    if workspace is None:
-        workspace = alloc_workspace(lib.tucker_cache_append_paged_workspace_bytes(desc, cache, T), dev)
-    else:
-        _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
     other = _enter_device(torch.cuda, dev)
     try:
+        if workspace is None:                          # the size goes by the current device's number of SMs
+            workspace = alloc_workspace(lib.tucker_cache_append_paged_workspace_bytes(desc, cache, T), dev)
+        else:
+            _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
         rc = lib.tucker_cache_append_paged(desc, X.data_ptr(), U3.data_ptr(), Ut3.data_ptr(), cache, cache_len.data_ptr(),
                                            tok_start.data_ptr(), T, workspace.data_ptr(), workspace.numel(), _stream_ptr(dev))
     finally:
