@@ -554,9 +554,11 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
        const int k0 = w.k0(t);
        // (cos, sin)(k0 theta_i) of this tile: lane l holds the values of pairs l and l + 32; they reach the
        // other lanes by shuffles (all lanes of a warp work on the same pair index at the same time).  At the
-       // first tile of a segment they are formed with the angle reduced in double precision; from tile to tile
-       // they advance by the rotation through 128 theta_i (at most 256 steps of 1e-7 each: far below bf16).
-       if (w.seg_start(t)) {
+       // first tile of a segment they are formed from the position; from tile to tile they advance by the rotation
+       // through 128 theta_i.  A step is off by up to 1e-7, always in the same direction: after the 7000 steps of a CTA's share of 2^27 keys
+       // by 4e-4 or more, a fifth of the once-rounded keys' 2^-9, but a hundred times the 2^-18 of PAGED's two halves, which
+       // therefore start afresh every 64 tiles (scores of 2000: output off by 0.26 of its norm without that).
+       if (w.seg_start(t) || (PAGED && (k0 / TK) % 64 == 0)) {
          base_lo = dec::rope_at(p.pos_base + k0, freqs, lane);
          base_hi = (HALF > 32) ? dec::rope_at(p.pos_base + k0, freqs, 32 + (lane & 31)) : make_float2(1.f, 0.f);
        } else {
