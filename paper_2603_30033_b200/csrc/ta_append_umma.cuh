@@ -132,8 +132,7 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
         if (p1.width)
           for (int j = 0; j < boxes(p1.width); ++j) tma_load_2d(b + j * BOX_BYTES, &tmB1, &full_bar[st], j * 64, kb * BK);
       }
-      if (ab.raised())                             // the copies in flight end before the CTA does
-        for (int i = max(0, issued - stages); i < issued; ++i) mbar_drain(&full_bar[i % stages], (uint32_t)((i / stages) & 1));
+      if (ab.raised()) mbar_drain_ring(full_bar, issued, stages);     // the copies in flight end before the CTA does
     }
   } else if (warp == 1) {
     if (elect_one()) {

@@ -314,7 +314,7 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         }
       }
       pdl_enter();
-      int it = 0, seg = -1;
+      int it = 0, seg = -1, q_issued = 0;
       for (; it < n_tiles; ++it) {
         const long t = t_begin + it;
         w.seek(t);
@@ -328,6 +328,7 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
               tma_load_2d(qbuf + (qb * 2 * ksub + kk) * QSUB_BYTES, &tmQ, &q_full[qb], (kk % ksub) * 64,
                           w.b * p.nH + (kk < ksub ? 0 : p.B * p.nH));
           }
+          q_issued = seg + 1;
         }
         if (it < ahead) continue;
         const int s = it % STAGES;
@@ -337,8 +338,8 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       }
       it = max(it, ahead);
       if (ab.raised()) {                           // the copies in flight end before the CTA does
-        for (int i = max(0, it - STAGES); i < it; ++i) mbar_drain(&full_bar[i % STAGES], (uint32_t)((i / STAGES) & 1));
-        if (seg >= 0) mbar_drain(&q_full[seg & (NQ - 1)], (uint32_t)((seg >> QSH) & 1));
+        mbar_drain_ring(full_bar, it, STAGES);
+        mbar_drain_ring(q_full, q_issued, NQ);
       }
     } else if (elect_one()) {
       tma_prefetch_desc(&tmK); tma_prefetch_desc(&tmV); tma_prefetch_desc(&tmQ);

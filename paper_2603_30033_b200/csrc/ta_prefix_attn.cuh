@@ -185,8 +185,8 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       ok = load(p.k, &tmK, kt, pk, ksub) && load(p.v, &tmV, kt, pv, vsub);
     }
     if (!ok) {                                                     // aborted: the copies in flight end before the CTA does
-      for (int i = max(0, n - n_buf); i < n; ++i) mbar_drain(&kv_full[i % n_buf], (uint32_t)((i / n_buf) & 1));
-      if (seg > 0) mbar_drain(&q_full, (uint32_t)((seg - 1) & 1));
+      mbar_drain_ring(kv_full, n, n_buf);
+      mbar_drain_ring(&q_full, seg, 1);
     }
    } else if (warp == 1) {
     // ------------------------------- MMA issuer ---------------------------------

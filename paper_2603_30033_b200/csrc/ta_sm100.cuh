@@ -92,6 +92,10 @@ __device__ __forceinline__ void mbar_drain(uint64_t* bar, uint32_t parity) {
   const long long t0 = clock64();
   while (!mbar_try_wait(bar, parity) && clock64() - t0 < 2000000LL) {}
 }
+// ... for all of a ring of n buffers, of which `issued` have been requested so far (buffer i % n, round i / n).
+__device__ __forceinline__ void mbar_drain_ring(uint64_t* bars, int issued, int n) {
+  for (int i = issued > n ? issued - n : 0; i < issued; ++i) mbar_drain(&bars[i % n], (uint32_t)((i / n) & 1));
+}
 
 // The same wait as a plain poll of mbarrier.test_wait, which never suspends the thread: for the single-thread MMA
 // issuers, whose reaction to a barrier sits on a kernel's critical path (measured on the long causal prefill: 1 %
