@@ -88,6 +88,136 @@ def test_block_whose_wait_ran_out_stays_until_the_late_bytes_have_come():
             Bd.selftest_cluster_wait(bad)
 
 
+# ---- steps whose CTAs work on many tiles and several sequences -----------------------------------------------------------
+
+class LongState:
+    """A bf16 step of `lens` own slots behind a prefix of P, on the GPU.  Rows grow along a sequence (prefix first) by `growth`,
+    so that the running maximum of the scores keeps moving; unused rows and pages hold NaN and infinities, unused table entries
+    bad page numbers."""
+
+    def __init__(self, d, h, r, t, lens, page, *, P=0, rope=True, one_pool=False, growth=7.0, seed=1):
+        import torch
+        g, dev, B = generator(seed), "cuda", len(lens)
+        normal = lambda *s, std=1.0: (torch.randn(*s, generator=g, device=dev) * std).bfloat16()
+        self.h, self.rope, self.one_pool, self.page, self.P, self.lens, self.base = h, rope, one_pool, page, P, lens, 500000.0
+        need, pre = [n // page + 1 for n in lens], -(-P // page)
+        n_pages, room = sum(need) + pre + 3, max(max(need) + 1, -(-32768 // page))
+        order = torch.randperm(n_pages, generator=g, device=dev).int()
+        table = torch.full((B, room), -9, dtype=torch.int32)
+        first = 0
+        for b, n in enumerate(need):
+            table[b, :n] = order[first:first + n].cpu()
+            first += n
+        table[:, -1] = 1 << 30
+        self.table, self.ptab = table.cuda(), order[first:first + pre].contiguous()
+        self.len = torch.tensor(lens, dtype=torch.int32, device=dev)
+        top = float(P + max(lens) + 1)
+        grow = lambda pos: 1.0 + growth * pos.double() / top
+        seq = torch.cat([torch.full((n,), b, device=dev) for b, n in enumerate(lens)])
+        slot = torch.cat([torch.arange(n, device=dev) for n in lens])
+        self.own_rows = self.table[seq, slot // page].long() * page + slot % page
+        at = torch.arange(P, device=dev)
+        self.pre_rows = self.ptab[at // page].long() * page + at % page if P else at
+        junk = torch.tensor([float("nan"), float("inf"), -float("inf"), 3e38], device=dev).bfloat16()
+
+        def pool(rank):
+            m = junk[torch.randint(0, 4, (n_pages * page, rank), generator=g, device=dev)]
+            m[self.own_rows] = (torch.randn(len(slot), rank, generator=g, device=dev) * grow(P + slot)[:, None]).bfloat16()
+            m[self.pre_rows] = (torch.randn(P, rank, generator=g, device=dev) * grow(at)[:, None]).bfloat16()
+            return m.view(n_pages, page, rank)
+
+        self.K = pool(r[2])
+        self.V = self.K if one_pool else pool(t[2])
+        self.x = normal(B, d)
+        C, U1, U2, U3 = normal(*r, std=(d / (r[0] * r[1] * r[2])) ** 0.5), normal(h, r[0], std=h ** -0.5), normal(d, r[1], std=d ** -0.5), normal(d, r[2], std=d ** -0.5)
+        Ct, Ut1, Ut2 = normal(*t, std=(t[1] * t[2]) ** -0.25), normal(h, t[0], std=h ** -0.5), normal(d, t[1], std=d ** -0.5)
+        self.w = [C, U1, U2, U3, Ct, Ut1, Ut2, U3 if one_pool else normal(d, t[2], std=d ** -0.5)]
+
+    def reference(self):
+        """y [B, d] and the new token's rows of K and V as the cache takes them, in 64 bits."""
+        import torch
+        C, U1, U2, U3, Ct, Ut1, Ut2, Ut3 = [a.double() for a in self.w]
+        x, B, P, n = self.x.double(), len(self.lens), self.P, self.len.long()
+        turn = (lambda a, pos: rotate(a, pos, self.base)) if self.rope else (lambda a, pos: a)
+        late = turn if self.one_pool else (lambda a, pos: a)            # one pool: keys are rotated when they are read
+        flat = lambda pool, rows: pool.view(-1, pool.shape[2])[rows].double()
+        scale = (x.shape[1] / self.h) ** -0.5
+        q = torch.einsum("ha,bac->bhc", U1, torch.einsum("bq,aqc->bac", x @ U2, C)) * scale
+        q = turn(q, (P + n)[:, None].expand(B, self.h))
+        new_k, new_v = x @ U3, x @ Ut3
+        kn = turn(new_k, P + n)
+        kp, vp = late(flat(self.K, self.pre_rows), torch.arange(P, device="cuda")), flat(self.V, self.pre_rows)
+        o, end = [], 0
+        for b, m in enumerate(self.lens):
+            rows = self.own_rows[end:end + m]
+            end += m
+            k = torch.cat((kp, late(flat(self.K, rows), P + torch.arange(m, device="cuda")), kn[b:b + 1]))
+            o.append((q[b] @ k.t()).softmax(1) @ torch.cat((vp, flat(self.V, rows), new_v[b:b + 1])))
+        z = torch.einsum("ha,ajc,bhc->bj", Ut1, Ct, torch.stack(o))
+        return z @ Ut2.t(), new_v if self.one_pool else kn, new_v
+
+    def check(self, what):
+        import torch
+        before = [self.K.clone(), self.V.clone()]
+        y_ref, kn, vn = self.reference()
+        kw = dict(n_H=self.h, rope=self.rope, rope_base=self.base)
+        y = Bd.tucker_attn_decode_prefix(self.x, *self.w, self.K, self.V, self.table, self.len, self.ptab if self.P else None, self.P, **kw)
+        assert Bd.last_device_error() == 0 and Bd.last_path() == 2
+        P.check_rows(y.double().cpu().numpy(), y_ref.cpu().numpy(), "bf16", what)
+        b = torch.arange(len(self.lens), device="cuda")
+        at = self.table[b, self.len.long() // self.page].long() * self.page + self.len.long() % self.page
+        for pool, was, rows in zip((self.K, self.V), before, (kn, vn)):
+            flat, old = pool.view(-1, pool.shape[2]), was.view(-1, pool.shape[2])
+            assert ((flat[at].double() - rows).abs() <= P.U_BF16 * rows.abs() + 5e-5).all(), what
+            keep = torch.ones(len(flat), dtype=torch.bool, device="cuda")
+            keep[at] = False
+            assert torch.equal(flat[keep].view(torch.int16), old[keep].view(torch.int16)), what
+
+
+RANKS = {"64": ((4, 64, 64), (4, 64, 64)), "96": ((3, 96, 96), (2, 32, 96)), "128": ((8, 96, 128), (8, 32, 128)),
+         "128/64": ((2, 32, 128), (1, 64, 64)), "64/128": ((5, 32, 64), (5, 96, 128))}
+
+
+# The tolerance of paged_helpers.check_rows holds with growing scores too: query and rotated keys are carried to 2^-17 (scores of up
+# to 50: 4e-4), cached rows are exact, and P, z and y are rounded whatever the scores.
+@pytest.mark.parametrize("page", [16, 64, 128])
+@pytest.mark.parametrize("pools", ["two", "one", "one, no rope"])
+@pytest.mark.parametrize("ranks", RANKS)
+def test_streaming_many_tiles_and_sequences_per_cta(ranks, pools, page):
+    """More tiles per CTA than its ring has stages, long and short sequences mixed: stages used again and again, the accumulator
+    rescaled, the rotation's base carried from tile to tile, several sequences in one CTA."""
+    r, t = RANKS[ranks]
+    if pools != "two" and r[2] != t[2]:
+        pytest.skip("one pool has one rank")
+    lens = [(b * b * 37 + 5 * b) % 4000 for b in range(100)]
+    for at, n in ((3, 0), (10, 1), (11, 127), (12, 128), (13, 0), (30, 129), (50, 0), (51, 0), (52, 16)):
+        lens[at] = n
+    tiles = sum(n // 128 + 1 for n in lens)
+    assert tiles > 148 * 7                                             # the deepest ring has six stages
+    LongState(256, 8, r, t, lens, page, rope=pools != "one, no rope", one_pool=pools != "two").check(f"{ranks} {pools} {page}")
+
+
+@pytest.mark.parametrize("pools", ["two", "one"])
+@pytest.mark.parametrize("lens", [[100003], [70000, 0, 50001]], ids=str)
+def test_streaming_one_sequence_over_many_ctas(lens, pools):
+    LongState(128, 32, (4, 64, 128), (4, 64, 128), lens, 64, one_pool=pools == "one").check(f"{lens} {pools}")
+
+
+@pytest.mark.parametrize("pools", ["two", "one, no rope"])
+@pytest.mark.parametrize("ranks", RANKS)
+@pytest.mark.parametrize("B,h,prefix,page", [(20, 32, 30001, 64), (41, 16, 29952, 128), (1200, 32, 500, 16)])
+def test_prefix_many_units_and_row_blocks_per_cta(B, h, prefix, page, ranks, pools):
+    """Several key tiles per CTA (ring and accumulator used again, rescaled), CTAs that end one block of 256 rows and begin the next, a last
+    block of 128 rows or fewer, a last key tile that is full or not."""
+    r, t = RANKS[ranks]
+    if pools != "two" and r[2] != t[2]:
+        pytest.skip("one pool has one rank")
+    units = -(-B * h // 256) * -(-prefix // 128)
+    assert units > 148 * 4                                             # three or six buffers, two a unit
+    lens = [(13 * b) % (300 if B < 100 else 3) for b in range(B)]
+    LongState(512, h, r, t, lens, page, P=prefix, rope=pools != "one, no rope", one_pool=pools != "two").check(f"{B} {ranks} {pools}")
+
+
 # ---- long sequences ----------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("pair", [0, 1, 2, 5])
