@@ -585,7 +585,7 @@ struct FastDecWs {
   float *part_o, *part_ml;
   int* seq_cta;            // [B][2], paged: CTAs of the streaming kernel that hold a sequence
   float *pre_o, *pre_ml;   // partials of the shared prefix
-  bf16* pre_k;             // one pool with latent RoPE: the prefix's keys, rotated (rows padded to whole tiles)
+  bf16* pre_k;             // one pool with latent RoPE: the prefix's keys, rotated (rows padded to whole tiles); their rests
 };
 
 // Width of one half of z in the paged step (see k_dec_out).
@@ -624,7 +624,7 @@ size_t carve_fast_dec(const tucker_attn_desc& d, bool paged, int32_t prefix_len,
     const size_t rows = (size_t)(dec::MAX_GRID + q.n_rb) * prefix::RB;
     t.pre_o = c.take<float>(rows * d.t3);
     t.pre_ml = c.take<float>(rows * 2);
-    t.pre_k = c.take<bf16>(rotated ? (size_t)q.n_kt * prefix::TK * d.r3 : 0);
+    t.pre_k = c.take<bf16>(rotated ? 2 * (size_t)q.n_kt * prefix::TK * d.r3 : 0);
   }
   if (w) *w = t;
   return c.off;
@@ -676,22 +676,28 @@ bool tmap_pages(CUtensorMap* m, const void* pool, int r, int n_pages, int page_s
 }
 
 // One pool with latent RoPE: the prefix's keys, rotated, one after another in the workspace.
-int launch_prefix_rotate(Problem& p, const FastDecWs& w) {
+int launch_prefix_rotate(Problem& p, const FastDecWs& w, const PrefixPlan& q) {
   const tucker_attn_desc& d = p.d;
   const long n = (long)p.prefix_len * (d.r3 / 8);
   (void)launch_pdl(prefix::k_prefix_rotate, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, p.stream, (const bf16*)p.Kc,
-                   prefix::Rows{p.prefix_table, p.pv.n_pages, p.pv.page_size}, w.pre_k, p.prefix_len, d.r3, rope_turns(d), p.dev_err);
+                   prefix::Rows{p.prefix_table, p.pv.n_pages, p.pv.page_size}, w.pre_k, (long)q.n_kt * prefix::TK * d.r3, p.prefix_len, d.r3, rope_turns(d),
+                   p.dev_err);
+  TA_LAUNCH_CHECK(p);
+  return TA_OK;
+}
+
+template <int KS, bool KLO>
+int launch_prefix_inst(Problem& p, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const prefix::Params& pp, int grid) {
+  static PerDeviceFlag attr;
+  TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)prefix::k_prefix_attn<KS, KLO>, (int)prefix::SMEM_BYTES));
+  (void)launch_pdl(prefix::k_prefix_attn<KS, KLO>, dim3(grid), dim3(prefix::THREADS), prefix::SMEM_BYTES, p.stream, tmQ, tmK, tmV, pp);
   TA_LAUNCH_CHECK(p);
   return TA_OK;
 }
 
 template <int KS>
-int launch_prefix_inst(Problem& p, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const prefix::Params& pp, int grid) {
-  static PerDeviceFlag attr;
-  TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)prefix::k_prefix_attn<KS>, (int)prefix::SMEM_BYTES));
-  (void)launch_pdl(prefix::k_prefix_attn<KS>, dim3(grid), dim3(prefix::THREADS), prefix::SMEM_BYTES, p.stream, tmQ, tmK, tmV, pp);
-  TA_LAUNCH_CHECK(p);
-  return TA_OK;
+int launch_prefix_ks(Problem& p, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const prefix::Params& pp, int grid) {
+  return p.shared_rope ? launch_prefix_inst<KS, true>(p, tmQ, tmK, tmV, pp, grid) : launch_prefix_inst<KS, false>(p, tmQ, tmK, tmV, pp, grid);
 }
 
 // Launched behind the streaming kernel, which does not write anything that it reads and lets it be launched only after it has
@@ -701,7 +707,7 @@ int launch_prefix(Problem& p, const FastDecWs& w, const PrefixPlan& q) {
   prefix::Params pp;
   pp.R = d.B * d.n_H; pp.P = p.prefix_len; pp.r3 = d.r3; pp.t3 = d.t3; pp.n_kt = q.n_kt; pp.n_rb = q.n_rb;
   pp.v = prefix::Rows{p.prefix_table, p.pv.n_pages, p.pv.page_size};
-  pp.k = p.shared_rope ? prefix::Rows{nullptr, q.n_kt, prefix::TK} : pp.v;
+  pp.k = p.shared_rope ? prefix::Rows{nullptr, 2 * q.n_kt, prefix::TK} : pp.v;
   pp.part_o = w.pre_o; pp.part_ml = w.pre_ml; pp.err = p.dev_err;
   const void* keys = p.shared_rope ? w.pre_k : p.Kc;
   CUtensorMap tmQ, tmK, tmV;
@@ -709,9 +715,9 @@ int launch_prefix(Problem& p, const FastDecWs& w, const PrefixPlan& q) {
   if (!tmap_pages(&tmK, keys, d.r3, pp.k.n_pages, pp.k.page_size)) return TA_ERR_CUDA;
   if (!tmap_pages(&tmV, p.Vc, d.t3, pp.v.n_pages, pp.v.page_size)) return TA_ERR_CUDA;
   switch (d.r3) {
-    case 64: return launch_prefix_inst<4>(p, tmQ, tmK, tmV, pp, q.grid);
-    case 96: return launch_prefix_inst<6>(p, tmQ, tmK, tmV, pp, q.grid);
-    case 128: return launch_prefix_inst<8>(p, tmQ, tmK, tmV, pp, q.grid);
+    case 64: return launch_prefix_ks<4>(p, tmQ, tmK, tmV, pp, q.grid);
+    case 96: return launch_prefix_ks<6>(p, tmQ, tmK, tmV, pp, q.grid);
+    case 128: return launch_prefix_ks<8>(p, tmQ, tmK, tmV, pp, q.grid);
     default: return TA_ERR_UNSUPPORTED_SHAPE;
   }
 }
@@ -823,7 +829,7 @@ int fast_decode(Problem& p) {
     TA_LAUNCH_CHECK(p);
   }
   const PrefixPlan pq = p.prefix_len > 0 ? prefix_plan(d, p.prefix_len) : PrefixPlan{0, 0, 0};
-  if (p.prefix_len > 0 && p.shared_rope && (rc = launch_prefix_rotate(p, w))) return rc;
+  if (p.prefix_len > 0 && p.shared_rope && (rc = launch_prefix_rotate(p, w, pq))) return rc;
   // ---- 3: attention over the latent cache ----
   {
     CUtensorMap tmK, tmV;

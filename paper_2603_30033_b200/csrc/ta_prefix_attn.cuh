@@ -22,6 +22,10 @@
 //
 // The query is carried as two bf16 halves, as in the paged streaming kernel.  The second half costs a third of the tensor
 // time (its eight MMAs per tile next to eight for the first half and eight for P V).
+// KLO: so are the keys, which one un-rotated pool with RoPE makes necessary (k_prefix_rotate): rotated keys rounded once moved
+// every score by 2^-9 of its size, and scores of a standard deviation of 8 the output by up to 2e-2 of its norm.
+// A unit then has three tiles, K, its rests and V: S_w = Qhi_w K^T + Qlo_w K^T + Qhi_w Klo^T.  At ranks above 64 the
+// ring just holds one unit, which is enough to go on: the scores of the next one need its two key tiles while V is still in use.
 // The value tile is used where it lies (MN-major B operand).
 // Slots past the prefix in its last page may hold anything: their scores are replaced by -inf, their value rows by zeros.
 #pragma once
@@ -77,10 +81,11 @@ __device__ __forceinline__ long owner_of(long t, long total, long grid) { return
 
 // KS = r3 / 16: with the number of K steps known the issue of an MMA takes about as long as the MMA; with a test in front of each
 // one the issuing thread set the pace (5900 against 5050 cycles per unit of two score tiles).
-template <int KS>
+template <int KS, bool KLO>
 __global__ void __launch_bounds__(THREADS, 1)
 k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
               const __grid_constant__ CUtensorMap tmV, const Params p) {
+  constexpr int NT = KLO ? 3 : 2;                          // tiles of a unit in the ring: keys, (their rests,) values
   extern __shared__ __align__(1024) uint8_t smem[];
   if (smem_u32(smem) & 1023u) {                            // never: the tiles' swizzle needs it
     if (threadIdx.x == 0) atomicOr(p.err, (unsigned)TA_DEVERR_BAD_INDEX);
@@ -182,7 +187,9 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         pk_next = lookup(p.k, nx);
         pv_next = lookup(p.v, nx);
       }
-      ok = load(p.k, &tmK, kt, pk, ksub) && load(p.v, &tmV, kt, pv, vsub);
+      ok = load(p.k, &tmK, kt, pk, ksub);
+      if (KLO) ok = ok && load(p.k, &tmK, kt, pk + p.n_kt, ksub);  // the rests lie n_kt tiles behind
+      ok = ok && load(p.v, &tmV, kt, pv, vsub);
     }
     if (!ok) {                                                     // aborted: the copies in flight end before the CTA does
       mbar_drain_ring(kv_full, n, n_buf);
@@ -196,7 +203,7 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       const uint64_t dq0 = umma_desc_kmajor_sw128(smem_u32(smem));
       const uint64_t dk0 = umma_desc_kmajor_sw128(smem_u32(ring));
       const uint64_t dv0 = umma_desc_mnmajor_sw128(smem_u32(ring), SUB_BYTES);
-      auto issue_qk = [&](int w, int s) {
+      auto issue_qk = [&](int w, int s, int sl) {            // ring buffers of the keys and of their rests
         const uint64_t dk = dk0 + (uint64_t)(s * (buf_bytes >> 4));
         const uint64_t dq = dq0 + (uint64_t)((w * q_tile) >> 4), dl = dq + (uint64_t)((ksub * SUB_BYTES) >> 4);
         const uint32_t d = tmem + (uint32_t)w * 128u;
@@ -210,6 +217,14 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           const uint64_t o = (uint64_t)((ks >> 2) * (SUB_BYTES >> 4) + (ks & 3) * 2);
           umma_ss(d, dl + o, dk + o, idesc_qk, 1u);
         }
+        if constexpr (KLO) {
+          const uint64_t dkl = dk0 + (uint64_t)(sl * (buf_bytes >> 4));
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            const uint64_t o = (uint64_t)((ks >> 2) * (SUB_BYTES >> 4) + (ks & 3) * 2);
+            umma_ss(d, dq + o, dkl + o, idesc_qk, 1u);
+          }
+        }
         umma_commit(&s_full[w]);
       };
       int n = 0;                          // ring buffers consumed so far
@@ -221,13 +236,21 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         const int nt = (int)min((long)(p.n_kt - kt0), u_end - u);
         const int nw = (p.R - rb * RB) > TQ ? 2 : 1;
         if (!(ok = mbar_wait(&q_full, (uint32_t)(seg & 1), ab))) break;
-        int sk = n % n_buf;
-        if (!(ok = mbar_wait(&kv_full[sk], (uint32_t)((n / n_buf) & 1), ab))) break;
+        // the keys in buffer n and, KLO, their rests in buffer n + 1 have arrived / are used no more
+        auto keys_full = [&]() -> bool {
+          return mbar_wait(&kv_full[n % n_buf], (uint32_t)((n / n_buf) & 1), ab) &&
+                 (!KLO || mbar_wait(&kv_full[(n + 1) % n_buf], (uint32_t)(((n + 1) / n_buf) & 1), ab));
+        };
+        auto keys_done = [&]() {
+          umma_commit(&kv_empty[n % n_buf]);
+          if (KLO) umma_commit(&kv_empty[(n + 1) % n_buf]);
+          n += NT - 1;
+        };
+        if (!(ok = keys_full())) break;
         tc_fence_after();
-        for (int w = 0; w < nw; ++w) issue_qk(w, sk);
-        umma_commit(&kv_empty[sk]);
+        for (int w = 0; w < nw; ++w) issue_qk(w, n % n_buf, (n + 1) % n_buf);
+        keys_done();
         if (nt == 1) umma_commit(&q_empty);
-        ++n;
         for (int i = 0; i < nt && ok; ++i) {
           const int sv = n % n_buf;
           if (!(ok = mbar_wait(&kv_full[sv], (uint32_t)((n / n_buf) & 1), ab))) break;
@@ -236,7 +259,6 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             if (!(ok = mbar_wait(&patched, (uint32_t)(n_patch & 1), ab))) break;
             ++n_patch;
           }
-          sk = n % n_buf;
           for (int w = 0; w < nw && ok; ++w) {
             if (!(ok = mbar_wait_poll(&p_half[w], (pf >> w) & 1u, ab))) break;
             if (i == 0) {                 // the accumulator of the group's previous segment must have been read
@@ -261,15 +283,14 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
               umma_ts(d, a + (uint32_t)ks * 8u, dv + (uint64_t)(ks * 128), idesc_pv, 1u);
             umma_commit(&o_full[w]);
             if (i + 1 < nt) {
-              if (w == 0 && !(ok = mbar_wait(&kv_full[sk], (uint32_t)((n / n_buf) & 1), ab))) break;
-              issue_qk(w, sk);
+              if (w == 0 && !(ok = keys_full())) break;
+              issue_qk(w, n % n_buf, (n + 1) % n_buf);
             }
           }
           if (!ok) break;
           umma_commit(&kv_empty[sv]);
           if (i + 1 < nt) {
-            umma_commit(&kv_empty[sk]);
-            ++n;
+            keys_done();
             if (i + 2 == nt) umma_commit(&q_empty);        // the segment's last scores are issued
           }
         }
@@ -303,7 +324,10 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
        const bool last = ragged && k0 + TK > p.P;
        if (last && w == 0) {
          // value rows past the prefix must not be trusted: zeros (a zero row is zero in any swizzle)
-         const int nv = n + 2 * i + 1, s = nv % n_buf;
+         // (KLO: the tile before it in its buffer may be the previous unit's values, which nothing here has waited for yet; until they
+         // have come, their buffer's barrier shows the parity that is waited for next)
+         if (KLO && i > 0 && !(ok = wait_all(&o_full[w], (uint32_t)((jt - 1) & 1)))) break;
+         const int nv = n + NT * i + NT - 1, s = nv % n_buf;
          if (!(ok = wait_all(&kv_full[s], (uint32_t)((nv / n_buf) & 1)))) break;
          if (k0 + rloc >= p.P)
            for (int kk = 0; kk < vsub; ++kk)
@@ -404,7 +428,7 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
        if (lane == 0) mbar_arrive(&o_read[w]);               // the next segment may overwrite the accumulator
        if (slot_ok) *reinterpret_cast<float2*>(p.part_ml + (slot * RB + w * TQ + rloc) * 2) = make_float2(m_used, l);
      }
-     n += 2 * nt;
+     n += NT * nt;
      u += nt;
    }
   }
@@ -415,9 +439,10 @@ k_prefix_attn(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 }
 
 // One pool with latent RoPE holds un-rotated rows: the prefix's keys, rotated at positions 0 .. P - 1 and laid one after
-// another (bf16 [P, r3]), for the call's attention kernel.  A thread per 8 columns of a row.
-__global__ void __launch_bounds__(256) k_prefix_rotate(const bf16* __restrict__ pool, const Rows rows, bf16* __restrict__ out, int P,
-                                                       int r3, const dec::RopeTurns turns, unsigned int* err) {
+// another, for the call's attention kernel: bf16 [P, r3], and `lo` elements behind it the rounded rests.  A thread per 8
+// columns of a row.
+__global__ void __launch_bounds__(256) k_prefix_rotate(const bf16* __restrict__ pool, const Rows rows, bf16* __restrict__ out, long lo,
+                                                       int P, int r3, const dec::RopeTurns turns, unsigned int* err) {
   pdl_enter();
   const int per = r3 / 8;
   const long i = (long)blockIdx.x * 256 + threadIdx.x;
@@ -427,15 +452,21 @@ __global__ void __launch_bounds__(256) k_prefix_rotate(const bf16* __restrict__ 
   uint4 v = make_uint4(0u, 0u, 0u, 0u);
   if (pg >= 0 && pg < rows.n_pages) v = *reinterpret_cast<const uint4*>(pool + ((long)pg * rows.page_size + n % rows.page_size) * r3 + c);
   else atomicOr(err, (unsigned)TA_DEVERR_BAD_PAGE);
-  uint32_t wv[4] = {v.x, v.y, v.z, v.w};
+  uint32_t wv[4] = {v.x, v.y, v.z, v.w}, wl[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[e]));
     const float2 cs = dec::rope_at(n, turns, c / 2 + e);
-    wv[e] = pack_bf16(x.x * cs.x - x.y * cs.y, x.x * cs.y + x.y * cs.x);
+    const float re = x.x * cs.x - x.y * cs.y, ro = x.x * cs.y + x.y * cs.x;
+    wv[e] = pack_bf16(re, ro);
+    const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&wv[e]));
+    wl[e] = pack_bf16(re - f.x, ro - f.y);
   }
-  if (TA_IDX_OK(err, (long)n * r3 + c, 8, (long)P * r3))
-    *reinterpret_cast<uint4*>(out + (long)n * r3 + c) = make_uint4(wv[0], wv[1], wv[2], wv[3]);
+  const long at = (long)n * r3 + c;
+  if (TA_IDX_OK(err, at, 8, lo)) {
+    *reinterpret_cast<uint4*>(out + at) = make_uint4(wv[0], wv[1], wv[2], wv[3]);
+    *reinterpret_cast<uint4*>(out + lo + at) = make_uint4(wl[0], wl[1], wl[2], wl[3]);
+  }
 }
 
 }  // namespace prefix

@@ -203,7 +203,7 @@ def test_streaming_one_sequence_over_many_ctas(lens, pools):
     LongState(128, 32, (4, 64, 128), (4, 64, 128), lens, 64, one_pool=pools == "one").check(f"{lens} {pools}")
 
 
-@pytest.mark.parametrize("pools", ["two", "one, no rope"])
+@pytest.mark.parametrize("pools", ["two", "one", "one, no rope"])
 @pytest.mark.parametrize("ranks", RANKS)
 @pytest.mark.parametrize("B,h,prefix,page", [(20, 32, 30001, 64), (41, 16, 29952, 128), (1200, 32, 500, 16)])
 def test_prefix_many_units_and_row_blocks_per_cta(B, h, prefix, page, ranks, pools):
