@@ -270,3 +270,34 @@ def test_rotation_late_in_a_long_share_of_one_sequence(pair):
     err = float((D(y)[0] - ref).norm() / ref.norm())
     print(f"pair {pair}: share {float(s.softmax(1)[0, 0]):.3f} error {err:.2e}")
     assert err <= 0.028, err
+
+
+# ---- large scores in the one-launch form --------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("gain", [8.0, 60.0])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_step_in_one_launch_large_scores_against_the_oracle(dtype, gain, monkeypatch):
+    """Scores up to the order of 60 and 500: few keys carry a head, in any tile of any CTA, and running maxima, rescaled sums and the
+    join of the CTAs' parts decide the values.
+
+    Tolerance: all arithmetic is fp32 from the stored values on.  The query (sums over 256, 64 and 4 terms, a rotation) and the
+    score (64 terms) are off by about sqrt(256) 2^-24 + 2 sqrt(64) 2^-24 = 2e-6 of |q| |k| at most, which counts twice in a quotient
+    of exponentials, and the rows of values that share the weight may be twice as long as their mean: 8e-6 |q| |k|.  On top of it what
+    small scores leave (1e-5, paged_helpers.check_rows) and, in bf16, the rounding of y: 2^-8 of each element."""
+    import numpy as np
+    from paper_2603_30033_b200 import workloads as W
+    from tests import helpers as H
+    monkeypatch.setattr(P, "ROOM", 0)
+    w = H.custom_workload(kind="decode", dtype=dtype, rope=True, rope_base=500000.0, seed=91, d_model=256, n_H=4, r=(4, 64, 64), t=(4, 64, 64))
+    for lens, pre in (([300, 3, 0], 200), ([1000, 77], 0), ([0, 1], 1100)):
+        st = P.PagedState(w, lens, 16, P=pre, core_gain=gain)
+        q = np.einsum("ha,bac->bhc", st.wt["U1"], np.einsum("bq,aqc->bac", st.x @ st.wt["U2"], st.wt["C"])) * (256 / 4) ** -0.5
+        keys = np.concatenate([st.pre_k, st.x @ st.wt["U3"], *st.own_k])
+        size = np.linalg.norm(q, axis=-1).max() * np.linalg.norm(keys, axis=-1).max()
+        x, dw, K, V, table, n, ptab = st.device()
+        y = Bd.tucker_attn_decode_prefix(x, *dw, K, V, table, n, ptab if pre else None, pre, n_H=4, rope=True, rope_base=w.rope_base)
+        assert Bd.last_path() == 3 and Bd.last_device_error() == 0
+        got, ref = y.double().cpu().numpy(), st.oracle_step()[0]
+        err = np.linalg.norm(got - ref, axis=-1) / np.linalg.norm(ref, axis=-1)
+        print(f"{dtype} gain {gain} |q||k| {size:.0f} errors {err}")
+        assert (err <= 8e-6 * size + 1e-5 + (P.U_BF16 if dtype == "bf16" else 0.0)).all(), (size, err)
