@@ -195,14 +195,17 @@ TA_API int tucker_attn_decode_static(const tucker_attn_desc* desc, const void* x
  * block_table, cache_len, tok_start and prefix_table are DEVICE memory and are read when the call's kernels run.  A
  * table entry that is needed and lies outside [0, n_pages) sets TA_DEVERR_BAD_PAGE: its rows count as zeros, nothing is
  * written through it.  A cache_len outside [0, max_pages * page_size) sets TA_DEVERR_BAD_CACHE_LEN (decode clamps it as
- * tucker_attn_decode does, and appends nothing to that sequence; append drops the tokens concerned).  Two sequences may read the same page (a prefix that
- * both hold); a page that a call WRITES belongs to one sequence only, else it is not defined whose row it holds.
+ * tucker_attn_decode does, and appends nothing to that sequence; append drops the tokens concerned).  Two sequences may
+ * read the same page (a prefix that both hold); a page that a call WRITES belongs to one sequence only, else it is not
+ * defined whose row it holds.
  *
  * Limits: B <= 65535, B n_H <= 2^24, max_pages * page_size + (pos0 or prefix_len) < 2^31 - 4096.  Any page_size >= 1.
- * bf16 decode shapes that the contiguous step runs on tensor cores do so here with a page_size of 16, 32, 64 or a multiple of
- * 128; bf16 appends with d_model a multiple of 64 and ranks that are multiples of 32 up to 256, with any page_size.  Everything
- * else runs on fp32 FMA kernels.  A workspace must not be in use by another call that may overlap on the GPU (other streams,
- * other captured graphs); nothing in it is kept from one call to the next.
+ * bf16 decode shapes that the contiguous step runs on tensor cores do so here with a page_size of 16, 32, 64 or a
+ * multiple of 128: d_model a multiple of 64, n_H, r1 and t1 up to 32, B up to 4096, r2 and t2 multiples of 32 up to
+ * 256, (r3, t3) one of (64, 64), (96, 96), (128, 128), (64, 128), (128, 64).  So do bf16 appends with d_model a
+ * multiple of 64 and ranks that are multiples of 32 up to 256, with any page_size.  Everything else runs on fp32 FMA
+ * kernels.  A workspace must not be in use by another call that may overlap on the GPU (other streams, other captured
+ * graphs); nothing in it is kept from one call to the next.
  */
 typedef struct {
   void* K;                    /* [n_pages, page_size, r3]  device */
@@ -218,15 +221,15 @@ typedef struct {
  * latent values X Ut3 (Sec. 3.1, Definition 2), written to the slots that follow each sequence's cached ones.
  *   X          [T, d_model]  token rows of all sequences, one after another
  *   cache_len  [B] tokens that each sequence has already; the caller adds what it appended afterwards
- *   tok_start  [B + 1] ascending: sequence b brings rows tok_start[b] .. tok_start[b + 1] - 1 (none is allowed); rows of X
- *              outside [tok_start[0], tok_start[B]) are padding and are not used
- * Row i of sequence b goes to slot cache_len[b] + i, at absolute position pos0 + cache_len[b] + i (pos0 >= 0: what stands in
- * front of slot 0, such as a shared prefix).  Used of desc: B, d_model, r3, t3, rope, rope_base, pos0, dtype, flags (the other
- * fields must be valid).  T = 0 is allowed.  Nothing else in the pools is touched.
- * workspace: >= tucker_cache_append_paged_workspace_bytes(desc, cache, T) bytes, 256-byte aligned.  The size depends on how the
- * call is divided over the current device's SMs: query with the device that the call will use, and note that it does not grow
- * with T (a few tokens split d and need partial sums, long prompts do not).  One buffer for calls of several T takes the largest
- * of their sizes.
+ *   tok_start  [B + 1] ascending: sequence b brings rows tok_start[b] .. tok_start[b + 1] - 1 (none is allowed); rows
+ *              of X outside [tok_start[0], tok_start[B]) are padding and are not used
+ * Row i of sequence b goes to slot cache_len[b] + i, at absolute position pos0 + cache_len[b] + i (pos0 >= 0: what
+ * stands in front of slot 0, such as a shared prefix).  Used of desc: B, d_model, r3, t3, rope, rope_base, pos0, dtype,
+ * flags (the other fields must be valid).  T = 0 is allowed.  Nothing else in the pools is touched.
+ * workspace: >= tucker_cache_append_paged_workspace_bytes(desc, cache, T) bytes, 256-byte aligned.  The size depends on
+ * how the call is divided over the current device's SMs: query with the device that the call will use, and note that it
+ * does not grow with T (a few tokens split d and need partial sums, long prompts do not).  One buffer for calls of
+ * several T takes the largest of their sizes.
  */
 TA_API size_t tucker_cache_append_paged_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache* cache, int32_t T);
 TA_API int tucker_cache_append_paged(const tucker_attn_desc* desc, const void* X, const void* U3, const void* Ut3,
@@ -246,17 +249,20 @@ TA_API int tucker_attn_decode_paged(const tucker_attn_desc* desc, const void* x,
                              void* y, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
- * The same step for a batch whose sequences all start with the same prefix_len tokens, stored once: slot i of the prefix
- * is row i % page_size of page prefix_table[i / page_size] of the same pools (filled, for instance, by an append with
- * B = 1 and prefix_table as its block table).  The new token of sequence b attends to the prefix, to its own slots
+ * The same step for a batch whose sequences all start with the same prefix_len tokens, stored once: slot i of the
+ * prefix is row i % page_size of page prefix_table[i / page_size] of the same pools (filled, for instance, by an append
+ * with B = 1 and prefix_table as its block table).  The new token of sequence b attends to the prefix, to its own slots
  * 0 .. cache_len[b] - 1 and to itself; its own slot i has position prefix_len + i.  The prefix is attended to once for
  * all B n_H query rows and joined with the own part by the softmax's maxima and sums: the result is that of the paged
  * step on sequences that hold the prefix themselves.  prefix_len = 0 (prefix_table may be NULL) is that step.
  * prefix_len is read on the host; the rest as for tucker_attn_decode_paged.
  *
- * Small batches of short contexts (by the sizes of the descriptor and the table, on the current device) run as one launch
- * that keeps everything on chip.  The queries then return TA_WORKSPACE_NONE, and a call of exactly those sizes may pass NULL
- * and 0 for the workspace.
+ * Small batches of short contexts (by the sizes of the descriptor and the table, on the current device) run as one
+ * launch that keeps everything on chip.  The queries then return TA_WORKSPACE_NONE, and a call of exactly those sizes
+ * may pass NULL and 0 for the workspace.  The lengths are device data, so that the choice goes by what the table has
+ * room for (max_pages * page_size): a server whose contexts are short for now gets this form with a table as narrow as
+ * they are (the same memory with another max_pages needs the rows laid out anew), and the forms for long contexts with
+ * a wide one.
  */
 #define TA_WORKSPACE_NONE ((size_t)1)
 TA_API size_t tucker_attn_decode_prefix_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache* cache,
@@ -364,8 +370,8 @@ TA_API int tucker_attn_last_device_error(void* cuda_stream);
  * far went through (no counterpart in the paper).  Synchronises `cuda_stream`, reads and clears the device
  * error word and returns TA_OK when it was clean, else TA_ERR_DEVICE_TIMEOUT (a bounded wait gave up: results
  * of the calls since the last read are invalid), TA_ERR_INVALID_ARG (a cache_len entry was out of range and
- * was clamped, or a page table entry was) or TA_ERR_CUDA (the read itself failed, or a bounds check of the checking build fired), in
- * that order of precedence.
+ * was clamped, or a page table entry was) or TA_ERR_CUDA (the read itself failed, or a bounds check of the checking
+ * build fired), in that order of precedence.
  */
 TA_API int tucker_attn_sync_status(void* cuda_stream);
 

@@ -1,18 +1,19 @@
-// Append to a paged latent cache on tcgen05: [K | V] = X [U3 | Ut3], latent RoPE on K, rows scattered to their pages; one
-// launch, nothing between X and the pages touches memory.
+// Append to a paged latent cache on tcgen05: [K | V] = X [U3 | Ut3], latent RoPE on K, rows scattered to their pages;
+// one launch, nothing between X and the pages touches memory.
 //
-// One CTA multiplies MT tiles of 128 token rows (A, K-major) with the factors as they lie in memory (B, MN-major), all columns of
-// both or of one of them, over a share of d.  The S CTAs of a cluster share the rows and split d: a batch of a few tokens is
-// bound by reading the factors, which S (times two) SMs then do at once, and a long prompt whose row tiles do not fill
-// the GPU gets more CTAs without reading X or the factors twice.  The sum over the cluster goes through the caller's
-// workspace, i.e. the L2 cache:
+// One CTA multiplies MT tiles of 128 token rows (A, K-major) with the factors as they lie in memory (B, MN-major), all
+// columns of both or of one of them, over a share of d.  The S CTAs of a cluster share the rows and split d: a batch of
+// a few tokens is bound by reading the factors, which S (times two) SMs then do at once, and a long prompt whose row
+// tiles do not fill the GPU gets more CTAs without reading X or the factors twice.  The sum over the cluster goes
+// through the caller's workspace, i.e. the L2 cache:
 //   unit       32 columns x 128 rows of fp32 sums; the units of a cluster are dealt evenly to its CTAs
-//   every CTA  writes the others' units, meets them at the cluster's barrier, reads its own units back and adds them in the
-//              order of the shares (its own share straight from TMEM): no atomics, the result does not depend on timing
-// (Through distributed shared memory, written or read, the same exchange moved about 13 bytes per cycle and SM: 128 KB per CTA
-// took 10 thousand cycles of the 16384-token call, and 7 of the 16 thousand cycles of the 64-token call.)
-//   epilogue   thread = token row: rotation at the row's position (angles formed while the products run), one rounding to bf16,
-//              64 adjacent bytes of eight rows per store instruction
+//   every CTA  writes the others' units, meets them at the cluster's barrier, reads its own units back and adds them in
+//              the order of the shares (its own share straight from TMEM): no atomics, the result does not depend on
+//              timing
+// (Through distributed shared memory, written or read, the same exchange moved about 13 bytes per cycle and SM: 128 KB
+// per CTA took 10 thousand cycles of the 16384-token call, and 7 of the 16 thousand cycles of the 64-token call.)
+//   epilogue   thread = token row: rotation at the row's position (angles formed while the products run), one rounding
+//              to bf16, 64 adjacent bytes of eight rows per store instruction
 // Bounds: X read once and the pages written once when T is large; per-CTA bytes of X and the factors over L2 otherwise,
 // which is what the choice of MT, S and the column split minimises (append_plan).
 //   warp 0  TMA producer      warp 1  TMEM, MMA issue      warps 2..9  epilogue, two per TMEM lane quadrant
@@ -32,8 +33,8 @@ constexpr int MAX_STAGES = 8;
 constexpr int RING_BYTES = 192 * 1024;
 constexpr size_t SMEM_BYTES = 1024 + (size_t)RING_BYTES;
 constexpr int A_BYTES = BM * BK * 2, BOX_BYTES = 64 * BK * 2, UNIT_BYTES = UC * BM * 4;
-// A finished unit's rounded rows wait in the idle ring for their stores: one place per half of the epilogue warps, however many
-// units a CTA finishes (up to 16).
+// A finished unit's rounded rows wait in the idle ring for their stores: one place per half of the epilogue warps,
+// however many units a CTA finishes (up to 16).
 constexpr int STAGED_BYTES = UC * BM * 2;
 static_assert(2 * STAGED_BYTES <= RING_BYTES, "both halves' staged units fit into the ring");
 constexpr int MAX_S = 8;
@@ -169,8 +170,8 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
       const int row = m0 + t * BM + rloc;
       if (t < MT && row < p.T) dst[t] = append_dst(row, p.tok_start, p.cache_len, p.B, p.pos0, p.pv, p.err);
     }
-    // ... and the angles of its first two units, where they are rotated (all of its rotated units, unless r3 > 128 or the CTA
-    // finishes two row tiles by itself)
+    // ... and the angles of its first two units, where they are rotated (all of its rotated units, unless r3 > 128 or
+    // the CTA finishes two row tiles by itself)
 #pragma unroll
     for (int k = 0; k < CSU; ++k) {
       const int u = u0 + hf + 2 * k, t = u / upt, c = (u % upt) * UC;
@@ -188,8 +189,8 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
   };
   // rows of this warp that exist: none of the others' sums are needed
   auto warp_rows = [&](int u) -> bool { return m0 + (u / upt) * BM + q * 32 < p.T; };
-  // 16-byte chunk `ch` of row `row` of the unit that this half has staged: a warp's rows of one chunk are adjacent, and the four
-  // chunks of one row lie on different banks.  A row belongs to one warp, which alone writes and reads it.
+  // 16-byte chunk `ch` of row `row` of the unit that this half has staged: a warp's rows of one chunk are adjacent, and
+  // the four chunks of one row lie on different banks.  A row belongs to one warp, which alone writes and reads it.
   auto chunk_at = [&](int row, int ch) -> uint32_t {
     return (uint32_t)(hf * STAGED_BYTES + ch * (BM * 16) + ((row ^ ch) << 4));
   };
@@ -287,9 +288,9 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
   if (warp == 1) tmem_dealloc(tmem, ncols);
 }
 
-// How a call is divided: MT row tiles per CTA, S shares of d per cluster, and whether the two factors go to different CTAs.
-// The CTA's time is taken as proportional to the bytes it moves into shared memory, times the waves of one CTA per SM;
-// a share of d costs the partial sums once to the L2 cache and back.
+// How a call is divided: MT row tiles per CTA, S shares of d per cluster, and whether the two factors go to different
+// CTAs. The CTA's time is taken as proportional to the bytes it moves into shared memory, times the waves of one CTA
+// per SM; a share of d costs the partial sums once to the L2 cache and back.
 struct Plan {
   int MT, S, split_parts;
 };

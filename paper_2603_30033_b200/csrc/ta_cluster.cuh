@@ -1,10 +1,11 @@
 // Exchange between the CTAs of a cluster through distributed shared memory.
 //
-// A receiver's mbarrier is told once how many bytes an exchange will bring (expect_tx) before the cluster's start barrier; senders store with
-// st.async, whose bytes complete on that mbarrier, and the receiver waits for its phase 0.  That is one way through the cluster and
-// no fence, where a cluster barrier costs the fence over all remote stores and a round of arrivals (join kernel of the paged step, cluster barriers against this: one-pool step
-// 32.7 -> 32.1 us, long batch 142.0 -> 141.5, document 87.6 -> 87.3, system prompt 45.9 -> 46.1).  Each buffer and mbarrier is used
-// once per launch.  A CTA may leave when it has received everything that is sent to it (stay_for, where a wait ran out).
+// A receiver's mbarrier is told once how many bytes an exchange will bring (expect_tx) before the cluster's start
+// barrier; senders store with st.async, whose bytes complete on that mbarrier, and the receiver waits for its phase 0.
+// That is one way through the cluster and no fence, where a cluster barrier costs the fence over all remote stores and
+// a round of arrivals (join kernel of the paged step, cluster barriers against this: one-pool step 32.7 -> 32.1 us,
+// long batch 142.0 -> 141.5, document 87.6 -> 87.3, system prompt 45.9 -> 46.1).  Each buffer and mbarrier is used once
+// per launch.  A CTA may leave when it has received everything that is sent to it (stay_for, where a wait ran out).
 #pragma once
 
 #include "ta_common.cuh"
@@ -47,8 +48,8 @@ __device__ __forceinline__ bool received_now(uint64_t* bar) {
       : "memory");
   return ok != 0;
 }
-// Waits for everything that one exchange sends to this CTA.  Bounded: a wait that runs out is flagged and returns false, and the CTA
-// goes on (every CTA sends whatever happens, so that no other one is left waiting), its result void.
+// Waits for everything that one exchange sends to this CTA.  Bounded: a wait that runs out is flagged and returns
+// false, and the CTA goes on (every CTA sends whatever happens, so that no other one is left waiting), its result void.
 __device__ __forceinline__ bool received(uint64_t* bar, unsigned int* err, long long budget_cycles = sm100::kWaitBudgetCycles) {
   if (received_now(bar)) return true;
   const long long t0 = clock64();
@@ -59,8 +60,9 @@ __device__ __forceinline__ bool received(uint64_t* bar, unsigned int* err, long 
     }
   return true;
 }
-// For a thread whose wait ran out, before it ends: it stays, and its CTA's shared memory with it, until the late bytes have come, so
-// that nothing is stored to a CTA that has gone.  They do come: a sender sends after sitting out its own waits, of which it has a few.
+// For a thread whose wait ran out, before it ends: it stays, and its CTA's shared memory with it, until the late bytes
+// have come, so that nothing is stored to a CTA that has gone.  They do come: a sender sends after sitting out its own
+// waits, of which it has a few.
 __device__ __forceinline__ void stay_for(uint64_t* bar) {
   const long long t0 = clock64();
   while (!received_now(bar) && clock64() - t0 < 8 * sm100::kWaitBudgetCycles) {}

@@ -24,8 +24,8 @@ namespace dec {
 struct RopeFreqs {
   double theta[128];
 };
-// The same frequencies as 64-bit fractions of a turn, theta / (2 pi) mod 1: position times fraction mod 2^64 is then the fraction of
-// the angle, by one integer product.
+// The same frequencies as 64-bit fractions of a turn, theta / (2 pi) mod 1: position times fraction mod 2^64 is then
+// the fraction of the angle, by one integer product.
 struct RopeTurns {
   unsigned long long turn[128];
 };
@@ -124,7 +124,8 @@ size_t generic_paged_decode_workspace(const tucker_attn_desc& d, int64_t Lmax, i
 int generic_paged_decode(Problem& p);
 int generic_paged_append(Problem& p, const int32_t* tok_start, int32_t T);
 
-// Paged decode step of few sequences with short contexts in one launch, both types (ta_paged_cluster.cu); needs no workspace.
+// Paged decode step of few sequences with short contexts in one launch, both types (ta_paged_cluster.cu); needs no
+// workspace.
 bool cluster_step_supported(const tucker_attn_desc& d, bool one_pool);
 bool cluster_step_pays(const tucker_attn_desc& d, int64_t slots, int32_t prefix_len, bool tensor_cores);
 int cluster_paged_decode(Problem& p);
@@ -172,9 +173,10 @@ __device__ __forceinline__ float2 rope_cos_sin_theta(int pos, double theta) {
   sincospif((float)(2.0 * turns), &sn, &co);
   return make_float2(co, sn);
 }
-// The same from the frequency as a fraction of a turn.  Exact but for the fraction's own rounding (2^-56 of a turn, as a double has it, times
-// the position) and the 2^-32 of a turn that the upper half drops.  It replaces a chain of eight 64-bit floating-point operations:
-// append of 16384 tokens 41.1 -> 40.6 us, of 5792 (d 768) 11.0 -> 10.5, fp32 14.4 -> 14.0.
+// The same from the frequency as a fraction of a turn.  Exact but for the fraction's own rounding (2^-56 of a turn, as
+// a double has it, times the position) and the 2^-32 of a turn that the upper half drops.  It replaces a chain of eight
+// 64-bit floating-point operations: append of 16384 tokens 41.1 -> 40.6 us, of 5792 (d 768) 11.0 -> 10.5, fp32 14.4 ->
+// 14.0.
 __device__ __forceinline__ float2 rope_cos_sin_turn(int pos, unsigned long long turn) {
   const unsigned long long a = (unsigned long long)(unsigned)pos * turn;
   float sn, co;

@@ -39,7 +39,6 @@ __device__ __forceinline__ int tiles_of(int L) { return L / TK + 1; }   // keys 
 // First global tile of CTA i when `total` tiles are split over `grid` CTAs.
 __device__ __forceinline__ long cta_first_tile(long i, long total, long grid) { return i * total / grid; }
 
-
 // Block-wide scan over the tile counts of all sequences.  Thread t owns the sequences
 // [lo, hi) = [t * chunk, (t + 1) * chunk); returns the total number of tiles and sets `excl` to the
 // number of tiles before sequence `lo`.  wtot_s needs one slot per warp of the block; contains a
@@ -97,7 +96,10 @@ __device__ __forceinline__ float2 rope_cos_sin(int pos, int i, int r, double log
 // warp w, lane (rg = lane / 4, ch = lane % 4) owns chunk ch of the CTA's 64-byte column range
 // in the core rows q = 8 w + rg + 64 i, AB slices a at a time (NQ = ceil(r2/64)); the eight row groups
 // of a warp are summed by exchanging halves (56 shuffles for 64 values instead of 192).
-// part: [splits][Mpad][r2 + r3 + t3] fp32.  With pv.table the caches are pools of pages; pos_base is the position of slot 0.
+// part: [splits][Mpad][r2 + r3 + t3] fp32.  With pv.table the caches are pools of pages; pos_base is the position of
+// slot 0.
+// The new token's key and value enter its own attention as the cache takes them, rounded to bf16: the row that this step
+// sees is the row that every later step reads.
 // ---------------------------------------------------------------------------------------
 constexpr int DQ_CW = 32;       // latent key coordinates per CTA
 constexpr int DQ_MAX_R1 = 32;   // head ranks r1, t1 supported by the shared-memory tables
@@ -230,8 +232,8 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
       }
     }
     if (a0 + AB < r1) load_batch(a0 + AB, v);       // next batch in flight during the reduction
-    // sums over the eight row groups (lane bits 2, 3, 4), in that order: at each level a lane keeps one half of its values
-    // and hands the other half to its partner
+    // sums over the eight row groups (lane bits 2, 3, 4), in that order: at each level a lane keeps one half of its
+    // values and hands the other half to its partner
     {
       float* v = &acc[0][0];
       constexpr int NV = AB * 8;

@@ -31,16 +31,19 @@
 // (registers) and the tile's 64 base values for k0 (formed per tile with the angle reduced in double precision).
 //   warps 12..15  rotation warpgroup (ROT only)
 //
-// PAGED = true: the caches are pools of pages and the tensor maps are [page][row][column].  A 128-key tile is one box when a
-// page holds a multiple of 128 rows, else 128 / page_size boxes of a page each, side by side in the same shared-memory
-// tile (a box of 16 rows or more keeps the 8-row groups of the 128-byte swizzle).  The producer is then a whole warp: lane i
-// looks up page i of the tile one tile ahead and issues its boxes.  Pages that hold no cached row of the sequence are not
-// loaded: what is left of an earlier tile there is masked (keys) or zeroed (values) as rows past the length always are.
-// This form also takes the query as the sum of two bf16 numbers (the rounded value and the rounded rest, 2^-17 together):
-// a query rounded once moves every score by 2^-9 of its size, which at scores of a standard deviation of 2 was two thirds of
-// the step's whole error (4.7e-3 of the output's norm, about 2e-3 with the second half).  The second half is eight more MMAs of
-// N = 32 per tile, hidden behind the loads.  With ROT the rotated keys are carried the same way (3.5e-3 -> 2.1e-3; 3 us of 42 at 24 sequences of up to 3001 tokens).  The two halves share the room of two segments' queries, so that with r3 > 64 one
-// segment's queries are in flight instead of two.
+// PAGED = true: the caches are pools of pages and the tensor maps are [page][row][column].  A 128-key tile is one box
+// when a page holds a multiple of 128 rows, else 128 / page_size boxes of a page each, side by side in the same
+// shared-memory tile (a box of 16 rows or more keeps the 8-row groups of the 128-byte swizzle).  The producer is then a
+// whole warp: lane i looks up page i of the tile one tile ahead and issues its boxes.  Pages that hold no cached row of
+// the sequence are not loaded: what is left of an earlier tile there is masked (keys) or zeroed (values) as rows past
+// the length always are.
+// This form also takes the query as the sum of two bf16 numbers (the rounded value and the rounded rest, 2^-17
+// together): a query rounded once moves every score by 2^-9 of its size, which at scores of a standard deviation of 2
+// was two thirds of the step's whole error (4.7e-3 of the output's norm, about 2e-3 with the second half).  The second
+// half is eight more MMAs of N = 32 per tile, hidden behind the loads.  With ROT the rotated keys are carried the same
+// way (3.5e-3 -> 2.1e-3; 3 us of 42 at 24 sequences of up to 3001 tokens).  The two halves share the room of two
+// segments' queries, so that with r3 > 64 one segment's queries are in flight instead of two.
+// Probabilities are rounded to bf16 once (they are an operand of the tensor cores), and the sum is of the rounded ones.
 #pragma once
 
 #include <type_traits>
@@ -228,7 +231,8 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
   int lo, hi;
   long excl;
   const long total = dec::block_tile_scan(p.cache_len, p.B, p.Lmax, lo, hi, excl, wtot_s);
-  // PAGED: with fewer tiles than CTAs the first `total` CTAs take one each, so that the CTAs of a sequence are neighbours
+  // PAGED: with fewer tiles than CTAs the first `total` CTAs take one each, so that the CTAs of a sequence are
+  // neighbours
   const long parts = PAGED ? min((long)gridDim.x, total) : (long)gridDim.x;
   const long t_begin = min(dec::cta_first_tile(blockIdx.x, total, parts), total);
   const long t_end = min(dec::cta_first_tile(blockIdx.x + 1, total, parts), total);
@@ -288,10 +292,11 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             for (int kk = 0; kk < vsub; ++kk) tma_load_3d(vt + kk * SUB_BYTES, &tmV, &full_bar[s], kk * 64, x.in_page, x.pg);
         }
       };
-      // A CTA whose tiles all fit into the ring requests them before the wait for the query kernel: the cached rows were final
-      // before it began (the row that it appends is patched in from the workspace wherever it lies in a tile), as were the tables
-      // and lengths.  One sequence of 37 tokens: step 21.9 -> 21.0 us; six behind a prefix 24.9 -> 23.6.  With more tiles the early
-      // loads only get in the query kernel's way (64 sequences to 32768 tokens: 142.7 -> 150.5 us).
+      // A CTA whose tiles all fit into the ring requests them before the wait for the query kernel: the cached rows
+      // were final before it began (the row that it appends is patched in from the workspace wherever it lies in a
+      // tile), as were the tables and lengths.  One sequence of 37 tokens: step 21.9 -> 21.0 us; six behind a prefix
+      // 24.9 -> 23.6.  With more tiles the early loads only get in the query kernel's way (64 sequences to 32768
+      // tokens: 142.7 -> 150.5 us).
       Walk w, wn;                                  // the tile in hand and the next one to be looked up
       w.init(p, t_begin, t_end, b0, seq_first);
       wn.init(p, t_begin, t_end, b0, seq_first);
@@ -388,7 +393,8 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       const uint64_t dk0 = umma_desc_kmajor_sw128(smem_u32(ring));
       const uint64_t dv0 = umma_desc_mnmajor_sw128(smem_u32(ring) + (p.shared_kv ? 0u : (uint32_t)(MAX_SUB * SUB_BYTES)), SUB_BYTES);
       const uint64_t stage_step = (uint64_t)(stage_bytes >> 4);          // descriptor address fields count 16 bytes
-      // pending P V products, oldest first; a tile's state in one word: it << 8 | stage << 4 | first tile of its segment
+      // pending P V products, oldest first; a tile's state in one word: it << 8 | stage << 4 | first tile of its
+      // segment
       uint32_t pq0 = 0, pq1 = 0;
       int pv_seg0 = 0, pv_seg1 = 0, n_pend = 0;
       bool ok = true;
@@ -506,9 +512,10 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
      constexpr int HALF = R3C / 2;                // coordinate pairs per row
      const int q = warp - 12;
      const int tid = q * 32 + lane;              // key row of a tile
-     // (cos, sin)(tid theta_i): in registers, which takes loops without an index left in them, or (PAGED) in shared memory, where the
-     // loops stay loops.  Code that runs once or a few times per CTA arrives at 3 to 4 bytes per cycle, and unrolled both the
-     // table (38 KB of code, 10.6 thousand cycles) and the first tile's rotation (7.9 thousand, later ones 4.2) were bound by that; now 6.7 and 4.2, the whole step 38.7 -> 32.7 us.
+     // (cos, sin)(tid theta_i): in registers, which takes loops without an index left in them, or (PAGED) in shared
+     // memory, where the loops stay loops.  Code that runs once or a few times per CTA arrives at 3 to 4 bytes per
+     // cycle, and unrolled both the table (38 KB of code, 10.6 thousand cycles) and the first tile's rotation (7.9
+     // thousand, later ones 4.2) were bound by that; now 6.7 and 4.2, the whole step 38.7 -> 32.7 us.
      constexpr int NREG = PAGED ? 1 : (HALF > 0 ? HALF : 1);
      float ac[NREG], as_[NREG];
      float2* const tab = reinterpret_cast<float2*>(ring + 4 * (size_t)stage_bytes) + tid;      // PAGED: pair i at i * 128
@@ -556,9 +563,10 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
        // (cos, sin)(k0 theta_i) of this tile: lane l holds the values of pairs l and l + 32; they reach the
        // other lanes by shuffles (all lanes of a warp work on the same pair index at the same time).  At the
        // first tile of a segment they are formed from the position; from tile to tile they advance by the rotation
-       // through 128 theta_i.  A step is off by up to 1e-7, always in the same direction: after the 7000 steps of a CTA's share of 2^27 keys
-       // by 4e-4 or more, a fifth of the once-rounded keys' 2^-9, but a hundred times the 2^-18 of PAGED's two halves, which
-       // therefore start afresh every 64 tiles (scores of 2000: output off by 0.26 of its norm without that).
+       // through 128 theta_i.  A step is off by up to 1e-7, always in the same direction: after the 7000 steps of a
+       // CTA's share of 2^27 keys by 4e-4 or more, a fifth of the once-rounded keys' 2^-9, but a hundred times the
+       // 2^-18 of PAGED's two halves, which therefore start afresh every 64 tiles (scores of 2000: output off by 0.26
+       // of its norm without that).
        if (w.seg_start(t) || (PAGED && (k0 / TK) % 64 == 0)) {
          base_lo = dec::rope_at(p.pos_base + k0, freqs, lane);
          base_hi = (HALF > 32) ? dec::rope_at(p.pos_base + k0, freqs, 32 + (lane & 31)) : make_float2(1.f, 0.f);

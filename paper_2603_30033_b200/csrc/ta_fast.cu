@@ -25,7 +25,8 @@
 namespace ta {
 
 // theta_i = base^(-2 i / r3) in double precision, i < r3 / 2; the first 128 (all of them on the tensor-core path).
-// The last table of each thread is kept (a table depends on the base and the rank only; 64 pow() take 0.7 us of every call).
+// The last table of each thread is kept (a table depends on the base and the rank only; 64 pow() take 0.7 us of every
+// call).
 dec::RopeFreqs rope_freqs(const tucker_attn_desc& d) {
   static thread_local struct { int r3 = 0; float base = 0.f; dec::RopeFreqs f; } last;
   if (!d.rope) return dec::RopeFreqs{};
@@ -700,8 +701,8 @@ int launch_prefix_ks(Problem& p, const CUtensorMap& tmQ, const CUtensorMap& tmK,
   return p.shared_rope ? launch_prefix_inst<KS, true>(p, tmQ, tmK, tmV, pp, grid) : launch_prefix_inst<KS, false>(p, tmQ, tmK, tmV, pp, grid);
 }
 
-// Launched behind the streaming kernel, which does not write anything that it reads and lets it be launched only after it has
-// itself waited for the kernels in front (queries, rotated keys): see ta_prefix_attn.cuh.
+// Launched behind the streaming kernel, which does not write anything that it reads and lets it be launched only after
+// it has itself waited for the kernels in front (queries, rotated keys): see ta_prefix_attn.cuh.
 int launch_prefix(Problem& p, const FastDecWs& w, const PrefixPlan& q) {
   const tucker_attn_desc& d = p.d;
   prefix::Params pp;
@@ -722,10 +723,11 @@ int launch_prefix(Problem& p, const FastDecWs& w, const PrefixPlan& q) {
   }
 }
 
-// Whether the join goes on to y: the output factor is then read once per sequence instead of once per 128 sequences, and a launch
-// (2 us of host time and a kernel boundary) is saved.  Whole step on the GPU, in the join against as a GEMM: d 768, t2 64: 22.1
-// against 23.0 us with one sequence, 25.7 against 27.5 with six behind a prefix; t2 96, 24 sequences (3.5 MB): 39.8 against 42.2;
-// d 4096, t2 128: 27.6 against 27.1 with 4 sequences (4 MB), 28.2 against 28.3 with 8, 32.9 against 30.3 with 16.
+// Whether the join goes on to y: the output factor is then read once per sequence instead of once per 128 sequences,
+// and a launch (2 us of host time and a kernel boundary) is saved.  Whole step on the GPU, in the join against as a
+// GEMM: d 768, t2 64: 22.1 against 23.0 us with one sequence, 25.7 against 27.5 with six behind a prefix; t2 96, 24
+// sequences (3.5 MB): 39.8 against 42.2; d 4096, t2 128: 27.6 against 27.1 with 4 sequences (4 MB), 28.2 against 28.3
+// with 8, 32.9 against 30.3 with 16.
 bool paged_out_fuses_y(const tucker_attn_desc& d) { return (size_t)d.B * d.d_model * d.t2 * sizeof(bf16) <= (size_t)4 << 20; }
 
 template <int CL>
@@ -746,7 +748,8 @@ int launch_paged_out(Problem& p, const FastDecWs& w, const PrefixPlan& q, int gr
   op.pre_o = w.pre_o; op.pre_ml = w.pre_ml; op.grid_p = q.grid; op.n_kt = q.n_kt; op.n_rb = q.n_rb;
   op.Ct = (const bf16*)p.Ct; op.Ut1 = (const bf16*)p.Ut1; op.z = w.z; op.err = p.dev_err;
   op.Ut2 = paged_out_fuses_y(d) ? (const bf16*)p.Ut2 : nullptr; op.y = (bf16*)p.Y; op.d = d.d_model;
-  // measured at 64 sequences of 32 heads, two to three partials each: 20.6 us with 8 CTAs per sequence (two waves), 13.8 us with 4
+  // measured at 64 sequences of 32 heads, two to three partials each: 20.6 us with 8 CTAs per sequence (two waves),
+  // 13.8 us with 4
   if (d.B * 8 <= 2 * sm_count()) return launch_paged_out_cl<8>(p, op);
   if (d.B * 4 <= 2 * sm_count()) return launch_paged_out_cl<4>(p, op);
   return launch_paged_out_cl<2>(p, op);
@@ -959,9 +962,9 @@ __global__ void k_wait_selftest(unsigned int* err, long long budget_cycles, int*
     out[2] = (int)((clock64() - t0) >> 10);
   }
 }
-// A cluster of two CTAs.  CTA 1 sends one number to CTA 0, but only after four times the budget that CTA 0's wait for it has: the
-// wait must give up and set the device error word, and CTA 0 must still be there when the number comes.  out[0] receives what
-// the wait returned (0 = gave up), out[1] whether the number had come when CTA 0 was about to end.
+// A cluster of two CTAs.  CTA 1 sends one number to CTA 0, but only after four times the budget that CTA 0's wait for
+// it has: the wait must give up and set the device error word, and CTA 0 must still be there when the number comes.
+// out[0] receives what the wait returned (0 = gave up), out[1] whether the number had come when CTA 0 was about to end.
 __global__ void __cluster_dims__(2, 1, 1) k_cluster_wait_selftest(unsigned int* err, long long budget_cycles, int* out) {
   __shared__ uint64_t bar;
   __shared__ float slot;

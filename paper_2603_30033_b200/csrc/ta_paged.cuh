@@ -49,9 +49,9 @@ __device__ __forceinline__ AppendDst append_dst(int t, const int32_t* __restrict
   return d;
 }
 
-// Partials of a sequence, from the first and last of `grid` CTAs that the streaming kernel has noted for it; 0 where they cannot be
-// its note.  (A streaming CTA whose wait ran out leaves without one, and the words hold whatever the workspace held: they must not
-// become an index.)
+// Partials of a sequence, from the first and last of `grid` CTAs that the streaming kernel has noted for it; 0 where
+// they cannot be its note.  (A streaming CTA whose wait ran out leaves without one, and the words hold whatever the
+// workspace held: they must not become an index.)
 __host__ __device__ inline int noted_parts(int first, int last, int grid) {
   return first >= 0 && first <= last && last < grid ? last - first + 1 : 0;
 }

@@ -1,26 +1,31 @@
-// Paged decode step for small work: one launch, a cluster of eight CTAs per sequence, everything between the token and y on chip.
+// Paged decode step for small work: one launch, a cluster of eight CTAs per sequence, everything between the token and
+// y on chip.
 //
-// A step over a short cache is a chain of dependent small products: projections of the token, queries, attention, output core,
-// output.  As launches each link costs a kernel boundary (about 2 us, and as much host time), ten times the work in it.
-// Here the links go through distributed shared memory: what a CTA computes is sent to the CTAs that need it by st.async, which counts the
-// bytes on the receiver's mbarrier, so that a link costs one way through the cluster and no fence.
+// A step over a short cache is a chain of dependent small products: projections of the token, queries, attention,
+// output core, output.  As launches each link costs a kernel boundary (about 2 us, and as much host time), ten times
+// the work in it.
+// Here the links go through distributed shared memory: what a CTA computes is sent to the CTAs that need it by
+// st.async, which counts the bytes on the receiver's mbarrier, so that a link costs one way through the cluster and no
+// fence.
 //   1  projections x [U2 | U3 | Ut3]: CTA r takes the r-th eighth of d; everybody receives the partial sums.
-//   2  v[a, :] = sum_j (x U2)_j C[a, j, :]: CTA r takes an eighth of the (a, eight columns) pairs, everybody receives them;
-//      every CTA then forms all queries q_h = scale sum_a U1[h, a] v[a, :], rotated.
-//   3  the keys of the sequence, prefix first, are split evenly over the eight CTAs: keys and values are shared by all heads, so a
-//      split over heads would read them eight times.  Rows come by cp.async; the first two tiles are requested before anything is
-//      computed, pages are looked up two tiles ahead.  Running maximum and sum per head; CTA 0 starts from the new token.
-//   4  the partial outputs' column groups of eight go to the CTAs that own them (group g: CTA g mod 8), which join the eight
-//      partials by their maxima and sums and form u[a, c] = sum_h Ut1[h, a] o_h[c] and their columns' share of
+//   2  v[a, :] = sum_j (x U2)_j C[a, j, :]: CTA r takes an eighth of the (a, eight columns) pairs, everybody receives
+//      them; every CTA then forms all queries q_h = scale sum_a U1[h, a] v[a, :], rotated.
+//   3  the keys of the sequence, prefix first, are split evenly over the eight CTAs: keys and values are shared by all
+//      heads, so a split over heads would read them eight times.  Rows come by cp.async; the first two tiles are
+//      requested before anything is computed, pages are looked up two tiles ahead.  Running maximum and sum per head;
+//      CTA 0 starts from the new token.
+//   4  the partial outputs' column groups of eight go to the CTAs that own them (group g: CTA g mod 8), which join the
+//      eight partials by their maxima and sums and form u[a, c] = sum_h Ut1[h, a] o_h[c] and their columns' share of
 //      z[j] = sum_a sum_c Ct[a, j, c] u[a, c], received by everybody.
 //   5  y = z Ut2^T: CTA r takes an eighth of the rows.
-// All arithmetic is fp32 from the stored values on (the tensor-core path carries q and z as two bf16 numbers each); only what is
-// stored is rounded.  Sums are taken in a fixed order.  The weights are read once per sequence and the scores take FMAs, so that this form
-// is for small batches of short contexts only: see cluster_step_pays.
+// All arithmetic is fp32 from the stored values on (the tensor-core path carries q and z as two bf16 numbers each);
+// only what is stored is rounded.  Sums are taken in a fixed order.  The weights are read once per sequence and the
+// scores take FMAs, so that this form is for small batches of short contexts only: see cluster_step_pays.
 //
-// Bounded by latency: d 768, 12 heads, ranks 64, one sequence of 37 tokens 11.2 us (19.3 as four launches), of which 1.4 wait for the
-// first loads and 0.6 to 1.5 go to each later phase; a tile of 64 keys per CTA 1.3 us (scores and values are issue and shared-memory
-// bound).  Exchanges by cluster barrier and remote reads, with less of the rest overlapped, were 16.3 us.
+// Bounded by latency: d 768, 12 heads, ranks 64, one sequence of 37 tokens 11.2 us (19.3 as four launches), of which
+// 1.4 wait for the first loads and 0.6 to 1.5 go to each later phase; a tile of 64 keys per CTA 1.3 us (scores and
+// values are issue and shared-memory bound).  Exchanges by cluster barrier and remote reads, with less of the rest
+// overlapped, were 16.3 us.
 #include "ta_paged.cuh"
 #include "ta_cluster.cuh"
 
@@ -36,8 +41,9 @@ constexpr int TK = 64;                                 // keys per tile
 constexpr int TPR = THREADS / TK;                      // threads that copy a row
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Division by a number that the launch fixes, for dividends below 2^20: (x + 1/2) / d is at least 1 / (2 d) from a whole number and
-// computed to x / d * 2^-22.  An integer division is some 150 cycles of latency, and a step has a dozen between its links.
+// Division by a number that the launch fixes, for dividends below 2^20: (x + 1/2) / d is at least 1 / (2 d) from a
+// whole number and computed to x / d * 2^-22.  An integer division is some 150 cycles of latency, and a step has a
+// dozen between its links.
 struct Div {
   int d;
   float inv;
@@ -358,7 +364,8 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
         for (int i = 0; i < 8; ++i) acc[i] = fmaf(xv, ff[i], acc[i]);
       }
     }
-    // sums over the lanes, halving the columns a lane holds as long as it holds more than one: column = bits 4, 3, 2 of the lane
+    // sums over the lanes, halving the columns a lane holds as long as it holds more than one: column = bits 4, 3, 2 of
+    // the lane
 #pragma unroll
     for (int st = 0; st < 3; ++st) {
       const int keep = 4 >> st, bit = 16 >> st;
@@ -512,7 +519,8 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
   }
   cp_wait<0>();
   __syncthreads();
-  // Key subsets joined through the ring's memory; the sums go to the owners of their columns, maxima and sums to everybody.
+  // Key subsets joined through the ring's memory; the sums go to the owners of their columns, maxima and sums to
+  // everybody.
   {
     float* const red = at(lay.ring);
     if (ks < KS) {
@@ -606,7 +614,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
       }
     if (za < SA) part[za * t2 + zj] = zacc;
   }
-  // ---- 5: y.  Lane = (row of rpw, eight columns of the factor's row); the first rows are requested before z is there ----
+  // ---- 5: y.  Lane = (row of rpw, eight columns of the factor's row); the first rows are requested before z is there
   const int nc = p.nc.d, rpw = p.rpw, sub = p.nc(lane), cz = lane - sub * nc;
   constexpr int YU = 4;
   const int y_step = WARPS * rpw, y0 = k_beg + warp * rpw + sub;      // rows [k_beg, k_end), y_step of them at a time
@@ -675,8 +683,8 @@ int smem_bytes(const tucker_attn_desc& d, bool one_pool) {
 }
 constexpr int kMaxSmem = 225 * 1024;
 
-// Clusters of this kernel that the current device runs at once (one CTA per SM: 15 on B200, whose GPCs are not all multiples of eight
-// SMs), asked once per device; 0: the runtime cannot tell.
+// Clusters of this kernel that the current device runs at once (one CTA per SM: 15 on B200, whose GPCs are not all
+// multiples of eight SMs), asked once per device; 0: the runtime cannot tell.
 template <typename T>
 int clusters_at_once() {
   static std::mutex mu;
@@ -734,13 +742,15 @@ bool cluster_step_supported(const tucker_attn_desc& d, bool one_pool) {
   return (d.dtype == TA_DTYPE_F32 ? pgc::smem_bytes<float>(d, one_pool) : pgc::smem_bytes<bf16>(d, one_pool)) <= pgc::kMaxSmem;
 }
 
-// Whether this form is the faster one, by the longest sequence the table can hold.  All in us, fitted to the device time of whole steps
-// over d 768 to 4096, 8 to 32 heads, ranks 64 to 128 and 1 to 36 sequences (w = heads * (r3 + t3)):
-//   here          10 + 3.2 (bf16) or 2.3 (fp32) per MB of weights + (2.9 + w / 940) per 1024 keys, for every wave of clusters
+// Whether this form is the faster one, by the longest sequence the table can hold.  All in us, fitted to the device
+// time of whole steps over d 768 to 4096, 8 to 32 heads, ranks 64 to 128 and 1 to 36 sequences (w = heads * (r3 + t3)):
+//   here          10 + 3.2 (bf16) or 2.3 (fp32) per MB of weights + (2.9 + w / 940) per 1024 keys, for every wave of
+//                 clusters
 //   tensor cores  20.5 + 1.6 per MB of weights, hardly more with keys and sequences as far as the rule reaches
 //   generic       30 + 1.6 per MB of weights + 0.8 per 1000 keys of all sequences and 1536 of w
-// E.g. d 768, 12 heads, ranks 64, here / there: bf16, 1 sequence of 64 keys 11.6 / 19.9, 1024 14.1 / 19.5, 3000 22.7 / 19.6; 15 of 2048
-// 19.0 / 27.6; 16 (a second wave) of 1024 27.6 / 23.6; fp32, 1 of 64 12.2 / 31.4, 4 of 2048 19.8 / 41.2, 36 of 8192 146 / 505.
+// E.g. d 768, 12 heads, ranks 64, here / there: bf16, 1 sequence of 64 keys 11.6 / 19.9, 1024 14.1 / 19.5, 3000 22.7 /
+// 19.6; 15 of 2048 19.0 / 27.6; 16 (a second wave) of 1024 27.6 / 23.6; fp32, 1 of 64 12.2 / 31.4, 4 of 2048 19.8 /
+// 41.2, 36 of 8192 146 / 505.
 // d 4096, 32 heads, ranks 128, 4 of 64 keys 25.2 / 27.2, of 1024 33.0 / 27.7.
 bool cluster_step_pays(const tucker_attn_desc& d, int64_t slots, int32_t prefix_len, bool tensor_cores) {
   const bool f32 = d.dtype == TA_DTYPE_F32;

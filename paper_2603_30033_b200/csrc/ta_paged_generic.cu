@@ -17,10 +17,10 @@ using fma::ld;
 using fma::st;
 
 // ---------------------------------------------------------------------------------------
-// 32 x 32 tile of A [M, K] B [K, N], fp32 accumulation.  512 threads: eight groups of 64 threads take an eighth of every
-// 128-deep K block each (4 x 4 outputs per thread) and are summed through shared memory at the end, so that the short
-// and narrow products of a decode step (few rows, K = d) have eight times the threads a plain tile would and a round trip
-// to memory covers 128 of K.  The next K block is in registers while the current one is multiplied.
+// 32 x 32 tile of A [M, K] B [K, N], fp32 accumulation.  512 threads: eight groups of 64 threads take an eighth of
+// every 128-deep K block each (4 x 4 outputs per thread) and are summed through shared memory at the end, so that the
+// short and narrow products of a decode step (few rows, K = d) have eight times the threads a plain tile would and a
+// round trip to memory covers 128 of K.  The next K block is in registers while the current one is multiplied.
 // ---------------------------------------------------------------------------------------
 constexpr int GM = 32, GN = 32, GK = 128, GG = 8, GT = 64 * GG;
 
@@ -35,7 +35,8 @@ struct MatB {              // element (k, n) at k * sk + n * sn
   long sk, sn;
 };
 
-// K blocks [k_beg, K).  On return s.part[0] holds the tile (rows and columns past the edge are zero); all threads are synchronised.
+// K blocks [k_beg, K).  On return s.part[0] holds the tile (rows and columns past the edge are zero); all threads are
+// synchronised.
 template <typename TA, typename TB>
 __device__ __forceinline__ void gemm_tile(const TA* __restrict__ A, long lda, const TB* __restrict__ Bm, MatB sb, int M, int N, int k_beg,
                                           int K, int m0, int n0, TileSmem& s) {
@@ -90,8 +91,8 @@ __device__ __forceinline__ void gemm_tile(const TA* __restrict__ A, long lda, co
   __syncthreads();
 }
 
-// C [M, N] (ld ldc) = A B for up to three (B, C) pairs that share A and K: blockIdx.z = share of K * pairs + pair.  The shares'
-// products lie `split` elements apart and are added up by whoever reads them.
+// C [M, N] (ld ldc) = A B for up to three (B, C) pairs that share A and K: blockIdx.z = share of K * pairs + pair.  The
+// shares' products lie `split` elements apart and are added up by whoever reads them.
 template <typename TB, typename TC>
 struct GemmPart {
   const TB* B;
@@ -186,8 +187,8 @@ __global__ void __launch_bounds__(GT) k_pg_append(const AppendArgs<T> g) {
   }
 }
 
-// w[a, b, c] = sum_q qt[b, q] C[a, q, c].  A block forms 32 columns of one slice for four sequences: thread (c, g) of 32 x 8 walks
-// the rows q = g, g + 8, ..., the eight sums per column are joined through shared memory.
+// w[a, b, c] = sum_q qt[b, q] C[a, q, c].  A block forms 32 columns of one slice for four sequences: thread (c, g) of
+// 32 x 8 walks the rows q = g, g + 8, ..., the eight sums per column are joined through shared memory.
 constexpr int WB = 4;
 template <typename T>
 __global__ void __launch_bounds__(256) k_pg_w(const float* __restrict__ qt_parts, int shares, const T* __restrict__ C,
@@ -474,8 +475,8 @@ __global__ void __launch_bounds__(256) k_pg_attn(const AttnArgs<T> g) {
 }
 
 // ---------------------------------------------------------------------------------------
-// o[b, h] from the partials of its own keys (splits_o) and of the prefix (splits_p, may be 0).  A block per (b, h); the partials are
-// dealt over its eight warps, whose sums are joined in order.
+// o[b, h] from the partials of its own keys (splits_o) and of the prefix (splits_p, may be 0).  A block per (b, h); the
+// partials are dealt over its eight warps, whose sums are joined in order.
 // ---------------------------------------------------------------------------------------
 constexpr int kMaxSplits = 128;       // of either kind, see pick_splits
 __global__ void __launch_bounds__(256) k_pg_merge(const float* __restrict__ po, const float* __restrict__ ml, int splits_o,
@@ -532,7 +533,8 @@ __global__ void __launch_bounds__(256) k_pg_merge(const float* __restrict__ po, 
   }
 }
 
-// Output-side core: u[b, a, c] = sum_h Ut1[h, a] o[b, h, c];  z[b, j] = sum_a sum_c Ct[a, j, c] u[b, a, c] (a warp per j).
+// Output-side core: u[b, a, c] = sum_h Ut1[h, a] o[b, h, c];  z[b, j] = sum_a sum_c Ct[a, j, c] u[b, a, c] (a warp per
+// j).
 template <typename T>
 __global__ void __launch_bounds__(256) k_pg_u(const float* __restrict__ o, const T* __restrict__ Ut1, float* __restrict__ u, int B,
                                               int nH, int t1, int t3) {
@@ -572,15 +574,19 @@ bool shape_ok(const tucker_attn_desc& d) {
          WB * (size_t)d.r2 * sizeof(float) <= kMaxQuerySmem;
 }
 
+// SMs that the shares are laid out for: B200's, whatever device is current, so that a workspace query does not depend on
+// it.
+constexpr int kSms = 148;
 // Shares per list of keys: about two blocks per SM, no more than there are tiles.
 int pick_splits(long blocks, long keys) {
   const long tiles = (keys + AK - 1) / AK;
-  return (int)std::max<long>(1, std::min<long>(std::min<long>(tiles, kMaxSplits), (2 * 148 + blocks - 1) / blocks));
+  return (int)std::max<long>(1, std::min<long>(std::min<long>(tiles, kMaxSplits), (2 * kSms + blocks - 1) / blocks));
 }
 int own_splits(const tucker_attn_desc& d, int64_t Lmax) { return pick_splits((long)d.B * ((d.n_H + AR - 1) / AR), Lmax); }
 int prefix_splits(const tucker_attn_desc& d, int32_t P) { return P > 0 ? pick_splits(((long)d.B * d.n_H + AR - 1) / AR, P) : 0; }
 
-// Shares of K = d of the new tokens' projections: one 128-deep block each while few tiles would otherwise be all there is.
+// Shares of K = d of the new tokens' projections: one 128-deep block each while few tiles would otherwise be all there
+// is.
 int proj_shares(const tucker_attn_desc& d) {
   const int kb = (d.d_model + GK - 1) / GK;
   return d.B <= 4 * GM ? std::min(kb, 8) : 1;
@@ -653,7 +659,7 @@ int decode_typed(Problem& p) {
   (void)launch_pdl(k_pg_w<T>, dim3((d.B + WB - 1) / WB, d.r1, (d.r3 + 31) / 32), dim3(256), WB * d.r2 * sizeof(float), p.stream, w.qt_parts,
                    shares, (const T*)p.C, w.w, d.B, d.r1, d.r2, d.r3);
   TA_LAUNCH_CHECK(p);
-  (void)launch_pdl(k_pg_queries<T>, dim3(d.B, std::max(1, std::min(8, 296 / d.B))), dim3(256), 0, p.stream, w.w, (const T*)p.U1, w.qhat,
+  (void)launch_pdl(k_pg_queries<T>, dim3(d.B, std::max(1, std::min(8, 2 * kSms / d.B))), dim3(256), 0, p.stream, w.w, (const T*)p.U1, w.qhat,
                    w.k_parts, w.v_parts, shares, w.knew, w.vnew, (T*)p.Kc, (T*)p.Vc, p.pv, p.cache_len, d.B, d.n_H, d.r1, d.r3, d.t3, p.Lmax,
                    P, p.scale, d.rope, (double)d.rope_base, rope_freqs(d), p.append, p.shared_kv, p.shared_rope, p.dev_err);
   TA_LAUNCH_CHECK(p);
@@ -675,7 +681,7 @@ int decode_typed(Problem& p) {
   const int rows = d.B * d.n_H;
   (void)launch_pdl(k_pg_merge, dim3(rows), dim3(256), 0, p.stream, w.po, w.ml, own_splits(d, p.Lmax), w.po_p, w.ml_p, sp, w.o, d.t3);
   TA_LAUNCH_CHECK(p);
-  (void)launch_pdl(k_pg_u<T>, dim3((unsigned)std::min<long>(148 * 8, ((long)d.B * d.t1 * d.t3 + 255) / 256)), dim3(256), 0, p.stream, w.o,
+  (void)launch_pdl(k_pg_u<T>, dim3((unsigned)std::min<long>(kSms * 8, ((long)d.B * d.t1 * d.t3 + 255) / 256)), dim3(256), 0, p.stream, w.o,
                    (const T*)p.Ut1, w.u, d.B, d.n_H, d.t1, d.t3);
   TA_LAUNCH_CHECK(p);
   (void)launch_pdl(k_pg_z<T>, dim3((d.t2 + 7) / 8, d.B), dim3(256), 0, p.stream, w.u, (const T*)p.Ct, w.z, d.t1, d.t2, d.t3);

@@ -1,14 +1,15 @@
-// Output side of the paged decode step: joins the partials of a sequence -- those of its own keys (streaming kernel) and of
-// the shared prefix (prefix kernel) -- by their maxima and sums and applies the output-side core:
+// Output side of the paged decode step: joins the partials of a sequence -- those of its own keys (streaming kernel)
+// and of the shared prefix (prefix kernel) -- by their maxima and sums and applies the output-side core:
 //   o_h = merged, normalised output of head h;  u[a, :] = sum_h Ut1[h, a] o_h;  z[j] = sum_a sum_c Ct[a, j, c] u[a, c]
-// A cluster of CL CTAs per sequence (8, 4 or 2: the most that still lets all of them run at once, two CTAs per SM).  CTA y merges t3 / CL value columns of all heads (every partial is read once per
-// sequence, where CTAs that split the rows of z would each have to merge everything), forms its columns of u, hands them to the
-// other CTAs through distributed shared memory, and computes t2 / CL rows of z.  For small batches (paged_out_fuses_y) it
-// goes on to y = z Ut2^T: z is handed round the cluster and every CTA computes d / CL outputs, each sequence reading the factor
-// again, which a launch and its boundary outweigh as long as there are few.  One user with a long cache has a partial
-// from every SM: the maxima, weights and sums of the partials are spread over all warps instead of walked by one.
-// The kernels before it fill their SMs, so that next to nothing of this one overlaps them: it takes the CTAs that hold a sequence
-// from the streaming kernel instead of scanning the lengths.
+// A cluster of CL CTAs per sequence (8, 4 or 2: the most that still lets all of them run at once, two CTAs per SM).
+// CTA y merges t3 / CL value columns of all heads (every partial is read once per sequence, where CTAs that split the
+// rows of z would each have to merge everything), forms its columns of u, hands them to the other CTAs through
+// distributed shared memory, and computes t2 / CL rows of z.  For small batches (paged_out_fuses_y) it goes on to y = z
+// Ut2^T: z is handed round the cluster and every CTA computes d / CL outputs, each sequence reading the factor again,
+// which a launch and its boundary outweigh as long as there are few.  One user with a long cache has a partial from
+// every SM: the maxima, weights and sums of the partials are spread over all warps instead of walked by one.
+// The kernels before it fill their SMs, so that next to nothing of this one overlaps them: it takes the CTAs that hold
+// a sequence from the streaming kernel instead of scanning the lengths.
 #pragma once
 
 #include "ta_cluster.cuh"
@@ -75,7 +76,8 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
     return (jl < jn && ga < rpl && a < p.t1) ? Cq[((long)a * p.t2 + jbeg + jl) * nch + ch] : make_uint4(0u, 0u, 0u, 0u);
   };
   {
-    // this CTA's rows of the core towards L2 (a long cache streamed through it has pushed them out) while the partials are merged
+    // this CTA's rows of the core towards L2 (a long cache streamed through it has pushed them out) while the partials
+    // are merged
     const char* rows = reinterpret_cast<const char*>(p.Ct) + (long)jbeg * t3 * 2;
     const int lines = (jn * t3 * 2 + 127) / 128;
     for (int a = warp; a < p.t1; a += WARPS)
@@ -83,7 +85,8 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
         asm volatile("prefetch.global.L2 [%0];" ::"l"(rows + (long)a * p.t2 * t3 * 2 + i * 128));
   }
   for (int i = tid; i < p.nH * p.t1; i += THREADS) ut1_s[i] = __bfloat162float(p.Ut1[i]);
-  // The prefix's partials of head h (rows of a sequence may lie in two row blocks): first slot, number, row in the block.
+  // The prefix's partials of head h (rows of a sequence may lie in two row blocks): first slot, number, row in the
+  // block.
   __shared__ int ps0_s[32], pc_s[32];
   if (warp == 0) {
     int slot0 = 0, cnt = 0;
@@ -140,7 +143,8 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 2) k_pg_ou
     hl_s[warp][h] = l;
   }
   __syncthreads();
-  // ---- merge: item = (four columns, head), heads adjacent (512 bytes per load of 32 heads); partials dealt over groups of threads ----
+  // ---- merge: item = (four columns, head), heads adjacent (512 bytes per load of 32 heads) ----
+  // (partials dealt over groups of threads)
   const int items = p.nH * q4, groups = min(16, THREADS / items);
   {
     const int g = tid / items, it = tid % items, h = it % p.nH, c = c0 + it / p.nH * 4;

@@ -86,8 +86,8 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, const 
   }
 }
 
-// For a producer that leaves because the CTA aborted: waits, ignoring the abort flag but no longer than about a millisecond, for a
-// copy that is still in flight, so that nothing writes the CTA's shared memory after it has gone.
+// For a producer that leaves because the CTA aborted: waits, ignoring the abort flag but no longer than about a
+// millisecond, for a copy that is still in flight, so that nothing writes the CTA's shared memory after it has gone.
 __device__ __forceinline__ void mbar_drain(uint64_t* bar, uint32_t parity) {
   const long long t0 = clock64();
   while (!mbar_try_wait(bar, parity) && clock64() - t0 < 2000000LL) {}
