@@ -43,14 +43,14 @@ L2_BYTES = 126 * 1024 * 1024
 # workload: value, the summary under profiles/ it comes from, and the SHA-256 of the kernel's source file at the
 # time of the capture.  A value is only reported while that file is unchanged (see ncu_traffic()).
 _ATTN = {"source": "ta_attn_prefill.cuh", "sha256": "83abe4f00b82ea24232967bb6792cee9c2eed58417272c517f4f348ff22e88c6"}
-_DEC = {"source": "ta_decode_umma.cuh", "sha256": "b29368639f2d9ea4a252a55117459bd2a1a167eff6dc63668ccc285447534b03"}
+_DEC = {"source": "ta_decode_umma.cuh", "sha256": "ac2d28fdc1b9e5b31d1f7a3a7edfd5150117f576b631404fd4b7f83ef1108023"}
 NCU_TRAFFIC = {
     "c4_long_prefill": {"bytes": 17971968 + 77637120, "profile": "profiles/k_attn_prefill_c4_long_prefill.md", **_ATTN},
     "c3_vit_prefill": {"bytes": 33884416 + 64199424, "profile": "profiles/k_attn_prefill_c3_vit_prefill.md", **_ATTN},
     "c2_gpt2_prefill": {"bytes": 3584256 + 0, "profile": "profiles/k_attn_prefill_c2_gpt2_prefill.md", **_ATTN},
-    "c5_decode": {"bytes": 1075363072 + 4196608, "profile": "profiles/k_dec_attn_umma_c5_decode.md", **_DEC},
-    "f1_decode_shared_kv": {"bytes": 537998592 + 4850688, "profile": "profiles/k_dec_attn_umma_f1_decode_shared_kv.md", **_DEC},
-    "f1r_decode_shared_kv_rope": {"bytes": 538054400 + 6371328,
+    "c5_decode": {"bytes": 1075300352 + 4221184, "profile": "profiles/k_dec_attn_umma_c5_decode.md", **_DEC},
+    "f1_decode_shared_kv": {"bytes": 538080256 + 4227328, "profile": "profiles/k_dec_attn_umma_f1_decode_shared_kv.md", **_DEC},
+    "f1r_decode_shared_kv_rope": {"bytes": 538077184 + 4449536,
                                   "profile": "profiles/k_dec_attn_umma_f1r_decode_shared_kv_rope.md", **_DEC},
 }
 NOMINAL_PEAKS = {"hbm_gbs": 8000.0, "bf16_tflops": 2250.0}     # the figures the targets are quoted against

@@ -33,10 +33,11 @@ constexpr int MAX_STAGES = 8;
 constexpr int RING_BYTES = 192 * 1024;
 constexpr size_t SMEM_BYTES = 1024 + (size_t)RING_BYTES;
 constexpr int A_BYTES = BM * BK * 2, BOX_BYTES = 64 * BK * 2, UNIT_BYTES = UC * BM * 4;
-// A finished unit's rounded rows wait in the idle ring for their stores: one place per half of the epilogue warps,
-// however many units a CTA finishes (up to 16).
-constexpr int STAGED_BYTES = UC * BM * 2;
-static_assert(2 * STAGED_BYTES <= RING_BYTES, "both halves' staged units fit into the ring");
+// A finished unit's rounded rows wait for their stores in the idle ring, a place per unit: places used again would have
+// to wait for the stores (64 single tokens 11.5 -> 12.7 us on the GPU).  A CTA finishes 16 units at most, 512 columns of
+// TMEM.
+constexpr int MAX_UNITS = 512 / UC, STAGED_BYTES = UC * BM * 2;
+static_assert(MAX_UNITS * STAGED_BYTES <= RING_BYTES, "all units of a CTA fit into the ring");
 constexpr int MAX_S = 8;
 constexpr int CSU = 2;                           // units per thread whose angles are formed ahead
 
@@ -189,10 +190,10 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
   };
   // rows of this warp that exist: none of the others' sums are needed
   auto warp_rows = [&](int u) -> bool { return m0 + (u / upt) * BM + q * 32 < p.T; };
-  // 16-byte chunk `ch` of row `row` of the unit that this half has staged: a warp's rows of one chunk are adjacent, and
-  // the four chunks of one row lie on different banks.  A row belongs to one warp, which alone writes and reads it.
-  auto chunk_at = [&](int row, int ch) -> uint32_t {
-    return (uint32_t)(hf * STAGED_BYTES + ch * (BM * 16) + ((row ^ ch) << 4));
+  // 16-byte chunk `ch` of row `row` of a staged unit: a warp's rows of one chunk are adjacent, and the four chunks of one
+  // row lie on different banks
+  auto chunk_at = [&](int slot, int row, int ch) -> uint32_t {
+    return (uint32_t)(slot * STAGED_BYTES + ch * (BM * 16) + ((row ^ ch) << 4));
   };
   // this cluster's partial sums, [share][unit][chunk][row] of 16 bytes
   float4* const part = reinterpret_cast<float4*>(p.part_sums) + ((long)blockIdx.y * (gridDim.x / S) * p.y_units + (long)(blockIdx.x / S) * units) * S * (UNIT_BYTES / 16);
@@ -258,7 +259,7 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
       // the rounded row into this thread's own place in the idle ring ...
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        *reinterpret_cast<uint4*>(ring + chunk_at(rloc, e)) =
+        *reinterpret_cast<uint4*>(ring + chunk_at(u - u0, rloc, e)) =
             make_uint4(pack_bf16(v[8 * e], v[8 * e + 1]), pack_bf16(v[8 * e + 2], v[8 * e + 3]), pack_bf16(v[8 * e + 4], v[8 * e + 5]),
                        pack_bf16(v[8 * e + 6], v[8 * e + 7]));
       __syncwarp();
@@ -269,11 +270,10 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
       for (int i = 0; i < 4; ++i) {
         const int rr = i * 8 + lane / 4;
         const long row = __shfl_sync(0xffffffffu, to.row, rr);
-        const uint4 w = *reinterpret_cast<const uint4*>(ring + chunk_at(q * 32 + rr, lane & 3));
+        const uint4 w = *reinterpret_cast<const uint4*>(ring + chunk_at(u - u0, q * 32 + rr, lane & 3));
         if (row >= 0 && TA_IDX_OK(p.err, row * wd + cc, 8, (long)p.pv.n_pages * p.pv.page_size * wd))
           *reinterpret_cast<uint4*>(pool + row * wd + cc) = w;
       }
-      __syncwarp();                               // read by all lanes before the next unit's rows take the place
     };
 #pragma unroll
     for (int k = 0; k < CSU; ++k) {

@@ -38,3 +38,32 @@ int main() {
 }
 """)
     assert out == ""
+
+
+def test_a_block_of_the_append_never_stages_more_units_than_there_is_room_for(tmp_path):
+    """Every division of a call that the plan can choose, over widths, d, T and numbers of SMs: the units that one CTA finishes."""
+    out = run_host_program(tmp_path, r"""
+#include "ta_append_umma.cuh"
+#include <cstdio>
+using namespace ta::append;
+int main() {
+  int most = 0;
+  for (int sms : {1, 16, 132, 148, 160})
+    for (int w0 = 32; w0 <= 256; w0 += 32)
+      for (int w1 = 0; w1 <= 256; w1 += 32)
+        for (int d : {64, 128, 768, 1024, 4096, 16384})
+          for (int T = 1; T < 200000; T = T < 1000 ? T + 37 : T + T / 23) {
+            const Plan q = append_plan(T, d, w0, w1, sms);
+            for (int part = 0; part < (q.split_parts ? 2 : 1); ++part) {
+              const int width = q.split_parts ? (part ? w1 : w0) : w0 + w1, units = q.MT * width / UC;
+              for (int s = 0; s < q.S; ++s) {
+                const int mine = units * (s + 1) / q.S - units * s / q.S;
+                if (mine > MAX_UNITS || mine * STAGED_BYTES > RING_BYTES) { printf("T %d d %d %d/%d: %d units\n", T, d, w0, w1, mine); return 1; }
+                most = mine > most ? mine : most;
+              }
+            }
+          }
+  return most == MAX_UNITS ? 0 : 2;
+}
+""")
+    assert out == ""
