@@ -301,3 +301,55 @@ def test_step_in_one_launch_large_scores_against_the_oracle(dtype, gain, monkeyp
         err = np.linalg.norm(got - ref, axis=-1) / np.linalg.norm(ref, axis=-1)
         print(f"{dtype} gain {gain} |q||k| {size:.0f} errors {err}")
         assert (err <= 8e-6 * size + 1e-5 + (P.U_BF16 if dtype == "bf16" else 0.0)).all(), (size, err)
+
+
+# ---- arguments and uses that the other tests leave out -------------------------------------------------------------------
+
+@pytest.mark.parametrize("room", [0, 32768])
+@pytest.mark.parametrize("flags", [0, Bd.TA_FLAG_FORCE_GENERIC])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_explicit_scale(dtype, flags, room, monkeypatch):
+    """Four times the default scale gives, bit for bit, what a core of four times the size gives: a power of two passes through
+    every rounding unchanged."""
+    import torch
+    from tests import helpers as H
+    monkeypatch.setattr(P, "ROOM", room)
+    w = H.custom_workload(kind="decode", dtype=dtype, rope=True, rope_base=500000.0, seed=5, d_model=256, n_H=4, r=(4, 64, 64), t=(4, 64, 64))
+    st = P.PagedState(w, [300, 3, 0], 16, P=200, core_gain=0.5)
+    x, dw, K, V, table, n, ptab = st.device()
+    kw = dict(n_H=4, rope=True, rope_base=w.rope_base, append=False, flags=flags)
+    a = Bd.tucker_attn_decode_prefix(x, *dw, K, V, table, n, ptab, 200, scale=4 * (256 / 4) ** -0.5, **kw)
+    b = Bd.tucker_attn_decode_prefix(x, dw[0] * 4, *dw[1:], K, V, table, n, ptab, 200, **kw)
+    c = Bd.tucker_attn_decode_prefix(x, *dw, K, V, table, n, ptab, 200, **kw)
+    assert Bd.last_device_error() == 0 and torch.equal(a, b) and not torch.equal(a, c)
+
+
+@pytest.mark.parametrize("pools", ["two", "one"])
+def test_captured_prefix_step_replays_while_another_graph_runs(pools):
+    """Two graphs of the same step on different states, each with its own workspace, replayed on two streams at once: what the calls give
+    alone, bit for bit."""
+    import torch
+    r, t = RANKS["128"]
+    sts = [LongState(512, 16, r, t, [90, 0, 1500, 7, 300], 64, P=3001, one_pool=pools == "one", seed=k) for k in (3, 4)]
+    step = lambda s, K, V, y: Bd.tucker_attn_decode_prefix(s.x, *s.w, K, V, s.table, s.len, s.ptab, s.P, n_H=s.h, rope=True, rope_base=s.base, out=y)
+    alone, graphs, out = [], [], []
+    for s in sts:
+        K = s.K.clone()
+        alone.append((step(s, K, K if s.one_pool else s.V.clone(), torch.empty_like(s.x)), K))
+    torch.cuda.synchronize()
+    for s in sts:
+        g, K, y = torch.cuda.CUDAGraph(), s.K.clone(), torch.empty_like(s.x)
+        V = K if s.one_pool else s.V.clone()
+        with torch.cuda.graph(g):
+            step(s, K, V, y)
+        graphs.append(g)
+        out.append((y, K))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(10):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    assert Bd.last_device_error() == 0
+    for (y0, k0), (y1, k1) in zip(alone, out):
+        assert torch.equal(y0, y1) and torch.equal(k0.view(torch.int16), k1.view(torch.int16))
