@@ -275,6 +275,76 @@ TA_API int tucker_attn_decode_prefix(const tucker_attn_desc* desc, const void* x
                               void* y, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
+ * Paged latent cache held in 8 bits (the paged calls above, at half the bytes per cached token).
+ *
+ * A row v of r numbers (a token's latent key or value) is held as r e4m3 codes and one scale, a power of two:
+ *   a = max |v|;  k = the least integer, but no less than -96, with a <= 448 * 2^k (a row of zeros: k = 0)
+ *   code_j = v_j 2^-k rounded to the nearest e4m3 number, ties to even;  scale byte = k + 127 (0 .. 254: 2^(byte - 127))
+ * and stands for code_j 2^k.  A code has four significant bits: each number is off by at most 2^-4 of itself (or 2^-10 of
+ * 2^k where it is smaller than 2^-6 2^k), 2.6 % in the mean square.  A row with a number that is not finite has the scale
+ * byte 255 and the codes 0x7f, and reads back as NaN.  The latent cache has one key row and one value row per token, whatever
+ * the number of heads, so this is a scale for every token of either; it never changes once its row is written.
+ *
+ * Pools, tables, lengths and limits are those of the paged calls above; a needed table entry out of range reads as rows of
+ * zeros and is not written through.  V == K (with Vs == Ks) is the shared projection: one pool, which holds un-rotated rows
+ * when rope is set.  `dtype` is the type of everything else.  The decode shapes that run on tensor cores do so here too.
+ * A row is rounded once, from the fp32 result of its projection.  A decode step's new token takes part in its own attention
+ * with the rows that the cache stores for it, whether it appends them or not.
+ */
+typedef struct {
+  void* K;                    /* [n_pages, page_size, r3] e4m3 codes  device */
+  void* V;                    /* [n_pages, page_size, t3] e4m3 codes  device; == K: one shared latent pool */
+  void* Ks;                   /* [n_pages, page_size] scale bytes  device */
+  void* Vs;                   /* [n_pages, page_size] scale bytes  device; == Ks exactly when V == K */
+  const int32_t* block_table; /* [B, max_pages]  device */
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t max_pages;
+} tucker_paged_cache_q8;
+
+/* tucker_cache_append_paged into an 8-bit cache: arguments as there. */
+TA_API size_t tucker_cache_append_paged_q8_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache_q8* cache, int32_t T);
+TA_API int tucker_cache_append_paged_q8(const tucker_attn_desc* desc, const void* X, const void* U3, const void* Ut3,
+                              const tucker_paged_cache_q8* cache, const int32_t* cache_len, const int32_t* tok_start, int32_t T,
+                              void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Latent rows that exist already, quantised into the pages: Krows [T, r3], Vrows [T, t3] as the cache is to hold them (keys
+ * rotated, except with one pool), such as Kcache_out / Vcache_out of tucker_attn_fwd with Lmax = N.  tok_start, cache_len and
+ * the slots that rows go to are those of tucker_cache_append_paged.  With one pool Vrows == Krows.  Used of desc: B, r3, t3,
+ * dtype (the rows' type); the other fields must be valid.  No workspace.  T = 0 is allowed.
+ */
+TA_API int tucker_cache_store_paged_q8(const tucker_attn_desc* desc, const void* Krows, const void* Vrows,
+                              const tucker_paged_cache_q8* cache, const int32_t* cache_len, const int32_t* tok_start, int32_t T,
+                              void* cuda_stream);
+
+/*
+ * Cached rows read back, the inverse of the store: row tok_start[b] + i of Krows and Vrows receives slot slot_start[b] + i of
+ * sequence b, for the tok_start[b + 1] - tok_start[b] rows of each.  Exact in either type (bf16 down to numbers of 2^-133).
+ * Rows outside [tok_start[0], tok_start[B]) are left as they are, as are the rows of slots that the table has no room for
+ * (TA_DEVERR_BAD_CACHE_LEN); a page number out of range gives rows of zeros (TA_DEVERR_BAD_PAGE).  What lies in a slot is read
+ * whether or not it was ever written.  With one pool Vrows == Krows.  desc as for the store.
+ */
+TA_API int tucker_cache_read_paged_q8(const tucker_attn_desc* desc, const tucker_paged_cache_q8* cache, const int32_t* slot_start,
+                             const int32_t* tok_start, int32_t T, void* Krows, void* Vrows, void* cuda_stream);
+
+/* tucker_attn_decode_paged and tucker_attn_decode_prefix over an 8-bit cache: arguments as there. */
+TA_API size_t tucker_attn_decode_paged_q8_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache_q8* cache);
+TA_API int tucker_attn_decode_paged_q8(const tucker_attn_desc* desc, const void* x,
+                             const void* C, const void* U1, const void* U2, const void* U3,
+                             const void* Ct, const void* Ut1, const void* Ut2, const void* Ut3,
+                             const tucker_paged_cache_q8* cache, const int32_t* cache_len, int32_t append,
+                             void* y, void* workspace, size_t workspace_bytes, void* cuda_stream);
+TA_API size_t tucker_attn_decode_prefix_q8_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache_q8* cache,
+                                                 int32_t prefix_len);
+TA_API int tucker_attn_decode_prefix_q8(const tucker_attn_desc* desc, const void* x,
+                              const void* C, const void* U1, const void* U2, const void* U3,
+                              const void* Ct, const void* Ut1, const void* Ut2, const void* Ut3,
+                              const tucker_paged_cache_q8* cache, const int32_t* cache_len,
+                              const int32_t* prefix_table, int32_t prefix_len, int32_t append,
+                              void* y, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Weight packers: the paper's special cases as Tucker attention (Sec. 2.2; Lemma 1 and
  * Theorems 1-3 and their proofs).  They write the two cores and six factors that
  * tucker_attn_fwd / tucker_attn_decode take, so that MHA, GQA / MQA and MLA weights run

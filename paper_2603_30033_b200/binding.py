@@ -33,6 +33,9 @@ EXPORTS = (
     "tucker_attn_bounds_checked", "tucker_attn_selftest_cluster_wait",
     "tucker_cache_append_paged", "tucker_cache_append_paged_workspace_bytes", "tucker_attn_decode_paged", "tucker_attn_decode_paged_workspace_bytes",
     "tucker_attn_decode_prefix", "tucker_attn_decode_prefix_workspace_bytes",
+    "tucker_cache_append_paged_q8", "tucker_cache_append_paged_q8_workspace_bytes", "tucker_cache_store_paged_q8",
+    "tucker_cache_read_paged_q8", "tucker_attn_decode_paged_q8", "tucker_attn_decode_paged_q8_workspace_bytes",
+    "tucker_attn_decode_prefix_q8", "tucker_attn_decode_prefix_q8_workspace_bytes",
     "tucker_pack_gqa", "tucker_pack_mha", "tucker_pack_mla",
     "tucker_hosvd_workspace_bytes", "tucker_hosvd_init", "tucker_mha_weight_tensors", "tucker_probe_plane_mix", "tucker_probe_mma_rate",
 )
@@ -55,6 +58,15 @@ class TuckerPagedCache(ctypes.Structure):
     """Mirror of `tucker_paged_cache`."""
     _fields_ = [
         ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+        ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+    ]
+
+
+class TuckerPagedCacheQ8(ctypes.Structure):
+    """Mirror of `tucker_paged_cache_q8`."""
+    _fields_ = [
+        ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("Ks", ctypes.c_void_p), ("Vs", ctypes.c_void_p),
+        ("block_table", ctypes.c_void_p),
         ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
     ]
 
@@ -103,6 +115,14 @@ def load_library() -> ctypes.CDLL:
     lib.tucker_attn_decode_prefix_workspace_bytes.argtypes = [vp, vp, i32]
     lib.tucker_attn_decode_prefix.restype = ctypes.c_int
     lib.tucker_attn_decode_prefix.argtypes = [vp] + [vp] * 9 + [vp, vp, vp, i32, i32, vp, vp, sz, vp]
+    for name in ("cache_append_paged", "attn_decode_paged", "attn_decode_prefix"):       # the 8-bit cache's: the same arguments
+        for tail in ("", "_workspace_bytes"):
+            q8, like = getattr(lib, f"tucker_{name}_q8{tail}"), getattr(lib, f"tucker_{name}{tail}")
+            q8.restype, q8.argtypes = like.restype, like.argtypes
+    lib.tucker_cache_store_paged_q8.restype = ctypes.c_int
+    lib.tucker_cache_store_paged_q8.argtypes = [vp] * 6 + [i32, vp]
+    lib.tucker_cache_read_paged_q8.restype = ctypes.c_int
+    lib.tucker_cache_read_paged_q8.argtypes = [vp] * 4 + [i32, vp, vp, vp]
     lib.tucker_attn_status_string.restype = ctypes.c_char_p
     lib.tucker_attn_status_string.argtypes = [ctypes.c_int]
     lib.tucker_attn_last_device_error.restype = ctypes.c_int
@@ -347,6 +367,7 @@ def tucker_attn_decode_static(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kcache, Vcach
 # call, and the usual outcome of the argument checks is decided in one expression (the checks one by one name the culprit).
 _DESC_PACK = struct.Struct("=12ififii").pack
 _CACHE_PACK = struct.Struct("=QQQiii4x").pack
+_CACHE_Q8_PACK = struct.Struct("=QQQQQiii4x").pack
 
 
 def _check_all(items, dtype, device):
@@ -484,6 +505,191 @@ def tucker_attn_decode_paged(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kpages, Vpages
     return tucker_attn_decode_prefix(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kpages, Vpages, block_table, cache_len, None, 0,
                                      n_H=n_H, rope=rope, rope_base=rope_base, scale=scale, append=append, out=out,
                                      workspace=workspace, flags=flags)
+
+
+# ---- the paged cache held in 8 bits ------------------------------------------------------------------------------------
+#
+# Pools Kpages [n_pages, page_size, r3], Vpages [n_pages, page_size, t3] of dtype torch.float8_e4m3fn, scales Kscale, Vscale
+# [n_pages, page_size] of dtype torch.float8_e8m0fnu: a row stands for its codes times its scale.  One shared latent pool: the
+# same tensors for keys and values.
+
+def _q8_cache(Kpages, Kscale, Vpages, Vscale, block_table, r3: int, t3: int, dev):
+    """Checks the tensors of an 8-bit cache; returns the packed structure."""
+    torch = _torch()
+    if Kpages.dim() != 3 or block_table.dim() != 2:
+        raise ValueError("Kpages must be [n_pages, page_size, r3] and block_table [B, max_pages]")
+    n_pages, page_size, _ = Kpages.shape
+    e4, e8, idx = torch.float8_e4m3fn, torch.float8_e8m0fnu, dev.index
+    if not (e4 is Kpages.dtype is Vpages.dtype and e8 is Kscale.dtype is Vscale.dtype and block_table.dtype is torch.int32
+            and idx == Kpages.get_device() == Vpages.get_device() == Kscale.get_device() == Vscale.get_device()
+            == block_table.get_device()
+            and Kpages.shape == (n_pages, page_size, r3) and Vpages.shape == (n_pages, page_size, t3)
+            and Kscale.shape == Vscale.shape == (n_pages, page_size)
+            and Kpages.is_contiguous() and Vpages.is_contiguous() and Kscale.is_contiguous() and Vscale.is_contiguous()
+            and block_table.is_contiguous()):
+        _check_all(((Kpages, "Kpages", (n_pages, page_size, r3)), (Vpages, "Vpages", (n_pages, page_size, t3))), e4, dev)
+        _check_all(((Kscale, "Kscale", (n_pages, page_size)), (Vscale, "Vscale", (n_pages, page_size))), e8, dev)
+        _check(block_table, "block_table", block_table.shape, torch.int32, dev)
+    return _CACHE_Q8_PACK(Kpages.data_ptr(), Vpages.data_ptr(), Kscale.data_ptr(), Vscale.data_ptr(), block_table.data_ptr(),
+                          n_pages, page_size, block_table.shape[1])
+
+
+def tucker_cache_append_paged_q8(X, U3, Ut3, Kpages, Kscale, Vpages, Vscale, block_table, cache_len, tok_start, *, rope: bool,
+                                 rope_base: float = 10000.0, pos0: int = 0, workspace=None, flags: int = 0) -> None:
+    """tucker_cache_append_paged into an 8-bit cache (same name and argument meaning as the C entry point): every row is
+    quantised on its way to its page."""
+    torch = _torch()
+    lib = load_library()
+    if X.dim() != 2 or cache_len.dim() != 1 or U3.dim() != 2 or Ut3.dim() != 2:
+        raise ValueError("X must be [T, d_model], U3 and Ut3 [d_model, rank] and cache_len [B]")
+    T, d = X.shape
+    r3, t3, B = U3.shape[1], Ut3.shape[1], cache_len.shape[0]
+    dt, dev, i32 = X.dtype, X.device, torch.int32
+    code = _dtype_code(X)
+    _check_all(((X, "X", (T, d)), (U3, "U3", (d, r3)), (Ut3, "Ut3", (d, t3))), dt, dev)
+    _check_all(((cache_len, "cache_len", (B,)), (tok_start, "tok_start", (B + 1,))), i32, dev)
+    cache = _q8_cache(Kpages, Kscale, Vpages, Vscale, block_table, r3, t3, dev)
+    if block_table.shape[0] != B:
+        raise ValueError(f"block_table has shape {tuple(block_table.shape)}, expected {B} rows")
+    desc = _DESC_PACK(B, 1, d, 1, 1, 1, r3, 1, 1, t3, 1, bool(rope), rope_base, pos0, 0.0, code, flags)
+    other = _enter_device(torch.cuda, dev)
+    try:
+        if workspace is None:                          # the size goes by the current device's number of SMs
+            workspace = alloc_workspace(lib.tucker_cache_append_paged_q8_workspace_bytes(desc, cache, T), dev)
+        else:
+            _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
+        rc = lib.tucker_cache_append_paged_q8(desc, X.data_ptr(), U3.data_ptr(), Ut3.data_ptr(), cache, cache_len.data_ptr(),
+                                              tok_start.data_ptr(), T, workspace.data_ptr(), workspace.numel(), _stream_ptr(dev))
+    finally:
+        if other is not None:
+            other.__exit__(None, None, None)
+    if rc != TA_OK:
+        raise TuckerAttnError(rc, "tucker_cache_append_paged_q8")
+
+
+def _q8_rows(Krows, Vrows, Kpages, Kscale, Vpages, Vscale, block_table, slots, tok_start, slots_name):
+    """Checks the arguments of the store and the read; returns (descriptor, cache, T, device)."""
+    torch = _torch()
+    if Krows.dim() != 2 or Vrows.dim() != 2 or slots.dim() != 1:
+        raise ValueError(f"Krows must be [T, r3], Vrows [T, t3] and {slots_name} [B]")
+    (T, r3), t3, B = Krows.shape, Vrows.shape[1], slots.shape[0]
+    dt, dev = Krows.dtype, Krows.device
+    code = _dtype_code(Krows)
+    _check_all(((Krows, "Krows", (T, r3)), (Vrows, "Vrows", (T, t3))), dt, dev)
+    _check_all(((slots, slots_name, (B,)), (tok_start, "tok_start", (B + 1,))), torch.int32, dev)
+    cache = _q8_cache(Kpages, Kscale, Vpages, Vscale, block_table, r3, t3, dev)
+    if block_table.shape[0] != B:
+        raise ValueError(f"block_table has shape {tuple(block_table.shape)}, expected {B} rows")
+    return _DESC_PACK(B, 1, 1, 1, 1, 1, r3, 1, 1, t3, 1, 0, 0.0, 0, 0.0, code, 0), cache, T, dev
+
+
+def tucker_cache_store_paged_q8(Krows, Vrows, Kpages, Kscale, Vpages, Vscale, block_table, cache_len, tok_start) -> None:
+    """Quantises latent rows that exist already (Krows [T, r3], Vrows [T, t3], as the cache is to hold them) into the slots
+    that follow each sequence's cached ones (same name and argument meaning as the C entry point)."""
+    torch = _torch()
+    lib = load_library()
+    desc, cache, T, dev = _q8_rows(Krows, Vrows, Kpages, Kscale, Vpages, Vscale, block_table, cache_len, tok_start, "cache_len")
+    other = _enter_device(torch.cuda, dev)
+    try:
+        rc = lib.tucker_cache_store_paged_q8(desc, Krows.data_ptr(), Vrows.data_ptr(), cache, cache_len.data_ptr(),
+                                             tok_start.data_ptr(), T, _stream_ptr(dev))
+    finally:
+        if other is not None:
+            other.__exit__(None, None, None)
+    if rc != TA_OK:
+        raise TuckerAttnError(rc, "tucker_cache_store_paged_q8")
+
+
+def tucker_cache_read_paged_q8(Kpages, Kscale, Vpages, Vscale, block_table, slot_start, tok_start, Krows, Vrows) -> None:
+    """Reads cached rows back into rows tok_start[b] .. tok_start[b + 1] - 1 of Krows [T, r3] and Vrows [T, t3]: the slots of
+    sequence b from slot_start[b] on (same name and argument meaning as the C entry point)."""
+    torch = _torch()
+    lib = load_library()
+    desc, cache, T, dev = _q8_rows(Krows, Vrows, Kpages, Kscale, Vpages, Vscale, block_table, slot_start, tok_start, "slot_start")
+    other = _enter_device(torch.cuda, dev)
+    try:
+        rc = lib.tucker_cache_read_paged_q8(desc, cache, slot_start.data_ptr(), tok_start.data_ptr(), T, Krows.data_ptr(),
+                                            Vrows.data_ptr(), _stream_ptr(dev))
+    finally:
+        if other is not None:
+            other.__exit__(None, None, None)
+    if rc != TA_OK:
+        raise TuckerAttnError(rc, "tucker_cache_read_paged_q8")
+
+
+def tucker_attn_decode_prefix_q8(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kpages, Kscale, Vpages, Vscale, block_table, cache_len,
+                                 prefix_table, prefix_len: int, *, n_H: int, rope: bool, rope_base: float = 10000.0,
+                                 scale: float = 0.0, append: bool = True, out=None, workspace=None, flags: int = 0):
+    """tucker_attn_decode_prefix over an 8-bit cache (same name and argument meaning as the C entry point).  Returns y [B, d]."""
+    torch = _torch()
+    lib = load_library()
+    if x.dim() != 2 or C.dim() != 3 or Ct.dim() != 3:
+        raise ValueError("x must be [B, d_model] and the cores 3-way tensors")
+    B, d = x.shape
+    r1, r2, r3 = C.shape
+    t1, t2, t3 = Ct.shape
+    dt, dev = x.dtype, x.device
+    i32, idx = torch.int32, dev.index
+    code = _dtype_code(x)
+    if out is None:
+        out = torch.empty_like(x)
+    if not (x.is_cuda and dt is C.dtype is U1.dtype is U2.dtype is U3.dtype is Ct.dtype is Ut1.dtype is Ut2.dtype is Ut3.dtype
+            is out.dtype and cache_len.dtype is i32
+            and idx == C.get_device() == U1.get_device() == U2.get_device() == U3.get_device() == Ct.get_device()
+            == Ut1.get_device() == Ut2.get_device() == Ut3.get_device() == out.get_device() == cache_len.get_device()
+            and U1.shape == (n_H, r1) and U2.shape == (d, r2) and U3.shape == (d, r3) and Ut1.shape == (n_H, t1)
+            and Ut2.shape == (d, t2) and Ut3.shape == (d, t3) and out.shape == (B, d) and cache_len.shape == (B,)
+            and x.is_contiguous() and C.is_contiguous() and U1.is_contiguous() and U2.is_contiguous() and U3.is_contiguous()
+            and Ct.is_contiguous() and Ut1.is_contiguous() and Ut2.is_contiguous() and Ut3.is_contiguous()
+            and out.is_contiguous() and cache_len.is_contiguous()):
+        _check_all(((x, "x", (B, d)), (C, "C", (r1, r2, r3)), (U1, "U1", (n_H, r1)), (U2, "U2", (d, r2)), (U3, "U3", (d, r3)),
+                    (Ct, "Ct", (t1, t2, t3)), (Ut1, "Ut1", (n_H, t1)), (Ut2, "Ut2", (d, t2)), (Ut3, "Ut3", (d, t3)),
+                    (out, "out", (B, d))), dt, dev)
+        _check(cache_len, "cache_len", (B,), i32, dev)
+    cache = _q8_cache(Kpages, Kscale, Vpages, Vscale, block_table, r3, t3, dev)
+    if block_table.shape[0] != B:
+        raise ValueError(f"block_table has shape {tuple(block_table.shape)}, expected {B} rows")
+    prefix_len = int(prefix_len)
+    if prefix_len < 0:
+        raise ValueError("prefix_len must not be negative")
+    prefix_ptr = None
+    if prefix_len > 0:
+        if prefix_table is None or prefix_table.dim() != 1 or prefix_table.shape[0] * Kpages.shape[1] < prefix_len:
+            raise ValueError("prefix_table must hold the ceil(prefix_len / page_size) pages of the prefix")
+        _check(prefix_table, "prefix_table", prefix_table.shape, i32, dev)
+        prefix_ptr = prefix_table.data_ptr()
+    desc = _DESC_PACK(B, 1, d, n_H, r1, r2, r3, t1, t2, t3, 1, bool(rope), rope_base, 0, scale, code, flags)
+    ws_ptr, ws_bytes = None, 0
+    other = _enter_device(torch.cuda, dev)
+    try:
+        if workspace is not None:
+            _check(workspace, "workspace", workspace.shape, torch.uint8, dev)
+            ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel()
+        else:
+            need = lib.tucker_attn_decode_prefix_q8_workspace_bytes(desc, cache, prefix_len)
+            if need != TA_WORKSPACE_NONE:
+                workspace = alloc_workspace(need, dev)
+                ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel()
+        rc = lib.tucker_attn_decode_prefix_q8(desc, x.data_ptr(), C.data_ptr(), U1.data_ptr(), U2.data_ptr(), U3.data_ptr(),
+                                              Ct.data_ptr(), Ut1.data_ptr(), Ut2.data_ptr(), Ut3.data_ptr(), cache,
+                                              cache_len.data_ptr(), prefix_ptr, prefix_len, bool(append), out.data_ptr(),
+                                              ws_ptr, ws_bytes, _stream_ptr(dev))
+    finally:
+        if other is not None:
+            other.__exit__(None, None, None)
+    if rc != TA_OK:
+        raise TuckerAttnError(rc, "tucker_attn_decode_prefix_q8")
+    return out
+
+
+def tucker_attn_decode_paged_q8(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kpages, Kscale, Vpages, Vscale, block_table, cache_len, *,
+                                n_H: int, rope: bool, rope_base: float = 10000.0, scale: float = 0.0, append: bool = True,
+                                out=None, workspace=None, flags: int = 0):
+    """tucker_attn_decode_paged over an 8-bit cache (same name and argument meaning as the C entry point): the step of
+    tucker_attn_decode_prefix_q8 without a prefix.  Returns y [B, d]."""
+    return tucker_attn_decode_prefix_q8(x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, Kpages, Kscale, Vpages, Vscale, block_table, cache_len,
+                                        None, 0, n_H=n_H, rope=rope, rope_base=rope_base, scale=scale, append=append, out=out,
+                                        workspace=workspace, flags=flags)
 
 
 _PACK_KEYS = ("C", "U1", "U2", "U3", "Ct", "Ut1", "Ut2", "Ut3")

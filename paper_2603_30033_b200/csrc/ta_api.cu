@@ -68,10 +68,36 @@ static bool paged_ok(const tucker_paged_cache* c, int64_t before) {
 }
 static int64_t paged_slots(const tucker_paged_cache& c) { return (int64_t)c.max_pages * c.page_size; }
 
+// Either kind of paged cache; the 8-bit one has scales.
+struct CacheArgs {
+  tucker_paged_cache c;
+  uint8_t *Ks, *Vs;
+  int q8;
+  bool one_pool() const { return c.K == c.V; }
+};
+static CacheArgs cache_args(const tucker_paged_cache* c) { return CacheArgs{c ? *c : tucker_paged_cache{}, nullptr, nullptr, 0}; }
+static CacheArgs cache_args(const tucker_paged_cache_q8* c) {
+  if (!c) return CacheArgs{};
+  return CacheArgs{{c->K, c->V, c->block_table, c->n_pages, c->page_size, c->max_pages}, (uint8_t*)c->Ks, (uint8_t*)c->Vs, 1};
+}
+
 // Grid limits of the paged kernels.
 static bool paged_batch_ok(const tucker_attn_desc& d) { return d.B <= 65535 && (int64_t)d.B * d.n_H <= (1 << 24); }
 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+static bool cache_ok(const CacheArgs& a, int64_t before) {
+  if (!paged_ok(&a.c, before)) return false;
+  if (!aligned16(a.c.K) || !aligned16(a.c.V)) return false;
+  return !a.q8 || (a.Ks && a.Vs && aligned16(a.Ks) && aligned16(a.Vs) && (a.Ks == a.Vs) == a.one_pool());
+}
+static void put_cache(Problem& p, const CacheArgs& a) {
+  p.Kc = a.c.K; p.Vc = a.c.V; p.Ks = a.Ks; p.Vs = a.Vs; p.q8 = a.q8;
+  p.paged = 1;
+  p.pv = PagedView{a.c.block_table, a.c.n_pages, a.c.page_size, a.c.max_pages};
+  p.shared_kv = a.one_pool() ? 1 : 0;
+  p.shared_rope = (p.shared_kv && p.d.rope) ? 1 : 0;
+}
 
 }  // namespace ta
 
@@ -165,41 +191,49 @@ int tucker_attn_decode(const tucker_attn_desc* desc, const void* x, const void* 
 }
 
 // Whether a step runs in its one-launch form, which needs no workspace.
-static bool paged_decode_small(const tucker_attn_desc& d, const tucker_paged_cache& c, int32_t prefix_len) {
-  return paged_batch_ok(d) && cluster_step_supported(d, c.K == c.V) &&
-         cluster_step_pays(d, paged_slots(c), prefix_len, fast_paged_supported(d, c.page_size));
+static bool paged_decode_fast(const tucker_attn_desc& d, const CacheArgs& a) { return !a.q8 && fast_paged_supported(d, a.c.page_size); }
+static bool paged_decode_small(const tucker_attn_desc& d, const CacheArgs& a, int32_t prefix_len) {
+  return !a.q8 && paged_batch_ok(d) && cluster_step_supported(d, a.one_pool()) &&
+         cluster_step_pays(d, paged_slots(a.c), prefix_len, paged_decode_fast(d, a));
 }
-static size_t paged_decode_need(const tucker_attn_desc& d, const tucker_paged_cache& c, int32_t prefix_len) {
+static size_t paged_decode_need(const tucker_attn_desc& d, const CacheArgs& a, int32_t prefix_len) {
   if (!paged_batch_ok(d)) return 0;
-  if (paged_decode_small(d, c, prefix_len)) return TA_WORKSPACE_NONE;
-  if (fast_paged_supported(d, c.page_size)) return fast_paged_workspace(d, prefix_len, c.K == c.V);
-  return generic_paged_decode_workspace(d, paged_slots(c), prefix_len);
+  if (paged_decode_small(d, a, prefix_len)) return TA_WORKSPACE_NONE;
+  if (paged_decode_fast(d, a)) return fast_paged_workspace(d, prefix_len, a.one_pool());
+  return generic_paged_decode_workspace(d, paged_slots(a.c), prefix_len);
+}
+static size_t paged_decode_query(const tucker_attn_desc* desc, const CacheArgs& a, int32_t prefix_len) {
+  return desc_ok(desc, true) && paged_ok(&a.c, prefix_len) ? paged_decode_need(*desc, a, prefix_len) : 0;
 }
 
 size_t tucker_attn_decode_paged_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache* cache) {
-  if (!desc_ok(desc, true) || !paged_ok(cache, 0)) return 0;
-  return paged_decode_need(*desc, *cache, 0);
+  return paged_decode_query(desc, cache_args(cache), 0);
 }
-
+size_t tucker_attn_decode_paged_q8_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache_q8* cache) {
+  return paged_decode_query(desc, cache_args(cache), 0);
+}
 size_t tucker_attn_decode_prefix_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache* cache,
                                                  int32_t prefix_len) {
-  if (!desc_ok(desc, true) || !paged_ok(cache, prefix_len)) return 0;
-  return paged_decode_need(*desc, *cache, prefix_len);
+  return paged_decode_query(desc, cache_args(cache), prefix_len);
+}
+size_t tucker_attn_decode_prefix_q8_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache_q8* cache,
+                                                    int32_t prefix_len) {
+  return paged_decode_query(desc, cache_args(cache), prefix_len);
 }
 
-int tucker_attn_decode_prefix(const tucker_attn_desc* desc, const void* x, const void* C, const void* U1, const void* U2,
-                              const void* U3, const void* Ct, const void* Ut1, const void* Ut2, const void* Ut3,
-                              const tucker_paged_cache* cache, const int32_t* cache_len, const int32_t* prefix_table,
-                              int32_t prefix_len, int32_t append, void* y, void* workspace, size_t workspace_bytes,
-                              void* cuda_stream) {
-  if (!desc_ok(desc, true) || !paged_ok(cache, prefix_len)) return TA_ERR_INVALID_ARG;
+static int paged_decode(const tucker_attn_desc* desc, const void* x, const void* C, const void* U1, const void* U2,
+                        const void* U3, const void* Ct, const void* Ut1, const void* Ut2, const void* Ut3,
+                        const CacheArgs& a, const int32_t* cache_len, const int32_t* prefix_table,
+                        int32_t prefix_len, int32_t append, void* y, void* workspace, size_t workspace_bytes,
+                        void* cuda_stream) {
+  if (!desc_ok(desc, true) || !cache_ok(a, prefix_len)) return TA_ERR_INVALID_ARG;
   if (!x || !C || !U1 || !U2 || !U3 || !Ct || !Ut1 || !Ut2 || !Ut3 || !y) return TA_ERR_INVALID_ARG;
   if (!cache_len || (prefix_len > 0 && !prefix_table)) return TA_ERR_INVALID_ARG;
-  if (cache->K == cache->V && !shared_kv_weights(*desc, U3, Ut3)) return TA_ERR_INVALID_ARG;
-  const void* ptrs[] = {x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, y, cache->K, cache->V};
+  if (a.one_pool() && !shared_kv_weights(*desc, U3, Ut3)) return TA_ERR_INVALID_ARG;
+  const void* ptrs[] = {x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, y};
   for (const void* q : ptrs)
     if (!aligned16(q)) return TA_ERR_INVALID_ARG;
-  const size_t need = paged_decode_need(*desc, *cache, prefix_len);
+  const size_t need = paged_decode_need(*desc, a, prefix_len);
   const bool small = need == TA_WORKSPACE_NONE;
   if (!small && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u))) return TA_ERR_INVALID_ARG;
   if (need == 0) return TA_ERR_UNSUPPORTED_SHAPE;
@@ -208,67 +242,141 @@ int tucker_attn_decode_prefix(const tucker_attn_desc* desc, const void* x, const
   p.d = *desc;
   p.scale = resolve_scale(*desc);
   p.X = x; p.C = C; p.U1 = U1; p.U2 = U2; p.U3 = U3; p.Ct = Ct; p.Ut1 = Ut1; p.Ut2 = Ut2; p.Ut3 = Ut3;
-  p.Y = y; p.Kc = cache->K; p.Vc = cache->V; p.Lmax = (int32_t)paged_slots(*cache);
+  p.Y = y; p.Lmax = (int32_t)paged_slots(a.c);
   p.cache_len = cache_len; p.append = append ? 1 : 0;
-  p.paged = 1;
-  p.pv = PagedView{cache->block_table, cache->n_pages, cache->page_size, cache->max_pages};
+  put_cache(p, a);
   p.prefix_table = prefix_table; p.prefix_len = prefix_len;
-  p.shared_kv = (cache->K == cache->V) ? 1 : 0;
-  p.shared_rope = (p.shared_kv && desc->rope) ? 1 : 0;
   p.ws = static_cast<char*>(workspace); p.ws_bytes = workspace_bytes;
   p.stream = static_cast<cudaStream_t>(cuda_stream);
   p.dev_err = device_error_ptr();
   p.prof_start = tl_prof_start; p.prof_stop = tl_prof_stop;
   if (!p.dev_err) return TA_ERR_CUDA;
-  const bool fast = fast_paged_supported(*desc, cache->page_size);
+  const bool fast = paged_decode_fast(*desc, a);
   const int rc = small ? cluster_paged_decode(p) : (fast ? fast_decode(p) : generic_paged_decode(p));
   tl_last_path = small ? 3 : (fast ? 2 : 1);
   tl_last_launches = p.launches;
   return rc;
 }
 
+int tucker_attn_decode_prefix(const tucker_attn_desc* desc, const void* x, const void* C, const void* U1, const void* U2,
+                              const void* U3, const void* Ct, const void* Ut1, const void* Ut2, const void* Ut3,
+                              const tucker_paged_cache* cache, const int32_t* cache_len, const int32_t* prefix_table,
+                              int32_t prefix_len, int32_t append, void* y, void* workspace, size_t workspace_bytes,
+                              void* cuda_stream) {
+  return paged_decode(desc, x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, cache_args(cache), cache_len, prefix_table, prefix_len, append, y,
+                      workspace, workspace_bytes, cuda_stream);
+}
+int tucker_attn_decode_prefix_q8(const tucker_attn_desc* desc, const void* x, const void* C, const void* U1, const void* U2,
+                                 const void* U3, const void* Ct, const void* Ut1, const void* Ut2, const void* Ut3,
+                                 const tucker_paged_cache_q8* cache, const int32_t* cache_len, const int32_t* prefix_table,
+                                 int32_t prefix_len, int32_t append, void* y, void* workspace, size_t workspace_bytes,
+                                 void* cuda_stream) {
+  return paged_decode(desc, x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, cache_args(cache), cache_len, prefix_table, prefix_len, append, y,
+                      workspace, workspace_bytes, cuda_stream);
+}
 int tucker_attn_decode_paged(const tucker_attn_desc* desc, const void* x, const void* C, const void* U1, const void* U2,
                              const void* U3, const void* Ct, const void* Ut1, const void* Ut2, const void* Ut3,
                              const tucker_paged_cache* cache, const int32_t* cache_len, int32_t append, void* y,
                              void* workspace, size_t workspace_bytes, void* cuda_stream) {
-  return tucker_attn_decode_prefix(desc, x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, cache, cache_len, nullptr, 0, append, y,
-                                   workspace, workspace_bytes, cuda_stream);
+  return paged_decode(desc, x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, cache_args(cache), cache_len, nullptr, 0, append, y, workspace,
+                      workspace_bytes, cuda_stream);
+}
+int tucker_attn_decode_paged_q8(const tucker_attn_desc* desc, const void* x, const void* C, const void* U1, const void* U2,
+                                const void* U3, const void* Ct, const void* Ut1, const void* Ut2, const void* Ut3,
+                                const tucker_paged_cache_q8* cache, const int32_t* cache_len, int32_t append, void* y,
+                                void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  return paged_decode(desc, x, C, U1, U2, U3, Ct, Ut1, Ut2, Ut3, cache_args(cache), cache_len, nullptr, 0, append, y, workspace,
+                      workspace_bytes, cuda_stream);
+}
+
+static bool append_fast(const tucker_attn_desc& d, const CacheArgs& a) { return !a.q8 && fast_append_supported(d); }
+static size_t append_query(const tucker_attn_desc* desc, const CacheArgs& a, int32_t T) {
+  if (!desc_ok(desc, true) || !paged_ok(&a.c, desc->pos0) || T < 0) return 0;
+  size_t need = 0;
+  if (T > 0 && append_fast(*desc, a)) need = fast_append_workspace(*desc, T, a.one_pool());
+  else if (T > 0 && a.q8) need = generic_q8_append_workspace(*desc, T, a.one_pool());
+  return need < 256 ? 256 : need;
 }
 
 size_t tucker_cache_append_paged_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache* cache, int32_t T) {
-  if (!desc_ok(desc, true) || !paged_ok(cache, desc->pos0) || T < 0) return 0;
-  const size_t need = T > 0 && fast_append_supported(*desc) ? fast_append_workspace(*desc, T, cache->K == cache->V) : 0;
-  return need < 256 ? 256 : need;
+  return append_query(desc, cache_args(cache), T);
+}
+size_t tucker_cache_append_paged_q8_workspace_bytes(const tucker_attn_desc* desc, const tucker_paged_cache_q8* cache, int32_t T) {
+  return append_query(desc, cache_args(cache), T);
+}
+
+static int append_tokens(const tucker_attn_desc* desc, const void* X, const void* U3, const void* Ut3, const CacheArgs& a,
+                         const int32_t* cache_len, const int32_t* tok_start, int32_t T, void* workspace, size_t workspace_bytes,
+                         void* cuda_stream) {
+  if (!desc_ok(desc, true) || !cache_ok(a, desc->pos0) || T < 0) return TA_ERR_INVALID_ARG;
+  if (!U3 || !Ut3 || !cache_len || !tok_start || !workspace || (T > 0 && !X)) return TA_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return TA_ERR_INVALID_ARG;
+  if (a.one_pool() && !shared_kv_weights(*desc, U3, Ut3)) return TA_ERR_INVALID_ARG;
+  const void* ptrs[] = {X, U3, Ut3};
+  for (const void* q : ptrs)
+    if (!aligned16(q)) return TA_ERR_INVALID_ARG;
+  if (a.q8 && !q8_rows_supported(*desc)) return TA_ERR_UNSUPPORTED_SHAPE;
+  if (workspace_bytes < append_query(desc, a, T)) return TA_ERR_WORKSPACE_TOO_SMALL;
+  Problem p = {};
+  p.d = *desc;
+  p.X = X; p.U3 = U3; p.Ut3 = Ut3; p.cache_len = cache_len;
+  p.ws = static_cast<char*>(workspace); p.ws_bytes = workspace_bytes;
+  put_cache(p, a);
+  p.stream = static_cast<cudaStream_t>(cuda_stream);
+  p.dev_err = device_error_ptr();
+  p.prof_start = tl_prof_start; p.prof_stop = tl_prof_stop;
+  if (!p.dev_err) return TA_ERR_CUDA;
+  const bool fast = append_fast(*desc, a);
+  const int rc = T == 0 ? TA_OK : (fast ? fast_append(p, tok_start, T) : generic_paged_append(p, tok_start, T));
+  tl_last_path = fast ? 2 : 1;
+  tl_last_launches = p.launches;
+  return rc;
 }
 
 int tucker_cache_append_paged(const tucker_attn_desc* desc, const void* X, const void* U3, const void* Ut3,
                               const tucker_paged_cache* cache, const int32_t* cache_len, const int32_t* tok_start, int32_t T,
                               void* workspace, size_t workspace_bytes, void* cuda_stream) {
-  if (!desc_ok(desc, true) || !paged_ok(cache, desc->pos0) || T < 0) return TA_ERR_INVALID_ARG;
-  if (!U3 || !Ut3 || !cache_len || !tok_start || !workspace || (T > 0 && !X)) return TA_ERR_INVALID_ARG;
-  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return TA_ERR_INVALID_ARG;
-  if (cache->K == cache->V && !shared_kv_weights(*desc, U3, Ut3)) return TA_ERR_INVALID_ARG;
-  const void* ptrs[] = {X, U3, Ut3, cache->K, cache->V};
-  for (const void* q : ptrs)
-    if (!aligned16(q)) return TA_ERR_INVALID_ARG;
-  if (workspace_bytes < tucker_cache_append_paged_workspace_bytes(desc, cache, T)) return TA_ERR_WORKSPACE_TOO_SMALL;
+  return append_tokens(desc, X, U3, Ut3, cache_args(cache), cache_len, tok_start, T, workspace, workspace_bytes, cuda_stream);
+}
+int tucker_cache_append_paged_q8(const tucker_attn_desc* desc, const void* X, const void* U3, const void* Ut3,
+                                 const tucker_paged_cache_q8* cache, const int32_t* cache_len, const int32_t* tok_start, int32_t T,
+                                 void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  return append_tokens(desc, X, U3, Ut3, cache_args(cache), cache_len, tok_start, T, workspace, workspace_bytes, cuda_stream);
+}
+
+// Rows into (store) or out of an 8-bit cache.
+static int move_rows(const tucker_attn_desc* desc, const void* Krows, const void* Vrows, const CacheArgs& a, const int32_t* slots,
+                     const int32_t* tok_start, int32_t T, bool store, void* cuda_stream) {
+  if (!desc_ok(desc, true) || !cache_ok(a, 0) || T < 0) return TA_ERR_INVALID_ARG;
+  if (!slots || !tok_start || (T > 0 && (!Krows || !Vrows))) return TA_ERR_INVALID_ARG;
+  if (!aligned16(Krows) || !aligned16(Vrows)) return TA_ERR_INVALID_ARG;
+  if (a.one_pool() ? (desc->r3 != desc->t3 || Krows != Vrows) : (!store && T > 0 && Krows == Vrows)) return TA_ERR_INVALID_ARG;
+  if (!q8_rows_supported(*desc)) return TA_ERR_UNSUPPORTED_SHAPE;
   Problem p = {};
   p.d = *desc;
-  p.X = X; p.U3 = U3; p.Ut3 = Ut3; p.Kc = cache->K; p.Vc = cache->V; p.cache_len = cache_len;
-  p.ws = static_cast<char*>(workspace); p.ws_bytes = workspace_bytes;
-  p.paged = 1;
-  p.pv = PagedView{cache->block_table, cache->n_pages, cache->page_size, cache->max_pages};
-  p.shared_kv = (cache->K == cache->V) ? 1 : 0;
-  p.shared_rope = (p.shared_kv && desc->rope) ? 1 : 0;
+  p.cache_len = slots;
+  put_cache(p, a);
   p.stream = static_cast<cudaStream_t>(cuda_stream);
   p.dev_err = device_error_ptr();
   p.prof_start = tl_prof_start; p.prof_stop = tl_prof_stop;
   if (!p.dev_err) return TA_ERR_CUDA;
-  const bool fast = fast_append_supported(*desc);
-  const int rc = T == 0 ? TA_OK : (fast ? fast_append(p, tok_start, T) : generic_paged_append(p, tok_start, T));
-  tl_last_path = fast ? 2 : 1;
+  int rc = TA_OK;
+  if (T > 0)
+    rc = store ? q8_store_rows(p, Krows, Vrows, desc->dtype, false, tok_start, T)
+               : q8_read_rows(p, const_cast<void*>(Krows), const_cast<void*>(Vrows), tok_start, T);
+  tl_last_path = 1;
   tl_last_launches = p.launches;
   return rc;
+}
+
+int tucker_cache_store_paged_q8(const tucker_attn_desc* desc, const void* Krows, const void* Vrows,
+                                const tucker_paged_cache_q8* cache, const int32_t* cache_len, const int32_t* tok_start, int32_t T,
+                                void* cuda_stream) {
+  return move_rows(desc, Krows, Vrows, cache_args(cache), cache_len, tok_start, T, true, cuda_stream);
+}
+int tucker_cache_read_paged_q8(const tucker_attn_desc* desc, const tucker_paged_cache_q8* cache, const int32_t* slot_start,
+                               const int32_t* tok_start, int32_t T, void* Krows, void* Vrows, void* cuda_stream) {
+  return move_rows(desc, Krows, Vrows, cache_args(cache), slot_start, tok_start, T, false, cuda_stream);
 }
 
 const char* tucker_attn_status_string(int status) {

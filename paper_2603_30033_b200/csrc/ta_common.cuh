@@ -44,6 +44,8 @@ struct Problem {
   const void *X, *C, *U1, *U2, *U3, *Ct, *Ut1, *Ut2, *Ut3;
   void* Y;
   void *Kc, *Vc;            // prefill: optional cache outputs; decode: caches
+  int q8;                   // paged: Kc / Vc hold e4m3 codes, with a scale byte per row in Ks / Vs
+  uint8_t *Ks, *Vs;
   int32_t Lmax;
   const int32_t* cache_len; // decode only (device)
   int32_t append;           // decode only
@@ -123,6 +125,14 @@ int umma_gemm_f32_partials(Problem& p, const bf16* A, long lda, int M, const bf1
 size_t generic_paged_decode_workspace(const tucker_attn_desc& d, int64_t Lmax, int32_t prefix_len);
 int generic_paged_decode(Problem& p);
 int generic_paged_append(Problem& p, const int32_t* tok_start, int32_t T);
+size_t generic_q8_append_workspace(const tucker_attn_desc& d, int32_t T, bool one_pool);
+
+// Rows of an 8-bit cache (ta_q8_rows.cu), with p.Kc, p.Vc, p.Ks, p.Vs, p.pv, p.shared_kv (one pool: keys only) and
+// p.cache_len = tokens cached before (store) or first slots (read).  Store: rows [T, r] of type `dtype`, keys rotated at
+// p.d.pos0 + slot when `rope`.  Read: rows of type p.d.dtype.
+bool q8_rows_supported(const tucker_attn_desc& d);
+int q8_store_rows(Problem& p, const void* Krows, const void* Vrows, int dtype, bool rope, const int32_t* tok_start, int32_t T);
+int q8_read_rows(Problem& p, void* Krows, void* Vrows, const int32_t* tok_start, int32_t T);
 
 // Paged decode step of few sequences with short contexts in one launch, both types (ta_paged_cluster.cu); needs no
 // workspace.

@@ -23,15 +23,17 @@ __device__ __forceinline__ long paged_row(const int32_t* __restrict__ row_table,
 
 // Where row `t` of a ragged batch of appended tokens goes.  tok_start [B + 1] ascending: sequence b owns the rows
 // [tok_start[b], tok_start[b + 1]).  Rows at or behind tok_start[B], and in front of tok_start[0], belong to nobody.
-// A token whose slot does not exist sets TA_DEVERR_BAD_CACHE_LEN and is dropped.
+// A token whose slot does not exist sets TA_DEVERR_BAD_CACHE_LEN and is dropped.  `room`: whether the token is somebody's and its slot
+// exists (its page may still not).
 struct AppendDst {
   long row;      // pool row, or -1: nothing is written
   int pos;       // absolute position (angle of the rotation)
 };
 __device__ __forceinline__ AppendDst append_dst(int t, const int32_t* __restrict__ tok_start, const int32_t* __restrict__ cache_len,
-                                                int B, int pos0, const PagedView& pv, unsigned int* err) {
+                                                int B, int pos0, const PagedView& pv, unsigned int* err, bool* room = nullptr) {
   AppendDst d;
   d.row = -1; d.pos = 0;
+  if (room) *room = false;
   if (t < tok_start[0] || t >= tok_start[B]) return d;
   int lo = 0, hi = B;                       // tok_start[lo] <= t < tok_start[hi]
   while (hi - lo > 1) {
@@ -44,6 +46,7 @@ __device__ __forceinline__ AppendDst append_dst(int t, const int32_t* __restrict
     atomicOr(err, (unsigned)TA_DEVERR_BAD_CACHE_LEN);
     return d;
   }
+  if (room) *room = true;
   d.pos = pos0 + (int)slot;
   d.row = paged_row(pv.table + (long)lo * pv.max_pages, (int)slot, pv, err);
   return d;

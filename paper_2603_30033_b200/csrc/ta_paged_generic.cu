@@ -5,16 +5,19 @@
 // over blocks and joined by their (max, sum, output) partials: a step with few sequences still fills the GPU.
 #include "ta_gemm_fma.cuh"
 #include "ta_paged.cuh"
+#include "ta_q8.cuh"
 
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ta {
 namespace {
 
 using fma::ld;
 using fma::st;
+__device__ __forceinline__ float ld(const e4m3* p) { return q8::value(p->v); }      // without its row's scale
 
 // ---------------------------------------------------------------------------------------
 // 32 x 32 tile of A [M, K] B [K, N], fp32 accumulation.  512 threads: eight groups of 64 threads take an eighth of
@@ -228,15 +231,17 @@ __global__ void __launch_bounds__(256) k_pg_w(const float* __restrict__ qt_parts
 
 // ---------------------------------------------------------------------------------------
 // Per-head queries and the new token: w [r1][B][r3] = qt C[a];  qhat[b, h] = scale * sum_a U1[h, a] w[a, b], rotated at
-// the new token's position prefix_len + cache_len[b]; the new key rotated in place; both appended.
+// the new token's position prefix_len + cache_len[b]; the new key rotated in place; both appended.  C: the pools' type.
+// An 8-bit cache's new rows go on as the cache stores them (one pool with RoPE: the key is the stored row, rotated).
 // ---------------------------------------------------------------------------------------
-template <typename T>
+template <typename T, typename C>
 __global__ void __launch_bounds__(256) k_pg_queries(const float* __restrict__ w, const T* __restrict__ U1, float* __restrict__ qhat,
                                                     const float* __restrict__ k_parts, const float* __restrict__ v_parts, int shares,
-                                                    float* __restrict__ knew, float* __restrict__ vnew, T* __restrict__ K,
-                                                    T* __restrict__ V, const PagedView pv, const int32_t* __restrict__ cache_len,
+                                                    float* __restrict__ knew, float* __restrict__ vnew, C* __restrict__ K,
+                                                    C* __restrict__ V, uint8_t* __restrict__ Ks, uint8_t* __restrict__ Vs, const PagedView pv, const int32_t* __restrict__ cache_len,
                                                     int B, int nH, int r1, int r3, int t3, int Lmax, int prefix_len, float scale, int rope,
                                                     double base, const dec::RopeFreqs freqs, int append, int shared_kv, int shared_rope, unsigned int* err) {
+  constexpr bool kQ8 = std::is_same<C, e4m3>::value;
   pdl_enter();
   const int b = blockIdx.x;
   __shared__ long dst_s;
@@ -282,7 +287,7 @@ __global__ void __launch_bounds__(256) k_pg_queries(const float* __restrict__ w,
       xe += px[0];
       if (2 * i + 1 < r3) xo += px[1];
     }
-    const float2 cs = rope ? cs_s[i] : make_float2(1.f, 0.f);
+    const float2 cs = rope && !(kQ8 && shared_rope) ? cs_s[i] : make_float2(1.f, 0.f);
     knew[(long)b * r3 + 2 * i] = xe * cs.x - xo * cs.y;
     if (2 * i + 1 < r3) knew[(long)b * r3 + 2 * i + 1] = xe * cs.y + xo * cs.x;
   }
@@ -292,12 +297,45 @@ __global__ void __launch_bounds__(256) k_pg_queries(const float* __restrict__ w,
     vnew[(long)b * t3 + c] = t;
   }
   __syncthreads();
-  if (dst_s < 0) return;
   [[maybe_unused]] const long rows = (long)pv.n_pages * pv.page_size;
+  if constexpr (kQ8) {
+    __shared__ uint32_t amax_s[2];
+    if (threadIdx.x < 2) amax_s[threadIdx.x] = 0;
+    __syncthreads();
+    const bool write = dst_s >= 0 && TA_IDX_OK(err, dst_s, 1, rows);
+    for (int part = 0; part < 2; ++part) {         // one pool: the value row is the pool's
+      const int r = part == 0 ? r3 : t3;
+      float* row = (part == 0 ? knew : vnew) + (long)b * r;
+      uint32_t a = 0;
+      for (int c = threadIdx.x; c < r; c += blockDim.x) a = max(a, q8::abs_bits(row[c]));
+      atomicMax(&amax_s[part], a);
+      __syncthreads();
+      const int byte = q8::scale_byte(amax_s[part]);
+      const float inv = q8::inverse(byte), sc = q8::scale(byte);
+      const bool put = write && (part == 1 || !shared_kv);
+      for (int c = threadIdx.x; c < r; c += blockDim.x) {
+        const uint32_t code = q8::codes2(row[c] * inv, 0.f);
+        row[c] = q8::values2(code).x * sc;
+        if (put) (part == 0 ? K : V)[dst_s * r + c].v = (uint8_t)code;
+      }
+      if (put && threadIdx.x == 0) (part == 0 ? Ks : Vs)[dst_s] = (uint8_t)byte;
+    }
+    if (shared_rope) {
+      __syncthreads();
+      for (int i = threadIdx.x; i < half; i += blockDim.x) {
+        const float xe = vnew[(long)b * r3 + 2 * i], xo = vnew[(long)b * r3 + 2 * i + 1];
+        knew[(long)b * r3 + 2 * i] = xe * cs_s[i].x - xo * cs_s[i].y;
+        knew[(long)b * r3 + 2 * i + 1] = xe * cs_s[i].y + xo * cs_s[i].x;
+      }
+    }
+    return;
+  } else {
+  if (dst_s < 0) return;
   if (!shared_kv && TA_IDX_OK(err, dst_s, 1, rows))
     for (int c = threadIdx.x; c < r3; c += blockDim.x) st(K + dst_s * r3 + c, knew[(long)b * r3 + c]);
   if (TA_IDX_OK(err, dst_s, 1, rows))      // one pool: the value row, which is the un-rotated latent row
     for (int c = threadIdx.x; c < t3; c += blockDim.x) st(V + dst_s * t3 + c, vnew[(long)b * t3 + c]);
+  }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -317,6 +355,7 @@ template <typename T>
 struct AttnArgs {
   const float* q;          // [rows, r3]
   const T *K, *V;          // pools
+  const uint8_t *Ks, *Vs;  // scale bytes of an 8-bit cache's rows
   PagedView pv;            // table: row z of it is used (the prefix: its only row)
   const int32_t* cache_len;// nullptr: the prefix, n_keys keys
   const float *knew, *vnew;// [B, r3] rotated, [B, t3]
@@ -334,11 +373,18 @@ __device__ __forceinline__ float4 ld4(const bf16* p) {
   return make_float4(a.x, a.y, b.x, b.y);
 }
 
+__device__ __forceinline__ float4 ld4(const e4m3* p) {
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+  const float2 a = q8::values2(w), b = q8::values2(w >> 16);
+  return make_float4(a.x, a.y, b.x, b.y);
+}
+
 // Rows of a tile to shared memory, zero-padded to the pitch.  VEC: r is a multiple of 4, so that rows can be read four
 // elements at a time (a tile's loads are then in flight together instead of one after another).
 template <bool VEC, typename T>
-__device__ __forceinline__ void load_rows(float* __restrict__ out, const T* __restrict__ pool, const float* __restrict__ fresh,
-                                          const long* __restrict__ rows_s, int r, int pitch) {
+__device__ __forceinline__ void load_rows(float* __restrict__ out, const T* __restrict__ pool, const uint8_t* __restrict__ scales,
+                                          const float* __restrict__ fresh, const long* __restrict__ rows_s, int r, int pitch) {
+  constexpr bool kQ8 = std::is_same<T, e4m3>::value;
   if (VEC) {
     const int n4 = pitch / 4;
 #pragma unroll 4
@@ -348,7 +394,13 @@ __device__ __forceinline__ void load_rows(float* __restrict__ out, const T* __re
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       if (c < r) {
         if (rw == -2) v = ld4(fresh + c);
-        else if (rw >= 0) v = ld4(pool + rw * r + c);
+        else if (rw >= 0) {
+          v = ld4(pool + rw * r + c);
+          if constexpr (kQ8) {
+            const float sc = q8::scale(scales[rw]);
+            v.x *= sc; v.y *= sc; v.z *= sc; v.w *= sc;
+          }
+        }
       }
       *reinterpret_cast<float4*>(out + j * pitch + c) = v;
     }
@@ -356,7 +408,10 @@ __device__ __forceinline__ void load_rows(float* __restrict__ out, const T* __re
     for (int i = threadIdx.x; i < AK * pitch; i += 256) {
       const int j = i / pitch, c = i - j * pitch;
       const long rw = rows_s[j];
-      out[i] = c >= r ? 0.f : (rw == -2 ? fresh[c] : (rw >= 0 ? ld(pool + rw * r + c) : 0.f));
+      float v = c >= r ? 0.f : (rw == -2 ? fresh[c] : (rw >= 0 ? ld(pool + rw * r + c) : 0.f));
+      if constexpr (kQ8)
+        if (c < r && rw >= 0) v *= q8::scale(scales[rw]);
+      out[i] = v;
     }
   }
 }
@@ -368,9 +423,9 @@ __global__ void __launch_bounds__(256) k_pg_attn(const AttnArgs<T> g) {
   __shared__ double theta_s[kMaxPairs];
   const int rp = pitch4(g.r3), tp = pitch4(g.t3);
   float* qs = sm;                       // [AR][rp]
-  float* Ks = qs + AR * rp;             // [AK][rp]
-  float* Vs = Ks + AK * rp;             // [AK][tp]
-  float* ps = Vs + AK * tp;             // [AR][AK + 1]
+  float* Kt = qs + AR * rp;             // [AK][rp]
+  float* Vt = Kt + AK * rp;             // [AK][tp]
+  float* ps = Vt + AK * tp;             // [AR][AK + 1]
   long* rows_s = reinterpret_cast<long*>(ps + AR * (AK + 1));   // AR * (AK + 1) is even: 8-byte aligned
   const int tid = threadIdx.x, r = tid / 16, l = tid % 16;
   const int split = blockIdx.y, row0 = blockIdx.x * AR, z = blockIdx.z;
@@ -404,8 +459,8 @@ __global__ void __launch_bounds__(256) k_pg_attn(const AttnArgs<T> g) {
       rows_s[tid] = s >= limit ? -1 : (g.cache_len && s == L ? -2 : paged_row(table, s, g.pv, g.err));
     }
     __syncthreads();
-    load_rows<VEC>(Ks, g.K, g.knew + (long)z * g.r3, rows_s, g.r3, rp);
-    load_rows<VEC>(Vs, g.V, g.vnew + (long)z * g.t3, rows_s, g.t3, tp);
+    load_rows<VEC>(Kt, g.K, g.Ks, g.knew + (long)z * g.r3, rows_s, g.r3, rp);
+    load_rows<VEC>(Vt, g.V, g.Vs, g.vnew + (long)z * g.t3, rows_s, g.t3, tp);
     __syncthreads();
     if (g.rotate_keys) {                // one pool with latent RoPE: the key is the cached row, rotated (the new token's is already)
       const int half = g.r3 / 2;
@@ -413,7 +468,7 @@ __global__ void __launch_bounds__(256) k_pg_attn(const AttnArgs<T> g) {
         const int j = i / half, c = i - j * half;
         if (rows_s[j] < 0) continue;
         const float2 cs = dec::rope_cos_sin_theta(g.pos_base + k0 + j, theta_s[c]);
-        float* px = Ks + j * rp + 2 * c;
+        float* px = Kt + j * rp + 2 * c;
         const float xe = px[0], xo = px[1];
         px[0] = xe * cs.x - xo * cs.y;
         px[1] = xe * cs.y + xo * cs.x;
@@ -422,8 +477,8 @@ __global__ void __launch_bounds__(256) k_pg_attn(const AttnArgs<T> g) {
     }
     float s0 = 0.f, s1 = 0.f;
     const float4* q4 = reinterpret_cast<const float4*>(qs + r * rp);
-    const float4* ka = reinterpret_cast<const float4*>(Ks + l * rp);
-    const float4* kb = reinterpret_cast<const float4*>(Ks + (l + 16) * rp);
+    const float4* ka = reinterpret_cast<const float4*>(Kt + l * rp);
+    const float4* kb = reinterpret_cast<const float4*>(Kt + (l + 16) * rp);
     for (int c = 0; c < n4; ++c) {
       const float4 q = q4[c], a = ka[c], b = kb[c];
       s0 = fmaf(q.x, a.x, s0); s0 = fmaf(q.y, a.y, s0); s0 = fmaf(q.z, a.z, s0); s0 = fmaf(q.w, a.w, s0);
@@ -449,7 +504,7 @@ __global__ void __launch_bounds__(256) k_pg_attn(const AttnArgs<T> g) {
       if (4 * l + 64 * i < g.t3) { o[i].x *= f; o[i].y *= f; o[i].z *= f; o[i].w *= f; }
     for (int j = 0; j < AK; ++j) {
       const float p = ps[r * (AK + 1) + j];
-      const float4* v4 = reinterpret_cast<const float4*>(Vs + j * tp);
+      const float4* v4 = reinterpret_cast<const float4*>(Vt + j * tp);
 #pragma unroll
       for (int i = 0; i < kMaxO4; ++i)
         if (4 * l + 64 * i < g.t3) {
@@ -638,7 +693,7 @@ int attn(Problem& p, const AttnArgs<T>& g, int zs) {
   return TA_OK;
 }
 
-template <typename T>
+template <typename T, typename C>      // C: the pools' type
 int decode_typed(Problem& p) {
   const tucker_attn_desc& d = p.d;
   const int P = p.prefix_len;
@@ -659,12 +714,12 @@ int decode_typed(Problem& p) {
   (void)launch_pdl(k_pg_w<T>, dim3((d.B + WB - 1) / WB, d.r1, (d.r3 + 31) / 32), dim3(256), WB * d.r2 * sizeof(float), p.stream, w.qt_parts,
                    shares, (const T*)p.C, w.w, d.B, d.r1, d.r2, d.r3);
   TA_LAUNCH_CHECK(p);
-  (void)launch_pdl(k_pg_queries<T>, dim3(d.B, std::max(1, std::min(8, 2 * kSms / d.B))), dim3(256), 0, p.stream, w.w, (const T*)p.U1, w.qhat,
-                   w.k_parts, w.v_parts, shares, w.knew, w.vnew, (T*)p.Kc, (T*)p.Vc, p.pv, p.cache_len, d.B, d.n_H, d.r1, d.r3, d.t3, p.Lmax,
+  (void)launch_pdl(k_pg_queries<T, C>, dim3(d.B, std::max(1, std::min(8, 2 * kSms / d.B))), dim3(256), 0, p.stream, w.w, (const T*)p.U1, w.qhat,
+                   w.k_parts, w.v_parts, shares, w.knew, w.vnew, (C*)p.Kc, (C*)p.Vc, p.Ks, p.Vs, p.pv, p.cache_len, d.B, d.n_H, d.r1, d.r3, d.t3, p.Lmax,
                    P, p.scale, d.rope, (double)d.rope_base, rope_freqs(d), p.append, p.shared_kv, p.shared_rope, p.dev_err);
   TA_LAUNCH_CHECK(p);
-  AttnArgs<T> a = {};
-  a.q = w.qhat; a.K = (const T*)p.Kc; a.V = (const T*)p.Vc; a.pv = p.pv; a.cache_len = p.cache_len;
+  AttnArgs<C> a = {};
+  a.q = w.qhat; a.K = (const C*)p.Kc; a.V = (const C*)p.Vc; a.Ks = p.Ks; a.Vs = p.Vs; a.pv = p.pv; a.cache_len = p.cache_len;
   a.knew = w.knew; a.vnew = w.vnew; a.rows_per_z = d.n_H; a.Lmax = p.Lmax; a.r3 = d.r3; a.t3 = d.t3;
   a.splits = own_splits(d, p.Lmax); a.rotate_keys = p.shared_rope; a.pos_base = P; a.base = (double)d.rope_base;
   a.part_o = w.po; a.part_ml = w.ml; a.err = p.dev_err;
@@ -693,6 +748,21 @@ int decode_typed(Problem& p) {
 }
 
 template <typename T>
+int append_q8_typed(Problem& p, const int32_t* tok_start, int32_t T_) {
+  const tucker_attn_desc& d = p.d;
+  Carver c(p.ws);
+  float* k = p.shared_kv ? nullptr : c.take<float>((size_t)T_ * d.r3);
+  float* v = c.take<float>((size_t)T_ * d.t3);
+  GemmArgs<T, T, float> g = {};
+  g.A = (const T*)p.X; g.lda = d.d_model; g.M = T_; g.K = d.d_model; g.kb_per_split = (d.d_model + GK - 1) / GK;
+  g.part[g.parts++] = {(const T*)p.Ut3, {d.t3, 1}, v, d.t3, d.t3, 0};
+  if (k) g.part[g.parts++] = {(const T*)p.U3, {d.r3, 1}, k, d.r3, d.r3, 0};
+  const int rc = launch_gemm(p, g, k ? std::max(d.r3, d.t3) : d.t3);
+  if (rc) return rc;
+  return q8_store_rows(p, k ? k : v, v, TA_DTYPE_F32, k && d.rope, tok_start, T_);
+}
+
+template <typename T>
 int append_typed(Problem& p, const int32_t* tok_start, int32_t T_) {
   const tucker_attn_desc& d = p.d;
   AppendArgs<T> g = {};
@@ -714,10 +784,19 @@ size_t generic_paged_decode_workspace(const tucker_attn_desc& d, int64_t Lmax, i
 
 int generic_paged_decode(Problem& p) {
   if (!shape_ok(p.d)) return TA_ERR_UNSUPPORTED_SHAPE;
-  return p.d.dtype == TA_DTYPE_F32 ? decode_typed<float>(p) : decode_typed<bf16>(p);
+  if (p.q8) return p.d.dtype == TA_DTYPE_F32 ? decode_typed<float, e4m3>(p) : decode_typed<bf16, e4m3>(p);
+  return p.d.dtype == TA_DTYPE_F32 ? decode_typed<float, float>(p) : decode_typed<bf16, bf16>(p);
+}
+
+size_t generic_q8_append_workspace(const tucker_attn_desc& d, int32_t T, bool one_pool) {
+  Carver c(nullptr);
+  if (!one_pool) c.take<float>((size_t)T * d.r3);
+  c.take<float>((size_t)T * d.t3);
+  return c.off;
 }
 
 int generic_paged_append(Problem& p, const int32_t* tok_start, int32_t T) {
+  if (p.q8) return p.d.dtype == TA_DTYPE_F32 ? append_q8_typed<float>(p, tok_start, T) : append_q8_typed<bf16>(p, tok_start, T);
   return p.d.dtype == TA_DTYPE_F32 ? append_typed<float>(p, tok_start, T) : append_typed<bf16>(p, tok_start, T);
 }
 
