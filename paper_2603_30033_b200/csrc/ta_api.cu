@@ -191,7 +191,9 @@ int tucker_attn_decode(const tucker_attn_desc* desc, const void* x, const void* 
 }
 
 // Whether a step runs in its one-launch form, which needs no workspace.
-static bool paged_decode_fast(const tucker_attn_desc& d, const CacheArgs& a) { return !a.q8 && fast_paged_supported(d, a.c.page_size); }
+static bool paged_decode_fast(const tucker_attn_desc& d, const CacheArgs& a) {
+  return fast_paged_supported(d, a.c.page_size) && !(a.q8 && a.one_pool() && d.rope);
+}
 static bool paged_decode_small(const tucker_attn_desc& d, const CacheArgs& a, int32_t prefix_len) {
   return !a.q8 && paged_batch_ok(d) && cluster_step_supported(d, a.one_pool()) &&
          cluster_step_pays(d, paged_slots(a.c), prefix_len, paged_decode_fast(d, a));
@@ -199,7 +201,7 @@ static bool paged_decode_small(const tucker_attn_desc& d, const CacheArgs& a, in
 static size_t paged_decode_need(const tucker_attn_desc& d, const CacheArgs& a, int32_t prefix_len) {
   if (!paged_batch_ok(d)) return 0;
   if (paged_decode_small(d, a, prefix_len)) return TA_WORKSPACE_NONE;
-  if (paged_decode_fast(d, a)) return fast_paged_workspace(d, prefix_len, a.one_pool());
+  if (paged_decode_fast(d, a)) return fast_paged_workspace(d, prefix_len, a.one_pool(), a.q8);
   return generic_paged_decode_workspace(d, paged_slots(a.c), prefix_len);
 }
 static size_t paged_decode_query(const tucker_attn_desc* desc, const CacheArgs& a, int32_t prefix_len) {

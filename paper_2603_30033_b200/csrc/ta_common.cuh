@@ -103,7 +103,7 @@ int fast_fwd(Problem& p);
 bool fast_decode_supported(const tucker_attn_desc& d, int32_t Lmax);
 // the same step over a paged cache (p.paged), behind a prefix of prefix_len shared tokens
 bool fast_paged_supported(const tucker_attn_desc& d, int32_t page_size);
-size_t fast_paged_workspace(const tucker_attn_desc& d, int32_t prefix_len, bool one_pool);
+size_t fast_paged_workspace(const tucker_attn_desc& d, int32_t prefix_len, bool one_pool, bool q8);
 size_t fast_decode_workspace(const tucker_attn_desc& d, int32_t Lmax);
 int fast_decode(Problem& p);
 bool fast_append_supported(const tucker_attn_desc& d);

@@ -10,6 +10,7 @@
 #pragma once
 
 #include "ta_common.cuh"
+#include "ta_q8.cuh"
 #include "ta_sm100.cuh"
 
 namespace ta {
@@ -100,7 +101,15 @@ __device__ __forceinline__ float2 rope_cos_sin(int pos, int i, int r, double log
 // slot 0.
 // The new token's key and value enter its own attention as the cache takes them, rounded to bf16: the row that this step
 // sees is the row that every later step reads.
+// Q8: the cache is in 8 bits.  A row's scale needs all of the row, so CTA y = 0 of a sequence finishes both rows (two passes over
+// the columns instead of one), codes and scales, and the others only the query.
 // ---------------------------------------------------------------------------------------
+struct NewRowsQ8 {
+  uint8_t *k, *v;          // [B, r3], [B, t3] codes of the new rows, for the attention kernel
+  uint8_t* scale;          // [B][2] their scale bytes
+  uint32_t* qmax;          // [B][4] bits of the largest |q| of each 32 coordinates
+  uint8_t *Kc, *Vc, *Ks, *Vs;      // pools
+};
 constexpr int DQ_CW = 32;       // latent key coordinates per CTA
 constexpr int DQ_MAX_R1 = 32;   // head ranks r1, t1 supported by the shared-memory tables
 constexpr int DQ_MAX_R2 = 256;
@@ -117,13 +126,13 @@ __device__ __forceinline__ float split_sum(const float* __restrict__ p, int n, l
   return acc;
 }
 
-template <int NQ>
+template <int NQ, bool Q8>
 __global__ void __launch_bounds__(256, 2)
 k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH, int r1, int r2, int r3, int t3,
            const bf16* __restrict__ C, const bf16* __restrict__ U1, float mult, bf16* __restrict__ qhat,
            bf16* __restrict__ knew, bf16* __restrict__ vnew, bf16* __restrict__ Kc, bf16* __restrict__ Vc, int Lmax,
            const int32_t* __restrict__ cache_len, int rope, const RopeFreqs freqs, int append, int shared_kv,
-           const PagedView pv, int pos_base, bf16* __restrict__ qhat_lo, unsigned int* err) {
+           const PagedView pv, int pos_base, bf16* __restrict__ qhat_lo, unsigned int* err, const NewRowsQ8 n8) {
   constexpr int AB = NQ == 1 ? 8 : 4;               // core slices per batch (8 to 16 loads of 16 bytes in flight per thread)
   __shared__ float qt_s[DQ_MAX_R2];                 // latent query of the new token
   __shared__ float k_s[DQ_CW];                      // this CTA's coordinates of the new key (unrotated)
@@ -131,6 +140,9 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
   __shared__ float u1_s[32 * DQ_MAX_R1];            // U1 as fp32
   __shared__ float w_s[DQ_MAX_R1][DQ_CW];
   __shared__ float red_s[2][8][AB][DQ_CW];          // by batch parity
+  __shared__ float row_s[Q8 ? 2 : 1][128];          // Q8: the new rows
+  __shared__ float2 csn_s[Q8 ? 64 : 1];             // Q8: (cos, sin) at position L
+  __shared__ uint32_t qmax_s;
   const int b = blockIdx.x, c0 = blockIdx.y * DQ_CW;
   const int ncol = r2 + r3 + t3;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -175,6 +187,11 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
   if (threadIdx.x < DQ_CW / 2) {
     cs_s[threadIdx.x] = rope ? rope_cos_sin_theta(pos_base + L, freqs.theta[c0 / 2 + threadIdx.x]) : make_float2(1.f, 0.f);
   }
+  if constexpr (Q8) {
+    if (threadIdx.x == 255) qmax_s = 0;
+    if (blockIdx.y == 0 && threadIdx.x >= 64 && threadIdx.x < 64 + r3 / 2)
+      csn_s[threadIdx.x - 64] = rope ? rope_cos_sin_theta(pos_base + L, freqs.theta[threadIdx.x - 64]) : make_float2(1.f, 0.f);
+  }
   pdl_enter();
   // split-K sums: all of qt, this CTA's 32 key coordinates, and the value coordinates c with
   // (c / 32) % gridDim.y == blockIdx.y
@@ -185,6 +202,42 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
                        TA_IDX_OK(err, (long)(splits - 1) * split_stride + (long)b * ncol, ncol, (long)splits * split_stride);
   // (one pass over all of them: the loads of a thread's column are in flight together, and so are the columns)
   const int ny = (int)gridDim.y, vblocks = max(0, (t3 / DQ_CW - (int)blockIdx.y + ny - 1) / ny);
+  if constexpr (Q8) {
+    const int cols = blockIdx.y == 0 ? r2 + r3 + (shared_kv ? 0 : t3) : r2;
+    for (int c = threadIdx.x; c < cols; c += blockDim.x) {
+      const float acc = prow_ok ? split_sum(prow + c, splits, split_stride) : 0.f;
+      if (c < r2) qt_s[c] = acc;
+      else if (c < r2 + r3) row_s[0][c - r2] = acc;
+      else row_s[1][c - r2 - r3] = acc;
+    }
+    __syncthreads();
+    if (blockIdx.y == 0 && warp < (shared_kv ? 1 : 2)) {      // warp 0: the key (one pool: the row), warp 1: the value
+      const int r = warp == 0 ? r3 : t3;
+      float v4[4] = {};                                       // columns 4 lane .. 4 lane + 3
+      if (4 * lane < r) {
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          const float xe = row_s[warp][4 * lane + e], xo = row_s[warp][4 * lane + e + 1];
+          const float2 cs = warp == 0 && shared_kv != 2 ? csn_s[2 * lane + e / 2] : make_float2(1.f, 0.f);
+          v4[e] = xe * cs.x - xo * cs.y;
+          v4[e + 1] = xe * cs.y + xo * cs.x;
+        }
+      }
+      const uint32_t a = __reduce_max_sync(0xffffffffu, max(max(q8::abs_bits(v4[0]), q8::abs_bits(v4[1])), max(q8::abs_bits(v4[2]), q8::abs_bits(v4[3]))));
+      const int byte = q8::scale_byte(a);
+      const float inv = q8::inverse(byte);
+      const uint32_t codes = q8::codes4(v4[0] * inv, v4[1] * inv, v4[2] * inv, v4[3] * inv);
+      for (int part = warp; part < (shared_kv ? 2 : warp + 1); ++part) {        // one pool: the row is key and value
+        if (4 * lane < r && TA_IDX_OK(err, (long)b * r + 4 * lane, 4, (long)nB * r))
+          *reinterpret_cast<uint32_t*>((part == 0 ? n8.k : n8.v) + (long)b * r + 4 * lane) = codes;
+        if (lane == 0) n8.scale[2 * b + part] = (uint8_t)byte;
+      }
+      if (append && TA_IDX_OK(err, new_row, 1, n_rows)) {
+        if (4 * lane < r) *reinterpret_cast<uint32_t*>((warp == 0 ? n8.Kc : n8.Vc) + new_row * r + 4 * lane) = codes;
+        if (lane == 0) (warp == 0 ? n8.Ks : n8.Vs)[new_row] = (uint8_t)byte;
+      }
+    }
+  } else {
   for (int c = threadIdx.x; c < r2 + DQ_CW + vblocks * DQ_CW; c += blockDim.x) {
     const int e = c - r2 - DQ_CW;                      // >= 0: value coordinate vc
     const int vc = (e / DQ_CW * ny + (int)blockIdx.y) * DQ_CW + e % DQ_CW;
@@ -211,6 +264,7 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
       *reinterpret_cast<__nv_bfloat162*>(knew + (long)b * r3 + c0 + 2 * i) = kv;
     if (append && shared_kv != 2 && TA_IDX_OK(err, new_row * r3 + c0 + 2 * i, 2, n_rows * r3))
       *reinterpret_cast<__nv_bfloat162*>(Kc + new_row * r3 + c0 + 2 * i) = kv;
+  }
   }
   // ---- w[a, c0 + .] for batches of AB slices ----
   for (int a0 = 0; a0 < r1; a0 += AB) {
@@ -268,6 +322,7 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
   }
   __syncthreads();
   // ---- qhat_h for this CTA's coordinates ----
+  [[maybe_unused]] uint32_t qm = 0;
   for (int item = threadIdx.x; item < nH * (DQ_CW / 2); item += blockDim.x) {
     const int h = item / (DQ_CW / 2), cp = item % (DQ_CW / 2);
     float xe = 0.f, xo = 0.f;
@@ -279,6 +334,7 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
     xe *= mult; xo *= mult;
     const float2 cs = cs_s[cp];
     const float qe = xe * cs.x - xo * cs.y, qo = xe * cs.y + xo * cs.x;
+    if constexpr (Q8) qm = max(qm, max(q8::abs_bits(qe), q8::abs_bits(qo)));
     const __nv_bfloat162 hi = __floats2bfloat162_rn(qe, qo);
     const long at = ((long)b * nH + h) * r3 + c0 + 2 * cp;
     if (TA_IDX_OK(err, at, 2, (long)nB * nH * r3)) {
@@ -288,6 +344,13 @@ k_dec_qhat(const float* __restrict__ part, int splits, long split_stride, int nH
         *reinterpret_cast<__nv_bfloat162*>(qhat_lo + at) = __floats2bfloat162_rn(qe - f.x, qo - f.y);
       }
     }
+  }
+  if constexpr (Q8) {
+    qm = __reduce_max_sync(0xffffffffu, qm);
+    if (lane == 0) atomicMax(&qmax_s, qm);
+    __syncthreads();
+    if (threadIdx.x < 4 && ((int)threadIdx.x == (int)blockIdx.y || (blockIdx.y == 0 && (int)threadIdx.x >= ny)))      // none there: 0
+      n8.qmax[4 * (long)b + threadIdx.x] = (int)threadIdx.x == (int)blockIdx.y ? qmax_s : 0u;
   }
 }
 

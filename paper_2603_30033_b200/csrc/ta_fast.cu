@@ -12,6 +12,7 @@
 #include "ta_umma_gemm.cuh"
 #include "ta_attn_prefill.cuh"
 #include "ta_decode.cuh"
+#include "ta_decode_q8.cuh"
 #include "ta_decode_umma.cuh"
 #include "ta_append_umma.cuh"
 #include "ta_paged_out.cuh"
@@ -72,16 +73,16 @@ EncodeTiledFn encode_tiled_fn() {
   return fn;
 }
 
-// bf16 tensor of up to 4 dims; dims[0] is innermost (contiguous); strides in elements for dims 1..rank-1.
+// bf16 tensor (or bytes) of up to 4 dims; dims[0] is innermost (contiguous); strides in elements for dims 1..rank-1.
 bool make_tmap(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_elems,
-               const uint32_t* box, CUtensorMapSwizzle swz) {
+               const uint32_t* box, CUtensorMapSwizzle swz, bool bytes = false) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (!fn) return false;
   cuuint64_t gdim[4], gstr[3];
   cuuint32_t bx[4], es[4];
   for (int i = 0; i < rank; ++i) { gdim[i] = dims[i]; bx[i] = box[i]; es[i] = 1; }
-  for (int i = 0; i + 1 < rank; ++i) gstr[i] = strides_elems[i] * 2;
-  CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), gdim, gstr, bx, es,
+  for (int i = 0; i + 1 < rank; ++i) gstr[i] = strides_elems[i] * (bytes ? 1 : 2);
+  CUresult r = fn(m, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), gdim, gstr, bx, es,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, swz, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS;
@@ -587,6 +588,10 @@ struct FastDecWs {
   int* seq_cta;            // [B][2], paged: CTAs of the streaming kernel that hold a sequence
   float *pre_o, *pre_ml;   // partials of the shared prefix
   bf16* pre_k;             // one pool with latent RoPE: the prefix's keys, rotated (rows padded to whole tiles); their rests
+                           // 8-bit cache: the prefix's keys in any case
+  bf16* pre_v;             // 8-bit cache: the prefix's values
+  uint8_t* new_scale;      // [B][2], 8-bit cache: scale bytes of the new rows (their codes in knew, vnew)
+  uint32_t* qmax;          // [B][4], 8-bit cache: see NewRowsQ8
 };
 
 // Width of one half of z in the paged step (see k_dec_out).
@@ -604,7 +609,7 @@ PrefixPlan prefix_plan(const tucker_attn_desc& d, int32_t P) {
   return q;
 }
 
-size_t carve_fast_dec(const tucker_attn_desc& d, bool paged, int32_t prefix_len, bool rotated, char* base, FastDecWs* w) {
+size_t carve_fast_dec(const tucker_attn_desc& d, bool paged, int32_t prefix_len, bool one_pool, bool q8, char* base, FastDecWs* w) {
   Carver c(base);
   FastDecWs t;
   const size_t Mpad = (size_t)((d.B + 127) / 128) * 128;
@@ -619,14 +624,19 @@ size_t carve_fast_dec(const tucker_attn_desc& d, bool paged, int32_t prefix_len,
   t.part_ml = c.take<float>(slots * 64);
   t.seq_cta = c.take<int>(paged ? (size_t)d.B * 2 : 0);
   t.pre_o = t.pre_ml = nullptr;
-  t.pre_k = nullptr;
+  t.pre_k = t.pre_v = nullptr;
+  const bool rotated = one_pool && d.rope;
   if (prefix_len > 0) {
     const PrefixPlan q = prefix_plan(d, prefix_len);
     const size_t rows = (size_t)(dec::MAX_GRID + q.n_rb) * prefix::RB;
     t.pre_o = c.take<float>(rows * d.t3);
     t.pre_ml = c.take<float>(rows * 2);
-    t.pre_k = c.take<bf16>(rotated ? 2 * (size_t)q.n_kt * prefix::TK * d.r3 : 0);
+    const size_t pre = (size_t)q.n_kt * prefix::TK;
+    t.pre_k = c.take<bf16>(rotated ? 2 * pre * d.r3 : (q8 ? pre * d.r3 : 0));
+    t.pre_v = q8 ? (one_pool && !rotated ? t.pre_k : c.take<bf16>(pre * d.t3)) : nullptr;
   }
+  t.new_scale = c.take<uint8_t>(q8 ? (size_t)d.B * 2 : 0);
+  t.qmax = c.take<uint32_t>(q8 ? (size_t)d.B * 4 : 0);
   if (w) *w = t;
   return c.off;
 }
@@ -701,6 +711,48 @@ int launch_prefix_ks(Problem& p, const CUtensorMap& tmQ, const CUtensorMap& tmK,
   return p.shared_rope ? launch_prefix_inst<KS, true>(p, tmQ, tmK, tmV, pp, grid) : launch_prefix_inst<KS, false>(p, tmQ, tmK, tmV, pp, grid);
 }
 
+// The same for an 8-bit cache.
+bool tmap_code_pages(CUtensorMap* m, const void* pool, int r, int n_pages, int page_size) {
+  const uint64_t dims[3] = {(uint64_t)r, (uint64_t)page_size, (uint64_t)n_pages}, str[2] = {(uint64_t)r, (uint64_t)page_size * r};
+  const uint32_t box[3] = {128, (uint32_t)std::min(page_size, 128), 1};
+  return make_tmap(m, pool, 3, dims, str, box, CU_TENSOR_MAP_SWIZZLE_128B, true);
+}
+
+int launch_dec_attn_q8(Problem& p, const FastDecWs& w, int grid) {
+  const tucker_attn_desc& d = p.d;
+  CUtensorMap tmK, tmV;
+  if (!tmap_code_pages(&tmK, p.Kc, d.r3, p.pv.n_pages, p.pv.page_size)) return TA_ERR_CUDA;
+  if (!tmap_code_pages(&tmV, p.Vc, d.t3, p.pv.n_pages, p.pv.page_size)) return TA_ERR_CUDA;
+  decq::Params q;
+  q.B = d.B; q.nH = d.n_H; q.Lmax = p.Lmax; q.r3 = d.r3; q.t3 = d.t3; q.shared_kv = p.shared_kv; q.cache_len = p.cache_len;
+  q.Ks = p.Ks; q.Vs = p.Vs; q.qhat = w.qhat; q.qmax = w.qmax; q.knew = (const uint8_t*)w.knew; q.vnew = (const uint8_t*)w.vnew;
+  q.new_scale = w.new_scale; q.part_o = w.part_o; q.part_ml = w.part_ml; q.err = p.dev_err; q.pv = p.pv; q.seq_cta = w.seq_cta;
+  static PerDeviceFlag attr;
+  TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)decq::k_dec_attn_q8, (int)decq::SMEM_BYTES));
+  prof_begin(p);
+  (void)launch_pdl(decq::k_dec_attn_q8, dim3(grid), dim3(decq::THREADS), decq::SMEM_BYTES, p.stream, tmK, tmV, q);
+  prof_end(p);
+  TA_LAUNCH_CHECK(p);
+  return TA_OK;
+}
+
+// The prefix of an 8-bit cache as bf16 rows in the workspace: exact, and for the kernel that attends to it no more than the
+// rows of all the batch's heads are many (32768 tokens: 8 MB in, 17 MB out and back).
+int launch_prefix_unpack(Problem& p, const FastDecWs& w, const PrefixPlan& q) {
+  const tucker_attn_desc& d = p.d;
+  auto part = [&](const void* codes, const uint8_t* scales, int r, bf16* out, bf16* rot) -> int {
+    const long n = (long)p.prefix_len * (r / 8);
+    (void)launch_pdl(decq::k_prefix_unpack_q8, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, p.stream, (const uint8_t*)codes, scales,
+                     p.prefix_table, p.pv.n_pages, p.pv.page_size, out, rot, (long)q.n_kt * prefix::TK * r, p.prefix_len, r, rope_turns(d),
+                     p.dev_err);
+    TA_LAUNCH_CHECK(p);
+    return TA_OK;
+  };
+  if (p.shared_rope) return part(p.Vc, p.Vs, d.t3, w.pre_v, w.pre_k);
+  const int rc = part(p.Kc, p.Ks, d.r3, w.pre_k, nullptr);
+  return rc || p.shared_kv ? rc : part(p.Vc, p.Vs, d.t3, w.pre_v, nullptr);
+}
+
 // Launched behind the streaming kernel, which does not write anything that it reads and lets it be launched only after
 // it has itself waited for the kernels in front (queries, rotated keys): see ta_prefix_attn.cuh.
 int launch_prefix(Problem& p, const FastDecWs& w, const PrefixPlan& q) {
@@ -709,12 +761,16 @@ int launch_prefix(Problem& p, const FastDecWs& w, const PrefixPlan& q) {
   pp.R = d.B * d.n_H; pp.P = p.prefix_len; pp.r3 = d.r3; pp.t3 = d.t3; pp.n_kt = q.n_kt; pp.n_rb = q.n_rb;
   pp.v = prefix::Rows{p.prefix_table, p.pv.n_pages, p.pv.page_size};
   pp.k = p.shared_rope ? prefix::Rows{nullptr, 2 * q.n_kt, prefix::TK} : pp.v;
+  if (p.q8) {
+    pp.v = prefix::Rows{nullptr, q.n_kt, prefix::TK};
+    if (!p.shared_rope) pp.k = pp.v;
+  }
   pp.part_o = w.pre_o; pp.part_ml = w.pre_ml; pp.err = p.dev_err;
-  const void* keys = p.shared_rope ? w.pre_k : p.Kc;
+  const void *keys = p.shared_rope || p.q8 ? w.pre_k : p.Kc, *values = p.q8 ? w.pre_v : p.Vc;
   CUtensorMap tmQ, tmK, tmV;
   if (!tmap_2d(&tmQ, w.qhat, (uint64_t)d.r3, (uint64_t)2 * pp.R, (uint64_t)d.r3, 64, prefix::TQ)) return TA_ERR_CUDA;
   if (!tmap_pages(&tmK, keys, d.r3, pp.k.n_pages, pp.k.page_size)) return TA_ERR_CUDA;
-  if (!tmap_pages(&tmV, p.Vc, d.t3, pp.v.n_pages, pp.v.page_size)) return TA_ERR_CUDA;
+  if (!tmap_pages(&tmV, values, d.t3, pp.v.n_pages, pp.v.page_size)) return TA_ERR_CUDA;
   switch (d.r3) {
     case 64: return launch_prefix_ks<4>(p, tmQ, tmK, tmV, pp, q.grid);
     case 96: return launch_prefix_ks<6>(p, tmQ, tmK, tmV, pp, q.grid);
@@ -777,9 +833,9 @@ bool fast_paged_supported(const tucker_attn_desc& d, int32_t page_size) {
   return page_ok && fast_decode_supported(d, 0);
 }
 
-size_t fast_decode_workspace(const tucker_attn_desc& d, int32_t) { return carve_fast_dec(d, false, 0, false, nullptr, nullptr); }
-size_t fast_paged_workspace(const tucker_attn_desc& d, int32_t prefix_len, bool one_pool) {
-  return carve_fast_dec(d, true, prefix_len, one_pool && d.rope, nullptr, nullptr);
+size_t fast_decode_workspace(const tucker_attn_desc& d, int32_t) { return carve_fast_dec(d, false, 0, false, false, nullptr, nullptr); }
+size_t fast_paged_workspace(const tucker_attn_desc& d, int32_t prefix_len, bool one_pool, bool q8) {
+  return carve_fast_dec(d, true, prefix_len, one_pool, q8, nullptr, nullptr);
 }
 
 // Launch sequence of one decode step (Eq. 9):
@@ -792,7 +848,7 @@ size_t fast_paged_workspace(const tucker_attn_desc& d, int32_t prefix_len, bool 
 int fast_decode(Problem& p) {
   const tucker_attn_desc& d = p.d;
   FastDecWs w;
-  carve_fast_dec(d, p.paged, p.prefix_len, p.shared_rope, p.ws, &w);
+  carve_fast_dec(d, p.paged, p.prefix_len, p.shared_kv, p.q8, p.ws, &w);
   const float LOG2E = 1.4426950408889634f;
   const int ncol = d.r2 + d.r3 + d.t3;
   const int Mpad = (d.B + 127) / 128 * 128;
@@ -821,22 +877,25 @@ int fast_decode(Problem& p) {
       (void)launch_pdl(kernel, grid, dim3(256), 0, p.stream, w.proj_part, splits, (long)Mpad * ncol, d.n_H, d.r1, d.r2,
                        d.r3, d.t3, (const bf16*)p.C, (const bf16*)p.U1, p.scale * LOG2E, w.qhat, w.knew, w.vnew,
                        (bf16*)p.Kc, (bf16*)p.Vc, p.Lmax, p.cache_len, d.rope, freqs, p.append, p.shared_rope ? 2 : p.shared_kv, p.pv, p.prefix_len,
-                       p.paged ? w.qhat + (size_t)d.B * d.n_H * d.r3 : (bf16*)nullptr, p.dev_err);
+                       p.paged ? w.qhat + (size_t)d.B * d.n_H * d.r3 : (bf16*)nullptr, p.dev_err,
+                       dec::NewRowsQ8{(uint8_t*)w.knew, (uint8_t*)w.vnew, w.new_scale, w.qmax, (uint8_t*)p.Kc, (uint8_t*)p.Vc, p.Ks, p.Vs});
     };
     switch ((d.r2 + 63) / 64) {
-      case 1: launch(dec::k_dec_qhat<1>); break;
-      case 2: launch(dec::k_dec_qhat<2>); break;
-      case 3: launch(dec::k_dec_qhat<3>); break;
-      default: launch(dec::k_dec_qhat<4>); break;
+      case 1: p.q8 ? launch(dec::k_dec_qhat<1, true>) : launch(dec::k_dec_qhat<1, false>); break;
+      case 2: p.q8 ? launch(dec::k_dec_qhat<2, true>) : launch(dec::k_dec_qhat<2, false>); break;
+      case 3: p.q8 ? launch(dec::k_dec_qhat<3, true>) : launch(dec::k_dec_qhat<3, false>); break;
+      default: p.q8 ? launch(dec::k_dec_qhat<4, true>) : launch(dec::k_dec_qhat<4, false>); break;
     }
     TA_LAUNCH_CHECK(p);
   }
   const PrefixPlan pq = p.prefix_len > 0 ? prefix_plan(d, p.prefix_len) : PrefixPlan{0, 0, 0};
-  if (p.prefix_len > 0 && p.shared_rope && (rc = launch_prefix_rotate(p, w, pq))) return rc;
+  if (p.prefix_len > 0 && p.q8 && (rc = launch_prefix_unpack(p, w, pq))) return rc;
+  if (p.prefix_len > 0 && p.shared_rope && !p.q8 && (rc = launch_prefix_rotate(p, w, pq))) return rc;
   // ---- 3: attention over the latent cache ----
   {
     CUtensorMap tmK, tmV;
-    if (p.paged) {
+    if (p.q8) {
+    } else if (p.paged) {
       if (!tmap_pages(&tmK, p.Kc, d.r3, p.pv.n_pages, p.pv.page_size)) return TA_ERR_CUDA;
       if (!tmap_pages(&tmV, p.Vc, d.t3, p.pv.n_pages, p.pv.page_size)) return TA_ERR_CUDA;
     } else {
@@ -848,7 +907,7 @@ int fast_decode(Problem& p) {
     dp.shared_kv = p.shared_kv;
     dp.cache_len = p.cache_len; dp.qhat = w.qhat; dp.knew = w.knew; dp.vnew = w.vnew;
     dp.part_o = w.part_o; dp.part_ml = w.part_ml; dp.err = p.dev_err; dp.seq_cta = w.seq_cta;
-    rc = p.paged ? launch_dec_attn_umma<true>(p, tmK, tmV, dp, dp.grid) : launch_dec_attn_umma<false>(p, tmK, tmV, dp, dp.grid);
+    rc = p.q8 ? launch_dec_attn_q8(p, w, dp.grid) : p.paged ? launch_dec_attn_umma<true>(p, tmK, tmV, dp, dp.grid) : launch_dec_attn_umma<false>(p, tmK, tmV, dp, dp.grid);
     if (rc) return rc;
     // ---- 3b: attention of all rows to the shared prefix ----
     if (p.prefix_len > 0 && (rc = launch_prefix(p, w, pq))) return rc;

@@ -45,6 +45,14 @@ def host(t):
     return t.float().cpu().numpy()
 
 
+def expected_path(st, flags=0):
+    """2 (tensor-core kernels) for the bf16 shapes of the bf16 cache's tensor-core step, one pool with RoPE apart; else 1."""
+    w = st.w
+    ranks = (w.r[2], w.t[2]) in [(128, 128), (64, 64), (96, 96), (128, 64), (64, 128)] and w.r[1] % 32 == 0 and w.t[1] % 32 == 0
+    tc = w.dtype == "bf16" and ranks and w.d_model % 64 == 0 and (st.page in (16, 32, 64) or st.page % 128 == 0)
+    return 2 if tc and not flags & Bd.TA_FLAG_FORCE_GENERIC and not (st.shared and w.rope) else 1
+
+
 def step(st, dev=None, append=True, flags=0, prefix_call=None, **kw):
     """(y, pools after the step)"""
     x, dw, pools, table, lens, ptab = dev or st.device()
@@ -54,6 +62,7 @@ def step(st, dev=None, append=True, flags=0, prefix_call=None, **kw):
         y = Bd.tucker_attn_decode_prefix_q8(x, *dw, *pools, table, lens, ptab if st.P else None, st.P, **args)
     else:
         y = Bd.tucker_attn_decode_paged_q8(x, *dw, *pools, table, lens, **args)
+    assert Bd.last_path() == expected_path(st, flags) or (Bd.last_path() == 3 and not flags)
     assert Bd.last_device_error() == 0
     return y, pools
 
@@ -462,3 +471,116 @@ def test_binding_refusals():
         Bd.tucker_cache_read_paged_q8(K, Ks, V, Vs, table, lens, i32([0, 1, 2]), rows, rows)
     with pytest.raises(ValueError):
         Bd.tucker_cache_store_paged_q8(rows, rows, K, Ks, V, Vs, table, lens, i32([0, 1]))
+
+
+# ---- many tiles per CTA ----------------------------------------------------------------------------------------------
+
+def big_state(shape, lens, page, P=0, rope=True, shared=False, seed=3, gain=1.0, ramp=None):
+    """A state whose pools are made on the device: (x, weights, pools, table, lengths, prefix table), workload."""
+    w = workload(shape, "bf16", rope=rope, shared=shared)
+    wt = {k: W.round_to_storage(v, "bf16") for k, v in W.make_weights(w, core_gain=gain).items()}
+    dw = H.weights_to_device(wt, "bf16")
+    if shared:
+        dw[7] = dw[3]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    need = [-(-(n + 1) // page) for n in lens]
+    pre = -(-P // page)
+    n = sum(need) + pre + 1
+    order = torch.randperm(n, generator=g, device="cuda").to(torch.int32)
+    table = torch.full((len(lens), max(max(need) + 1, -(-32768 // page))), -1, dtype=torch.int32, device="cuda")
+    o = 0
+    for b, m in enumerate(need):
+        table[b, :m] = order[o:o + m]
+        o += m
+    def pool(r):
+        codes = torch.randn(n, page, r, generator=g, device="cuda").mul_(100).clamp_(-448, 448).to(torch.float8_e4m3fn)
+        scales = (torch.randint(-2, 3, (n, page), generator=g, device="cuda") + 120).to(torch.uint8)
+        return codes, scales.view(torch.float8_e8m0fnu)
+    K, Ks = pool(w.r[2])
+    V, Vs = (K, Ks) if shared else pool(w.t[2])
+    if ramp is not None:                             # key sizes grow along every sequence
+        for b, m in enumerate(lens):
+            i = torch.arange(m, device="cuda")
+            e = (ramp[0] + (ramp[1] - ramp[0]) * i.double() / max(m, 1)).round().to(torch.uint8) + 0
+            Ks.view(torch.uint8)[table[b, i // page].long(), i % page] = (e + 120).to(torch.uint8)
+    x = torch.randn(len(lens), w.d_model, generator=g, device="cuda").bfloat16()
+    return (x, dw, (K, Ks, V, Vs), table, i32(lens), order[o:o + pre].contiguous()), w
+
+
+def reference64(state, w, P, stored_k, stored_v):
+    """y in 64 bits on the device; stored_k, stored_v: the new rows as the cache holds them."""
+    x, dw, (K, Ks, V, Vs), table, lens, ptab = state
+    C, U1, U2, U3, Ct, Ut1, Ut2, Ut3 = (t.double() for t in dw)
+    page = K.shape[1]
+    G, Gt = torch.einsum("ha,aqc->hqc", U1, C), torch.einsum("ha,ajc->hjc", Ut1, Ct)
+    def rows(codes, scales, pages, m):
+        i = torch.arange(m, device="cuda")
+        pg = pages[i // page].long()
+        return codes.view(torch.uint8)[pg, i % page].view(torch.float8_e4m3fn).double() * torch.exp2(scales.view(torch.uint8)[pg, i % page].double() - 127)[:, None]
+    def rot(t, pos):
+        r = t.shape[-1]
+        a = pos.double()[:, None] * w.rope_base ** (-torch.arange(0, r, 2, device="cuda", dtype=torch.float64) / r)
+        e, o = t[:, 0::2], t[:, 1::2]
+        return torch.stack((e * a.cos() - o * a.sin(), e * a.sin() + o * a.cos()), -1).flatten(-2)
+    out = []
+    for b, m in enumerate(lens.tolist()):
+        q = torch.einsum("q,hqc->hc", x[b].double() @ U2, G)
+        k = torch.cat((rows(K, Ks, ptab, P), rows(K, Ks, table[b], m), stored_k[b:b + 1]))
+        v = torch.cat((rows(V, Vs, ptab, P), rows(V, Vs, table[b], m), stored_v[b:b + 1]))
+        if w.rope:
+            q = rot(q, torch.full((w.n_H,), P + m, device="cuda"))
+            if w.shared_kv:
+                k = rot(k, torch.arange(len(k), device="cuda"))
+        p = torch.softmax(q @ k.T * (w.d_model / w.n_H) ** -0.5, -1)
+        out.append(Ut2 @ torch.einsum("hjc,hc->j", Gt, p @ v))
+    return torch.stack(out).cpu().numpy()
+
+
+LONG = [("one sequence over all CTAs", TC128, [60000], 64),
+        ("odd numbers of tiles, ends inside pages", TC64, [20011, 127, 128, 129, 0, 40000, 255, 256, 9999], 16),
+        ("many short sequences per CTA", TC96, [(37 * i) % 300 for i in range(1500)], 16),
+        ("one tile each, several per CTA", TC_KV, [(11 * i) % 128 for i in range(900)], 128),
+        ("two tiles each", TC_VK, [128 + (7 * i) % 100 for i in range(500)], 32),
+        ("ragged batch", TC128, [1000 * (i % 13) + 77 * i for i in range(64)], 256)]
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("what,shape,lens,page", LONG, ids=[c[0] for c in LONG])
+def test_many_tiles(what, shape, lens, page, shared):
+    if shared:
+        shape = {**shape, "t": (shape["t"][0], shape["t"][1], shape["r"][2])}
+    state, w = big_state(shape, lens, page, rope=not shared, shared=shared)
+    x, dw, pools, table, dl, _ = state
+    y = Bd.tucker_attn_decode_paged_q8(x, *dw, *pools, table, dl, n_H=w.n_H, rope=w.rope, rope_base=w.rope_base)
+    assert Bd.last_path() == 2 and Bd.last_device_error() == 0
+    check_against_64(state, w, 0, y, what)
+
+
+def check_against_64(state, w, P_len, y, what):
+    x, dw, pools, table, dl, _ = state
+    n, page = dl.cpu().numpy(), pools[0].shape[1]
+    at = (table.cpu().numpy()[np.arange(len(n)), n // page], n % page)
+    sk, sv = (torch.from_numpy(stored_rows(pools[i], pools[i + 1], at)).cuda() for i in (0, 2))
+    P.check_rows(host(y), reference64(state, w, P_len, sk, sv), "bf16", what)
+
+
+@pytest.mark.parametrize("ramp", [(0, 6), (6, 0)], ids=str)
+def test_many_tiles_scores_that_grow_or_fall(ramp):
+    """Key sizes that change by 2^6 along 20000 tokens: references move late in a segment, accumulators are rescaled, parts of a
+    sequence with maxima far apart are joined."""
+    state, w = big_state(TC128, [20000, 777, 20000], 64, gain=0.25, ramp=ramp)
+    x, dw, pools, table, dl, _ = state
+    y = Bd.tucker_attn_decode_paged_q8(x, *dw, *pools, table, dl, n_H=w.n_H, rope=True, rope_base=w.rope_base)
+    assert Bd.last_device_error() == 0
+    check_against_64(state, w, 0, y, f"ramp {ramp}")
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("rope", [True, False])
+def test_long_prefix(shared, rope):
+    state, w = big_state(TC128 if not shared else {**TC128, "t": (8, 32, 128)}, [0, 300, 4000, 127] * 4, 64, P=20001, rope=rope, shared=shared)
+    x, dw, pools, table, dl, ptab = state
+    y = Bd.tucker_attn_decode_prefix_q8(x, *dw, *pools, table, dl, ptab, 20001, n_H=w.n_H, rope=rope, rope_base=w.rope_base)
+    assert Bd.last_device_error() == 0
+    check_against_64(state, w, 20001, y, "long prefix")
