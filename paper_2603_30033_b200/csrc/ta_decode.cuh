@@ -35,7 +35,8 @@ struct Params {
 };
 
 __device__ __forceinline__ int clamp_len(int L, int Lmax) { return L < 0 ? 0 : (L >= Lmax ? Lmax - 1 : L); }
-__device__ __forceinline__ int tiles_of(int L) { return L / TK + 1; }   // keys 0..L inclusive (L = the new token)
+template <int T = TK>
+__device__ __forceinline__ int tiles_of(int L) { return L / T + 1; }    // of T keys, keys 0..L inclusive (L = the new token)
 
 // First global tile of CTA i when `total` tiles are split over `grid` CTAs.
 __device__ __forceinline__ long cta_first_tile(long i, long total, long grid) { return i * total / grid; }
@@ -44,6 +45,7 @@ __device__ __forceinline__ long cta_first_tile(long i, long total, long grid) { 
 // [lo, hi) = [t * chunk, (t + 1) * chunk); returns the total number of tiles and sets `excl` to the
 // number of tiles before sequence `lo`.  wtot_s needs one slot per warp of the block; contains a
 // __syncthreads.
+template <int T = TK>
 __device__ __forceinline__ long block_tile_scan(const int32_t* __restrict__ cache_len, int B, int Lmax, int& lo,
                                                 int& hi, long& excl, long long* wtot_s) {
   const int nthr = blockDim.x, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, nwarp = (nthr + 31) >> 5;
@@ -51,7 +53,7 @@ __device__ __forceinline__ long block_tile_scan(const int32_t* __restrict__ cach
   lo = min(B, tid * chunk);
   hi = min(B, lo + chunk);
   long long cnt = 0;
-  for (int b = lo; b < hi; ++b) cnt += tiles_of(clamp_len(cache_len[b], Lmax));
+  for (int b = lo; b < hi; ++b) cnt += tiles_of<T>(clamp_len(cache_len[b], Lmax));
   long long incl = cnt;
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {

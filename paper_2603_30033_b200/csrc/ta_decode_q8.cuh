@@ -5,8 +5,9 @@
 // tiles go to the tensor cores as TMA wrote them (kind::f8f6f4), and everything else is arranged around that.
 //
 //   S^T [128 keys x 32 heads] = K_codes * q^T      The query is carried as three e4m3 numbers per coordinate (the rounded
-//       value, the rounded rest, the rest's rounded rest: 2^-12 of it together), which are three products into one
-//       accumulator.  Its own scale is a power of two per sequence.  Two numbers (2^-8) would move scores of a standard
+//       value, the rounded rest, the rest's rounded rest: 2^-12 of it together), 96 columns of one product that are added up
+//       when they are read (as three products into one accumulator the key tile was read three times: at N = 32 an
+//       instruction takes the 40 cycles of its 4 KB of A from shared memory, and the tensor core was the limit).  Its own scale is a power of two per sequence.  Two numbers (2^-8) would move scores of a standard
 //       deviation of 2 by what the rounding of y to bf16 moves the output.
 //   p 2^k' [128 keys x 32 heads]                   A thread owns a key, so the row's scales are two numbers of its own: 2^k
 //       multiplies the scores, 2^k' the weight of the value row, as a term of the exponent.  The sums are of p alone.
@@ -16,49 +17,60 @@
 //       down to 2^-27 of the largest count in full precision or to 2^-28 absolute.  The three are 96 columns of one product
 //       and of the accumulator, and are added up once per segment.
 //
-// Two softmax warpgroups take tiles in turn, each with its own scores, weights, running maxima, sums and accumulator (two of
-// each fit TMEM here), so that a tile's chain of waits has the time of two tiles; the bf16 kernel's warpgroups share every
-// tile.  What agreement on a tile still takes is one vote over a warpgroup: whether any score lies more than 2^15 above its
-// head's reference.  Then, at the first tile of a segment and seldom after, the maxima are taken and the accumulator rescaled.
-// At the end of a (CTA, sequence) segment one warpgroup hands its part to the other through its weights' buffer.
+// Everything goes by steps of 256 keys.  The two softmax warpgroups take a half each, with scores, weights, running maxima, sums
+// and an accumulator of its own (TMEM has room for two of each here; the bf16 kernel's warpgroups share every tile's heads and
+// its accumulator).  What the threads of one have to agree on is one vote per step: whether any score lies more than 2^kTop
+// above its head's reference.  Then, at the first step of a segment and seldom after, the maxima are taken and the accumulator
+// rescaled.  At the end of a (CTA, sequence) segment warpgroup 1 hands its part to warpgroup 0 through its weights' buffer.
 //
-//   warp 0       TMA producer: pages of codes, and their scale bytes by plain bulk copies
-//   warp 1       TMEM allocation, MMA issue: scores two tiles ahead of the values
-//   warps 2, 3   split the next segment's queries; put the new token's row into the tile that holds it
-//   warps 4 + 4 g .. 7 + 4 g   softmax warpgroup g: tiles g, g + 2, ...
-// TMEM columns: S_0 [0, 32), S_1 [32, 64), O_0 [64, 160), O_1 [160, 256).
+//   warp 0       TMA producer of keys and values
+//   warp 1       TMEM allocation, MMA issue of the scores, a step ahead of the values
+//   warp 2       MMA issue of the values; scale bytes
+//   warp 3       splits the next segment's queries; puts the new token's row into the tile that holds it
+//   warps 4 + 4 g .. 7 + 4 g   softmax warpgroup g: keys 128 g .. 128 g + 127 of a step
+// A warp that works alone gets through about a hundred instructions in a thousand cycles, waits and issues among them, and a
+// step of 128 keys was too short for that: with the warpgroups on alternate tiles of 128 keys one warp or another of the
+// first four set the pace (110 to 94 us for 1.3 million keys, whatever was moved from one to another; six of them instead of
+// four took the softmax warps' issue slots and registers, 108 us).
+// TMEM columns: S_0 [0, 96), S_1 [96, 192), O_0 [192, 288), O_1 [288, 384).
 // Every wait is bounded (Abort).
 #pragma once
 
 #include "ta_common.cuh"
 #include "ta_decode.cuh"
 #include "ta_decode_umma.cuh"
+#include "ta_prefix_attn.cuh"
 #include "ta_q8.cuh"
 #include "ta_sm100.cuh"
 
 #include <cuda_fp16.h>
+#include <limits.h>
 
 namespace ta {
 namespace decq {
 
 using namespace sm100;
 using decu::ex2;
+using prefix::max3;
 using decu::warp_max;
 
-constexpr int TK = 128;                          // keys per tile
+constexpr int TK = 128, SK = 2 * TK;             // keys of a warpgroup, of a step
 constexpr int NWG = 2, THREADS = 128 + 128 * NWG;
 constexpr int NH = 32;                           // head columns
-constexpr int TILE_BYTES = TK * 128;             // rows of 128 bytes, the last of them zeros where a rank is smaller
-constexpr int RING_BYTES = 10 * TILE_BYTES;      // five K + V stages, or ten of one shared pool
-constexpr int MAX_STAGES = 10;
-constexpr int PIECES = 3;
+constexpr int STEP_BYTES = SK * 128;             // rows of 128 bytes, the last of them zeros where a rank is smaller
+// Keys and values in rings of their own: keys are done with when their scores are, values a softmax later.
+constexpr int K_STAGES = 2, V_STAGES = 3;
+constexpr int MAX_STAGES = K_STAGES + V_STAGES;  // of one shared pool, whose rows are both
+constexpr int RING_BYTES = MAX_STAGES * STEP_BYTES;
+constexpr int PIECES = 3, PC = PIECES * NH;      // columns of a product
+constexpr uint32_t TMEM_COLS = 512, TMEM_O = NWG * PC;
 constexpr int QPIECE_BYTES = NH * 128, QBUF_BYTES = PIECES * QPIECE_BYTES;
 constexpr int PBUF_BYTES = TK * 128;             // a key's 96 weights in a row of 128 bytes
-constexpr int SCALE_BYTES = 2 * TK;              // of a stage
-// ring | queries of two segments | weights of two tiles | scales
-constexpr size_t SMEM_BYTES = 1024 + (size_t)RING_BYTES + 2 * QBUF_BYTES + 2 * PBUF_BYTES + MAX_STAGES * SCALE_BYTES;
-static_assert(SMEM_BYTES <= 225 * 1024, "one CTA's shared memory, with the static part");
-constexpr float kTop = 15.f, kStart = 11.f;      // weights reach 2^kTop at most, the largest is 2^kStart when a reference is set
+constexpr int S_SLOTS = 4, S_AHEAD = 3;          // steps whose scale bytes have a place (a power of two), how far they run ahead
+// rings | queries of two segments | weights of two warpgroups | scales
+constexpr size_t SMEM_BYTES = 1024 + (size_t)RING_BYTES + 2 * QBUF_BYTES + 2 * PBUF_BYTES + S_SLOTS * 2 * SK;
+static_assert(SMEM_BYTES <= 224 * 1024, "one CTA's shared memory, with the static part");
+constexpr float kTop = 15.f, kStart = 5.f;      // weights reach 2^kTop at most, the largest is 2^kStart when a reference is set
 
 struct Params {
   int B, nH, Lmax, r3, t3;
@@ -90,76 +102,162 @@ __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t adesc, uint64_
       ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc)
       : "memory");
 }
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
-}
 // 16-byte chunk of a row of 128 bytes, 128-byte swizzle
 __device__ __forceinline__ uint32_t swz(int row, int chunk) { return (uint32_t)(row * 128 + ((chunk ^ (row & 7)) << 4)); }
 
-// Sums of v[h] over the 32 lanes of the warp; lane h returns that of v[h].  At each level a lane hands half of its values on.
-__device__ __forceinline__ float lane_sums(float (&v)[32]) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int half = 16; half >= 1; half >>= 1) {
-    const bool up = lane & half;
-#pragma unroll
-    for (int i = 0; i < half; ++i) {
-      const float mine = up ? v[i + half] : v[i], give = up ? v[i] : v[i + half];
-      v[i] = mine + __shfl_xor_sync(0xffffffffu, give, half);
-    }
-  }
-  return v[0];
+// pairs of fp32 numbers
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
 }
+__device__ __forceinline__ uint64_t pairu(uint32_t lo, uint32_t hi) { return pack2(__uint_as_float(lo), __uint_as_float(hi)); }
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+
+// Scale bytes of rows that no page holds: they are rows of zeros, with any scale but NaN.
+__device__ __align__(16) const uint8_t g_ones[16] = {127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127};
+
+// This CTA's steps [0, n), sequence by sequence: a segment is its part of one.
+struct Segments {
+  const int32_t* cache_len;
+  int Lmax, n;
+  int b, L, it0, it1, k0;      // sequence, its cached rows; steps [it0, it1); first key
+  bool head, tail;             // the sequence begins / ends (with the new token, key L) in it
+  __device__ void init(const Params& p, long t_begin, int n_, int b0, long first) {
+    cache_len = p.cache_len; Lmax = p.Lmax; n = n_;
+    b = b0;
+    L = dec::clamp_len(cache_len[b], Lmax);
+    const int done = (int)(t_begin - first), left = dec::tiles_of<SK>(L) - done;
+    it0 = 0; it1 = min(n, left);
+    k0 = done * SK;
+    head = done == 0; tail = left <= n;
+  }
+  __device__ bool more() const { return it0 < n; }
+  __device__ void next() {
+    it0 = it1;
+    if (it0 >= n) return;
+    ++b;
+    L = dec::clamp_len(cache_len[b], Lmax);
+    const int nt = dec::tiles_of<SK>(L);
+    it1 = min(n, it0 + nt);
+    k0 = 0;
+    head = true; tail = it0 + nt <= n;
+  }
+  // whether warpgroup 1 has any of the keys of step it
+  __device__ bool both(int it) const { return k0 + (it - it0) * SK + TK <= L; }
+};
+
+// Page entries of a CTA's steps in turn: lane i has box i (a page, or 128 rows of one) of a step.  Without divisions in the loop,
+// which is one warp's chain of instructions.
+struct Place { int pg, in_page, rows; };         // entry, first row in the page, whether the box has cached rows
+struct Lookup {
+  Segments g;
+  const int32_t* entry;                          // this lane's of the next step
+  int it, rows_left, in_page, my_row, page0, in0, L_next;
+  __device__ void init(const Params& p, const Segments& s, int lane) {
+    g = s;
+    it = 0;
+    const int ps = p.pv.page_size, box_rows = min(ps, TK), n_box = SK / box_rows, off = lane * box_rows;
+    my_row = lane < n_box ? off : INT_MAX;
+    page0 = off / ps; in0 = off % ps;
+    rows_left = g.L - g.k0;
+    in_page = (g.k0 + off) % ps;
+    entry = p.pv.table + (long)g.b * p.pv.max_pages + (g.k0 + off) / ps;
+  }
+  __device__ Place next(const Params& p) {
+    Place x{-1, in_page, 0};
+    if (it < g.n) {
+      if (my_row < rows_left) {
+        x.rows = 1;
+        x.pg = *entry;
+      }
+      if (++it == g.it1) {
+        g.next();
+        rows_left = g.L;
+        in_page = in0;
+        entry = p.pv.table + (long)g.b * p.pv.max_pages + page0;
+      } else {
+        const int ps = p.pv.page_size;
+        rows_left -= SK;
+        in_page += SK;
+        if (ps <= TK) { in_page -= SK; entry += SK >> (31 - __clz(ps)); }
+        else if (in_page >= ps) { in_page -= ps; ++entry; }      // a larger page size is a multiple of 128, at least 256
+      }
+    }
+    return x;
+  }
+};
 
 __global__ void __launch_bounds__(THREADS, 1)
 k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const Params p) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t full_bar[MAX_STAGES], empty_bar[MAX_STAGES], patched[MAX_STAGES], q_full[2], q_empty[2];
-  __shared__ uint64_t s_full[NWG], s_free[NWG], p_full[NWG], p_free[NWG], o_read[NWG], handed[NWG], taken[NWG], wg_bar[NWG], wanted;
+  __shared__ uint64_t kfull[K_STAGES], kempty[K_STAGES], vfull[MAX_STAGES], vempty[MAX_STAGES], sfull[S_SLOTS], q_full[2], q_empty[2];
+  __shared__ uint64_t s_full[NWG], s_free[NWG], p_full[NWG], p_free[NWG], o_read[NWG], wg_bar[NWG], handed, taken, wanted, patched;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
   __shared__ float q_scale[8];                   // of segment i at i & 7: the queries are split at most three segments ahead
-  __shared__ uint32_t votes[NWG][2];             // a byte per warp, by parity of the warpgroup's tiles
-  __shared__ float max_s[NWG][4][NH], sum_s[NWG][4][NH], hand_m[NWG][NH], hand_l[NWG][NH];
+  __shared__ uint32_t votes[NWG][2];             // a byte per warp, by parity of the step
+  __shared__ float max_s[NWG][4][NH], sum_s[NWG][4][NH], hand_m[NH], hand_l[NH];
+  __shared__ __align__(16) float up_s[NWG][4][NH];
   __shared__ long long wtot_s[THREADS / 32];
   __shared__ int loc_b;
   __shared__ long long loc_first;
 
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  uint8_t* ring = smem_raw + (base - smem_u32(smem_raw));
-  uint8_t* qbuf = ring + RING_BYTES;
-  uint8_t* pbuf = qbuf + 2 * QBUF_BYTES;
-  uint8_t* scales = pbuf + 2 * PBUF_BYTES;
-  const int STAGES = p.shared_kv ? 10 : 5;
-  const int stage_bytes = p.shared_kv ? TILE_BYTES : 2 * TILE_BYTES;
+  uint8_t* const ring = smem_raw + (base - smem_u32(smem_raw));
+  uint8_t* const qbuf = ring + RING_BYTES;
+  uint8_t* const pbuf = qbuf + 2 * QBUF_BYTES;
+  uint8_t* const scales = pbuf + 2 * PBUF_BYTES;
+  const bool shared = p.shared_kv;
+  const int VS = shared ? MAX_STAGES : V_STAGES;
+  uint8_t* const vring = ring + (shared ? 0 : K_STAGES * STEP_BYTES);      // one shared pool: no ring of keys
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   Abort ab{&abort_flag, p.err};
 
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int s = 0; s < MAX_STAGES; ++s) {
-      mbar_init(&full_bar[s], 1);
-      mbar_init(&empty_bar[s], 1);
-      mbar_init(&patched[s], 2);          // the new token's row is in its place: one arrival per helping warp
+      mbar_init(&vfull[s], 1);
+      mbar_init(&vempty[s], 1);
     }
+    for (int s = 0; s < K_STAGES; ++s) {
+      mbar_init(&kfull[s], 1);
+      mbar_init(&kempty[s], 1);
+    }
+    for (int s = 0; s < S_SLOTS; ++s) mbar_init(&sfull[s], 32);      // one arrival per copying lane, when its bytes are there
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&q_full[i], 2);
+      mbar_init(&q_full[i], 1);
       mbar_init(&q_empty[i], 1);
       mbar_init(&s_full[i], 1);
       mbar_init(&s_free[i], 4);           // the scores are in registers
       mbar_init(&p_full[i], 4);           // the weights are in shared memory
       mbar_init(&p_free[i], 1);           // the product that read them is complete
       mbar_init(&o_read[i], 4);           // the accumulator of a finished segment has been read
-      mbar_init(&handed[i], 4);           // warpgroup i has laid its part of a segment down ...
-      mbar_init(&taken[i], 4);            // ... and the other one has picked it up
       mbar_init(&wg_bar[i], 4);
     }
-    mbar_init(&wanted, 1);                // the next tile with a new token's row has arrived
+    mbar_init(&handed, 4);                // warpgroup 1 has laid its part of a segment down ...
+    mbar_init(&taken, 4);                 // ... and warpgroup 0 has picked it up
+    mbar_init(&wanted, 1);                // the next step with a new token's row has arrived ...
+    mbar_init(&patched, 1);               // ... and the row is in its place
     fence_barrier_init();
   }
   if (warp == 1) {
-    tmem_alloc(&tmem_slot, 256);
+    tmem_alloc(&tmem_slot, TMEM_COLS);
     tmem_relinquish();
   }
   tc_fence_before();
@@ -167,29 +265,35 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
 
-  // ---- this CTA's range of the flat tile list (see k_dec_attn_umma) ----
+  // ---- this CTA's range of the flat list of steps (see k_dec_attn_umma) ----
   int lo, hi;
   long excl;
-  const long total = dec::block_tile_scan(p.cache_len, p.B, p.Lmax, lo, hi, excl, wtot_s);
+  const long total = dec::block_tile_scan<SK>(p.cache_len, p.B, p.Lmax, lo, hi, excl, wtot_s);
   const long parts = min((long)gridDim.x, total);
   const long t_begin = min(dec::cta_first_tile(blockIdx.x, total, parts), total);
   const long t_end = min(dec::cta_first_tile(blockIdx.x + 1, total, parts), total);
   {
     long f = excl;
     for (int b = lo; b < hi; ++b) {
-      const long nt = dec::tiles_of(dec::clamp_len(p.cache_len[b], p.Lmax));
+      const long nt = dec::tiles_of<SK>(dec::clamp_len(p.cache_len[b], p.Lmax));
       if (t_begin >= f && t_begin < f + nt) { loc_b = b; loc_first = f; }
       f += nt;
     }
   }
   __syncthreads();
   const bool have_work = t_begin < t_end;
-  const int n_tiles = (int)(t_end - t_begin);
-  decu::Walk w;
-  if (have_work) w.init(p, t_begin, t_end, loc_b, (long)loc_first);
+  const int n_steps = (int)(t_end - t_begin);
+  Segments sg;
+  if (have_work) sg.init(p, t_begin, n_steps, loc_b, (long)loc_first);
   auto wait_all = [&](uint64_t* bar, uint32_t parity) -> bool {
     const bool good = mbar_wait(bar, parity, ab);
     return __all_sync(0xffffffffu, good);
+  };
+  // Two barriers at once: one after the other, each costs a warp a hundred cycles of its chain even when it is complete.
+  auto wait_both = [&](uint64_t* bar0, uint32_t parity0, uint64_t* bar1, uint32_t parity1) -> bool {
+    const bool r0 = mbar_try_wait(bar0, parity0), r1 = mbar_try_wait(bar1, parity1);
+    if (__all_sync(0xffffffffu, r0 && r1)) return true;
+    return wait_all(bar0, parity0) && wait_all(bar1, parity1);
   };
 
   // 88 x 128 + 208 x 256 = 64512 = 168 x 384 registers, what the CTA was launched with
@@ -199,164 +303,179 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
     // ------------------------------- TMA producer -------------------------------
     if (elect_one()) { tma_prefetch_desc(&tmK); tma_prefetch_desc(&tmV); }
     __syncwarp();
-    const int ps = p.pv.page_size;
-    const int box_rows = ps < TK ? ps : TK, n_box = TK / box_rows, kinds = p.shared_kv ? 1 : 2;
-    // page of box `lane` of the tile that ww is positioned on; -1 where the box holds no cached row
-    auto lookup = [&](const decu::Walk& ww, long t) -> int {
-      const int r = ww.k0(t) + lane * box_rows;
-      return (lane < n_box && r < ww.L) ? p.pv.table[(long)ww.b * p.pv.max_pages + r / ps] : -1;
-    };
-    struct Box { int pg, in_page; uint32_t bytes; bool mine, good; };
-    auto box_of = [&](const decu::Walk& ww, long t, int pg) -> Box {
-      const int row = ww.k0(t) + lane * box_rows;
-      Box x;
-      x.mine = lane < n_box && row < ww.L;
-      x.good = x.mine && pg >= 0 && pg < p.pv.n_pages;
-      if (x.mine && !x.good) {
+    const int box_rows = min(p.pv.page_size, TK);
+    Lookup look;
+    look.init(p, sg, lane);
+    Place cur = look.next(p);
+    int n = 0, sk = 0, sv = 0;                     // steps requested so far; stages, and the parities that their release has
+    uint32_t k_par = 1, v_par = 1;
+    auto request = [&](bool wait) -> bool {        // the next step
+      const Place nxt = look.next(p);              // on its way while this step's stages are waited for
+      int pg = cur.pg;
+      if (cur.rows && (pg < 0 || pg >= p.pv.n_pages)) {
         atomicOr(p.err, (unsigned)TA_DEVERR_BAD_PAGE);
         pg = p.pv.n_pages;                         // outside the tensor: the box is filled with zeros
       }
-      x.pg = pg;
-      x.in_page = row % ps;
-      x.bytes = (uint32_t)(__popc(__ballot_sync(0xffffffffu, x.mine)) * kinds * box_rows * 128 +
-                           __popc(__ballot_sync(0xffffffffu, x.good)) * kinds * box_rows);
-      return x;
-    };
-    auto load_tile = [&](const Box& x, int s) {
-      uint8_t* sc = scales + s * SCALE_BYTES + lane * box_rows;
-      if (x.mine && !x.good)                       // rows of zeros: any scale but NaN
-        for (int i = 0; i < box_rows; i += 16)
-          for (int k = 0; k < kinds; ++k) *reinterpret_cast<uint4*>(sc + k * TK + i) = make_uint4(0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu);
-      __syncwarp();
-      if (lane == 0) mbar_expect_tx(&full_bar[s], x.bytes);
-      __syncwarp();
-      if (x.mine) {
-        uint8_t* kt = ring + (size_t)s * stage_bytes + lane * box_rows * 128;
-        tma_load_3d(kt, &tmK, &full_bar[s], 0, x.in_page, x.pg);
-        if (kinds == 2) tma_load_3d(kt + TILE_BYTES, &tmV, &full_bar[s], 0, x.in_page, x.pg);
-        if (x.good) {
-          const long at = (long)x.pg * ps + x.in_page;
-          bulk_load(sc, p.Ks + at, box_rows, &full_bar[s]);
-          if (kinds == 2) bulk_load(sc + TK, p.Vs + at, box_rows, &full_bar[s]);
-        }
+      const uint32_t bytes = (uint32_t)(__popc(__ballot_sync(0xffffffffu, cur.rows)) * box_rows * 128);
+      if (wait && !(shared ? wait_all(&vempty[sv], v_par) : wait_both(&kempty[sk], k_par, &vempty[sv], v_par))) return false;
+      if (lane == 0) {
+        if (!shared) mbar_expect_tx(&kfull[sk], bytes);
+        mbar_expect_tx(&vfull[sv], bytes);
       }
-    };
-    // A CTA whose tiles all fit into the ring requests them before the wait for the query kernel (see k_dec_attn_umma).
-    decu::Walk wn = w, wp = w;                     // the next tile to be looked up, to be requested
-    const int ahead = n_tiles <= STAGES ? n_tiles : 0;
-    int pg_next = lookup(wn, t_begin);
-    auto request = [&](int i, bool wait) -> bool { // tile i; the page of tile i + 1 is on its way
-      const int pg = pg_next;
-      if (i + 1 < n_tiles) {
-        wn.seek(t_begin + i + 1);
-        pg_next = lookup(wn, t_begin + i + 1);
+      __syncwarp();
+      if (cur.rows) {
+        if (!shared) tma_load_3d(ring + sk * STEP_BYTES + look.my_row * 128, &tmK, &kfull[sk], 0, cur.in_page, pg);
+        tma_load_3d(vring + sv * STEP_BYTES + look.my_row * 128, &tmV, &vfull[sv], 0, cur.in_page, pg);
       }
-      wp.seek(t_begin + i);
-      const Box x = box_of(wp, t_begin + i, pg);
-      const int s = i % STAGES;
-      if (wait && !wait_all(&empty_bar[s], ((i / STAGES) & 1) ^ 1)) return false;
-      load_tile(x, s);
+      ++n;
+      if (++sk == K_STAGES) { sk = 0; k_par ^= 1u; }
+      if (++sv == VS) { sv = 0; v_par ^= 1u; }
+      cur = nxt;
       return true;
     };
+    // A CTA whose steps all fit into the rings requests them before the wait for the query kernel (see k_dec_attn_umma).
+    const int ahead = n_steps <= K_STAGES ? n_steps : 0;
     int it = 0;
-    for (; it < ahead; ++it) (void)request(it, false);
+    for (; it < ahead; ++it) (void)request(false);
     pdl_enter();
-    for (; it < n_tiles; ++it)
-      if (!request(it, true)) break;
-    if (ab.raised()) mbar_drain_ring(full_bar, it, STAGES);      // the copies in flight end before the CTA does
+    for (; it < n_steps; ++it)
+      if (!request(true)) break;
+    if (ab.raised()) {                             // the copies in flight end before the CTA does
+      if (!shared) mbar_drain_ring(kfull, n, K_STAGES);
+      mbar_drain_ring(vfull, n, VS);
+    }
    } else if (have_work && warp == 1) {
-    // ------------------------------- MMA issuer ---------------------------------
+    // ------------------------------- issuer of the scores -----------------------
     pdl_enter();
     if (elect_one()) {
-      const uint32_t idesc_qk = idesc_f8(0, TK, NH);
-      const uint32_t idesc_pv = idesc_f8(1, TK, PIECES * NH) | (1u << 15) | (1u << 16);      // both with their M / N index contiguous
+      const uint32_t idesc_qk = idesc_f8(0, TK, PC);
       const int ksteps = p.r3 / 32;
       const uint64_t dq0 = umma_desc_kmajor_sw128(smem_u32(qbuf));
       const uint64_t dk0 = umma_desc_kmajor_sw128(smem_u32(ring));
-      const uint64_t dv0 = umma_desc_mnmajor_sw128(smem_u32(ring) + (p.shared_kv ? 0u : (uint32_t)TILE_BYTES), TILE_BYTES);
-      const uint64_t dp0 = umma_desc_mnmajor_sw128(smem_u32(pbuf), PBUF_BYTES);
-      const uint64_t stage_step = (uint64_t)(stage_bytes >> 4);
-      uint32_t begun = 0;                          // per warpgroup, 16 bits each: segments in which it has had a tile
-      // the two tiles between score issue and value issue: stage << 1 | first of its warpgroup's in the segment
-      uint32_t h1 = 0, h2 = 0;
-      auto issue_pv = [&](int it, uint32_t code) -> bool {
-        const int g = it & 1, st = (int)(code >> 1);
-        if (!mbar_wait(&p_full[g], (uint32_t)((it >> 1) & 1), ab)) return false;
-        if (code & 1u) {
-          const uint32_t n = (begun >> (16 * g)) & 0xffffu;
-          // the accumulator of the segment before must have been read
-          if (n > 0 && !mbar_wait(&o_read[g], (n - 1) & 1, ab)) return false;
-          begun = (begun & ~(0xffffu << (16 * g))) | (((n == 2 ? 1 : n + 1)) << (16 * g));      // 0, then 1 and 2 in turn
-        }
-        tc_fence_after();
-        const uint64_t dv = dv0 + stage_step * (uint64_t)st, dp = dp0 + (uint64_t)(g * (PBUF_BYTES >> 4));
-        const uint32_t d = tmem + 64u + (uint32_t)g * 96u;
-#pragma unroll
-        for (int ks = 0; ks < TK / 32; ++ks)
-          umma_f8(d, dv + (uint64_t)(ks * 256), dp + (uint64_t)(ks * 256), idesc_pv, (ks != 0 || !(code & 1u)) ? 1u : 0u);
-        umma_commit(&p_free[g]);
-        umma_commit(&empty_bar[st]);
-        return true;
-      };
-      int seg = -1, st = 0, seg_it = 0;
-      uint32_t st_par = 0, pp = 0;                 // parity of the ring; of each stage's patches
+      int sv = 0, sk = 0, seg = 0, n_patch = 0;    // stages
+      uint32_t v_par = 0, k_par = 0;               // parity of the rings
+      uint32_t used = 0, par = 0;                  // per warpgroup, a bit each: any scores before; parity of their being taken
       bool ok = true;
-      for (int it = 0; it < n_tiles + 2 && ok; ++it) {
-        uint32_t code = 0;
-        if (it < n_tiles) {
-          const long t = t_begin + it;
-          const int g = it & 1;
-          w.seek(t);
-          if (w.seg_start(t)) {
-            ++seg;
-            seg_it = it;
-            if (!(ok = mbar_wait(&q_full[seg & 1], (uint32_t)((seg >> 1) & 1), ab))) break;
-          }
-          if (!(ok = mbar_wait(&full_bar[st], st_par, ab))) break;
-          if (w.last_tile(t)) {
+      for (; sg.more() && ok; sg.next(), ++seg) {
+        const uint64_t dq = dq0 + (uint64_t)((seg & 1) * (QBUF_BYTES >> 4));
+        if (!(ok = mbar_wait(&q_full[seg & 1], (uint32_t)((seg >> 1) & 1), ab))) break;
+        for (int it = sg.it0; it < sg.it1; ++it) {
+          const bool last = sg.tail && it == sg.it1 - 1;
+          if (!shared && !(ok = mbar_wait(&kfull[sk], k_par, ab))) break;
+          if ((shared || last) && !(ok = mbar_wait(&vfull[sv], v_par, ab))) break;
+          if (last) {
             mbar_arrive(&wanted);
-            if (!(ok = mbar_wait(&patched[st], (pp >> st) & 1u, ab))) break;
-            pp ^= 1u << st;
+            if (!(ok = mbar_wait(&patched, (uint32_t)(n_patch & 1), ab))) break;
+            ++n_patch;
           }
-          // the scores of tile it - 2 are in registers
-          if (it >= 2 && !(ok = mbar_wait(&s_free[g], (uint32_t)(((it >> 1) - 1) & 1), ab))) break;
-          tc_fence_after();
-          const uint64_t dk = dk0 + stage_step * (uint64_t)st, dq = dq0 + (uint64_t)((seg & 1) * (QBUF_BYTES >> 4));
-          const uint32_t d = tmem + (uint32_t)g * 32u;
-#pragma unroll
-          for (int pc = 0; pc < PIECES; ++pc)
+          const uint64_t dk = dk0 + (uint64_t)((shared ? sv : sk) * (STEP_BYTES >> 4));
+          const int nw = sg.both(it) ? 2 : 1;
+          for (int g = 0; g < nw && ok; ++g) {
+            // the step before's scores are in registers
+            if ((used >> g) & 1u) {
+              if (!(ok = mbar_wait(&s_free[g], (par >> g) & 1u, ab))) break;
+              par ^= 1u << g;
+            }
+            used |= 1u << g;
+            tc_fence_after();
+            const uint32_t d = tmem + (uint32_t)(g * PC);
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks)
-              if (ks < ksteps)
-                umma_f8(d, dk + (uint64_t)(ks * 2), dq + (uint64_t)(pc * (QPIECE_BYTES >> 4) + ks * 2), idesc_qk, (pc | ks) != 0 ? 1u : 0u);
-          umma_commit(&s_full[g]);
-          if (w.seg_end(t)) umma_commit(&q_empty[seg & 1]);
-          code = ((uint32_t)st << 1) | (it - seg_it < 2 ? 1u : 0u);
-          if (++st == STAGES) { st = 0; st_par ^= 1u; }
+              if (ks < ksteps) umma_f8(d, dk + (uint64_t)(g * (TK * 128 >> 4) + ks * 2), dq + (uint64_t)(ks * 2), idesc_qk, ks != 0 ? 1u : 0u);
+            umma_commit(&s_full[g]);
+          }
+          if (!ok) break;
+          if (!shared) umma_commit(&kempty[sk]);
+          if (++sv == VS) { sv = 0; v_par ^= 1u; }
+          if (++sk == K_STAGES) { sk = 0; k_par ^= 1u; }
         }
-        if (it >= 2) ok = issue_pv(it - 2, h2);
-        h2 = h1;
-        h1 = code;
+        if (ok) umma_commit(&q_empty[seg & 1]);
       }
     }
-   } else if (have_work) {
-    // ------------------------------- helpers ------------------------------------
-    pdl_enter();
-    const int hid = threadIdx.x - 64;
-    const int nch = p.r3 / 16;                     // 16-byte chunks of a query's codes
-    decu::Walk wq = w;                             // the segment whose queries are split
-    int tq = 0, n_q = 0, n_wanted = 0;
+   } else if (have_work && warp == 2) {
+    // ------------------------------- issuer of the values; scales ---------------
+    // Scale bytes by cp.async, 16 rows of a kind per lane, S_AHEAD steps ahead of the values.  (As bulk copies they took the
+    // producer 700 cycles per 128 keys to issue; as loads into registers, by these lanes or by the softmax threads for
+    // themselves, they were waited for, 1200 cycles.)
+    const int ps = p.pv.page_size, box_rows = min(ps, TK);
+    const int kind = lane >> 4, row = (lane & 15) * 16, box = row / box_rows, in_box = row - box * box_rows;
+    const uint8_t* const pool = (kind == 0 ? p.Ks : p.Vs) + in_box;
+    Lookup look;
+    look.init(p, sg, lane);
+    Place cur = look.next(p);
+    int n_req = 0;
+    auto request = [&]() {                         // of the next step, if there is one
+      if (n_req >= n_steps) return;
+      const Place nxt = look.next(p);
+      const int pg = __shfl_sync(0xffffffffu, cur.pg, box), rows = __shfl_sync(0xffffffffu, cur.rows, box);
+      const int in_page = __shfl_sync(0xffffffffu, cur.in_page, box);
+      const uint8_t* const src = rows && pg >= 0 && pg < p.pv.n_pages ? pool + (long)pg * ps + in_page : g_ones;
+      const int slot = n_req & (S_SLOTS - 1);
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(scales + slot * 2 * SK + kind * SK + row)), "l"(src) : "memory");
+      asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sfull[slot])) : "memory");
+      cur = nxt;
+      ++n_req;
+    };
+    if (n_steps > K_STAGES) pdl_enter();           // see the producer
+    for (int i = 0; i < S_AHEAD; ++i) request();
+    if (n_steps <= K_STAGES) pdl_enter();
+    const uint32_t idesc_pv = idesc_f8(1, TK, PC) | (1u << 15) | (1u << 16);      // both with their M / N index contiguous
+    const uint64_t dv0 = umma_desc_mnmajor_sw128(smem_u32(vring), TK * 128);
+    const uint64_t dp0 = umma_desc_mnmajor_sw128(smem_u32(pbuf), PBUF_BYTES);
+    uint32_t v_par = 0;
+    uint32_t par = 0, used = 0, o_par = 0;         // per warpgroup, a bit each: parity of the weights; any segment before; its accumulator's
+    int sv = 0;
     bool ok = true;
-    auto split_queries = [&]() -> bool {           // of the segment that starts at tile tq
+    for (; sg.more() && ok; sg.next()) {
+      uint32_t begun = 0;                          // ... in this segment
+      for (int it = sg.it0; it < sg.it1 && ok; ++it) {
+        const int nw = sg.both(it) ? 2 : 1;
+        for (int g = 0; g < nw; ++g) {
+          if (g == 0) ok = wait_both(&vfull[sv], v_par, &p_full[0], par & 1u);      // (the patches came before the scores)
+          else ok = wait_all(&p_full[1], par >> 1);
+          if (!ok) break;
+          par ^= 1u << g;
+          const bool first = !((begun >> g) & 1u);
+          if (first && ((used >> g) & 1u)) {
+            // the accumulator of the segment before must have been read
+            if (!(ok = wait_all(&o_read[g], (o_par >> g) & 1u))) break;
+            o_par ^= 1u << g;
+          }
+          begun |= 1u << g;
+          used |= 1u << g;
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t dv = dv0 + (uint64_t)(sv * (STEP_BYTES >> 4) + g * (TK * 128 >> 4)), dp = dp0 + (uint64_t)(g * (PBUF_BYTES >> 4));
+            const uint32_t d = tmem + TMEM_O + (uint32_t)(g * PC);
+#pragma unroll
+            for (int ks = 0; ks < TK / 32; ++ks)
+              umma_f8(d, dv + (uint64_t)(ks * 256), dp + (uint64_t)(ks * 256), idesc_pv, (ks != 0 || !first) ? 1u : 0u);
+            umma_commit(&p_free[g]);
+            if (g == nw - 1) umma_commit(&vempty[sv]);
+          }
+          __syncwarp();
+        }
+        if (++sv == VS) { sv = 0; v_par ^= 1u; }
+        request();                                 // S_AHEAD steps on: into a slot whose step has had its weights taken
+      }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+   } else if (have_work) {
+    // ------------------------------- queries, new rows --------------------------
+    pdl_enter();
+    const int nch = p.r3 / 16;                     // 16-byte chunks of a query's codes
+    Segments sq = sg;                              // the segment whose queries are split next
+    int n_q = 0, n_wanted = 0;
+    bool ok = true;
+    auto split_queries = [&]() -> bool {
       const int qb = n_q & 1;
-      wq.seek(t_begin + tq);
-      const long row0 = (long)wq.b * p.nH;
-      const uint4 mx = *reinterpret_cast<const uint4*>(p.qmax + 4 * (long)wq.b);
+      const long row0 = (long)sq.b * p.nH;
+      const uint4 mx = *reinterpret_cast<const uint4*>(p.qmax + 4 * (long)sq.b);
       const int byte = q8::scale_byte(max(max(mx.x, mx.y), max(mx.z, mx.w)));
       const float inv = q8::inverse(byte);
       if (!wait_all(&q_empty[qb], (uint32_t)(((n_q >> 1) & 1) ^ 1))) return false;
       uint8_t* dst = qbuf + qb * QBUF_BYTES;
-      for (int i = hid; i < NH * nch; i += 64) {
+      for (int i = lane; i < NH * nch; i += 32) {
         const int h = i / nch, ch = i - h * nch;
         uint4 out[PIECES] = {};
         if (h < p.nH && TA_IDX_OK(p.err, (row0 + h) * p.r3 + ch * 16, 16, (long)p.B * p.nH * p.r3)) {
@@ -387,58 +506,57 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
 #pragma unroll
         for (int pc = 0; pc < PIECES; ++pc) *reinterpret_cast<uint4*>(dst + pc * QPIECE_BYTES + swz(h, ch)) = out[pc];
       }
-      if (hid == 0) q_scale[n_q & 7] = q8::scale(byte);
+      if (lane == 0) q_scale[n_q & 7] = q8::scale(byte);
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&q_full[qb]);
       ++n_q;
-      tq = min(n_tiles, (int)(wq.first + wq.nt - t_begin));
+      sq.next();
       return true;
     };
     ok = split_queries();
-    for (int it0 = 0; it0 < n_tiles && ok;) {
-      w.seek(t_begin + it0);
-      const int it1 = min(n_tiles, (int)(w.first + w.nt - t_begin));      // end of the segment
-      if (tq < n_tiles && !(ok = split_queries())) break;
-      const long tl = t_begin + it1 - 1;
-      if (w.last_tile(tl)) {
-        // the tile with the new token: its row, and zeros behind it as values (their weights are zero, but the slots may
-        // hold anything)
-        const int s = (it1 - 1) % STAGES, row = w.L - w.k0(tl);
-        const int kch = p.r3 / 16, vch = p.t3 / 16;
-        uint4 nk = make_uint4(0u, 0u, 0u, 0u);     // lanes 0 .. 7 of the warps: chunks of the key, of the value
-        if (hid < kch) nk = reinterpret_cast<const uint4*>(p.knew + (long)w.b * p.r3)[hid];
-        else if (hid >= 32 && hid - 32 < vch) nk = reinterpret_cast<const uint4*>(p.vnew + (long)w.b * p.t3)[hid - 32];
-        const uint8_t ns = lane == 0 ? p.new_scale[2 * (long)w.b + (warp - 2)] : 0;
-        // (the issuer's word, not full_bar: these warps do not follow the ring, whose rounds they could not tell apart)
-        if (!(ok = wait_all(&wanted, (uint32_t)(n_wanted & 1)))) break;
-        ++n_wanted;
-        uint8_t* kt = ring + (size_t)s * stage_bytes;
-        uint8_t* vt = p.shared_kv ? kt : kt + TILE_BYTES;
-        if (hid < kch && !p.shared_kv) *reinterpret_cast<uint4*>(kt + swz(row, hid)) = nk;
-        if (hid >= 32 && hid - 32 < vch) *reinterpret_cast<uint4*>(vt + swz(row, hid - 32)) = nk;
-        if (lane == 0) scales[s * SCALE_BYTES + (warp - 2) * TK + row] = ns;
-        for (int i = (row + 1) * 8 + hid; i < TK * 8; i += 64) *reinterpret_cast<uint4*>(vt + i * 16) = make_uint4(0u, 0u, 0u, 0u);
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&patched[s]);
-      }
-      it0 = it1;
+    for (; sg.more() && ok; sg.next()) {
+      if (sq.more() && !(ok = split_queries())) break;
+      if (!sg.tail) continue;
+      // the step with the new token: its row, and zeros behind it as values (their weights are zero, but the slots may hold
+      // anything)
+      const int it = sg.it1 - 1, row = sg.L - (sg.k0 + (it - sg.it0) * SK), end = row < TK ? TK : SK;
+      const int kch = p.r3 / 16, vch = p.t3 / 16;
+      uint4 nr = make_uint4(0u, 0u, 0u, 0u);       // lanes 0 .. 7: chunks of the key; 8 .. 15: of the value
+      if (lane < kch) nr = reinterpret_cast<const uint4*>(p.knew + (long)sg.b * p.r3)[lane];
+      else if (lane >= 8 && lane - 8 < vch) nr = reinterpret_cast<const uint4*>(p.vnew + (long)sg.b * p.t3)[lane - 8];
+      const uint8_t ns = lane < 2 ? p.new_scale[2 * (long)sg.b + lane] : 0;
+      // (the issuer's word, not vfull: this warp does not follow the ring, whose rounds it could not tell apart)
+      if (!(ok = wait_all(&wanted, (uint32_t)(n_wanted & 1)))) break;
+      ++n_wanted;
+      const int slot = it & (S_SLOTS - 1);
+      if (!(ok = wait_all(&sfull[slot], (uint32_t)((it / S_SLOTS) & 1)))) break;
+      if (lane < 2) scales[slot * 2 * SK + lane * SK + row] = ns;
+      uint8_t* vt = vring + (size_t)(it % VS) * STEP_BYTES;
+      uint8_t* kt = shared ? vt : ring + (size_t)(it % K_STAGES) * STEP_BYTES;
+      if (lane < kch && !shared) *reinterpret_cast<uint4*>(kt + swz(row, lane)) = nr;
+      if (lane >= 8 && lane - 8 < vch) *reinterpret_cast<uint4*>(vt + swz(row, lane - 8)) = nr;
+#pragma unroll 4
+      for (int i = (row + 1) * 8 + lane; i < end * 8; i += 32) *reinterpret_cast<uint4*>(vt + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&patched);
     }
    }
   } else {
    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
    if (have_work) {
-    pdl_enter();
     // ------------------------------- softmax warpgroups --------------------------
-    const int g = (warp - 4) / 4;               // tiles g, g + 2, ...
+    const int g = (warp - 4) / 4;               // half of every step
     const int q = warp % 4;                     // TMEM lane quadrant
-    const int tid = q * 32 + lane;              // key of a score tile / value coordinate of O^T
+    const int tid = q * 32 + lane;              // key of the half / value coordinate of O^T
     const uint32_t lane_addr = (uint32_t)(q * 32) << 16;
-    const uint32_t tm_s = tmem + (uint32_t)g * 32u + lane_addr, tm_o = tmem + 64u + (uint32_t)g * 96u + lane_addr;
+    const uint32_t tm_s = tmem + (uint32_t)(g * PC) + lane_addr, tm_o = tm_s + TMEM_O;
     uint8_t* const my_p = pbuf + g * PBUF_BYTES;
-    uint32_t wg_phase = 0, pp = 0;              // parity of each stage's patches
-    int n_handed[NWG] = {};                     // parts handed over so far by either warpgroup
+    uint32_t wg_phase = 0, n_mine = 0, n_handed = 0;      // steps in which this warpgroup had keys; parts handed over so far
+    // Code that is new to the SM arrives at 3 bytes per cycle: the first step took 9000 cycles more than the others.  So the loop
+    // runs once on whatever the memories hold, its waits and arrivals left out, while the query kernel is waited for.
+    int warm = 1;
     bool ok = true, owe = false;                // owe: my part lies in the weights' buffer until it is taken
     auto wg_sync = [&]() -> bool {
       __syncwarp();
@@ -448,47 +566,53 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
       return __all_sync(0xffffffffu, good);
     };
     int seg = 0;
-    for (int it0 = 0; it0 < n_tiles && ok; ++seg) {
-      w.seek(t_begin + it0);
-      const int it1 = min(n_tiles, (int)(w.first + w.nt - t_begin));
-      const bool last_seg = w.last_tile(t_begin + it1 - 1);
-      const int mine0 = it0 + ((it0 ^ g) & 1);
-      float m[NH], l[NH], m_lane = -INFINITY;   // reference of head h; sum of this thread's keys; m[lane]
+    for (; sg.more() && ok; sg.next(), ++seg) {
+      uint64_t neg_m[NH / 2], l2[NH / 2];       // pairs of heads: minus the references; sums of this thread's keys
+      float m_lane = 0.f;                       // reference of head `lane`
 #pragma unroll
-      for (int h = 0; h < NH; ++h) { m[h] = -INFINITY; l[h] = 0.f; }
-      int it = mine0;
-      for (; it < it1 && ok; it += 2) {
-        const int st = it % STAGES, j = it >> 1;
-        const bool last = last_seg && it == it1 - 1;
-        if (!(ok = wait_all(&s_full[g], (uint32_t)(j & 1)))) break;
-        // long complete: for the scale bytes, which other proxies and threads wrote
-        if (!(ok = wait_all(&full_bar[st], (uint32_t)((it / STAGES) & 1)))) break;
-        if (last && !(ok = wait_all(&patched[st], (pp >> st) & 1u))) break;
+      for (int h = 0; h < NH / 2; ++h) neg_m[h] = l2[h] = 0;
+      int first = 1;
+#pragma unroll 1
+      for (int it = sg.it0 - warm; it < sg.it1 && ok; ++it) {
+        asm volatile("" : "+r"(first));         // no copy of the loop for the first step
+        if (g == 1 && !warm && !sg.both(it)) break;      // (the last step only)
+        const uint32_t par = n_mine & 1u;
+        const int slot = it & (S_SLOTS - 1);
+        if (!warm && !(ok = wait_both(&sfull[slot], (uint32_t)((it / S_SLOTS) & 1), &s_full[g], par))) break;
         tc_fence_after();
-        uint32_t sr[NH];
-        tmem_ld32(tm_s, sr);
-        const uint8_t* sc = scales + st * SCALE_BYTES + tid;
-        const int kb = sc[0], vb = p.shared_kv ? kb : sc[TK];
-        float kq = q8::scale(kb) * q_scale[seg & 7], ev = vb == q8::kNan ? NAN : (float)(vb - 127);
-        float inv = vb == q8::kNan ? NAN : q8::scale(254 - vb);
+        uint32_t s0[NH], s1[NH], s2[NH];
+        tmem_ld32(tm_s, s0);
+        tmem_ld32(tm_s + NH, s1);
+        tmem_ld32(tm_s + 2 * NH, s2);
+        const uint8_t* sc = scales + slot * 2 * SK + g * TK + tid;
+        const int kb = sc[0], vb = sc[SK];
+        float kq = q8::scale(kb) * q_scale[seg & 7];
+        float ev = vb == q8::kNan ? NAN : (float)(vb - 127), inv = vb == q8::kNan ? NAN : q8::scale(254 - vb);
         tmem_ld_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&s_free[g]);        // the scores of tile it + 2 may overwrite the buffer
-        const bool none = last && w.k0(t_begin + it) + tid > w.L;      // keys past the new token do not exist
-        if (none) { ev = 0.f; inv = 0.f; }
-        float a[NH], over = -INFINITY;                 // log2 of p 2^k'
+        if (lane == 0 && !warm) mbar_arrive(&s_free[g]);       // the next step's scores may overwrite the buffer
+        if (sg.tail && it == sg.it1 - 1 && sg.k0 + (it - sg.it0) * SK + g * TK + tid > sg.L) {
+          // keys past the new token do not exist: weights of zero whatever the scores are
+          ev = -INFINITY; kq = inv = 0.f;
 #pragma unroll
-        for (int h = 0; h < NH; ++h) {
-          a[h] = none ? -INFINITY : fmaf(__uint_as_float(sr[h]), kq, ev);
-          over = fmaxf(over, a[h] - m[h]);
+          for (int h = 0; h < NH; ++h) s0[h] = s1[h] = s2[h] = 0u;
         }
-        const bool vote = __any_sync(0xffffffffu, over > kTop);
-        if (lane == 0) reinterpret_cast<uint8_t*>(&votes[g][j & 1])[q] = vote ? 1 : 0;
+        // log2 of p 2^k', relative to the references
+        const uint64_t kq2 = pack2(kq, kq), ev2 = pack2(ev, ev);
+        float a[NH], over = -INFINITY;
+#pragma unroll
+        for (int h = 0; h < NH; h += 2) {
+          const uint64_t s = add2(add2(pairu(s0[h], s0[h + 1]), pairu(s1[h], s1[h + 1])), pairu(s2[h], s2[h + 1]));
+          unpack2(fma2(s, kq2, add2(ev2, neg_m[h / 2])), a[h], a[h + 1]);
+          over = max3(over, a[h], a[h + 1]);
+        }
+        const bool vote = first || __any_sync(0xffffffffu, over > kTop);
+        if (lane == 0) reinterpret_cast<uint8_t*>(&votes[g][par])[q] = vote ? 1 : 0;
         if (!(ok = wg_sync())) break;
-        bool free_seen = false;
-        if (*reinterpret_cast<volatile uint32_t*>(&votes[g][j & 1]) != 0u) {
-          // ---- new references: the tile's maxima where they are needed ----
+        bool free_seen = n_mine == 0;                  // (warm too) the step before's product has read the weights
+        if (*reinterpret_cast<volatile uint32_t*>(&votes[g][par]) != 0u) {
+          // ---- new references: the maxima of these keys where they are needed ----
           float mine = -INFINITY;
 #pragma unroll
           for (int h = 0; h < NH; ++h) {
@@ -497,42 +621,52 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
           }
           max_s[g][q][lane] = mine;
           if (!(ok = wg_sync())) break;
+          // by how much the reference of head `lane` rises (it is 0 until the first step sets it)
           const float mt = fmaxf(fmaxf(max_s[g][0][lane], max_s[g][1][lane]), fmaxf(max_s[g][2][lane], max_s[g][3][lane]));
-          const bool need = mt - m_lane > kTop;
-          const float m_new = need ? mt - kStart : m_lane;
-          const float f_lane = need ? ex2(m_lane - m_new) : 1.f;       // exp2(-inf) = 0 on the first tile
-          float f[NH];
+          const float up = mt > kTop || first ? mt - kStart : 0.f;
+          m_lane += up;
+          up_s[g][q][lane] = -up;
+          __syncwarp();
+          uint64_t f[NH / 2];
 #pragma unroll
-          for (int h = 0; h < NH; ++h) {
-            f[h] = __shfl_sync(0xffffffffu, f_lane, h);
-            m[h] = __shfl_sync(0xffffffffu, m_new, h);
-            l[h] *= f[h];
+          for (int h = 0; h < NH; h += 4) {
+            const float4 u = *reinterpret_cast<const float4*>(&up_s[g][q][h]);
+            a[h] += u.x; a[h + 1] += u.y; a[h + 2] += u.z; a[h + 3] += u.w;
+            neg_m[h / 2] = add2(neg_m[h / 2], pack2(u.x, u.y));
+            neg_m[h / 2 + 1] = add2(neg_m[h / 2 + 1], pack2(u.z, u.w));
+            f[h / 2] = pack2(ex2(u.x), ex2(u.y));
+            f[h / 2 + 1] = pack2(ex2(u.z), ex2(u.w));
           }
-          m_lane = m_new;
-          if (it > mine0) {
-            // the product of the tile before must be complete before its accumulator is rescaled
-            if (!(ok = wait_all(&p_free[g], (uint32_t)((j - 1) & 1)))) break;
+          if (!first || warm) {
+            // the product of the step before must be complete before its accumulator is rescaled
+            if (!warm && !(ok = wait_all(&p_free[g], par ^ 1u))) break;
             free_seen = true;
             tc_fence_after();
 #pragma unroll
+            for (int h = 0; h < NH / 2; ++h) l2[h] = mul2(l2[h], f[h]);
+#pragma unroll 1
             for (int pc = 0; pc < PIECES; ++pc) {
               uint32_t o[NH];
               tmem_ld32(tm_o + pc * NH, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int h = 0; h < NH; ++h) o[h] = __float_as_uint(__uint_as_float(o[h]) * f[h]);
+              for (int h = 0; h < NH; h += 2) {
+                float x, y;
+                unpack2(mul2(pairu(o[h], o[h + 1]), f[h / 2]), x, y);
+                o[h] = __float_as_uint(x); o[h + 1] = __float_as_uint(y);
+              }
               tmem_st32(tm_o + pc * NH, o);
             }
             tmem_st_wait();
           }
         }
-        // the product of tile it - 2 must have finished reading the weights' buffer, and a part laid down there be taken
-        if (it >= 2 && !free_seen && !(ok = wait_all(&p_free[g], (uint32_t)((j - 1) & 1)))) break;
-        if (owe) {
-          if (!(ok = wait_all(&taken[g], (uint32_t)((n_handed[g] - 1) & 1)))) break;
+        if (!free_seen && !(ok = wait_all(&p_free[g], par ^ 1u))) break;
+        if (owe) {                                     // a part laid down in the weights' buffer must have been taken
+          if (!(ok = wait_all(&taken, (n_handed - 1) & 1u))) break;
           owe = false;
         }
         // ---- weights in three bytes; sums ----
+        const uint64_t inv2 = pack2(inv, inv);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           uint32_t out[PIECES][4];
@@ -542,9 +676,8 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const int h = half * 16 + u * 4 + e * 2;
-              const float w0 = ex2(a[h] - m[h]), w1 = ex2(a[h + 1] - m[h + 1]);
-              l[h] = fmaf(w0, inv, l[h]);
-              l[h + 1] = fmaf(w1, inv, l[h + 1]);
+              const float w0 = ex2(a[h]), w1 = ex2(a[h + 1]);
+              l2[h / 2] = fma2(pack2(w0, w1), inv2, l2[h / 2]);
               const __half2 x = __floats2half2_rn(w0, w1);
               hv[e] = *reinterpret_cast<const uint32_t*>(&x);
 #pragma unroll
@@ -566,84 +699,102 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
           for (int pc = 0; pc < PIECES; ++pc)
             *reinterpret_cast<uint4*>(my_p + swz(tid, pc * 2 + half)) = make_uint4(out[pc][0], out[pc][1], out[pc][2], out[pc][3]);
         }
+        if (warm) {
+          warm = 0;
+          pdl_enter();
+          m_lane = 0.f;
+#pragma unroll
+          for (int h = 0; h < NH / 2; ++h) neg_m[h] = l2[h] = 0;
+          continue;
+        }
         fence_proxy_async_smem();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&p_full[g]);
+        ++n_mine;
+        first = 0;
       }
       if (!ok) break;
-      const int fin = (it1 - 1) & 1;                   // the warpgroup of the last tile finishes the segment
-      const bool two = it1 - it0 >= 2;                 // the other one has a part too
-      if (mine0 < it1) {
-        const int jl = (it - 2) >> 1;
-        if (!(ok = wait_all(&p_free[g], (uint32_t)(jl & 1)))) break;     // the product of my last tile is complete
+      const bool two = sg.both(sg.it0);                // warpgroup 1 has a part too
+      if (g == 0 || two) {
+        if (!(ok = wait_all(&p_free[g], (n_mine - 1) & 1u))) break;      // the product of my last step is complete
         tc_fence_after();
-        float o[NH];
+        // the sums, over the keys of the warpgroup's threads, through its weights' buffer: thread by thread, then a head a lane
         {
-          uint32_t c0[NH], c1[NH];
-          tmem_ld32(tm_o, c0);
-          tmem_ld32(tm_o + NH, c1);
+          uint64_t* const mine = reinterpret_cast<uint64_t*>(my_p + tid * 128);
+#pragma unroll
+          for (int h = 0; h < NH / 2; h += 2) *reinterpret_cast<ulonglong2*>(mine + ((h + 2 * tid) & (NH / 2 - 1))) = make_ulonglong2(l2[h], l2[h + 1]);
+          __syncwarp();
+          float t = 0.f;
+#pragma unroll 4
+          for (int i = q * 32; i < q * 32 + 32; ++i) t += reinterpret_cast<const float*>(my_p + i * 128)[(lane + 4 * i) & (NH - 1)];
+          sum_s[g][q][lane] = t;
+        }
+        if (!(ok = wg_sync())) break;
+        float l_lane = sum_s[g][0][lane] + sum_s[g][1][lane] + sum_s[g][2][lane] + sum_s[g][3][lane];
+        // the accumulator, its three parts added up, [32 heads][32 groups of four coordinates], groups swizzled
+#pragma unroll 1
+        for (int h0 = 0; h0 < NH; h0 += 8) {
+          uint32_t c0[8], c1[8], c2[8];
+          tmem_ld8(tm_o + h0, c0);
+          tmem_ld8(tm_o + NH + h0, c1);
+          tmem_ld8(tm_o + 2 * NH + h0, c2);
           tmem_ld_wait();
 #pragma unroll
-          for (int h = 0; h < NH; ++h) o[h] = __uint_as_float(c0[h]) + __uint_as_float(c1[h]);
-          tmem_ld32(tm_o + 2 * NH, c0);
-          tmem_ld_wait();
-#pragma unroll
-          for (int h = 0; h < NH; ++h) o[h] += __uint_as_float(c0[h]);
+          for (int e = 0; e < 8; ++e)
+            reinterpret_cast<float*>(my_p)[(h0 + e) * 128 + (((tid >> 2) ^ (h0 + e)) << 2) + (tid & 3)] =
+                (__uint_as_float(c0[e]) + __uint_as_float(c1[e])) + __uint_as_float(c2[e]);
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&o_read[g]);        // the next segment may overwrite the accumulator
-        sum_s[g][q][lane] = lane_sums(l);
-        if (!(ok = wg_sync())) break;
-        float l_lane = sum_s[g][0][lane] + sum_s[g][1][lane] + sum_s[g][2][lane] + sum_s[g][3][lane];
-        if (g != fin) {
-          float* part = reinterpret_cast<float*>(my_p);                // [32][128]
-#pragma unroll
-          for (int h = 0; h < NH; ++h) part[h * 128 + tid] = o[h];
-          if (q == 0) { hand_m[g][lane] = m_lane; hand_l[g][lane] = l_lane; }
+        float fm = 1.f, fo = 0.f;                      // of head `lane`: what my part and the other one are multiplied by
+        if (g == 1) {
+          if (q == 0) { hand_m[lane] = m_lane; hand_l[lane] = l_lane; }
+        } else if (two) {
+          if (!(ok = wait_all(&handed, n_handed & 1u))) break;
+          const float mo = hand_m[lane], mn = fmaxf(m_lane, mo);
+          fm = ex2(m_lane - mn); fo = ex2(mo - mn);
+          l_lane = l_lane * fm + hand_l[lane] * fo;
+          m_lane = mn;
+        }
+        if (g == 1) {
           __syncwarp();
-          if (lane == 0) mbar_arrive(&handed[g]);
+          if (lane == 0) mbar_arrive(&handed);
           owe = true;
         } else {
-          if (two) {
-            const int x = g ^ 1;
-            if (!(ok = wait_all(&handed[x], (uint32_t)(n_handed[x] & 1)))) break;
-            const float mo = hand_m[x][lane], mn = fmaxf(m_lane, mo);
-            const float fm = ex2(m_lane - mn), fo = ex2(mo - mn);
-            l_lane = l_lane * fm + hand_l[x][lane] * fo;
-            m_lane = mn;
-            const float* part = reinterpret_cast<const float*>(pbuf + x * PBUF_BYTES);
-#pragma unroll
-            for (int h = 0; h < NH; ++h)
-              o[h] = o[h] * __shfl_sync(0xffffffffu, fm, h) + part[h * 128 + tid] * __shfl_sync(0xffffffffu, fo, h);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&taken[x]);
-          }
-          if (tid == 0) {
-            if (t_begin <= w.first && TA_IDX_OK(p.err, 2 * w.b, 2, 2L * p.B)) p.seq_cta[2 * w.b] = (int)blockIdx.x;
-            if (last_seg && TA_IDX_OK(p.err, 2 * w.b, 2, 2L * p.B)) p.seq_cta[2 * w.b + 1] = (int)blockIdx.x;
-          }
-          const long slot = (long)blockIdx.x + w.b;    // one per (CTA, sequence) pair that can occur
-          if (TA_IDX_OK(p.err, slot, 1, (long)gridDim.x + p.B)) {
-            if (q == 0) reinterpret_cast<float2*>(p.part_ml)[slot * NH + lane] = make_float2(m_lane, l_lane);
-            if (tid < p.t3) {
-              float* dst = p.part_o + slot * NH * p.t3 + (long)(tid / 4) * NH * 4 + tid % 4;
-#pragma unroll
-              for (int h = 0; h < NH; ++h) dst[h * 4] = o[h];
+          // joined and stored by head: lane = head, four coordinates at a time (a thread's own coordinate of one head after
+          // another, 16 adjacent bytes per four lanes, took 5000 cycles)
+          const long slot = (long)blockIdx.x + sg.b;   // one per (CTA, sequence) pair that can occur
+          const bool slot_ok = TA_IDX_OK(p.err, slot, 1, (long)gridDim.x + p.B);
+          if (!(ok = wg_sync())) break;
+          float4* const dst = reinterpret_cast<float4*>(p.part_o + slot * NH * p.t3) + lane;
+          const float4 *const a4 = reinterpret_cast<const float4*>(my_p) + lane * 32, *const b4 = reinterpret_cast<const float4*>(pbuf + PBUF_BYTES) + lane * 32;
+#pragma unroll 2
+          for (int c = q; c < p.t3 / 4; c += 4) {
+            float4 v = a4[c ^ lane];
+            if (two) {
+              const float4 u = b4[c ^ lane];
+              v.x = v.x * fm + u.x * fo; v.y = v.y * fm + u.y * fo; v.z = v.z * fm + u.z * fo; v.w = v.w * fm + u.w * fo;
             }
+            if (slot_ok) dst[c * NH] = v;
           }
+          __syncwarp();
+          if (two && lane == 0) mbar_arrive(&taken);
+          if (tid == 0) {
+            if (sg.head && TA_IDX_OK(p.err, 2 * sg.b, 2, 2L * p.B)) p.seq_cta[2 * sg.b] = (int)blockIdx.x;
+            if (sg.tail && TA_IDX_OK(p.err, 2 * sg.b, 2, 2L * p.B)) p.seq_cta[2 * sg.b + 1] = (int)blockIdx.x;
+          }
+          if (slot_ok && q == 0) reinterpret_cast<float2*>(p.part_ml)[slot * NH + lane] = make_float2(m_lane, l_lane);
         }
       }
-      if (two) ++n_handed[fin ^ 1];
-      if (last_seg) pp ^= 1u << ((it1 - 1) % STAGES);
-      it0 = it1;
+      if (two) ++n_handed;
     }
    }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 1) tmem_dealloc(tmem, 256);
+  if (warp == 1) tmem_dealloc(tmem, TMEM_COLS);
 }
 
 // The prefix that all sequences share, as the attention kernel of all rows reads it: values of the codes, bf16 (exact), row

@@ -100,8 +100,7 @@ struct Walk {
   int b;
   long first, nt;
   int L;
-  template <typename P>      // Params of this kernel or of the 8-bit cache's
-  __device__ void init(const P& p, long tb, long te, int b0, long first0) {
+  __device__ void init(const Params& p, long tb, long te, int b0, long first0) {
     cache_len = p.cache_len; Lmax = p.Lmax; t_begin = tb; t_end = te;
     b = b0; first = first0;
     L = clamp_len(cache_len[b], Lmax);
