@@ -291,11 +291,10 @@ int tucker_attn_decode_paged_q8(const tucker_attn_desc* desc, const void* x, con
                       workspace_bytes, cuda_stream);
 }
 
-static bool append_fast(const tucker_attn_desc& d, const CacheArgs& a) { return !a.q8 && fast_append_supported(d); }
 static size_t append_query(const tucker_attn_desc* desc, const CacheArgs& a, int32_t T) {
   if (!desc_ok(desc, true) || !paged_ok(&a.c, desc->pos0) || T < 0) return 0;
   size_t need = 0;
-  if (T > 0 && append_fast(*desc, a)) need = fast_append_workspace(*desc, T, a.one_pool());
+  if (T > 0 && fast_append_supported(*desc)) need = fast_append_workspace(*desc, T, a.one_pool());
   else if (T > 0 && a.q8) need = generic_q8_append_workspace(*desc, T, a.one_pool());
   return need < 256 ? 256 : need;
 }
@@ -328,7 +327,7 @@ static int append_tokens(const tucker_attn_desc* desc, const void* X, const void
   p.dev_err = device_error_ptr();
   p.prof_start = tl_prof_start; p.prof_stop = tl_prof_stop;
   if (!p.dev_err) return TA_ERR_CUDA;
-  const bool fast = append_fast(*desc, a);
+  const bool fast = fast_append_supported(*desc);
   const int rc = T == 0 ? TA_OK : (fast ? fast_append(p, tok_start, T) : generic_paged_append(p, tok_start, T));
   tl_last_path = fast ? 2 : 1;
   tl_last_launches = p.launches;

@@ -17,9 +17,17 @@
 // Bounds: X read once and the pages written once when T is large; per-CTA bytes of X and the factors over L2 otherwise,
 // which is what the choice of MT, S and the column split minimises (append_plan).
 //   warp 0  TMA producer      warp 1  TMEM, MMA issue      warps 2..9  epilogue, two per TMEM lane quadrant
+//
+// Q8: into an 8-bit cache.  A row's codes wait for the largest number of the whole row, which no thread sees:
+//   S = 1   the two warps of a quadrant, which have every other 32 columns of its rows each, rotate (back into TMEM) and take
+//           maxima first, exchange them through shared memory, and round and store in a second pass over TMEM
+//   S > 1   the CTAs divide the finishing by rows instead of units: a warp adds up the shares of a row of one factor, eight
+//           columns per lane, so that the maximum is a warp's and a row is stored whole (units over the cluster would have had
+//           to meet a second time); the shares come with eight loads of 32 bytes in flight per lane
 #pragma once
 
 #include "ta_paged.cuh"
+#include "ta_q8.cuh"
 #include "ta_sm100.cuh"
 
 namespace ta {
@@ -43,7 +51,8 @@ constexpr int CSU = 2;                           // units per thread whose angle
 
 // A factor [d, width] and where its products go.
 struct Part {
-  bf16* pool;
+  void* pool;         // bf16, Q8: codes
+  uint8_t* scale;     // Q8: scale bytes
   int width;          // r3 or t3, a multiple of 32, at most 256
   int rope;           // 1: rotated before rounding
 };
@@ -68,6 +77,8 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// LG: S = 2^LG, for Q8 (else unused).
+template <bool Q8, int LG>
 __global__ void __launch_bounds__(THREADS, 1)
 k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmB1,
          const Params p, const dec::RopeTurns turns) {
@@ -83,7 +94,7 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
   Abort ab{&abort_flag, p.err};
   // this CTA's parts, their place among a row tile's TMEM columns, and the K blocks of its share of d
   const Part p0 = p.part[blockIdx.y];
-  const Part p1 = p.n_parts > 1 ? p.part[1] : Part{nullptr, 0, 0};
+  const Part p1 = p.n_parts > 1 ? p.part[1] : Part{nullptr, nullptr, 0, 0};
   const int width = p0.width + p1.width;
   const uint32_t c1 = acc_cols(p0.width);                                  // first column of the second part
   const uint32_t tile_cols = c1 + (p1.width ? acc_cols(p1.width) : 0u);
@@ -117,6 +128,10 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
   AppendDst dst[2];
   float2 cs[CSU][UC / 2];
   const int q = warp % 4, hf = (warp - 2) >> 2, rloc = q * 32 + lane;
+  constexpr bool kRows = Q8 && LG > 0;            // this CTA finishes rows instead of units
+  __shared__ uint32_t amax_s[Q8 ? 2 : 1][2][2][BM];      // S = 1: [row tile][part][half of the warps][row]
+  __shared__ AppendDst dst_s[kRows ? BM : 1];     // of this CTA's rows (256 / 2 at most)
+  const int rows_here = min(p.T - m0, MT * BM), row0 = rows_here * s / S, row1 = rows_here * (s + 1) / S;
   if (warp == 0) {
     if (elect_one()) {
       tma_prefetch_desc(&tmX); tma_prefetch_desc(&tmB0); tma_prefetch_desc(&tmB1);
@@ -165,6 +180,10 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
   } else {
     // ------------------------------- epilogue warps -------------------------------
     // while the products run: where this thread's rows go
+    if constexpr (kRows) {
+      const int i = (warp - 2) * 32 + lane;
+      if (row0 + i < row1) dst_s[i] = append_dst(m0 + row0 + i, p.tok_start, p.cache_len, p.B, p.pos0, p.pv, p.err);
+    } else
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       dst[t].row = -1; dst[t].pos = 0;
@@ -173,6 +192,7 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
     }
     // ... and the angles of its first two units, where they are rotated (all of its rotated units, unless r3 > 128 or
     // the CTA finishes two row tiles by itself)
+    if constexpr (!kRows)
 #pragma unroll
     for (int k = 0; k < CSU; ++k) {
       const int u = u0 + hf + 2 * k, t = u / upt, c = (u % upt) * UC;
@@ -201,7 +221,7 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
   if (S > 1) {
     if (warp >= 2 && ok) {
       for (int u = hf; u < units; u += 2) {
-        if ((u >= u0 && u < u1) || !warp_rows(u)) continue;
+        if ((!kRows && u >= u0 && u < u1) || !warp_rows(u)) continue;
         uint32_t r[32];
         tmem_ld32(unit_tmem(u), r);
         tmem_ld_wait();
@@ -216,7 +236,136 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
     __syncwarp();
     cluster_sync();                     // orders the writes above before the reads below, across the cluster
   }
-  if (warp >= 2 && ok) {
+  if constexpr (kRows) {
+    if (warp >= 2 && ok) {
+      constexpr int NB = 8 >> LG;                  // rows of one factor in flight per warp
+      const int n_tasks = (row1 - row0) * p.n_parts, c = lane * 8;
+      for (int t0 = warp - 2; t0 < n_tasks; t0 += 8 * NB) {
+        float4 v[8][2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {              // share i % S of task i / S
+          const int task = t0 + (i >> LG) * 8, r = row0 + task / p.n_parts, pi = p.n_parts > 1 ? task & 1 : 0;
+          const int cc = (pi ? p0.width : 0) + c, u = (r / BM) * upt + cc / UC;
+          const long at = ((long)(i & ((1 << LG) - 1)) * units + u) * (UNIT_BYTES / 16) + (cc % UC) / 4 * BM + r % BM;
+          const bool there = task < n_tasks && c < (pi ? p1.width : p0.width);
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            v[i][e] = there && TA_IDX_OK(p.err, at + e * BM, 1, part_n) ? __ldcg(part + at + e * BM) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const int task = t0 + b * 8, pi = p.n_parts > 1 ? task & 1 : 0;
+          const Part& pt = pi ? p1 : p0;
+          const AppendDst to = dst_s[task < n_tasks ? task / p.n_parts : 0];
+          float2 cs[4];
+          if (pt.rope && c < pt.width)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) cs[e] = dec::rope_at(to.pos, turns, c / 2 + e);
+          float f[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] = 0.f;
+#pragma unroll
+          for (int o = 0; o < (1 << LG); ++o) {    // in the order of the shares of d
+            const float4 x = v[(b << LG) + o][0], y = v[(b << LG) + o][1];
+            f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w; f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
+          }
+          if (pt.rope && c < pt.width)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float xe = f[2 * e], xo = f[2 * e + 1];
+              f[2 * e] = xe * cs[e].x - xo * cs[e].y;
+              f[2 * e + 1] = xe * cs[e].y + xo * cs[e].x;
+            }
+          uint32_t a = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) a = max(a, q8::abs_bits(f[e]));
+          a = __reduce_max_sync(0xffffffffu, a);
+          const int byte = q8::scale_byte(a);
+          if (task < n_tasks && to.row >= 0 && TA_IDX_OK(p.err, to.row, 1, (long)p.pv.n_pages * p.pv.page_size)) {
+            if (c < pt.width) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(pt.pool) + to.row * pt.width + c) = q8::codes8(f, q8::inverse(byte));
+            if (lane == 0) pt.scale[to.row] = (uint8_t)byte;
+          }
+        }
+      }
+    }
+  } else if constexpr (Q8) {
+    // S = 1: this CTA has all columns of its parts
+    uint32_t a[2][2] = {};                         // largest |v| of this thread's columns, by row tile and part
+    auto first_pass = [&](int u, bool have, const float2 (&an)[UC / 2]) {
+      const int t = u / upt, c = (u % upt) * UC;
+      const bool key = c < p0.width;
+      uint32_t r[32], m = 0;
+      tmem_ld32(unit_tmem(u), r);
+      tmem_ld_wait();
+      if (key && p0.rope) {
+        const int pos = (t == 0 ? dst[0] : dst[1]).pos;
+#pragma unroll
+        for (int e = 0; e < UC / 2; ++e) {
+          const float2 cse = have ? an[e] : dec::rope_at(pos, turns, c / 2 + e);
+          const float xe = __uint_as_float(r[2 * e]), xo = __uint_as_float(r[2 * e + 1]);
+          r[2 * e] = __float_as_uint(xe * cse.x - xo * cse.y);
+          r[2 * e + 1] = __float_as_uint(xe * cse.y + xo * cse.x);
+        }
+        tmem_st32(unit_tmem(u), r);
+        tmem_st_wait();
+      }
+#pragma unroll
+      for (int e = 0; e < UC; ++e) m = max(m, r[e] & 0x7fffffffu);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i == t * 2 + (key ? 0 : 1)) a[i >> 1][i & 1] = max(a[i >> 1][i & 1], m);
+    };
+    if (warp >= 2) {
+      if (ok) {
+#pragma unroll
+        for (int k = 0; k < CSU; ++k) {
+          const int u = hf + 2 * k;
+          if (u < units && warp_rows(u)) first_pass(u, true, cs[k]);
+        }
+        for (int u = hf + 2 * CSU; u < units; u += 2)
+          if (warp_rows(u)) first_pass(u, false, cs[0]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) amax_s[i >> 1][i & 1][hf][rloc] = a[i >> 1][i & 1];
+      asm volatile("bar.sync 1, 256;" ::: "memory");     // the eight epilogue warps, whatever became of their waits
+    }
+    if (warp >= 2 && ok) {
+      for (int u = hf; u < units; u += 2) {
+        if (!warp_rows(u)) continue;
+        const int t = u / upt, c = (u % upt) * UC;
+        const bool key = c < p0.width;
+        const Part& pt = key ? p0 : p1;
+        const AppendDst& to = t == 0 ? dst[0] : dst[1];
+        const int byte = q8::scale_byte(max(amax_s[t][key ? 0 : 1][0][rloc], amax_s[t][key ? 0 : 1][1][rloc]));
+        const float inv = q8::inverse(byte);
+        uint32_t r[32];
+        tmem_ld32(unit_tmem(u), r);
+        tmem_ld_wait();
+        const int cc = key ? c : c - p0.width;
+        // 32 codes of the row, through the idle ring: 32 adjacent bytes of sixteen rows per store instruction
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          uint32_t w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int b = e * 16 + i * 4;
+            w[i] = q8::codes4(__uint_as_float(r[b]) * inv, __uint_as_float(r[b + 1]) * inv, __uint_as_float(r[b + 2]) * inv, __uint_as_float(r[b + 3]) * inv);
+          }
+          *reinterpret_cast<uint4*>(ring + u * STAGED_BYTES + e * (BM * 16) + rloc * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        if (cc == 0 && to.row >= 0 && TA_IDX_OK(p.err, to.row, 1, (long)p.pv.n_pages * p.pv.page_size)) pt.scale[to.row] = (uint8_t)byte;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int rr = i * 16 + lane / 2, ch = lane & 1;
+          const long row = __shfl_sync(0xffffffffu, to.row, rr);
+          const uint4 w = *reinterpret_cast<const uint4*>(ring + u * STAGED_BYTES + ch * (BM * 16) + (q * 32 + rr) * 16);
+          if (row >= 0 && TA_IDX_OK(p.err, row * pt.width + cc + ch * 16, 16, (long)p.pv.n_pages * p.pv.page_size * pt.width))
+            *reinterpret_cast<uint4*>(static_cast<uint8_t*>(pt.pool) + row * pt.width + cc + ch * 16) = w;
+        }
+      }
+    }
+  } else if (warp >= 2 && ok) {
     auto finish = [&](int u, bool have, const float2 (&a)[UC / 2]) {
       const int t = u / upt, c = (u % upt) * UC;
       const AppendDst& to = t == 0 ? dst[0] : dst[1];
@@ -264,7 +413,7 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
                        pack_bf16(v[8 * e + 6], v[8 * e + 7]));
       __syncwarp();
       // ... and from there to the pages, the 64 bytes of eight rows per store instruction
-      bf16* pool = first ? p0.pool : p1.pool;
+      bf16* pool = static_cast<bf16*>(first ? p0.pool : p1.pool);
       const int wd = first ? p0.width : p1.width, cc = (first ? c : c - p0.width) + (lane & 3) * 8;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {

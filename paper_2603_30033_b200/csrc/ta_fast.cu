@@ -959,7 +959,7 @@ int fast_append(Problem& p, const int32_t* tok_start, int32_t T) {
   ap.T = T; ap.d = d.d_model; ap.tok_start = tok_start; ap.cache_len = p.cache_len; ap.B = d.B; ap.pos0 = d.pos0;
   ap.pv = p.pv; ap.err = p.dev_err;
   // one pool: the value rows, which are the un-rotated latent rows, are all there is
-  const append::Part keys = {(bf16*)p.Kc, d.r3, d.rope ? 1 : 0}, values = {(bf16*)p.Vc, d.t3, 0};
+  const append::Part keys = {p.Kc, p.Ks, d.r3, d.rope ? 1 : 0}, values = {p.Vc, p.Vs, d.t3, 0};
   ap.part[0] = p.shared_kv ? values : keys;
   ap.part[1] = values;
   const append::Plan plan = plan_append(d, T, p.shared_kv);
@@ -972,8 +972,12 @@ int fast_append(Problem& p, const int32_t* tok_start, int32_t T) {
   if (!tmap_2d(&tm1, p.Ut3, (uint64_t)d.t3, (uint64_t)d.d_model, (uint64_t)d.t3, 64, 64)) return TA_ERR_CUDA;
   if (p.shared_kv) tm0 = tm1;
   else if (!tmap_2d(&tm0, p.U3, (uint64_t)d.r3, (uint64_t)d.d_model, (uint64_t)d.r3, 64, 64)) return TA_ERR_CUDA;
-  static PerDeviceFlag attr;
-  TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)append::k_append, (int)append::SMEM_BYTES));
+  // the kernel: bf16, or an 8-bit cache by the number of shares of d
+  static PerDeviceFlag attr[5];
+  const int which = !p.q8 ? 0 : plan.S == 1 ? 1 : plan.S == 2 ? 2 : plan.S == 4 ? 3 : 4;
+  auto* const kernel = which == 0 ? append::k_append<false, 0> : which == 1 ? append::k_append<true, 0> : which == 2 ? append::k_append<true, 1>
+                       : which == 3 ? append::k_append<true, 2> : append::k_append<true, 3>;
+  TA_CUDA_TRY(ensure_dynamic_smem(attr[which], (const void*)kernel, (int)append::SMEM_BYTES));
   const long tiles = ((long)T + append::BM * plan.MT - 1) / (append::BM * plan.MT);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * plan.S), plan.split_parts ? 2 : 1);
@@ -988,7 +992,7 @@ int fast_append(Problem& p, const int32_t* tok_start, int32_t T) {
   cfg.attrs = la;
   cfg.numAttrs = 2;
   prof_begin(p);
-  (void)cudaLaunchKernelEx(&cfg, append::k_append, tmX, tm0, tm1, ap, rope_turns(d));
+  (void)cudaLaunchKernelEx(&cfg, kernel, tmX, tm0, tm1, ap, rope_turns(d));
   prof_end(p);
   TA_LAUNCH_CHECK(p);
   return TA_OK;

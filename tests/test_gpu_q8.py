@@ -584,3 +584,55 @@ def test_long_prefix(shared, rope):
     y = Bd.tucker_attn_decode_prefix_q8(x, *dw, *pools, table, dl, ptab, 20001, n_H=w.n_H, rope=rope, rope_base=w.rope_base)
     assert Bd.last_device_error() == 0
     check_against_64(state, w, 20001, y, "long prefix")
+
+
+# ---- long appends ----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d,r3,t3,T,one_pool", [(64, 128, 128, 19000, False), (64, 96, 128, 19400, False), (64, 256, 256, 9600, False),
+                                                (64, 224, 224, 19000, True), (64, 32, 256, 5000, False), (1024, 64, 64, 6000, False),
+                                                (4096, 128, 128, 16384, False), (4096, 160, 96, 700, False)])
+@pytest.mark.parametrize("rope", [True, False])
+def test_append_of_long_prompts(d, r3, t3, T, one_pool, rope):
+    """Every division of the work: one CTA for all columns of one or two row tiles, d split over 2, 4 and 8 CTAs, factors apart."""
+    g, base, page = torch.Generator(device="cuda"), 500000.0, 64
+    g.manual_seed(T + r3)
+    lens, new = [70, 0, 5], [T // 3, 1, T - T // 3 - 1]
+    need = [-(-(n + m) // page) for n, m in zip(lens, new)]
+    n_pages = sum(need) + 2
+    order = torch.randperm(n_pages, generator=g, device="cuda").int()
+    table = torch.full((3, max(need)), -3, dtype=torch.int32, device="cuda")
+    for b in range(3):
+        table[b, :need[b]] = order[sum(need[:b]):sum(need[:b + 1])]
+    normal = lambda *s, std=1.0: (torch.randn(*s, generator=g, device="cuda") * std).bfloat16()
+    X, U3 = normal(T + 40, d), normal(d, r3, std=d ** -0.5)
+    X[T:] = float("nan")                                     # rows of nobody behind the last sequence
+    Ut3 = U3 if one_pool else normal(d, t3, std=d ** -0.5)
+    pool = lambda r: (torch.randint(0, 255, (n_pages, page, r), generator=g, device="cuda", dtype=torch.uint8),
+                      torch.randint(0, 255, (n_pages, page), generator=g, device="cuda", dtype=torch.uint8))
+    K, Ks = pool(r3)
+    V, Vs = (K, Ks) if one_pool else pool(t3)
+    before = [t.clone() for t in (K, Ks, V, Vs)]
+    as8 = lambda c, s: (c.view(torch.float8_e4m3fn), s.view(torch.float8_e8m0fnu))
+    start = [0, new[0], new[0] + 1, T]
+    Bd.tucker_cache_append_paged_q8(X, U3, Ut3, *as8(K, Ks), *as8(V, Vs), table, i32(lens), i32(start), rope=rope, rope_base=base)
+    assert Bd.last_device_error() == 0 and Bd.last_path() == 2
+    pos = torch.cat([torch.arange(n, n + m, device="cuda") for n, m in zip(lens, new)])
+    seq = torch.repeat_interleave(torch.arange(3, device="cuda"), torch.tensor(new, device="cuda"))
+    rows = table[seq, pos // page].long() * page + pos % page
+    x = X[:T].double()
+    v64, k64 = x @ Ut3.double(), x @ U3.double()
+    if rope and not one_pool:
+        a = pos.double()[:, None] * base ** (-torch.arange(0, r3, 2, device="cuda", dtype=torch.float64) / r3)
+        e, o = k64[:, 0::2], k64[:, 1::2]
+        k64 = torch.stack((e * a.cos() - o * a.sin(), e * a.sin() + o * a.cos()), -1).flatten(-2)
+    for codes, scales, c0, s0, want in ((K, Ks, *before[:2], v64 if one_pool else k64), (V, Vs, *before[2:], v64)):
+        codes, scales, c0, s0 = codes.view(-1, codes.shape[-1]), scales.view(-1), c0.view(-1, codes.shape[-1]), s0.view(-1)
+        rest = torch.ones(len(s0), dtype=torch.bool, device="cuda")
+        rest[rows] = False
+        assert torch.equal(codes[rest], c0[rest]) and torch.equal(scales[rest], s0[rest])
+        s = torch.exp2(scales[rows].double() - 127)[:, None]
+        got = codes[rows].view(torch.float8_e4m3fn).double() * s
+        top = want.abs().amax(1, keepdim=True)
+        assert (top <= 448 * s * (1 + 5e-5)).all() and ((top >= 224 * s * (1 - 5e-5))).all()
+        bound = torch.maximum(Q.U_E4M3 * want.abs(), 2.0 ** -10 * s) + 1e-4 * top        # see check_pool
+        assert ((got - want).abs() <= bound).all()
