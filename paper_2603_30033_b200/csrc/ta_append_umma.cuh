@@ -21,9 +21,12 @@
 // Q8: into an 8-bit cache.  A row's codes wait for the largest number of the whole row, which no thread sees:
 //   S = 1   the two warps of a quadrant, which have every other 32 columns of its rows each, rotate (back into TMEM) and take
 //           maxima first, exchange them through shared memory, and round and store in a second pass over TMEM
-//   S > 1   the CTAs divide the finishing by rows instead of units: a warp adds up the shares of a row of one factor, eight
-//           columns per lane, so that the maximum is a warp's and a row is stored whole (units over the cluster would have had
-//           to meet a second time); the shares come with eight loads of 32 bytes in flight per lane
+//   S > 1   the CTAs divide the finishing by rows instead of units (units over the cluster would have had to meet a second time).
+//     8       few rows: a warp adds up the shares of a row of one factor, eight columns per lane, so that the maximum is a
+//             warp's and a row is stored whole
+//     2, 4    many rows: each CTA takes whole groups of 32, a warp 32 columns of a group at a time, lane = row, so that the
+//             shares are read 512 adjacent bytes at a time (row by row, 16384 tokens took 63 us); sums wait in the idle ring
+//             for the maxima
 #pragma once
 
 #include "ta_paged.cuh"
@@ -128,9 +131,10 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
   AppendDst dst[2];
   float2 cs[CSU][UC / 2];
   const int q = warp % 4, hf = (warp - 2) >> 2, rloc = q * 32 + lane;
-  constexpr bool kRows = Q8 && LG > 0;            // this CTA finishes rows instead of units
+  constexpr bool kRows = Q8 && LG == 3, kGroups = Q8 && (LG == 1 || LG == 2);      // finished by rows, by groups of 32 rows
   __shared__ uint32_t amax_s[Q8 ? 2 : 1][2][2][BM];      // S = 1: [row tile][part][half of the warps][row]
-  __shared__ AppendDst dst_s[kRows ? BM : 1];     // of this CTA's rows (256 / 2 at most)
+  __shared__ AppendDst dst_s[kRows || kGroups ? BM : 1];     // of the rows that this CTA finishes (256 / 2 at most)
+  __shared__ uint32_t gmax_s[2][kGroups ? BM : 1];           // ... and their largest |v|, by part
   const int rows_here = min(p.T - m0, MT * BM), row0 = rows_here * s / S, row1 = rows_here * (s + 1) / S;
   if (warp == 0) {
     if (elect_one()) {
@@ -183,6 +187,16 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
     if constexpr (kRows) {
       const int i = (warp - 2) * 32 + lane;
       if (row0 + i < row1) dst_s[i] = append_dst(m0 + row0 + i, p.tok_start, p.cache_len, p.B, p.pos0, p.pv, p.err);
+    } else if constexpr (kGroups) {
+      const int i = (warp - 2) * 32 + lane, n = MT * BM >> LG;
+      if (i < n) {
+        const int row = m0 + s * n + i;
+        AppendDst to;
+        to.row = -1; to.pos = 0;
+        if (row < p.T) to = append_dst(row, p.tok_start, p.cache_len, p.B, p.pos0, p.pv, p.err);
+        dst_s[i] = to;
+        gmax_s[0][i] = gmax_s[1][i] = 0;
+      }
     } else
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -192,7 +206,7 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
     }
     // ... and the angles of its first two units, where they are rotated (all of its rotated units, unless r3 > 128 or
     // the CTA finishes two row tiles by itself)
-    if constexpr (!kRows)
+    if constexpr (!kRows && !kGroups)
 #pragma unroll
     for (int k = 0; k < CSU; ++k) {
       const int u = u0 + hf + 2 * k, t = u / upt, c = (u % upt) * UC;
@@ -221,7 +235,7 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
   if (S > 1) {
     if (warp >= 2 && ok) {
       for (int u = hf; u < units; u += 2) {
-        if ((!kRows && u >= u0 && u < u1) || !warp_rows(u)) continue;
+        if ((!kRows && !kGroups && u >= u0 && u < u1) || !warp_rows(u)) continue;
         uint32_t r[32];
         tmem_ld32(unit_tmem(u), r);
         tmem_ld_wait();
@@ -288,6 +302,92 @@ k_append(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtens
         }
       }
     }
+  } else if constexpr (kGroups) {
+    // items (group, 32 columns), dealt to the warps; sums in the ring as [item][column][row]
+    constexpr int N_SH = 1 << LG;
+    const int n_groups = MT * 4 >> LG, items = n_groups * upt;
+    float* const sums = reinterpret_cast<float*>(ring);
+    uint8_t* const stage = ring + 128 * 1024;
+    if (warp >= 2) {
+      if (ok)
+        for (int i = warp - 2; i < items; i += 8) {
+          const int k = i / upt, ul = i - k * upt, grp = s * n_groups + k, c = ul * UC;
+          if (m0 + grp * 32 >= p.T) continue;
+          const bool key = c < p0.width;
+          const long at = (long)((grp / 4) * upt + ul) * (UNIT_BYTES / 16) + (grp % 4) * 32 + lane;
+          float4 v[2][8];
+          float f[UC];
+#pragma unroll
+          for (int o = 0; o < N_SH; o += 2) {      // in the order of the shares of d
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const long w = at + (long)(o + x) * units * (UNIT_BYTES / 16) + e * BM;
+                v[x][e] = TA_IDX_OK(p.err, w, 1, part_n) ? __ldcg(part + w) : make_float4(0.f, 0.f, 0.f, 0.f);
+              }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float4 a = v[0][e], b = v[1][e];
+              if (o == 0) { f[4 * e] = a.x + b.x; f[4 * e + 1] = a.y + b.y; f[4 * e + 2] = a.z + b.z; f[4 * e + 3] = a.w + b.w; }
+              else {
+                f[4 * e] = (f[4 * e] + a.x) + b.x; f[4 * e + 1] = (f[4 * e + 1] + a.y) + b.y;
+                f[4 * e + 2] = (f[4 * e + 2] + a.z) + b.z; f[4 * e + 3] = (f[4 * e + 3] + a.w) + b.w;
+              }
+            }
+          }
+          if (key && p0.rope) {
+            const int pos = dst_s[k * 32 + lane].pos;
+#pragma unroll
+            for (int e = 0; e < UC / 2; ++e) {
+              const float2 cse = dec::rope_at(pos, turns, c / 2 + e);
+              const float xe = f[2 * e], xo = f[2 * e + 1];
+              f[2 * e] = xe * cse.x - xo * cse.y;
+              f[2 * e + 1] = xe * cse.y + xo * cse.x;
+            }
+          }
+          uint32_t m = 0;
+#pragma unroll
+          for (int e = 0; e < UC; ++e) {
+            m = max(m, q8::abs_bits(f[e]));
+            sums[(i * UC + e) * 32 + lane] = f[e];
+          }
+          atomicMax(&gmax_s[key ? 0 : 1][k * 32 + lane], m);
+        }
+      asm volatile("bar.sync 1, 256;" ::: "memory");     // the eight epilogue warps, whatever became of their waits
+    }
+    if (warp >= 2 && ok)
+      for (int i = warp - 2; i < items; i += 8) {
+        const int k = i / upt, ul = i - k * upt, c = ul * UC;
+        if (m0 + (s * n_groups + k) * 32 >= p.T) continue;
+        const bool key = c < p0.width;
+        const Part& pt = key ? p0 : p1;
+        const int cc = key ? c : c - p0.width, byte = q8::scale_byte(gmax_s[key ? 0 : 1][k * 32 + lane]);
+        const float inv = q8::inverse(byte);
+        const long my_row = dst_s[k * 32 + lane].row;
+        uint8_t* const mine = stage + i * 1024;
+        // 32 codes of the row: 32 adjacent bytes of sixteen rows per store instruction
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          uint32_t w[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const float* a = sums + (i * UC + e * 16 + x * 4) * 32 + lane;
+            w[x] = q8::codes4(a[0] * inv, a[32] * inv, a[64] * inv, a[96] * inv);
+          }
+          *reinterpret_cast<uint4*>(mine + e * 512 + lane * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        if (cc == 0 && my_row >= 0 && TA_IDX_OK(p.err, my_row, 1, (long)p.pv.n_pages * p.pv.page_size)) pt.scale[my_row] = (uint8_t)byte;
+        __syncwarp();
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int rr = x * 16 + lane / 2, ch = lane & 1;
+          const long row = __shfl_sync(0xffffffffu, my_row, rr);
+          const uint4 w = *reinterpret_cast<const uint4*>(mine + ch * 512 + rr * 16);
+          if (row >= 0 && TA_IDX_OK(p.err, row * pt.width + cc + ch * 16, 16, (long)p.pv.n_pages * p.pv.page_size * pt.width))
+            *reinterpret_cast<uint4*>(static_cast<uint8_t*>(pt.pool) + row * pt.width + cc + ch * 16) = w;
+        }
+      }
   } else if constexpr (Q8) {
     // S = 1: this CTA has all columns of its parts
     uint32_t a[2][2] = {};                         // largest |v| of this thread's columns, by row tile and part
