@@ -195,8 +195,8 @@ static bool paged_decode_fast(const tucker_attn_desc& d, const CacheArgs& a) {
   return fast_paged_supported(d, a.c.page_size) && !(a.q8 && a.one_pool() && d.rope);
 }
 static bool paged_decode_small(const tucker_attn_desc& d, const CacheArgs& a, int32_t prefix_len) {
-  return !a.q8 && paged_batch_ok(d) && cluster_step_supported(d, a.one_pool()) &&
-         cluster_step_pays(d, paged_slots(a.c), prefix_len, paged_decode_fast(d, a));
+  return paged_batch_ok(d) && cluster_step_supported(d, a.one_pool(), a.q8) &&
+         cluster_step_pays(d, paged_slots(a.c), prefix_len, paged_decode_fast(d, a), a.q8);
 }
 static size_t paged_decode_need(const tucker_attn_desc& d, const CacheArgs& a, int32_t prefix_len) {
   if (!paged_batch_ok(d)) return 0;

@@ -136,8 +136,8 @@ int q8_read_rows(Problem& p, void* Krows, void* Vrows, const int32_t* tok_start,
 
 // Paged decode step of few sequences with short contexts in one launch, both types (ta_paged_cluster.cu); needs no
 // workspace.
-bool cluster_step_supported(const tucker_attn_desc& d, bool one_pool);
-bool cluster_step_pays(const tucker_attn_desc& d, int64_t slots, int32_t prefix_len, bool tensor_cores);
+bool cluster_step_supported(const tucker_attn_desc& d, bool one_pool, bool q8);
+bool cluster_step_pays(const tucker_attn_desc& d, int64_t slots, int32_t prefix_len, bool tensor_cores, bool q8);
 int cluster_paged_decode(Problem& p);
 
 // HOSVD initialiser (ta_hosvd.cu)

@@ -19,7 +19,8 @@
 //      z[j] = sum_a sum_c Ct[a, j, c] u[a, c], received by everybody.
 //   5  y = z Ut2^T: CTA r takes an eighth of the rows.
 // All arithmetic is fp32 from the stored values on (the tensor-core path carries q and z as two bf16 numbers each);
-// only what is stored is rounded.  Sums are taken in a fixed order.  The weights are read once per sequence and the
+// only what is stored is rounded.  Sums are taken in a fixed order.  Over an 8-bit cache (C = e4m3) a key's scale multiplies its
+// scores, a value's scale the weights that its row is taken with; the new token's rows are rounded before they are used.  The weights are read once per sequence and the
 // scores take FMAs, so that this form is for small batches of short contexts only: see cluster_step_pays.
 //
 // Bounded by latency: d 768, 12 heads, ranks 64, one sequence of 37 tokens 11.2 us (19.3 as four launches), of which
@@ -28,8 +29,10 @@
 // overlapped, were 16.3 us.
 #include "ta_paged.cuh"
 #include "ta_cluster.cuh"
+#include "ta_q8.cuh"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ta {
 namespace pgc {
@@ -51,10 +54,12 @@ struct Div {
   __device__ __forceinline__ int operator()(int x) const { return __float2int_rz(((float)x + 0.5f) * inv); }
 };
 
-template <typename T>
+template <typename T, typename Cache>
 struct Params {
   const T *x, *C, *U1, *U2, *U3, *Ct, *Ut1, *Ut2, *Ut3;
-  T *y, *K, *V;
+  T* y;
+  Cache *K, *V;
+  uint8_t *Ks, *Vs;                                    // scale bytes of an 8-bit cache
   PagedView pv;
   const int32_t *cache_len, *prefix_table;
   int B, d, nH, r1, r2, r3, t1, t2, t3, Lmax, P, append, one_pool, rope;
@@ -77,14 +82,14 @@ struct Params {
 };
 
 // Shared memory (offsets in bytes, multiples of 16).
-template <typename T>
+template <typename Cache>
 struct Layout {
   int kp, vp, stage;                                   // bytes of a key row, a value row, a stage of the ring
   int ring, xs, part, q, gat, sum, xq, v, u1, s, orc, mlg, w, oc, u, ut1, zg, total;
   __host__ __device__ Layout(int d, int nH, int r1, int r2, int r3, int t1, int t2, int t3, bool one_pool) {
     const int N = r2 + r3 + t3, nco = (t3 / 8 + CL - 1) / CL;
-    kp = r3 * (int)sizeof(T) + 16;                     // one 16-byte column on per row: 32 rows read at one column hit all banks
-    vp = one_pool ? 0 : t3 * (int)sizeof(T) + 16;
+    kp = r3 * (int)sizeof(Cache) + 16;                 // one 16-byte column on per row: 32 rows read at one column hit all banks
+    vp = one_pool ? 0 : t3 * (int)sizeof(Cache) + 16;
     stage = TK * (kp + vp);
     int off = 0;
     auto take = [&](int floats) { const int o_ = off; off += (floats * 4 + 15) / 16 * 16; return o_; };
@@ -144,6 +149,12 @@ struct Raw8<float> {
     f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
   }
 };
+template <>
+struct Raw8<e4m3> {
+  uint2 a;
+  __device__ __forceinline__ void load(const e4m3* p) { a = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void get(float (&f)[8]) const { q8::values8(a, f); }
+};
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(bf16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
@@ -175,10 +186,11 @@ __device__ __forceinline__ void scores(const char* row, int step, const float* c
   }
 }
 
-template <typename T>
-__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_step(const __grid_constant__ Params<T> p) {
+template <typename T, typename Cache>
+__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_step(const __grid_constant__ Params<T, Cache> p) {
+  constexpr bool kQ8 = std::is_same<Cache, e4m3>::value;
   extern __shared__ __align__(16) char sm[];
-  const Layout<T> lay(p.d, p.nH, p.r1, p.r2, p.r3, p.t1, p.t2, p.t3, p.one_pool);
+  const Layout<Cache> lay(p.d, p.nH, p.r1, p.r2, p.r3, p.t1, p.t2, p.t3, p.one_pool);
   auto at = [&](int off) { return reinterpret_cast<float*>(sm + off); };
   float *const xs = at(lay.xs), *const part = at(lay.part), *const gat = at(lay.gat), *const sum_s = at(lay.sum), *const xq = at(lay.xq);
   float *const v_s = at(lay.v), *const u1_s = at(lay.u1), *const q_s = at(lay.q), *const s_s = at(lay.s), *const orc = at(lay.orc);
@@ -189,6 +201,9 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
   __shared__ float m_s[32], l_s[32], al_s[32];
   __shared__ long dst_s;                               // row of the new token, -1: not written (by this CTA)
   __shared__ long rows_s[2][TK];                       // pool rows of the keys of a tile, -1: none
+  __shared__ float ks_s[kQ8 ? 2 : 1][kQ8 ? TK : 1], vs_s[kQ8 ? 2 : 1][kQ8 ? TK : 1];      // scales of the rows of a tile
+  __shared__ uint32_t code_s[kQ8 ? 2 : 1][32];         // the new token's codes, key and value
+  __shared__ uint8_t byte_s[2];                        // ... and scale bytes
 
   const int b = blockIdx.x / CL, rank = blockIdx.x % CL, tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const int d = p.d, nH = p.nH, r1 = p.r1, r2 = p.r2, r3 = p.r3, t1 = p.t1, t2 = p.t2, t3 = p.t3;
@@ -252,7 +267,8 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
     atomicOr(p.err, (unsigned)TA_DEVERR_BAD_PAGE);
     return -1;
   };
-  const int kc = r3 * (int)sizeof(T) / 16, vc = tp * (int)sizeof(T) / 16;
+  const int kc = r3 * (int)sizeof(Cache) / 16, vc = tp * (int)sizeof(Cache) / 16;
+  int kb_n = 127, vb_n = 127;                          // 8-bit: scale bytes of this thread's key of the tile requested last, on their way
   auto request = [&](int tile) {                       // one commit group per call, also without rows
     if (tile < tiles) {
       char* const st = sm + lay.ring + (tile & 1) * lay.stage;
@@ -266,8 +282,19 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
       for (int c = tid % TPR; c < kc; c += TPR) cp16(st + j * lay.kp + c * 16, k + c * 16, there);
 #pragma unroll 4
       for (int c = tid % TPR; c < vc; c += TPR) cp16(st + TK * lay.kp + j * lay.vp + c * 16, v + c * 16, there);
+      if constexpr (kQ8) {
+        kb_n = vb_n = 127;                             // no row: zeros, with any scale but NaN
+        if (tid < TK) {
+          const long mine = rows_s[tile & 1][tid];
+          if (mine >= 0 && TA_IDX_OK(p.err, mine, 1, rows)) { kb_n = p.Ks[mine]; vb_n = p.Vs[mine]; }
+        }
+      }
     }
     cp_commit();
+  };
+  auto put_scales = [&](int tile) {                    // of the tile requested last
+    if constexpr (kQ8)
+      if (tid < TK) { ks_s[tile & 1][tid] = q8::scale(kb_n); vs_s[tile & 1][tid] = q8::scale(vb_n); }
   };
   // page entries of the first two tiles, and of the new token's row
   int pg0 = 0, in0 = 0;
@@ -340,6 +367,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
     send4(gat + rank * N + c, i % CL, &bar_x, *reinterpret_cast<const float4*>(sum_s + c));
   }
   request(0);
+  put_scales(0);
   request(1);
   bool came = received(&bar_x, p.err);
   for (int c = tid; c < N; c += THREADS) {
@@ -383,7 +411,28 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
     send(dst, (lane & 3) + 4, &bar_v, acc[0]);
   }
   const int vofs = p.one_pool ? r2 : r2 + r3;          // the new value row in xq; the new key, rotated in place, at r2
-  if (p.rope && tid < r3 / 2) {
+  if constexpr (kQ8) {                                 // a warp per row: rotated, rounded, back as the cache holds it
+    if (warp < (p.one_pool ? 1 : 2)) {
+      float* const row = xq + (warp == 0 ? r2 : vofs) + 4 * lane;
+      const int r = warp == 0 ? r3 : t3;
+      float v4[4] = {};
+      if (4 * lane < r)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          const float2 cs = p.rope && warp == 0 ? cs_s[2 * lane + e / 2] : make_float2(1.f, 0.f);
+          v4[e] = row[e] * cs.x - row[e + 1] * cs.y;
+          v4[e + 1] = row[e] * cs.y + row[e + 1] * cs.x;
+        }
+      const uint32_t a = __reduce_max_sync(0xffffffffu, max(max(q8::abs_bits(v4[0]), q8::abs_bits(v4[1])), max(q8::abs_bits(v4[2]), q8::abs_bits(v4[3]))));
+      const int byte = q8::scale_byte(a);
+      const float inv = q8::inverse(byte), sc = q8::scale(byte);
+      const uint32_t codes = q8::codes4(v4[0] * inv, v4[1] * inv, v4[2] * inv, v4[3] * inv);
+      const float2 lo = q8::values2(codes), hi = q8::values2(codes >> 16);
+      if (4 * lane < r) { row[0] = lo.x * sc; row[1] = lo.y * sc; row[2] = hi.x * sc; row[3] = hi.y * sc; }
+      code_s[warp][lane] = codes;
+      if (lane == 0) byte_s[warp] = (uint8_t)byte;
+    }
+  } else if (p.rope && tid < r3 / 2) {
     const float xe = xq[r2 + 2 * tid], xo = xq[r2 + 2 * tid + 1];
     const float2 cs = cs_s[tid];
     xq[r2 + 2 * tid] = xe * cs.x - xo * cs.y;
@@ -432,6 +481,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
     const int here = min(TK, n_keys - t * TK);
     if (t == 0) cp_wait<1>();
     else cp_wait<0>();
+    if (t >= 1) put_scales(t);
     __syncthreads();                                   // the tile is there for all; the one before it is done with
     if (t >= 1) request(t + 1);
     const int i2 = (t + 2) * TK + tid;                 // the tile after the next
@@ -444,7 +494,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
 #pragma unroll
       for (int i = 0; i < 4; ++i) qh[i] = q_s + min(hb + i, nH - 1) * r3;
       float a[2][4];
-      scores<T>(st + lane * lay.kp, 32 * lay.kp, qh, (p.ch3.d * share >> cs_log) * 8, (p.ch3.d * (share + 1) >> cs_log) * 8, a);
+      scores<Cache>(st + lane * lay.kp, 32 * lay.kp, qh, (p.ch3.d * share >> cs_log) * 8, (p.ch3.d * (share + 1) >> cs_log) * 8, a);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (hb + i < nH) {
@@ -463,6 +513,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
         sc[e] = s_s[h * TK + j];
         sc[e] += s_s[(nH + h) * TK + j];
         if (CS > 2) sc[e] += s_s[(2 * nH + h) * TK + j] + s_s[(3 * nH + h) * TK + j];
+        if constexpr (kQ8) sc[e] *= ks_s[t & 1][j];
         if (j >= here) sc[e] = -INFINITY;
         mt = fmaxf(mt, sc[e]);
       }
@@ -473,7 +524,8 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
 #pragma unroll
       for (int e = 0; e < TK / 32; ++e) {
         const float pe = dec::ex2(sc[e] - mr);
-        s_s[h * TK + lane + 32 * e] = pe;
+        if constexpr (kQ8) s_s[h * TK + lane + 32 * e] = lane + 32 * e < here ? pe * vs_s[t & 1][lane + 32 * e] : 0.f;
+        else s_s[h * TK + lane + 32 * e] = pe;
         sum += pe;
       }
 #pragma unroll
@@ -505,9 +557,9 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          Raw8<T> vv;
+          Raw8<Cache> vv;
           float ff[8];
-          vv.load(reinterpret_cast<const T*>(vt + (kb * 4 + k) * vpitch) + vcol);
+          vv.load(reinterpret_cast<const Cache*>(vt + (kb * 4 + k) * vpitch) + vcol);
           vv.get(ff);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -562,8 +614,17 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
   {
     [[maybe_unused]] const long rows = (long)p.pv.n_pages * p.pv.page_size;
     if (dst_s >= 0 && TA_IDX_OK(p.err, dst_s, 1, rows)) {
-      if (tid < t3) put(p.V + dst_s * t3 + tid, xq[vofs + tid]);
-      if (!p.one_pool && tid >= THREADS - r3) put(p.K + dst_s * r3 + tid - (THREADS - r3), xq[r2 + tid - (THREADS - r3)]);
+      if constexpr (kQ8) {
+        const int part = warp;                         // one pool: the key row is the row
+        if (part < (p.one_pool ? 1 : 2)) {
+          const int r = part == 0 ? r3 : t3;
+          if (4 * lane < r) reinterpret_cast<uint32_t*>((part == 0 ? p.K : p.V) + dst_s * r)[lane] = code_s[part][lane];
+          if (lane == 0) (part == 0 ? p.Ks : p.Vs)[dst_s] = byte_s[part];
+        }
+      } else {
+        if (tid < t3) put(p.V + dst_s * t3 + tid, xq[vofs + tid]);
+        if (!p.one_pool && tid >= THREADS - r3) put(p.K + dst_s * r3 + tid - (THREADS - r3), xq[r2 + tid - (THREADS - r3)]);
+      }
     }
   }
   came &= received(&bar_o, p.err);
@@ -677,15 +738,17 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(THREADS, 1) k_pg_st
   }
 }
 
-template <typename T>
+template <typename Cache>
 int smem_bytes(const tucker_attn_desc& d, bool one_pool) {
-  return Layout<T>(d.d_model, d.n_H, d.r1, d.r2, d.r3, d.t1, d.t2, d.t3, one_pool).total;
+  return Layout<Cache>(d.d_model, d.n_H, d.r1, d.r2, d.r3, d.t1, d.t2, d.t3, one_pool).total;
 }
-constexpr int kMaxSmem = 225 * 1024;
+// dynamic shared memory; the 8-bit form has more static (scales), and smaller rows
+template <typename Cache>
+constexpr int kMaxSmem = (std::is_same<Cache, e4m3>::value ? 223 : 225) * 1024;
 
 // Clusters of this kernel that the current device runs at once (one CTA per SM: 15 on B200, whose GPCs are not all
 // multiples of eight SMs), asked once per device; 0: the runtime cannot tell.
-template <typename T>
+template <typename T, typename Cache>
 int clusters_at_once() {
   static std::mutex mu;
   static int known[kMaxDevices] = {};
@@ -696,7 +759,7 @@ int clusters_at_once() {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(CL);
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = kMaxSmem;
+    cfg.dynamicSmemBytes = kMaxSmem<Cache>;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = CL; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
@@ -704,29 +767,29 @@ int clusters_at_once() {
     cfg.numAttrs = 1;
     static PerDeviceFlag attr_smem;
     int n = 0;
-    if (ensure_dynamic_smem(attr_smem, (const void*)k_pg_step<T>, kMaxSmem) != cudaSuccess ||
-        cudaOccupancyMaxActiveClusters(&n, k_pg_step<T>, &cfg) != cudaSuccess)
+    if (ensure_dynamic_smem(attr_smem, (const void*)k_pg_step<T, Cache>, kMaxSmem<Cache>) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, k_pg_step<T, Cache>, &cfg) != cudaSuccess)
       (void)cudaGetLastError();
     known[dev] = n > 0 ? n : -1;
   }
   return std::max(known[dev], 0);
 }
 
-template <typename T>
+template <typename T, typename Cache>
 int launch(Problem& p) {
   const tucker_attn_desc& d = p.d;
-  Params<T> g(d, p.shared_kv);
+  Params<T, Cache> g(d, p.shared_kv);
   g.x = (const T*)p.X; g.C = (const T*)p.C; g.U1 = (const T*)p.U1; g.U2 = (const T*)p.U2; g.U3 = (const T*)p.U3;
   g.Ct = (const T*)p.Ct; g.Ut1 = (const T*)p.Ut1; g.Ut2 = (const T*)p.Ut2; g.Ut3 = (const T*)p.Ut3;
-  g.y = (T*)p.Y; g.K = (T*)p.Kc; g.V = (T*)p.Vc;
+  g.y = (T*)p.Y; g.K = (Cache*)p.Kc; g.V = (Cache*)p.Vc; g.Ks = p.Ks; g.Vs = p.Vs;
   g.pv = p.pv; g.cache_len = p.cache_len; g.prefix_table = p.prefix_table;
   g.B = d.B; g.d = d.d_model; g.nH = d.n_H; g.r1 = d.r1; g.r2 = d.r2; g.r3 = d.r3; g.t1 = d.t1; g.t2 = d.t2; g.t3 = d.t3;
   g.Lmax = p.Lmax; g.P = p.prefix_len; g.append = p.append; g.one_pool = p.shared_kv; g.rope = d.rope;
   g.scale = p.scale; g.turns = rope_turns(d); g.err = p.dev_err;
   static PerDeviceFlag attr;
-  TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)k_pg_step<T>, kMaxSmem));
+  TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)k_pg_step<T, Cache>, kMaxSmem<Cache>));
   prof_begin(p);
-  (void)launch_pdl(k_pg_step<T>, dim3((unsigned)d.B * CL), dim3(THREADS), (size_t)smem_bytes<T>(d, p.shared_kv), p.stream, g);
+  (void)launch_pdl(k_pg_step<T, Cache>, dim3((unsigned)d.B * CL), dim3(THREADS), (size_t)smem_bytes<Cache>(d, p.shared_kv), p.stream, g);
   TA_LAUNCH_CHECK(p);
   prof_end(p);
   return TA_OK;
@@ -734,12 +797,14 @@ int launch(Problem& p) {
 
 }  // namespace pgc
 
-bool cluster_step_supported(const tucker_attn_desc& d, bool one_pool) {
+bool cluster_step_supported(const tucker_attn_desc& d, bool one_pool, bool q8) {
   auto ok8 = [](int r, int most) { return r % 8 == 0 && r <= most; };
   if (!ok8(d.r2, 256) || !ok8(d.t2, 256) || !ok8(d.r3, 128) || !ok8(d.t3, 128) || d.d_model % 8) return false;
   if (d.n_H > 32 || d.r1 > 32 || d.t1 > 32 || (d.flags & TA_FLAG_FORCE_GENERIC)) return false;
   if (one_pool && d.rope) return false;                // the cached rows would have to be rotated
-  return (d.dtype == TA_DTYPE_F32 ? pgc::smem_bytes<float>(d, one_pool) : pgc::smem_bytes<bf16>(d, one_pool)) <= pgc::kMaxSmem;
+  if (q8 && (d.r3 % 16 || d.t3 % 16)) return false;     // rows are copied 16 bytes at a time
+  if (q8) return pgc::smem_bytes<e4m3>(d, one_pool) <= pgc::kMaxSmem<e4m3>;
+  return d.dtype == TA_DTYPE_F32 ? pgc::smem_bytes<float>(d, one_pool) <= pgc::kMaxSmem<float> : pgc::smem_bytes<bf16>(d, one_pool) <= pgc::kMaxSmem<bf16>;
 }
 
 // Whether this form is the faster one, by the longest sequence the table can hold.  All in us, fitted to the device
@@ -752,9 +817,10 @@ bool cluster_step_supported(const tucker_attn_desc& d, bool one_pool) {
 // 19.6; 15 of 2048 19.0 / 27.6; 16 (a second wave) of 1024 27.6 / 23.6; fp32, 1 of 64 12.2 / 31.4, 4 of 2048 19.8 /
 // 41.2, 36 of 8192 146 / 505.
 // d 4096, 32 heads, ranks 128, 4 of 64 keys 25.2 / 27.2, of 1024 33.0 / 27.7.
-bool cluster_step_pays(const tucker_attn_desc& d, int64_t slots, int32_t prefix_len, bool tensor_cores) {
+bool cluster_step_pays(const tucker_attn_desc& d, int64_t slots, int32_t prefix_len, bool tensor_cores, bool q8) {
   const bool f32 = d.dtype == TA_DTYPE_F32;
-  const int at_once = f32 ? pgc::clusters_at_once<float>() : pgc::clusters_at_once<bf16>();
+  const int at_once = q8 ? (f32 ? pgc::clusters_at_once<float, e4m3>() : pgc::clusters_at_once<bf16, e4m3>())
+                         : (f32 ? pgc::clusters_at_once<float, float>() : pgc::clusters_at_once<bf16, bf16>());
   if (at_once == 0) return false;
   const double mb = ((double)d.d_model * (d.r2 + d.r3 + d.t2 + d.t3) + (double)d.r1 * d.r2 * d.r3 + (double)d.t1 * d.t2 * d.t3) * (f32 ? 4e-6 : 2e-6);
   const double keys = (double)slots + prefix_len, w = (double)d.n_H * (d.r3 + d.t3);
@@ -764,6 +830,9 @@ bool cluster_step_pays(const tucker_attn_desc& d, int64_t slots, int32_t prefix_
   return here < there;
 }
 
-int cluster_paged_decode(Problem& p) { return p.d.dtype == TA_DTYPE_F32 ? pgc::launch<float>(p) : pgc::launch<bf16>(p); }
+int cluster_paged_decode(Problem& p) {
+  if (p.q8) return p.d.dtype == TA_DTYPE_F32 ? pgc::launch<float, e4m3>(p) : pgc::launch<bf16, e4m3>(p);
+  return p.d.dtype == TA_DTYPE_F32 ? pgc::launch<float, float>(p) : pgc::launch<bf16, bf16>(p);
+}
 
 }  // namespace ta

@@ -77,6 +77,14 @@ def stored_rows(codes, scales, at):
     return Q.decode(Q.bytes_of(codes)[at]) * 2.0 ** (Q.bytes_of(scales)[at].astype(np.float64) - 127)[:, None]
 
 
+@pytest.mark.parametrize("shape", [SMALL16, TC64, dict(d_model=768, n_H=12, r=(12, 64, 64), t=(12, 64, 64))], ids=str)
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_short_contexts_run_in_one_launch(dtype, shape):
+    for prefix in (0, 100):
+        check_step(Q.Q8State(workload(shape, dtype), [37, 0], 16, P=prefix), what="one launch")
+        assert Bd.last_path() == 3 and Bd.last_launch_count() == 1
+
+
 def check_step(st, flags=0, what="", tol=None, **kw):
     """A step that appends, and one that does not: pools, y against 64 bits on the rows that the cache then holds."""
     y, (K, Ks, V, Vs) = step(st, flags=flags, **kw)
