@@ -191,9 +191,7 @@ int tucker_attn_decode(const tucker_attn_desc* desc, const void* x, const void* 
 }
 
 // Whether a step runs in its one-launch form, which needs no workspace.
-static bool paged_decode_fast(const tucker_attn_desc& d, const CacheArgs& a) {
-  return fast_paged_supported(d, a.c.page_size) && !(a.q8 && a.one_pool() && d.rope);
-}
+static bool paged_decode_fast(const tucker_attn_desc& d, const CacheArgs& a) { return fast_paged_supported(d, a.c.page_size); }
 static bool paged_decode_small(const tucker_attn_desc& d, const CacheArgs& a, int32_t prefix_len) {
   return paged_batch_ok(d) && cluster_step_supported(d, a.one_pool(), a.q8) &&
          cluster_step_pays(d, paged_slots(a.c), prefix_len, paged_decode_fast(d, a), a.q8);

@@ -44,12 +44,20 @@
 // way (3.5e-3 -> 2.1e-3; 3 us of 42 at 24 sequences of up to 3001 tokens).  The two halves share the room of two
 // segments' queries, so that with r3 > 64 one segment's queries are in flight instead of two.
 // Probabilities are rounded to bf16 once (they are an operand of the tensor cores), and the sum is of the rounded ones.
+//
+// Q8 = true (with PAGED and ROT): the pool is in 8 bits.  (8-bit caches that need no rotation have a kernel of their own, which
+// feeds the codes to the tensor cores as they are; here every row passes through the rotation warpgroup anyway.)  That
+// warpgroup multiplies the codes by the row's scale, which is exact in bf16, and besides the rotated key writes the row as a
+// value into one of two bf16 tiles; the stages hold codes and are free again when it has read them.  Everything else is the
+// bf16 pool's.  24 sequences to 3001 tokens: the step takes 34.5 us, on the generic kernels 117, over the bf16 pool 32; what
+// bounds it is the same as there, the rotation warpgroup's work per tile, not the half as many bytes.
 #pragma once
 
 #include <type_traits>
 
 #include "ta_common.cuh"
 #include "ta_decode.cuh"
+#include "ta_q8.cuh"
 #include "ta_sm100.cuh"
 
 namespace ta {
@@ -90,6 +98,7 @@ struct Params {
   PagedView pv;        // PAGED
   int pos_base;        // ROT: position of slot 0
   int* seq_cta;        // PAGED: [B][2] first and last CTA that holds a part of the sequence, for the join
+  const uint8_t *scales, *new_codes, *new_scale;      // Q8: the pool's scale bytes; [B, r3] codes of the new rows; [B][2] their scale bytes
 };
 
 // Walks this CTA's range of the flat tile list, sequence by sequence.
@@ -155,7 +164,7 @@ template <> struct TmemCols<8> {
 template <bool PAGED>
 using RopeTable = typename std::conditional<PAGED, dec::RopeTurns, dec::RopeFreqs>::type;
 
-template <bool ROT, int R3C, bool PAGED>
+template <bool ROT, int R3C, bool PAGED, bool Q8 = false>
 __global__ void __launch_bounds__(ROT ? THREADS_ROT : THREADS, 1)
 k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                 const __grid_constant__ CUtensorMap tmQ, const Params p, const RopeTable<PAGED> freqs) {
@@ -163,6 +172,7 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
   // began: set-up and the tile split run while it finishes, and every role passes pdl_enter() before it
   // touches anything else.  (Requesting the first cache tiles ahead of that wait as well was measured:
   // no gain with two caches, 6 us slower with the shared cache.)
+  static_assert(!Q8 || (ROT && PAGED), "8-bit pools with rotation only");
   constexpr uint32_t TMEM_COLS = ROT ? (PAGED ? 512u : 256u) : 128u;
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full_bar[MAX_STAGES], empty_bar[MAX_STAGES], q_full[2], q_empty[2];
@@ -186,7 +196,9 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
   // With one shared latent cache a stage holds a K tile only: twice the stages.
   // PAGED with ROT: four of them, the last two hold the rotation's table.
   const int STAGES = p.shared_kv ? (ROT && PAGED ? 4 : 6) : 3;
-  const int stage_bytes = p.shared_kv ? MAX_SUB * SUB_BYTES : STAGE_BYTES;
+  const int stage_bytes = Q8 ? SUB_BYTES : p.shared_kv ? MAX_SUB * SUB_BYTES : STAGE_BYTES;
+  // Q8: the value tiles, behind the four stages of codes
+  [[maybe_unused]] uint8_t* const vtiles = ring + 4 * SUB_BYTES;
 
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   Abort ab{&abort_flag, p.err};
@@ -198,7 +210,7 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     abort_flag = 0;
     for (int s = 0; s < MAX_STAGES; ++s) {
       mbar_init(&full_bar[s], 1);
-      mbar_init(&empty_bar[s], 1);
+      mbar_init(&empty_bar[s], Q8 ? 4 : 1);       // Q8: one arrival per rotation warp
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&q_full[i], 1);
@@ -264,7 +276,7 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         return (lane < n_box && r < ww.L) ? p.pv.table[(long)ww.b * p.pv.max_pages + r / ps] : -1;
       };
       const uint32_t box_bytes = (uint32_t)box_rows * 128u;
-      const uint32_t per_page = (uint32_t)(ksub + (p.shared_kv ? 0 : vsub)) * box_bytes;
+      const uint32_t per_page = Q8 ? box_bytes : (uint32_t)(ksub + (p.shared_kv ? 0 : vsub)) * box_bytes;
       // Two steps, so that all arithmetic of a tile lies in front of the wait for its stage: what this lane loads ...
       struct Box { int pg, in_page; uint32_t bytes; bool mine; };
       auto box_of = [&](const Walk& ww, long t, int pg) -> Box {
@@ -287,7 +299,7 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         if (x.mine) {
           uint8_t* kt = ring + (size_t)s * stage_bytes + (size_t)lane * box_bytes;
           uint8_t* vt = kt + MAX_SUB * SUB_BYTES;
-          for (int kk = 0; kk < ksub; ++kk) tma_load_3d(kt + kk * SUB_BYTES, &tmK, &full_bar[s], kk * 64, x.in_page, x.pg);
+          for (int kk = 0; kk < (Q8 ? 1 : ksub); ++kk) tma_load_3d(kt + kk * SUB_BYTES, &tmK, &full_bar[s], kk * 64, x.in_page, x.pg);
           if (!p.shared_kv)
             for (int kk = 0; kk < vsub; ++kk) tma_load_3d(vt + kk * SUB_BYTES, &tmV, &full_bar[s], kk * 64, x.in_page, x.pg);
         }
@@ -391,7 +403,7 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       const uint64_t dq0 = umma_desc_kmajor_sw128(smem_u32(qbuf));
       const uint64_t dp0 = umma_desc_kmajor_sw128(smem_u32(pbuf));
       const uint64_t dk0 = umma_desc_kmajor_sw128(smem_u32(ring));
-      const uint64_t dv0 = umma_desc_mnmajor_sw128(smem_u32(ring) + (p.shared_kv ? 0u : (uint32_t)(MAX_SUB * SUB_BYTES)), SUB_BYTES);
+      const uint64_t dv0 = umma_desc_mnmajor_sw128(Q8 ? smem_u32(vtiles) : smem_u32(ring) + (p.shared_kv ? 0u : (uint32_t)(MAX_SUB * SUB_BYTES)), SUB_BYTES);
       const uint64_t stage_step = (uint64_t)(stage_bytes >> 4);          // descriptor address fields count 16 bytes
       // pending P V products, oldest first; a tile's state in one word: it << 8 | stage << 4 | first tile of its
       // segment
@@ -405,14 +417,14 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         // the accumulator of the previous segment must have been read before it is overwritten
         if (first && sg > 0 && !mbar_wait(&o_read, (uint32_t)((sg - 1) & 1), ab)) return false;
         tc_fence_after();
-        const uint64_t dv = dv0 + stage_step * (uint64_t)st;
+        const uint64_t dv = dv0 + (Q8 ? (uint64_t)(buf * (MAX_SUB * SUB_BYTES >> 4)) : stage_step * (uint64_t)st);
         const uint64_t dp = dp0 + (uint64_t)(buf * (PBUF_BYTES >> 4));
         umma_ss(tm_o, dv, dp, idesc_pv, first ? 0u : 1u);
 #pragma unroll
         for (int ks = 1; ks < TK / 16; ++ks)
           umma_ss(tm_o, dv + (uint64_t)(ks * 128), dp + (uint64_t)((ks >> 2) * (QSUB_BYTES >> 4) + (ks & 3) * 2), idesc_pv, 1u);
         umma_commit(&p_free[buf]);
-        umma_commit(&empty_bar[st]);
+        if (!Q8) umma_commit(&empty_bar[st]);
         return true;
       };
       auto pop_pv = [&]() -> bool {
@@ -518,7 +530,7 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
      // thousand, later ones 4.2) were bound by that; now 6.7 and 4.2, the whole step 38.7 -> 32.7 us.
      constexpr int NREG = PAGED ? 1 : (HALF > 0 ? HALF : 1);
      float ac[NREG], as_[NREG];
-     float2* const tab = reinterpret_cast<float2*>(ring + 4 * (size_t)stage_bytes) + tid;      // PAGED: pair i at i * 128
+     float2* const tab = reinterpret_cast<float2*>(ring + (Q8 ? 4 * SUB_BYTES + 2 * MAX_SUB * SUB_BYTES : 4 * stage_bytes)) + tid;      // PAGED: pair i at i * 128
      static_assert(!PAGED || (size_t)HALF * 128 * sizeof(float2) <= 2 * (size_t)MAX_SUB * SUB_BYTES, "two stages of the ring");
      if constexpr (PAGED) {
 #pragma unroll 4
@@ -542,13 +554,36 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
      w.init(p, t_begin, t_end, b0, seq_first);
      int it = 0;
      bool ok = true;
+     // Q8: this row's page entry of tile t (0 of the new token's and later rows), its scale byte
+     [[maybe_unused]] auto entry_of = [&](const Walk& ww, long t) -> int {
+       const int n = ww.k0(t) + tid;
+       return n < ww.L ? p.pv.table[(long)ww.b * p.pv.max_pages + n / p.pv.page_size] : -1;
+     };
+     [[maybe_unused]] auto byte_of = [&](const Walk& ww, long t, int pg) -> int {
+       const int n = ww.k0(t) + tid;
+       if (n < ww.L) return pg >= 0 && pg < p.pv.n_pages ? p.scales[(long)pg * p.pv.page_size + n % p.pv.page_size] : 127;      // no page: rows of zeros
+       return n == ww.L ? p.new_scale[2 * (long)ww.b + 1] : 127;
+     };
+     [[maybe_unused]] Walk wn;
+     [[maybe_unused]] int byte_next = 127;
+     if constexpr (Q8) {
+       wn.init(p, t_begin, t_end, b0, seq_first);
+       byte_next = byte_of(wn, t_begin, entry_of(wn, t_begin));
+     }
      for (long t = t_begin; t < t_end && ok; ++t, ++it) {
        w.seek(t);
        const int s = it % STAGES, buf = it & 1, j = it >> 1;
+       [[maybe_unused]] int pg_next = -1;
+       [[maybe_unused]] const int byte = byte_next;
+       if constexpr (Q8)
+         if (t + 1 < t_end) {                   // the next tile's entry is on its way during the waits, its scale during the rotation
+           wn.seek(t + 1);
+           pg_next = entry_of(wn, t + 1);
+         }
        // the new token's rows, by the warp whose tile rows they replace one of: lane = 16-byte chunk
        const bool mine = PAGED && w.last_tile(t) && (w.L - w.k0(t)) >> 5 == q;
        uint4 nk = make_uint4(0u, 0u, 0u, 0u), nv = nk;
-       if (mine && lane < R3C / 8) {
+       if (!Q8 && mine && lane < R3C / 8) {
          nk = reinterpret_cast<const uint4*>(p.knew + (long)w.b * p.r3)[lane];
          nv = reinterpret_cast<const uint4*>(p.vnew + (long)w.b * p.t3)[lane];
        }
@@ -558,6 +593,7 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
        };
        if (!(ok = wait_all(&full_bar[s], (uint32_t)((it / STAGES) & 1)))) break;
        if (j > 0 && !(ok = wait_all(&kr_free[buf], (uint32_t)((j - 1) & 1)))) break;   // score product of tile it - 2 is done
+       if (Q8 && j > 0 && !(ok = wait_all(&p_free[buf], (uint32_t)((j - 1) & 1)))) break;   // ... and its P V product
        tc_fence_after();
        const int k0 = w.k0(t);
        // (cos, sin)(k0 theta_i) of this tile: lane l holds the values of pairs l and l + 32; they reach the
@@ -618,6 +654,44 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
            tmem_st32(kaddr + (uint32_t)hf * 32u, o);
          }
        }
+       } else if constexpr (Q8) {
+       if (t + 1 < t_end) byte_next = byte_of(wn, t + 1, pg_next);
+       const float sc = q8::scale(byte);
+       uint8_t* const vt = vtiles + (size_t)buf * (MAX_SUB * SUB_BYTES);
+       const uint4* const fresh = reinterpret_cast<const uint4*>(p.new_codes + (long)w.b * p.r3);
+       const bool none = last && tid > rnew;    // rows that do not exist: zeros, whatever the slots hold
+#pragma unroll 1
+       for (int hf = 0; hf < R3C / 32; ++hf) {  // 16 TMEM columns = 32 coordinates at a time, rounded values and rounded rests
+         uint32_t o[16], ol[16], xv[16];
+         const float2 bl = hf < 2 ? base_lo : base_hi;
+#pragma unroll
+         for (int cc = 0; cc < 2; ++cc) {       // 16 codes
+           const int ch = hf * 2 + cc;
+           uint4 v = make_uint4(0u, 0u, 0u, 0u);
+           if (is_new) v = fresh[ch];
+           else if (!none) v = *reinterpret_cast<const uint4*>(raw + tid * 128 + ((ch ^ (tid & 7)) << 4));
+           const uint32_t wv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+           for (int e = 0; e < 8; ++e) {
+             const int k = cc * 8 + e, i = hf * 16 + k;
+             float2 x = q8::values2(wv[e >> 1] >> (16 * (e & 1)));
+             x.x *= sc; x.y *= sc;
+             const float2 bs = make_float2(__shfl_sync(0xffffffffu, bl.x, i & 31), __shfl_sync(0xffffffffu, bl.y, i & 31));
+             const float2 a = tab[i * 128];
+             const float cs_c = a.x * bs.x - a.y * bs.y, cs_s = a.y * bs.x + a.x * bs.y;   // angle addition
+             const float re = x.x * cs_c - x.y * cs_s, ro = x.x * cs_s + x.y * cs_c;
+             xv[k] = pack_bf16(x.x, x.y);       // exact
+             o[k] = pack_bf16(re, ro);
+             const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&o[k]));
+             ol[k] = pack_bf16(re - f.x, ro - f.y);
+           }
+         }
+#pragma unroll
+         for (int c = 0; c < 4; ++c)
+           *reinterpret_cast<uint4*>(vt + swz(tid, hf * 4 + c)) = make_uint4(xv[4 * c], xv[4 * c + 1], xv[4 * c + 2], xv[4 * c + 3]);
+         tmem_st16(kaddr + (uint32_t)hf * 16u, o);
+         tmem_st16(kaddr + (TMEM_KROT_LO - TMEM_KROT) + (uint32_t)hf * 16u, ol);
+       }
        } else {
 #pragma unroll 1
        for (int hf = 0; hf < R3C / 32; ++hf) {  // 16 TMEM columns = 32 coordinates at a time, rounded values and rounded rests
@@ -655,7 +729,11 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
        }
        }
        tmem_st_wait();
-       if (last) {
+       if (Q8) {
+         __syncwarp();
+         if (lane == 0) mbar_arrive(&empty_bar[s]);
+       }
+       if (!Q8 && last) {
          // as VALUES the new token's un-rotated latent row comes from the workspace and rows past it must be
          // zero (their probabilities are zero, but the slots may hold anything)
          if constexpr (PAGED) {

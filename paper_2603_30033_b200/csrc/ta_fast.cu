@@ -718,8 +718,36 @@ bool tmap_code_pages(CUtensorMap* m, const void* pool, int r, int n_pages, int p
   return make_tmap(m, pool, 3, dims, str, box, CU_TENSOR_MAP_SWIZZLE_128B, true);
 }
 
+// One 8-bit pool with latent RoPE: rows pass through a rotation warpgroup.
+template <int R3C>
+int launch_dec_attn_q8_rot(Problem& p, const CUtensorMap& tmK, const CUtensorMap& tmQ, const decu::Params& up, int grid) {
+  static PerDeviceFlag attr;
+  TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)decu::k_dec_attn_umma<true, R3C, true, true>, (int)decu::SMEM_BYTES));
+  prof_begin(p);
+  (void)launch_pdl(decu::k_dec_attn_umma<true, R3C, true, true>, dim3(grid), dim3(decu::THREADS_ROT), decu::SMEM_BYTES, p.stream, tmK, tmK, tmQ,
+                   up, rope_turns(p.d));
+  prof_end(p);
+  TA_LAUNCH_CHECK(p);
+  return TA_OK;
+}
+
 int launch_dec_attn_q8(Problem& p, const FastDecWs& w, int grid) {
   const tucker_attn_desc& d = p.d;
+  if (p.shared_rope) {
+    CUtensorMap tmK, tmQ;
+    if (!tmap_code_pages(&tmK, p.Kc, d.r3, p.pv.n_pages, p.pv.page_size)) return TA_ERR_CUDA;
+    if (!tmap_2d(&tmQ, w.qhat, (uint64_t)d.r3, (uint64_t)d.B * d.n_H * 2, (uint64_t)d.r3, 64, 32)) return TA_ERR_CUDA;
+    decu::Params up = {};
+    up.B = d.B; up.nH = d.n_H; up.Lmax = p.Lmax; up.r3 = d.r3; up.t3 = d.t3; up.shared_kv = 1; up.cache_len = p.cache_len;
+    up.part_o = w.part_o; up.part_ml = w.part_ml; up.err = p.dev_err; up.pv = p.pv; up.pos_base = p.prefix_len; up.seq_cta = w.seq_cta;
+    up.scales = p.Vs; up.new_codes = (const uint8_t*)w.vnew; up.new_scale = w.new_scale;
+    switch (d.r3) {
+      case 64: return launch_dec_attn_q8_rot<64>(p, tmK, tmQ, up, grid);
+      case 96: return launch_dec_attn_q8_rot<96>(p, tmK, tmQ, up, grid);
+      case 128: return launch_dec_attn_q8_rot<128>(p, tmK, tmQ, up, grid);
+      default: return TA_ERR_UNSUPPORTED_SHAPE;
+    }
+  }
   CUtensorMap tmK, tmV;
   if (!tmap_code_pages(&tmK, p.Kc, d.r3, p.pv.n_pages, p.pv.page_size)) return TA_ERR_CUDA;
   if (!tmap_code_pages(&tmV, p.Vc, d.t3, p.pv.n_pages, p.pv.page_size)) return TA_ERR_CUDA;

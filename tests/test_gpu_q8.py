@@ -46,11 +46,11 @@ def host(t):
 
 
 def expected_path(st, flags=0):
-    """2 (tensor-core kernels) for the bf16 shapes of the bf16 cache's tensor-core step, one pool with RoPE apart; else 1."""
+    """2 (tensor-core kernels) for the bf16 shapes of the bf16 cache's tensor-core step, else 1."""
     w = st.w
     ranks = (w.r[2], w.t[2]) in [(128, 128), (64, 64), (96, 96), (128, 64), (64, 128)] and w.r[1] % 32 == 0 and w.t[1] % 32 == 0
     tc = w.dtype == "bf16" and ranks and w.d_model % 64 == 0 and (st.page in (16, 32, 64) or st.page % 128 == 0)
-    return 2 if tc and not flags & Bd.TA_FLAG_FORCE_GENERIC and not (st.shared and w.rope) else 1
+    return 2 if tc and not flags & Bd.TA_FLAG_FORCE_GENERIC else 1
 
 
 def step(st, dev=None, append=True, flags=0, prefix_call=None, **kw):
@@ -553,12 +553,13 @@ LONG = [("one sequence over all CTAs", TC128, [60000], 64),
         ("ragged batch", TC128, [1000 * (i % 13) + 77 * i for i in range(64)], 256)]
 
 
-@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("shared", ["two pools", "one pool", "one pool, rotated"])
 @pytest.mark.parametrize("what,shape,lens,page", LONG, ids=[c[0] for c in LONG])
 def test_many_tiles(what, shape, lens, page, shared):
+    rope, shared = shared != "one pool", shared != "two pools"
     if shared:
         shape = {**shape, "t": (shape["t"][0], shape["t"][1], shape["r"][2])}
-    state, w = big_state(shape, lens, page, rope=not shared, shared=shared)
+    state, w = big_state(shape, lens, page, rope=rope, shared=shared)
     x, dw, pools, table, dl, _ = state
     y = Bd.tucker_attn_decode_paged_q8(x, *dw, *pools, table, dl, n_H=w.n_H, rope=w.rope, rope_base=w.rope_base)
     assert Bd.last_path() == 2 and Bd.last_device_error() == 0
