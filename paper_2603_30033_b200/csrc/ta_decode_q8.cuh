@@ -7,21 +7,30 @@
 //   S^T [128 keys x 32 heads] = K_codes * q^T      The query is carried as three e4m3 numbers per coordinate (the rounded
 //       value, the rounded rest, the rest's rounded rest: 2^-12 of it together), 96 columns of one product that are added up
 //       when they are read (as three products into one accumulator the key tile was read three times: at N = 32 an
-//       instruction takes the 40 cycles of its 4 KB of A from shared memory, and the tensor core was the limit).  Its own scale is a power of two per sequence.  Two numbers (2^-8) would move scores of a standard
-//       deviation of 2 by what the rounding of y to bf16 moves the output.
+//       instruction takes the 40 cycles of its 4 KB of A from shared memory, and the tensor core was the limit).  Its own scale
+//       is a power of two per sequence.  Two numbers (2^-8) would move scores of a standard deviation of 2 by what the
+//       rounding of y to bf16 moves the output.
 //   p 2^k' [128 keys x 32 heads]                   A thread owns a key, so the row's scales are two numbers of its own: 2^k
 //       multiplies the scores, 2^k' the weight of the value row, as a term of the exponent.  The sums are of p alone.
 //   O^T [t3 x 32 heads] += V_codes^T * (p 2^k')    The weight is carried as three e5m2 numbers: the upper byte of an f16, the
-//       upper byte of what is left, and of what is left then, rounded (2^-10 together; a byte's worth of an f16 is an e5m2,
-//       so this is masking and exact subtraction).  e5m2 for its range: with the reference maximum at 2^11 .. 2^15, weights
-//       down to 2^-27 of the largest count in full precision or to 2^-28 absolute.  The three are 96 columns of one product
-//       and of the accumulator, and are added up once per segment.
+//       upper byte of 8 times what is left, and of 8 times what is left then, rounded (2^-10 together; a byte's worth of an f16
+//       is an e5m2, so this is masking and exact subtraction).  The three are 96 columns of one product and of the accumulator,
+//       and are added up once per segment.  With a head's largest weight at 2^5 .. 2^15, all are held to 2^-28 of the largest.
+//       (Without the factors, for which their columns have room, to 2^-22: 12000 equal weights behind one of e^14 times theirs
+//       came out 6% off; the factors cost 1 us of 109.)
 //
 // Everything goes by steps of 256 keys.  The two softmax warpgroups take a half each, with scores, weights, running maxima, sums
 // and an accumulator of its own (TMEM has room for two of each here; the bf16 kernel's warpgroups share every tile's heads and
 // its accumulator).  What the threads of one have to agree on is one vote per step: whether any score lies more than 2^kTop
-// above its head's reference.  Then, at the first step of a segment and seldom after, the maxima are taken and the accumulator
-// rescaled.  At the end of a (CTA, sequence) segment warpgroup 1 hands its part to warpgroup 0 through its weights' buffer.
+// above its head's reference.  Half of the weights are formed while it is counted.  At the first step of a segment and seldom
+// after (64 ragged sequences of random rows: 2 to 9 of a CTA's 35 steps, 2000 cycles each; with
+// kStart = 8 the step takes 119 us instead of 109), the maxima are taken and the accumulator rescaled where a reference moved.
+// At the end of a (CTA, sequence) segment warpgroup 1 hands its part to warpgroup 0 through its weights' buffer.
+// 64 ragged sequences to 32768 tokens (1.3 million keys, 347 MB: 54 us at the copy rate): 90 us.  A CTA's 35 steps take 2600
+// to 3000 cycles each, what the bytes and the softmax warps' chains (2100) need, and about 25 thousand cycles go to the
+// division of the work, the first pass over cold code and the last segment's end.  What was tried: references and sums in
+// registers with everything of a step formed at once (300 bytes of spills, 126 us); four softmax warpgroups of 16 heads
+// (113); a pass over the loop before the queries are there, for the code (109).
 //
 //   warp 0       TMA producer of keys and values
 //   warp 1       TMEM allocation, MMA issue of the scores, a step ahead of the values
@@ -52,7 +61,6 @@ namespace decq {
 using namespace sm100;
 using decu::ex2;
 using prefix::max3;
-using decu::warp_max;
 
 constexpr int TK = 128, SK = 2 * TK;             // keys of a warpgroup, of a step
 constexpr int NWG = 2, THREADS = 128 + 128 * NWG;
@@ -71,6 +79,7 @@ constexpr int S_SLOTS = 4, S_AHEAD = 3;          // steps whose scale bytes have
 constexpr size_t SMEM_BYTES = 1024 + (size_t)RING_BYTES + 2 * QBUF_BYTES + 2 * PBUF_BYTES + S_SLOTS * 2 * SK;
 static_assert(SMEM_BYTES <= 224 * 1024, "one CTA's shared memory, with the static part");
 constexpr float kTop = 15.f, kStart = 5.f;      // weights reach 2^kTop at most, the largest is 2^kStart when a reference is set
+constexpr float kRestUp = 8.f;                  // what a piece leaves of a weight is below 2^(kTop - 3)
 
 struct Params {
   int B, nH, Lmax, r3, t3;
@@ -104,6 +113,11 @@ __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t adesc, uint64_
 }
 // 16-byte chunk of a row of 128 bytes, 128-byte swizzle
 __device__ __forceinline__ uint32_t swz(int row, int chunk) { return (uint32_t)(row * 128 + ((chunk ^ (row & 7)) << 4)); }
+
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
 
 // pairs of fp32 numbers
 __device__ __forceinline__ uint64_t pack2(float lo, float hi) {
@@ -213,7 +227,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
   __shared__ float q_scale[8];                   // of segment i at i & 7: the queries are split at most three segments ahead
   __shared__ uint32_t votes[NWG][2];             // a byte per warp, by parity of the step
   __shared__ float max_s[NWG][4][NH], sum_s[NWG][4][NH], hand_m[NH], hand_l[NH];
-  __shared__ __align__(16) float up_s[NWG][4][NH];
+  __shared__ __align__(16) float up_s[NWG][4][NH], neg_s[NWG][4][NH];      // a warp's own: minus the references, minus their rise
   __shared__ long long wtot_s[THREADS / 32];
   __shared__ int loc_b;
   __shared__ long long loc_first;
@@ -554,9 +568,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
     const uint32_t tm_s = tmem + (uint32_t)(g * PC) + lane_addr, tm_o = tm_s + TMEM_O;
     uint8_t* const my_p = pbuf + g * PBUF_BYTES;
     uint32_t wg_phase = 0, n_mine = 0, n_handed = 0;      // steps in which this warpgroup had keys; parts handed over so far
-    // Code that is new to the SM arrives at 3 bytes per cycle: the first step took 9000 cycles more than the others.  So the loop
-    // runs once on whatever the memories hold, its waits and arrivals left out, while the query kernel is waited for.
-    int warm = 1;
+    pdl_enter();
     bool ok = true, owe = false;                // owe: my part lies in the weights' buffer until it is taken
     auto wg_sync = [&]() -> bool {
       __syncwarp();
@@ -567,109 +579,61 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
     };
     int seg = 0;
     for (; sg.more() && ok; sg.next(), ++seg) {
-      uint64_t neg_m[NH / 2], l2[NH / 2];       // pairs of heads: minus the references; sums of this thread's keys
+      uint64_t l2[NH / 2];                      // pairs of heads: sums of this thread's keys
       float m_lane = 0.f;                       // reference of head `lane`
+      neg_s[g][q][lane] = 0.f;
+      __syncwarp();
 #pragma unroll
-      for (int h = 0; h < NH / 2; ++h) neg_m[h] = l2[h] = 0;
+      for (int h = 0; h < NH / 2; ++h) l2[h] = 0;
       int first = 1;
 #pragma unroll 1
-      for (int it = sg.it0 - warm; it < sg.it1 && ok; ++it) {
+      for (int it = sg.it0; it < sg.it1 && ok; ++it) {
         asm volatile("" : "+r"(first));         // no copy of the loop for the first step
-        if (g == 1 && !warm && !sg.both(it)) break;      // (the last step only)
+        if (g == 1 && !sg.both(it)) break;      // (the last step only)
         const uint32_t par = n_mine & 1u;
         const int slot = it & (S_SLOTS - 1);
-        if (!warm && !(ok = wait_both(&sfull[slot], (uint32_t)((it / S_SLOTS) & 1), &s_full[g], par))) break;
+        if (!(ok = wait_both(&sfull[slot], (uint32_t)((it / S_SLOTS) & 1), &s_full[g], par))) break;
         tc_fence_after();
-        uint32_t s0[NH], s1[NH], s2[NH];
-        tmem_ld32(tm_s, s0);
-        tmem_ld32(tm_s + NH, s1);
-        tmem_ld32(tm_s + 2 * NH, s2);
         const uint8_t* sc = scales + slot * 2 * SK + g * TK + tid;
         const int kb = sc[0], vb = sc[SK];
-        float kq = q8::scale(kb) * q_scale[seg & 7];
-        float ev = vb == q8::kNan ? NAN : (float)(vb - 127), inv = vb == q8::kNan ? NAN : q8::scale(254 - vb);
-        tmem_ld_wait();
+        const float kq = q8::scale(kb) * q_scale[seg & 7], ev = vb == q8::kNan ? NAN : (float)(vb - 127);
+        float inv = vb == q8::kNan ? NAN : q8::scale(254 - vb);
+        // log2 of p 2^k', relative to the references (by halves, for the registers)
+        const uint64_t kq2 = pack2(kq, kq), ev2 = pack2(ev, ev);
+        float a[NH];
+#pragma unroll
+        for (int h0 = 0; h0 < NH; h0 += 16) {
+          uint32_t s0[16], s1[16], s2[16];
+          tmem_ld16(tm_s + h0, s0);
+          tmem_ld16(tm_s + NH + h0, s1);
+          tmem_ld16(tm_s + 2 * NH + h0, s2);
+          tmem_ld_wait();
+#pragma unroll
+          for (int h = 0; h < 16; h += 4) {
+            const float4 neg = *reinterpret_cast<const float4*>(&neg_s[g][q][h0 + h]);
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+              const int i = h + e;
+              const uint64_t s = add2(add2(pairu(s0[i], s0[i + 1]), pairu(s1[i], s1[i + 1])), pairu(s2[i], s2[i + 1]));
+              unpack2(fma2(s, kq2, add2(ev2, e == 0 ? pack2(neg.x, neg.y) : pack2(neg.z, neg.w))), a[h0 + i], a[h0 + i + 1]);
+            }
+          }
+        }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0 && !warm) mbar_arrive(&s_free[g]);       // the next step's scores may overwrite the buffer
+        if (lane == 0) mbar_arrive(&s_free[g]);       // the next step's scores may overwrite the buffer
         if (sg.tail && it == sg.it1 - 1 && sg.k0 + (it - sg.it0) * SK + g * TK + tid > sg.L) {
           // keys past the new token do not exist: weights of zero whatever the scores are
-          ev = -INFINITY; kq = inv = 0.f;
+          inv = 0.f;
 #pragma unroll
-          for (int h = 0; h < NH; ++h) s0[h] = s1[h] = s2[h] = 0u;
+          for (int h = 0; h < NH; ++h) a[h] = -INFINITY;
         }
-        // log2 of p 2^k', relative to the references
-        const uint64_t kq2 = pack2(kq, kq), ev2 = pack2(ev, ev);
-        float a[NH], over = -INFINITY;
-#pragma unroll
-        for (int h = 0; h < NH; h += 2) {
-          const uint64_t s = add2(add2(pairu(s0[h], s0[h + 1]), pairu(s1[h], s1[h + 1])), pairu(s2[h], s2[h + 1]));
-          unpack2(fma2(s, kq2, add2(ev2, neg_m[h / 2])), a[h], a[h + 1]);
-          over = max3(over, a[h], a[h + 1]);
-        }
-        const bool vote = first || __any_sync(0xffffffffu, over > kTop);
-        if (lane == 0) reinterpret_cast<uint8_t*>(&votes[g][par])[q] = vote ? 1 : 0;
-        if (!(ok = wg_sync())) break;
-        bool free_seen = n_mine == 0;                  // (warm too) the step before's product has read the weights
-        if (*reinterpret_cast<volatile uint32_t*>(&votes[g][par]) != 0u) {
-          // ---- new references: the maxima of these keys where they are needed ----
-          float mine = -INFINITY;
-#pragma unroll
-          for (int h = 0; h < NH; ++h) {
-            const float mx = warp_max(a[h]);
-            if (lane == h) mine = mx;
-          }
-          max_s[g][q][lane] = mine;
-          if (!(ok = wg_sync())) break;
-          // by how much the reference of head `lane` rises (it is 0 until the first step sets it)
-          const float mt = fmaxf(fmaxf(max_s[g][0][lane], max_s[g][1][lane]), fmaxf(max_s[g][2][lane], max_s[g][3][lane]));
-          const float up = mt > kTop || first ? mt - kStart : 0.f;
-          m_lane += up;
-          up_s[g][q][lane] = -up;
-          __syncwarp();
-          uint64_t f[NH / 2];
-#pragma unroll
-          for (int h = 0; h < NH; h += 4) {
-            const float4 u = *reinterpret_cast<const float4*>(&up_s[g][q][h]);
-            a[h] += u.x; a[h + 1] += u.y; a[h + 2] += u.z; a[h + 3] += u.w;
-            neg_m[h / 2] = add2(neg_m[h / 2], pack2(u.x, u.y));
-            neg_m[h / 2 + 1] = add2(neg_m[h / 2 + 1], pack2(u.z, u.w));
-            f[h / 2] = pack2(ex2(u.x), ex2(u.y));
-            f[h / 2 + 1] = pack2(ex2(u.z), ex2(u.w));
-          }
-          if (!first || warm) {
-            // the product of the step before must be complete before its accumulator is rescaled
-            if (!warm && !(ok = wait_all(&p_free[g], par ^ 1u))) break;
-            free_seen = true;
-            tc_fence_after();
-#pragma unroll
-            for (int h = 0; h < NH / 2; ++h) l2[h] = mul2(l2[h], f[h]);
-#pragma unroll 1
-            for (int pc = 0; pc < PIECES; ++pc) {
-              uint32_t o[NH];
-              tmem_ld32(tm_o + pc * NH, o);
-              tmem_ld_wait();
-#pragma unroll
-              for (int h = 0; h < NH; h += 2) {
-                float x, y;
-                unpack2(mul2(pairu(o[h], o[h + 1]), f[h / 2]), x, y);
-                o[h] = __float_as_uint(x); o[h + 1] = __float_as_uint(y);
-              }
-              tmem_st32(tm_o + pc * NH, o);
-            }
-            tmem_st_wait();
-          }
-        }
-        if (!free_seen && !(ok = wait_all(&p_free[g], par ^ 1u))) break;
-        if (owe) {                                     // a part laid down in the weights' buffer must have been taken
-          if (!(ok = wait_all(&taken, (n_handed - 1) & 1u))) break;
-          owe = false;
-        }
-        // ---- weights in three bytes; sums ----
         const uint64_t inv2 = pack2(inv, inv);
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          uint32_t out[PIECES][4];
+        bool free_seen = n_mine == 0;                  // the step before's product has read the weights
+        uint32_t out[2][PIECES][4];
+        uint64_t sum[NH / 4];
+        // ---- weights in three bytes, of heads 16 half ..; sums ----
+        auto weights = [&](int half, uint64_t* into) {
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             uint32_t hv[2], piece[PIECES][2];
@@ -677,7 +641,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             for (int e = 0; e < 2; ++e) {
               const int h = half * 16 + u * 4 + e * 2;
               const float w0 = ex2(a[h]), w1 = ex2(a[h + 1]);
-              l2[h / 2] = fma2(pack2(w0, w1), inv2, l2[h / 2]);
+              into[u * 2 + e] = fma2(pack2(w0, w1), inv2, l2[h / 2]);
               const __half2 x = __floats2half2_rn(w0, w1);
               hv[e] = *reinterpret_cast<const uint32_t*>(&x);
 #pragma unroll
@@ -687,32 +651,120 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
                 } else {
                   piece[pc][e] = hv[e];
                   const uint32_t top = hv[e] & 0xff00ff00u;
-                  const __half2 rest = __hsub2(*reinterpret_cast<const __half2*>(&hv[e]), *reinterpret_cast<const __half2*>(&top));
+                  const __half2 rest = __hmul2(__hsub2(*reinterpret_cast<const __half2*>(&hv[e]), *reinterpret_cast<const __half2*>(&top)),
+                                               __float2half2_rn(kRestUp));
                   hv[e] = *reinterpret_cast<const uint32_t*>(&rest);
                 }
               }
             }
 #pragma unroll
-            for (int pc = 0; pc < PIECES; ++pc) out[pc][u] = __byte_perm(piece[pc][0], piece[pc][1], 0x7531);
+            for (int pc = 0; pc < PIECES; ++pc) out[half][pc][u] = __byte_perm(piece[pc][0], piece[pc][1], 0x7531);
           }
+        };
+        int renew = first;
+#pragma unroll 1
+        for (;;) {
+          if (renew) {
+            // ---- new references: the maxima of these keys where they are needed ----
+            // Of pairs of heads in bf16 (a reference only has to be near; what the rounding leaves above 2^kTop comes here
+            // again), by a butterfly whose levels keep half of the pairs each: lane 2 i + {0, 1} is left with pair i.
+            uint32_t mx[NH / 2];
+#pragma unroll
+            for (int h = 0; h < NH / 2; ++h) mx[h] = pack_bf16(a[2 * h], a[2 * h + 1]);
+#pragma unroll
+            for (int lev = 8; lev >= 1; lev >>= 1) {
+              const bool upper = lane & (2 * lev);
+#pragma unroll
+              for (int h = 0; h < lev; ++h) {
+                const uint32_t keep = upper ? mx[h + lev] : mx[h], give = upper ? mx[h] : mx[h + lev];
+                mx[h] = max_bf16x2(keep, __shfl_xor_sync(0xffffffffu, give, 2 * lev));
+              }
+            }
+            mx[0] = max_bf16x2(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], 1));
+            max_s[g][q][lane] = __uint_as_float(lane & 1 ? mx[0] & 0xffff0000u : mx[0] << 16);
+            if (!(ok = wg_sync())) break;
+            // by how much the reference of head `lane` rises (it is 0 until the first step sets it)
+            const float mt = fmaxf(fmaxf(max_s[g][0][lane], max_s[g][1][lane]), fmaxf(max_s[g][2][lane], max_s[g][3][lane]));
+            const float up = mt >= kTop || first ? mt - kStart : 0.f;
+            m_lane += up;
+            up_s[g][q][lane] = -up;
+            neg_s[g][q][lane] = -m_lane;
+            __syncwarp();
+#pragma unroll
+            for (int h = 0; h < NH; h += 4) {
+              const float4 u = *reinterpret_cast<const float4*>(&up_s[g][q][h]);
+              a[h] += u.x; a[h + 1] += u.y; a[h + 2] += u.z; a[h + 3] += u.w;
+            }
+            if (!first) {
+              // the product of the step before must be complete before its accumulator is rescaled
+              if (!free_seen && !(ok = wait_all(&p_free[g], par ^ 1u))) break;
+              free_seen = true;
+              tc_fence_after();
+#pragma unroll
+              for (int h = 0; h < NH; h += 2) {
+                const float2 u = *reinterpret_cast<const float2*>(&up_s[g][q][h]);
+                l2[h / 2] = mul2(l2[h / 2], pack2(ex2(u.x), ex2(u.y)));
+              }
+#pragma unroll 1
+              for (int h0 = 0; h0 < NH; h0 += 8) {
+                if (!__any_sync(0xffffffffu, up != 0.f && lane >> 3 == h0 >> 3)) continue;      // none of these heads' (all warps alike)
+                uint32_t o[PIECES][8];
+#pragma unroll
+                for (int pc = 0; pc < PIECES; ++pc) tmem_ld8(tm_o + pc * NH + h0, o[pc]);
+                tmem_ld_wait();
+#pragma unroll
+                for (int h = 0; h < 8; h += 2) {
+                  const float2 u = *reinterpret_cast<const float2*>(&up_s[g][q][h0 + h]);
+                  const uint64_t f = pack2(ex2(u.x), ex2(u.y));
+#pragma unroll
+                  for (int pc = 0; pc < PIECES; ++pc) {
+                    float x, y;
+                    unpack2(mul2(pairu(o[pc][h], o[pc][h + 1]), f), x, y);
+                    o[pc][h] = __float_as_uint(x); o[pc][h + 1] = __float_as_uint(y);
+                  }
+                }
+#pragma unroll
+                for (int pc = 0; pc < PIECES; ++pc) tmem_st8(tm_o + pc * NH + h0, o[pc]);
+              }
+              tmem_st_wait();
+            }
+            first = 0;
+          }
+          // The vote is counted while half of the weights are formed, on the strength of there being none as a rule.
+          float over = -INFINITY;
+#pragma unroll
+          for (int h = 0; h < NH; h += 2) over = max3(over, a[h], a[h + 1]);
+          const uint32_t ph = wg_phase & 1u;
+          const bool vote = __any_sync(0xffffffffu, over > kTop);
+          if (lane == 0) {
+            reinterpret_cast<uint8_t*>(&votes[g][ph])[q] = vote ? 1 : 0;
+            mbar_arrive(&wg_bar[g]);
+          }
+          weights(0, sum);
+          if (!(ok = wait_all(&wg_bar[g], ph))) break;
+          ++wg_phase;
+          renew = *reinterpret_cast<volatile uint32_t*>(&votes[g][ph]) != 0u;
+          if (!renew) break;
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int h = 0; h < NH / 4; ++h) l2[h] = sum[h];
+        weights(1, l2 + NH / 4);
+        if (!free_seen && !(ok = wait_all(&p_free[g], par ^ 1u))) break;
+        if (owe) {                                     // a part laid down in the weights' buffer must have been taken
+          if (!(ok = wait_all(&taken, (n_handed - 1) & 1u))) break;
+          owe = false;
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int pc = 0; pc < PIECES; ++pc)
-            *reinterpret_cast<uint4*>(my_p + swz(tid, pc * 2 + half)) = make_uint4(out[pc][0], out[pc][1], out[pc][2], out[pc][3]);
-        }
-        if (warm) {
-          warm = 0;
-          pdl_enter();
-          m_lane = 0.f;
-#pragma unroll
-          for (int h = 0; h < NH / 2; ++h) neg_m[h] = l2[h] = 0;
-          continue;
-        }
+            *reinterpret_cast<uint4*>(my_p + swz(tid, pc * 2 + half)) = make_uint4(out[half][pc][0], out[half][pc][1], out[half][pc][2], out[half][pc][3]);
         fence_proxy_async_smem();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&p_full[g]);
         ++n_mine;
-        first = 0;
       }
       if (!ok) break;
       const bool two = sg.both(sg.it0);                // warpgroup 1 has a part too
@@ -743,7 +795,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             reinterpret_cast<float*>(my_p)[(h0 + e) * 128 + (((tid >> 2) ^ (h0 + e)) << 2) + (tid & 3)] =
-                (__uint_as_float(c0[e]) + __uint_as_float(c1[e])) + __uint_as_float(c2[e]);
+                __uint_as_float(c0[e]) + (__uint_as_float(c1[e]) + __uint_as_float(c2[e]) * (1.f / kRestUp)) * (1.f / kRestUp);
         }
         tc_fence_before();
         __syncwarp();

@@ -585,6 +585,41 @@ def test_many_tiles_scores_that_grow_or_fall(ramp):
     check_against_64(state, w, 0, y, f"ramp {ramp}")
 
 
+@pytest.mark.parametrize("nats", [9.5, 11, 12, 13, 14])
+def test_one_key_outweighs_thousands_of_equal_ones(nats):
+    """Weights e^-9.5 .. e^-14 of the largest, 12000 of them in one segment, and the largest's value row is zeros: all are rounded
+    alike, and y is off by as much.  To 2^-28 of the largest each: 0.5% at 14."""
+    B, m, page = 150, 12000, 64
+    state, w = big_state({**TC128, "n_H": 8}, [m] + [0] * (B - 1), page, rope=False)      # (as many heads as core slices: queries independent)
+    x, dw, (K, Ks, V, Vs), table, dl, _ = state
+    x[1:] = x[0]                                              # every sequence the same, on the same pages
+    table[1:] = table[0]
+    dl[1:] = m
+    C, U1, U2 = (t.double() for t in dw[:3])
+    q = torch.einsum("q,ha,aqc->hc", x[0].double() @ U2, U1, C) * (w.d_model / w.n_H) ** -0.5
+    top = q.T @ torch.linalg.solve(q @ q.T, torch.full((w.n_H,), float(nats), device="cuda", dtype=torch.float64))
+    g = torch.Generator(device="cuda").manual_seed(5)
+    value = torch.randn(V.shape[2], generator=g, device="cuda")
+    kb, vb = K.view(torch.uint8), V.view(torch.uint8)
+    kb[:] = 0
+    vb[:] = value.to(torch.float8_e4m3fn).view(torch.uint8)
+    Ks.view(torch.uint8)[:] = 127
+    Vs.view(torch.uint8)[:] = 127
+    k = torch.frexp(top.abs().amax() / 448).exponent
+    first = int(table[0, 0])
+    kb[first, 7] = (top * torch.exp2(-k.double())).float().to(torch.float8_e4m3fn).view(torch.uint8)
+    Ks.view(torch.uint8)[first, 7] = 127 + k
+    vb[first, 7] = 0
+    y = Bd.tucker_attn_decode_paged_q8(x, *dw, K, Ks, V, Vs, table, dl, n_H=w.n_H, rope=False, append=False)
+    assert Bd.last_device_error() == 0 and Bd.last_path() == 2
+    u3, ut3 = (x[:1].double() @ dw[i].double() for i in (3, 7))
+    def stored(t):
+        c, sc = Q.quantise(t.cpu().numpy())
+        return torch.from_numpy(c * sc[:, None]).cuda()
+    one = ((x[:1], dw, (K, Ks, V, Vs), table[:1], dl[:1], state[5]), w)
+    P.check_rows(host(y), np.repeat(reference64(*one, 0, stored(u3), stored(ut3)), B, 0), "bf16", f"{nats} nats")
+
+
 @pytest.mark.parametrize("shared", [False, True])
 @pytest.mark.parametrize("rope", [True, False])
 def test_long_prefix(shared, rope):
