@@ -768,17 +768,14 @@ int launch_dec_attn_q8(Problem& p, const FastDecWs& w, int grid) {
 // rows of all the batch's heads are many (32768 tokens: 8 MB in, 17 MB out and back).
 int launch_prefix_unpack(Problem& p, const FastDecWs& w, const PrefixPlan& q) {
   const tucker_attn_desc& d = p.d;
-  auto part = [&](const void* codes, const uint8_t* scales, int r, bf16* out, bf16* rot) -> int {
-    const long n = (long)p.prefix_len * (r / 8);
-    (void)launch_pdl(decq::k_prefix_unpack_q8, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, p.stream, (const uint8_t*)codes, scales,
-                     p.prefix_table, p.pv.n_pages, p.pv.page_size, out, rot, (long)q.n_kt * prefix::TK * r, p.prefix_len, r, rope_turns(d),
-                     p.dev_err);
-    TA_LAUNCH_CHECK(p);
-    return TA_OK;
-  };
-  if (p.shared_rope) return part(p.Vc, p.Vs, d.t3, w.pre_v, w.pre_k);
-  const int rc = part(p.Kc, p.Ks, d.r3, w.pre_k, nullptr);
-  return rc || p.shared_kv ? rc : part(p.Vc, p.Vs, d.t3, w.pre_v, nullptr);
+  const decq::UnpackPart k = {(const uint8_t*)p.Kc, p.Ks, w.pre_k, nullptr, d.r3};
+  const decq::UnpackPart v = {(const uint8_t*)p.Vc, p.Vs, w.pre_v, p.shared_rope ? w.pre_k : nullptr, d.t3};
+  const long n = (long)p.prefix_len * (std::max(d.r3, d.t3) / 8);
+  (void)launch_pdl(decq::k_prefix_unpack_q8, dim3((unsigned)((n + 255) / 256), p.shared_kv ? 1 : 2), dim3(256), 0, p.stream,
+                   p.shared_rope ? v : k, v, p.prefix_table, p.pv.n_pages, p.pv.page_size, (long)q.n_kt * prefix::TK, p.prefix_len,
+                   rope_turns(d), p.dev_err);
+  TA_LAUNCH_CHECK(p);
+  return TA_OK;
 }
 
 // Launched behind the streaming kernel, which does not write anything that it reads and lets it be launched only after
