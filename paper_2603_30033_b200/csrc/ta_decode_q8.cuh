@@ -26,7 +26,7 @@
 // after (64 ragged sequences of random rows: 2 to 9 of a CTA's 35 steps, 2000 cycles each; with
 // kStart = 8 the step takes 119 us instead of 109), the maxima are taken and the accumulator rescaled where a reference moved.
 // At the end of a (CTA, sequence) segment warpgroup 1 hands its part to warpgroup 0 through its weights' buffer.
-// 64 ragged sequences to 32768 tokens (1.3 million keys, 347 MB: 54 us at the copy rate): 90 us.  A CTA's 35 steps take 2600
+// 64 ragged sequences to 32768 tokens (1.3 million keys, 347 MB: 54 us at the copy rate): 89 us.  A CTA's 35 steps take 2600
 // to 3000 cycles each, what the bytes and the softmax warps' chains (2100) need, and about 25 thousand cycles go to the
 // division of the work, the first pass over cold code and the last segment's end.  What was tried: references and sums in
 // registers with everything of a step formed at once (300 bytes of spills, 126 us); four softmax warpgroups of 16 heads
@@ -35,7 +35,7 @@
 //   warp 0       TMA producer of keys and values
 //   warp 1       TMEM allocation, MMA issue of the scores, a step ahead of the values
 //   warp 2       MMA issue of the values; scale bytes
-//   warp 3       splits the next segment's queries; puts the new token's row into the tile that holds it
+//   warp 3       splits the next segment's queries (the first's: warps 4 ..); puts the new token's row into the tile that holds it
 //   warps 4 + 4 g .. 7 + 4 g   softmax warpgroup g: keys 128 g .. 128 g + 127 of a step
 // A warp that works alone gets through about a hundred instructions in a thousand cycles, waits and issues among them, and a
 // step of 128 keys was too short for that: with the warpgroups on alternate tiles of 128 keys one warp or another of the
@@ -217,11 +217,48 @@ struct Lookup {
   }
 };
 
+// Scale byte of a sequence's queries
+__device__ __forceinline__ int query_byte(const Params& p, int b) {
+  const uint4 mx = *reinterpret_cast<const uint4*>(p.qmax + 4 * (long)b);
+  return q8::scale_byte(max(max(mx.x, mx.y), max(mx.z, mx.w)));
+}
+// Sixteen coordinates (chunk item % 8 of the row) of head item / 8 in three pieces, zeros where there is no head or coordinate
+__device__ __forceinline__ void split_query(const Params& p, int b, int item, float inv, uint8_t* dst) {
+  const int h = item >> 3, ch = item & 7;
+  const long at = ((long)b * p.nH + h) * p.r3 + ch * 16, half = (long)p.B * p.nH * p.r3;
+  uint4 out[PIECES] = {};
+  if (h < p.nH && ch * 16 < p.r3 && TA_IDX_OK(p.err, at, 16, half)) {
+    uint4 a[2], b4[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      a[e] = reinterpret_cast<const uint4*>(p.qhat + at)[e];
+      b4[e] = reinterpret_cast<const uint4*>(p.qhat + half + at)[e];
+    }
+    const uint32_t aw[8] = {a[0].x, a[0].y, a[0].z, a[0].w, a[1].x, a[1].y, a[1].z, a[1].w};
+    const uint32_t bw[8] = {b4[0].x, b4[0].y, b4[0].z, b4[0].w, b4[1].x, b4[1].y, b4[1].z, b4[1].w};
+    uint32_t* o = reinterpret_cast<uint32_t*>(out);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float x0 = (__uint_as_float(aw[e] << 16) + __uint_as_float(bw[e] << 16)) * inv;
+      float x1 = (__uint_as_float(aw[e] & 0xffff0000u) + __uint_as_float(bw[e] & 0xffff0000u)) * inv;
+#pragma unroll
+      for (int pc = 0; pc < PIECES; ++pc) {
+        const uint32_t c = q8::codes2(x0, x1);
+        const float2 v = q8::values2(c);
+        x0 -= v.x; x1 -= v.y;
+        o[pc * 4 + (e >> 1)] |= c << (16 * (e & 1));
+      }
+    }
+  }
+#pragma unroll
+  for (int pc = 0; pc < PIECES; ++pc) *reinterpret_cast<uint4*>(dst + pc * QPIECE_BYTES + swz(h, ch)) = out[pc];
+}
+
 __global__ void __launch_bounds__(THREADS, 1)
 k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const Params p) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t kfull[K_STAGES], kempty[K_STAGES], vfull[MAX_STAGES], vempty[MAX_STAGES], sfull[S_SLOTS], q_full[2], q_empty[2];
-  __shared__ uint64_t s_full[NWG], s_free[NWG], p_full[NWG], p_free[NWG], o_read[NWG], wg_bar[NWG], handed, taken, wanted, patched;
+  __shared__ uint64_t s_full[NWG], s_free[NWG], p_full[NWG], p_free[NWG], o_read[NWG], wg_bar[NWG], handed, taken, wanted, patched, q_first;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
   __shared__ float q_scale[8];                   // of segment i at i & 7: the queries are split at most three segments ahead
@@ -268,6 +305,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
     mbar_init(&taken, 4);                 // ... and warpgroup 0 has picked it up
     mbar_init(&wanted, 1);                // the next step with a new token's row has arrived ...
     mbar_init(&patched, 1);               // ... and the row is in its place
+    mbar_init(&q_first, 4 * NWG);         // the first segment's queries
     fence_barrier_init();
   }
   if (warp == 1) {
@@ -372,7 +410,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
       bool ok = true;
       for (; sg.more() && ok; sg.next(), ++seg) {
         const uint64_t dq = dq0 + (uint64_t)((seg & 1) * (QBUF_BYTES >> 4));
-        if (!(ok = mbar_wait(&q_full[seg & 1], (uint32_t)((seg >> 1) & 1), ab))) break;
+        if (!(ok = seg == 0 ? mbar_wait(&q_first, 0, ab) : mbar_wait(&q_full[seg & 1], (uint32_t)(((seg - 1) >> 1) & 1), ab))) break;
         for (int it = sg.it0; it < sg.it1; ++it) {
           const bool last = sg.tail && it == sg.it1 - 1;
           if (!shared && !(ok = mbar_wait(&kfull[sk], k_par, ab))) break;
@@ -477,49 +515,16 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
    } else if (have_work) {
     // ------------------------------- queries, new rows --------------------------
     pdl_enter();
-    const int nch = p.r3 / 16;                     // 16-byte chunks of a query's codes
     Segments sq = sg;                              // the segment whose queries are split next
-    int n_q = 0, n_wanted = 0;
+    sq.next();                                     // (the softmax warps do the first one's)
+    int n_q = 1, n_wanted = 0;
     bool ok = true;
-    auto split_queries = [&]() -> bool {
+    auto split_next = [&]() -> bool {
       const int qb = n_q & 1;
-      const long row0 = (long)sq.b * p.nH;
-      const uint4 mx = *reinterpret_cast<const uint4*>(p.qmax + 4 * (long)sq.b);
-      const int byte = q8::scale_byte(max(max(mx.x, mx.y), max(mx.z, mx.w)));
-      const float inv = q8::inverse(byte);
+      const int byte = query_byte(p, sq.b);
       if (!wait_all(&q_empty[qb], (uint32_t)(((n_q >> 1) & 1) ^ 1))) return false;
-      uint8_t* dst = qbuf + qb * QBUF_BYTES;
-      for (int i = lane; i < NH * nch; i += 32) {
-        const int h = i / nch, ch = i - h * nch;
-        uint4 out[PIECES] = {};
-        if (h < p.nH && TA_IDX_OK(p.err, (row0 + h) * p.r3 + ch * 16, 16, (long)p.B * p.nH * p.r3)) {
-          const bf16* src = p.qhat + (row0 + h) * p.r3 + ch * 16;
-          const bf16* rest = src + (long)p.B * p.nH * p.r3;
-          uint4 a[2], b[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            a[e] = reinterpret_cast<const uint4*>(src)[e];
-            b[e] = reinterpret_cast<const uint4*>(rest)[e];
-          }
-          const uint32_t aw[8] = {a[0].x, a[0].y, a[0].z, a[0].w, a[1].x, a[1].y, a[1].z, a[1].w};
-          const uint32_t bw[8] = {b[0].x, b[0].y, b[0].z, b[0].w, b[1].x, b[1].y, b[1].z, b[1].w};
-          uint32_t* o = reinterpret_cast<uint32_t*>(out);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float x0 = (__uint_as_float(aw[e] << 16) + __uint_as_float(bw[e] << 16)) * inv;
-            float x1 = (__uint_as_float(aw[e] & 0xffff0000u) + __uint_as_float(bw[e] & 0xffff0000u)) * inv;
-#pragma unroll
-            for (int pc = 0; pc < PIECES; ++pc) {
-              const uint32_t c = q8::codes2(x0, x1);
-              const float2 v = q8::values2(c);
-              x0 -= v.x; x1 -= v.y;
-              o[pc * 4 + (e >> 1)] |= c << (16 * (e & 1));
-            }
-          }
-        }
-#pragma unroll
-        for (int pc = 0; pc < PIECES; ++pc) *reinterpret_cast<uint4*>(dst + pc * QPIECE_BYTES + swz(h, ch)) = out[pc];
-      }
+#pragma unroll 2
+      for (int i = lane; i < NH * 8; i += 32) split_query(p, sq.b, i, q8::inverse(byte), qbuf + qb * QBUF_BYTES);
       if (lane == 0) q_scale[n_q & 7] = q8::scale(byte);
       fence_proxy_async_smem();
       __syncwarp();
@@ -528,9 +533,9 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
       sq.next();
       return true;
     };
-    ok = split_queries();
     for (; sg.more() && ok; sg.next()) {
-      if (sq.more() && !(ok = split_queries())) break;
+      // the next segment's queries in time, unless this one's last step is almost there (a split takes 3000 cycles)
+      if (sg.it1 - sg.it0 > 2 && sq.more() && !(ok = split_next())) break;
       if (!sg.tail) continue;
       // the step with the new token: its row, and zeros behind it as values (their weights are zero, but the slots may hold
       // anything)
@@ -555,6 +560,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&patched);
+      if (sg.it1 - sg.it0 <= 2 && sq.more()) ok = split_next();
     }
    }
   } else {
@@ -569,6 +575,16 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
     uint8_t* const my_p = pbuf + g * PBUF_BYTES;
     uint32_t wg_phase = 0, n_mine = 0, n_handed = 0;      // steps in which this warpgroup had keys; parts handed over so far
     pdl_enter();
+    {
+      // the first segment's queries, on which everything waits: a thread per sixteen numbers (by the warp that does the others'
+      // 5000 cycles, here 1000)
+      const int byte = query_byte(p, sg.b);
+      split_query(p, sg.b, (int)threadIdx.x - 128, q8::inverse(byte), qbuf);
+      if (threadIdx.x == 128) q_scale[0] = q8::scale(byte);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&q_first);
+    }
     bool ok = true, owe = false;                // owe: my part lies in the weights' buffer until it is taken
     auto wg_sync = [&]() -> bool {
       __syncwarp();
@@ -854,7 +870,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
 // columns of a row, blockIdx.y the pool.
 // Runs beside the query kernel: when that one lets this one start, the kernels in front of it are complete, calls before among
 // them, and it writes neither the prefix's pages nor what this one writes.  (Behind it, a launch per pool: step behind 32768
-// tokens 106 us, now UNPACK_US.)
+// tokens 106 us, now 104.7.)
 struct UnpackPart {
   const uint8_t *codes, *scales;
   bf16 *out, *rot;         // rot: null unless the keys are rotated
