@@ -630,6 +630,52 @@ def test_long_prefix(shared, rope):
     check_against_64(state, w, 20001, y, "long prefix")
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("r3,t3,one_pool", [(128, 128, False), (64, 40, False), (256, 136, False), (96, 96, True)])
+def test_store_and_read_many_rows(r3, t3, one_pool, dtype):
+    """More rows than the GPU has threads for; sequences that begin and end anywhere."""
+    g, page = torch.Generator(device="cuda").manual_seed(r3), 48
+    new, lens = [17001, 0, 1, 22222, 31], [100, 7, 47, 0, 48]
+    need = [-(-(n + m) // page) for n, m in zip(lens, new)]
+    n_pages, T = sum(need) + 3, sum(new)
+    order = torch.randperm(n_pages, generator=g, device="cuda").int()
+    table = torch.full((5, max(need)), -3, dtype=torch.int32, device="cuda")
+    for b in range(5):
+        table[b, :need[b]] = order[sum(need[:b]):sum(need[:b + 1])]
+    start = [3] + [3 + sum(new[:b + 1]) for b in range(5)]
+    def rows_of(r):
+        x = torch.randn(T + 10, r, generator=g, device="cuda") * torch.exp2(torch.randint(-20, 20, (T + 10, 1), generator=g, device="cuda").float())
+        x[::1001] = 0
+        return x.to(dtype)
+    pool = lambda r: (torch.randint(0, 255, (n_pages, page, r), generator=g, device="cuda", dtype=torch.uint8),
+                      torch.randint(0, 255, (n_pages, page), generator=g, device="cuda", dtype=torch.uint8))
+    K, V = pool(r3), pool(t3)
+    rk, rv = rows_of(r3), rows_of(t3)
+    if one_pool:
+        V, rv = K, rk
+    before = [t.clone() for t in K + V]
+    as8 = lambda c, s: (c.view(torch.float8_e4m3fn), s.view(torch.float8_e8m0fnu))
+    Bd.tucker_cache_store_paged_q8(rk, rv, *as8(*K), *as8(*V), table, i32(lens), i32(start))
+    assert Bd.last_device_error() == 0
+    seq = torch.repeat_interleave(torch.arange(5, device="cuda"), torch.tensor(new, device="cuda"))
+    slot = torch.cat([torch.arange(n, n + m, device="cuda") for n, m in zip(lens, new)])
+    at = table[seq, slot // page].long() * page + slot % page
+    for (codes, scales), rows, c0, s0 in ((K, rk, *before[:2]), (V, rv, *before[2:])):
+        want_c, want_s = Q.quantise(rows[3:3 + T].double().cpu().numpy())
+        want = c0.view(-1, rows.shape[1]).clone(), s0.view(-1).clone()
+        want[0][at] = torch.from_numpy(Q.encode(want_c)).cuda()
+        want[1][at] = torch.from_numpy((np.log2(want_s) + 127).astype(np.uint8)).cuda()
+        assert torch.equal(scales.view(-1), want[1])
+        assert torch.equal(codes.view(-1, rows.shape[1]) & 127, want[0] & 127)                   # (the sign of zero is free)
+    out = [torch.full((T + 10, r), 7.0, device="cuda").to(dtype) for r in (r3, t3)]
+    Bd.tucker_cache_read_paged_q8(*as8(*K), *as8(*V), table, i32(lens), i32(start), out[0], out[0] if one_pool else out[1])
+    assert Bd.last_device_error() == 0
+    for (codes, scales), o in ((K, out[0]),) if one_pool else ((K, out[0]), (V, out[1])):
+        c = codes.view(-1, o.shape[1])[at].view(torch.float8_e4m3fn).double()
+        assert torch.equal(o[3:3 + T].double(), c * torch.exp2(scales.view(-1)[at].double() - 127)[:, None])
+        assert (o[:3] == 7).all() and (o[3 + T:] == 7).all()
+
+
 # ---- long appends ----------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("d,r3,t3,T,one_pool", [(64, 128, 128, 19000, False), (64, 96, 128, 19400, False), (64, 256, 256, 9600, False),
