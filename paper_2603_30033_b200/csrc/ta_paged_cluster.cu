@@ -19,9 +19,10 @@
 //      z[j] = sum_a sum_c Ct[a, j, c] u[a, c], received by everybody.
 //   5  y = z Ut2^T: CTA r takes an eighth of the rows.
 // All arithmetic is fp32 from the stored values on (the tensor-core path carries q and z as two bf16 numbers each);
-// only what is stored is rounded.  Sums are taken in a fixed order.  Over an 8-bit cache (C = e4m3) a key's scale multiplies its
-// scores, a value's scale the weights that its row is taken with; the new token's rows are rounded before they are used.  The weights are read once per sequence and the
-// scores take FMAs, so that this form is for small batches of short contexts only: see cluster_step_pays.
+// only what is stored is rounded.  Sums are taken in a fixed order.  Over an 8-bit cache (Cache = e4m3) a key's scale multiplies
+// its scores, a value's scale the weights that its row is taken with; the new token's rows are rounded before they are used.
+// The weights are read once per sequence and the scores take FMAs, so that this form is for small batches of short contexts
+// only: see cluster_step_pays.
 //
 // Bounded by latency: d 768, 12 heads, ranks 64, one sequence of 37 tokens 11.2 us (19.3 as four launches), of which
 // 1.4 wait for the first loads and 0.6 to 1.5 go to each later phase; a tile of 64 keys per CTA 1.3 us (scores and
@@ -817,6 +818,9 @@ bool cluster_step_supported(const tucker_attn_desc& d, bool one_pool, bool q8) {
 // 19.6; 15 of 2048 19.0 / 27.6; 16 (a second wave) of 1024 27.6 / 23.6; fp32, 1 of 64 12.2 / 31.4, 4 of 2048 19.8 /
 // 41.2, 36 of 8192 146 / 505.
 // d 4096, 32 heads, ranks 128, 4 of 64 keys 25.2 / 27.2, of 1024 33.0 / 27.7.
+// Over an 8-bit cache (this form / tensor cores, whose streaming kernel has more to set up): 1 of 64 12.1 / 23.8, of 2048 19.6 /
+// 23.7, of 4096 29.6 / 22.6; 15 of 2048 19.9 / 25.6; 16 of 1024 29.0 / 24.6; d 4096, 4 of 64 25.7 / 29.8, of 1024 34.0 / 29.3;
+// fp32 (generic kernels), 1 of 64 11.8 / 33.2, of 8192 49.2 / 48.0.
 bool cluster_step_pays(const tucker_attn_desc& d, int64_t slots, int32_t prefix_len, bool tensor_cores, bool q8) {
   const bool f32 = d.dtype == TA_DTYPE_F32;
   const int at_once = q8 ? (f32 ? pgc::clusters_at_once<float, e4m3>() : pgc::clusters_at_once<bf16, e4m3>())
@@ -826,7 +830,7 @@ bool cluster_step_pays(const tucker_attn_desc& d, int64_t slots, int32_t prefix_
   const double keys = (double)slots + prefix_len, w = (double)d.n_H * (d.r3 + d.t3);
   const double waves = (d.B + at_once - 1) / at_once;
   const double here = waves * (10. + (f32 ? 2.3 : 3.2) * mb + keys / 1024. * (2.9 + w / 940.));
-  const double there = tensor_cores ? 20.5 + 1.6 * mb : 30. + 1.6 * mb + 0.8e-3 * d.B * keys * w / 1536.;
+  const double there = tensor_cores ? (q8 ? 23.5 : 20.5) + 1.6 * mb : 30. + 1.6 * mb + 0.8e-3 * d.B * keys * w / 1536.;
   return here < there;
 }
 

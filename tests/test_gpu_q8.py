@@ -2,6 +2,10 @@
 
 Whatever no call may use (slots past a length, pages of nobody, table entries past a sequence's last page) holds NaN codes, any
 scale bytes and bad page numbers in every state here."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -726,3 +730,27 @@ def test_append_of_long_prompts(d, r3, t3, T, one_pool, rope):
         assert (top <= 448 * s * (1 + 5e-5)).all() and ((top >= 224 * s * (1 - 5e-5))).all()
         bound = torch.maximum(Q.U_E4M3 * want.abs(), 2.0 ** -10 * s) + 1e-4 * top        # see check_pool
         assert ((got - want).abs() <= bound).all()
+
+
+# ---- the bounds-checking build ---------------------------------------------------------------------------------------
+
+CHILD = "TA_BOUNDS_CHECK_CHILD"
+
+
+@pytest.mark.skipif(os.environ.get(CHILD) == "1", reason="already inside the bounds-checking run")
+def test_under_the_bounds_checking_build():
+    """Every global index that the kernels form lies in its tensor: the tests that assert a device error word of zero, once more in a
+    child process that loads the build which checks."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    env = dict(os.environ, TUCKER_ATTN_LIB="checked")
+    env[CHILD] = "1"
+    sel = "decode_shapes or decode_prefix or page_sizes or many_tiles or long_prefix or append or store or read or one_launch or q8_library"
+    r = subprocess.run([sys.executable, "-m", "pytest", "-x", "-v", "-m", "gpu", "-k", sel, "-p", "no:cacheprovider", os.path.abspath(__file__)],
+                       env=env, cwd=root, capture_output=True, text=True, timeout=1500)
+    assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
+    assert "test_q8_library_checks PASSED" in r.stdout
+
+
+@pytest.mark.skipif(os.environ.get(CHILD) != "1", reason="runs only inside the bounds-checking run")
+def test_q8_library_checks():
+    assert Bd.bounds_checked()
