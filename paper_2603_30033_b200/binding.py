@@ -546,8 +546,13 @@ def tucker_cache_append_paged_q8(X, U3, Ut3, Kpages, Kscale, Vpages, Vscale, blo
     r3, t3, B = U3.shape[1], Ut3.shape[1], cache_len.shape[0]
     dt, dev, i32 = X.dtype, X.device, torch.int32
     code = _dtype_code(X)
-    _check_all(((X, "X", (T, d)), (U3, "U3", (d, r3)), (Ut3, "Ut3", (d, t3))), dt, dev)
-    _check_all(((cache_len, "cache_len", (B,)), (tok_start, "tok_start", (B + 1,))), i32, dev)
+    idx = dev.index
+    if not (X.is_cuda and dt is U3.dtype is Ut3.dtype and i32 is cache_len.dtype is tok_start.dtype
+            and idx == U3.get_device() == Ut3.get_device() == cache_len.get_device() == tok_start.get_device()
+            and U3.shape[0] == Ut3.shape[0] == d and tok_start.shape == (B + 1,)
+            and X.is_contiguous() and U3.is_contiguous() and Ut3.is_contiguous() and cache_len.is_contiguous() and tok_start.is_contiguous()):
+        _check_all(((X, "X", (T, d)), (U3, "U3", (d, r3)), (Ut3, "Ut3", (d, t3))), dt, dev)
+        _check_all(((cache_len, "cache_len", (B,)), (tok_start, "tok_start", (B + 1,))), i32, dev)
     cache = _q8_cache(Kpages, Kscale, Vpages, Vscale, block_table, r3, t3, dev)
     if block_table.shape[0] != B:
         raise ValueError(f"block_table has shape {tuple(block_table.shape)}, expected {B} rows")
@@ -575,8 +580,12 @@ def _q8_rows(Krows, Vrows, Kpages, Kscale, Vpages, Vscale, block_table, slots, t
     (T, r3), t3, B = Krows.shape, Vrows.shape[1], slots.shape[0]
     dt, dev = Krows.dtype, Krows.device
     code = _dtype_code(Krows)
-    _check_all(((Krows, "Krows", (T, r3)), (Vrows, "Vrows", (T, t3))), dt, dev)
-    _check_all(((slots, slots_name, (B,)), (tok_start, "tok_start", (B + 1,))), torch.int32, dev)
+    if not (Krows.is_cuda and dt is Vrows.dtype and slots.dtype is tok_start.dtype is torch.int32
+            and dev.index == Vrows.get_device() == slots.get_device() == tok_start.get_device()
+            and Vrows.shape[0] == T and tok_start.shape == (B + 1,)
+            and Krows.is_contiguous() and Vrows.is_contiguous() and slots.is_contiguous() and tok_start.is_contiguous()):
+        _check_all(((Krows, "Krows", (T, r3)), (Vrows, "Vrows", (T, t3))), dt, dev)
+        _check_all(((slots, slots_name, (B,)), (tok_start, "tok_start", (B + 1,))), torch.int32, dev)
     cache = _q8_cache(Kpages, Kscale, Vpages, Vscale, block_table, r3, t3, dev)
     if block_table.shape[0] != B:
         raise ValueError(f"block_table has shape {tuple(block_table.shape)}, expected {B} rows")
