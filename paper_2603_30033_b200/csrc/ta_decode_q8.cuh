@@ -867,39 +867,53 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
 
 // The prefix that all sequences share, as the attention kernel of all rows reads it: values of the codes, bf16 (exact), row
 // after row; one pool with RoPE: the keys rotated, in two halves (see k_prefix_rotate), and the rows.  A thread per eight
-// columns of a row, blockIdx.y the pool.
+// columns of UNPACK_ROWS rows, blockIdx.y the pool.
 // Runs beside the query kernel: when that one lets this one start, the kernels in front of it are complete, calls before among
-// them, and it writes neither the prefix's pages nor what this one writes.  (Behind it, a launch per pool: step behind 32768
-// tokens 106 us, now 104.7.)
+// them, and it writes neither the prefix's pages nor what this one writes.  (Step behind 32768 tokens, 100 us: 1.3 more behind it
+// with a launch per pool; 0.8 more with a row per thread, found by long divisions.)
 struct UnpackPart {
   const uint8_t *codes, *scales;
   bf16 *out, *rot;         // rot: null unless the keys are rotated
   int r;
 };
-__global__ void __launch_bounds__(256) k_prefix_unpack_q8(const UnpackPart first, const UnpackPart second, const int32_t* __restrict__ table,
+constexpr int UNPACK_THREADS = 256, UNPACK_ROWS = 4;
+__host__ __device__ inline int unpack_block_rows(int r) { return UNPACK_THREADS / (r / 8) * UNPACK_ROWS; }
+__global__ void __launch_bounds__(UNPACK_THREADS) k_prefix_unpack_q8(const UnpackPart first, const UnpackPart second, const int32_t* __restrict__ table,
                                                           int n_pages, int page_size, long rows, int P, const dec::RopeTurns turns,
                                                           unsigned int* err) {
   const UnpackPart& u = blockIdx.y == 0 ? first : second;
-  const int r = u.r, per = r / 8;
-  const long lo = rows * r, i = (long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (long)P * per) {
-    pdl_enter();
-    return;
-  }
-  const int n = (int)(i / per), c = (int)(i % per) * 8;
-  const int pg = table[n / page_size];
-  float f[8] = {};
-  if (pg >= 0 && pg < n_pages) {
-    const long row = (long)pg * page_size + n % page_size;
-    const float s = q8::scale(u.scales[row]);
-    q8::values8(*reinterpret_cast<const uint2*>(u.codes + row * r + c), f);
+  const int r = u.r, per = r / 8, at_once = UNPACK_THREADS / per;
+  const int mine = (int)threadIdx.x / per, c = ((int)threadIdx.x - mine * per) * 8;
+  const long lo = rows * r, n0 = (long)blockIdx.x * (at_once * UNPACK_ROWS) + mine;
+  const uint8_t* src[UNPACK_ROWS];
+  float sc[UNPACK_ROWS];
+  uint2 codes[UNPACK_ROWS];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] *= s;
-  } else {
-    atomicOr(err, (unsigned)TA_DEVERR_BAD_PAGE);
+  for (int k = 0; k < UNPACK_ROWS; ++k) {
+    const long n = n0 + k * at_once;
+    src[k] = nullptr;
+    sc[k] = 0.f;
+    if (mine < at_once && n < P) {
+      const int slot = (int)n, j = slot / page_size, pg = table[j];
+      if (pg >= 0 && pg < n_pages) {
+        const long row = (long)pg * page_size + (slot - j * page_size);
+        src[k] = u.codes + row * r + c;
+        sc[k] = q8::scale(u.scales[row]);
+      } else {
+        atomicOr(err, (unsigned)TA_DEVERR_BAD_PAGE);
+      }
+    }
   }
-  const long at = (long)n * r + c;
-  if (TA_IDX_OK(err, at, 8, lo)) {
+#pragma unroll
+  for (int k = 0; k < UNPACK_ROWS; ++k) codes[k] = src[k] ? *reinterpret_cast<const uint2*>(src[k]) : make_uint2(0u, 0u);
+#pragma unroll
+  for (int k = 0; k < UNPACK_ROWS; ++k) {
+    const long n = n0 + k * at_once, at = n * r + c;
+    if (mine >= at_once || n >= P || !TA_IDX_OK(err, at, 8, lo)) continue;
+    float f[8];
+    q8::values8(codes[k], f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] *= sc[k];
     uint32_t w[4], wl[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[e] = pack_bf16(f[2 * e], f[2 * e + 1]);
@@ -907,7 +921,7 @@ __global__ void __launch_bounds__(256) k_prefix_unpack_q8(const UnpackPart first
     if (u.rot) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float2 cs = dec::rope_at(n, turns, c / 2 + e);
+        const float2 cs = dec::rope_at((int)n, turns, c / 2 + e);
         const float re = f[2 * e] * cs.x - f[2 * e + 1] * cs.y, ro = f[2 * e] * cs.y + f[2 * e + 1] * cs.x;
         w[e] = pack_bf16(re, ro);
         const float2 v = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[e]));

@@ -770,8 +770,8 @@ int launch_prefix_unpack(Problem& p, const FastDecWs& w, const PrefixPlan& q) {
   const tucker_attn_desc& d = p.d;
   const decq::UnpackPart k = {(const uint8_t*)p.Kc, p.Ks, w.pre_k, nullptr, d.r3};
   const decq::UnpackPart v = {(const uint8_t*)p.Vc, p.Vs, w.pre_v, p.shared_rope ? w.pre_k : nullptr, d.t3};
-  const long n = (long)p.prefix_len * (std::max(d.r3, d.t3) / 8);
-  (void)launch_pdl(decq::k_prefix_unpack_q8, dim3((unsigned)((n + 255) / 256), p.shared_kv ? 1 : 2), dim3(256), 0, p.stream,
+  const int per = decq::unpack_block_rows(std::max(d.r3, d.t3));      // the wider pool's blocks, at least as many as the other's
+  (void)launch_pdl(decq::k_prefix_unpack_q8, dim3((unsigned)((p.prefix_len + (long)per - 1) / per), p.shared_kv ? 1 : 2), dim3(decq::UNPACK_THREADS), 0, p.stream,
                    p.shared_rope ? v : k, v, p.prefix_table, p.pv.n_pages, p.pv.page_size, (long)q.n_kt * prefix::TK, p.prefix_len,
                    rope_turns(d), p.dev_err);
   TA_LAUNCH_CHECK(p);
