@@ -79,6 +79,9 @@ constexpr int S_SLOTS = 4, S_AHEAD = 3;          // steps whose scale bytes have
 constexpr size_t SMEM_BYTES = 1024 + (size_t)RING_BYTES + 2 * QBUF_BYTES + 2 * PBUF_BYTES + S_SLOTS * 2 * SK;
 static_assert(SMEM_BYTES <= 224 * 1024, "one CTA's shared memory, with the static part");
 constexpr float kTop = 15.f, kStart = 5.f;      // weights reach 2^kTop at most, the largest is 2^kStart when a reference is set
+// Rows of zeros count as if of this scale's exponent, negated: far below any other's, and not so far that their part of the sum
+// is lost (2^-126) where the other rows' scales are below 2^29.
+constexpr int kZeroRow = 90;
 constexpr float kRestUp = 8.f;                  // what a piece leaves of a weight is below 2^(kTop - 3)
 
 struct Params {
@@ -612,8 +615,25 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         tc_fence_after();
         const uint8_t* sc = scales + slot * 2 * SK + g * TK + tid;
         const int kb = sc[0], vb = sc[SK];
-        const float kq = q8::scale(kb) * q_scale[seg & 7], ev = vb == q8::kNan ? NAN : (float)(vb - 127);
-        float inv = vb == q8::kNan ? NAN : q8::scale(254 - vb);
+        const float kq = q8::scale(kb) * q_scale[seg & 7];
+        float ev = vb == q8::kNan ? NAN : (float)(vb - 127), inv = vb == q8::kNan ? NAN : q8::scale(254 - vb);
+        if (__any_sync(0xffffffffu, vb == 127)) {
+          // A row of zeros has the scale 1, among value rows of 2^-30 too, whose weights it would push below what their bytes hold;
+          // as would one with a key that most queries like, among any.  It adds nothing to the output whatever its weight is
+          // multiplied by, so that is 2^-kZeroRow for it.  (Other rows come here only with a largest number of 224 to 448; the
+          // tile has not been waited for otherwise.)
+          if (!(ok = wait_all(&vfull[it % VS], (uint32_t)((it / VS) & 1)))) break;
+          if (vb == 127) {
+            const uint8_t* const row = vring + (size_t)(it % VS) * STEP_BYTES + (g * TK + tid) * 128;
+            uint32_t any = 0;
+#pragma unroll 1
+            for (int c = 0; c < 8; ++c) {
+              const uint4 v = *reinterpret_cast<const uint4*>(row + ((c ^ (tid & 7)) << 4));
+              any |= v.x | v.y | v.z | v.w;
+            }
+            if ((any & 0x7f7f7f7fu) == 0) { ev = (float)-kZeroRow; inv = q8::scale(127 + kZeroRow); }
+          }
+        }
         // log2 of p 2^k', relative to the references (by halves, for the registers)
         const uint64_t kq2 = pack2(kq, kq), ev2 = pack2(ev, ev);
         float a[NH];

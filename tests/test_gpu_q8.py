@@ -624,6 +624,33 @@ def test_one_key_outweighs_thousands_of_equal_ones(nats):
     P.check_rows(host(y), np.repeat(reference64(*one, 0, stored(u3), stored(ut3)), B, 0), "bf16", f"{nats} nats")
 
 
+@pytest.mark.parametrize("scale", [-30, -12, 0, 30])
+@pytest.mark.parametrize("shared", [False, True])
+def test_value_rows_of_zeros_among_small_and_large_ones(scale, shared):
+    """Rows of zeros have the scale 1 whatever the others have; some of them get most of the weight (a key that many queries like,
+    whose value row is nothing)."""
+    state, w = big_state({**TC64, "n_H": 4}, [3000, 500, 129], 64, rope=False, shared=shared)
+    x, dw, (K, Ks, V, Vs), table, dl, _ = state
+    dw[7] *= 2.0 ** (scale // 5 if shared else scale)           # the new tokens' value rows of the others' size (one pool: dw[3] too)
+    if not shared:
+        Vs.view(torch.uint8)[:] = 120 + scale
+        V.view(torch.uint8)[:, ::5] = 0
+        Vs.view(torch.uint8)[:, ::5] = 127
+        Ks.view(torch.uint8)[:, 10] += 3
+    else:
+        Ks.view(torch.uint8)[:] = 120 + scale // 5
+        K.view(torch.uint8)[:, ::5] = 0
+        Ks.view(torch.uint8)[:, ::5] = 127
+    y = Bd.tucker_attn_decode_paged_q8(x, *dw, K, Ks, V, Vs, table, dl, n_H=w.n_H, rope=False, append=False)
+    assert Bd.last_device_error() == 0 and Bd.last_path() == 2
+    u3, ut3 = (x.double() @ dw[i].double() for i in (3, 7))
+    def stored(t):
+        c, sc = Q.quantise(t.cpu().numpy())
+        return torch.from_numpy(c * sc[:, None]).cuda()
+    ref = reference64(state, w, 0, stored(u3), stored(ut3))
+    P.check_rows(host(y), ref, "bf16", f"scale {scale}")
+
+
 @pytest.mark.parametrize("shared", [False, True])
 @pytest.mark.parametrize("rope", [True, False])
 def test_long_prefix(shared, rope):
