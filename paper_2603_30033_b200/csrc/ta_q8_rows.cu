@@ -5,8 +5,8 @@
 // shuffle away and a warp's loads and stores are whole rows next to each other.  A row's place (its sequence, the table, two
 // divisions) is 80 instructions and a chain of loads.  One lane finds it, not all of the row's, and where there are more rows than
 // the GPU has threads for, a warp finds those of kRows times as many rows at once.  112 thousand rows of 128 and 128 read (87 MB, 13.4 us
-// at the copy rate): 27.3 us with a search per thread, 25.6 with four rows each, 14.8 with a search per row as well; 32768 rows
-// stored 8.3 -> 6.8.
+// at the copy rate): 27.3 us with a search per thread, 25.6 with four rows each, 14.8 with a search per row as well; 23 thousand
+// rows stored 8.3 -> 6.8.
 #include "ta_paged.cuh"
 #include "ta_q8.cuh"
 
