@@ -554,7 +554,9 @@ LONG = [("one sequence over all CTAs", TC128, [60000], 64),
         ("many short sequences per CTA", TC96, [(37 * i) % 300 for i in range(1500)], 16),
         ("one tile each, several per CTA", TC_KV, [(11 * i) % 128 for i in range(900)], 128),
         ("two tiles each", TC_VK, [128 + (7 * i) % 100 for i in range(500)], 32),
-        ("ragged batch", TC128, [1000 * (i % 13) + 77 * i for i in range(64)], 256)]
+        ("ragged batch", TC128, [1000 * (i % 13) + 77 * i for i in range(64)], 256),
+        ("pages that a step straddles", TC64, [383, 384, 385, 6000, 767, 129, 9001], 384),
+        ("one head, pages of 640", dict(d_model=64, n_H=1, r=(1, 32, 96), t=(1, 32, 96)), [641, 639, 1280, 5000, 0], 640)]
 
 
 @pytest.mark.parametrize("shared", ["two pools", "one pool", "one pool, rotated"])
