@@ -30,7 +30,8 @@
 // to 3000 cycles each, what the bytes and the softmax warps' chains (2100) need, and about 25 thousand cycles go to the
 // division of the work, the first pass over cold code and the last segment's end.  What was tried: references and sums in
 // registers with everything of a step formed at once (300 bytes of spills, 126 us); four softmax warpgroups of 16 heads
-// (113); a pass over the loop before the queries are there, for the code (109).
+// (113); a pass over the loop before the queries are there, for the code (109); all scores loaded at once, or the accumulator
+// rescaled behind the weights instead of in front of them (both 110, with spills).
 //
 //   warp 0       TMA producer of keys and values
 //   warp 1       TMEM allocation, MMA issue of the scores, a step ahead of the values
