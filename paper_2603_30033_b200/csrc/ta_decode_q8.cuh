@@ -15,7 +15,7 @@
 //   O^T [t3 x 32 heads] += V_codes^T * (p 2^k')    The weight is carried as three e5m2 numbers: the upper byte of an f16, the
 //       upper byte of 8 times what is left, and of 8 times what is left then, rounded (2^-10 together; a byte's worth of an f16
 //       is an e5m2, so this is masking and exact subtraction).  The three are 96 columns of one product and of the accumulator,
-//       and are added up once per segment.  With a head's largest weight at 2^5 .. 2^15, all are held to 2^-28 of the largest.
+//       and are added up once per segment.  With a head's largest weight at 2^4 .. 2^15, all are held to 2^-27 of the largest.
 //       (Without the factors, for which their columns have room, to 2^-22: 12000 equal weights behind one of e^14 times theirs
 //       came out 6% off; the factors cost 1 us of 109.)
 //
@@ -79,7 +79,8 @@ constexpr int S_SLOTS = 4, S_AHEAD = 3;          // steps whose scale bytes have
 // rings | queries of two segments | weights of two warpgroups | scales
 constexpr size_t SMEM_BYTES = 1024 + (size_t)RING_BYTES + 2 * QBUF_BYTES + 2 * PBUF_BYTES + S_SLOTS * 2 * SK;
 static_assert(SMEM_BYTES <= 224 * 1024, "one CTA's shared memory, with the static part");
-constexpr float kTop = 15.f, kStart = 5.f;      // weights reach 2^kTop at most, the largest is 2^kStart when a reference is set
+// Weights reach 2^kTop at most; the largest is 2^(kStart - 1) to 2^(kStart + 1) when a reference is set, from a maximum of kFine at most.
+constexpr float kTop = 15.f, kStart = 5.f, kFine = 256.f;
 // Rows of zeros count as if of this scale's exponent, negated: far below any other's, and not so far that their part of the sum
 // is lost (2^-126) where the other rows' scales are below 2^29.
 constexpr int kZeroRow = 90;
@@ -699,12 +700,16 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
           }
         };
         int renew = first;
+        int coarse = 0;                                // a bit per head: its reference was set from a maximum too large for bf16
 #pragma unroll 1
         for (;;) {
           if (renew) {
             // ---- new references: the maxima of these keys where they are needed ----
-            // Of pairs of heads in bf16 (a reference only has to be near; what the rounding leaves above 2^kTop comes here
-            // again), by a butterfly whose levels keep half of the pairs each: lane 2 i + {0, 1} is left with pair i.
+            // Of pairs of heads in bf16 (a reference only has to be near), by a butterfly whose levels keep half of the pairs
+            // each: lane 2 i + {0, 1} is left with pair i.  The rounding is half a step, 2^-8 of the maximum: up to kFine it
+            // leaves the largest weight within a factor of two of 2^kStart.  Beyond, the reference can lie above every score by more
+            // than the weights have bits (from 2^13 on it left them all zero, and the output with them), and nothing but a
+            // second round here, on what is left of the scores, would bring it down again.
             uint32_t mx[NH / 2];
 #pragma unroll
             for (int h = 0; h < NH / 2; ++h) mx[h] = pack_bf16(a[2 * h], a[2 * h + 1]);
@@ -722,7 +727,9 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             if (!(ok = wg_sync())) break;
             // by how much the reference of head `lane` rises (it is 0 until the first step sets it)
             const float mt = fmaxf(fmaxf(max_s[g][0][lane], max_s[g][1][lane]), fmaxf(max_s[g][2][lane], max_s[g][3][lane]));
-            const float up = mt >= kTop || first ? mt - kStart : 0.f;
+            const bool move = mt >= kTop || first || (coarse >> lane & 1);
+            const float up = move ? mt - kStart : 0.f;
+            coarse = (int)__ballot_sync(0xffffffffu, move && fabsf(mt) > kFine && fabsf(mt) < INFINITY);
             m_lane += up;
             up_s[g][q][lane] = -up;
             neg_s[g][q][lane] = -m_lane;
@@ -733,6 +740,8 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
               a[h] += u.x; a[h + 1] += u.y; a[h + 2] += u.z; a[h + 3] += u.w;
             }
             if (!first) {
+              // (A reference comes down in a second round only, after a rise by more than kFine - kStart, which has left zeros of
+              // the sums and of the accumulator.)
               // the product of the step before must be complete before its accumulator is rescaled
               if (!free_seen && !(ok = wait_all(&p_free[g], par ^ 1u))) break;
               free_seen = true;
@@ -740,7 +749,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
 #pragma unroll
               for (int h = 0; h < NH; h += 2) {
                 const float2 u = *reinterpret_cast<const float2*>(&up_s[g][q][h]);
-                l2[h / 2] = mul2(l2[h / 2], pack2(ex2(u.x), ex2(u.y)));
+                l2[h / 2] = mul2(l2[h / 2], pack2(ex2(fminf(u.x, 0.f)), ex2(fminf(u.y, 0.f))));
               }
 #pragma unroll 1
               for (int h0 = 0; h0 < NH; h0 += 8) {
@@ -752,7 +761,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
 #pragma unroll
                 for (int h = 0; h < 8; h += 2) {
                   const float2 u = *reinterpret_cast<const float2*>(&up_s[g][q][h0 + h]);
-                  const uint64_t f = pack2(ex2(u.x), ex2(u.y));
+                  const uint64_t f = pack2(ex2(fminf(u.x, 0.f)), ex2(fminf(u.y, 0.f)));
 #pragma unroll
                   for (int pc = 0; pc < PIECES; ++pc) {
                     float x, y;
@@ -765,7 +774,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
               }
               tmem_st_wait();
             }
-            first = 0;
+            first = first && coarse;
           }
           // The vote is counted while half of the weights are formed, on the strength of there being none as a rule.
           float over = -INFINITY;
@@ -780,7 +789,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
           weights(0, sum);
           if (!(ok = wait_all(&wg_bar[g], ph))) break;
           ++wg_phase;
-          renew = *reinterpret_cast<volatile uint32_t*>(&votes[g][ph]) != 0u;
+          renew = ((int)*reinterpret_cast<volatile uint32_t*>(&votes[g][ph]) | coarse) != 0;
           if (!renew) break;
         }
         if (!ok) break;

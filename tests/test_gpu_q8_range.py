@@ -1,0 +1,73 @@
+"""8-bit paged cache at the ends of its range: scores of thousands, value rows of zeros among rows of any size, weights far below the
+largest.  Against 64 bits on the rows as the cache holds them."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_30033_b200 import binding as Bd
+from tests import paged_helpers as P
+from tests import q8_helpers as Q
+from tests.test_gpu_q8 import TC64, TC96, TC128, big_state, host, reference64
+
+pytestmark = pytest.mark.gpu
+
+
+def stored(rows):
+    """Rows (64 bits, on the device) as the cache holds them."""
+    c, s = Q.quantise(rows.cpu().numpy())
+    return torch.from_numpy(c * s[:, None]).cuda()
+
+
+def check(state, w, y, what, same=False):
+    """y of a step without a prefix and without RoPE; same: all sequences are the first."""
+    x, dw, pools, table, lens, ptab = state
+    assert Bd.last_device_error() == 0 and Bd.last_path() == 2, what
+    n = 1 if same else len(lens)
+    one = ((x[:n], dw, pools, table[:n], lens[:n], ptab), w)
+    new = [stored(x[:n].double() @ dw[i].double()) for i in (3, 7)]
+    ref = reference64(*one, 0, *new)
+    P.check_rows(host(y), np.repeat(ref, len(lens), 0) if same else ref, "bf16", what)
+
+
+def repeated(m, page=64):
+    """A state of 150 sequences that are the first one, m cached tokens each: every CTA has several steps, segments begin and end at
+    every place.  As many heads as core slices, so that the heads' queries [heads, r3] (64 bits, scaled) are independent."""
+    state, w = big_state({**TC128, "n_H": 8}, [m] + [0] * 149, page, rope=False)
+    x, dw, _, table, lens, _ = state
+    x[1:], table[1:], lens[1:] = x[0].clone(), table[0].clone(), m
+    C, U1, U2 = (t.double() for t in dw[:3])
+    q = torch.einsum("q,ha,aqc->hc", x[0].double() @ U2, U1, C) * (w.d_model / w.n_H) ** -0.5
+    return state, w, q
+
+
+def towards(q, target):
+    """The shortest key that every query gives the score `target`."""
+    return q.T @ torch.linalg.solve(q @ q.T, torch.full((len(q),), float(target), device=q.device, dtype=q.dtype))
+
+
+@pytest.mark.parametrize("nats", [1400, 5700, 11500])
+@pytest.mark.parametrize("since", [0, 1000])
+def test_scores_with_a_large_common_part(nats, since):
+    """All keys from slot `since` on share a part that adds `nats` (to a few percent) to every score, besides scores of a
+    standard deviation of 2.  A softmax does not see a common part.
+
+    Tolerance: the common part's codes are the same bytes in every row, and so is what the queries' rounding does to it.  Left is
+    fp32: eight roundings (four products of 32 coordinates, three pieces, a multiply-add) of at most 2^-23 of 16600 (11500 nats
+    in log2 units) are 0.016 at worst and 0.003 in the mean square, 0.2% of a weight, and independent from key to key; the bound of a step
+    with small scores holds as it is."""
+    m, split = 3000, 96
+    state, w, q = repeated(m)
+    x, dw, (K, Ks, V, Vs), table, lens, _ = state
+    top = towards(q[:, :split], nats)
+    k = int(torch.frexp(top.abs().amax() / 448).exponent)      # the codes' scale: the common part fills their range
+    g = torch.Generator(device="cuda").manual_seed(7)
+    kb = K.view(torch.uint8)
+    code = lambda v: (v * 2.0 ** -k).float().to(torch.float8_e4m3fn).view(torch.uint8)
+    kb[:, :, :split] = code(top)
+    noise = torch.randn(*K.shape[:2], K.shape[2] - split, generator=g, device="cuda") * (2.0 / q[:, split:].norm(dim=1).mean())
+    kb[:, :, split:] = code(noise)
+    Ks.view(torch.uint8)[:] = 127 + k
+    early = torch.arange(since, device="cuda")
+    kb[table[0, early // 64].long(), early % 64, :split] = 0
+    y = Bd.tucker_attn_decode_paged_q8(x, *dw, K, Ks, V, Vs, table, lens, n_H=w.n_H, rope=False, append=False)
+    check(state, w, y, f"{nats} nats since {since}", same=True)
