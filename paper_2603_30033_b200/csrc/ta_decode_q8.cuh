@@ -559,7 +559,9 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
       uint8_t* vt = vring + (size_t)(it % VS) * STEP_BYTES;
       uint8_t* kt = shared ? vt : ring + (size_t)(it % K_STAGES) * STEP_BYTES;
       if (lane < kch && !shared) *reinterpret_cast<uint4*>(kt + swz(row, lane)) = nr;
-      if (lane >= 8 && lane - 8 < vch) *reinterpret_cast<uint4*>(vt + swz(row, lane - 8)) = nr;
+      // (a value's whole line, of which a narrower row leaves zeros: where no box was requested nobody else fills it, and the
+      // softmax warps look for rows of zeros by the line)
+      if (lane >= 8 && lane < 16) *reinterpret_cast<uint4*>(vt + swz(row, lane - 8)) = nr;
 #pragma unroll 4
       for (int i = (row + 1) * 8 + lane; i < end * 8; i += 32) *reinterpret_cast<uint4*>(vt + i * 16) = make_uint4(0u, 0u, 0u, 0u);
       fence_proxy_async_smem();

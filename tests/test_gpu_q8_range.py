@@ -71,3 +71,19 @@ def test_scores_with_a_large_common_part(nats, since):
     kb[table[0, early // 64].long(), early % 64, :split] = 0
     y = Bd.tucker_attn_decode_paged_q8(x, *dw, K, Ks, V, Vs, table, lens, n_H=w.n_H, rope=False, append=False)
     check(state, w, y, f"{nats} nats since {since}", same=True)
+
+
+@pytest.mark.parametrize("shape", [TC64, {**TC96, "n_H": 8}], ids=["64", "96"])
+@pytest.mark.parametrize("cached", [64, 256])
+def test_new_value_row_of_zeros_in_a_fresh_tile(shape, cached):
+    """The new token's value row is zeros (x = 0) and lies where nothing was requested from the pools, among rows of 2^-30.  The row is
+    narrower than a line of the tile, whose rest is the kernel's to fill: a larger step before leaves other bytes there."""
+    before, wb = big_state(TC128, [5000] * 40, 64, rope=False)
+    state, w = big_state(shape, [cached] * 300, 64, rope=False)
+    x, dw, (K, Ks, V, Vs), table, lens, _ = state
+    x.zero_()
+    Vs.view(torch.uint8)[:] = 90
+    for _ in range(3):
+        Bd.tucker_attn_decode_paged_q8(before[0], *before[1], *before[2], *before[3:5], n_H=wb.n_H, rope=False, append=False)
+        y = Bd.tucker_attn_decode_paged_q8(x, *dw, K, Ks, V, Vs, table, lens, n_H=w.n_H, rope=False, append=False)
+        check(state, w, y, f"{cached} cached")
