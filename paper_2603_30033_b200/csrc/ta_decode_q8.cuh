@@ -81,9 +81,11 @@ constexpr size_t SMEM_BYTES = 1024 + (size_t)RING_BYTES + 2 * QBUF_BYTES + 2 * P
 static_assert(SMEM_BYTES <= 224 * 1024, "one CTA's shared memory, with the static part");
 // Weights reach 2^kTop at most; the largest is 2^(kStart - 1) to 2^(kStart + 1) when a reference is set, from a maximum of kFine at most.
 constexpr float kTop = 15.f, kStart = 5.f, kFine = 256.f;
-// Rows of zeros count as if of this scale's exponent, negated: far below any other's, and not so far that their part of the sum
-// is lost (2^-126) where the other rows' scales are below 2^29.
-constexpr int kZeroRow = 90;
+// What references are set by is this much less for a row of zeros: below any other row's (scales are 2^-96 and more), and no more
+// than leaves its weights, 2^(kTop + kZeroRow) at most, in fp32.  The sums are in units of 2^kSumUnit, so that a million such weights
+// fit.  Upwards there is room for scales of 2^87: then 2^-24 of the largest weight is 2^-126 of the sum's unit.
+constexpr float kZeroRow = 108.f;
+constexpr int kSumUnit = 20;
 constexpr float kRestUp = 8.f;                  // what a piece leaves of a weight is below 2^(kTop - 3)
 
 struct Params {
@@ -268,7 +270,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
   __shared__ int abort_flag;
   __shared__ float q_scale[8];                   // of segment i at i & 7: the queries are split at most three segments ahead
   __shared__ uint32_t votes[NWG][2];             // a byte per warp, by parity of the step
-  __shared__ float max_s[NWG][4][NH], sum_s[NWG][4][NH], hand_m[NH], hand_l[NH];
+  __shared__ float max_s[NWG][4][NH], sum_s[NWG][4][NH], hand_m[NH], hand_l[NH], hand_f[NH];
   __shared__ __align__(16) float up_s[NWG][4][NH], neg_s[NWG][4][NH];      // a warp's own: minus the references, minus their rise
   __shared__ long long wtot_s[THREADS / 32];
   __shared__ int loc_b;
@@ -620,12 +622,13 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         const uint8_t* sc = scales + slot * 2 * SK + g * TK + tid;
         const int kb = sc[0], vb = sc[SK];
         const float kq = q8::scale(kb) * q_scale[seg & 7];
-        float ev = vb == q8::kNan ? NAN : (float)(vb - 127), inv = vb == q8::kNan ? NAN : q8::scale(254 - vb);
+        const float ev = vb == q8::kNan ? NAN : (float)(vb - 127);
+        float inv = vb == q8::kNan ? NAN : q8::scale(max(254 - kSumUnit - vb, 0)), low = 0.f;
         if (__any_sync(0xffffffffu, vb == 127)) {
           // A row of zeros has the scale 1, among value rows of 2^-30 too, whose weights it would push below what their bytes hold;
-          // as would one with a key that most queries like, among any.  It adds nothing to the output whatever its weight is
-          // multiplied by, so that is 2^-kZeroRow for it.  (Other rows come here only with a largest number of 224 to 448; the
-          // tile has not been waited for otherwise.)
+          // as would one with a key that most queries like, among any.  It adds nothing to the output, whatever its weight: that
+          // goes into the sum as it is, into the product as zero, and into references as if 2^-kZeroRow.  (Other rows come here only
+          // with a largest number of 224 to 448; the tile has not been waited for otherwise.)
           if (!(ok = wait_all(&vfull[it % VS], (uint32_t)((it / VS) & 1)))) break;
           if (vb == 127) {
             const uint8_t* const row = vring + (size_t)(it % VS) * STEP_BYTES + (g * TK + tid) * 128;
@@ -635,7 +638,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
               const uint4 v = *reinterpret_cast<const uint4*>(row + ((c ^ (tid & 7)) << 4));
               any |= v.x | v.y | v.z | v.w;
             }
-            if ((any & 0x7f7f7f7fu) == 0) { ev = (float)-kZeroRow; inv = q8::scale(127 + kZeroRow); }
+            if ((any & 0x7f7f7f7fu) == 0) low = kZeroRow;
           }
         }
         // log2 of p 2^k', relative to the references (by halves, for the registers)
@@ -714,7 +717,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             // second round here, on what is left of the scores, would bring it down again.
             uint32_t mx[NH / 2];
 #pragma unroll
-            for (int h = 0; h < NH / 2; ++h) mx[h] = pack_bf16(a[2 * h], a[2 * h + 1]);
+            for (int h = 0; h < NH / 2; ++h) mx[h] = pack_bf16(a[2 * h] - low, a[2 * h + 1] - low);
 #pragma unroll
             for (int lev = 8; lev >= 1; lev >>= 1) {
               const bool upper = lane & (2 * lev);
@@ -783,7 +786,7 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
 #pragma unroll
           for (int h = 0; h < NH; h += 2) over = max3(over, a[h], a[h + 1]);
           const uint32_t ph = wg_phase & 1u;
-          const bool vote = __any_sync(0xffffffffu, over > kTop);
+          const bool vote = __any_sync(0xffffffffu, over - low > kTop);
           if (lane == 0) {
             reinterpret_cast<uint8_t*>(&votes[g][ph])[q] = vote ? 1 : 0;
             mbar_arrive(&wg_bar[g]);
@@ -798,6 +801,10 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
 #pragma unroll
         for (int h = 0; h < NH / 4; ++h) l2[h] = sum[h];
         weights(1, l2 + NH / 4);
+        if (low != 0.f) {
+#pragma unroll
+          for (int i = 0; i < 2 * PIECES * 4; ++i) (&out[0][0][0])[i] = 0;
+        }
         if (!free_seen && !(ok = wait_all(&p_free[g], par ^ 1u))) break;
         if (owe) {                                     // a part laid down in the weights' buffer must have been taken
           if (!(ok = wait_all(&taken, (n_handed - 1) & 1u))) break;
@@ -848,14 +855,25 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&o_read[g]);        // the next segment may overwrite the accumulator
+        // From here on references are of the weights alone, without the scales (exponents in which parts would differ by more than
+        // fp32 holds, one of rows of zeros and one of large values): the sum becomes a number of [1, 2).
         float fm = 1.f, fo = 0.f;                      // of head `lane`: what my part and the other one are multiplied by
+        {
+          const int e = (int)(__float_as_uint(l_lane) >> 23) - 127;
+          if (e > -127 && e < 127) {
+            const float f = q8::scale(127 - e);
+            l_lane *= f;
+            fm = f * (1.f / (1 << kSumUnit));
+            m_lane += (float)(e + kSumUnit);
+          }
+        }
         if (g == 1) {
-          if (q == 0) { hand_m[lane] = m_lane; hand_l[lane] = l_lane; }
+          if (q == 0) { hand_m[lane] = m_lane; hand_l[lane] = l_lane; hand_f[lane] = fm; }
         } else if (two) {
           if (!(ok = wait_all(&handed, n_handed & 1u))) break;
-          const float mo = hand_m[lane], mn = fmaxf(m_lane, mo);
-          fm = ex2(m_lane - mn); fo = ex2(mo - mn);
-          l_lane = l_lane * fm + hand_l[lane] * fo;
+          const float mo = hand_m[lane], mn = fmaxf(m_lane, mo), um = ex2(m_lane - mn), uo = ex2(mo - mn);
+          fm *= um; fo = hand_f[lane] * uo;
+          l_lane = l_lane * um + hand_l[lane] * uo;
           m_lane = mn;
         }
         if (g == 1) {
@@ -873,9 +891,10 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
 #pragma unroll 2
           for (int c = q; c < p.t3 / 4; c += 4) {
             float4 v = a4[c ^ lane];
+            v.x *= fm; v.y *= fm; v.z *= fm; v.w *= fm;
             if (two) {
               const float4 u = b4[c ^ lane];
-              v.x = v.x * fm + u.x * fo; v.y = v.y * fm + u.y * fo; v.z = v.z * fm + u.z * fo; v.w = v.w * fm + u.w * fo;
+              v.x = fmaf(u.x, fo, v.x); v.y = fmaf(u.y, fo, v.y); v.z = fmaf(u.z, fo, v.z); v.w = fmaf(u.w, fo, v.w);
             }
             if (slot_ok) dst[c * NH] = v;
           }

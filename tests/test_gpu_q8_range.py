@@ -87,3 +87,25 @@ def test_new_value_row_of_zeros_in_a_fresh_tile(shape, cached):
         Bd.tucker_attn_decode_paged_q8(before[0], *before[1], *before[2], *before[3:5], n_H=wb.n_H, rope=False, append=False)
         y = Bd.tucker_attn_decode_paged_q8(x, *dw, K, Ks, V, Vs, table, lens, n_H=w.n_H, rope=False, append=False)
         check(state, w, y, f"{cached} cached")
+
+
+@pytest.mark.parametrize("scale", [-89, -60, 12, 30, 60, 100])
+@pytest.mark.parametrize("run", [0, 700])
+def test_value_rows_of_zeros_among_rows_of_any_size(scale, run):
+    """Every fifth value row, and the first `run` of a sequence, are zeros (whose scale is 1 whatever the others' is); some of them have
+    keys that get most of the weight.  A row of zeros adds nothing to the output and its weight to the sum.  Whole steps of nothing but
+    such rows are joined with others."""
+    state, w = big_state({**TC64, "n_H": 4}, [3000, 700, 129], 64, rope=False)
+    x, dw, (K, Ks, V, Vs), table, lens, _ = state
+    dw[7] *= 2.0 ** scale                                       # the new tokens' value rows of the others' size
+    vb, vs = V.view(torch.uint8), Vs.view(torch.uint8)
+    vs[:] = 120 + scale
+    vb[:, ::5] = 0
+    vs[:, ::5] = 127
+    Ks.view(torch.uint8)[:, 10] += 3
+    i = torch.arange(run, device="cuda")
+    for b in (0, 1):
+        at = (table[b, i // 64].long(), i % 64)
+        vb[at], vs[at] = 0, 127
+    y = Bd.tucker_attn_decode_paged_q8(x, *dw, K, Ks, V, Vs, table, lens, n_H=w.n_H, rope=False, append=False)
+    check(state, w, y, f"scale {scale}")
