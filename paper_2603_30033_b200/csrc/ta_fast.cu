@@ -305,7 +305,6 @@ bool tmap_3d(CUtensorMap* m, const void* base, uint64_t cols, uint64_t rows, uin
   return make_tmap(m, base, 3, dims, str, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-int sm_count();
 size_t l2_bytes();
 
 // Consecutive head pairs per work item.  Causal items differ in size, so many small items balance best over
@@ -547,6 +546,7 @@ int current_device_slot() {
   return dev;
 }
 
+}  // namespace
 int sm_count() {
   const int dev = current_device_slot();
   std::lock_guard<std::mutex> lock(g_props.m);
@@ -557,6 +557,7 @@ int sm_count() {
   }
   return g_props.sms[dev];
 }
+namespace {
 
 size_t l2_bytes() {
   const int dev = current_device_slot();

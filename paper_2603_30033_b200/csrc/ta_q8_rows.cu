@@ -215,7 +215,7 @@ int launch_rows(Problem& p, const RowsArgs& g, bool store, int parts) {
 template <typename T, int LPR, int STEPS, bool VEC>
 int launch(Problem& p, const RowsArgs& g, bool store, int parts) {
   if constexpr (VEC && STEPS == 1)
-    if ((long)g.T * parts * LPR > 2048L * 148) return launch_rows<T, LPR, STEPS, VEC, kRows>(p, g, store, parts);      // more than one row per thread of the GPU
+    if ((long)g.T * parts * LPR > 2048L * sm_count()) return launch_rows<T, LPR, STEPS, VEC, kRows>(p, g, store, parts);      // more lanes than the GPU holds threads
   return launch_rows<T, LPR, STEPS, VEC, 1>(p, g, store, parts);
 }
 
