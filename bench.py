@@ -43,14 +43,14 @@ L2_BYTES = 126 * 1024 * 1024
 # workload: value, the summary under profiles/ it comes from, and the SHA-256 of the kernel's source file at the
 # time of the capture.  A value is only reported while that file is unchanged (see ncu_traffic()).
 _ATTN = {"source": "ta_attn_prefill.cuh", "sha256": "83abe4f00b82ea24232967bb6792cee9c2eed58417272c517f4f348ff22e88c6"}
-_DEC = {"source": "ta_decode_umma.cuh", "sha256": "a43fa2dd3385c5a93c47d4ce1323d8a1cb1bdc69095662d0b8acbe6729a9960f"}
+_DEC = {"source": "ta_decode_umma.cuh", "sha256": "10d24edcce12fa915f17ac5511da56ff64bcf095a844a0928bce0960368261d5"}
 NCU_TRAFFIC = {
     "c4_long_prefill": {"bytes": 17971968 + 77637120, "profile": "profiles/k_attn_prefill_c4_long_prefill.md", **_ATTN},
     "c3_vit_prefill": {"bytes": 33884416 + 64199424, "profile": "profiles/k_attn_prefill_c3_vit_prefill.md", **_ATTN},
     "c2_gpt2_prefill": {"bytes": 3584256 + 0, "profile": "profiles/k_attn_prefill_c2_gpt2_prefill.md", **_ATTN},
-    "c5_decode": {"bytes": 1075370496 + 4010752, "profile": "profiles/k_dec_attn_umma_c5_decode.md", **_DEC},
-    "f1_decode_shared_kv": {"bytes": 538028544 + 3977216, "profile": "profiles/k_dec_attn_umma_f1_decode_shared_kv.md", **_DEC},
-    "f1r_decode_shared_kv_rope": {"bytes": 538411776 + 4151552,
+    "c5_decode": {"bytes": 1075375360 + 4142080, "profile": "profiles/k_dec_attn_umma_c5_decode.md", **_DEC},
+    "f1_decode_shared_kv": {"bytes": 538012928 + 4123392, "profile": "profiles/k_dec_attn_umma_f1_decode_shared_kv.md", **_DEC},
+    "f1r_decode_shared_kv_rope": {"bytes": 538150144 + 4430336,
                                   "profile": "profiles/k_dec_attn_umma_f1r_decode_shared_kv_rope.md", **_DEC},
 }
 NOMINAL_PEAKS = {"hbm_gbs": 8000.0, "bf16_tflops": 2250.0}     # the figures the targets are quoted against

@@ -98,7 +98,11 @@ struct Params {
   PagedView pv;        // PAGED
   int pos_base;        // ROT: position of slot 0
   int* seq_cta;        // PAGED: [B][2] first and last CTA that holds a part of the sequence, for the join
-  const uint8_t *scales, *new_codes, *new_scale;      // Q8: the pool's scale bytes; [B, r3] codes of the new rows; [B][2] their scale bytes
+};
+// Q8.  (Apart: three pointers more in the parameters of the other instances and one of them, over one contiguous cache, took 126 us
+// instead of 119 for 64 sequences of 32768 tokens.)
+struct ParamsQ8 : Params {
+  const uint8_t *scales, *new_codes, *new_scale;      // the pool's scale bytes; [B, r3] codes of the new rows; [B][2] their scale bytes
 };
 
 // Walks this CTA's range of the flat tile list, sequence by sequence.
@@ -164,10 +168,13 @@ template <> struct TmemCols<8> {
 template <bool PAGED>
 using RopeTable = typename std::conditional<PAGED, dec::RopeTurns, dec::RopeFreqs>::type;
 
+template <bool Q8>
+using ParamsOf = typename std::conditional<Q8, ParamsQ8, Params>::type;
+
 template <bool ROT, int R3C, bool PAGED, bool Q8 = false>
 __global__ void __launch_bounds__(ROT ? THREADS_ROT : THREADS, 1)
 k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                const __grid_constant__ CUtensorMap tmQ, const Params p, const RopeTable<PAGED> freqs) {
+                const __grid_constant__ CUtensorMap tmQ, const ParamsOf<Q8> p, const RopeTable<PAGED> freqs) {
   // cache_len was final before the preceding kernel (which forms the queries and appends the new row)
   // began: set-up and the tile split run while it finishes, and every role passes pdl_enter() before it
   // touches anything else.  (Requesting the first cache tiles ahead of that wait as well was measured:
@@ -560,9 +567,12 @@ k_dec_attn_umma(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
        return n < ww.L ? p.pv.table[(long)ww.b * p.pv.max_pages + n / p.pv.page_size] : -1;
      };
      [[maybe_unused]] auto byte_of = [&](const Walk& ww, long t, int pg) -> int {
-       const int n = ww.k0(t) + tid;
-       if (n < ww.L) return pg >= 0 && pg < p.pv.n_pages ? p.scales[(long)pg * p.pv.page_size + n % p.pv.page_size] : 127;      // no page: rows of zeros
-       return n == ww.L ? p.new_scale[2 * (long)ww.b + 1] : 127;
+       if constexpr (Q8) {
+         const int n = ww.k0(t) + tid;
+         if (n < ww.L) return pg >= 0 && pg < p.pv.n_pages ? p.scales[(long)pg * p.pv.page_size + n % p.pv.page_size] : 127;      // no page: rows of zeros
+         if (n == ww.L) return p.new_scale[2 * (long)ww.b + 1];
+       }
+       return 127;
      };
      [[maybe_unused]] Walk wn;
      [[maybe_unused]] int byte_next = 127;

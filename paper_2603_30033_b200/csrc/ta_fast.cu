@@ -721,7 +721,7 @@ bool tmap_code_pages(CUtensorMap* m, const void* pool, int r, int n_pages, int p
 
 // One 8-bit pool with latent RoPE: rows pass through a rotation warpgroup.
 template <int R3C>
-int launch_dec_attn_q8_rot(Problem& p, const CUtensorMap& tmK, const CUtensorMap& tmQ, const decu::Params& up, int grid) {
+int launch_dec_attn_q8_rot(Problem& p, const CUtensorMap& tmK, const CUtensorMap& tmQ, const decu::ParamsQ8& up, int grid) {
   static PerDeviceFlag attr;
   TA_CUDA_TRY(ensure_dynamic_smem(attr, (const void*)decu::k_dec_attn_umma<true, R3C, true, true>, (int)decu::SMEM_BYTES));
   prof_begin(p);
@@ -738,7 +738,7 @@ int launch_dec_attn_q8(Problem& p, const FastDecWs& w, int grid) {
     CUtensorMap tmK, tmQ;
     if (!tmap_code_pages(&tmK, p.Kc, d.r3, p.pv.n_pages, p.pv.page_size)) return TA_ERR_CUDA;
     if (!tmap_2d(&tmQ, w.qhat, (uint64_t)d.r3, (uint64_t)d.B * d.n_H * 2, (uint64_t)d.r3, 64, 32)) return TA_ERR_CUDA;
-    decu::Params up = {};
+    decu::ParamsQ8 up = {};
     up.B = d.B; up.nH = d.n_H; up.Lmax = p.Lmax; up.r3 = d.r3; up.t3 = d.t3; up.shared_kv = 1; up.cache_len = p.cache_len;
     up.part_o = w.part_o; up.part_ml = w.part_ml; up.err = p.dev_err; up.pv = p.pv; up.pos_base = p.prefix_len; up.seq_cta = w.seq_cta;
     up.scales = p.Vs; up.new_codes = (const uint8_t*)w.vnew; up.new_scale = w.new_scale;
