@@ -5,7 +5,7 @@
 // lands in (224, 448] 2^k, so at most one of the 18 binades below it is given away.  In return every code times its
 // scale is exact in bf16, scales multiply exactly, and a byte holds them.
 // Rows whose largest number is below 2^-96 448 lose what is smaller than 2^-106; the limit keeps 2^-k and what the
-// attention kernels form with it (probabilities times 2^k) inside fp32.
+// attention kernels form with it (probabilities times 2^k) inside fp32.  No call writes a byte below 31.
 #pragma once
 
 #include <cuda_fp8.h>
@@ -61,8 +61,6 @@ __device__ __forceinline__ void values8(uint2 c, float (&f)[8]) {
 __device__ __forceinline__ uint2 codes8(const float (&f)[8], float inv) {
   return make_uint2(codes4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv), codes4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv));
 }
-// v as its code and scale stand for it
-__device__ __forceinline__ float stored(float v, float inv, float sc) { return values2(codes2(v * inv, 0.f)).x * sc; }
 #endif
 
 }  // namespace q8
