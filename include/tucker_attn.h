@@ -279,15 +279,22 @@ TA_API int tucker_attn_decode_prefix(const tucker_attn_desc* desc, const void* x
  *
  * A row v of r numbers (a token's latent key or value) is held as r e4m3 codes and one scale, a power of two:
  *   a = max |v|;  k = the least integer, but no less than -96, with a <= 448 * 2^k (a row of zeros: k = 0)
- *   code_j = v_j 2^-k rounded to the nearest e4m3 number, ties to even;  scale byte = k + 127 (0 .. 254: 2^(byte - 127))
+ *   code_j = v_j 2^-k rounded to the nearest e4m3 number, ties to even;  scale byte = k + 127 (31 .. 247: 2^(byte - 127))
  * and stands for code_j 2^k.  A code has four significant bits: each number is off by at most 2^-4 of itself (or 2^-10 of
  * 2^k where it is smaller than 2^-6 2^k), 2.6 % in the mean square.  A row with a number that is not finite has the scale
  * byte 255 and the codes 0x7f, and reads back as NaN.  The latent cache has one key row and one value row per token, whatever
  * the number of heads, so this is a scale for every token of either; it never changes once its row is written.
  *
- * Pools, tables, lengths and limits are those of the paged calls above; a needed table entry out of range reads as rows of
- * zeros and is not written through.  V == K (with Vs == Ks) is the shared projection: one pool, which holds un-rotated rows
- * when rope is set.  `dtype` is the type of everything else.  The decode shapes that run on tensor cores do so here too.
+ * Pools, tables, lengths and limits are those of the paged calls above, but for these.  Append, store and read take r3 and t3
+ * up to 1280, more than a decode step does (TA_ERR_UNSUPPORTED_SHAPE beyond).  The append's workspace grows with T for shapes
+ * without a tensor-core form and for fp32: query it with the T of the call.  A decode step on tensor cores sums in 32 bits what
+ * it has multiplied by the rows' scales: value rows of one sequence may have scales of 2^-96 to 2^87 (and rows of zeros among
+ * them), of which any two that matter to a head may lie 2^100 apart.  Scale bytes 0 .. 30 and 248 .. 254, which no call writes,
+ * read back as 2^(byte - 127); what a decode step makes of them is not specified.
+ *
+ * A needed table entry out of range reads as rows of zeros and is not written through.  V == K (with Vs == Ks) is the shared
+ * projection: one pool, which holds un-rotated rows when rope is set.  `dtype` is the type of everything else.  The decode
+ * shapes that run on tensor cores do so here too.
  * A row is rounded once, from the fp32 result of its projection.  A decode step's new token takes part in its own attention
  * with the rows that the cache stores for it, whether it appends them or not.
  */

@@ -137,3 +137,14 @@ def test_weights_far_below_the_largest_keep_their_bits(nats):
     vb[first, 7, ignored] = 0x7E
     y = Bd.tucker_attn_decode_paged_q8(x, *dw, K, Ks, V, Vs, table, lens, n_H=w.n_H, rope=False, append=False)
     check(state, w, y, f"{nats} nats", same=True)
+
+
+def test_value_rows_of_sizes_far_apart():
+    """Scales 2^90 apart in one sequence, at random: the large rows are the output, all rows are the sum."""
+    state, w = big_state({**TC64, "n_H": 4}, [3000, 700, 129], 64, rope=False)
+    x, dw, (K, Ks, V, Vs), table, lens, _ = state
+    g = torch.Generator(device="cuda").manual_seed(9)
+    small = torch.rand(Vs.shape, generator=g, device="cuda") < 0.5
+    Vs.view(torch.uint8)[:] = torch.where(small, 70, 160).to(torch.uint8)
+    y = Bd.tucker_attn_decode_paged_q8(x, *dw, K, Ks, V, Vs, table, lens, n_H=w.n_H, rope=False, append=False)
+    check(state, w, y, "2^90")
