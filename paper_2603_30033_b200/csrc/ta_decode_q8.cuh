@@ -9,14 +9,15 @@
 //       when they are read (as three products into one accumulator the key tile was read three times: at N = 32 an
 //       instruction takes the 40 cycles of its 4 KB of A from shared memory, and the tensor core was the limit).  Its own scale
 //       is a power of two per sequence.  Two numbers (2^-8) would move scores of a standard deviation of 2 by what the
-//       rounding of y to bf16 moves the output.
+//       rounding of y to bf16 moves the output.  (It is how much the scores differ that counts: what the rounding adds to a part
+//       that all keys share is the same for all.  1000 nats of it: y 1.6e-3 off, as without.)
 //   p 2^k' [128 keys x 32 heads]                   A thread owns a key, so the row's scales are two numbers of its own: 2^k
 //       multiplies the scores, 2^k' the weight of the value row, as a term of the exponent.  The sums are of p alone.
 //   O^T [t3 x 32 heads] += V_codes^T * (p 2^k')    The weight is carried as three e5m2 numbers: the upper byte of an f16, the
 //       upper byte of 8 times what is left, and of 8 times what is left then, rounded (2^-10 together; a byte's worth of an f16
 //       is an e5m2, so this is masking and exact subtraction).  The three are 96 columns of one product and of the accumulator,
 //       and are added up once per segment.  With a head's largest weight at 2^4 .. 2^15, all are held to 2^-27 of the largest.
-//       (Without the factors, for which their columns have room, to 2^-22: 12000 equal weights behind one of e^14 times theirs
+//       (Without the factors, for which their columns have room, to 2^-21: 12000 equal weights behind one of e^14 times theirs
 //       came out 6% off; the factors cost 1 us of 109.)
 //
 // Everything goes by steps of 256 keys.  The two softmax warpgroups take a half each, with scores, weights, running maxima, sums
@@ -716,8 +717,13 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             // than the weights have bits (from 2^13 on it left them all zero, and the output with them), and nothing but a
             // second round here, on what is left of the scores, would bring it down again.
             uint32_t mx[NH / 2];
+            const uint64_t low2 = pack2(-low, -low);
 #pragma unroll
-            for (int h = 0; h < NH / 2; ++h) mx[h] = pack_bf16(a[2 * h] - low, a[2 * h + 1] - low);
+            for (int h = 0; h < NH / 2; ++h) {
+              float x, y;
+              unpack2(add2(pack2(a[2 * h], a[2 * h + 1]), low2), x, y);
+              mx[h] = pack_bf16(x, y);
+            }
 #pragma unroll
             for (int lev = 8; lev >= 1; lev >>= 1) {
               const bool upper = lane & (2 * lev);
