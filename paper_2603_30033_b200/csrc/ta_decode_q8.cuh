@@ -27,7 +27,7 @@
 // after (64 ragged sequences of random rows: 2 to 9 of a CTA's 35 steps, 2000 cycles each; with
 // kStart = 8 the step takes 119 us instead of 109), the maxima are taken and the accumulator rescaled where a reference moved.
 // At the end of a (CTA, sequence) segment warpgroup 1 hands its part to warpgroup 0 through its weights' buffer.
-// 64 ragged sequences to 32768 tokens (1.3 million keys, 347 MB: 54 us at the copy rate): 89 us.  A CTA's 35 steps take 2600
+// 64 ragged sequences to 32768 tokens (1.3 million keys, 347 MB: 54 us at the copy rate): 90 us.  A CTA's 35 steps take 2600
 // to 3000 cycles each, what the bytes and the softmax warps' chains (2100) need, and about 25 thousand cycles go to the
 // division of the work, the first pass over cold code and the last segment's end.  What was tried: references and sums in
 // registers with everything of a step formed at once (300 bytes of spills, 126 us); four softmax warpgroups of 16 heads
@@ -863,16 +863,11 @@ k_dec_attn_q8(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         if (lane == 0) mbar_arrive(&o_read[g]);        // the next segment may overwrite the accumulator
         // From here on references are of the weights alone, without the scales (exponents in which parts would differ by more than
         // fp32 holds, one of rows of zeros and one of large values): the sum becomes a number of [1, 2).
-        float fm = 1.f, fo = 0.f;                      // of head `lane`: what my part and the other one are multiplied by
-        {
-          const int e = (int)(__float_as_uint(l_lane) >> 23) - 127;
-          if (e > -127 && e < 127) {
-            const float f = q8::scale(127 - e);
-            l_lane *= f;
-            fm = f * (1.f / (1 << kSumUnit));
-            m_lane += (float)(e + kSumUnit);
-          }
-        }
+        const int e2 = min(max((int)(__float_as_uint(l_lane) >> 23) - 127, -126), 126);
+        const float f2 = q8::scale(127 - e2);
+        l_lane *= f2;
+        m_lane += (float)(e2 + kSumUnit);
+        float fm = f2 * (1.f / (1 << kSumUnit)), fo = 0.f;      // of head `lane`: what my part and the other one are multiplied by
         if (g == 1) {
           if (q == 0) { hand_m[lane] = m_lane; hand_l[lane] = l_lane; hand_f[lane] = fm; }
         } else if (two) {
